@@ -317,6 +317,39 @@ cbm_status cbm_gcn2_forward(const cbm_handle* h, const float* X, int32_t f_in, c
                             void* hip_stream);
 size_t cbm_gcn2_workspace_bytes(const cbm_handle* h, int32_t f_in, int32_t hidden, int32_t f_out);
 
+/*
+ * What stands between the products of a training step.  Matrices here are row-major device matrices of one of three types with any
+ * leading dimension (in elements, >= the row); statistics and the sums of gradients are fp32.  Pointers need the alignment of one element
+ * (a workspace 16 bytes).  What is written must not overlap anything else of the same call (CBM_ERR_INVALID_ARG; also for
+ * column slices interleaved in one buffer) unless the call says so.  The calls only enqueue kernels on the stream, allocate nothing and
+ * keep nothing from one call to the next, so they can be captured and may overlap as long as they have workspaces of
+ * their own; sums are added in a fixed order, so the same call gives the same bits.  n = 0 is a call without rows.  Rows of up to 2^30 columns.
+ */
+typedef enum { CBM_F32 = 0, CBM_BF16 = 1, CBM_F16 = 2 } cbm_dtype;
+
+/*
+ * cbm_layer_norm -- y = (x - m) r gamma + beta along each row, m = mean(x), r = (mean((x - m)^2) + eps)^-1/2.
+ *   X, Y         n x k, of `type`.
+ *   gamma, beta  k fp32 values each; NULL stands for ones, zeros.
+ *   eps          >= 0 and finite.  With eps = 0 a row of equal values has r = infinity and a y of NaN, as the formula says.
+ *   mean, rstd   receive m and r (n fp32 values each), which the backward pass reads; either may be NULL.
+ */
+cbm_status cbm_layer_norm(int64_t n, int32_t k, int32_t type, const void* X, int64_t ldx, const float* gamma, const float* beta,
+                          float eps, void* Y, int64_t ldy, float* mean, float* rstd, void* hip_stream);
+
+/*
+ * cbm_layer_norm_backward -- with h = (x - mean) rstd and u = dy gamma, along each row
+ *   dX = rstd (u - mean(u) - h mean(u h)),  and over the rows  dgamma = sum(dy h),  dbeta = sum(dy).
+ *   dY, X, dX    n x k, of `type`.  dX may be NULL (nothing before the layer learns).
+ *   gamma        as forward; mean, rstd as the forward pass gave them.
+ *   dgamma, dbeta  k fp32 values each, overwritten (zeros for n = 0); either may be NULL, not all three outputs.
+ *   workspace    cbm_layer_norm_workspace_bytes(n, k) bytes; may be NULL where dgamma and dbeta are.
+ */
+cbm_status cbm_layer_norm_backward(int64_t n, int32_t k, int32_t type, const void* dY, int64_t lddy, const void* X, int64_t ldx,
+                                   const float* gamma, const float* mean, const float* rstd, void* dX, int64_t lddx,
+                                   float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t cbm_layer_norm_workspace_bytes(int64_t n, int32_t k);
+
 /* Counters of the built format (Properties 1 and 2, Lemma 2.2). */
 cbm_status cbm_stats(const cbm_handle* h, cbm_stats_t* out);
 

@@ -22,6 +22,7 @@ EXPORTS = [
     "cbm_build", "cbm_spmm", "cbm_spmm_noalloc", "cbm_spmm_normalized", "cbm_spmm_normalized_relu", "cbm_spmm_mean", "cbm_spmm_gin",
     "cbm_dense_matmul", "cbm_reserve", "cbm_release_captures",
     "cbm_gcn2_forward", "cbm_gcn2_workspace_bytes", "cbm_stats", "cbm_get_tree", "cbm_decompress",
+    "cbm_layer_norm", "cbm_layer_norm_backward", "cbm_layer_norm_workspace_bytes",
     "cbm_profile_enable", "cbm_profile_read", "cbm_free", "cbm_status_string", "cbm_last_error_detail",
 ]
 
@@ -60,6 +61,7 @@ class cbm_launch_record(C.Structure):
 
 _LIB = None
 _F32 = None  # torch.float32, known once the library is loaded
+_DTYPES = {}  # torch's types of the operators between the products: cbm_dtype, likewise
 
 
 def _lib():
@@ -72,6 +74,7 @@ def _lib():
         import torch
 
         _F32 = torch.float32
+        _DTYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
         lib = C.CDLL(LIB_PATH)
         vp, i64, i32, f32p = C.c_void_p, C.c_int64, C.c_int32, C.c_void_p
         lib.cbm_build.argtypes = [i64, i64, vp, vp, C.POINTER(cbm_build_opts), C.POINTER(vp)]
@@ -84,6 +87,10 @@ def _lib():
         lib.cbm_gcn2_forward.argtypes = [vp, f32p, i32, f32p, i32, f32p, i32, f32p, vp, C.c_size_t, vp]
         lib.cbm_gcn2_workspace_bytes.argtypes = [vp, i32, i32, i32]
         lib.cbm_gcn2_workspace_bytes.restype = C.c_size_t
+        lib.cbm_layer_norm.argtypes = [i64, i32, i32, vp, i64, f32p, f32p, C.c_float, vp, i64, f32p, f32p, vp]
+        lib.cbm_layer_norm_backward.argtypes = [i64, i32, i32, vp, i64, vp, i64, f32p, f32p, f32p, vp, i64, f32p, f32p, vp, C.c_size_t, vp]
+        lib.cbm_layer_norm_workspace_bytes.argtypes = [i64, i32]
+        lib.cbm_layer_norm_workspace_bytes.restype = C.c_size_t
         lib.cbm_stats.argtypes = [vp, C.POINTER(cbm_stats_t)]
         lib.cbm_get_tree.argtypes = [vp, vp, vp, vp, vp]
         lib.cbm_decompress.argtypes = [vp, vp, vp]
@@ -250,6 +257,64 @@ def cbm_gcn2_forward(h: Handle, X, W0, W1, out, workspace, stream=None):
     _check(lib.cbm_gcn2_forward(h.ptr, xp, f_in, w0, hidden, w1, f_out, op, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                 _stream_ptr(stream)), "cbm_gcn2_forward")
     return out
+
+
+def _matrix(t, name, dtypes=None):
+    """(address, leading dimension, rows, columns, cbm_dtype) of a device matrix of one of the operators' types, or of `dtypes`."""
+    dtypes = _DTYPES if dtypes is None else dtypes
+    code = dtypes.get(t.dtype) if t.is_cuda else None
+    strides = t.stride() if code is not None else ()
+    if len(strides) != 2 or (strides[1] != 1 and t.shape[1] > 1):
+        raise ValueError(f"{name} must be a 2-D device tensor of {', '.join(str(d) for d in dtypes)} with unit column stride")
+    rows, cols = t.shape
+    return t.data_ptr(), max(strides[0], cols) if rows <= 1 else strides[0], rows, cols, code
+
+
+def _vector(t, name, size, dtype=None):
+    """Address of a packed device vector of `size` values (fp32 unless said otherwise); None stays None."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype is not (dtype or _F32) or t.dim() != 1 or t.shape[0] != size or (size > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be a packed device vector of {size} {dtype or _F32} values")
+    return t.data_ptr()
+
+
+def _workspace(t):
+    return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
+
+
+def _same(shape_and_type, other, what):
+    if shape_and_type != other:
+        raise ValueError(f"{what} must have the same shape and type")
+
+
+def cbm_layer_norm(X, gamma, beta, eps: float, Y, mean=None, rstd=None, stream=None):
+    lib = _LIB or _lib()
+    xp, ldx, n, k, dtype = _matrix(X, "X")
+    yp, ldy, *y = _matrix(Y, "Y")
+    _same([n, k, dtype], y, "X and Y")
+    _check(lib.cbm_layer_norm(n, k, dtype, xp, ldx, _vector(gamma, "gamma", k), _vector(beta, "beta", k), float(eps), yp, ldy, _vector(mean, "mean", n),
+                              _vector(rstd, "rstd", n), _stream_ptr(stream)), "cbm_layer_norm")
+    return Y
+
+
+def cbm_layer_norm_workspace_bytes(n: int, k: int) -> int:
+    return int((_LIB or _lib()).cbm_layer_norm_workspace_bytes(n, k))
+
+
+def cbm_layer_norm_backward(dY, X, gamma, mean, rstd, dX, dgamma, dbeta, workspace, stream=None):
+    lib = _LIB or _lib()
+    gp, ldg, n, k, dtype = _matrix(dY, "dY")
+    xp, ldx, *x = _matrix(X, "X")
+    _same([n, k, dtype], x, "dY and X")
+    dp, ldd = None, k
+    if dX is not None:
+        dp, ldd, *d = _matrix(dX, "dX")
+        _same([n, k, dtype], d, "dY and dX")
+    wp, wbytes = _workspace(workspace)
+    _check(lib.cbm_layer_norm_backward(n, k, dtype, gp, ldg, xp, ldx, _vector(gamma, "gamma", k), _vector(mean, "mean", n), _vector(rstd, "rstd", n), dp, ldd,
+                                       _vector(dgamma, "dgamma", k), _vector(dbeta, "dbeta", k), wp, wbytes, _stream_ptr(stream)), "cbm_layer_norm_backward")
+    return dX
 
 
 def cbm_stats(h: Handle) -> dict:

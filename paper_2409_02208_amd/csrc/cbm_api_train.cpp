@@ -1,0 +1,81 @@
+// extern "C" boundary of the operators between the products: layer norm, 8-bit checkpoints, log probabilities.  Argument checks and dispatch.
+#include <cmath>
+#include <cstdint>
+
+#include "cbm_internal.h"
+
+namespace {
+
+constexpr int32_t MOST_COLUMNS = 1 << 30;
+
+int64_t element_bytes(int32_t type) { return type == CBM_F32 ? 4 : type == CBM_BF16 || type == CBM_F16 ? 2 : 0; }
+
+// The memory that an operand spans, from its first element to its last.
+struct Span {
+    const void* p;
+    uintptr_t b, e;
+};
+// A matrix of n rows of k elements.  *st: what is wrong with it, if anything is.
+Span matrix(const void* p, int64_t n, int64_t k, int64_t ld, int64_t bytes, cbm_status* st) {
+    Span s{p, (uintptr_t)p, (uintptr_t)p};
+    if (ld < k || (n > 0 && k > 0 && !p) || (uintptr_t)p % (uintptr_t)bytes) {
+        *st = CBM_ERR_INVALID_ARG;
+    } else if (n > 0 && k > 0) {
+        if (ld > (INT64_MAX / 16) / n) *st = *st == CBM_OK ? CBM_ERR_UNSUPPORTED : *st;
+        else s.e = s.b + (uintptr_t)(((n - 1) * ld + k) * bytes);
+    }
+    return s;
+}
+Span maybe(const void* p, int64_t count, int64_t bytes, cbm_status* st) { return p ? matrix(p, 1, count, count, bytes, st) : Span{nullptr, 0, 0}; }
+// Whether one of the outputs overlaps an input or another output.
+template <int I, int O>
+bool overlap(const Span (&in)[I], const Span (&out)[O]) {
+    auto meet = [](const Span& a, const Span& b) { return a.b < b.e && b.b < a.e; };
+    for (int o = 0; o < O; ++o) {
+        for (const Span& s : in)
+            if (meet(s, out[o])) return true;
+        for (int q = 0; q < o; ++q)
+            if (meet(out[q], out[o])) return true;
+    }
+    return false;
+}
+
+}  // namespace
+
+extern "C" {
+
+cbm_status cbm_layer_norm(int64_t n, int32_t k, int32_t type, const void* X, int64_t ldx, const float* gamma, const float* beta, float eps, void* Y, int64_t ldy,
+                          float* mean, float* rstd, void* hip_stream) {
+    const int64_t bytes = element_bytes(type);
+    if (n < 0 || k <= 0 || !bytes || !(eps >= 0.0f) || !std::isfinite(eps)) return CBM_ERR_INVALID_ARG;
+    if (k > MOST_COLUMNS) return CBM_ERR_UNSUPPORTED;
+    cbm_status st = CBM_OK;
+    const Span in[3] = {matrix(X, n, k, ldx, bytes, &st), maybe(gamma, k, 4, &st), maybe(beta, k, 4, &st)};
+    const Span out[3] = {matrix(Y, n, k, ldy, bytes, &st), maybe(mean, n, 4, &st), maybe(rstd, n, 4, &st)};
+    if (st != CBM_OK) return st;
+    if (overlap(in, out)) return CBM_ERR_INVALID_ARG;
+    return cbm_launch_norm(n, k, type, X, ldx, gamma, beta, eps, Y, ldy, mean, rstd, hip_stream);
+}
+
+size_t cbm_layer_norm_workspace_bytes(int64_t n, int32_t k) {
+    return n < 0 || k <= 0 || k > MOST_COLUMNS ? 0 : (size_t)cbm_norm_parts(n) * 2 * (size_t)k * sizeof(float);
+}
+
+cbm_status cbm_layer_norm_backward(int64_t n, int32_t k, int32_t type, const void* dY, int64_t lddy, const void* X, int64_t ldx, const float* gamma, const float* mean,
+                                   const float* rstd, void* dX, int64_t lddx, float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    const int64_t bytes = element_bytes(type);
+    if (n < 0 || k <= 0 || !bytes || (!dX && !dgamma && !dbeta)) return CBM_ERR_INVALID_ARG;
+    if (k > MOST_COLUMNS) return CBM_ERR_UNSUPPORTED;
+    cbm_status st = CBM_OK;
+    const bool sums = dgamma || dbeta;
+    const size_t need = sums ? cbm_layer_norm_workspace_bytes(n, k) : 0;
+    if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15))) return CBM_ERR_INVALID_ARG;
+    const Span in[5] = {matrix(dY, n, k, lddy, bytes, &st), matrix(X, n, k, ldx, bytes, &st), maybe(gamma, k, 4, &st), matrix(mean, 1, n, n, 4, &st), matrix(rstd, 1, n, n, 4, &st)};
+    const Span out[4] = {dX ? matrix(dX, n, k, lddx, bytes, &st) : Span{nullptr, 0, 0}, maybe(dgamma, k, 4, &st), maybe(dbeta, k, 4, &st),
+                         Span{workspace, (uintptr_t)workspace, (uintptr_t)workspace + need}};
+    if (st != CBM_OK) return st;
+    if (overlap(in, out)) return CBM_ERR_INVALID_ARG;
+    return cbm_launch_norm_backward(n, k, type, dY, lddy, X, ldx, gamma, mean, rstd, dX, lddx, dgamma, dbeta, (float*)workspace, hip_stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,89 @@
+// Matrices of fp32, bf16 or fp16 values seen as fp32, rows cut into pieces for lanes, and sums over lanes (device code of the operators that go
+// along rows: layer norm, 8-bit checkpoints, log probabilities).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "cbm.h"
+
+// V values of a row as fp32.  The loads ask for the alignment of one element: on gfx950 a 128-bit load may start at any of them.
+template <class T, int V>
+struct Piece {
+    typedef T type __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+};
+template <int V, class T>
+__device__ __forceinline__ void load_piece(float (&x)[V], const T* p) {
+    if constexpr (V == 1) {
+        x[0] = (float)*p;
+    } else {
+        const typename Piece<T, V>::type v = *reinterpret_cast<const typename Piece<T, V>::type*>(p);
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = (float)v[j];
+    }
+}
+template <int V, class T>
+__device__ __forceinline__ void store_piece(T* p, const float (&x)[V]) {
+    if constexpr (V == 1) {
+        *p = (T)x[0];
+    } else {
+        typename Piece<T, V>::type v;
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = (T)x[j];
+        *reinterpret_cast<typename Piece<T, V>::type*>(p) = v;
+    }
+}
+
+// Piece c of a row of k >= V values: it starts at column c V, the last one at k - V where V does not divide k (WHOLE: it does).  The first `seen` of its values
+// then belong to the piece before it: they are read (and written with the same bits) twice, and counted once.  A piece beyond the row has seen >= V.
+template <int V, bool WHOLE>
+struct Place {
+    int at, seen;
+    __device__ __forceinline__ Place(int c, int k) {
+        at = min(c * V, k - V);
+        seen = c * V - at;
+    }
+    __device__ __forceinline__ bool any() const { return seen < V; }
+    __device__ __forceinline__ bool counts(int j) const { return WHOLE ? seen <= 0 : j >= seen; }
+};
+
+// Sums and maxima over groups of LANES consecutive lanes, the same bits in all of them: inside a row of 16 lanes by DPP, across rows by swaps.
+template <int CTRL>
+__device__ __forceinline__ uint32_t lane_moved(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, true);
+}
+template <int STEP>  // the value of the lane at distance STEP of a butterfly whose smaller steps are done
+__device__ __forceinline__ uint32_t lane_other(uint32_t v) {
+    static_assert(STEP >= 1 && STEP <= 32, "");
+    if constexpr (STEP == 1) return lane_moved<0xb1>(v);         // quad_perm 1 0 3 2
+    else if constexpr (STEP == 2) return lane_moved<0x4e>(v);    // quad_perm 2 3 0 1
+    else if constexpr (STEP == 4) return lane_moved<0x141>(v);   // row_half_mirror: all four lanes of a quad are alike by now
+    else if constexpr (STEP == 8) return lane_moved<0x140>(v);   // row_mirror
+    else return (uint32_t)__shfl_xor((int)v, STEP);
+}
+template <int STEP>
+__device__ __forceinline__ float lane_other(float v) {
+    return __uint_as_float(lane_other<STEP>(__float_as_uint(v)));
+}
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v) {
+    if constexpr (LANES >= 2) v += lane_other<1>(v);
+    if constexpr (LANES >= 4) v += lane_other<2>(v);
+    if constexpr (LANES >= 8) v += lane_other<4>(v);
+    if constexpr (LANES >= 16) v += lane_other<8>(v);
+    if constexpr (LANES >= 32) v += lane_other<16>(v);
+    if constexpr (LANES >= 64) v += lane_other<32>(v);
+    return v;
+}
+
+// f(one of float, __bf16, _Float16), by a cbm_dtype; false: there is no such type
+template <class F>
+inline bool cbm_with_type(int32_t type, F&& f) {
+    switch (type) {
+        case CBM_F32: f(float{}); return true;
+        case CBM_BF16: f(__bf16{}); return true;
+        case CBM_F16: f(_Float16{}); return true;
+    }
+    return false;
+}

@@ -1,0 +1,418 @@
+// Layer norm over the rows of a matrix, forward and backward.
+//   y = (x - m) r g + b,  m = mean(x),  r = (mean((x - m)^2) + eps)^-1/2 along a row of k columns;
+//   with h = (x - m) r and u = dy g:  dx = r (u - mean(u) - h mean(u h)),  dg = sum over rows of dy h,  db = sum over rows of dy.
+// All of it is bound by memory: 8 (forward) and 14 (backward) operations a value against 8 and 12 bytes in fp32.  A row is read once and stays in the registers of
+// a group of lanes (a workgroup for wide rows), so the second pass of the variance, which keeps it exact where |m| is large beside the deviations, costs no
+// traffic.  Statistics and sums are fp32; y and dx are rounded once, to their type.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "cbm_elems.h"
+#include "cbm_internal.h"
+
+namespace {
+
+constexpr int NORM_THREADS = 256;
+constexpr int BACK_THREADS = 512, BACK_GROUPS = 512;  // backward: workgroups at most, each with partial sums of dg and db of its own
+
+// Sums of `values` values over a workgroup of THREADS, in every thread.  `room` holds 2 values of every wave.
+template <int THREADS>
+__device__ __forceinline__ void block_sum2(float& a, float& b, float* room) {
+    constexpr int WAVES = THREADS / 64;
+    a = lanes_sum<64>(a);
+    b = lanes_sum<64>(b);
+    __syncthreads();  // (what the last call left in `room` has been read)
+    if ((threadIdx.x & 63) == 0) {
+        room[2 * (threadIdx.x / 64)] = a;
+        room[2 * (threadIdx.x / 64) + 1] = b;
+    }
+    __syncthreads();
+    a = b = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        a += room[2 * w];
+        b += room[2 * w + 1];
+    }
+}
+// over the LANES lanes of a row: part of a wave, or the whole workgroup
+template <int LANES>
+__device__ __forceinline__ void row_sum2(float& a, float& b, float* room) {
+    if constexpr (LANES <= 64) {
+        a = lanes_sum<LANES>(a);
+        b = lanes_sum<LANES>(b);
+    } else {
+        block_sum2<LANES>(a, b, room);
+    }
+}
+
+// LANES lanes have a row, each R pieces of V columns.
+template <class T, int V, int LANES, int R, bool WHOLE>
+__global__ __launch_bounds__(LANES > NORM_THREADS ? LANES : NORM_THREADS) void cbm_norm_kernel(int64_t n, int k, const T* __restrict__ X, int64_t ldx, const float* __restrict__ gamma,
+                                                                                              const float* __restrict__ beta, float eps, T* __restrict__ Y, int64_t ldy,
+                                                                                              float* __restrict__ mean, float* __restrict__ rstd) {
+    constexpr int THREADS = LANES > NORM_THREADS ? LANES : NORM_THREADS, ROWS = THREADS / LANES;
+    __shared__ float room[LANES > 64 ? 2 * (LANES / 64) : 1];
+    const int lane = threadIdx.x % LANES;
+    float g[R][V], b[R][V];
+#pragma unroll
+    for (int c = 0; c < R; ++c) {
+        const Place<V, WHOLE> p(c * LANES + lane, k);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            g[c][j] = gamma ? gamma[p.at + j] : 1.0f;
+            b[c][j] = beta ? beta[p.at + j] : 0.0f;
+        }
+    }
+    for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < n; row0 += (int64_t)gridDim.x * ROWS) {
+        const int64_t row = row0 + threadIdx.x / LANES;
+        const T* x_row = X + (row < n ? row : n - 1) * ldx;
+        float x[R][V], sum = 0.0f, none = 0.0f;
+#pragma unroll
+        for (int c = 0; c < R; ++c) {
+            const Place<V, WHOLE> p(c * LANES + lane, k);
+            load_piece<V>(x[c], x_row + p.at);
+        }
+#pragma unroll
+        for (int c = 0; c < R; ++c) {
+            const Place<V, WHOLE> p(c * LANES + lane, k);
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum += p.counts(j) ? x[c][j] : 0.0f;
+        }
+        row_sum2<LANES>(sum, none, room);
+        const float m = sum / (float)k;
+        float squares = 0.0f;
+#pragma unroll
+        for (int c = 0; c < R; ++c) {
+            const Place<V, WHOLE> p(c * LANES + lane, k);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                x[c][j] -= m;
+                squares += p.counts(j) ? x[c][j] * x[c][j] : 0.0f;
+            }
+        }
+        row_sum2<LANES>(squares, none, room);
+        const float r = 1.0f / sqrtf(squares / (float)k + eps);
+        if (row >= n) continue;  // (only where a row is part of a wave: with a workgroup a row, row0 is the row)
+        T* y_row = Y + row * ldy;
+#pragma unroll
+        for (int c = 0; c < R; ++c) {
+            const Place<V, WHOLE> p(c * LANES + lane, k);
+            float y[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) y[j] = x[c][j] * r * g[c][j] + b[c][j];
+            if (p.any()) store_piece<V>(y_row + p.at, y);
+        }
+        if (lane == 0) {
+            if (mean) mean[row] = m;
+            if (rstd) rstd[row] = r;
+        }
+    }
+}
+
+// Rows too wide for registers: a workgroup reads its row three times (all but the first time out of L2).
+template <class T, int V, bool WHOLE>
+__global__ __launch_bounds__(1024) void cbm_norm_wide_kernel(int64_t n, int k, const T* __restrict__ X, int64_t ldx, const float* __restrict__ gamma, const float* __restrict__ beta,
+                                                             float eps, T* __restrict__ Y, int64_t ldy, float* __restrict__ mean, float* __restrict__ rstd) {
+    __shared__ float room[32];
+    const int pieces = (k + V - 1) / V;
+    for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
+        const T* x_row = X + row * ldx;
+        float sum = 0.0f, none = 0.0f, x[V];
+        for (int c = threadIdx.x; c < pieces; c += 1024) {
+            const Place<V, WHOLE> p(c, k);
+            load_piece<V>(x, x_row + p.at);
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum += p.counts(j) ? x[j] : 0.0f;
+        }
+        block_sum2<1024>(sum, none, room);
+        const float m = sum / (float)k;
+        float squares = 0.0f;
+        for (int c = threadIdx.x; c < pieces; c += 1024) {
+            const Place<V, WHOLE> p(c, k);
+            load_piece<V>(x, x_row + p.at);
+#pragma unroll
+            for (int j = 0; j < V; ++j) squares += p.counts(j) ? (x[j] - m) * (x[j] - m) : 0.0f;
+        }
+        block_sum2<1024>(squares, none, room);
+        const float r = 1.0f / sqrtf(squares / (float)k + eps);
+        for (int c = threadIdx.x; c < pieces; c += 1024) {
+            const Place<V, WHOLE> p(c, k);
+            load_piece<V>(x, x_row + p.at);
+#pragma unroll
+            for (int j = 0; j < V; ++j) x[j] = (x[j] - m) * r * (gamma ? gamma[p.at + j] : 1.0f) + (beta ? beta[p.at + j] : 0.0f);
+            store_piece<V>(Y + row * ldy + p.at, x);
+        }
+        if (threadIdx.x == 0) {
+            if (mean) mean[row] = m;
+            if (rstd) rstd[row] = r;
+        }
+    }
+}
+
+// Backward in the same shape.  A lane has the same columns in all rows that it meets, so dg and db of these columns add up in its registers; a workgroup adds its
+// lanes' sums in LDS, in a fixed order, and writes one partial row of each to `parts` (workgroup, dg then db, column).
+template <class T, int V, int LANES, int R, int THREADS, bool WHOLE>
+__global__ __launch_bounds__(THREADS) void cbm_norm_back_kernel(int64_t n, int k, const T* __restrict__ dY, int64_t lddy, const T* __restrict__ X, int64_t ldx,
+                                                                const float* __restrict__ gamma, const float* __restrict__ mean, const float* __restrict__ rstd,
+                                                                T* __restrict__ dX, int64_t lddx, float* __restrict__ parts) {
+    constexpr int ROWS = THREADS / LANES;
+    constexpr int COLUMNS = LANES * R * V;
+    __shared__ float room[LANES > 64 ? 2 * (LANES / 64) : (THREADS / 64) * 2 * COLUMNS];
+    const int lane = threadIdx.x % LANES;
+    float g[R][V], dg[R][V], db[R][V];
+#pragma unroll
+    for (int c = 0; c < R; ++c) {
+        const Place<V, WHOLE> p(c * LANES + lane, k);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            g[c][j] = gamma ? gamma[p.at + j] : 1.0f;
+            dg[c][j] = db[c][j] = 0.0f;
+        }
+    }
+    for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < n; row0 += (int64_t)gridDim.x * ROWS) {
+        const int64_t row = row0 + threadIdx.x / LANES, at = row < n ? row : n - 1;
+        const T *x_row = X + at * ldx, *dy_row = dY + at * lddy;
+        float h[R][V], u[R][V], sum = 0.0f, along = 0.0f;
+#pragma unroll
+        for (int c = 0; c < R; ++c) {
+            const Place<V, WHOLE> p(c * LANES + lane, k);
+            load_piece<V>(h[c], x_row + p.at);
+            load_piece<V>(u[c], dy_row + p.at);
+        }
+        const float m = mean[at], r = rstd[at];
+#pragma unroll
+        for (int c = 0; c < R; ++c) {
+            const Place<V, WHOLE> p(c * LANES + lane, k);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                h[c][j] = (h[c][j] - m) * r;
+                const bool counts = p.counts(j) && row < n;
+                const float dy = u[c][j];
+                dg[c][j] += counts ? dy * h[c][j] : 0.0f;
+                db[c][j] += counts ? dy : 0.0f;
+                u[c][j] = dy * g[c][j];
+                sum += counts ? u[c][j] : 0.0f;
+                along += counts ? u[c][j] * h[c][j] : 0.0f;
+            }
+        }
+        if (!dX) continue;
+        row_sum2<LANES>(sum, along, room);
+        sum /= (float)k;
+        along /= (float)k;
+        if (row >= n) continue;
+#pragma unroll
+        for (int c = 0; c < R; ++c) {
+            const Place<V, WHOLE> p(c * LANES + lane, k);
+            float dx[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) dx[j] = r * (u[c][j] - sum - h[c][j] * along);
+            if (p.any()) store_piece<V>(dX + row * lddx + p.at, dx);
+        }
+    }
+    if (!parts) return;
+    float* out = parts + (int64_t)blockIdx.x * 2 * k;
+    if constexpr (LANES > 64) {
+#pragma unroll
+        for (int c = 0; c < R; ++c) {
+            const Place<V, WHOLE> p(c * LANES + lane, k);
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (p.counts(j)) {
+                    out[p.at + j] = dg[c][j];
+                    out[k + p.at + j] = db[c][j];
+                }
+        }
+    } else {
+        const int wave = threadIdx.x / 64;
+        __syncthreads();
+#pragma unroll
+        for (int c = 0; c < R; ++c)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                float a = dg[c][j], b = db[c][j];
+#pragma unroll
+                for (int step = LANES; step < 64; step *= 2) {  // the rows of a wave
+                    a += __shfl_xor(a, step);
+                    b += __shfl_xor(b, step);
+                }
+                if ((threadIdx.x & 63) < LANES) {
+                    const int slot = (c * LANES + lane) * V + j;
+                    room[(2 * wave) * COLUMNS + slot] = a;
+                    room[(2 * wave + 1) * COLUMNS + slot] = b;
+                }
+            }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * COLUMNS; i += THREADS) {
+            const int slot = i % COLUMNS, which = i / COLUMNS;
+            const Place<V, WHOLE> p(slot / V, k);
+            if (!p.counts(slot % V)) continue;
+            float s = 0.0f;
+#pragma unroll
+            for (int w = 0; w < THREADS / 64; ++w) s += room[(2 * w + which) * COLUMNS + slot];
+            out[which * k + p.at + slot % V] = s;
+        }
+    }
+}
+
+// Rows too wide for registers: dx by a workgroup a row, which reads x and dy twice; dg and db by workgroups of 256 columns and a share of the rows.
+template <class T, int V, bool WHOLE>
+__global__ __launch_bounds__(1024) void cbm_norm_back_wide_kernel(int64_t n, int k, const T* __restrict__ dY, int64_t lddy, const T* __restrict__ X, int64_t ldx,
+                                                                  const float* __restrict__ gamma, const float* __restrict__ mean, const float* __restrict__ rstd,
+                                                                  T* __restrict__ dX, int64_t lddx) {
+    __shared__ float room[32];
+    const int pieces = (k + V - 1) / V;
+    for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
+        const float m = mean[row], r = rstd[row];
+        float sum = 0.0f, along = 0.0f, x[V], dy[V];
+        for (int c = threadIdx.x; c < pieces; c += 1024) {
+            const Place<V, WHOLE> p(c, k);
+            load_piece<V>(x, X + row * ldx + p.at);
+            load_piece<V>(dy, dY + row * lddy + p.at);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float u = dy[j] * (gamma ? gamma[p.at + j] : 1.0f);
+                sum += p.counts(j) ? u : 0.0f;
+                along += p.counts(j) ? u * ((x[j] - m) * r) : 0.0f;
+            }
+        }
+        block_sum2<1024>(sum, along, room);
+        sum /= (float)k;
+        along /= (float)k;
+        for (int c = threadIdx.x; c < pieces; c += 1024) {
+            const Place<V, WHOLE> p(c, k);
+            load_piece<V>(x, X + row * ldx + p.at);
+            load_piece<V>(dy, dY + row * lddy + p.at);
+#pragma unroll
+            for (int j = 0; j < V; ++j) x[j] = r * (dy[j] * (gamma ? gamma[p.at + j] : 1.0f) - sum - (x[j] - m) * r * along);
+            store_piece<V>(dX + row * lddx + p.at, x);
+        }
+    }
+}
+template <class T>
+__global__ __launch_bounds__(256) void cbm_norm_back_columns_kernel(int64_t n, int k, const T* __restrict__ dY, int64_t lddy, const T* __restrict__ X, int64_t ldx,
+                                                                    const float* __restrict__ mean, const float* __restrict__ rstd, float* __restrict__ parts) {
+    const int column = blockIdx.x * 256 + threadIdx.x;
+    if (column >= k) return;
+    float dg = 0.0f, db = 0.0f;
+    for (int64_t row = blockIdx.y; row < n; row += gridDim.y) {
+        const float dy = (float)dY[row * lddy + column];
+        dg += dy * (((float)X[row * ldx + column] - mean[row]) * rstd[row]);
+        db += dy;
+    }
+    float* out = parts + (int64_t)blockIdx.y * 2 * k;
+    out[column] = dg;
+    out[k + column] = db;
+}
+
+// dg and db from `count` partial rows of each, in a fixed order: 32 columns a workgroup, the partial rows shared by its 32 groups of lanes.
+__global__ __launch_bounds__(1024) void cbm_norm_join_kernel(int count, int k, const float* __restrict__ parts, float* __restrict__ dgamma, float* __restrict__ dbeta) {
+    __shared__ float room[32][33];
+    const int which = blockIdx.y, column = blockIdx.x * 32 + (threadIdx.x & 31), slice = threadIdx.x / 32;
+    float* out = which ? dbeta : dgamma;
+    if (!out) return;  // (the whole workgroup)
+    float s = 0.0f;
+    if (column < k)
+#pragma unroll 16
+        for (int i = slice; i < count; i += 32) s += parts[((int64_t)i * 2 + which) * k + column];
+    room[slice][threadIdx.x & 31] = s;
+    __syncthreads();
+    if (slice == 0 && column < k) {
+        s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) s += room[i][threadIdx.x];
+        out[column] = s;
+    }
+}
+
+cbm_status launched(const char* what) {
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess) return CBM_OK;
+    cbm_set_error_detail(what, hipGetErrorString(e));
+    return CBM_ERR_HIP;
+}
+
+int64_t at_most(int64_t rows, int rows_each, int64_t most) { return std::min<int64_t>((rows + rows_each - 1) / rows_each, most); }
+
+// f(a value of the type, whether its 16-byte pieces divide a row of k)
+template <class F>
+void with_shape(int32_t type, int32_t k, F&& f) {
+    cbm_with_type(type, [&](auto t) {
+        if (k % (16 / (int)sizeof(t)) == 0) f(t, std::true_type{});
+        else f(t, std::false_type{});
+    });
+}
+
+}  // namespace
+
+// Partial rows of the backward pass, whatever its shape.
+int64_t cbm_norm_parts(int64_t n) { return std::min<int64_t>(n, BACK_GROUPS); }
+
+cbm_status cbm_launch_norm(int64_t n, int32_t k, int32_t type, const void* X_, int64_t ldx, const float* gamma, const float* beta, float eps, void* Y_, int64_t ldy,
+                           float* mean, float* rstd, void* stream_) {
+    if (n == 0) return CBM_OK;
+    hipStream_t stream = (hipStream_t)stream_;
+    with_shape(type, k, [&](auto t, auto whole) {
+        using T = decltype(t);
+        constexpr bool WHOLE = decltype(whole)::value;
+        const T* X = (const T*)X_;
+        T* Y = (T*)Y_;
+        constexpr int V = 16 / (int)sizeof(T);
+        const int64_t pieces = ((int64_t)k + V - 1) / V;
+#define CBM_NORM(V_, LANES, R)                                                                                                                                              \
+    hipLaunchKernelGGL((cbm_norm_kernel<T, V_, LANES, R, WHOLE>), dim3((unsigned)at_most(n, (LANES > NORM_THREADS ? LANES : NORM_THREADS) / LANES, 256 * (LANES > NORM_THREADS ? 2 : 8))), \
+                       dim3(LANES > NORM_THREADS ? LANES : NORM_THREADS), 0, stream, n, k, X, ldx, gamma, beta, eps, Y, ldy, mean, rstd)
+        if (k < V) CBM_NORM(1, 8, 1);  // (V = 1: every place is whole)
+        else if (pieces <= 4) CBM_NORM(V, 4, 1);
+        else if (pieces <= 8) CBM_NORM(V, 8, 1);
+        else if (pieces <= 16) CBM_NORM(V, 16, 1);
+        else if (pieces <= 32) CBM_NORM(V, 32, 1);
+        else if (pieces <= 64) CBM_NORM(V, 64, 1);
+        else if (pieces <= 128) CBM_NORM(V, 64, 2);
+        else if (pieces <= 256) CBM_NORM(V, 256, 1);
+        else if (pieces <= 512) CBM_NORM(V, 256, 2);
+        else if (pieces <= 1024) CBM_NORM(V, 512, 2);
+        else if (pieces <= 2048) CBM_NORM(V, 1024, 2);
+        else hipLaunchKernelGGL((cbm_norm_wide_kernel<T, V, WHOLE>), dim3((unsigned)std::min<int64_t>(n, 512)), dim3(1024), 0, stream, n, k, X, ldx, gamma, beta, eps, Y, ldy, mean, rstd);
+#undef CBM_NORM
+    });
+    return launched("layer norm launch");
+}
+
+cbm_status cbm_launch_norm_backward(int64_t n, int32_t k, int32_t type, const void* dY_, int64_t lddy, const void* X_, int64_t ldx, const float* gamma, const float* mean,
+                                    const float* rstd, void* dX_, int64_t lddx, float* dgamma, float* dbeta, float* parts, void* stream_) {
+    hipStream_t stream = (hipStream_t)stream_;
+    const int64_t most = cbm_norm_parts(n);
+    int64_t count = 0;  // partial rows written
+    if (!dgamma && !dbeta) parts = nullptr;
+    if (n > 0)
+        with_shape(type, k, [&](auto t, auto whole) {
+            using T = decltype(t);
+            constexpr bool WHOLE = decltype(whole)::value;
+            const T *dY = (const T*)dY_, *X = (const T*)X_;
+            T* dX = (T*)dX_;
+            constexpr int V = 16 / (int)sizeof(T);
+            const int64_t pieces = ((int64_t)k + V - 1) / V;
+#define CBM_BACK(V_, LANES, R, THREADS)                                                                                                                                    \
+    cbm_norm_back_kernel<T, V_, LANES, R, THREADS, WHOLE><<<(unsigned)(count = at_most(n, THREADS / LANES, most)), THREADS, 0, stream>>>(n, k, dY, lddy, X, ldx, gamma, mean, rstd, dX, lddx, \
+                                                                                                                                 parts)
+            if (k < V) CBM_BACK(1, 8, 1, BACK_THREADS);
+            else if (pieces <= 4) CBM_BACK(V, 4, 1, BACK_THREADS);
+            else if (pieces <= 8) CBM_BACK(V, 8, 1, BACK_THREADS);
+            else if (pieces <= 16) CBM_BACK(V, 16, 1, BACK_THREADS);
+            else if (pieces <= 32) CBM_BACK(V, 32, 1, BACK_THREADS);
+            else if (pieces <= 64) CBM_BACK(V, 64, 1, BACK_THREADS);
+            else if (pieces <= 256) CBM_BACK(V, 256, 1, 256);
+            else if (pieces <= 512) CBM_BACK(V, 256, 2, 256);
+            else if (pieces <= 1024) CBM_BACK(V, 512, 2, 512);
+            else {
+                if (dX) hipLaunchKernelGGL((cbm_norm_back_wide_kernel<T, V, WHOLE>), dim3((unsigned)std::min<int64_t>(n, 512)), dim3(1024), 0, stream, n, k, dY, lddy, X, ldx, gamma, mean, rstd, dX, lddx);
+                count = std::min<int64_t>(most, 64);
+                if (parts) hipLaunchKernelGGL((cbm_norm_back_columns_kernel<T>), dim3((unsigned)((k + 255) / 256), (unsigned)count), dim3(256), 0, stream, n, k, dY, lddy, X, ldx, mean, rstd, parts);
+            }
+#undef CBM_BACK
+        });
+    if (dgamma || dbeta) hipLaunchKernelGGL(cbm_norm_join_kernel, dim3((unsigned)(((int64_t)k + 31) / 32), 2), dim3(1024), 0, stream, (int)count, k, parts, dgamma, dbeta);
+    return launched("layer norm backward launch");
+}
