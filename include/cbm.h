@@ -323,7 +323,7 @@ size_t cbm_gcn2_workspace_bytes(const cbm_handle* h, int32_t f_in, int32_t hidde
  * (a workspace 16 bytes).  What is written must not overlap anything else of the same call (CBM_ERR_INVALID_ARG; also for
  * column slices interleaved in one buffer) unless the call says so.  The calls only enqueue kernels on the stream, allocate nothing and
  * keep nothing from one call to the next, so they can be captured and may overlap as long as they have workspaces of
- * their own; sums are added in a fixed order, so the same call gives the same bits.  n = 0 is a call without rows.  Rows of up to 2^30 columns.
+ * their own; sums are added in a fixed order, so the same call gives the same bits.  n = 0 is a call without rows.  Rows of up to 2^24 columns.
  */
 typedef enum { CBM_F32 = 0, CBM_BF16 = 1, CBM_F16 = 2 } cbm_dtype;
 
@@ -349,6 +349,33 @@ cbm_status cbm_layer_norm_backward(int64_t n, int32_t k, int32_t type, const voi
                                    const float* gamma, const float* mean, const float* rstd, void* dX, int64_t lddx,
                                    float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes, void* hip_stream);
 size_t cbm_layer_norm_workspace_bytes(int64_t n, int32_t k);
+
+/*
+ * Activations kept in 8 bits until the backward pass.  Each 32 columns of a row (the last block of a row may be shorter) share a step 2^e:
+ *   e = max(floor(log2(largest |x| of them)) - 6, -126);  q = sign(x) min(127, max(1, round-to-even(|x| 2^-e))), 0 for x = 0;  x~ = q 2^e.
+ * So |x~ - x| <= 2^e (half of that but for the smallest values and the topmost 1 / 256 of a binade), x~ is never larger than its type's largest value, a
+ * value other than zero keeps its sign, and x~ is a bf16 value.  A block with a value that is not finite comes back as NaN throughout.
+ *   Q   n x k int8, leading dimension ldq >= k: the q.
+ *   E   n x ceil(k / 32) uint8, leading dimension lde: e + 127; 255 for a block that is not finite (its q are 0).
+ * k not a multiple of 4, or of 32, is not an error; the weights' gradient then loads Q a byte at a time.
+ *   cbm_checkpoint_save           X (n x k, of `type`) -> Q, E.
+ *   cbm_checkpoint_restore        Q, E -> X (rounded to `type`; exact in fp32 and bf16).
+ *   cbm_checkpoint_relu_backward  dX = dY where q > 0, else 0 (n x k, of `type`; NaN in a block that is not finite): the backward pass of a
+ *                                 ReLU whose output, or input, was kept.  dX may be dY itself with lddx = lddy.
+ *   cbm_checkpoint_weight_grad    dW = X~^T dY (k x c, fp32, leading dimension lddw, overwritten; zeros for n = 0): the weights' gradient of Y = X W.
+ *                                 dY n x c of `type`.  On the bf16 matrix cores with dY in parts that add up to it: exact products (parts
+ *                                 below 2^-126 are taken for zero), fp32 sums.  workspace: cbm_checkpoint_workspace_bytes(n, k, c) bytes (may be 0).
+ */
+cbm_status cbm_checkpoint_save(int64_t n, int32_t k, int32_t type, const void* X, int64_t ldx, int8_t* Q, int64_t ldq, uint8_t* E,
+                               int64_t lde, void* hip_stream);
+cbm_status cbm_checkpoint_restore(int64_t n, int32_t k, const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int32_t type,
+                                  void* X, int64_t ldx, void* hip_stream);
+cbm_status cbm_checkpoint_relu_backward(int64_t n, int32_t k, const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int32_t type,
+                                        const void* dY, int64_t lddy, void* dX, int64_t lddx, void* hip_stream);
+cbm_status cbm_checkpoint_weight_grad(int64_t n, int32_t k, int32_t c, const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde,
+                                      int32_t type, const void* dY, int64_t lddy, float* dW, int64_t lddw, void* workspace,
+                                      size_t workspace_bytes, void* hip_stream);
+size_t cbm_checkpoint_workspace_bytes(int64_t n, int32_t k, int32_t c);
 
 /* Counters of the built format (Properties 1 and 2, Lemma 2.2). */
 cbm_status cbm_stats(const cbm_handle* h, cbm_stats_t* out);

@@ -23,6 +23,8 @@ EXPORTS = [
     "cbm_dense_matmul", "cbm_reserve", "cbm_release_captures",
     "cbm_gcn2_forward", "cbm_gcn2_workspace_bytes", "cbm_stats", "cbm_get_tree", "cbm_decompress",
     "cbm_layer_norm", "cbm_layer_norm_backward", "cbm_layer_norm_workspace_bytes",
+    "cbm_checkpoint_save", "cbm_checkpoint_restore", "cbm_checkpoint_relu_backward",
+    "cbm_checkpoint_weight_grad", "cbm_checkpoint_workspace_bytes",
     "cbm_profile_enable", "cbm_profile_read", "cbm_free", "cbm_status_string", "cbm_last_error_detail",
 ]
 
@@ -62,6 +64,7 @@ class cbm_launch_record(C.Structure):
 _LIB = None
 _F32 = None  # torch.float32, known once the library is loaded
 _DTYPES = {}  # torch's types of the operators between the products: cbm_dtype, likewise
+_INT8, _UINT8 = {}, {}
 
 
 def _lib():
@@ -75,6 +78,7 @@ def _lib():
 
         _F32 = torch.float32
         _DTYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+        _INT8[torch.int8] = _UINT8[torch.uint8] = 0
         lib = C.CDLL(LIB_PATH)
         vp, i64, i32, f32p = C.c_void_p, C.c_int64, C.c_int32, C.c_void_p
         lib.cbm_build.argtypes = [i64, i64, vp, vp, C.POINTER(cbm_build_opts), C.POINTER(vp)]
@@ -91,6 +95,12 @@ def _lib():
         lib.cbm_layer_norm_backward.argtypes = [i64, i32, i32, vp, i64, vp, i64, f32p, f32p, f32p, vp, i64, f32p, f32p, vp, C.c_size_t, vp]
         lib.cbm_layer_norm_workspace_bytes.argtypes = [i64, i32]
         lib.cbm_layer_norm_workspace_bytes.restype = C.c_size_t
+        lib.cbm_checkpoint_save.argtypes = [i64, i32, i32, vp, i64, vp, i64, vp, i64, vp]
+        lib.cbm_checkpoint_restore.argtypes = [i64, i32, vp, i64, vp, i64, i32, vp, i64, vp]
+        lib.cbm_checkpoint_relu_backward.argtypes = [i64, i32, vp, i64, vp, i64, i32, vp, i64, vp, i64, vp]
+        lib.cbm_checkpoint_weight_grad.argtypes = [i64, i32, i32, vp, i64, vp, i64, i32, vp, i64, f32p, i64, vp, C.c_size_t, vp]
+        lib.cbm_checkpoint_workspace_bytes.argtypes = [i64, i32, i32]
+        lib.cbm_checkpoint_workspace_bytes.restype = C.c_size_t
         lib.cbm_stats.argtypes = [vp, C.POINTER(cbm_stats_t)]
         lib.cbm_get_tree.argtypes = [vp, vp, vp, vp, vp]
         lib.cbm_decompress.argtypes = [vp, vp, vp]
@@ -315,6 +325,63 @@ def cbm_layer_norm_backward(dY, X, gamma, mean, rstd, dX, dgamma, dbeta, workspa
     _check(lib.cbm_layer_norm_backward(n, k, dtype, gp, ldg, xp, ldx, _vector(gamma, "gamma", k), _vector(mean, "mean", n), _vector(rstd, "rstd", n), dp, ldd,
                                        _vector(dgamma, "dgamma", k), _vector(dbeta, "dbeta", k), wp, wbytes, _stream_ptr(stream)), "cbm_layer_norm_backward")
     return dX
+
+
+def _kept(Q, E):
+    """(n, k, arguments) of an 8-bit checkpoint."""
+    qp, ldq, n, k, _ = _matrix(Q, "Q", _INT8)
+    ep, lde, rows, blocks, _ = _matrix(E, "E", _UINT8)
+    if rows != n or blocks != (k + 31) // 32:
+        raise ValueError("E must have a row for each of Q's and a column for each 32 of Q's")
+    return n, k, (qp, ldq, ep, lde)
+
+
+def cbm_checkpoint_save(X, Q, E, stream=None):
+    lib = _LIB or _lib()
+    xp, ldx, n, k, dtype = _matrix(X, "X")
+    rows, cols, kept = _kept(Q, E)
+    if (rows, cols) != (n, k):
+        raise ValueError("X and Q must have the same shape")
+    _check(lib.cbm_checkpoint_save(n, k, dtype, xp, ldx, *kept, _stream_ptr(stream)), "cbm_checkpoint_save")
+    return Q
+
+
+def cbm_checkpoint_restore(Q, E, X, stream=None):
+    lib = _LIB or _lib()
+    xp, ldx, n, k, dtype = _matrix(X, "X")
+    rows, cols, kept = _kept(Q, E)
+    if (rows, cols) != (n, k):
+        raise ValueError("X and Q must have the same shape")
+    _check(lib.cbm_checkpoint_restore(n, k, *kept, dtype, xp, ldx, _stream_ptr(stream)), "cbm_checkpoint_restore")
+    return X
+
+
+def cbm_checkpoint_relu_backward(Q, E, dY, dX, stream=None):
+    lib = _LIB or _lib()
+    gp, ldg, n, k, dtype = _matrix(dY, "dY")
+    dp, ldd, *d = _matrix(dX, "dX")
+    _same([n, k, dtype], d, "dY and dX")
+    rows, cols, kept = _kept(Q, E)
+    if (rows, cols) != (n, k):
+        raise ValueError("dY and Q must have the same shape")
+    _check(lib.cbm_checkpoint_relu_backward(n, k, *kept, dtype, gp, ldg, dp, ldd, _stream_ptr(stream)), "cbm_checkpoint_relu_backward")
+    return dX
+
+
+def cbm_checkpoint_workspace_bytes(n: int, k: int, c: int) -> int:
+    return int((_LIB or _lib()).cbm_checkpoint_workspace_bytes(n, k, c))
+
+
+def cbm_checkpoint_weight_grad(Q, E, dY, dW, workspace, stream=None):
+    lib = _LIB or _lib()
+    gp, ldg, rows, c, dtype = _matrix(dY, "dY")
+    n, k, kept = _kept(Q, E)
+    wp, ldw, kw, cw = _dev_f32(dW, "dW")
+    if rows != n or kw != k or cw != c:
+        raise ValueError("shape mismatch")
+    sp, sbytes = _workspace(workspace)
+    _check(lib.cbm_checkpoint_weight_grad(n, k, c, *kept, dtype, gp, ldg, wp, ldw, sp, sbytes, _stream_ptr(stream)), "cbm_checkpoint_weight_grad")
+    return dW
 
 
 def cbm_stats(h: Handle) -> dict:

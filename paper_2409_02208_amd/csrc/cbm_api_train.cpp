@@ -6,9 +6,11 @@
 
 namespace {
 
-constexpr int32_t MOST_COLUMNS = 1 << 30;
+constexpr int32_t MOST_COLUMNS = 1 << 24;
 
 int64_t element_bytes(int32_t type) { return type == CBM_F32 ? 4 : type == CBM_BF16 || type == CBM_F16 ? 2 : 0; }
+
+int64_t steps(int32_t k) { return ((int64_t)k + 31) / 32; }  // blocks of columns in a row of the 8-bit form
 
 // The memory that an operand spans, from its first element to its last.
 struct Span {
@@ -76,6 +78,66 @@ cbm_status cbm_layer_norm_backward(int64_t n, int32_t k, int32_t type, const voi
     if (st != CBM_OK) return st;
     if (overlap(in, out)) return CBM_ERR_INVALID_ARG;
     return cbm_launch_norm_backward(n, k, type, dY, lddy, X, ldx, gamma, mean, rstd, dX, lddx, dgamma, dbeta, (float*)workspace, hip_stream);
+}
+
+cbm_status cbm_checkpoint_save(int64_t n, int32_t k, int32_t type, const void* X, int64_t ldx, int8_t* Q, int64_t ldq, uint8_t* E, int64_t lde, void* hip_stream) {
+    const int64_t bytes = element_bytes(type);
+    if (n < 0 || k <= 0 || !bytes) return CBM_ERR_INVALID_ARG;
+    if (k > MOST_COLUMNS) return CBM_ERR_UNSUPPORTED;
+    cbm_status st = CBM_OK;
+    const Span in[1] = {matrix(X, n, k, ldx, bytes, &st)};
+    const Span out[2] = {matrix(Q, n, k, ldq, 1, &st), matrix(E, n, steps(k), lde, 1, &st)};
+    if (st != CBM_OK) return st;
+    if (overlap(in, out)) return CBM_ERR_INVALID_ARG;
+    return cbm_launch_checkpoint_save(n, k, type, X, ldx, Q, ldq, E, lde, hip_stream);
+}
+
+cbm_status cbm_checkpoint_restore(int64_t n, int32_t k, const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int32_t type, void* X, int64_t ldx, void* hip_stream) {
+    const int64_t bytes = element_bytes(type);
+    if (n < 0 || k <= 0 || !bytes) return CBM_ERR_INVALID_ARG;
+    if (k > MOST_COLUMNS) return CBM_ERR_UNSUPPORTED;
+    cbm_status st = CBM_OK;
+    const Span in[2] = {matrix(Q, n, k, ldq, 1, &st), matrix(E, n, steps(k), lde, 1, &st)};
+    const Span out[1] = {matrix(X, n, k, ldx, bytes, &st)};
+    if (st != CBM_OK) return st;
+    if (overlap(in, out)) return CBM_ERR_INVALID_ARG;
+    return cbm_launch_checkpoint_load(n, k, Q, ldq, E, lde, type, nullptr, 0, X, ldx, hip_stream);
+}
+
+cbm_status cbm_checkpoint_relu_backward(int64_t n, int32_t k, const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int32_t type, const void* dY, int64_t lddy, void* dX,
+                                        int64_t lddx, void* hip_stream) {
+    const int64_t bytes = element_bytes(type);
+    if (n < 0 || k <= 0 || !bytes) return CBM_ERR_INVALID_ARG;
+    if (k > MOST_COLUMNS) return CBM_ERR_UNSUPPORTED;
+    cbm_status st = CBM_OK;
+    const Span dy = matrix(dY, n, k, lddy, bytes, &st);
+    const bool in_place = dX == dY && lddx == lddy;  // (a value is read and written by one lane)
+    const Span in[3] = {matrix(Q, n, k, ldq, 1, &st), matrix(E, n, steps(k), lde, 1, &st), in_place ? Span{nullptr, 0, 0} : dy};
+    const Span out[1] = {matrix(dX, n, k, lddx, bytes, &st)};
+    if (st != CBM_OK) return st;
+    if (overlap(in, out)) return CBM_ERR_INVALID_ARG;
+    return cbm_launch_checkpoint_load(n, k, Q, ldq, E, lde, type, dY, lddy, dX, lddx, hip_stream);
+}
+
+size_t cbm_checkpoint_workspace_bytes(int64_t n, int32_t k, int32_t c) {
+    if (n <= 0 || k <= 0 || c <= 0 || k > MOST_COLUMNS || c > MOST_COLUMNS) return 0;
+    const int64_t splits = cbm_grad_splits(n, k, c);
+    return splits == 1 ? 0 : (size_t)splits * (size_t)k * (size_t)c * sizeof(float);
+}
+
+cbm_status cbm_checkpoint_weight_grad(int64_t n, int32_t k, int32_t c, const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int32_t type, const void* dY, int64_t lddy,
+                                      float* dW, int64_t lddw, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    const int64_t bytes = element_bytes(type);
+    if (n < 0 || k <= 0 || c <= 0 || !bytes) return CBM_ERR_INVALID_ARG;
+    if (k > MOST_COLUMNS || c > MOST_COLUMNS || (int64_t)k * c > (int64_t)1 << 32) return CBM_ERR_UNSUPPORTED;
+    const size_t need = cbm_checkpoint_workspace_bytes(n, k, c);
+    if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15))) return CBM_ERR_INVALID_ARG;
+    cbm_status st = CBM_OK;
+    const Span in[3] = {matrix(Q, n, k, ldq, 1, &st), matrix(E, n, steps(k), lde, 1, &st), matrix(dY, n, c, lddy, bytes, &st)};
+    const Span out[2] = {matrix(dW, k, c, lddw, 4, &st), Span{workspace, (uintptr_t)workspace, (uintptr_t)workspace + need}};
+    if (st != CBM_OK) return st;
+    if (overlap(in, out)) return CBM_ERR_INVALID_ARG;
+    return cbm_launch_checkpoint_grad(n, k, c, Q, ldq, E, lde, type, dY, lddy, dW, lddw, (float*)workspace, hip_stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,392 @@
+// Activations kept in 8 bits until the backward pass.  32 columns of a row share a step 2^e, e six below the exponent of the largest of them:
+//   q = sign(x) min(127, max(1, round(|x| 2^-e))), 0 for 0;  x~ = q 2^e.
+// A step that is a power of two costs half a bit against largest / 127, and gives: quotients and x~ that are exact, a byte a step, and x~ that is a bf16 value, so that
+// the weights' gradient takes one operand of the matrix cores as it is.  Values other than zero keep a step at least, so the sign, and with it a ReLU's mask, is kept.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "cbm_elems.h"
+#include "cbm_internal.h"
+#include "cbm_split.h"
+
+namespace {
+
+constexpr int BLOCK = 32;      // columns that share a step
+constexpr int NOT_FINITE = 255;  // the code of a block that holds a value that is not finite: all of it comes back NaN
+
+__device__ __forceinline__ float step_of(uint32_t code) { return __uint_as_float(code << 23); }  // 2^(code - 127); of NOT_FINITE: infinity
+__device__ __forceinline__ float value_of(int q, uint32_t code) { return code == NOT_FINITE ? NAN : (float)q * step_of(code); }
+
+// What a lane has of a row: V columns from `at` on, the first `seen` of them another lane's; fewer than V columns where the row has no more (SHORT rows).
+template <int V, class T>
+__device__ __forceinline__ void load_row_piece(float (&x)[V], const T* row, const Place<V, false>& p, int k) {
+    if (k >= V) {
+        load_piece<V>(x, row + p.at);
+    } else {  // (at < 0: column at + j from 0 on)
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = p.at + j >= 0 ? (float)row[p.at + j] : 0.0f;
+    }
+}
+template <int V>
+__device__ __forceinline__ void load_row_bytes(int (&q)[V], const int8_t* row, const Place<V, false>& p, int k) {
+    if (k >= V) {
+        const typename Piece<int8_t, V>::type v = *reinterpret_cast<const typename Piece<int8_t, V>::type*>(row + p.at);
+#pragma unroll
+        for (int j = 0; j < V; ++j) q[j] = v[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) q[j] = p.at + j >= 0 ? row[p.at + j] : 0;
+    }
+}
+
+// LANES lanes a row (and a share of its columns: blockIdx.y), V columns a lane and turn.  A block of 32 columns is 32 / V lanes.
+template <class T, int LANES>
+__global__ __launch_bounds__(256) void cbm_checkpoint_save_kernel(int64_t n, int k, const T* __restrict__ X, int64_t ldx, int8_t* __restrict__ Q, int64_t ldq,
+                                                                  uint8_t* __restrict__ E, int64_t lde, int turns) {
+    constexpr int V = 16 / (int)sizeof(T), PER_BLOCK = BLOCK / V;
+    const int lane = threadIdx.x % LANES;
+    const int pieces = (k + V - 1) / V;
+    for (int64_t row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES; row < n; row += (int64_t)gridDim.x * (256 / LANES))  // (the lanes of a block of columns together)
+    for (int turn = 0; turn < turns; ++turn) {
+        const int c = (blockIdx.y * turns + turn) * LANES + lane;
+        if (c / PER_BLOCK * PER_BLOCK >= pieces) break;  // (likewise)
+        const Place<V, false> p(c, k);
+        float x[V];
+        load_row_piece<V>(x, X + row * ldx, p, k);
+        // the largest size by its bits, which order sizes, infinity and NaN as they should
+        uint32_t largest = 0;
+#pragma unroll
+        for (int j = 0; j < V; ++j) largest = max(largest, p.counts(j) ? __float_as_uint(x[j]) & 0x7fffffffu : 0u);
+        largest = max(largest, lane_other<1>(largest));
+        largest = max(largest, lane_other<2>(largest));
+        if constexpr (PER_BLOCK == 8) largest = max(largest, lane_other<4>(largest));
+        const bool finite = largest < 0x7f800000u;
+        const uint32_t code = finite ? (uint32_t)max((int)(largest >> 23) - 6, 1) : NOT_FINITE;
+        const float up = __uint_as_float((254u - (finite ? code : 127u)) << 23);
+        uint32_t packed[V / 4];
+#pragma unroll
+        for (int w = 0; w < V / 4; ++w) {
+            packed[w] = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float v = x[4 * w + i], size = fminf(fmaxf(rintf(fabsf(v) * up), 1.0f), 127.0f);
+                const int q = v == 0.0f || !finite ? 0 : (int)copysignf(size, v);
+                packed[w] |= ((uint32_t)q & 255u) << (8 * i);
+            }
+        }
+        int8_t* out = Q + row * ldq + p.at;
+        if (p.seen == 0) {
+            typedef uint32_t Words __attribute__((ext_vector_type(V / 4), aligned(1)));
+            Words words;
+#pragma unroll
+            for (int w = 0; w < V / 4; ++w) words[w] = packed[w];
+            *reinterpret_cast<Words*>(out) = words;
+        } else if (p.any()) {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (p.counts(j)) out[j] = (int8_t)(packed[j / 4] >> (8 * (j % 4)));
+        }
+        if (c % PER_BLOCK == 0) E[row * lde + c / PER_BLOCK] = (uint8_t)code;
+    }
+}
+
+// GATED: dx = q > 0 ? dy : 0, else x~.
+template <class T, int LANES, bool GATED>
+__global__ __launch_bounds__(256) void cbm_checkpoint_load_kernel(int64_t n, int k, const int8_t* __restrict__ Q, int64_t ldq, const uint8_t* __restrict__ E, int64_t lde, const T* dY,
+                                                                  int64_t lddy, T* out, int64_t ldo, int turns) {
+    constexpr int V = 16 / (int)sizeof(T);
+    const int lane = threadIdx.x % LANES;
+    const int pieces = (k + V - 1) / V;
+    for (int64_t row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES; row < n; row += (int64_t)gridDim.x * (256 / LANES))
+    for (int turn = 0; turn < turns; ++turn) {
+        const int c = (blockIdx.y * turns + turn) * LANES + lane;
+        if (c >= pieces) break;
+        const Place<V, false> p(c, k);
+        int q[V];
+        float x[V];
+        load_row_bytes<V>(q, Q + row * ldq, p, k);
+        if constexpr (GATED) load_row_piece<V>(x, dY + row * lddy, p, k);
+        const uint32_t code = E[row * lde + c * V / BLOCK];
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = !GATED ? value_of(q[j], code) : code == NOT_FINITE ? NAN : q[j] > 0 ? x[j] : 0.0f;
+        T* to = out + row * ldo + p.at;
+        if (p.seen == 0) {
+            store_piece<V>(to, x);
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (p.counts(j)) to[j] = (T)x[j];
+        }
+    }
+}
+
+// dW = X~^T dY, a sum over the rows.  Both operands lie along their columns in memory and the matrix cores want eight rows of a column in a lane, so a lane loads, for
+// eight rows, four neighbouring columns of Q and two of dY: 128 columns of Q and 64 of dY by 16 rows a wave, with neither LDS nor transposes, only with columns of dW in
+// an order of their own (tile t has columns 4 i + t of Q, and 2 i + t of dY).  x~ is a bf16 value; dY is split into one, two (fp16) or three (fp32) bf16 values that add
+// up to it, so the products are exact and the sums fp32.  The waves of a workgroup and the workgroups of a tile share the rows; a workgroup adds its waves' sums in LDS, in order.
+constexpr int GRAD_WAVES = 4, GRAD_ROWS = 16, GRAD_K = 128, GRAD_C = 64;
+
+template <class T>
+struct GradStep {  // what a lane has loaded: eight rows
+    uint32_t q[8];
+    uint32_t e[8];
+    float y[2][8];
+};
+template <class T>
+struct GradArgs {
+    int64_t n;
+    int k, c;
+    const int8_t* Q;
+    int64_t ldq;
+    const uint8_t* E;
+    int64_t lde;
+    const T* dY;
+    int64_t lddy;
+};
+template <class T, bool RAGGED>
+__device__ __forceinline__ void grad_load(GradStep<T>& s, const GradArgs<T>& a, int64_t row0, int k0, int c0, int half) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int64_t row = row0 + 8 * half + j, at = min(row, a.n - 1);
+        const int8_t* q = a.Q + at * a.ldq;
+        const T* y = a.dY + at * a.lddy;
+        s.e[j] = a.E[at * a.lde + min(k0, a.k - 1) / BLOCK];
+        if constexpr (RAGGED) {
+            uint32_t v = 0;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) v |= (uint32_t)(uint8_t)q[min(k0 + t, a.k - 1)] << (8 * t);
+            s.q[j] = v;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) s.y[t][j] = (float)y[min(c0 + t, a.c - 1)];
+        } else {
+            typedef uint32_t Word __attribute__((aligned(1)));
+            s.q[j] = *reinterpret_cast<const Word*>(q + min(k0, a.k - 4));
+            float pair[2];
+            load_piece<2>(pair, y + min(c0, a.c - 2));
+            s.y[0][j] = pair[0];
+            s.y[1][j] = pair[1];
+        }
+    }
+    if (row0 + GRAD_ROWS > a.n) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (row0 + 8 * half + j >= a.n) {
+                s.q[j] = 0;
+                s.e[j] = 127;
+                s.y[0][j] = s.y[1][j] = 0.0f;
+            }
+    }
+}
+
+template <class T, bool RAGGED>
+__global__ __launch_bounds__(64 * GRAD_WAVES) void cbm_checkpoint_grad_kernel(GradArgs<T> a, int tiles_c, int tiles, int splits, float* __restrict__ parts, int64_t ldp, int64_t part) {
+    constexpr int PARTS = std::is_same<T, float>::value ? 3 : std::is_same<T, _Float16>::value ? 2 : 1;  // 24, 11 and 8 bits, eight a part
+    __shared__ float room[2][GRAD_K * GRAD_C];
+    // consecutive workgroups run on different XCDs: the tiles of one share of the rows are eight apart, on one XCD, where there are so many shares
+    const int b = blockIdx.x, beside = min(CBM_XCD, splits), split = b / (beside * tiles) * beside + b % beside, tile = b / beside % tiles;
+    if (split >= splits) return;
+    const int lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x / 64;
+    const int k0 = tile / tiles_c * GRAD_K + 4 * (lane & 31), c0 = tile % tiles_c * GRAD_C + 2 * (lane & 31);
+    const int64_t steps = (a.n + GRAD_ROWS - 1) / GRAD_ROWS;
+    const int64_t first = steps * split / splits, last = steps * (split + 1) / splits;
+    floatx16 acc[4][2];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[t][u][v] = 0.0f;
+    uint32_t minus_low = 0xbf80u;
+    asm("" : "+s"(minus_low));
+    for (int64_t i = first + wave; i < last; i += GRAD_WAVES) {
+        GradStep<T> s;
+        grad_load<T, RAGGED>(s, a, i * GRAD_ROWS, k0, c0, half);
+        uintx4 y[2][PARTS];
+        if constexpr (PARTS == 1) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[u][0][j] = high_halves(s.y[u][2 * j], s.y[u][2 * j + 1]);
+        } else {
+            float odd = 0.0f;  // NaN where a value of dY has no parts
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t part[3];
+                    split_pair_nearest(s.y[u][2 * j], s.y[u][2 * j + 1], minus_low, part[0], part[1], part[2]);
+                    odd = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, part[1]), __builtin_bit_cast(bf16x2, 0u), odd, false);
+#pragma unroll
+                    for (int p = 0; p < PARTS; ++p) y[u][p][j] = part[p];
+                }
+            if (__any(odd != odd)) {  // values that are not finite, which are their own high part, or that round up to infinity: parts by truncation
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float v0 = s.y[u][2 * j], v1 = s.y[u][2 * j + 1];
+                        const bool fine0 = fabsf(v0) < INFINITY, fine1 = fabsf(v1) < INFINITY;
+                        uint32_t part[3];  // (with zeros: the remainder of one value reads the parts of both)
+                        split_pair(fine0 ? v0 : 0.0f, fine1 ? v1 : 0.0f, minus_low, part[0], part[1], part[2]);
+                        y[u][0][j] = part[0] | (fine0 ? 0u : (__float_as_uint(v0) >> 16) | (v0 != v0 ? 0x40u : 0u)) |
+                                     (fine1 ? 0u : (__float_as_uint(v1) & 0xffff0000u) | (v1 != v1 ? 0x400000u : 0u));
+#pragma unroll
+                        for (int p = 1; p < PARTS; ++p) y[u][p][j] = part[p];
+                    }
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            uintx4 x;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float v[2];
+#pragma unroll
+                for (int i2 = 0; i2 < 2; ++i2) {
+                    const int r = 2 * j + i2;
+                    const float q = (float)(int8_t)(s.q[r] >> (8 * t));
+                    v[i2] = q * step_of(s.e[r]);  // (NOT_FINITE: 0 times infinity)
+                }
+                x[j] = high_halves(v[0], v[1]);
+            }
+#pragma unroll
+            for (int p = PARTS - 1; p >= 0; --p)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    acc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y[u][p]), acc[t][u], 0, 0, 0);
+        }
+    }
+    // the sums of waves 2 and 3 to 0 and 1, then 1 to 0
+#pragma unroll
+    for (int from = 2; from >= 1; --from) {
+        __syncthreads();
+        if (wave >= from && wave < 2 * from) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) room[wave - from][((t * 2 + u) * 16 + v) * 64 + lane] = acc[t][u][v];
+        }
+        __syncthreads();
+        if (wave < from) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) acc[t][u][v] += room[wave][((t * 2 + u) * 16 + v) * 64 + lane];
+        }
+    }
+    if (wave) return;
+    float* out = parts + split * part;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int row = tile / tiles_c * GRAD_K + 4 * (8 * (v / 4) + 4 * half + v % 4) + t, column = c0 + u;
+                if (row < a.k && column < a.c) out[(int64_t)row * ldp + column] = acc[t][u][v];
+            }
+}
+
+// dW from `count` partial sums, in order: 32 values a workgroup, the partial sums shared by its 32 groups of lanes.
+__global__ __launch_bounds__(1024) void cbm_checkpoint_join_kernel(int count, int64_t size, int c, const float* __restrict__ parts, float* __restrict__ dW, int64_t lddw) {
+    __shared__ float room[32][33];
+    const int slice = threadIdx.x / 32;
+    for (int64_t i0 = (int64_t)blockIdx.x * 32; i0 < size; i0 += (int64_t)gridDim.x * 32) {
+        const int64_t i = i0 + (threadIdx.x & 31);
+        float s = 0.0f;
+        if (i < size)
+#pragma unroll 16
+            for (int p = slice; p < count; p += 32) s += parts[p * size + i];
+        room[slice][threadIdx.x & 31] = s;
+        __syncthreads();
+        if (slice == 0 && i < size) {
+            s = 0.0f;
+#pragma unroll
+            for (int p = 0; p < 32; ++p) s += room[p][threadIdx.x];
+            dW[i / c * lddw + i % c] = s;
+        }
+        __syncthreads();
+    }
+}
+
+cbm_status launched(const char* what) {
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess) return CBM_OK;
+    cbm_set_error_detail(what, hipGetErrorString(e));
+    return CBM_ERR_HIP;
+}
+
+// f(lanes a row, workgroups, turns a workgroup) for rows of `pieces` pieces
+template <class F>
+void along_rows(int64_t n, int64_t pieces, F&& f) {
+    auto go = [&](auto lanes) {
+        constexpr int LANES = decltype(lanes)::value;
+        const int turns = pieces <= LANES ? 1 : 4;
+        f(lanes, dim3((unsigned)std::min<int64_t>((n + 256 / LANES - 1) / (256 / LANES), 1 << 23), (unsigned)((pieces + LANES * turns - 1) / (LANES * turns))), turns);
+    };
+    if (pieces <= 8) go(std::integral_constant<int, 8>{});
+    else if (pieces <= 16) go(std::integral_constant<int, 16>{});
+    else if (pieces <= 32) go(std::integral_constant<int, 32>{});
+    else go(std::integral_constant<int, 64>{});
+}
+
+}  // namespace
+
+int64_t cbm_grad_splits(int64_t n, int32_t k, int32_t c) {
+    const int64_t tiles = ((int64_t)k + GRAD_K - 1) / GRAD_K * (((int64_t)c + GRAD_C - 1) / GRAD_C);
+    return std::max<int64_t>(1, std::min<int64_t>((512 + tiles - 1) / tiles, (n + GRAD_WAVES * GRAD_ROWS - 1) / (GRAD_WAVES * GRAD_ROWS)));
+}
+
+cbm_status cbm_launch_checkpoint_save(int64_t n, int32_t k, int32_t type, const void* X, int64_t ldx, int8_t* Q, int64_t ldq, uint8_t* E, int64_t lde, void* stream) {
+    if (n == 0) return CBM_OK;
+    cbm_with_type(type, [&](auto t) {
+        using T = decltype(t);
+        constexpr int V = 16 / (int)sizeof(T);
+        along_rows(n, ((int64_t)k + V - 1) / V, [&](auto lanes, dim3 grid, int turns) {
+            cbm_checkpoint_save_kernel<T, decltype(lanes)::value><<<grid, 256, 0, (hipStream_t)stream>>>(n, k, (const T*)X, ldx, Q, ldq, E, lde, turns);
+        });
+    });
+    return launched("checkpoint save launch");
+}
+
+cbm_status cbm_launch_checkpoint_load(int64_t n, int32_t k, const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int32_t type, const void* dY, int64_t lddy, void* out,
+                                      int64_t ldo, void* stream) {
+    if (n == 0) return CBM_OK;
+    cbm_with_type(type, [&](auto t) {
+        using T = decltype(t);
+        constexpr int V = 16 / (int)sizeof(T);
+        along_rows(n, ((int64_t)k + V - 1) / V, [&](auto lanes, dim3 grid, int turns) {
+            constexpr int LANES = decltype(lanes)::value;
+            if (dY) cbm_checkpoint_load_kernel<T, LANES, true><<<grid, 256, 0, (hipStream_t)stream>>>(n, k, Q, ldq, E, lde, (const T*)dY, lddy, (T*)out, ldo, turns);
+            else cbm_checkpoint_load_kernel<T, LANES, false><<<grid, 256, 0, (hipStream_t)stream>>>(n, k, Q, ldq, E, lde, nullptr, 0, (T*)out, ldo, turns);
+        });
+    });
+    return launched("checkpoint load launch");
+}
+
+cbm_status cbm_launch_checkpoint_grad(int64_t n, int32_t k, int32_t c, const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int32_t type, const void* dY, int64_t lddy,
+                                      float* dW, int64_t lddw, float* parts, void* stream_) {
+    hipStream_t stream = (hipStream_t)stream_;
+    const int64_t size = (int64_t)k * c;
+    const int splits = n == 0 ? 0 : (int)cbm_grad_splits(n, k, c);
+    if (splits)
+        cbm_with_type(type, [&](auto t) {
+            using T = decltype(t);
+            const int tiles_c = (int)(((int64_t)c + GRAD_C - 1) / GRAD_C), tiles = (int)(((int64_t)k + GRAD_K - 1) / GRAD_K) * tiles_c;
+            const int beside = std::min(CBM_XCD, splits);
+            const unsigned grid = (unsigned)((splits + beside - 1) / beside * beside * tiles);
+            const GradArgs<T> a{n, k, c, Q, ldq, E, lde, (const T*)dY, lddy};
+            float* to = splits == 1 ? dW : parts;
+            const int64_t ldp = splits == 1 ? lddw : c;
+            if (k % 4 || c % 2) cbm_checkpoint_grad_kernel<T, true><<<grid, 64 * GRAD_WAVES, 0, stream>>>(a, tiles_c, tiles, splits, to, ldp, size);
+            else cbm_checkpoint_grad_kernel<T, false><<<grid, 64 * GRAD_WAVES, 0, stream>>>(a, tiles_c, tiles, splits, to, ldp, size);
+        });
+    if (splits != 1) cbm_checkpoint_join_kernel<<<(unsigned)std::min<int64_t>((size + 31) / 32, 1 << 20), 1024, 0, stream>>>(splits, size, c, parts, dW, lddw);
+    return launched("checkpoint gradient launch");
+}

@@ -288,3 +288,12 @@ cbm_status cbm_launch_norm(int64_t n, int32_t k, int32_t type, const void* X, in
                            float* mean, float* rstd, void* stream);
 cbm_status cbm_launch_norm_backward(int64_t n, int32_t k, int32_t type, const void* dY, int64_t lddy, const void* X, int64_t ldx, const float* gamma, const float* mean,
                                     const float* rstd, void* dX, int64_t lddx, float* dgamma, float* dbeta, float* parts, void* stream);
+
+// activations in 8 bits (cbm_checkpoint.hip)
+int64_t cbm_grad_splits(int64_t n, int32_t k, int32_t c);  // shares of the rows, each with a k x c partial sum; 1: none is needed
+cbm_status cbm_launch_checkpoint_save(int64_t n, int32_t k, int32_t type, const void* X, int64_t ldx, int8_t* Q, int64_t ldq, uint8_t* E, int64_t lde, void* stream);
+// restored values, or with a dY its ReLU backward pass
+cbm_status cbm_launch_checkpoint_load(int64_t n, int32_t k, const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int32_t type, const void* dY, int64_t lddy, void* out,
+                                      int64_t ldo, void* stream);
+cbm_status cbm_launch_checkpoint_grad(int64_t n, int32_t k, int32_t c, const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int32_t type, const void* dY, int64_t lddy,
+                                      float* dW, int64_t lddw, float* parts, void* stream);

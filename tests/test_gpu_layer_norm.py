@@ -273,6 +273,6 @@ def test_refusals(env):
     lib, p, q = binding._lib(), X.data_ptr(), Y.data_ptr()
     call = lambda n, k, t, ldx, ldy, x=p, y=q: lib.cbm_layer_norm(n, k, t, x, ldx, None, None, 1e-5, y, ldy, None, None, None)  # noqa: E731
     assert [call(4, 8, 3, 8, 8), call(-1, 8, 0, 8, 8), call(4, 0, 0, 8, 8), call(4, 8, 0, 7, 8), call(4, 8, 0, 8, 7), call(4, 8, 0, 8, 8, None), call(4, 8, 0, 8, 8, p + 1)] == [1] * 7
-    assert call(4, (1 << 30) + 1, 0, 1 << 31, 1 << 31) == 5 and call(1 << 40, 8, 0, 1 << 40, 8) == 5
+    assert call(4, (1 << 24) + 1, 0, 1 << 31, 1 << 31) == 5 and call(1 << 40, 8, 0, 1 << 40, 8) == 5
     assert cbm.cbm_layer_norm_workspace_bytes(4, 0) == 0 and isinstance(ctypes.c_size_t(ws.numel()).value, int)
     assert not bool(Y.any()) and not bool(X.any())

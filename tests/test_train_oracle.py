@@ -28,3 +28,36 @@ def test_layer_norm_by_hand():
     y, m, r = orc.layer_norm([[1.0, 3.0], [5.0, 5.0]], [2.0, 2.0], [0.5, 0.5], eps=0.25)
     assert np.allclose(m, [2, 5]) and np.allclose(r, [1.25 ** -0.5, 2.0])
     assert np.allclose(y, [[0.5 - 2 * 1.25 ** -0.5, 0.5 + 2 * 1.25 ** -0.5], [0.5, 0.5]])
+
+
+def test_kept_values_by_hand():
+    x = np.zeros((3, 34))
+    x[0, :4] = [64.0, -0.4, 0.5, 1.5]       # step 1: ties to even, nothing becomes zero
+    x[0, 32:] = [127.75, 3e-3]              # step 1 again: 128 does not fit 8 bits
+    x[1, 0], x[1, 33] = np.inf, -2.0 ** -140  # the smallest step is 2^-126
+    q, e = orc.keep(x)
+    assert q[0, :5].tolist() == [64, -1, 1, 2, 0] and q[0, 32:].tolist() == [127, 1] and e[0].tolist() == [0, 0]
+    assert e[1].tolist() == [128, -126] and not q[1, :32].any() and q[1, 33] == -1 and not q[2].any()
+    v = orc.kept_values(q, e)
+    assert np.isnan(v[1, :32]).all() and v[1, 33] == -(2.0 ** -126) and v[0, 1] == -1
+
+
+def test_kept_values_are_within_a_step_and_keep_the_sign():
+    rng = np.random.default_rng(1)
+    x = rng.standard_normal((200, 70)) * np.exp2(rng.integers(-100, 100, (200, 1)))
+    q, e = orc.keep(x)
+    v, step = orc.kept_values(q, e), np.repeat(np.ldexp(1.0, e), 32, axis=1)[:, :70]
+    assert np.all(np.abs(v - x) <= step) and np.array_equal(np.sign(v), np.sign(x))
+    plain = (np.abs(x) >= step / 2) & (np.abs(x) <= 127.5 * step)
+    assert np.all(np.abs(v - x)[plain] <= step[plain] / 2)
+
+
+def test_weight_and_relu_gradients_are_the_slopes():
+    """Of a loss that is linear in Y = X~ W, and in relu(Z) with X~ = relu(Z) kept."""
+    rng = np.random.default_rng(2)
+    z, w, dy, v = rng.standard_normal((9, 40)), rng.standard_normal((40, 5)), rng.standard_normal((9, 5)), rng.standard_normal((40, 5))
+    q, e = orc.keep(np.maximum(z, 0))
+    x = orc.kept_values(q, e)
+    assert (orc.weight_grad(q, e, dy) * v).sum() == pytest.approx(_slope(lambda t: (x @ t * dy).sum(), w, v), rel=1e-7)
+    g, u = rng.standard_normal(z.shape), rng.standard_normal(z.shape)
+    assert (orc.relu_backward(q, e, g) * u).sum() == pytest.approx(_slope(lambda t: (np.maximum(t, 0) * g).sum(), z, u, 1e-9), rel=1e-5)
