@@ -377,6 +377,31 @@ cbm_status cbm_checkpoint_weight_grad(int64_t n, int32_t k, int32_t c, const int
                                       size_t workspace_bytes, void* hip_stream);
 size_t cbm_checkpoint_workspace_bytes(int64_t n, int32_t k, int32_t c);
 
+/*
+ * cbm_log_probs -- along each row z of scores, with m = max z, l = log sum exp(z - m) and log p = z - m - l:
+ *   Z            n x c, of `type`.  A score of -infinity rules its class out.
+ *   labels       n whole numbers of label_bits 32 or 64; a row whose label is outside [0, c) has none.  May be NULL where logp is.
+ *   logp         log p[label], 0 for a row without a label.
+ *   entropy      -sum p log p.
+ *   stats        n x 2: m and l, which the backward pass reads.
+ *   top          0 to 32 alternatives: top_values (n x top) receives the largest log p in descending order, top_columns (n x top) their classes, the
+ *                lower one first among equal scores; where fewer classes are not ruled out, -infinity and -1.
+ *   workspace    cbm_log_probs_workspace_bytes(n, c, top) bytes; may be 0 (few and long rows are shared by several workgroups).
+ * logp, entropy and stats may be NULL; fp32, packed.  A row with every class ruled out has m = l = log p[label] = -infinity and entropy 0.  A row
+ * with NaN or +infinity has NaN for all of it (0 without a label, classes -1).
+ *
+ * cbm_log_probs_backward -- dZ = a (1[label] - p) - b p (log p + entropy), a = dlogp, the gradient of log p[label] (0 without a label), and
+ * b = dentropy, that of the entropy.  labels may be NULL where dlogp is, entropy where dentropy is; one of the two gradients has to be there.
+ * Zeros in a row with every class ruled out.  dZ (n x c, of `type`) may be Z itself with lddz = ldz.
+ */
+cbm_status cbm_log_probs(int64_t n, int32_t c, int32_t type, const void* Z, int64_t ldz, const void* labels, int32_t label_bits,
+                         float* logp, float* entropy, float* stats, int32_t top, float* top_values, int32_t* top_columns,
+                         void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t cbm_log_probs_workspace_bytes(int64_t n, int32_t c, int32_t top);
+cbm_status cbm_log_probs_backward(int64_t n, int32_t c, int32_t type, const void* Z, int64_t ldz, const void* labels, int32_t label_bits,
+                                  const float* stats, const float* entropy, const float* dlogp, const float* dentropy, void* dZ,
+                                  int64_t lddz, void* hip_stream);
+
 /* Counters of the built format (Properties 1 and 2, Lemma 2.2). */
 cbm_status cbm_stats(const cbm_handle* h, cbm_stats_t* out);
 

@@ -63,3 +63,48 @@ def relu_backward(q, e, dy):
 def weight_grad(q, e, dy):
     with np.errstate(invalid="ignore"):
         return kept_values(q, e).T @ np.asarray(dy, dtype=np.float64)
+
+
+def log_probs(z, labels, top=0):
+    """(log p[label], entropy, (m, l), values, columns): see the C ABI's header for rows without a distribution."""
+    z = np.asarray(z, dtype=np.float64)
+    n, c = z.shape
+    with np.errstate(invalid="ignore", divide="ignore", over="ignore"):
+        m = z.max(axis=1)
+        bad, empty = ~(m < np.inf), m == -np.inf  # (NaN passes through max)
+        d = z - np.where(empty, 0.0, m)[:, None]
+        e = np.exp(d)
+        s = e.sum(axis=1)
+        l = np.log(s)  # noqa: E741
+        entropy = np.where(empty, 0.0, l - np.where(e > 0, d * e, 0.0).sum(axis=1) / np.where(empty, 1.0, s))
+        logs = np.where(empty[:, None], -np.inf, d - np.where(empty, 0.0, l)[:, None])
+    labels = np.asarray(labels)
+    given = (labels >= 0) & (labels < c)
+    logp = np.where(given, logs[np.arange(n), np.where(given, labels, 0)], 0.0)
+    m, l, entropy = (np.where(bad, np.nan, a) for a in (m, l, entropy))  # noqa: E741
+    logp = np.where(bad & given, np.nan, logp)
+    values, columns = np.full((n, top), -np.inf), np.full((n, top), -1, dtype=np.int64)
+    if top:
+        order = np.argsort(-np.where(np.isnan(z), -np.inf, z), axis=1, kind="stable")[:, :top]  # (equal scores: the lower column first)
+        some = order.shape[1]
+        there = np.take_along_axis(z, order, axis=1) > -np.inf
+        columns[:, :some] = np.where(there & ~bad[:, None], order, -1)
+        values[:, :some] = np.where(there, np.take_along_axis(logs, order, axis=1), -np.inf)
+        values[bad] = np.nan
+    return logp, entropy, np.stack([m, l], axis=1), values, columns
+
+
+def log_probs_backward(z, labels, stats, entropy, dlogp, dentropy):
+    z, stats = np.asarray(z, dtype=np.float64), np.asarray(stats, dtype=np.float64)
+    n, c = z.shape
+    labels = np.asarray(labels)
+    given = (labels >= 0) & (labels < c)
+    empty = stats[:, 0] == -np.inf
+    with np.errstate(invalid="ignore"):
+        logs = np.where(empty[:, None], -np.inf, z - stats[:, :1] - stats[:, 1:])
+    p = np.exp(logs)
+    a = np.where(given & ~empty, dlogp, 0.0)[:, None]
+    hot = np.zeros_like(z)
+    hot[np.arange(n), np.where(given, labels, 0)] = 1.0
+    slope = np.where(logs == -np.inf, 0.0, p * (np.where(logs == -np.inf, 0.0, logs) + np.asarray(entropy, dtype=np.float64)[:, None]))
+    return a * (hot - p) - np.asarray(dentropy, dtype=np.float64)[:, None] * slope

@@ -25,6 +25,7 @@ EXPORTS = [
     "cbm_layer_norm", "cbm_layer_norm_backward", "cbm_layer_norm_workspace_bytes",
     "cbm_checkpoint_save", "cbm_checkpoint_restore", "cbm_checkpoint_relu_backward",
     "cbm_checkpoint_weight_grad", "cbm_checkpoint_workspace_bytes",
+    "cbm_log_probs", "cbm_log_probs_workspace_bytes", "cbm_log_probs_backward",
     "cbm_profile_enable", "cbm_profile_read", "cbm_free", "cbm_status_string", "cbm_last_error_detail",
 ]
 
@@ -62,13 +63,14 @@ class cbm_launch_record(C.Structure):
 
 
 _LIB = None
-_F32 = None  # torch.float32, known once the library is loaded
+_F32 = _INT32 = None  # torch.float32 and int32, known once the library is loaded
 _DTYPES = {}  # torch's types of the operators between the products: cbm_dtype, likewise
 _INT8, _UINT8 = {}, {}
+_LABELS = {}  # torch's types of labels: bits
 
 
 def _lib():
-    global _LIB, _F32
+    global _LIB, _F32, _INT32
     if _LIB is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is not built: run `python -m paper_2409_02208_amd.build`")
@@ -76,9 +78,10 @@ def _lib():
         # the library binds to that same runtime: device pointers and streams are only meaningful within one.
         import torch
 
-        _F32 = torch.float32
+        _F32, _INT32 = torch.float32, torch.int32
         _DTYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
         _INT8[torch.int8] = _UINT8[torch.uint8] = 0
+        _LABELS.update({torch.int32: 32, torch.int64: 64})
         lib = C.CDLL(LIB_PATH)
         vp, i64, i32, f32p = C.c_void_p, C.c_int64, C.c_int32, C.c_void_p
         lib.cbm_build.argtypes = [i64, i64, vp, vp, C.POINTER(cbm_build_opts), C.POINTER(vp)]
@@ -101,6 +104,10 @@ def _lib():
         lib.cbm_checkpoint_weight_grad.argtypes = [i64, i32, i32, vp, i64, vp, i64, i32, vp, i64, f32p, i64, vp, C.c_size_t, vp]
         lib.cbm_checkpoint_workspace_bytes.argtypes = [i64, i32, i32]
         lib.cbm_checkpoint_workspace_bytes.restype = C.c_size_t
+        lib.cbm_log_probs.argtypes = [i64, i32, i32, vp, i64, vp, i32, f32p, f32p, f32p, i32, f32p, vp, vp, C.c_size_t, vp]
+        lib.cbm_log_probs_workspace_bytes.argtypes = [i64, i32, i32]
+        lib.cbm_log_probs_workspace_bytes.restype = C.c_size_t
+        lib.cbm_log_probs_backward.argtypes = [i64, i32, i32, vp, i64, vp, i32, f32p, f32p, f32p, f32p, vp, i64, vp]
         lib.cbm_stats.argtypes = [vp, C.POINTER(cbm_stats_t)]
         lib.cbm_get_tree.argtypes = [vp, vp, vp, vp, vp]
         lib.cbm_decompress.argtypes = [vp, vp, vp]
@@ -382,6 +389,52 @@ def cbm_checkpoint_weight_grad(Q, E, dY, dW, workspace, stream=None):
     sp, sbytes = _workspace(workspace)
     _check(lib.cbm_checkpoint_weight_grad(n, k, c, *kept, dtype, gp, ldg, wp, ldw, sp, sbytes, _stream_ptr(stream)), "cbm_checkpoint_weight_grad")
     return dW
+
+
+def _labels(t, size):
+    """(address, bits) of `size` labels; none: (None, 64)."""
+    if t is None:
+        return None, 64
+    bits = _LABELS.get(t.dtype)
+    if bits is None:
+        raise ValueError("labels must be int32 or int64")
+    return _vector(t, "labels", size, t.dtype), bits
+
+
+def _packed(t, name, rows, cols, dtype):
+    """Address of a packed device matrix of rows x cols; None stays None."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype is not dtype or tuple(t.shape) != (rows, cols) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a packed {rows} x {cols} device matrix of {dtype}")
+    return t.data_ptr()
+
+
+def cbm_log_probs_workspace_bytes(n: int, c: int, top: int = 0) -> int:
+    return int((_LIB or _lib()).cbm_log_probs_workspace_bytes(n, c, top))
+
+
+def cbm_log_probs(Z, labels, logp, entropy=None, stats=None, top_values=None, top_columns=None, workspace=None, stream=None):
+    lib = _LIB or _lib()
+    zp, ldz, n, c, dtype = _matrix(Z, "Z")
+    lp, bits = _labels(labels, n)
+    top = 0 if top_values is None else top_values.shape[-1]
+    tv, tc = _packed(top_values, "top_values", n, top, _F32), _packed(top_columns, "top_columns", n, top, _INT32)
+    wp, wbytes = _workspace(workspace)
+    _check(lib.cbm_log_probs(n, c, dtype, zp, ldz, lp, bits, _vector(logp, "logp", n), _vector(entropy, "entropy", n), _packed(stats, "stats", n, 2, _F32), top, tv, tc, wp, wbytes,
+                             _stream_ptr(stream)), "cbm_log_probs")
+    return logp
+
+
+def cbm_log_probs_backward(Z, labels, stats, entropy, dlogp, dentropy, dZ, stream=None):
+    lib = _LIB or _lib()
+    zp, ldz, n, c, dtype = _matrix(Z, "Z")
+    dp, ldd, *d = _matrix(dZ, "dZ")
+    _same([n, c, dtype], d, "Z and dZ")
+    lp, bits = _labels(labels, n)
+    _check(lib.cbm_log_probs_backward(n, c, dtype, zp, ldz, lp, bits, _packed(stats, "stats", n, 2, _F32), _vector(entropy, "entropy", n), _vector(dlogp, "dlogp", n),
+                                      _vector(dentropy, "dentropy", n), dp, ldd, _stream_ptr(stream)), "cbm_log_probs_backward")
+    return dZ
 
 
 def cbm_stats(h: Handle) -> dict:

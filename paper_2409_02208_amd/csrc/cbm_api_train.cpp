@@ -140,4 +140,43 @@ cbm_status cbm_checkpoint_weight_grad(int64_t n, int32_t k, int32_t c, const int
     return cbm_launch_checkpoint_grad(n, k, c, Q, ldq, E, lde, type, dY, lddy, dW, lddw, (float*)workspace, hip_stream);
 }
 
+size_t cbm_log_probs_workspace_bytes(int64_t n, int32_t c, int32_t top) {
+    if (n <= 0 || c <= 0 || c > MOST_COLUMNS || top < 0 || top > CBM_MOST_TOP) return 0;
+    const int splits = cbm_scores_splits(n, c);
+    return splits == 1 ? 0 : (size_t)n * (size_t)splits * cbm_scores_part_bytes(top);
+}
+
+cbm_status cbm_log_probs(int64_t n, int32_t c, int32_t type, const void* Z, int64_t ldz, const void* labels, int32_t label_bits, float* logp, float* entropy, float* stats, int32_t top,
+                         float* top_values, int32_t* top_columns, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    const int64_t bytes = element_bytes(type);
+    if (n < 0 || c <= 0 || !bytes || top < 0 || top > CBM_MOST_TOP || (label_bits != 32 && label_bits != 64)) return CBM_ERR_INVALID_ARG;
+    if (c > MOST_COLUMNS) return CBM_ERR_UNSUPPORTED;
+    const size_t need = cbm_log_probs_workspace_bytes(n, c, top);
+    if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15))) return CBM_ERR_INVALID_ARG;
+    cbm_status st = CBM_OK;
+    const Span none{nullptr, 0, 0};
+    const Span in[2] = {matrix(Z, n, c, ldz, bytes, &st), logp ? matrix(labels, 1, n, n, label_bits / 8, &st) : none};
+    const Span out[6] = {maybe(logp, n, 4, &st), maybe(entropy, n, 4, &st), maybe(stats, 2 * n, 4, &st), top ? matrix(top_values, n, top, top, 4, &st) : none,
+                         top ? matrix(top_columns, n, top, top, 4, &st) : none, Span{workspace, (uintptr_t)workspace, (uintptr_t)workspace + need}};
+    if (st != CBM_OK) return st;
+    if (overlap(in, out)) return CBM_ERR_INVALID_ARG;
+    return cbm_launch_scores(n, c, type, Z, ldz, labels, label_bits, logp, entropy, stats, top, top_values, top_columns, workspace, hip_stream);
+}
+
+cbm_status cbm_log_probs_backward(int64_t n, int32_t c, int32_t type, const void* Z, int64_t ldz, const void* labels, int32_t label_bits, const float* stats, const float* entropy,
+                                  const float* dlogp, const float* dentropy, void* dZ, int64_t lddz, void* hip_stream) {
+    const int64_t bytes = element_bytes(type);
+    if (n < 0 || c <= 0 || !bytes || (label_bits != 32 && label_bits != 64) || (n > 0 && !dlogp && !dentropy)) return CBM_ERR_INVALID_ARG;
+    if (c > MOST_COLUMNS) return CBM_ERR_UNSUPPORTED;
+    cbm_status st = CBM_OK;
+    const Span none{nullptr, 0, 0}, z = matrix(Z, n, c, ldz, bytes, &st);
+    const bool in_place = dZ == Z && lddz == ldz;  // (a value is read for good before it is written, by one lane)
+    const Span in[6] = {in_place ? none : z, dlogp ? matrix(labels, 1, n, n, label_bits / 8, &st) : none, matrix(stats, 1, 2 * n, 2 * n, 4, &st),
+                        dentropy ? matrix(entropy, 1, n, n, 4, &st) : none, maybe(dlogp, n, 4, &st), maybe(dentropy, n, 4, &st)};
+    const Span out[1] = {matrix(dZ, n, c, lddz, bytes, &st)};
+    if (st != CBM_OK) return st;
+    if (overlap(in, out)) return CBM_ERR_INVALID_ARG;
+    return cbm_launch_scores_backward(n, c, type, Z, ldz, labels, label_bits, stats, entropy, dlogp, dentropy, dZ, lddz, hip_stream);
+}
+
 }  // extern "C"

@@ -297,3 +297,12 @@ cbm_status cbm_launch_checkpoint_load(int64_t n, int32_t k, const int8_t* Q, int
                                       int64_t ldo, void* stream);
 cbm_status cbm_launch_checkpoint_grad(int64_t n, int32_t k, int32_t c, const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int32_t type, const void* dY, int64_t lddy,
                                       float* dW, int64_t lddw, float* parts, void* stream);
+
+// log probabilities (cbm_scores.hip)
+constexpr int32_t CBM_MOST_TOP = 32;                // alternatives
+int cbm_scores_splits(int64_t n, int32_t c);        // workgroups that share a row; 1: no workspace
+size_t cbm_scores_part_bytes(int32_t top);          // of the workspace for each of them
+cbm_status cbm_launch_scores(int64_t n, int32_t c, int32_t type, const void* z, int64_t ldz, const void* labels, int label_bits, float* logp, float* entropy, float* stats, int32_t top,
+                             float* values, int32_t* columns, void* parts, void* stream);
+cbm_status cbm_launch_scores_backward(int64_t n, int32_t c, int32_t type, const void* z, int64_t ldz, const void* labels, int label_bits, const float* stats, const float* entropy,
+                                      const float* dlogp, const float* dentropy, void* dz, int64_t lddz, void* stream);

@@ -1,0 +1,490 @@
+// Log probabilities of given labels, with entropy and the top alternatives, and their gradient.  Along a row z of C scores
+//   m = max z,  l = log sum exp(z - m),  log p = z - m - l,  H = -sum p log p = l - sum (z - m) exp(z - m) / sum exp(z - m);
+//   dz = a (1[label] - p) - h p (log p + H),  a and h the gradients of log p[label] and of H.
+// Bound by memory: z is read once, forward and backward.  Short rows stay in the registers of a group of lanes; long ones pass through a workgroup with a
+// running maximum and sums in every lane, few and long ones through several, which a second launch joins.  Statistics are fp32; exp is the hardware's 2^x.
+// Scores of -infinity are ruled out; a row with nothing else has no distribution (m = l = -infinity, H = 0).  NaN or +infinity makes the sums NaN, and with them all of the row.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "cbm_elems.h"
+#include "cbm_internal.h"
+
+namespace {
+
+constexpr float LOG2E = 1.44269504088896341f;
+constexpr int MOST_TOP = CBM_MOST_TOP;
+constexpr int MOST_SPLITS = 64;    // workgroups that share a row: a lane each when they are joined
+constexpr int LONG_THREADS = 256;
+constexpr float FAR = -200.0f;     // exp of less is 0 in fp32: stands for -infinity where it is multiplied by that 0
+
+__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * LOG2E); }
+// values in an order of whole numbers: 0 for what is no alternative (-infinity), -0 as 0
+__device__ __forceinline__ uint32_t ordered(float v) {
+    const uint32_t b = __float_as_uint(v + 0.0f);
+    return v > -INFINITY ? b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u) : 0u;
+}
+__device__ __forceinline__ float in_order(uint32_t o) { return __uint_as_float(o ^ ((uint32_t)((int32_t)~o >> 31) | 0x80000000u)); }
+// the larger value first, of equal ones the lower column; 0: none
+__device__ __forceinline__ uint64_t key_of(uint32_t o, int column) { return o ? (uint64_t)o << 32 | (uint32_t)~column : 0; }
+
+struct Scores {
+    int64_t n;
+    int c;
+    const void* z;
+    int64_t ldz;
+    const void* labels;
+    int wide_labels;  // 64 bits
+    float *logp, *entropy, *stats;
+    int top;
+    float* values;
+    int32_t* columns;
+};
+__device__ __forceinline__ int64_t label_of(const void* labels, int wide, int64_t row) { return wide ? ((const int64_t*)labels)[row] : (int64_t)((const int32_t*)labels)[row]; }
+
+// What one lane writes of a row, from its statistics and its score at the label (`given`: it has one).
+__device__ __forceinline__ void write_row(const Scores& a, int64_t row, float m, float l, float entropy, float at_label, bool given) {
+    if (a.stats) {
+        a.stats[2 * row] = m;
+        a.stats[2 * row + 1] = l;
+    }
+    if (a.entropy) a.entropy[row] = entropy;
+    if (a.logp) a.logp[row] = !given ? 0.0f : m == -INFINITY ? m : at_label - m - l;
+}
+// statistics from the maximum and the sums of e = exp(z - m) and of (z - m) e
+__device__ __forceinline__ void finish(float& m, float s, float t, float& l, float& entropy) {
+    if (m == -INFINITY && s == 0.0f) {
+        l = m;
+        entropy = 0.0f;
+    } else {
+        l = logf(s);
+        entropy = l - t / s;
+        if (s != s) m = s;
+    }
+}
+
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return max(a, b); }
+template <int LANES, class U>
+__device__ __forceinline__ U lanes_max(U v) {
+    if constexpr (LANES >= 2) v = larger(v, lane_other<1>(v));
+    if constexpr (LANES >= 4) v = larger(v, lane_other<2>(v));
+    if constexpr (LANES >= 8) v = larger(v, lane_other<4>(v));
+    if constexpr (LANES >= 16) v = larger(v, lane_other<8>(v));
+    if constexpr (LANES >= 32) v = larger(v, lane_other<16>(v));
+    if constexpr (LANES >= 64) v = larger(v, lane_other<32>(v));
+    return v;
+}
+
+// LANES lanes a row, each R pieces of V columns.
+template <class T, int V, int LANES, int R>
+__global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
+    const int lane = threadIdx.x % LANES;
+    for (int64_t row0 = (int64_t)blockIdx.x * (256 / LANES); row0 < a.n; row0 += (int64_t)gridDim.x * (256 / LANES)) {
+        const int64_t row = row0 + threadIdx.x / LANES, at = row < a.n ? row : a.n - 1;
+        const T* z_row = (const T*)a.z + at * a.ldz;
+        float x[R][V], m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const Place<V, false> p(i * LANES + lane, a.c);
+            load_piece<V>(x[i], z_row + p.at);
+        }
+        bool given = false;
+        float at_label = 0.0f;
+        if (a.logp && lane == 0) {
+            const int64_t label = label_of(a.labels, a.wide_labels, at);
+            given = label >= 0 && label < a.c;
+            if (given) at_label = (float)z_row[label];
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const Place<V, false> p(i * LANES + lane, a.c);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                x[i][j] = p.counts(j) ? x[i][j] : -INFINITY;
+                m = fmaxf(m, x[i][j]);
+            }
+        }
+        m = lanes_max<LANES>(m);
+        const float base = m == -INFINITY ? 0.0f : m;
+        float s = 0.0f, t = 0.0f, l, entropy;
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float d = x[i][j] - base, e = exp_of(d);
+                s += e;
+                t += e * fmaxf(d, FAR);
+            }
+        s = lanes_sum<LANES>(s);
+        t = lanes_sum<LANES>(t);
+        finish(m, s, t, l, entropy);
+        if (lane == 0 && row < a.n) write_row(a, row, m, l, entropy, at_label, given);
+        if (!a.top) continue;
+        uint32_t o[R][V];
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int j = 0; j < V; ++j) o[i][j] = m == m ? ordered(x[i][j]) : 0u;
+        for (int r = 0; r < a.top; ++r) {  // the largest, then the lowest column that has it, then without that one
+            uint32_t best = 0;
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+#pragma unroll
+                for (int j = 0; j < V; ++j) best = max(best, o[i][j]);
+            best = lanes_max<LANES>(best);
+            uint32_t column = 0xffffffffu;
+#pragma unroll
+            for (int i = R - 1; i >= 0; --i) {
+                const Place<V, false> p(i * LANES + lane, a.c);
+#pragma unroll
+                for (int j = V - 1; j >= 0; --j) column = o[i][j] == best ? (uint32_t)(p.at + j) : column;
+            }
+            column = best ? ~lanes_max<LANES>(~column) : 0xffffffffu;
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const Place<V, false> p(i * LANES + lane, a.c);
+#pragma unroll
+                for (int j = 0; j < V; ++j) o[i][j] = (uint32_t)(p.at + j) == column ? 0u : o[i][j];
+            }
+            if (lane == 0 && row < a.n) {
+                a.values[row * a.top + r] = m != m ? m : best ? in_order(best) - m - l : -INFINITY;
+                a.columns[row * a.top + r] = (int32_t)column;
+            }
+        }
+    }
+}
+
+// The `top` largest keys of a workgroup of LONG_THREADS.  `head`: 64 keys that are in the collection, at most one of each of 64 parts of it, so that its top-th largest
+// bounds the answer from below; keys of at least that are collected, with those found before, and ranked by counting.
+template <int CAP>
+struct Select {
+    uint64_t head[64], list[MOST_TOP], found[CAP];
+    uint64_t bound;
+    int count;
+};
+template <int CAP, class F>
+__device__ __forceinline__ void select_keys(Select<CAP>& s, int top, F&& each) {
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        const uint64_t mine = s.head[threadIdx.x];
+        int rank = 0, there = 0;
+#pragma unroll 8
+        for (int i = 0; i < 64; ++i) {
+            const uint64_t other = s.head[i];
+            rank += other > mine;
+            there += other != 0;
+        }
+        if (there < top ? threadIdx.x == 0 : mine && rank == top - 1) s.bound = there < top ? 1 : mine;
+        if (threadIdx.x == 0) s.count = 0;
+    }
+    __syncthreads();
+    auto take = [&](uint64_t key) {
+        if (key >= s.bound) s.found[atomicAdd(&s.count, 1)] = key;
+    };
+    each(take);
+    if (threadIdx.x < top) take(s.list[threadIdx.x]);
+    __syncthreads();
+    const int count = s.count;
+    if (threadIdx.x < top) s.list[threadIdx.x] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < count; i += LONG_THREADS) {
+        const uint64_t mine = s.found[i];
+        int rank = 0;
+        for (int j = 0; j < count; ++j) rank += s.found[j] > mine;
+        if (rank < top) s.list[rank] = mine;  // (keys differ, so do ranks)
+    }
+    __syncthreads();
+}
+
+__device__ __forceinline__ void write_top(const Scores& a, int64_t row, const uint64_t* list, float m, float l) {
+    if ((int)threadIdx.x >= a.top) return;
+    const uint64_t key = m == m ? list[threadIdx.x] : 0;
+    a.values[row * a.top + threadIdx.x] = m != m ? m : key ? in_order((uint32_t)(key >> 32)) - m - l : -INFINITY;
+    a.columns[row * a.top + threadIdx.x] = key ? (int32_t)~(uint32_t)key : -1;
+}
+
+struct Part {  // of a row that several workgroups share; `top` keys follow
+    float m, s, t, unused;
+};
+__device__ __forceinline__ char* part_at(char* parts, int64_t i, int top) { return parts + i * (int64_t)(sizeof(Part) + top * sizeof(uint64_t)); }
+
+// Sums over the lanes of a wave, each with a maximum of its own.
+__device__ __forceinline__ void join_wave(float& m, float& s, float& t) {
+    const float all = lanes_max<64>(m), base = all == -INFINITY ? 0.0f : all;
+    const float d = m - base, f = exp_of(d);
+    t = lanes_sum<64>(f * (t + fmaxf(d, FAR) * s));
+    s = lanes_sum<64>(f * s);
+    m = all;
+}
+
+// A workgroup a row, or a share of `columns` of its columns (a multiple of V); R pieces of V columns a lane and turn.
+template <class T, int V, int R, bool TOP>
+__global__ __launch_bounds__(LONG_THREADS) void cbm_scores_long_kernel(Scores a, int splits, int columns, char* __restrict__ parts) {
+    constexpr int TURN = LONG_THREADS * R * V, CAP = TOP ? MOST_TOP * 4 * R * V + MOST_TOP : 1;
+    __shared__ Select<CAP> sel;
+    __shared__ float room[3][LONG_THREADS / 64];
+    const int wave = threadIdx.x / 64;
+    for (int64_t item = blockIdx.x; item < a.n * splits; item += gridDim.x) {
+        const int64_t row = item / splits;
+        const int split = (int)(item % splits);
+        const T* z_row = (const T*)a.z + row * a.ldz;
+        const int begin = split * columns, end = min(begin + columns, a.c);
+        float m = -INFINITY, s = 0.0f, t = 0.0f;
+        float least = -INFINITY;  // the last of the alternatives so far; a later column has to exceed it
+        if constexpr (TOP) {
+            __syncthreads();
+            if ((int)threadIdx.x < MOST_TOP) sel.list[threadIdx.x] = 0;
+        }
+        for (int turn = begin; turn < end; turn += TURN) {
+            float x[R][V], most = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const Place<V, false> p(turn / V + i * LONG_THREADS + threadIdx.x, a.c);
+                load_piece<V>(x[i], z_row + p.at);
+            }
+            if (turn + TURN > end) {
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                    const int piece = turn / V + i * LONG_THREADS + threadIdx.x, seen = piece * V < end ? Place<V, false>(piece, a.c).seen : V;
+#pragma unroll
+                    for (int j = 0; j < V; ++j) x[i][j] = j >= seen ? x[i][j] : -INFINITY;
+                    __builtin_amdgcn_sched_barrier(0);  // (one piece's comparisons at a time: all of them need more scalar registers than there are)
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+#pragma unroll
+                for (int j = 0; j < V; ++j) most = fmaxf(most, x[i][j]);
+            const float now = fmaxf(m, most), base = now == -INFINITY ? 0.0f : now;
+            {
+                const float d = m - base, f = exp_of(d);
+                t = f * (t + fmaxf(d, FAR) * s);
+                s *= f;
+                m = now;
+            }
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float d = x[i][j] - base, e = exp_of(d);
+                    s += e;
+                    t += e * fmaxf(d, FAR);
+                }
+            if constexpr (TOP) {
+                if (!__syncthreads_or(most > least)) continue;
+                // the best key of each lane, and of each four lanes
+                int column = 0;
+#pragma unroll
+                for (int i = R - 1; i >= 0; --i) {
+                    const Place<V, false> p(turn / V + i * LONG_THREADS + threadIdx.x, a.c);
+#pragma unroll
+                    for (int j = V - 1; j >= 0; --j) column = x[i][j] == most ? p.at + j : column;
+                }
+                const uint64_t mine = most > least ? key_of(ordered(most), column) : 0;
+                uint64_t best = mine;
+#pragma unroll
+                for (int step = 1; step <= 2; step *= 2) {
+                    const uint64_t other = (uint64_t)__shfl_xor((unsigned long long)best, step);
+                    best = other > best ? other : best;
+                }
+                if (threadIdx.x % 4 == 0) sel.head[threadIdx.x / 4] = best;
+                select_keys(sel, a.top, [&](auto&& take) {
+                    if (mine < sel.bound) return;  // (0 < 1 <= bound)
+                    float before = least;
+                    asm("" : "+v"(before));  // (compared anew: what the first comparisons gave is more than the scalar registers hold)
+#pragma unroll
+                    for (int i = 0; i < R; ++i) {
+                        const Place<V, false> p(turn / V + i * LONG_THREADS + threadIdx.x, a.c);
+#pragma unroll
+                        for (int j = 0; j < V; ++j) take(x[i][j] > before ? key_of(ordered(x[i][j]), p.at + j) : 0);
+                    }
+                });
+                const uint64_t last = sel.list[a.top - 1];
+                least = last ? in_order((uint32_t)(last >> 32)) : -INFINITY;
+            }
+        }
+        join_wave(m, s, t);
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) {
+            room[0][wave] = m;
+            room[1][wave] = s;
+            room[2][wave] = t;
+        }
+        __syncthreads();
+        const int w = min((int)threadIdx.x & 63, LONG_THREADS / 64 - 1);
+        const bool first = (threadIdx.x & 63) < LONG_THREADS / 64;
+        m = first ? room[0][w] : -INFINITY;
+        s = first ? room[1][w] : 0.0f;
+        t = first ? room[2][w] : 0.0f;
+        join_wave(m, s, t);
+        if (splits > 1) {
+            char* part = part_at(parts, item, a.top);
+            if (threadIdx.x == 0) *(Part*)part = Part{m, s, t, 0.0f};
+            if constexpr (TOP)
+                if ((int)threadIdx.x < a.top) ((uint64_t*)(part + sizeof(Part)))[threadIdx.x] = sel.list[threadIdx.x];
+        } else {
+            float l, entropy;
+            finish(m, s, t, l, entropy);
+            if (threadIdx.x == 0) {
+                const int64_t label = a.logp ? label_of(a.labels, a.wide_labels, row) : -1;
+                const bool given = label >= 0 && label < a.c;
+                write_row(a, row, m, l, entropy, given ? (float)z_row[label] : 0.0f, given);
+            }
+            if constexpr (TOP) write_top(a, row, sel.list, m, l);
+        }
+    }
+}
+
+// Rows that several workgroups have shared: a workgroup each.
+template <class T>
+__global__ __launch_bounds__(LONG_THREADS) void cbm_scores_join_kernel(Scores a, int splits, char* __restrict__ parts) {
+    __shared__ Select<MOST_TOP * MOST_TOP> sel;  // (of at most `top` parts, `top` keys each)
+    for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+        const int lane = threadIdx.x & 63;
+        Part mine{-INFINITY, 0.0f, 0.0f, 0.0f};
+        if (lane < splits) mine = *(const Part*)part_at(parts, row * splits + lane, a.top);
+        float m = mine.m, s = mine.s, t = mine.t, l, entropy;
+        join_wave(m, s, t);
+        finish(m, s, t, l, entropy);
+        if (threadIdx.x == 0) {
+            const int64_t label = a.logp ? label_of(a.labels, a.wide_labels, row) : -1;
+            const bool given = label >= 0 && label < a.c;
+            write_row(a, row, m, l, entropy, given ? (float)((const T*)a.z)[row * a.ldz + label] : 0.0f, given);
+        }
+        if (!a.top) continue;
+        auto key_at = [&](int split, int i) { return ((const uint64_t*)(part_at(parts, row * splits + split, a.top) + sizeof(Part)))[i]; };
+        __syncthreads();
+        if (threadIdx.x < 64) sel.head[lane] = lane < splits ? key_at(lane, 0) : 0;
+        if ((int)threadIdx.x < MOST_TOP) sel.list[threadIdx.x] = 0;
+        select_keys(sel, a.top, [&](auto&& take) {
+            for (int i = threadIdx.x; i < splits * a.top; i += LONG_THREADS)
+                if (const uint64_t key = key_at(i / a.top, i % a.top)) take(key);
+        });
+        write_top(a, row, sel.list, m, l);
+    }
+}
+
+struct Slopes {
+    int64_t n;
+    int c;
+    const void* z;
+    int64_t ldz;
+    const void* labels;
+    int wide_labels;
+    const float *stats, *entropy, *dlogp, *dentropy;
+    void* dz;
+    int64_t lddz;
+};
+// LANES lanes a row and a share of its columns (blockIdx.y), V columns a lane and turn.
+template <class T, int V, int LANES>
+__global__ __launch_bounds__(256) void cbm_scores_back_kernel(Slopes a, int turns) {
+    const int lane = threadIdx.x % LANES, pieces = (a.c + V - 1) / V;
+    for (int64_t row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES; row < a.n; row += (int64_t)gridDim.x * (256 / LANES)) {
+        const float m = a.stats[2 * row], l = a.stats[2 * row + 1];
+        const int64_t label = a.dlogp ? label_of(a.labels, a.wide_labels, row) : -1;
+        const bool given = label >= 0 && label < a.c, empty = m == -INFINITY;
+        const float slope = given ? a.dlogp[row] : 0.0f, of_entropy = a.dentropy ? a.dentropy[row] : 0.0f, entropy = a.dentropy ? a.entropy[row] : 0.0f;
+        const T* z_row = (const T*)a.z + row * a.ldz;
+        T* out = (T*)a.dz + row * a.lddz;
+        for (int turn = 0; turn < turns; ++turn) {
+            const int piece = (blockIdx.y * turns + turn) * LANES + lane;
+            if (piece >= pieces) break;
+            const Place<V, false> p(piece, a.c);
+            float x[V];
+            load_piece<V>(x, z_row + p.at);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float log_p = x[j] - m - l, pr = exp_of(log_p);
+                const float own = p.at + j == label ? slope : 0.0f;
+                const float v = own - pr * (slope + of_entropy * (fmaxf(log_p, FAR) + entropy));
+                x[j] = empty ? 0.0f : v;
+            }
+            if (p.seen == 0) {
+                store_piece<V>(out + p.at, x);
+            } else {  // (the other values are another lane's, which may not have read them yet where dz is z)
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (p.counts(j)) out[p.at + j] = (T)x[j];
+            }
+        }
+    }
+}
+
+cbm_status launched(const char* what) {
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess) return CBM_OK;
+    cbm_set_error_detail(what, hipGetErrorString(e));
+    return CBM_ERR_HIP;
+}
+constexpr int SHORT_ROW = 1024;  // columns that a wave keeps in its registers
+
+}  // namespace
+
+// Workgroups that share a row: some for every compute unit, of 1,024 columns at least (one turn of a workgroup is 2,048).
+int cbm_scores_splits(int64_t n, int32_t c) {
+    if (c <= SHORT_ROW || n == 0) return 1;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(MOST_SPLITS, 512 / n), ((int64_t)c + 2047) / 2048));
+}
+size_t cbm_scores_part_bytes(int32_t top) { return sizeof(Part) + (size_t)top * sizeof(uint64_t); }
+
+cbm_status cbm_launch_scores(int64_t n, int32_t c, int32_t type, const void* z, int64_t ldz, const void* labels, int label_bits, float* logp, float* entropy, float* stats, int32_t top,
+                             float* values, int32_t* columns, void* parts, void* stream_) {
+    if (n == 0) return CBM_OK;
+    hipStream_t stream = (hipStream_t)stream_;
+    const Scores a{n, c, z, ldz, labels, label_bits == 64, logp, entropy, stats, top, values, columns};
+    cbm_with_type(type, [&](auto t) {
+        using T = decltype(t);
+        constexpr int V = 16 / (int)sizeof(T);
+        const int pieces = (c + V - 1) / V;
+#define CBM_SCORES(V_, LANES, R) \
+    cbm_scores_kernel<T, V_, LANES, R><<<(unsigned)std::min<int64_t>((n + 256 / LANES - 1) / (256 / LANES), 1 << 23), 256, 0, stream>>>(a)
+        if (c < V) CBM_SCORES(1, 8, 1);
+        else if (pieces <= 4) CBM_SCORES(V, 4, 1);
+        else if (pieces <= 8) CBM_SCORES(V, 8, 1);
+        else if (pieces <= 16) CBM_SCORES(V, 16, 1);
+        else if (pieces <= 32) CBM_SCORES(V, 32, 1);
+        else if (pieces <= 64) CBM_SCORES(V, 64, 1);
+        else if (pieces <= 128) CBM_SCORES(V, 64, 2);
+        else if (c <= SHORT_ROW) CBM_SCORES(V, 64, SHORT_ROW / 64 / V);
+#undef CBM_SCORES
+        else {
+            const int splits = cbm_scores_splits(n, c);
+            int share = ((c + splits - 1) / splits + V - 1) / V * V;
+            const unsigned grid = (unsigned)std::min<int64_t>(n * splits, 1 << 20);
+#define CBM_LONG(R, TOP) cbm_scores_long_kernel<T, V, R, TOP><<<grid, LONG_THREADS, 0, stream>>>(a, splits, share, (char*)parts)
+            if (share <= 2048) top ? CBM_LONG(8 / V, true) : CBM_LONG(8 / V, false);
+            else top ? CBM_LONG(32 / V, true) : CBM_LONG(32 / V, false);
+#undef CBM_LONG
+            if (splits > 1) cbm_scores_join_kernel<T><<<(unsigned)std::min<int64_t>(n, 1 << 20), LONG_THREADS, 0, stream>>>(a, splits, (char*)parts);
+        }
+    });
+    return launched("log probabilities launch");
+}
+
+cbm_status cbm_launch_scores_backward(int64_t n, int32_t c, int32_t type, const void* z, int64_t ldz, const void* labels, int label_bits, const float* stats, const float* entropy,
+                                      const float* dlogp, const float* dentropy, void* dz, int64_t lddz, void* stream_) {
+    if (n == 0) return CBM_OK;
+    hipStream_t stream = (hipStream_t)stream_;
+    const Slopes a{n, c, z, ldz, labels, label_bits == 64, stats, entropy, dlogp, dentropy, dz, lddz};
+    cbm_with_type(type, [&](auto t) {
+        using T = decltype(t);
+        constexpr int V = 16 / (int)sizeof(T);
+        const int64_t pieces = (c + V - 1) / V;
+#define CBM_BACK(V_, LANES)                                                                                                                                                  \
+    {                                                                                                                                                                        \
+        const int turns = pieces <= LANES ? 1 : 4;                                                                                                                           \
+        cbm_scores_back_kernel<T, V_, LANES><<<dim3((unsigned)std::min<int64_t>((n + 256 / LANES - 1) / (256 / LANES), 1 << 23),                                             \
+                                                    (unsigned)((pieces + LANES * turns - 1) / (LANES * turns))), 256, 0, stream>>>(a, turns);                                \
+    }
+        if (c < V) CBM_BACK(1, 8)
+        else if (pieces <= 4) CBM_BACK(V, 4)
+        else if (pieces <= 8) CBM_BACK(V, 8)
+        else if (pieces <= 16) CBM_BACK(V, 16)
+        else if (pieces <= 32) CBM_BACK(V, 32)
+        else CBM_BACK(V, 64)
+#undef CBM_BACK
+    });
+    return launched("log probabilities backward launch");
+}

@@ -61,3 +61,27 @@ def test_weight_and_relu_gradients_are_the_slopes():
     assert (orc.weight_grad(q, e, dy) * v).sum() == pytest.approx(_slope(lambda t: (x @ t * dy).sum(), w, v), rel=1e-7)
     g, u = rng.standard_normal(z.shape), rng.standard_normal(z.shape)
     assert (orc.relu_backward(q, e, g) * u).sum() == pytest.approx(_slope(lambda t: (np.maximum(t, 0) * g).sum(), z, u, 1e-9), rel=1e-5)
+
+
+@pytest.mark.parametrize("n,c", [(1, 2), (4, 7), (3, 50)])
+def test_log_probability_gradient_is_the_slope(n, c):
+    rng = np.random.default_rng(c)
+    z, v = 2 * rng.standard_normal((n, c)), rng.standard_normal((n, c))
+    labels, a, h = rng.integers(-1, c, n), rng.standard_normal(n), rng.standard_normal(n)
+    logp, entropy, stats, _, _ = orc.log_probs(z, labels)
+    dz = orc.log_probs_backward(z, labels, stats, entropy, a, h)
+    loss = lambda t: (orc.log_probs(t, labels)[0] * a + orc.log_probs(t, labels)[1] * h).sum()  # noqa: E731
+    assert (dz * v).sum() == pytest.approx(_slope(loss, z, v), rel=1e-6, abs=1e-8)
+
+
+def test_log_probabilities_by_hand():
+    inf = np.inf
+    z = np.array([[0.0, 0.0, 0.0], [np.log(3.0), 0.0, -inf], [-inf, -inf, -inf], [0.0, np.nan, 1.0], [inf, 0.0, 1.0], [5.0, 5.0, 6.0]])
+    logp, entropy, stats, values, columns = orc.log_probs(z, [1, 0, 2, 0, 3, 7], top=4)
+    assert np.allclose(logp[:2], [-np.log(3), np.log(0.75)]) and logp[2] == -inf and np.isnan(logp[3]) and logp[4] == 0 and logp[5] == 0
+    assert np.allclose(entropy[:3], [np.log(3), np.log(4) - 0.75 * np.log(3), 0]) and np.isnan(entropy[3:5]).all()
+    assert np.allclose(stats[:2], [[0, np.log(3)], [np.log(3), np.log(4 / 3)]]) and (stats[2] == -inf).all() and np.isnan(stats[3:5]).all()
+    assert columns.tolist() == [[0, 1, 2, -1], [0, 1, -1, -1], [-1] * 4, [-1] * 4, [-1] * 4, [2, 0, 1, -1]]
+    assert np.allclose(values[1, :2], np.log([0.75, 0.25])) and (values[1, 2:] == -inf).all() and np.isnan(values[3]).all()
+    dz = orc.log_probs_backward(z[:3], [1, 0, 2], stats[:3], entropy[:3], [1.0, 1.0, 1.0], [0.0, 0.0, 1.0])
+    assert np.allclose(dz, [[-1 / 3, 2 / 3, -1 / 3], [0.25, -0.25, 0], [0, 0, 0]])
