@@ -126,13 +126,18 @@ __global__ __launch_bounds__(256) void cbm_checkpoint_load_kernel(int64_t n, int
 // eight rows, four neighbouring columns of Q and two of dY: 128 columns of Q and 64 of dY by 16 rows a wave, with neither LDS nor transposes, only with columns of dW in
 // an order of their own (tile t has columns 4 i + t of Q, and 2 i + t of dY).  x~ is a bf16 value; dY is split into one, two (fp16) or three (fp32) bf16 values that add
 // up to it, so the products are exact and the sums fp32.  The waves of a workgroup and the workgroups of a tile share the rows; a workgroup adds its waves' sums in LDS, in order.
-constexpr int GRAD_WAVES = 4, GRAD_ROWS = 16, GRAD_K = 128, GRAD_C = 64;
+constexpr int GRAD_WAVES = 8, GRAD_ROWS = 16, GRAD_K = 128, GRAD_C = 64;
 
+enum GradEdge {  // how the last columns of a row are loaded
+    GRAD_WHOLE,    // k is a multiple of 4 and c of 2
+    GRAD_SHIFTED,  // the last load of a row starts earlier, and is shifted
+    GRAD_SINGLE    // k < 4 or c < 2: value by value
+};
 template <class T>
 struct GradStep {  // what a lane has loaded: eight rows
     uint32_t q[8];
-    uint32_t e[8];
-    float y[2][8];
+    uint8_t e[8];
+    T y[8][2];
 };
 template <class T>
 struct GradArgs {
@@ -145,42 +150,33 @@ struct GradArgs {
     const T* dY;
     int64_t lddy;
 };
-template <class T, bool RAGGED>
+// Rows row0 + 8 half .. + 7 (of the last row where there are none), columns k0 .. + 3 of Q and c0, c0 + 1 of dY.
+template <class T, GradEdge EDGE>
 __device__ __forceinline__ void grad_load(GradStep<T>& s, const GradArgs<T>& a, int64_t row0, int k0, int c0, int half) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const int64_t row = row0 + 8 * half + j, at = min(row, a.n - 1);
+        const int64_t at = min(row0 + 8 * half + j, a.n - 1);
         const int8_t* q = a.Q + at * a.ldq;
         const T* y = a.dY + at * a.lddy;
         s.e[j] = a.E[at * a.lde + min(k0, a.k - 1) / BLOCK];
-        if constexpr (RAGGED) {
+        if constexpr (EDGE == GRAD_SINGLE) {
             uint32_t v = 0;
 #pragma unroll
             for (int t = 0; t < 4; ++t) v |= (uint32_t)(uint8_t)q[min(k0 + t, a.k - 1)] << (8 * t);
             s.q[j] = v;
 #pragma unroll
-            for (int t = 0; t < 2; ++t) s.y[t][j] = (float)y[min(c0 + t, a.c - 1)];
+            for (int t = 0; t < 2; ++t) s.y[j][t] = y[min(c0 + t, a.c - 1)];
         } else {
             typedef uint32_t Word __attribute__((aligned(1)));
             s.q[j] = *reinterpret_cast<const Word*>(q + min(k0, a.k - 4));
-            float pair[2];
-            load_piece<2>(pair, y + min(c0, a.c - 2));
-            s.y[0][j] = pair[0];
-            s.y[1][j] = pair[1];
+            const typename Piece<T, 2>::type pair = *reinterpret_cast<const typename Piece<T, 2>::type*>(y + min(c0, a.c - 2));
+            s.y[j][0] = pair[0];
+            s.y[j][1] = pair[1];
         }
-    }
-    if (row0 + GRAD_ROWS > a.n) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (row0 + 8 * half + j >= a.n) {
-                s.q[j] = 0;
-                s.e[j] = 127;
-                s.y[0][j] = s.y[1][j] = 0.0f;
-            }
     }
 }
 
-template <class T, bool RAGGED>
+template <class T, GradEdge EDGE>
 __global__ __launch_bounds__(64 * GRAD_WAVES) void cbm_checkpoint_grad_kernel(GradArgs<T> a, int tiles_c, int tiles, int splits, float* __restrict__ parts, int64_t ldp, int64_t part) {
     constexpr int PARTS = std::is_same<T, float>::value ? 3 : std::is_same<T, _Float16>::value ? 2 : 1;  // 24, 11 and 8 bits, eight a part
     __shared__ float room[2][GRAD_K * GRAD_C];
@@ -200,9 +196,34 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void cbm_checkpoint_grad_kernel(Gr
             for (int v = 0; v < 16; ++v) acc[t][u][v] = 0.0f;
     uint32_t minus_low = 0xbf80u;
     asm("" : "+s"(minus_low));
+    const int late_q = EDGE == GRAD_SHIFTED ? 8 * max(0, min(k0 - (a.k - 4), 3)) : 0;  // bits before the lane's first column in what it loads
+    const bool late_y = EDGE == GRAD_SHIFTED && c0 > a.c - 2;
+    GradStep<T> next;
+    constexpr bool AHEAD = EDGE != GRAD_SINGLE;  // (single values have no registers left for the next step's)
+    if (AHEAD && first + wave < last) grad_load<T, EDGE>(next, a, (first + wave) * GRAD_ROWS, k0, c0, half);
     for (int64_t i = first + wave; i < last; i += GRAD_WAVES) {
-        GradStep<T> s;
-        grad_load<T, RAGGED>(s, a, i * GRAD_ROWS, k0, c0, half);
+        struct {
+            uint32_t q[8];
+            float step[8], y[2][8];
+        } s;
+        if (!AHEAD) grad_load<T, EDGE>(next, a, i * GRAD_ROWS, k0, c0, half);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            s.q[j] = EDGE == GRAD_SHIFTED ? next.q[j] >> late_q : next.q[j];
+            s.step[j] = step_of(next.e[j]);
+            s.y[0][j] = (float)(EDGE == GRAD_SHIFTED && late_y ? next.y[j][1] : next.y[j][0]);
+            s.y[1][j] = (float)next.y[j][1];
+        }
+        if ((i + 1) * GRAD_ROWS > a.n) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (i * GRAD_ROWS + 8 * half + j >= a.n) {
+                    s.q[j] = 0;
+                    s.step[j] = 1.0f;
+                    s.y[0][j] = s.y[1][j] = 0.0f;
+                }
+        }
+        if (AHEAD && i + GRAD_WAVES < last) grad_load<T, EDGE>(next, a, (i + GRAD_WAVES) * GRAD_ROWS, k0, c0, half);
         uintx4 y[2][PARTS];
         if constexpr (PARTS == 1) {
 #pragma unroll
@@ -247,7 +268,7 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void cbm_checkpoint_grad_kernel(Gr
                 for (int i2 = 0; i2 < 2; ++i2) {
                     const int r = 2 * j + i2;
                     const float q = (float)(int8_t)(s.q[r] >> (8 * t));
-                    v[i2] = q * step_of(s.e[r]);  // (NOT_FINITE: 0 times infinity)
+                    v[i2] = q * s.step[r];  // (NOT_FINITE: 0 times infinity)
                 }
                 x[j] = high_halves(v[0], v[1]);
             }
@@ -258,11 +279,12 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void cbm_checkpoint_grad_kernel(Gr
                     acc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y[u][p]), acc[t][u], 0, 0, 0);
         }
     }
-    // the sums of waves 2 and 3 to 0 and 1, then 1 to 0
+    // waves 4 and 5 to 0 and 1, 6 and 7 to 2 and 3, 2 and 3 to 0 and 1, 1 to 0
 #pragma unroll
-    for (int from = 2; from >= 1; --from) {
+    for (int round = 0; round < 4; ++round) {
+        const int from = round == 0 ? 4 : round == 1 ? 6 : round == 2 ? 2 : 1, to = round == 1 ? 2 : 0, count = round == 3 ? 1 : 2;
         __syncthreads();
-        if (wave >= from && wave < 2 * from) {
+        if (wave >= from && wave < from + count) {
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -271,13 +293,13 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void cbm_checkpoint_grad_kernel(Gr
                     for (int v = 0; v < 16; ++v) room[wave - from][((t * 2 + u) * 16 + v) * 64 + lane] = acc[t][u][v];
         }
         __syncthreads();
-        if (wave < from) {
+        if (wave >= to && wave < to + count) {
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) acc[t][u][v] += room[wave][((t * 2 + u) * 16 + v) * 64 + lane];
+                    for (int v = 0; v < 16; ++v) acc[t][u][v] += room[wave - to][((t * 2 + u) * 16 + v) * 64 + lane];
         }
     }
     if (wave) return;
@@ -340,7 +362,7 @@ void along_rows(int64_t n, int64_t pieces, F&& f) {
 
 int64_t cbm_grad_splits(int64_t n, int32_t k, int32_t c) {
     const int64_t tiles = ((int64_t)k + GRAD_K - 1) / GRAD_K * (((int64_t)c + GRAD_C - 1) / GRAD_C);
-    return std::max<int64_t>(1, std::min<int64_t>((512 + tiles - 1) / tiles, (n + GRAD_WAVES * GRAD_ROWS - 1) / (GRAD_WAVES * GRAD_ROWS)));
+    return std::max<int64_t>(1, std::min<int64_t>((256 + tiles - 1) / tiles, (n + 4 * GRAD_ROWS - 1) / (4 * GRAD_ROWS)));
 }
 
 cbm_status cbm_launch_checkpoint_save(int64_t n, int32_t k, int32_t type, const void* X, int64_t ldx, int8_t* Q, int64_t ldq, uint8_t* E, int64_t lde, void* stream) {
@@ -384,8 +406,9 @@ cbm_status cbm_launch_checkpoint_grad(int64_t n, int32_t k, int32_t c, const int
             const GradArgs<T> a{n, k, c, Q, ldq, E, lde, (const T*)dY, lddy};
             float* to = splits == 1 ? dW : parts;
             const int64_t ldp = splits == 1 ? lddw : c;
-            if (k % 4 || c % 2) cbm_checkpoint_grad_kernel<T, true><<<grid, 64 * GRAD_WAVES, 0, stream>>>(a, tiles_c, tiles, splits, to, ldp, size);
-            else cbm_checkpoint_grad_kernel<T, false><<<grid, 64 * GRAD_WAVES, 0, stream>>>(a, tiles_c, tiles, splits, to, ldp, size);
+            if (k < 4 || c < 2) cbm_checkpoint_grad_kernel<T, GRAD_SINGLE><<<grid, 64 * GRAD_WAVES, 0, stream>>>(a, tiles_c, tiles, splits, to, ldp, size);
+            else if (k % 4 || c % 2) cbm_checkpoint_grad_kernel<T, GRAD_SHIFTED><<<grid, 64 * GRAD_WAVES, 0, stream>>>(a, tiles_c, tiles, splits, to, ldp, size);
+            else cbm_checkpoint_grad_kernel<T, GRAD_WHOLE><<<grid, 64 * GRAD_WAVES, 0, stream>>>(a, tiles_c, tiles, splits, to, ldp, size);
         });
     if (splits != 1) cbm_checkpoint_join_kernel<<<(unsigned)std::min<int64_t>((size + 31) / 32, 1 << 20), 1024, 0, stream>>>(splits, size, c, parts, dW, lddw);
     return launched("checkpoint gradient launch");
