@@ -131,7 +131,7 @@ constexpr int GRAD_WAVES = 8, GRAD_ROWS = 16, GRAD_K = 128, GRAD_C = 64;
 enum GradEdge {  // how the last columns of a row are loaded
     GRAD_WHOLE,    // k is a multiple of 4 and c of 2
     GRAD_SHIFTED,  // the last load of a row starts earlier, and is shifted
-    GRAD_SINGLE    // k < 4 or c < 2: value by value
+    GRAD_SINGLE    // k < 4 or c < 2, or strides so long that eight rows are not within 32 bits: value by value
 };
 template <class T>
 struct GradStep {  // what a lane has loaded: eight rows
@@ -173,17 +173,34 @@ __device__ __forceinline__ void grad_load(GradStep<T>& s, const GradArgs<T>& a, 
             s.y[j][0] = pair[0];
             s.y[j][1] = pair[1];
         }
+        __builtin_amdgcn_sched_barrier(0);  // (a row's addresses at a time: registers)
+    }
+}
+
+// The same for rows that are all there, with what all lanes share of an address in scalar registers and a lane's own 32 bits beside it (64-bit products of a row and
+// a stride for each load of each lane took more time than everything else).
+template <class T>
+__device__ __forceinline__ void grad_load_whole(GradStep<T>& s, const GradArgs<T>& a, int64_t row0, uint32_t of_q, uint32_t of_e, uint32_t of_y) {
+    const char *q = (const char*)a.Q + row0 * a.ldq, *e = (const char*)a.E + row0 * a.lde, *y = (const char*)(a.dY + row0 * a.lddy);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        typedef uint32_t Word __attribute__((aligned(1)));
+        s.q[j] = *reinterpret_cast<const Word*>(q + j * (uint32_t)a.ldq + of_q);
+        s.e[j] = *reinterpret_cast<const uint8_t*>(e + j * (uint32_t)a.lde + of_e);
+        const typename Piece<T, 2>::type pair = *reinterpret_cast<const typename Piece<T, 2>::type*>(y + j * (uint32_t)(a.lddy * sizeof(T)) + of_y);
+        s.y[j][0] = pair[0];
+        s.y[j][1] = pair[1];
     }
 }
 
 template <class T, GradEdge EDGE>
 __global__ __launch_bounds__(64 * GRAD_WAVES) void cbm_checkpoint_grad_kernel(GradArgs<T> a, int tiles_c, int tiles, int splits, float* __restrict__ parts, int64_t ldp, int64_t part) {
     constexpr int PARTS = std::is_same<T, float>::value ? 3 : std::is_same<T, _Float16>::value ? 2 : 1;  // 24, 11 and 8 bits, eight a part
-    __shared__ float room[2][GRAD_K * GRAD_C];
+    __shared__ floatx2 room[GRAD_WAVES * 2 * 8 * 64];
     // consecutive workgroups run on different XCDs: the tiles of one share of the rows are eight apart, on one XCD, where there are so many shares
     const int b = blockIdx.x, beside = min(CBM_XCD, splits), split = b / (beside * tiles) * beside + b % beside, tile = b / beside % tiles;
     if (split >= splits) return;
-    const int lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x / 64;
+    const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int k0 = tile / tiles_c * GRAD_K + 4 * (lane & 31), c0 = tile % tiles_c * GRAD_C + 2 * (lane & 31);
     const int64_t steps = (a.n + GRAD_ROWS - 1) / GRAD_ROWS;
     const int64_t first = steps * split / splits, last = steps * (split + 1) / splits;
@@ -198,15 +215,21 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void cbm_checkpoint_grad_kernel(Gr
     asm("" : "+s"(minus_low));
     const int late_q = EDGE == GRAD_SHIFTED ? 8 * max(0, min(k0 - (a.k - 4), 3)) : 0;  // bits before the lane's first column in what it loads
     const bool late_y = EDGE == GRAD_SHIFTED && c0 > a.c - 2;
+    const uint32_t of_q = (uint32_t)(8 * half * a.ldq + min(k0, a.k - 4)), of_e = (uint32_t)(8 * half * a.lde + min(k0, a.k - 1) / BLOCK),
+                   of_y = (uint32_t)((8 * half * a.lddy + min(c0, a.c - 2)) * (int64_t)sizeof(T));
     GradStep<T> next;
+    auto load = [&](int64_t step) {
+        if (EDGE == GRAD_SINGLE || (step + 1) * GRAD_ROWS > a.n) grad_load<T, EDGE>(next, a, step * GRAD_ROWS, k0, c0, half);
+        else grad_load_whole<T>(next, a, step * GRAD_ROWS, of_q, of_e, of_y);
+    };
     constexpr bool AHEAD = EDGE != GRAD_SINGLE;  // (single values have no registers left for the next step's)
-    if (AHEAD && first + wave < last) grad_load<T, EDGE>(next, a, (first + wave) * GRAD_ROWS, k0, c0, half);
+    if (AHEAD && first + wave < last) load(first + wave);
     for (int64_t i = first + wave; i < last; i += GRAD_WAVES) {
         struct {
             uint32_t q[8];
             float step[8], y[2][8];
         } s;
-        if (!AHEAD) grad_load<T, EDGE>(next, a, i * GRAD_ROWS, k0, c0, half);
+        if (!AHEAD) load(i);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             s.q[j] = EDGE == GRAD_SHIFTED ? next.q[j] >> late_q : next.q[j];
@@ -223,7 +246,7 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void cbm_checkpoint_grad_kernel(Gr
                     s.y[0][j] = s.y[1][j] = 0.0f;
                 }
         }
-        if (AHEAD && i + GRAD_WAVES < last) grad_load<T, EDGE>(next, a, (i + GRAD_WAVES) * GRAD_ROWS, k0, c0, half);
+        if (AHEAD && i + GRAD_WAVES < last) load(i + GRAD_WAVES);
         uintx4 y[2][PARTS];
         if constexpr (PARTS == 1) {
 #pragma unroll
@@ -279,40 +302,37 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void cbm_checkpoint_grad_kernel(Gr
                     acc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y[u][p]), acc[t][u], 0, 0, 0);
         }
     }
-    // waves 4 and 5 to 0 and 1, 6 and 7 to 2 and 3, 2 and 3 to 0 and 1, 1 to 0
-#pragma unroll
-    for (int round = 0; round < 4; ++round) {
-        const int from = round == 0 ? 4 : round == 1 ? 6 : round == 2 ? 2 : 1, to = round == 1 ? 2 : 0, count = round == 3 ? 1 : 2;
-        __syncthreads();
-        if (wave >= from && wave < from + count) {
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) room[wave - from][((t * 2 + u) * 16 + v) * 64 + lane] = acc[t][u][v];
-        }
-        __syncthreads();
-        if (wave >= to && wave < to + count) {
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) acc[t][u][v] += room[wave - to][((t * 2 + u) * 16 + v) * 64 + lane];
-        }
-    }
-    if (wave) return;
+    // The waves' sums, a tile of Q's columns at a time: every wave writes its own, then every thread adds two rows of two neighbouring columns.
     float* out = parts + split * part;
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < 4; ++t) {
+        __syncthreads();
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int row = tile / tiles_c * GRAD_K + 4 * (8 * (v / 4) + 4 * half + v % 4) + t, column = c0 + u;
-                if (row < a.k && column < a.c) out[(int64_t)row * ldp + column] = acc[t][u][v];
+            for (int v = 0; v < 8; ++v) room[((wave * 2 + u) * 8 + v) * 64 + lane] = floatx2{acc[t][u][2 * v], acc[t][u][2 * v + 1]};
+        __syncthreads();
+        floatx2 sum[2] = {};
+#pragma unroll
+        for (int w = 0; w < GRAD_WAVES; ++w)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const floatx2 x = room[((w * 2 + u) * 8 + wave) * 64 + lane];
+                sum[u][0] += x[0];
+                sum[u][1] += x[1];
             }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int v = 2 * wave + i, row = tile / tiles_c * GRAD_K + 4 * (8 * (v / 4) + 4 * half + v % 4) + t;
+            float* to = out + (int64_t)row * ldp + c0;
+            if (row < a.k && c0 + 1 < a.c) {
+                const float both[2] = {sum[0][i], sum[1][i]};
+                store_piece<2>(to, both);
+            } else if (row < a.k && c0 < a.c) {
+                *to = sum[0][i];
+            }
+        }
+    }
 }
 
 // dW from `count` partial sums, in order: 32 values a workgroup, the partial sums shared by its 32 groups of lanes.
@@ -406,7 +426,8 @@ cbm_status cbm_launch_checkpoint_grad(int64_t n, int32_t k, int32_t c, const int
             const GradArgs<T> a{n, k, c, Q, ldq, E, lde, (const T*)dY, lddy};
             float* to = splits == 1 ? dW : parts;
             const int64_t ldp = splits == 1 ? lddw : c;
-            if (k < 4 || c < 2) cbm_checkpoint_grad_kernel<T, GRAD_SINGLE><<<grid, 64 * GRAD_WAVES, 0, stream>>>(a, tiles_c, tiles, splits, to, ldp, size);
+            const int64_t far = std::max(std::max(ldq, lde), lddy * (int64_t)sizeof(T));
+            if (k < 4 || c < 2 || far >= 1 << 27) cbm_checkpoint_grad_kernel<T, GRAD_SINGLE><<<grid, 64 * GRAD_WAVES, 0, stream>>>(a, tiles_c, tiles, splits, to, ldp, size);
             else if (k % 4 || c % 2) cbm_checkpoint_grad_kernel<T, GRAD_SHIFTED><<<grid, 64 * GRAD_WAVES, 0, stream>>>(a, tiles_c, tiles, splits, to, ldp, size);
             else cbm_checkpoint_grad_kernel<T, GRAD_WHOLE><<<grid, 64 * GRAD_WAVES, 0, stream>>>(a, tiles_c, tiles, splits, to, ldp, size);
         });
