@@ -136,8 +136,8 @@ enum GradEdge {  // how the last columns of a row are loaded
 template <class T>
 struct GradStep {  // what a lane has loaded: eight rows
     uint32_t q[8];
-    uint8_t e[8];
     T y[8][2];
+    uint8_t e;  // of row lane / 4 of the sixteen, and block lane % 4 of the 128 columns
 };
 template <class T>
 struct GradArgs {
@@ -152,13 +152,13 @@ struct GradArgs {
 };
 // Rows row0 + 8 half .. + 7 (of the last row where there are none), columns k0 .. + 3 of Q and c0, c0 + 1 of dY.
 template <class T, GradEdge EDGE>
-__device__ __forceinline__ void grad_load(GradStep<T>& s, const GradArgs<T>& a, int64_t row0, int k0, int c0, int half) {
+__device__ __forceinline__ void grad_load(GradStep<T>& s, const GradArgs<T>& a, int64_t row0, int k0, int c0, int half, int block) {
+    s.e = a.E[min(row0 + (int)(threadIdx.x & 63) / 4, a.n - 1) * a.lde + block];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const int64_t at = min(row0 + 8 * half + j, a.n - 1);
         const int8_t* q = a.Q + at * a.ldq;
         const T* y = a.dY + at * a.lddy;
-        s.e[j] = a.E[at * a.lde + min(k0, a.k - 1) / BLOCK];
         if constexpr (EDGE == GRAD_SINGLE) {
             uint32_t v = 0;
 #pragma unroll
@@ -182,11 +182,11 @@ __device__ __forceinline__ void grad_load(GradStep<T>& s, const GradArgs<T>& a, 
 template <class T>
 __device__ __forceinline__ void grad_load_whole(GradStep<T>& s, const GradArgs<T>& a, int64_t row0, uint32_t of_q, uint32_t of_e, uint32_t of_y) {
     const char *q = (const char*)a.Q + row0 * a.ldq, *e = (const char*)a.E + row0 * a.lde, *y = (const char*)(a.dY + row0 * a.lddy);
+    s.e = *reinterpret_cast<const uint8_t*>(e + of_e);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         typedef uint32_t Word __attribute__((aligned(1)));
         s.q[j] = *reinterpret_cast<const Word*>(q + j * (uint32_t)a.ldq + of_q);
-        s.e[j] = *reinterpret_cast<const uint8_t*>(e + j * (uint32_t)a.lde + of_e);
         const typename Piece<T, 2>::type pair = *reinterpret_cast<const typename Piece<T, 2>::type*>(y + j * (uint32_t)(a.lddy * sizeof(T)) + of_y);
         s.y[j][0] = pair[0];
         s.y[j][1] = pair[1];
@@ -215,11 +215,12 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void cbm_checkpoint_grad_kernel(Gr
     asm("" : "+s"(minus_low));
     const int late_q = EDGE == GRAD_SHIFTED ? 8 * max(0, min(k0 - (a.k - 4), 3)) : 0;  // bits before the lane's first column in what it loads
     const bool late_y = EDGE == GRAD_SHIFTED && c0 > a.c - 2;
-    const uint32_t of_q = (uint32_t)(8 * half * a.ldq + min(k0, a.k - 4)), of_e = (uint32_t)(8 * half * a.lde + min(k0, a.k - 1) / BLOCK),
+    const int block = min(tile / tiles_c * (GRAD_K / BLOCK) + (lane & 3), (a.k + BLOCK - 1) / BLOCK - 1), from = (32 * half + (lane & 31) / 8) * 4;
+    const uint32_t of_q = (uint32_t)(8 * half * a.ldq + min(k0, a.k - 4)), of_e = (uint32_t)(lane / 4 * a.lde + block),
                    of_y = (uint32_t)((8 * half * a.lddy + min(c0, a.c - 2)) * (int64_t)sizeof(T));
     GradStep<T> next;
     auto load = [&](int64_t step) {
-        if (EDGE == GRAD_SINGLE || (step + 1) * GRAD_ROWS > a.n) grad_load<T, EDGE>(next, a, step * GRAD_ROWS, k0, c0, half);
+        if (EDGE == GRAD_SINGLE || (step + 1) * GRAD_ROWS > a.n) grad_load<T, EDGE>(next, a, step * GRAD_ROWS, k0, c0, half, block);
         else grad_load_whole<T>(next, a, step * GRAD_ROWS, of_q, of_e, of_y);
     };
     constexpr bool AHEAD = EDGE != GRAD_SINGLE;  // (single values have no registers left for the next step's)
@@ -233,7 +234,7 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void cbm_checkpoint_grad_kernel(Gr
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             s.q[j] = EDGE == GRAD_SHIFTED ? next.q[j] >> late_q : next.q[j];
-            s.step[j] = step_of(next.e[j]);
+            s.step[j] = step_of(__builtin_amdgcn_ds_bpermute(from + 16 * j, (int)next.e));
             s.y[0][j] = (float)(EDGE == GRAD_SHIFTED && late_y ? next.y[j][1] : next.y[j][0]);
             s.y[1][j] = (float)next.y[j][1];
         }
