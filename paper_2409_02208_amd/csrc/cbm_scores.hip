@@ -156,16 +156,17 @@ __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
     }
 }
 
-// The `top` largest keys of a workgroup of LONG_THREADS.  `head`: 64 keys that are in the collection, at most one of each of 64 parts of it, so that its top-th largest
-// bounds the answer from below; keys of at least that are collected, with those found before, and ranked by counting.
+// The `top` largest keys of a workgroup of LONG_THREADS.  `head`: a key of each of 64 parts of the collection that is no larger than the largest there, so that the top-th
+// largest head bounds the answer from below (VALUES: only its value does); keys of at least that are collected, with those of `list`, and ranked by counting.
+// VALUES: gives up, and returns false, where there is no room for them; otherwise the caller's parts are so small that there is.
 template <int CAP>
 struct Select {
     uint64_t head[64], list[MOST_TOP], found[CAP];
     uint64_t bound;
     int count;
 };
-template <int CAP, class F>
-__device__ __forceinline__ void select_keys(Select<CAP>& s, int top, F&& each) {
+template <bool VALUES, int CAP, class F>
+__device__ __forceinline__ bool select_keys(Select<CAP>& s, int top, F&& each) {
     __syncthreads();
     if (threadIdx.x < 64) {
         const uint64_t mine = s.head[threadIdx.x];
@@ -176,18 +177,22 @@ __device__ __forceinline__ void select_keys(Select<CAP>& s, int top, F&& each) {
             rank += other > mine;
             there += other != 0;
         }
-        if (there < top ? threadIdx.x == 0 : mine && rank == top - 1) s.bound = there < top ? 1 : mine;
+        if (there < top ? threadIdx.x == 0 : mine && rank == top - 1) s.bound = there < top ? 1 : VALUES ? mine >> 32 << 32 : mine;
         if (threadIdx.x == 0) s.count = 0;
     }
     __syncthreads();
+    const uint64_t bound = s.bound;
     auto take = [&](uint64_t key) {
-        if (key >= s.bound) s.found[atomicAdd(&s.count, 1)] = key;
+        if (key < bound) return;
+        const int at = atomicAdd(&s.count, 1);
+        if (!VALUES || at < CAP) s.found[at] = key;
     };
     each(take);
-    if (threadIdx.x < top) take(s.list[threadIdx.x]);
+    if (!VALUES && (int)threadIdx.x < top) take(s.list[threadIdx.x]);
     __syncthreads();
     const int count = s.count;
-    if (threadIdx.x < top) s.list[threadIdx.x] = 0;
+    if (VALUES && count > CAP) return false;
+    if ((int)threadIdx.x < top) s.list[threadIdx.x] = 0;
     __syncthreads();
     for (int i = threadIdx.x; i < count; i += LONG_THREADS) {
         const uint64_t mine = s.found[i];
@@ -196,6 +201,7 @@ __device__ __forceinline__ void select_keys(Select<CAP>& s, int top, F&& each) {
         if (rank < top) s.list[rank] = mine;  // (keys differ, so do ranks)
     }
     __syncthreads();
+    return true;
 }
 
 __device__ __forceinline__ void write_top(const Scores& a, int64_t row, const uint64_t* list, float m, float l) {
@@ -219,10 +225,13 @@ __device__ __forceinline__ void join_wave(float& m, float& s, float& t) {
     m = all;
 }
 
-// A workgroup a row, or a share of `columns` of its columns (a multiple of V); R pieces of V columns a lane and turn.
+// A workgroup a row, or a share of `columns` of its columns (a multiple of V); R pieces of V columns a lane and turn.  The alternatives come last: of what each four lanes
+// have met, the maximum is known by then; the top-th largest of these 64 bounds the answer from below, the few lanes that hold as much look through their columns
+// once more (out of L2, most likely), and what they find is ranked.  Where that is more than there is room for (equal scores, or orders that leave the largest
+// to a few lanes), all columns are gone through again in turns of one piece a lane, each of which adds to the list what exceeds it.
 template <class T, int V, int R, bool TOP>
 __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_long_kernel(Scores a, int splits, int columns, char* __restrict__ parts) {
-    constexpr int TURN = LONG_THREADS * R * V, CAP = TOP ? MOST_TOP * 4 * R * V + MOST_TOP : 1;
+    constexpr int TURN = LONG_THREADS * R * V, CAP = TOP ? MOST_TOP * 4 * V + MOST_TOP : 1;
     __shared__ Select<CAP> sel;
     __shared__ float room[3][LONG_THREADS / 64];
     const int wave = threadIdx.x / 64;
@@ -232,11 +241,6 @@ __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_long_kernel(Scores a,
         const T* z_row = (const T*)a.z + row * a.ldz;
         const int begin = split * columns, end = min(begin + columns, a.c);
         float m = -INFINITY, s = 0.0f, t = 0.0f;
-        float least = -INFINITY;  // the last of the alternatives so far; a later column has to exceed it
-        if constexpr (TOP) {
-            __syncthreads();
-            if ((int)threadIdx.x < MOST_TOP) sel.list[threadIdx.x] = 0;
-        }
         for (int turn = begin; turn < end; turn += TURN) {
             float x[R][V], most = -INFINITY;
 #pragma unroll
@@ -272,45 +276,21 @@ __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_long_kernel(Scores a,
                     s += e;
                     t += e * fmaxf(d, FAR);
                 }
-            if constexpr (TOP) {
-                if (!__syncthreads_or(most > least)) continue;
-                // the best key of each lane, and of each four lanes
-                int column = 0;
-#pragma unroll
-                for (int i = R - 1; i >= 0; --i) {
-                    const Place<V, false> p(turn / V + i * LONG_THREADS + threadIdx.x, a.c);
-#pragma unroll
-                    for (int j = V - 1; j >= 0; --j) column = x[i][j] == most ? p.at + j : column;
-                }
-                const uint64_t mine = most > least ? key_of(ordered(most), column) : 0;
-                uint64_t best = mine;
-#pragma unroll
-                for (int step = 1; step <= 2; step *= 2) {
-                    const uint64_t other = (uint64_t)__shfl_xor((unsigned long long)best, step);
-                    best = other > best ? other : best;
-                }
-                if (threadIdx.x % 4 == 0) sel.head[threadIdx.x / 4] = best;
-                select_keys(sel, a.top, [&](auto&& take) {
-                    if (mine < sel.bound) return;  // (0 < 1 <= bound)
-                    float before = least;
-                    asm("" : "+v"(before));  // (compared anew: what the first comparisons gave is more than the scalar registers hold)
-#pragma unroll
-                    for (int i = 0; i < R; ++i) {
-                        const Place<V, false> p(turn / V + i * LONG_THREADS + threadIdx.x, a.c);
-#pragma unroll
-                        for (int j = 0; j < V; ++j) take(x[i][j] > before ? key_of(ordered(x[i][j]), p.at + j) : 0);
-                    }
-                });
-                const uint64_t last = sel.list[a.top - 1];
-                least = last ? in_order((uint32_t)(last >> 32)) : -INFINITY;
-            }
         }
+        const float best = m;  // of this lane's columns
         join_wave(m, s, t);
         __syncthreads();
         if ((threadIdx.x & 63) == 0) {
             room[0][wave] = m;
             room[1][wave] = s;
             room[2][wave] = t;
+        }
+        if constexpr (TOP) {  // a key for each four lanes: its value, and a number that tells equal ones apart
+            float four = best;
+            four = fmaxf(four, lane_other<1>(four));
+            four = fmaxf(four, lane_other<2>(four));
+            if (threadIdx.x % 4 == 0) sel.head[threadIdx.x / 4] = key_of(ordered(four), threadIdx.x / 4);
+            if ((int)threadIdx.x < MOST_TOP) sel.list[threadIdx.x] = 0;
         }
         __syncthreads();
         const int w = min((int)threadIdx.x & 63, LONG_THREADS / 64 - 1);
@@ -319,6 +299,45 @@ __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_long_kernel(Scores a,
         s = first ? room[1][w] : 0.0f;
         t = first ? room[2][w] : 0.0f;
         join_wave(m, s, t);
+        if constexpr (TOP) {
+            // f(value, column) for the lane's columns that count, of the piece `piece`
+            auto scan = [&](int piece, auto&& f) {
+                if (piece * V >= end) return;
+                const Place<V, false> p(piece, a.c);
+                float x[V];
+                load_piece<V>(x, z_row + p.at);
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (p.counts(j)) f(x[j], p.at + j);
+            };
+            const bool done = select_keys<true>(sel, a.top, [&](auto&& take) {
+                if (ordered(best) < (uint32_t)(sel.bound >> 32)) return;
+                for (int piece = begin / V + threadIdx.x; piece * V < end; piece += LONG_THREADS) scan(piece, [&](float v, int column) { take(key_of(ordered(v), column)); });
+            });
+            if (!done) {
+                float least = -INFINITY;  // the last of the alternatives so far; a later column has to exceed it
+                for (int turn = begin / V; turn * V < end; turn += LONG_THREADS) {
+                    uint64_t mine = 0;
+                    scan(turn + threadIdx.x, [&](float v, int column) {
+                        const uint64_t key = v > least ? key_of(ordered(v), column) : 0;
+                        mine = key > mine ? key : mine;
+                    });
+                    if (!__syncthreads_or(mine != 0)) continue;
+                    uint64_t four = mine;
+#pragma unroll
+                    for (int step = 1; step <= 2; step *= 2) {
+                        const uint64_t other = (uint64_t)__shfl_xor((unsigned long long)four, step);
+                        four = other > four ? other : four;
+                    }
+                    if (threadIdx.x % 4 == 0) sel.head[threadIdx.x / 4] = four;
+                    select_keys<false>(sel, a.top, [&](auto&& take) {
+                        if (mine >= sel.bound) scan(turn + threadIdx.x, [&](float v, int column) { take(v > least ? key_of(ordered(v), column) : 0); });  // (0 < 1 <= bound)
+                    });
+                    const uint64_t last = sel.list[a.top - 1];
+                    least = last ? in_order((uint32_t)(last >> 32)) : -INFINITY;
+                }
+            }
+        }
         if (splits > 1) {
             char* part = part_at(parts, item, a.top);
             if (threadIdx.x == 0) *(Part*)part = Part{m, s, t, 0.0f};
@@ -358,7 +377,7 @@ __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_join_kernel(Scores a,
         __syncthreads();
         if (threadIdx.x < 64) sel.head[lane] = lane < splits ? key_at(lane, 0) : 0;
         if ((int)threadIdx.x < MOST_TOP) sel.list[threadIdx.x] = 0;
-        select_keys(sel, a.top, [&](auto&& take) {
+        select_keys<false>(sel, a.top, [&](auto&& take) {
             for (int i = threadIdx.x; i < splits * a.top; i += LONG_THREADS)
                 if (const uint64_t key = key_at(i / a.top, i % a.top)) take(key);
         });
