@@ -122,36 +122,134 @@ __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
         finish(m, s, t, l, entropy);
         if (lane == 0 && row < a.n) write_row(a, row, m, l, entropy, at_label, given);
         if (!a.top) continue;
-        uint32_t o[R][V];
+        const bool none = m != m;  // of the row's scores is an alternative
+        float* values = a.values + at * a.top;
+        int32_t* columns = a.columns + at * a.top;
+        if constexpr (R == 1 && sizeof(T) == 2) {
+            // A value's 16 bits in order, then its column from behind, make one whole number; every lane's in descending order, then `top` times the largest head.
+            uint32_t key[V];
+            const int at0 = Place<V, false>(lane, a.c).at;
 #pragma unroll
-        for (int i = 0; i < R; ++i)
+            for (int j = 0; j < V; ++j) {
+                const uint32_t u = __builtin_bit_cast(uint16_t, (T)(x[0][j] + 0.0f));
+                key[j] = !none && x[0][j] > -INFINITY ? (u ^ (u & 0x8000u ? 0xffffu : 0x8000u)) << 16 | (0xffffu - (uint32_t)(at0 + j)) : 0u;
+            }
 #pragma unroll
-            for (int j = 0; j < V; ++j) o[i][j] = m == m ? ordered(x[i][j]) : 0u;
-        for (int r = 0; r < a.top; ++r) {  // the largest, then the lowest column that has it, then without that one
-            uint32_t best = 0;
+            for (int round = 0; round < V; ++round)
 #pragma unroll
-            for (int i = 0; i < R; ++i)
+                for (int j = round % 2; j + 1 < V; j += 2) {
+                    const uint32_t first = max(key[j], key[j + 1]), second = min(key[j], key[j + 1]);
+                    key[j] = first, key[j + 1] = second;
+                }
+            for (int r = 0; r < a.top; ++r) {
+                const uint32_t best = lanes_max<LANES>(key[0]);
+                const bool mine = key[0] == best;
+                if ((best ? mine : lane == 0) && row < a.n) {
+                    const uint32_t o = best >> 16, u = o ^ (o & 0x8000u ? 0x8000u : 0xffffu);
+                    values[r] = none ? NAN : best ? (float)__builtin_bit_cast(T, (uint16_t)u) - m - l : -INFINITY;
+                    columns[r] = best ? (int32_t)(0xffffu - (best & 0xffffu)) : -1;
+                }
 #pragma unroll
-                for (int j = 0; j < V; ++j) best = max(best, o[i][j]);
-            best = lanes_max<LANES>(best);
-            uint32_t column = 0xffffffffu;
+                for (int j = 0; j < V; ++j) {
+                    const uint32_t stays = key[j], comes = j + 1 < V ? +key[j + 1] : 0u;  // (values: a choice of places would become an index)
+                    key[j] = mine ? comes : stays;
+                }
+            }
+        } else if constexpr (R == 1) {
+            // Every lane's values in descending order (neighbours change places only where the later one is larger, so the lower column stays first), then `top` times the
+            // largest head: of equal ones the first lane's, whose columns are lower.
+            float v[V];
+            int which[V];
+            const int at0 = Place<V, false>(lane, a.c).at;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                v[j] = none ? -INFINITY : x[0][j];
+                which[j] = j;
+            }
+#pragma unroll
+            for (int round = 0; round < V; ++round)
+#pragma unroll
+                for (int j = round % 2; j + 1 < V; j += 2) {
+                    const bool change = v[j] < v[j + 1];
+                    const float first = fmaxf(v[j], v[j + 1]), second = fminf(v[j], v[j + 1]);
+                    const int here = which[j], next = which[j + 1];  // (values: a choice of places would become an index)
+                    const int w1 = change ? next : here, w2 = change ? here : next;
+                    v[j] = first, v[j + 1] = second, which[j] = w1, which[j + 1] = w2;
+                }
+            const uint64_t group = (LANES == 64 ? ~0ull : (1ull << LANES) - 1) << (threadIdx.x & 63 & ~(LANES - 1));
+            for (int r = 0; r < a.top; ++r) {
+                const float best = lanes_max<LANES>(v[0]);
+                const uint64_t have = __ballot(v[0] == best) & group;
+                const bool mine = __builtin_amdgcn_mbcnt_hi((uint32_t)(have >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)have, 0)) == 0 && v[0] == best;
+                if (mine && row < a.n) {
+                    values[r] = none ? NAN : best == -INFINITY ? best : best - m - l;
+                    columns[r] = best == -INFINITY ? -1 : at0 + which[0];
+                }
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float stays = v[j], comes = j + 1 < V ? +v[j + 1] : -INFINITY;
+                    const int w1 = which[j], w2 = which[j + 1 < V ? j + 1 : j];
+                    v[j] = mine ? comes : stays;
+                    which[j] = mine ? w2 : w1;
+                }
+            }
+        } else {
+            // As for a long row: the top-th largest of the lanes' largest bounds the answer from below; what is as large is collected and ranked by counting.
+            static_assert(R == 1 || LANES == 64, "");
+            __shared__ uint64_t room[256 / 64][MOST_TOP * R * V];  // (in at most `top` lanes)
+            uint64_t* found = room[threadIdx.x / 64];
+            float most = -INFINITY;
+            int column = 0;
 #pragma unroll
             for (int i = R - 1; i >= 0; --i) {
                 const Place<V, false> p(i * LANES + lane, a.c);
 #pragma unroll
-                for (int j = V - 1; j >= 0; --j) column = o[i][j] == best ? (uint32_t)(p.at + j) : column;
+                for (int j = V - 1; j >= 0; --j) {
+                    column = x[i][j] >= most ? p.at + j : column;
+                    most = fmaxf(most, x[i][j]);
+                }
             }
-            column = best ? ~lanes_max<LANES>(~column) : 0xffffffffu;
+            const uint64_t mine = none ? 0 : key_of(ordered(most), column);
+            const int there = __popcll(__ballot(mine != 0));
+            uint64_t bound = 1;
+            if (there >= a.top) {
+                int rank = 0;
+#pragma unroll 8
+                for (int i = 0; i < 64; ++i) {
+                    const uint64_t other = (uint64_t)__builtin_amdgcn_readlane((uint32_t)(mine >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((uint32_t)mine, i);
+                    rank += other > mine;
+                }
+                const int last = __ffsll((unsigned long long)__ballot(mine && rank == a.top - 1)) - 1;
+                bound = (uint64_t)__builtin_amdgcn_readlane((uint32_t)(mine >> 32), last) << 32 | (uint32_t)__builtin_amdgcn_readlane((uint32_t)mine, last);
+            }
+            int count = 0;
 #pragma unroll
             for (int i = 0; i < R; ++i) {
                 const Place<V, false> p(i * LANES + lane, a.c);
 #pragma unroll
-                for (int j = 0; j < V; ++j) o[i][j] = (uint32_t)(p.at + j) == column ? 0u : o[i][j];
+                for (int j = 0; j < V; ++j) {
+                    const uint32_t o = none ? 0 : ordered(x[i][j]);
+                    if (!__any(o >= (uint32_t)(bound >> 32) && o)) continue;
+                    const uint64_t key = key_of(o, p.at + j), takes = __ballot(key >= bound);
+                    if (key >= bound) found[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(takes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)takes, 0))] = key;
+                    count += __popcll(takes);
+                }
             }
-            if (lane == 0 && row < a.n) {
-                a.values[row * a.top + r] = m != m ? m : best ? in_order(best) - m - l : -INFINITY;
-                a.columns[row * a.top + r] = (int32_t)column;
+            __builtin_amdgcn_wave_barrier();
+            for (int i = lane; i < count; i += 64) {
+                const uint64_t key = found[i];
+                int rank = 0;
+                for (int j = 0; j < count; ++j) rank += found[j] > key;
+                if (rank < a.top && row < a.n) {
+                    values[rank] = in_order((uint32_t)(key >> 32)) - m - l;
+                    columns[rank] = (int32_t)~(uint32_t)key;
+                }
             }
+            if (lane >= count && lane < a.top && row < a.n) {
+                values[lane] = none ? NAN : -INFINITY;
+                columns[lane] = -1;
+            }
+            __builtin_amdgcn_wave_barrier();  // (found is the next row's)
         }
     }
 }
@@ -163,7 +261,8 @@ template <int CAP>
 struct Select {
     uint64_t head[64], list[MOST_TOP], found[CAP];
     uint64_t bound;
-    int count;
+    int count, lanes;
+    uint16_t lane[LONG_THREADS];
 };
 template <bool VALUES, int CAP, class F>
 __device__ __forceinline__ bool select_keys(Select<CAP>& s, int top, F&& each) {
@@ -178,7 +277,7 @@ __device__ __forceinline__ bool select_keys(Select<CAP>& s, int top, F&& each) {
             there += other != 0;
         }
         if (there < top ? threadIdx.x == 0 : mine && rank == top - 1) s.bound = there < top ? 1 : VALUES ? mine >> 32 << 32 : mine;
-        if (threadIdx.x == 0) s.count = 0;
+        if (threadIdx.x == 0) s.count = s.lanes = 0;
     }
     __syncthreads();
     const uint64_t bound = s.bound;
@@ -226,8 +325,8 @@ __device__ __forceinline__ void join_wave(float& m, float& s, float& t) {
 }
 
 // A workgroup a row, or a share of `columns` of its columns (a multiple of V); R pieces of V columns a lane and turn.  The alternatives come last: of what each four lanes
-// have met, the maximum is known by then; the top-th largest of these 64 bounds the answer from below, the few lanes that hold as much look through their columns
-// once more (out of L2, most likely), and what they find is ranked.  Where that is more than there is room for (equal scores, or orders that leave the largest
+// have met, the maximum is known by then; the top-th largest of these 64 bounds the answer from below, the columns of the few lanes that hold as much are looked through
+// once more (out of L2, most likely), and what is found is ranked.  Where that is more than there is room for (equal scores, or orders that leave the largest
 // to a few lanes), all columns are gone through again in turns of one piece a lane, each of which adds to the list what exceeds it.
 template <class T, int V, int R, bool TOP>
 __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_long_kernel(Scores a, int splits, int columns, char* __restrict__ parts) {
@@ -310,9 +409,12 @@ __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_long_kernel(Scores a,
                 for (int j = 0; j < V; ++j)
                     if (p.counts(j)) f(x[j], p.at + j);
             };
-            const bool done = select_keys<true>(sel, a.top, [&](auto&& take) {
-                if (ordered(best) < (uint32_t)(sel.bound >> 32)) return;
-                for (int piece = begin / V + threadIdx.x; piece * V < end; piece += LONG_THREADS) scan(piece, [&](float v, int column) { take(key_of(ordered(v), column)); });
+            const bool done = select_keys<true>(sel, a.top, [&](auto&& take) {  // (the lanes' pieces are shared out, so that they are loaded at once)
+                if (ordered(best) >= (uint32_t)(sel.bound >> 32)) sel.lane[atomicAdd(&sel.lanes, 1)] = (uint16_t)threadIdx.x;
+                __syncthreads();
+                const int lanes = sel.lanes, turns = (end - begin + LONG_THREADS * V - 1) / (LONG_THREADS * V);
+                for (int i = threadIdx.x; i < lanes * turns; i += LONG_THREADS)
+                    scan(begin / V + i / lanes * LONG_THREADS + sel.lane[i % lanes], [&](float v, int column) { take(key_of(ordered(v), column)); });
             });
             if (!done) {
                 float least = -INFINITY;  // the last of the alternatives so far; a later column has to exceed it
