@@ -77,6 +77,20 @@ __device__ __forceinline__ U lanes_max(U v) {
     return v;
 }
 
+// The largest whole number that at least `top` lanes of the wave have or exceed, bit by bit; the smallest that is an alternative where fewer lanes have one.
+__device__ __forceinline__ uint32_t bound_of_heads(uint32_t head, int top) {
+    uint32_t bound = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+        const int have = __popcll(__ballot(head >= (bound | 1u << bit)));
+        if (have >= top) bound |= 1u << bit;
+        if (have == top) break;  // (they all exceed what the bits below could add, or the bound is a little low, which costs nothing)
+    }
+    return max(bound, 0x00800000u);  // (of the lowest finite value; what is below it is no value's)
+}
+__device__ __forceinline__ uint64_t lane_value(uint64_t v, int lane) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+}
+
 // LANES lanes a row, each R pieces of V columns.
 template <class T, int V, int LANES, int R>
 __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
@@ -106,6 +120,7 @@ __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
                 m = fmaxf(m, x[i][j]);
             }
         }
+        const float own = m;  // of the lane's columns
         m = lanes_max<LANES>(m);
         const float base = m == -INFINITY ? 0.0f : m;
         float s = 0.0f, t = 0.0f, l, entropy;
@@ -125,6 +140,22 @@ __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
         const bool none = m != m;  // of the row's scores is an alternative
         float* values = a.values + at * a.top;
         int32_t* columns = a.columns + at * a.top;
+        if (a.top == 1) {  // the largest is known: the lowest column that has it
+            uint32_t column = 0;  // (its complement)
+#pragma unroll
+            for (int i = R - 1; i >= 0; --i) {
+                const Place<V, false> p(i * LANES + lane, a.c);
+#pragma unroll
+                for (int j = V - 1; j >= 0; --j) column = x[i][j] == m ? ~(uint32_t)(p.at + j) : column;
+            }
+            column = lanes_max<LANES>(column);
+            if (lane == 0 && row < a.n) {
+                const bool is = m > -INFINITY;
+                values[0] = is ? -l : none ? m : -INFINITY;  // (m - m - l)
+                columns[0] = is ? (int32_t)~column : -1;
+            }
+            continue;
+        }
         if constexpr (R == 1 && sizeof(T) == 2) {
             // A value's 16 bits in order, then its column from behind, make one whole number; every lane's in descending order, then `top` times the largest head.
             uint32_t key[V];
@@ -158,91 +189,70 @@ __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
         } else if constexpr (R == 1) {
             // Every lane's values in descending order (neighbours change places only where the later one is larger, so the lower column stays first), then `top` times the
             // largest head: of equal ones the first lane's, whose columns are lower.
-            float v[V];
-            int which[V];
+            uint32_t o[V], which[V];
             const int at0 = Place<V, false>(lane, a.c).at;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                v[j] = none ? -INFINITY : x[0][j];
+                o[j] = none ? 0u : ordered(x[0][j]);
                 which[j] = j;
             }
 #pragma unroll
             for (int round = 0; round < V; ++round)
 #pragma unroll
                 for (int j = round % 2; j + 1 < V; j += 2) {
-                    const bool change = v[j] < v[j + 1];
-                    const float first = fmaxf(v[j], v[j + 1]), second = fminf(v[j], v[j + 1]);
-                    const int here = which[j], next = which[j + 1];  // (values: a choice of places would become an index)
-                    const int w1 = change ? next : here, w2 = change ? here : next;
-                    v[j] = first, v[j + 1] = second, which[j] = w1, which[j + 1] = w2;
+                    const bool change = o[j] < o[j + 1];
+                    const uint32_t first = max(o[j], o[j + 1]), second = min(o[j], o[j + 1]);
+                    const uint32_t here = which[j], next = which[j + 1];  // (values: a choice of places would become an index)
+                    o[j] = first, o[j + 1] = second;
+                    which[j] = change ? next : here, which[j + 1] = change ? here : next;
                 }
             const uint64_t group = (LANES == 64 ? ~0ull : (1ull << LANES) - 1) << (threadIdx.x & 63 & ~(LANES - 1));
             for (int r = 0; r < a.top; ++r) {
-                const float best = lanes_max<LANES>(v[0]);
-                const uint64_t have = __ballot(v[0] == best) & group;
-                const bool mine = __builtin_amdgcn_mbcnt_hi((uint32_t)(have >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)have, 0)) == 0 && v[0] == best;
+                const uint32_t best = lanes_max<LANES>(o[0]);
+                const uint64_t have = __ballot(o[0] == best) & group;
+                const bool mine = o[0] == best && __builtin_amdgcn_mbcnt_hi((uint32_t)(have >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)have, 0)) == 0;
                 if (mine && row < a.n) {
-                    values[r] = none ? NAN : best == -INFINITY ? best : best - m - l;
-                    columns[r] = best == -INFINITY ? -1 : at0 + which[0];
+                    values[r] = none ? NAN : best ? in_order(best) - m - l : -INFINITY;
+                    columns[r] = best ? at0 + (int)which[0] : -1;
                 }
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const float stays = v[j], comes = j + 1 < V ? +v[j + 1] : -INFINITY;
-                    const int w1 = which[j], w2 = which[j + 1 < V ? j + 1 : j];
-                    v[j] = mine ? comes : stays;
+                    const uint32_t stays = o[j], comes = j + 1 < V ? +o[j + 1] : 0u, w1 = which[j], w2 = which[j + 1 < V ? j + 1 : j];
+                    o[j] = mine ? comes : stays;
                     which[j] = mine ? w2 : w1;
                 }
             }
         } else {
             // As for a long row: the top-th largest of the lanes' largest bounds the answer from below; what is as large is collected and ranked by counting.
             static_assert(R == 1 || LANES == 64, "");
-            __shared__ uint64_t room[256 / 64][MOST_TOP * R * V];  // (in at most `top` lanes)
+            __shared__ uint64_t room[256 / 64][64 * R * V];
             uint64_t* found = room[threadIdx.x / 64];
-            float most = -INFINITY;
-            int column = 0;
-#pragma unroll
-            for (int i = R - 1; i >= 0; --i) {
-                const Place<V, false> p(i * LANES + lane, a.c);
-#pragma unroll
-                for (int j = V - 1; j >= 0; --j) {
-                    column = x[i][j] >= most ? p.at + j : column;
-                    most = fmaxf(most, x[i][j]);
-                }
-            }
-            const uint64_t mine = none ? 0 : key_of(ordered(most), column);
-            const int there = __popcll(__ballot(mine != 0));
-            uint64_t bound = 1;
-            if (there >= a.top) {
-                int rank = 0;
-#pragma unroll 8
-                for (int i = 0; i < 64; ++i) {
-                    const uint64_t other = (uint64_t)__builtin_amdgcn_readlane((uint32_t)(mine >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((uint32_t)mine, i);
-                    rank += other > mine;
-                }
-                const int last = __ffsll((unsigned long long)__ballot(mine && rank == a.top - 1)) - 1;
-                bound = (uint64_t)__builtin_amdgcn_readlane((uint32_t)(mine >> 32), last) << 32 | (uint32_t)__builtin_amdgcn_readlane((uint32_t)mine, last);
-            }
+            const uint32_t bound = none ? ~0u : bound_of_heads(ordered(own), a.top);
+            const float least = in_order(bound);
             int count = 0;
 #pragma unroll
             for (int i = 0; i < R; ++i) {
                 const Place<V, false> p(i * LANES + lane, a.c);
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const uint32_t o = none ? 0 : ordered(x[i][j]);
-                    if (!__any(o >= (uint32_t)(bound >> 32) && o)) continue;
-                    const uint64_t key = key_of(o, p.at + j), takes = __ballot(key >= bound);
-                    if (key >= bound) found[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(takes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)takes, 0))] = key;
+                    const uint64_t takes = none ? 0 : __ballot(x[i][j] >= least);
+                    if (!takes) continue;
+                    if (x[i][j] >= least) found[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(takes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)takes, 0))] = key_of(ordered(x[i][j]), p.at + j);
                     count += __popcll(takes);
                 }
             }
             __builtin_amdgcn_wave_barrier();
-            for (int i = lane; i < count; i += 64) {
-                const uint64_t key = found[i];
+            for (int i0 = 0; i0 < count; i0 += 64) {
+                const uint64_t mine = i0 + lane < count ? found[i0 + lane] : 0;
                 int rank = 0;
-                for (int j = 0; j < count; ++j) rank += found[j] > key;
-                if (rank < a.top && row < a.n) {
-                    values[rank] = in_order((uint32_t)(key >> 32)) - m - l;
-                    columns[rank] = (int32_t)~(uint32_t)key;
+                for (int j0 = 0; j0 < count; j0 += 64) {
+                    const uint64_t other = j0 + lane < count ? found[j0 + lane] : 0;
+                    const int some = min(64, count - j0);
+                    for (int j = 0; j < some; ++j) rank += lane_value(other, j) > mine;
+                }
+                if (mine && rank < a.top && row < a.n) {
+                    values[rank] = in_order((uint32_t)(mine >> 32)) - m - l;
+                    columns[rank] = (int32_t)~(uint32_t)mine;
                 }
             }
             if (lane >= count && lane < a.top && row < a.n) {
@@ -269,14 +279,16 @@ __device__ __forceinline__ bool select_keys(Select<CAP>& s, int top, F&& each) {
     __syncthreads();
     if (threadIdx.x < 64) {
         const uint64_t mine = s.head[threadIdx.x];
-        int rank = 0, there = 0;
-#pragma unroll 8
-        for (int i = 0; i < 64; ++i) {
-            const uint64_t other = s.head[i];
-            rank += other > mine;
-            there += other != 0;
+        if constexpr (VALUES) {
+            const uint32_t bound = bound_of_heads((uint32_t)(mine >> 32), top);
+            if (threadIdx.x == 0) s.bound = (uint64_t)bound << 32;
+        } else {
+            const int there = __popcll(__ballot(mine != 0));
+            int rank = 0;
+#pragma unroll 2
+            for (int i = 0; i < 64; ++i) rank += lane_value(mine, i) > mine;
+            if (there < top ? threadIdx.x == 0 : mine && rank == top - 1) s.bound = there < top ? 1 : mine;
         }
-        if (there < top ? threadIdx.x == 0 : mine && rank == top - 1) s.bound = there < top ? 1 : VALUES ? mine >> 32 << 32 : mine;
         if (threadIdx.x == 0) s.count = s.lanes = 0;
     }
     __syncthreads();
@@ -296,6 +308,7 @@ __device__ __forceinline__ bool select_keys(Select<CAP>& s, int top, F&& each) {
     for (int i = threadIdx.x; i < count; i += LONG_THREADS) {
         const uint64_t mine = s.found[i];
         int rank = 0;
+#pragma unroll 8
         for (int j = 0; j < count; ++j) rank += s.found[j] > mine;
         if (rank < top) s.list[rank] = mine;  // (keys differ, so do ranks)
     }
@@ -384,11 +397,11 @@ __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_long_kernel(Scores a,
             room[1][wave] = s;
             room[2][wave] = t;
         }
-        if constexpr (TOP) {  // a key for each four lanes: its value, and a number that tells equal ones apart
+        if constexpr (TOP) {  // a key for each four lanes, of which only the value matters
             float four = best;
             four = fmaxf(four, lane_other<1>(four));
             four = fmaxf(four, lane_other<2>(four));
-            if (threadIdx.x % 4 == 0) sel.head[threadIdx.x / 4] = key_of(ordered(four), threadIdx.x / 4);
+            if (threadIdx.x % 4 == 0) sel.head[threadIdx.x / 4] = key_of(ordered(four), 0);
             if ((int)threadIdx.x < MOST_TOP) sel.list[threadIdx.x] = 0;
         }
         __syncthreads();
@@ -462,10 +475,18 @@ __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_long_kernel(Scores a,
 template <class T>
 __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_join_kernel(Scores a, int splits, char* __restrict__ parts) {
     __shared__ Select<MOST_TOP * MOST_TOP> sel;  // (of at most `top` parts, `top` keys each)
+    constexpr int WAVES = LONG_THREADS / 64, EACH = MOST_TOP / WAVES;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
-        const int lane = threadIdx.x & 63;
         Part mine{-INFINITY, 0.0f, 0.0f, 0.0f};
-        if (lane < splits) mine = *(const Part*)part_at(parts, row * splits + lane, a.top);
+        uint64_t keys[EACH] = {};  // every fourth of a share's, from its first (wave 0), second ... on
+        if (lane < splits) {
+            const char* part = part_at(parts, row * splits + lane, a.top);
+            mine = *(const Part*)part;
+#pragma unroll
+            for (int i = 0; i < EACH; ++i)
+                if (i * WAVES + wave < a.top) keys[i] = ((const uint64_t*)(part + sizeof(Part)))[i * WAVES + wave];
+        }
         float m = mine.m, s = mine.s, t = mine.t, l, entropy;
         join_wave(m, s, t);
         finish(m, s, t, l, entropy);
@@ -475,13 +496,13 @@ __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_join_kernel(Scores a,
             write_row(a, row, m, l, entropy, given ? (float)((const T*)a.z)[row * a.ldz + label] : 0.0f, given);
         }
         if (!a.top) continue;
-        auto key_at = [&](int split, int i) { return ((const uint64_t*)(part_at(parts, row * splits + split, a.top) + sizeof(Part)))[i]; };
         __syncthreads();
-        if (threadIdx.x < 64) sel.head[lane] = lane < splits ? key_at(lane, 0) : 0;
+        if ((int)threadIdx.x < 64) sel.head[lane] = keys[0];
         if ((int)threadIdx.x < MOST_TOP) sel.list[threadIdx.x] = 0;
         select_keys<false>(sel, a.top, [&](auto&& take) {
-            for (int i = threadIdx.x; i < splits * a.top; i += LONG_THREADS)
-                if (const uint64_t key = key_at(i / a.top, i % a.top)) take(key);
+#pragma unroll
+            for (int i = 0; i < EACH; ++i)
+                if (keys[i]) take(keys[i]);
         });
         write_top(a, row, sel.list, m, l);
     }
