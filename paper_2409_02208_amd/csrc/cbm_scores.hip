@@ -156,7 +156,9 @@ __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
             }
             continue;
         }
+        __shared__ uint64_t room[R == 1 ? 256 / LANES * MOST_TOP : 256 * R * V];  // what a row (a wave) has found
         if constexpr (R == 1 && sizeof(T) == 2) {
+            uint64_t* kept = room + threadIdx.x / LANES * MOST_TOP;
             // A value's 16 bits in order, then its column from behind, make one whole number; every lane's in descending order, then `top` times the largest head.
             uint32_t key[V];
             const int at0 = Place<V, false>(lane, a.c).at;
@@ -175,20 +177,25 @@ __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
             for (int r = 0; r < a.top; ++r) {
                 const uint32_t best = lanes_max<LANES>(key[0]);
                 const bool mine = key[0] == best;
-                if ((best ? mine : lane == 0) && row < a.n) {
-                    const uint32_t o = best >> 16, u = o ^ (o & 0x8000u ? 0x8000u : 0xffffu);
-                    values[r] = none ? NAN : best ? (float)__builtin_bit_cast(T, (uint16_t)u) - m - l : -INFINITY;
-                    columns[r] = best ? (int32_t)(0xffffu - (best & 0xffffu)) : -1;
-                }
+                if (mine) kept[r] = best;
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
                     const uint32_t stays = key[j], comes = j + 1 < V ? +key[j + 1] : 0u;  // (values: a choice of places would become an index)
                     key[j] = mine ? comes : stays;
                 }
             }
+            __builtin_amdgcn_wave_barrier();
+            for (int r = lane; r < a.top; r += LANES) {
+                const uint32_t best = (uint32_t)kept[r], o = best >> 16, u = o ^ (o & 0x8000u ? 0x8000u : 0xffffu);
+                if (row >= a.n) break;
+                values[r] = none ? NAN : best ? (float)__builtin_bit_cast(T, (uint16_t)u) - m - l : -INFINITY;
+                columns[r] = best ? (int32_t)(0xffffu - (best & 0xffffu)) : -1;
+            }
+            __builtin_amdgcn_wave_barrier();  // (kept is the next row's)
         } else if constexpr (R == 1) {
             // Every lane's values in descending order (neighbours change places only where the later one is larger, so the lower column stays first), then `top` times the
             // largest head: of equal ones the first lane's, whose columns are lower.
+            uint64_t* kept = room + threadIdx.x / LANES * MOST_TOP;
             uint32_t o[V], which[V];
             const int at0 = Place<V, false>(lane, a.c).at;
 #pragma unroll
@@ -211,10 +218,7 @@ __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
                 const uint32_t best = lanes_max<LANES>(o[0]);
                 const uint64_t have = __ballot(o[0] == best) & group;
                 const bool mine = o[0] == best && __builtin_amdgcn_mbcnt_hi((uint32_t)(have >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)have, 0)) == 0;
-                if (mine && row < a.n) {
-                    values[r] = none ? NAN : best ? in_order(best) - m - l : -INFINITY;
-                    columns[r] = best ? at0 + (int)which[0] : -1;
-                }
+                if (mine) kept[r] = (uint64_t)best << 32 | (uint32_t)(at0 + (int)which[0]);
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
                     const uint32_t stays = o[j], comes = j + 1 < V ? +o[j + 1] : 0u, w1 = which[j], w2 = which[j + 1 < V ? j + 1 : j];
@@ -222,11 +226,18 @@ __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
                     which[j] = mine ? w2 : w1;
                 }
             }
+            __builtin_amdgcn_wave_barrier();
+            for (int r = lane; r < a.top; r += LANES) {
+                const uint32_t best = (uint32_t)(kept[r] >> 32);
+                if (row >= a.n) break;
+                values[r] = none ? NAN : best ? in_order(best) - m - l : -INFINITY;
+                columns[r] = best ? (int32_t)kept[r] : -1;
+            }
+            __builtin_amdgcn_wave_barrier();  // (kept is the next row's)
         } else {
             // As for a long row: the top-th largest of the lanes' largest bounds the answer from below; what is as large is collected and ranked by counting.
             static_assert(R == 1 || LANES == 64, "");
-            __shared__ uint64_t room[256 / 64][64 * R * V];
-            uint64_t* found = room[threadIdx.x / 64];
+            uint64_t* found = room + threadIdx.x / 64 * (64 * R * V);
             const uint32_t bound = none ? ~0u : bound_of_heads(ordered(own), a.top);
             const float least = in_order(bound);
             int count = 0;
