@@ -91,8 +91,133 @@ __device__ __forceinline__ uint64_t lane_value(uint64_t v, int lane) {
     return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
 }
 
-// LANES lanes a row, each R pieces of V columns.
+// More than one alternative of a row in registers.  own: the largest of the lane's scores.
 template <class T, int V, int LANES, int R>
+__device__ __forceinline__ void write_alternatives(const Scores& a, int64_t row, int lane, const float (&x)[R][V], float own, float m, float l) {
+    const bool none = m != m;  // of the row's scores is an alternative
+    float* values = a.values + (row < a.n ? row : a.n - 1) * a.top;
+    int32_t* columns = a.columns + (row < a.n ? row : a.n - 1) * a.top;
+    __shared__ uint64_t room[R == 1 ? 256 / LANES * MOST_TOP : 256 * R * V];  // what a row (a wave) has found
+    if constexpr (R == 1 && sizeof(T) == 2) {
+        uint64_t* kept = room + threadIdx.x / LANES * MOST_TOP;
+        // A value's 16 bits in order, then its column from behind, make one whole number; every lane's in descending order, then `top` times the largest head.
+        uint32_t key[V];
+        const int at0 = Place<V, false>(lane, a.c).at;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const uint32_t u = __builtin_bit_cast(uint16_t, (T)(x[0][j] + 0.0f));
+            key[j] = !none && x[0][j] > -INFINITY ? (u ^ (u & 0x8000u ? 0xffffu : 0x8000u)) << 16 | (0xffffu - (uint32_t)(at0 + j)) : 0u;
+        }
+#pragma unroll
+        for (int round = 0; round < V; ++round)
+#pragma unroll
+            for (int j = round % 2; j + 1 < V; j += 2) {
+                const uint32_t first = max(key[j], key[j + 1]), second = min(key[j], key[j + 1]);
+                key[j] = first, key[j + 1] = second;
+            }
+        for (int r = 0; r < a.top; ++r) {
+            const uint32_t best = lanes_max<LANES>(key[0]);
+            const bool mine = key[0] == best;
+            if (mine) kept[r] = best;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const uint32_t stays = key[j], comes = j + 1 < V ? +key[j + 1] : 0u;  // (values: a choice of places would become an index)
+                key[j] = mine ? comes : stays;
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+        for (int r = lane; r < a.top; r += LANES) {
+            const uint32_t best = (uint32_t)kept[r], o = best >> 16, u = o ^ (o & 0x8000u ? 0x8000u : 0xffffu);
+            if (row >= a.n) break;
+            values[r] = none ? NAN : best ? (float)__builtin_bit_cast(T, (uint16_t)u) - m - l : -INFINITY;
+            columns[r] = best ? (int32_t)(0xffffu - (best & 0xffffu)) : -1;
+        }
+        __builtin_amdgcn_wave_barrier();  // (kept is the next row's)
+    } else if constexpr (R == 1) {
+        // Every lane's values in descending order (neighbours change places only where the later one is larger, so the lower column stays first), then `top` times the
+        // largest head: of equal ones the first lane's, whose columns are lower.
+        uint64_t* kept = room + threadIdx.x / LANES * MOST_TOP;
+        uint32_t o[V], which[V];
+        const int at0 = Place<V, false>(lane, a.c).at;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            o[j] = none ? 0u : ordered(x[0][j]);
+            which[j] = j;
+        }
+#pragma unroll
+        for (int round = 0; round < V; ++round)
+#pragma unroll
+            for (int j = round % 2; j + 1 < V; j += 2) {
+                const bool change = o[j] < o[j + 1];
+                const uint32_t first = max(o[j], o[j + 1]), second = min(o[j], o[j + 1]);
+                const uint32_t here = which[j], next = which[j + 1];  // (values: a choice of places would become an index)
+                o[j] = first, o[j + 1] = second;
+                which[j] = change ? next : here, which[j + 1] = change ? here : next;
+            }
+        const uint64_t group = (LANES == 64 ? ~0ull : (1ull << LANES) - 1) << (threadIdx.x & 63 & ~(LANES - 1));
+        for (int r = 0; r < a.top; ++r) {
+            const uint32_t best = lanes_max<LANES>(o[0]);
+            const uint64_t have = __ballot(o[0] == best) & group;
+            const bool mine = o[0] == best && __builtin_amdgcn_mbcnt_hi((uint32_t)(have >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)have, 0)) == 0;
+            if (mine) kept[r] = (uint64_t)best << 32 | (uint32_t)(at0 + (int)which[0]);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const uint32_t stays = o[j], comes = j + 1 < V ? +o[j + 1] : 0u, w1 = which[j], w2 = which[j + 1 < V ? j + 1 : j];
+                o[j] = mine ? comes : stays;
+                which[j] = mine ? w2 : w1;
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+        for (int r = lane; r < a.top; r += LANES) {
+            const uint32_t best = (uint32_t)(kept[r] >> 32);
+            if (row >= a.n) break;
+            values[r] = none ? NAN : best ? in_order(best) - m - l : -INFINITY;
+            columns[r] = best ? (int32_t)kept[r] : -1;
+        }
+        __builtin_amdgcn_wave_barrier();  // (kept is the next row's)
+    } else {
+        // As for a long row: the top-th largest of the lanes' largest bounds the answer from below; what is as large is collected and ranked by counting.
+        static_assert(R == 1 || LANES == 64, "");
+        uint64_t* found = room + threadIdx.x / 64 * (64 * R * V);
+        const uint32_t bound = none ? ~0u : bound_of_heads(ordered(own), a.top);
+        const float least = in_order(bound);
+        int count = 0;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const Place<V, false> p(i * LANES + lane, a.c);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const uint64_t takes = none ? 0 : __ballot(x[i][j] >= least);
+                if (!takes) continue;
+                if (x[i][j] >= least) found[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(takes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)takes, 0))] = key_of(ordered(x[i][j]), p.at + j);
+                count += __popcll(takes);
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+        for (int i0 = 0; i0 < count; i0 += 64) {
+            const uint64_t mine = i0 + lane < count ? found[i0 + lane] : 0;
+            int rank = 0;
+            for (int j0 = 0; j0 < count; j0 += 64) {
+                const uint64_t other = j0 + lane < count ? found[j0 + lane] : 0;
+                const int some = min(64, count - j0);
+                for (int j = 0; j < some; ++j) rank += lane_value(other, j) > mine;
+            }
+            if (mine && rank < a.top && row < a.n) {
+                values[rank] = in_order((uint32_t)(mine >> 32)) - m - l;
+                columns[rank] = (int32_t)~(uint32_t)mine;
+            }
+        }
+        if (lane >= count && lane < a.top && row < a.n) {
+            values[lane] = none ? NAN : -INFINITY;
+            columns[lane] = -1;
+        }
+        __builtin_amdgcn_wave_barrier();  // (found is the next row's)
+    }
+}
+
+// LANES lanes a row, each R pieces of V columns.  SELECT: more alternatives than the best one.  Without it four pieces of fp32 (two of 16 bits) a lane, so that many rows share a
+// wave's reductions (235868 x 112 33 us with one piece a lane, 20 with four); with it one piece as long as that is enough, since alternatives come out of sorted lanes.
+template <class T, int V, int LANES, int R, bool SELECT>
 __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
     const int lane = threadIdx.x % LANES;
     for (int64_t row0 = (int64_t)blockIdx.x * (256 / LANES); row0 < a.n; row0 += (int64_t)gridDim.x * (256 / LANES)) {
@@ -136,11 +261,8 @@ __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
         t = lanes_sum<LANES>(t);
         finish(m, s, t, l, entropy);
         if (lane == 0 && row < a.n) write_row(a, row, m, l, entropy, at_label, given);
-        if (!a.top) continue;
-        const bool none = m != m;  // of the row's scores is an alternative
-        float* values = a.values + at * a.top;
-        int32_t* columns = a.columns + at * a.top;
-        if (a.top == 1) {  // the largest is known: the lowest column that has it
+        if (!SELECT && !a.top) continue;
+        if constexpr (!SELECT) {  // one: the largest is known, it is the lowest column that has it
             uint32_t column = 0;  // (its complement)
 #pragma unroll
             for (int i = R - 1; i >= 0; --i) {
@@ -151,126 +273,11 @@ __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
             column = lanes_max<LANES>(column);
             if (lane == 0 && row < a.n) {
                 const bool is = m > -INFINITY;
-                values[0] = is ? -l : none ? m : -INFINITY;  // (m - m - l)
-                columns[0] = is ? (int32_t)~column : -1;
+                a.values[row] = is ? -l : m;  // (m - m - l)
+                a.columns[row] = is ? (int32_t)~column : -1;
             }
-            continue;
-        }
-        __shared__ uint64_t room[R == 1 ? 256 / LANES * MOST_TOP : 256 * R * V];  // what a row (a wave) has found
-        if constexpr (R == 1 && sizeof(T) == 2) {
-            uint64_t* kept = room + threadIdx.x / LANES * MOST_TOP;
-            // A value's 16 bits in order, then its column from behind, make one whole number; every lane's in descending order, then `top` times the largest head.
-            uint32_t key[V];
-            const int at0 = Place<V, false>(lane, a.c).at;
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const uint32_t u = __builtin_bit_cast(uint16_t, (T)(x[0][j] + 0.0f));
-                key[j] = !none && x[0][j] > -INFINITY ? (u ^ (u & 0x8000u ? 0xffffu : 0x8000u)) << 16 | (0xffffu - (uint32_t)(at0 + j)) : 0u;
-            }
-#pragma unroll
-            for (int round = 0; round < V; ++round)
-#pragma unroll
-                for (int j = round % 2; j + 1 < V; j += 2) {
-                    const uint32_t first = max(key[j], key[j + 1]), second = min(key[j], key[j + 1]);
-                    key[j] = first, key[j + 1] = second;
-                }
-            for (int r = 0; r < a.top; ++r) {
-                const uint32_t best = lanes_max<LANES>(key[0]);
-                const bool mine = key[0] == best;
-                if (mine) kept[r] = best;
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const uint32_t stays = key[j], comes = j + 1 < V ? +key[j + 1] : 0u;  // (values: a choice of places would become an index)
-                    key[j] = mine ? comes : stays;
-                }
-            }
-            __builtin_amdgcn_wave_barrier();
-            for (int r = lane; r < a.top; r += LANES) {
-                const uint32_t best = (uint32_t)kept[r], o = best >> 16, u = o ^ (o & 0x8000u ? 0x8000u : 0xffffu);
-                if (row >= a.n) break;
-                values[r] = none ? NAN : best ? (float)__builtin_bit_cast(T, (uint16_t)u) - m - l : -INFINITY;
-                columns[r] = best ? (int32_t)(0xffffu - (best & 0xffffu)) : -1;
-            }
-            __builtin_amdgcn_wave_barrier();  // (kept is the next row's)
-        } else if constexpr (R == 1) {
-            // Every lane's values in descending order (neighbours change places only where the later one is larger, so the lower column stays first), then `top` times the
-            // largest head: of equal ones the first lane's, whose columns are lower.
-            uint64_t* kept = room + threadIdx.x / LANES * MOST_TOP;
-            uint32_t o[V], which[V];
-            const int at0 = Place<V, false>(lane, a.c).at;
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                o[j] = none ? 0u : ordered(x[0][j]);
-                which[j] = j;
-            }
-#pragma unroll
-            for (int round = 0; round < V; ++round)
-#pragma unroll
-                for (int j = round % 2; j + 1 < V; j += 2) {
-                    const bool change = o[j] < o[j + 1];
-                    const uint32_t first = max(o[j], o[j + 1]), second = min(o[j], o[j + 1]);
-                    const uint32_t here = which[j], next = which[j + 1];  // (values: a choice of places would become an index)
-                    o[j] = first, o[j + 1] = second;
-                    which[j] = change ? next : here, which[j + 1] = change ? here : next;
-                }
-            const uint64_t group = (LANES == 64 ? ~0ull : (1ull << LANES) - 1) << (threadIdx.x & 63 & ~(LANES - 1));
-            for (int r = 0; r < a.top; ++r) {
-                const uint32_t best = lanes_max<LANES>(o[0]);
-                const uint64_t have = __ballot(o[0] == best) & group;
-                const bool mine = o[0] == best && __builtin_amdgcn_mbcnt_hi((uint32_t)(have >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)have, 0)) == 0;
-                if (mine) kept[r] = (uint64_t)best << 32 | (uint32_t)(at0 + (int)which[0]);
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const uint32_t stays = o[j], comes = j + 1 < V ? +o[j + 1] : 0u, w1 = which[j], w2 = which[j + 1 < V ? j + 1 : j];
-                    o[j] = mine ? comes : stays;
-                    which[j] = mine ? w2 : w1;
-                }
-            }
-            __builtin_amdgcn_wave_barrier();
-            for (int r = lane; r < a.top; r += LANES) {
-                const uint32_t best = (uint32_t)(kept[r] >> 32);
-                if (row >= a.n) break;
-                values[r] = none ? NAN : best ? in_order(best) - m - l : -INFINITY;
-                columns[r] = best ? (int32_t)kept[r] : -1;
-            }
-            __builtin_amdgcn_wave_barrier();  // (kept is the next row's)
         } else {
-            // As for a long row: the top-th largest of the lanes' largest bounds the answer from below; what is as large is collected and ranked by counting.
-            static_assert(R == 1 || LANES == 64, "");
-            uint64_t* found = room + threadIdx.x / 64 * (64 * R * V);
-            const uint32_t bound = none ? ~0u : bound_of_heads(ordered(own), a.top);
-            const float least = in_order(bound);
-            int count = 0;
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-                const Place<V, false> p(i * LANES + lane, a.c);
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const uint64_t takes = none ? 0 : __ballot(x[i][j] >= least);
-                    if (!takes) continue;
-                    if (x[i][j] >= least) found[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(takes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)takes, 0))] = key_of(ordered(x[i][j]), p.at + j);
-                    count += __popcll(takes);
-                }
-            }
-            __builtin_amdgcn_wave_barrier();
-            for (int i0 = 0; i0 < count; i0 += 64) {
-                const uint64_t mine = i0 + lane < count ? found[i0 + lane] : 0;
-                int rank = 0;
-                for (int j0 = 0; j0 < count; j0 += 64) {
-                    const uint64_t other = j0 + lane < count ? found[j0 + lane] : 0;
-                    const int some = min(64, count - j0);
-                    for (int j = 0; j < some; ++j) rank += lane_value(other, j) > mine;
-                }
-                if (mine && rank < a.top && row < a.n) {
-                    values[rank] = in_order((uint32_t)(mine >> 32)) - m - l;
-                    columns[rank] = (int32_t)~(uint32_t)mine;
-                }
-            }
-            if (lane >= count && lane < a.top && row < a.n) {
-                values[lane] = none ? NAN : -INFINITY;
-                columns[lane] = -1;
-            }
-            __builtin_amdgcn_wave_barrier();  // (found is the next row's)
+            write_alternatives<T, V, LANES, R>(a, row, lane, x, own, m, l);
         }
     }
 }
@@ -591,16 +598,23 @@ cbm_status cbm_launch_scores(int64_t n, int32_t c, int32_t type, const void* z, 
         using T = decltype(t);
         constexpr int V = 16 / (int)sizeof(T);
         const int pieces = (c + V - 1) / V;
-#define CBM_SCORES(V_, LANES, R) \
-    cbm_scores_kernel<T, V_, LANES, R><<<(unsigned)std::min<int64_t>((n + 256 / LANES - 1) / (256 / LANES), 1 << 23), 256, 0, stream>>>(a)
-        if (c < V) CBM_SCORES(1, 8, 1);
-        else if (pieces <= 4) CBM_SCORES(V, 4, 1);
-        else if (pieces <= 8) CBM_SCORES(V, 8, 1);
-        else if (pieces <= 16) CBM_SCORES(V, 16, 1);
-        else if (pieces <= 32) CBM_SCORES(V, 32, 1);
-        else if (pieces <= 64) CBM_SCORES(V, 64, 1);
-        else if (pieces <= 128) CBM_SCORES(V, 64, 2);
-        else if (c <= SHORT_ROW) CBM_SCORES(V, 64, SHORT_ROW / 64 / V);
+#define CBM_SCORES(V_, LANES, R, SELECT) \
+    cbm_scores_kernel<T, V_, LANES, R, SELECT><<<(unsigned)std::min<int64_t>((n + 256 / LANES - 1) / (256 / LANES), 1 << 23), 256, 0, stream>>>(a)
+        constexpr int R = 16 / V;
+        if (c < V) top > 1 ? CBM_SCORES(1, 8, 1, true) : CBM_SCORES(1, 8, 1, false);
+        else if (top > 1 && pieces <= 64) {
+            if (pieces <= 4) CBM_SCORES(V, 4, 1, true);
+            else if (pieces <= 8) CBM_SCORES(V, 8, 1, true);
+            else if (pieces <= 16) CBM_SCORES(V, 16, 1, true);
+            else if (pieces <= 32) CBM_SCORES(V, 32, 1, true);
+            else CBM_SCORES(V, 64, 1, true);
+        } else if (top > 1 && c <= SHORT_ROW) CBM_SCORES(V, 64, SHORT_ROW / 64 / V, true);
+        else if (pieces <= 4) CBM_SCORES(V, 4, 1, false);
+        else if (pieces <= 4 * R) CBM_SCORES(V, 4, R, false);
+        else if (pieces <= 8 * R) CBM_SCORES(V, 8, R, false);
+        else if (pieces <= 16 * R) CBM_SCORES(V, 16, R, false);
+        else if (pieces <= 32 * R) CBM_SCORES(V, 32, R, false);
+        else if (c <= SHORT_ROW) CBM_SCORES(V, 64, R, false);
 #undef CBM_SCORES
         else {
             const int splits = cbm_scores_splits(n, c);
