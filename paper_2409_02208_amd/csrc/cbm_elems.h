@@ -14,14 +14,17 @@ struct Piece {
     typedef T type __attribute__((ext_vector_type(V), aligned(sizeof(T))));
 };
 template <int V, class T>
-__device__ __forceinline__ void load_piece(float (&x)[V], const T* p) {
-    if constexpr (V == 1) {
-        x[0] = (float)*p;
-    } else {
-        const typename Piece<T, V>::type v = *reinterpret_cast<const typename Piece<T, V>::type*>(p);
+__device__ __forceinline__ typename Piece<T, V>::type raw_piece(const T* p) {
+    return *reinterpret_cast<const typename Piece<T, V>::type*>(p);
+}
+template <int V, class T>
+__device__ __forceinline__ void widen(float (&x)[V], const typename Piece<T, V>::type& v) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) x[j] = (float)v[j];
-    }
+    for (int j = 0; j < V; ++j) x[j] = (float)v[j];
+}
+template <int V, class T>
+__device__ __forceinline__ void load_piece(float (&x)[V], const T* p) {
+    widen<V, T>(x, raw_piece<V>(p));
 }
 template <int V, class T>
 __device__ __forceinline__ void store_piece(T* p, const float (&x)[V]) {

@@ -65,15 +65,21 @@ __global__ __launch_bounds__(LANES > NORM_THREADS ? LANES : NORM_THREADS) void c
             b[c][j] = beta ? beta[p.at + j] : 0.0f;
         }
     }
+    typename Piece<T, V>::type next[R];  // AHEAD: of the workgroup's next row, whose loads pass the barriers of this one
+    constexpr bool AHEAD = LANES > 64;
+    auto load = [&](int64_t row) {
+        const T* x_row = X + (row < n ? row : n - 1) * ldx;
+#pragma unroll
+        for (int c = 0; c < R; ++c) next[c] = raw_piece<V>(x_row + Place<V, WHOLE>(c * LANES + lane, k).at);
+    };
+    if (AHEAD) load(blockIdx.x);
     for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < n; row0 += (int64_t)gridDim.x * ROWS) {
         const int64_t row = row0 + threadIdx.x / LANES;
-        const T* x_row = X + (row < n ? row : n - 1) * ldx;
         float x[R][V], sum = 0.0f, none = 0.0f;
+        if (!AHEAD) load(row);
 #pragma unroll
-        for (int c = 0; c < R; ++c) {
-            const Place<V, WHOLE> p(c * LANES + lane, k);
-            load_piece<V>(x[c], x_row + p.at);
-        }
+        for (int c = 0; c < R; ++c) widen<V, T>(x[c], next[c]);
+        if (AHEAD) load(row + gridDim.x);
 #pragma unroll
         for (int c = 0; c < R; ++c) {
             const Place<V, WHOLE> p(c * LANES + lane, k);
@@ -171,17 +177,33 @@ __global__ __launch_bounds__(THREADS) void cbm_norm_back_kernel(int64_t n, int k
             dg[c][j] = db[c][j] = 0.0f;
         }
     }
-    for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < n; row0 += (int64_t)gridDim.x * ROWS) {
-        const int64_t row = row0 + threadIdx.x / LANES, at = row < n ? row : n - 1;
+    typename Piece<T, V>::type next_x[R], next_dy[R];
+    float next_m, next_r;
+    constexpr bool AHEAD = LANES > 64 && (R * V < 16 || (WHOLE && LANES < 1024));  // (as far as registers go)
+    auto load = [&](int64_t row) {
+        const int64_t at = row < n ? row : n - 1;
         const T *x_row = X + at * ldx, *dy_row = dY + at * lddy;
-        float h[R][V], u[R][V], sum = 0.0f, along = 0.0f;
 #pragma unroll
         for (int c = 0; c < R; ++c) {
             const Place<V, WHOLE> p(c * LANES + lane, k);
-            load_piece<V>(h[c], x_row + p.at);
-            load_piece<V>(u[c], dy_row + p.at);
+            next_x[c] = raw_piece<V>(x_row + p.at);
+            next_dy[c] = raw_piece<V>(dy_row + p.at);
         }
-        const float m = mean[at], r = rstd[at];
+        next_m = mean[at];
+        next_r = rstd[at];
+    };
+    if (AHEAD) load(blockIdx.x);
+    for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < n; row0 += (int64_t)gridDim.x * ROWS) {
+        const int64_t row = row0 + threadIdx.x / LANES;
+        float h[R][V], u[R][V], sum = 0.0f, along = 0.0f;
+        if (!AHEAD) load(row);
+#pragma unroll
+        for (int c = 0; c < R; ++c) {
+            widen<V, T>(h[c], next_x[c]);
+            widen<V, T>(u[c], next_dy[c]);
+        }
+        const float m = next_m, r = next_r;
+        if (AHEAD) load(row + gridDim.x);
 #pragma unroll
         for (int c = 0; c < R; ++c) {
             const Place<V, WHOLE> p(c * LANES + lane, k);
@@ -403,9 +425,11 @@ cbm_status cbm_launch_norm_backward(int64_t n, int32_t k, int32_t type, const vo
             else if (pieces <= 16) CBM_BACK(V, 16, 1, BACK_THREADS);
             else if (pieces <= 32) CBM_BACK(V, 32, 1, BACK_THREADS);
             else if (pieces <= 64) CBM_BACK(V, 64, 1, BACK_THREADS);
+            else if (pieces <= 128) CBM_BACK(V, 64, 2, 256);
             else if (pieces <= 256) CBM_BACK(V, 256, 1, 256);
             else if (pieces <= 512) CBM_BACK(V, 256, 2, 256);
             else if (pieces <= 1024) CBM_BACK(V, 512, 2, 512);
+            else if (pieces <= 2048) CBM_BACK(V, 1024, 2, 1024);
             else {
                 if (dX) hipLaunchKernelGGL((cbm_norm_back_wide_kernel<T, V, WHOLE>), dim3((unsigned)std::min<int64_t>(n, 512)), dim3(1024), 0, stream, n, k, dY, lddy, X, ldx, gamma, mean, rstd, dX, lddx);
                 count = std::min<int64_t>(most, 64);
