@@ -14,36 +14,36 @@
 
 namespace {
 
+typedef float floatx2 __attribute__((ext_vector_type(2)));
 constexpr int NORM_THREADS = 256;
 constexpr int BACK_THREADS = 512, BACK_GROUPS = 512;  // backward: workgroups at most, each with partial sums of dg and db of its own
 
-// Sums of `values` values over a workgroup of THREADS, in every thread.  `room` holds 2 values of every wave.
+// Sums of two values over a workgroup, in every thread.  `room` has a pair for every wave, twice: calls take turns (`turn`), so one barrier each is enough (who writes a
+// room again has passed the barrier of the call between, and with it everybody's reads).
 template <int THREADS>
-__device__ __forceinline__ void block_sum2(float& a, float& b, float* room) {
+__device__ __forceinline__ void block_sum2(float& a, float& b, floatx2* room, int& turn) {
     constexpr int WAVES = THREADS / 64;
     a = lanes_sum<64>(a);
     b = lanes_sum<64>(b);
-    __syncthreads();  // (what the last call left in `room` has been read)
-    if ((threadIdx.x & 63) == 0) {
-        room[2 * (threadIdx.x / 64)] = a;
-        room[2 * (threadIdx.x / 64) + 1] = b;
-    }
+    floatx2* mine = room + turn * WAVES;
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 0) mine[threadIdx.x / 64] = floatx2{a, b};
     __syncthreads();
     a = b = 0.0f;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-        a += room[2 * w];
-        b += room[2 * w + 1];
+        a += mine[w][0];
+        b += mine[w][1];
     }
 }
 // over the LANES lanes of a row: part of a wave, or the whole workgroup
 template <int LANES>
-__device__ __forceinline__ void row_sum2(float& a, float& b, float* room) {
+__device__ __forceinline__ void row_sum2(float& a, float& b, floatx2* room, int& turn) {
     if constexpr (LANES <= 64) {
         a = lanes_sum<LANES>(a);
         b = lanes_sum<LANES>(b);
     } else {
-        block_sum2<LANES>(a, b, room);
+        block_sum2<LANES>(a, b, room, turn);
     }
 }
 
@@ -53,8 +53,9 @@ __global__ __launch_bounds__(LANES > NORM_THREADS ? LANES : NORM_THREADS) void c
                                                                                               const float* __restrict__ beta, float eps, T* __restrict__ Y, int64_t ldy,
                                                                                               float* __restrict__ mean, float* __restrict__ rstd) {
     constexpr int THREADS = LANES > NORM_THREADS ? LANES : NORM_THREADS, ROWS = THREADS / LANES;
-    __shared__ float room[LANES > 64 ? 2 * (LANES / 64) : 1];
+    __shared__ floatx2 room[LANES > 64 ? 2 * (LANES / 64) : 1];
     const int lane = threadIdx.x % LANES;
+    int turn = 0;
     float g[R][V], b[R][V];
 #pragma unroll
     for (int c = 0; c < R; ++c) {
@@ -75,7 +76,7 @@ __global__ __launch_bounds__(LANES > NORM_THREADS ? LANES : NORM_THREADS) void c
     if (AHEAD) load(blockIdx.x);
     for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < n; row0 += (int64_t)gridDim.x * ROWS) {
         const int64_t row = row0 + threadIdx.x / LANES;
-        float x[R][V], sum = 0.0f, none = 0.0f;
+        float x[R][V], sum = 0.0f, squares = 0.0f, none = 0.0f;
         if (!AHEAD) load(row);
 #pragma unroll
         for (int c = 0; c < R; ++c) widen<V, T>(x[c], next[c]);
@@ -86,9 +87,8 @@ __global__ __launch_bounds__(LANES > NORM_THREADS ? LANES : NORM_THREADS) void c
 #pragma unroll
             for (int j = 0; j < V; ++j) sum += p.counts(j) ? x[c][j] : 0.0f;
         }
-        row_sum2<LANES>(sum, none, room);
+        row_sum2<LANES>(sum, none, room, turn);
         const float m = sum / (float)k;
-        float squares = 0.0f;
 #pragma unroll
         for (int c = 0; c < R; ++c) {
             const Place<V, WHOLE> p(c * LANES + lane, k);
@@ -98,7 +98,7 @@ __global__ __launch_bounds__(LANES > NORM_THREADS ? LANES : NORM_THREADS) void c
                 squares += p.counts(j) ? x[c][j] * x[c][j] : 0.0f;
             }
         }
-        row_sum2<LANES>(squares, none, room);
+        row_sum2<LANES>(squares, none, room, turn);
         const float r = 1.0f / sqrtf(squares / (float)k + eps);
         if (row >= n) continue;  // (only where a row is part of a wave: with a workgroup a row, row0 is the row)
         T* y_row = Y + row * ldy;
@@ -121,7 +121,8 @@ __global__ __launch_bounds__(LANES > NORM_THREADS ? LANES : NORM_THREADS) void c
 template <class T, int V, bool WHOLE>
 __global__ __launch_bounds__(1024) void cbm_norm_wide_kernel(int64_t n, int k, const T* __restrict__ X, int64_t ldx, const float* __restrict__ gamma, const float* __restrict__ beta,
                                                              float eps, T* __restrict__ Y, int64_t ldy, float* __restrict__ mean, float* __restrict__ rstd) {
-    __shared__ float room[32];
+    __shared__ floatx2 room[32];
+    int turn = 0;
     const int pieces = (k + V - 1) / V;
     for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
         const T* x_row = X + row * ldx;
@@ -132,7 +133,7 @@ __global__ __launch_bounds__(1024) void cbm_norm_wide_kernel(int64_t n, int k, c
 #pragma unroll
             for (int j = 0; j < V; ++j) sum += p.counts(j) ? x[j] : 0.0f;
         }
-        block_sum2<1024>(sum, none, room);
+        block_sum2<1024>(sum, none, room, turn);
         const float m = sum / (float)k;
         float squares = 0.0f;
         for (int c = threadIdx.x; c < pieces; c += 1024) {
@@ -141,7 +142,7 @@ __global__ __launch_bounds__(1024) void cbm_norm_wide_kernel(int64_t n, int k, c
 #pragma unroll
             for (int j = 0; j < V; ++j) squares += p.counts(j) ? (x[j] - m) * (x[j] - m) : 0.0f;
         }
-        block_sum2<1024>(squares, none, room);
+        block_sum2<1024>(squares, none, room, turn);
         const float r = 1.0f / sqrtf(squares / (float)k + eps);
         for (int c = threadIdx.x; c < pieces; c += 1024) {
             const Place<V, WHOLE> p(c, k);
@@ -165,8 +166,9 @@ __global__ __launch_bounds__(THREADS) void cbm_norm_back_kernel(int64_t n, int k
                                                                 T* __restrict__ dX, int64_t lddx, float* __restrict__ parts) {
     constexpr int ROWS = THREADS / LANES;
     constexpr int COLUMNS = LANES * R * V;
-    __shared__ float room[LANES > 64 ? 2 * (LANES / 64) : (THREADS / 64) * 2 * COLUMNS];
+    __shared__ floatx2 room[LANES > 64 ? 2 * (LANES / 64) : (THREADS / 64) * COLUMNS];
     const int lane = threadIdx.x % LANES;
+    int turn = 0;
     float g[R][V], dg[R][V], db[R][V];
 #pragma unroll
     for (int c = 0; c < R; ++c) {
@@ -179,7 +181,7 @@ __global__ __launch_bounds__(THREADS) void cbm_norm_back_kernel(int64_t n, int k
     }
     typename Piece<T, V>::type next_x[R], next_dy[R];
     float next_m, next_r;
-    constexpr bool AHEAD = LANES > 64 && (R * V < 16 || (WHOLE && LANES < 1024));  // (as far as registers go)
+    constexpr bool AHEAD = LANES > 64 && (R * V <= 8 || (WHOLE && LANES < 1024));  // (as far as registers go)
     auto load = [&](int64_t row) {
         const int64_t at = row < n ? row : n - 1;
         const T *x_row = X + at * ldx, *dy_row = dY + at * lddy;
@@ -220,7 +222,7 @@ __global__ __launch_bounds__(THREADS) void cbm_norm_back_kernel(int64_t n, int k
             }
         }
         if (!dX) continue;
-        row_sum2<LANES>(sum, along, room);
+        row_sum2<LANES>(sum, along, room, turn);
         sum /= (float)k;
         along /= (float)k;
         if (row >= n) continue;
@@ -261,29 +263,32 @@ __global__ __launch_bounds__(THREADS) void cbm_norm_back_kernel(int64_t n, int k
                 }
                 if ((threadIdx.x & 63) < LANES) {
                     const int slot = (c * LANES + lane) * V + j;
-                    room[(2 * wave) * COLUMNS + slot] = a;
-                    room[(2 * wave + 1) * COLUMNS + slot] = b;
+                    room[wave * COLUMNS + slot] = floatx2{a, b};
                 }
             }
         __syncthreads();
-        for (int i = threadIdx.x; i < 2 * COLUMNS; i += THREADS) {
-            const int slot = i % COLUMNS, which = i / COLUMNS;
+        for (int slot = threadIdx.x; slot < COLUMNS; slot += THREADS) {
             const Place<V, WHOLE> p(slot / V, k);
             if (!p.counts(slot % V)) continue;
-            float s = 0.0f;
+            float a = 0.0f, b = 0.0f;
 #pragma unroll
-            for (int w = 0; w < THREADS / 64; ++w) s += room[(2 * w + which) * COLUMNS + slot];
-            out[which * k + p.at + slot % V] = s;
+            for (int w = 0; w < THREADS / 64; ++w) {
+                a += room[w * COLUMNS + slot][0];
+                b += room[w * COLUMNS + slot][1];
+            }
+            out[p.at + slot % V] = a;
+            out[k + p.at + slot % V] = b;
         }
     }
 }
 
-// Rows too wide for registers: dx by a workgroup a row, which reads x and dy twice; dg and db by workgroups of 256 columns and a share of the rows.
+// Rows too wide for registers: dx by a workgroup a row, which reads x and dy twice; dg and db by workgroups of 256 pieces and a share of the rows.
 template <class T, int V, bool WHOLE>
 __global__ __launch_bounds__(1024) void cbm_norm_back_wide_kernel(int64_t n, int k, const T* __restrict__ dY, int64_t lddy, const T* __restrict__ X, int64_t ldx,
                                                                   const float* __restrict__ gamma, const float* __restrict__ mean, const float* __restrict__ rstd,
                                                                   T* __restrict__ dX, int64_t lddx) {
-    __shared__ float room[32];
+    __shared__ floatx2 room[32];
+    int turn = 0;
     const int pieces = (k + V - 1) / V;
     for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
         const float m = mean[row], r = rstd[row];
@@ -299,7 +304,7 @@ __global__ __launch_bounds__(1024) void cbm_norm_back_wide_kernel(int64_t n, int
                 along += p.counts(j) ? u * ((x[j] - m) * r) : 0.0f;
             }
         }
-        block_sum2<1024>(sum, along, room);
+        block_sum2<1024>(sum, along, room, turn);
         sum /= (float)k;
         along /= (float)k;
         for (int c = threadIdx.x; c < pieces; c += 1024) {
@@ -312,20 +317,31 @@ __global__ __launch_bounds__(1024) void cbm_norm_back_wide_kernel(int64_t n, int
         }
     }
 }
-template <class T>
+template <class T, int V, bool WHOLE>
 __global__ __launch_bounds__(256) void cbm_norm_back_columns_kernel(int64_t n, int k, const T* __restrict__ dY, int64_t lddy, const T* __restrict__ X, int64_t ldx,
                                                                     const float* __restrict__ mean, const float* __restrict__ rstd, float* __restrict__ parts) {
-    const int column = blockIdx.x * 256 + threadIdx.x;
-    if (column >= k) return;
-    float dg = 0.0f, db = 0.0f;
+    const Place<V, WHOLE> p(blockIdx.x * 256 + threadIdx.x, k);
+    if (!p.any()) return;
+    float dg[V] = {}, db[V] = {};
+#pragma unroll 4
     for (int64_t row = blockIdx.y; row < n; row += gridDim.y) {
-        const float dy = (float)dY[row * lddy + column];
-        dg += dy * (((float)X[row * ldx + column] - mean[row]) * rstd[row]);
-        db += dy;
+        float x[V], dy[V];
+        load_piece<V>(x, X + row * ldx + p.at);
+        load_piece<V>(dy, dY + row * lddy + p.at);
+        const float m = mean[row], r = rstd[row];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            dg[j] += dy[j] * ((x[j] - m) * r);
+            db[j] += dy[j];
+        }
     }
-    float* out = parts + (int64_t)blockIdx.y * 2 * k;
-    out[column] = dg;
-    out[k + column] = db;
+    float* out = parts + (int64_t)blockIdx.y * 2 * k + p.at;
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+        if (p.counts(j)) {
+            out[j] = dg[j];
+            out[k + j] = db[j];
+        }
 }
 
 // dg and db from `count` partial rows of each, in a fixed order: 32 columns a workgroup, the partial rows shared by its 32 groups of lanes.
@@ -395,7 +411,8 @@ cbm_status cbm_launch_norm(int64_t n, int32_t k, int32_t type, const void* X_, i
         else if (pieces <= 256) CBM_NORM(V, 256, 1);
         else if (pieces <= 512) CBM_NORM(V, 256, 2);
         else if (pieces <= 1024) CBM_NORM(V, 512, 2);
-        else if (pieces <= 2048) CBM_NORM(V, 1024, 2);
+        else if (V == 4 && pieces <= 2048) CBM_NORM(V, 1024, 2);
+        else if (k <= 16384) CBM_NORM(V, 1024, 16 / V);
         else hipLaunchKernelGGL((cbm_norm_wide_kernel<T, V, WHOLE>), dim3((unsigned)std::min<int64_t>(n, 512)), dim3(1024), 0, stream, n, k, X, ldx, gamma, beta, eps, Y, ldy, mean, rstd);
 #undef CBM_NORM
     });
@@ -429,11 +446,14 @@ cbm_status cbm_launch_norm_backward(int64_t n, int32_t k, int32_t type, const vo
             else if (pieces <= 256) CBM_BACK(V, 256, 1, 256);
             else if (pieces <= 512) CBM_BACK(V, 256, 2, 256);
             else if (pieces <= 1024) CBM_BACK(V, 512, 2, 512);
-            else if (pieces <= 2048) CBM_BACK(V, 1024, 2, 1024);
+            else if (V == 4 && pieces <= 2048) CBM_BACK(V, 1024, 2, 1024);
+            else if (pieces <= (V == 4 ? 3072 : 2048)) CBM_BACK(V, 1024, V == 4 ? 3 : 2, 1024);
             else {
                 if (dX) hipLaunchKernelGGL((cbm_norm_back_wide_kernel<T, V, WHOLE>), dim3((unsigned)std::min<int64_t>(n, 512)), dim3(1024), 0, stream, n, k, dY, lddy, X, ldx, gamma, mean, rstd, dX, lddx);
-                count = std::min<int64_t>(most, 64);
-                if (parts) hipLaunchKernelGGL((cbm_norm_back_columns_kernel<T>), dim3((unsigned)((k + 255) / 256), (unsigned)count), dim3(256), 0, stream, n, k, dY, lddy, X, ldx, mean, rstd, parts);
+                const int64_t across = (pieces + 255) / 256;
+                count = std::min<int64_t>(most, std::max<int64_t>(1, 2048 / across));
+                if (parts)
+                    cbm_norm_back_columns_kernel<T, V, WHOLE><<<dim3((unsigned)across, (unsigned)count), 256, 0, stream>>>(n, k, dY, lddy, X, ldx, mean, rstd, parts);
             }
 #undef CBM_BACK
         });
