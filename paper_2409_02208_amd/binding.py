@@ -278,26 +278,31 @@ def cbm_gcn2_forward(h: Handle, X, W0, W1, out, workspace, stream=None):
 
 def _matrix(t, name, dtypes=None):
     """(address, leading dimension, rows, columns, cbm_dtype) of a device matrix of one of the operators' types, or of `dtypes`."""
-    dtypes = _DTYPES if dtypes is None else dtypes
-    code = dtypes.get(t.dtype) if t.is_cuda else None
-    strides = t.stride() if code is not None else ()
-    if len(strides) != 2 or (strides[1] != 1 and t.shape[1] > 1):
-        raise ValueError(f"{name} must be a 2-D device tensor of {', '.join(str(d) for d in dtypes)} with unit column stride")
-    rows, cols = t.shape
-    return t.data_ptr(), max(strides[0], cols) if rows <= 1 else strides[0], rows, cols, code
+    code = (_DTYPES if dtypes is None else dtypes).get(t.dtype)
+    if code is not None and t.is_cuda:
+        strides = t.stride()
+        if len(strides) == 2:
+            rows, cols = t.shape
+            if strides[1] == 1 or cols <= 1:
+                return t.data_ptr(), strides[0] if rows > 1 else max(strides[0], cols), rows, cols, code
+    raise ValueError(f"{name} must be a 2-D device tensor of {', '.join(str(d) for d in dtypes or _DTYPES)} with unit column stride")
 
 
 def _vector(t, name, size, dtype=None):
     """Address of a packed device vector of `size` values (fp32 unless said otherwise); None stays None."""
     if t is None:
         return None
-    if not t.is_cuda or t.dtype is not (dtype or _F32) or t.dim() != 1 or t.shape[0] != size or (size > 1 and t.stride(0) != 1):
-        raise ValueError(f"{name} must be a packed device vector of {size} {dtype or _F32} values")
-    return t.data_ptr()
+    if t.dtype is (dtype or _F32) and t.is_cuda and t.shape == (size,) and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name} must be a packed device vector of {size} {dtype or _F32} values")
 
 
 def _workspace(t):
-    return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
+    if t is None:
+        return None, 0
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("workspace must be a packed device tensor")
+    return t.data_ptr(), t.nbytes
 
 
 def _same(shape_and_type, other, what):
@@ -405,9 +410,9 @@ def _packed(t, name, rows, cols, dtype):
     """Address of a packed device matrix of rows x cols; None stays None."""
     if t is None:
         return None
-    if not t.is_cuda or t.dtype is not dtype or tuple(t.shape) != (rows, cols) or not t.is_contiguous():
-        raise ValueError(f"{name} must be a packed {rows} x {cols} device matrix of {dtype}")
-    return t.data_ptr()
+    if t.dtype is dtype and t.is_cuda and t.shape == (rows, cols) and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name} must be a packed {rows} x {cols} device matrix of {dtype}")
 
 
 def cbm_log_probs_workspace_bytes(n: int, c: int, top: int = 0) -> int:

@@ -58,26 +58,42 @@ __device__ __forceinline__ uint32_t lane_moved(uint32_t v) {
 }
 template <int STEP>  // the value of the lane at distance STEP of a butterfly whose smaller steps are done
 __device__ __forceinline__ uint32_t lane_other(uint32_t v) {
-    static_assert(STEP >= 1 && STEP <= 32, "");
-    if constexpr (STEP == 1) return lane_moved<0xb1>(v);         // quad_perm 1 0 3 2
-    else if constexpr (STEP == 2) return lane_moved<0x4e>(v);    // quad_perm 2 3 0 1
-    else if constexpr (STEP == 4) return lane_moved<0x141>(v);   // row_half_mirror: all four lanes of a quad are alike by now
-    else if constexpr (STEP == 8) return lane_moved<0x140>(v);   // row_mirror
-    else return (uint32_t)__shfl_xor((int)v, STEP);
+    static_assert(STEP == 1 || STEP == 2 || STEP == 4 || STEP == 8, "");
+    if constexpr (STEP == 1) return lane_moved<0xb1>(v);        // quad_perm 1 0 3 2
+    else if constexpr (STEP == 2) return lane_moved<0x4e>(v);   // quad_perm 2 3 0 1
+    else if constexpr (STEP == 4) return lane_moved<0x141>(v);  // row_half_mirror: all four lanes of a quad are alike by now
+    else return lane_moved<0x140>(v);                           // row_mirror
 }
 template <int STEP>
 __device__ __forceinline__ float lane_other(float v) {
     return __uint_as_float(lane_other<STEP>(__float_as_uint(v)));
 }
+// f(v of the lane's even row, or half, v of its odd one): both lanes of a pair have the same two values, in the same order
+template <int STEP, class U, class F>
+__device__ __forceinline__ U lane_pair(U v, F&& f) {
+    static_assert(STEP == 16 || STEP == 32, "");
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    if constexpr (STEP == 16) {
+        const auto both = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        return f(__builtin_bit_cast(U, (uint32_t)both[0]), __builtin_bit_cast(U, (uint32_t)both[1]));
+    } else {
+        const auto both = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        return f(__builtin_bit_cast(U, (uint32_t)both[0]), __builtin_bit_cast(U, (uint32_t)both[1]));
+    }
+}
+template <int LANES, class U, class F>
+__device__ __forceinline__ U lanes_all(U v, F&& f) {
+    if constexpr (LANES >= 2) v = f(v, lane_other<1>(v));
+    if constexpr (LANES >= 4) v = f(v, lane_other<2>(v));
+    if constexpr (LANES >= 8) v = f(v, lane_other<4>(v));
+    if constexpr (LANES >= 16) v = f(v, lane_other<8>(v));
+    if constexpr (LANES >= 32) v = lane_pair<16>(v, f);
+    if constexpr (LANES >= 64) v = lane_pair<32>(v, f);
+    return v;
+}
 template <int LANES>
 __device__ __forceinline__ float lanes_sum(float v) {
-    if constexpr (LANES >= 2) v += lane_other<1>(v);
-    if constexpr (LANES >= 4) v += lane_other<2>(v);
-    if constexpr (LANES >= 8) v += lane_other<4>(v);
-    if constexpr (LANES >= 16) v += lane_other<8>(v);
-    if constexpr (LANES >= 32) v += lane_other<16>(v);
-    if constexpr (LANES >= 64) v += lane_other<32>(v);
-    return v;
+    return lanes_all<LANES>(v, [](float a, float b) { return a + b; });
 }
 
 // f(one of float, __bf16, _Float16), by a cbm_dtype; false: there is no such type

@@ -64,17 +64,13 @@ __device__ __forceinline__ void finish(float& m, float s, float t, float& l, flo
     }
 }
 
-__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
-__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return max(a, b); }
-template <int LANES, class U>
-__device__ __forceinline__ U lanes_max(U v) {
-    if constexpr (LANES >= 2) v = larger(v, lane_other<1>(v));
-    if constexpr (LANES >= 4) v = larger(v, lane_other<2>(v));
-    if constexpr (LANES >= 8) v = larger(v, lane_other<4>(v));
-    if constexpr (LANES >= 16) v = larger(v, lane_other<8>(v));
-    if constexpr (LANES >= 32) v = larger(v, lane_other<16>(v));
-    if constexpr (LANES >= 64) v = larger(v, lane_other<32>(v));
-    return v;
+template <int LANES>
+__device__ __forceinline__ float lanes_max(float v) {
+    return lanes_all<LANES>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int LANES>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
+    return lanes_all<LANES>(v, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
 
 // The largest whole number that at least `top` lanes of the wave have or exceed, bit by bit; the smallest that is an alternative where fewer lanes have one.
