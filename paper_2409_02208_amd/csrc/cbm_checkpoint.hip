@@ -95,7 +95,7 @@ __global__ __launch_bounds__(256) void cbm_checkpoint_save_kernel(int64_t n, int
 // GATED: dx = q > 0 ? dy : 0, else x~.
 template <class T, int LANES, bool GATED>
 __global__ __launch_bounds__(256) void cbm_checkpoint_load_kernel(int64_t n, int k, const int8_t* __restrict__ Q, int64_t ldq, const uint8_t* __restrict__ E, int64_t lde, const T* dY,
-                                                                  int64_t lddy, T* out, int64_t ldo, int turns) {
+                                                                  int64_t lddy, T* out, int64_t ldo, int turns, bool far) {
     constexpr int V = 16 / (int)sizeof(T);
     const int lane = threadIdx.x % LANES;
     const int pieces = (k + V - 1) / V;
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256) void cbm_checkpoint_load_kernel(int64_t n, int
         for (int j = 0; j < V; ++j) x[j] = !GATED ? value_of(q[j], code) : code == NOT_FINITE ? NAN : q[j] > 0 ? x[j] : 0.0f;
         T* to = out + row * ldo + p.at;
         if (p.seen == 0) {
-            store_piece<V>(to, x);
+            store_piece<V>(to, x, far);
         } else {
 #pragma unroll
             for (int j = 0; j < V; ++j)
@@ -406,8 +406,9 @@ cbm_status cbm_launch_checkpoint_load(int64_t n, int32_t k, const int8_t* Q, int
         constexpr int V = 16 / (int)sizeof(T);
         along_rows(n, ((int64_t)k + V - 1) / V, [&](auto lanes, dim3 grid, int turns) {
             constexpr int LANES = decltype(lanes)::value;
-            if (dY) cbm_checkpoint_load_kernel<T, LANES, true><<<grid, 256, 0, (hipStream_t)stream>>>(n, k, Q, ldq, E, lde, (const T*)dY, lddy, (T*)out, ldo, turns);
-            else cbm_checkpoint_load_kernel<T, LANES, false><<<grid, 256, 0, (hipStream_t)stream>>>(n, k, Q, ldq, E, lde, nullptr, 0, (T*)out, ldo, turns);
+            const bool far = n * k * (int64_t)sizeof(T) >= CBM_FAR_BYTES;
+            if (dY) cbm_checkpoint_load_kernel<T, LANES, true><<<grid, 256, 0, (hipStream_t)stream>>>(n, k, Q, ldq, E, lde, (const T*)dY, lddy, (T*)out, ldo, turns, far);
+            else cbm_checkpoint_load_kernel<T, LANES, false><<<grid, 256, 0, (hipStream_t)stream>>>(n, k, Q, ldq, E, lde, nullptr, 0, (T*)out, ldo, turns, far);
         });
     });
     return launched("checkpoint load launch");

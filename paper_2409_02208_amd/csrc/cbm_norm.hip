@@ -51,7 +51,7 @@ __device__ __forceinline__ void row_sum2(float& a, float& b, floatx2* room, int&
 template <class T, int V, int LANES, int R, bool WHOLE>
 __global__ __launch_bounds__(LANES > NORM_THREADS ? LANES : NORM_THREADS) void cbm_norm_kernel(int64_t n, int k, const T* __restrict__ X, int64_t ldx, const float* __restrict__ gamma,
                                                                                               const float* __restrict__ beta, float eps, T* __restrict__ Y, int64_t ldy,
-                                                                                              float* __restrict__ mean, float* __restrict__ rstd) {
+                                                                                              float* __restrict__ mean, float* __restrict__ rstd, bool far) {
     constexpr int THREADS = LANES > NORM_THREADS ? LANES : NORM_THREADS, ROWS = THREADS / LANES;
     __shared__ floatx2 room[LANES > 64 ? 2 * (LANES / 64) : 1];
     const int lane = threadIdx.x % LANES;
@@ -108,7 +108,7 @@ __global__ __launch_bounds__(LANES > NORM_THREADS ? LANES : NORM_THREADS) void c
             float y[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) y[j] = x[c][j] * r * g[c][j] + b[c][j];
-            if (p.any()) store_piece<V>(y_row + p.at, y);
+            if (p.any()) store_piece<V>(y_row + p.at, y, far);
         }
         if (lane == 0) {
             if (mean) mean[row] = m;
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(LANES > NORM_THREADS ? LANES : NORM_THREADS) void c
 // Rows too wide for registers: a workgroup reads its row three times (all but the first time out of L2).
 template <class T, int V, bool WHOLE>
 __global__ __launch_bounds__(1024) void cbm_norm_wide_kernel(int64_t n, int k, const T* __restrict__ X, int64_t ldx, const float* __restrict__ gamma, const float* __restrict__ beta,
-                                                             float eps, T* __restrict__ Y, int64_t ldy, float* __restrict__ mean, float* __restrict__ rstd) {
+                                                             float eps, T* __restrict__ Y, int64_t ldy, float* __restrict__ mean, float* __restrict__ rstd, bool far) {
     __shared__ floatx2 room[32];
     int turn = 0;
     const int pieces = (k + V - 1) / V;
@@ -149,7 +149,7 @@ __global__ __launch_bounds__(1024) void cbm_norm_wide_kernel(int64_t n, int k, c
             load_piece<V>(x, x_row + p.at);
 #pragma unroll
             for (int j = 0; j < V; ++j) x[j] = (x[j] - m) * r * (gamma ? gamma[p.at + j] : 1.0f) + (beta ? beta[p.at + j] : 0.0f);
-            store_piece<V>(Y + row * ldy + p.at, x);
+            store_piece<V>(Y + row * ldy + p.at, x, far);
         }
         if (threadIdx.x == 0) {
             if (mean) mean[row] = m;
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(1024) void cbm_norm_wide_kernel(int64_t n, int k, c
 template <class T, int V, int LANES, int R, int THREADS, bool WHOLE>
 __global__ __launch_bounds__(THREADS) void cbm_norm_back_kernel(int64_t n, int k, const T* __restrict__ dY, int64_t lddy, const T* __restrict__ X, int64_t ldx,
                                                                 const float* __restrict__ gamma, const float* __restrict__ mean, const float* __restrict__ rstd,
-                                                                T* __restrict__ dX, int64_t lddx, float* __restrict__ parts) {
+                                                                T* __restrict__ dX, int64_t lddx, float* __restrict__ parts, bool far) {
     constexpr int ROWS = THREADS / LANES;
     constexpr int COLUMNS = LANES * R * V;
     __shared__ floatx2 room[LANES > 64 ? 2 * (LANES / 64) : (THREADS / 64) * COLUMNS];
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(THREADS) void cbm_norm_back_kernel(int64_t n, int k
             float dx[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) dx[j] = r * (u[c][j] - sum - h[c][j] * along);
-            if (p.any()) store_piece<V>(dX + row * lddx + p.at, dx);
+            if (p.any()) store_piece<V>(dX + row * lddx + p.at, dx, (WHOLE || R * V < 16) && far);  // (as far as registers go)
         }
     }
     if (!parts) return;
@@ -286,7 +286,7 @@ __global__ __launch_bounds__(THREADS) void cbm_norm_back_kernel(int64_t n, int k
 template <class T, int V, bool WHOLE>
 __global__ __launch_bounds__(1024) void cbm_norm_back_wide_kernel(int64_t n, int k, const T* __restrict__ dY, int64_t lddy, const T* __restrict__ X, int64_t ldx,
                                                                   const float* __restrict__ gamma, const float* __restrict__ mean, const float* __restrict__ rstd,
-                                                                  T* __restrict__ dX, int64_t lddx) {
+                                                                  T* __restrict__ dX, int64_t lddx, bool far) {
     __shared__ floatx2 room[32];
     int turn = 0;
     const int pieces = (k + V - 1) / V;
@@ -313,7 +313,7 @@ __global__ __launch_bounds__(1024) void cbm_norm_back_wide_kernel(int64_t n, int
             load_piece<V>(dy, dY + row * lddy + p.at);
 #pragma unroll
             for (int j = 0; j < V; ++j) x[j] = r * (dy[j] * (gamma ? gamma[p.at + j] : 1.0f) - sum - (x[j] - m) * r * along);
-            store_piece<V>(dX + row * lddx + p.at, x);
+            store_piece<V>(dX + row * lddx + p.at, x, far);
         }
     }
 }
@@ -398,9 +398,10 @@ cbm_status cbm_launch_norm(int64_t n, int32_t k, int32_t type, const void* X_, i
         T* Y = (T*)Y_;
         constexpr int V = 16 / (int)sizeof(T);
         const int64_t pieces = ((int64_t)k + V - 1) / V;
+        const bool far = n * k * (int64_t)sizeof(T) >= CBM_FAR_BYTES;
 #define CBM_NORM(V_, LANES, R)                                                                                                                                              \
     hipLaunchKernelGGL((cbm_norm_kernel<T, V_, LANES, R, WHOLE>), dim3((unsigned)at_most(n, (LANES > NORM_THREADS ? LANES : NORM_THREADS) / LANES, 256 * (LANES > NORM_THREADS ? 2 : 8))), \
-                       dim3(LANES > NORM_THREADS ? LANES : NORM_THREADS), 0, stream, n, k, X, ldx, gamma, beta, eps, Y, ldy, mean, rstd)
+                       dim3(LANES > NORM_THREADS ? LANES : NORM_THREADS), 0, stream, n, k, X, ldx, gamma, beta, eps, Y, ldy, mean, rstd, far)
         if (k < V) CBM_NORM(1, 8, 1);  // (V = 1: every place is whole)
         else if (pieces <= 4) CBM_NORM(V, 4, 1);
         else if (pieces <= 8) CBM_NORM(V, 8, 1);
@@ -413,7 +414,7 @@ cbm_status cbm_launch_norm(int64_t n, int32_t k, int32_t type, const void* X_, i
         else if (pieces <= 1024) CBM_NORM(V, 512, 2);
         else if (V == 4 && pieces <= 2048) CBM_NORM(V, 1024, 2);
         else if (k <= 16384) CBM_NORM(V, 1024, 16 / V);
-        else hipLaunchKernelGGL((cbm_norm_wide_kernel<T, V, WHOLE>), dim3((unsigned)std::min<int64_t>(n, 512)), dim3(1024), 0, stream, n, k, X, ldx, gamma, beta, eps, Y, ldy, mean, rstd);
+        else hipLaunchKernelGGL((cbm_norm_wide_kernel<T, V, WHOLE>), dim3((unsigned)std::min<int64_t>(n, 512)), dim3(1024), 0, stream, n, k, X, ldx, gamma, beta, eps, Y, ldy, mean, rstd, far);
 #undef CBM_NORM
     });
     return launched("layer norm launch");
@@ -433,9 +434,10 @@ cbm_status cbm_launch_norm_backward(int64_t n, int32_t k, int32_t type, const vo
             T* dX = (T*)dX_;
             constexpr int V = 16 / (int)sizeof(T);
             const int64_t pieces = ((int64_t)k + V - 1) / V;
+            const bool far = n * k * (int64_t)sizeof(T) >= CBM_FAR_BYTES;
 #define CBM_BACK(V_, LANES, R, THREADS)                                                                                                                                    \
     cbm_norm_back_kernel<T, V_, LANES, R, THREADS, WHOLE><<<(unsigned)(count = at_most(n, THREADS / LANES, most)), THREADS, 0, stream>>>(n, k, dY, lddy, X, ldx, gamma, mean, rstd, dX, lddx, \
-                                                                                                                                 parts)
+                                                                                                                                 parts, far)
             if (k < V) CBM_BACK(1, 8, 1, BACK_THREADS);
             else if (pieces <= 4) CBM_BACK(V, 4, 1, BACK_THREADS);
             else if (pieces <= 8) CBM_BACK(V, 8, 1, BACK_THREADS);
@@ -449,7 +451,7 @@ cbm_status cbm_launch_norm_backward(int64_t n, int32_t k, int32_t type, const vo
             else if (V == 4 && pieces <= 2048) CBM_BACK(V, 1024, 2, 1024);
             else if (pieces <= (V == 4 ? 3072 : 2048)) CBM_BACK(V, 1024, V == 4 ? 3 : 2, 1024);
             else {
-                if (dX) hipLaunchKernelGGL((cbm_norm_back_wide_kernel<T, V, WHOLE>), dim3((unsigned)std::min<int64_t>(n, 512)), dim3(1024), 0, stream, n, k, dY, lddy, X, ldx, gamma, mean, rstd, dX, lddx);
+                if (dX) hipLaunchKernelGGL((cbm_norm_back_wide_kernel<T, V, WHOLE>), dim3((unsigned)std::min<int64_t>(n, 512)), dim3(1024), 0, stream, n, k, dY, lddy, X, ldx, gamma, mean, rstd, dX, lddx, far);
                 const int64_t across = (pieces + 255) / 256;
                 count = std::min<int64_t>(most, std::max<int64_t>(1, 2048 / across));
                 if (parts)

@@ -535,7 +535,7 @@ struct Slopes {
 };
 // LANES lanes a row and a share of its columns (blockIdx.y), V columns a lane and turn.
 template <class T, int V, int LANES>
-__global__ __launch_bounds__(256) void cbm_scores_back_kernel(Slopes a, int turns) {
+__global__ __launch_bounds__(256) void cbm_scores_back_kernel(Slopes a, int turns, bool far) {
     const int lane = threadIdx.x % LANES, pieces = (a.c + V - 1) / V;
     for (int64_t row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES; row < a.n; row += (int64_t)gridDim.x * (256 / LANES)) {
         const float m = a.stats[2 * row], l = a.stats[2 * row + 1];
@@ -558,7 +558,7 @@ __global__ __launch_bounds__(256) void cbm_scores_back_kernel(Slopes a, int turn
                 x[j] = empty ? 0.0f : v;
             }
             if (p.seen == 0) {
-                store_piece<V>(out + p.at, x);
+                store_piece<V>(out + p.at, x, far);
             } else {  // (the other values are another lane's, which may not have read them yet where dz is z)
 #pragma unroll
                 for (int j = 0; j < V; ++j)
@@ -635,11 +635,12 @@ cbm_status cbm_launch_scores_backward(int64_t n, int32_t c, int32_t type, const 
         using T = decltype(t);
         constexpr int V = 16 / (int)sizeof(T);
         const int64_t pieces = (c + V - 1) / V;
+        const bool far = n * c * (int64_t)sizeof(T) >= CBM_FAR_BYTES;
 #define CBM_BACK(V_, LANES)                                                                                                                                                  \
     {                                                                                                                                                                        \
         const int turns = pieces <= LANES ? 1 : 4;                                                                                                                           \
         cbm_scores_back_kernel<T, V_, LANES><<<dim3((unsigned)std::min<int64_t>((n + 256 / LANES - 1) / (256 / LANES), 1 << 23),                                             \
-                                                    (unsigned)((pieces + LANES * turns - 1) / (LANES * turns))), 256, 0, stream>>>(a, turns);                                \
+                                                    (unsigned)((pieces + LANES * turns - 1) / (LANES * turns))), 256, 0, stream>>>(a, turns, far);                              \
     }
         if (c < V) CBM_BACK(1, 8)
         else if (pieces <= 4) CBM_BACK(V, 4)
