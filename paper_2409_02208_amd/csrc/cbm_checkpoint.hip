@@ -41,83 +41,91 @@ __device__ __forceinline__ void load_row_bytes(int (&q)[V], const int8_t* row, c
     }
 }
 
-// LANES lanes a row (and a share of its columns: blockIdx.y), V columns a lane and turn.  A block of 32 columns is 32 / V lanes.
-template <class T, int LANES>
+// LANES lanes a row (and a share of its columns: blockIdx.y), R times V columns a lane.  A block of 32 columns is 32 / V lanes.
+template <class T, int LANES, int R>
 __global__ __launch_bounds__(256) void cbm_checkpoint_save_kernel(int64_t n, int k, const T* __restrict__ X, int64_t ldx, int8_t* __restrict__ Q, int64_t ldq,
-                                                                  uint8_t* __restrict__ E, int64_t lde, int turns) {
+                                                                  uint8_t* __restrict__ E, int64_t lde) {
     constexpr int V = 16 / (int)sizeof(T), PER_BLOCK = BLOCK / V;
-    const int lane = threadIdx.x % LANES;
-    const int pieces = (k + V - 1) / V;
-    for (int64_t row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES; row < n; row += (int64_t)gridDim.x * (256 / LANES))  // (the lanes of a block of columns together)
-    for (int turn = 0; turn < turns; ++turn) {
-        const int c = (blockIdx.y * turns + turn) * LANES + lane;
-        if (c / PER_BLOCK * PER_BLOCK >= pieces) break;  // (likewise)
-        const Place<V, false> p(c, k);
-        float x[V];
-        load_row_piece<V>(x, X + row * ldx, p, k);
-        // the largest size by its bits, which order sizes, infinity and NaN as they should
-        uint32_t largest = 0;
+    const int lane = threadIdx.x % LANES, first = blockIdx.y * R * LANES + lane, blocks = (k + BLOCK - 1) / BLOCK;
+    for (int64_t row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES; row < n; row += (int64_t)gridDim.x * (256 / LANES)) {
+        float x[R][V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) largest = max(largest, p.counts(j) ? __float_as_uint(x[j]) & 0x7fffffffu : 0u);
-        largest = max(largest, lane_other<1>(largest));
-        largest = max(largest, lane_other<2>(largest));
-        if constexpr (PER_BLOCK == 8) largest = max(largest, lane_other<4>(largest));
-        const bool finite = largest < 0x7f800000u;
-        const uint32_t code = finite ? (uint32_t)max((int)(largest >> 23) - 6, 1) : NOT_FINITE;
-        const float up = __uint_as_float((254u - (finite ? code : 127u)) << 23);
-        uint32_t packed[V / 4];
+        for (int i = 0; i < R; ++i) load_row_piece<V>(x[i], X + row * ldx, Place<V, false>(first + i * LANES, k), k);
 #pragma unroll
-        for (int w = 0; w < V / 4; ++w) {
-            packed[w] = 0;
+        for (int i = 0; i < R; ++i) {
+            int c = first + i * LANES;
+            asm volatile("" : "+v"(c));  // (every row's comparisons anew: kept from row to row they are more than the scalar registers hold)
+            const Place<V, false> p(c, k);
+            // the largest size by its bits, which order sizes, infinity and NaN as they should
+            uint32_t largest = 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float v = x[4 * w + i], size = fminf(fmaxf(rintf(fabsf(v) * up), 1.0f), 127.0f);
-                const int q = v == 0.0f || !finite ? 0 : (int)copysignf(size, v);
-                packed[w] |= ((uint32_t)q & 255u) << (8 * i);
+            for (int j = 0; j < V; ++j) largest = max(largest, p.counts(j) ? __float_as_uint(x[i][j]) & 0x7fffffffu : 0u);
+            largest = max(largest, lane_other<1>(largest));
+            largest = max(largest, lane_other<2>(largest));
+            if constexpr (PER_BLOCK == 8) largest = max(largest, lane_other<4>(largest));
+            const bool finite = largest < 0x7f800000u;
+            const uint32_t code = finite ? (uint32_t)max((int)(largest >> 23) - 6, 1) : NOT_FINITE;
+            const float up = __uint_as_float((254u - (finite ? code : 127u)) << 23);
+            uint32_t packed[V / 4];
+#pragma unroll
+            for (int w = 0; w < V / 4; ++w) {
+                packed[w] = 0;
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const float v = x[i][4 * w + b], size = fminf(fmaxf(rintf(fabsf(v) * up), 1.0f), 127.0f);
+                    const int q = v == 0.0f || !finite ? 0 : (int)copysignf(size, v);
+                    packed[w] |= ((uint32_t)q & 255u) << (8 * b);
+                }
             }
-        }
-        int8_t* out = Q + row * ldq + p.at;
-        if (p.seen == 0) {
-            typedef uint32_t Words __attribute__((ext_vector_type(V / 4), aligned(1)));
-            Words words;
+            int8_t* out = Q + row * ldq + p.at;
+            if (p.seen <= 0) {
+                typedef uint32_t Words __attribute__((ext_vector_type(V / 4), aligned(1)));
+                Words words;
 #pragma unroll
-            for (int w = 0; w < V / 4; ++w) words[w] = packed[w];
-            *reinterpret_cast<Words*>(out) = words;
-        } else if (p.any()) {
+                for (int w = 0; w < V / 4; ++w) words[w] = packed[w];
+                *reinterpret_cast<Words*>(out) = words;
+            } else if (p.any()) {
 #pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (p.counts(j)) out[j] = (int8_t)(packed[j / 4] >> (8 * (j % 4)));
+                for (int j = 0; j < V; ++j)
+                    if (p.counts(j)) out[j] = (int8_t)(packed[j / 4] >> (8 * (j % 4)));
+            }
+            if (c % PER_BLOCK == 0 && c / PER_BLOCK < blocks) E[row * lde + c / PER_BLOCK] = (uint8_t)code;
         }
-        if (c % PER_BLOCK == 0) E[row * lde + c / PER_BLOCK] = (uint8_t)code;
     }
 }
 
 // GATED: dx = q > 0 ? dy : 0, else x~.
-template <class T, int LANES, bool GATED>
+template <class T, int LANES, int R, bool GATED>
 __global__ __launch_bounds__(256) void cbm_checkpoint_load_kernel(int64_t n, int k, const int8_t* __restrict__ Q, int64_t ldq, const uint8_t* __restrict__ E, int64_t lde, const T* dY,
-                                                                  int64_t lddy, T* out, int64_t ldo, int turns, bool far) {
+                                                                  int64_t lddy, T* out, int64_t ldo, bool far) {
     constexpr int V = 16 / (int)sizeof(T);
-    const int lane = threadIdx.x % LANES;
-    const int pieces = (k + V - 1) / V;
-    for (int64_t row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES; row < n; row += (int64_t)gridDim.x * (256 / LANES))
-    for (int turn = 0; turn < turns; ++turn) {
-        const int c = (blockIdx.y * turns + turn) * LANES + lane;
-        if (c >= pieces) break;
-        const Place<V, false> p(c, k);
-        int q[V];
-        float x[V];
-        load_row_bytes<V>(q, Q + row * ldq, p, k);
-        if constexpr (GATED) load_row_piece<V>(x, dY + row * lddy, p, k);
-        const uint32_t code = E[row * lde + c * V / BLOCK];
+    const int lane = threadIdx.x % LANES, first = blockIdx.y * R * LANES + lane, blocks = (k + BLOCK - 1) / BLOCK;
+    for (int64_t row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES; row < n; row += (int64_t)gridDim.x * (256 / LANES)) {
+        int q[R][V];
+        float x[R][V];
+        uint32_t code[R];
 #pragma unroll
-        for (int j = 0; j < V; ++j) x[j] = !GATED ? value_of(q[j], code) : code == NOT_FINITE ? NAN : q[j] > 0 ? x[j] : 0.0f;
-        T* to = out + row * ldo + p.at;
-        if (p.seen == 0) {
-            store_piece<V>(to, x, far);
-        } else {
+        for (int i = 0; i < R; ++i) {
+            const Place<V, false> p(first + i * LANES, k);
+            load_row_bytes<V>(q[i], Q + row * ldq, p, k);
+            if constexpr (GATED) load_row_piece<V>(x[i], dY + row * lddy, p, k);
+            code[i] = E[row * lde + min((first + i * LANES) * V / BLOCK, blocks - 1)];
+        }
 #pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (p.counts(j)) to[j] = (T)x[j];
+        for (int i = 0; i < R; ++i) {
+            int c = first + i * LANES;
+            asm volatile("" : "+v"(c));  // (as above)
+            const Place<V, false> p(c, k);
+#pragma unroll
+            for (int j = 0; j < V; ++j) x[i][j] = !GATED ? value_of(q[i][j], code[i]) : code[i] == NOT_FINITE ? NAN : q[i][j] > 0 ? x[i][j] : 0.0f;
+            T* to = out + row * ldo + p.at;
+            if (p.seen <= 0) {
+                store_piece<V>(to, x[i], far);
+            } else if (p.any()) {
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (p.counts(j)) to[j] = (T)x[i][j];
+            }
         }
     }
 }
@@ -365,18 +373,19 @@ cbm_status launched(const char* what) {
     return CBM_ERR_HIP;
 }
 
-// f(lanes a row, workgroups, turns a workgroup) for rows of `pieces` pieces
+// f(lanes a row, pieces a lane, workgroups) for rows of `pieces` pieces
 template <class F>
 void along_rows(int64_t n, int64_t pieces, F&& f) {
-    auto go = [&](auto lanes) {
-        constexpr int LANES = decltype(lanes)::value;
-        const int turns = pieces <= LANES ? 1 : 4;
-        f(lanes, dim3((unsigned)std::min<int64_t>((n + 256 / LANES - 1) / (256 / LANES), 1 << 23), (unsigned)((pieces + LANES * turns - 1) / (LANES * turns))), turns);
+    auto go = [&](auto lanes, auto each) {
+        constexpr int ROWS = 256 / decltype(lanes)::value, AT_ONCE = decltype(lanes)::value * decltype(each)::value;
+        f(lanes, each, dim3((unsigned)std::min<int64_t>((n + ROWS - 1) / ROWS, 1 << 23), (unsigned)((pieces + AT_ONCE - 1) / AT_ONCE)));
     };
-    if (pieces <= 8) go(std::integral_constant<int, 8>{});
-    else if (pieces <= 16) go(std::integral_constant<int, 16>{});
-    else if (pieces <= 32) go(std::integral_constant<int, 32>{});
-    else go(std::integral_constant<int, 64>{});
+    using std::integral_constant;
+    if (pieces <= 8) go(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+    else if (pieces <= 16) go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+    else if (pieces <= 32) go(integral_constant<int, 32>{}, integral_constant<int, 1>{});
+    else if (pieces <= 64) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    else go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
 }
 
 }  // namespace
@@ -391,8 +400,8 @@ cbm_status cbm_launch_checkpoint_save(int64_t n, int32_t k, int32_t type, const 
     cbm_with_type(type, [&](auto t) {
         using T = decltype(t);
         constexpr int V = 16 / (int)sizeof(T);
-        along_rows(n, ((int64_t)k + V - 1) / V, [&](auto lanes, dim3 grid, int turns) {
-            cbm_checkpoint_save_kernel<T, decltype(lanes)::value><<<grid, 256, 0, (hipStream_t)stream>>>(n, k, (const T*)X, ldx, Q, ldq, E, lde, turns);
+        along_rows(n, ((int64_t)k + V - 1) / V, [&](auto lanes, auto each, dim3 grid) {
+            cbm_checkpoint_save_kernel<T, decltype(lanes)::value, decltype(each)::value><<<grid, 256, 0, (hipStream_t)stream>>>(n, k, (const T*)X, ldx, Q, ldq, E, lde);
         });
     });
     return launched("checkpoint save launch");
@@ -404,11 +413,11 @@ cbm_status cbm_launch_checkpoint_load(int64_t n, int32_t k, const int8_t* Q, int
     cbm_with_type(type, [&](auto t) {
         using T = decltype(t);
         constexpr int V = 16 / (int)sizeof(T);
-        along_rows(n, ((int64_t)k + V - 1) / V, [&](auto lanes, dim3 grid, int turns) {
-            constexpr int LANES = decltype(lanes)::value;
+        along_rows(n, ((int64_t)k + V - 1) / V, [&](auto lanes, auto each, dim3 grid) {
+            constexpr int LANES = decltype(lanes)::value, R = decltype(each)::value;
             const bool far = n * k * (int64_t)sizeof(T) >= CBM_FAR_BYTES;
-            if (dY) cbm_checkpoint_load_kernel<T, LANES, true><<<grid, 256, 0, (hipStream_t)stream>>>(n, k, Q, ldq, E, lde, (const T*)dY, lddy, (T*)out, ldo, turns, far);
-            else cbm_checkpoint_load_kernel<T, LANES, false><<<grid, 256, 0, (hipStream_t)stream>>>(n, k, Q, ldq, E, lde, nullptr, 0, (T*)out, ldo, turns, far);
+            if (dY) cbm_checkpoint_load_kernel<T, LANES, R, true><<<grid, 256, 0, (hipStream_t)stream>>>(n, k, Q, ldq, E, lde, (const T*)dY, lddy, (T*)out, ldo, far);
+            else cbm_checkpoint_load_kernel<T, LANES, R, false><<<grid, 256, 0, (hipStream_t)stream>>>(n, k, Q, ldq, E, lde, nullptr, 0, (T*)out, ldo, far);
         });
     });
     return launched("checkpoint load launch");
