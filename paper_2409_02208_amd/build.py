@@ -11,7 +11,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libcbm.so")
 SOURCES = ["cbm_api.cpp", "cbm_builder.cpp", "cbm_kernels.hip", "cbm_blocks.hip", "cbm_sums.hip", "cbm_flat.hip", "cbm_gemm.hip", "cbm_gemm_split.hip", "cbm_gemm_held.hip", "cbm_build_kernels.hip",
-           "cbm_api_train.cpp", "cbm_norm.hip", "cbm_checkpoint.hip", "cbm_scores.hip"]
+           "train/cbm_api_train.cpp", "train/cbm_norm.hip", "train/cbm_checkpoint.hip", "train/cbm_scores.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-Wall", "-Wno-unused-result", "-Wno-unused-value"]
@@ -70,7 +70,7 @@ def build(verbose: bool = False) -> str:
     objs = []
     cmds = []
     for src in SOURCES:
-        obj = os.path.join(objdir, src + ".o")
+        obj = os.path.join(objdir, src.replace("/", "_") + ".o")
         objs.append(obj)
         flags = COMMON + (DEVICE + RESOURCES if src.endswith(".hip") else [])
         cmds.append([HIPCC] + flags + ["-c", os.path.join(CSRC, src), "-o", obj])
