@@ -276,47 +276,73 @@ def cbm_gcn2_forward(h: Handle, X, W0, W1, out, workspace, stream=None):
     return out
 
 
-def _matrix(t, name, dtypes=None):
-    """(address, leading dimension, rows, columns, cbm_dtype) of a device matrix of one of the operators' types, or of `dtypes`."""
-    code = (_DTYPES if dtypes is None else dtypes).get(t.dtype)
+# The operators between the products.  A small call's time is this code as much as the launch, so every attribute of a tensor is asked for once, and what is checked
+# is compared in one go.
+def _matrix(t, name, dtypes):
+    """(address, leading dimension, rows, columns, code of its type in `dtypes`) of a device matrix."""
+    code = dtypes.get(t.dtype)
     if code is not None and t.is_cuda:
         strides = t.stride()
         if len(strides) == 2:
             rows, cols = t.shape
-            if strides[1] == 1 or cols <= 1:
-                return t.data_ptr(), strides[0] if rows > 1 else max(strides[0], cols), rows, cols, code
-    raise ValueError(f"{name} must be a 2-D device tensor of {', '.join(str(d) for d in dtypes or _DTYPES)} with unit column stride")
+            ld, unit = strides
+            if unit == 1 or cols <= 1:
+                return t.data_ptr(), ld if rows > 1 or ld > cols else cols, rows, cols, code
+    raise ValueError(f"{name} must be a 2-D device tensor of {', '.join(str(d) for d in dtypes)} with unit column stride")
 
 
-def _vector(t, name, size, dtype=None):
-    """Address of a packed device vector of `size` values (fp32 unless said otherwise); None stays None."""
+def _packed(t, name, shape, dtype):
+    """Address of a packed device tensor; None stays None."""
     if t is None:
         return None
-    if t.dtype is (dtype or _F32) and t.is_cuda and t.shape == (size,) and t.is_contiguous():
+    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
         return t.data_ptr()
-    raise ValueError(f"{name} must be a packed device vector of {size} {dtype or _F32} values")
+    raise ValueError(f"{name} must be a packed device tensor of {dtype} and shape {tuple(shape)}")
 
 
 def _workspace(t):
     if t is None:
         return None, 0
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError("workspace must be a packed device tensor")
-    return t.data_ptr(), t.nbytes
+    if t.is_cuda and t.is_contiguous():
+        return t.data_ptr(), t.nbytes
+    raise ValueError("workspace must be a packed device tensor")
 
 
-def _same(shape_and_type, other, what):
-    if shape_and_type != other:
+def _labels(t, n):
+    """(address, bits) of n labels; none: (None, 64)."""
+    if t is None:
+        return None, 64
+    bits = _LABELS.get(t.dtype)
+    if bits is None:
+        raise ValueError("labels must be int32 or int64")
+    return _packed(t, "labels", (n,), t.dtype), bits
+
+
+def _alike(a, b, what):
+    """Of what _matrix gives: the same rows, columns and type."""
+    if a[2:] != b[2:]:
         raise ValueError(f"{what} must have the same shape and type")
+
+
+def _kept(Q, E):
+    """(arguments, n, k) of an 8-bit checkpoint."""
+    qp, ldq, n, k, _ = _matrix(Q, "Q", _INT8)
+    ep, lde, rows, blocks, _ = _matrix(E, "E", _UINT8)
+    if rows != n or blocks != (k + 31) // 32:
+        raise ValueError("E must have a row for each of Q's and a column for each 32 of Q's")
+    return (qp, ldq, ep, lde), n, k
 
 
 def cbm_layer_norm(X, gamma, beta, eps: float, Y, mean=None, rstd=None, stream=None):
     lib = _LIB or _lib()
-    xp, ldx, n, k, dtype = _matrix(X, "X")
-    yp, ldy, *y = _matrix(Y, "Y")
-    _same([n, k, dtype], y, "X and Y")
-    _check(lib.cbm_layer_norm(n, k, dtype, xp, ldx, _vector(gamma, "gamma", k), _vector(beta, "beta", k), float(eps), yp, ldy, _vector(mean, "mean", n),
-                              _vector(rstd, "rstd", n), _stream_ptr(stream)), "cbm_layer_norm")
+    x, y = _matrix(X, "X", _DTYPES), _matrix(Y, "Y", _DTYPES)
+    _alike(x, y, "X and Y")
+    xp, ldx, n, k, dtype = x
+    rows, cols, f32 = (n,), (k,), _F32
+    status = lib.cbm_layer_norm(n, k, dtype, xp, ldx, _packed(gamma, "gamma", cols, f32), _packed(beta, "beta", cols, f32), eps, y[0], y[1], _packed(mean, "mean", rows, f32),
+                                _packed(rstd, "rstd", rows, f32), _current_stream() if stream is None else _stream_ptr(stream))
+    if status:
+        raise CbmError(status, "cbm_layer_norm")
     return Y
 
 
@@ -326,57 +352,59 @@ def cbm_layer_norm_workspace_bytes(n: int, k: int) -> int:
 
 def cbm_layer_norm_backward(dY, X, gamma, mean, rstd, dX, dgamma, dbeta, workspace, stream=None):
     lib = _LIB or _lib()
-    gp, ldg, n, k, dtype = _matrix(dY, "dY")
-    xp, ldx, *x = _matrix(X, "X")
-    _same([n, k, dtype], x, "dY and X")
+    g, x = _matrix(dY, "dY", _DTYPES), _matrix(X, "X", _DTYPES)
+    _alike(g, x, "dY and X")
+    gp, ldg, n, k, dtype = g
     dp, ldd = None, k
     if dX is not None:
-        dp, ldd, *d = _matrix(dX, "dX")
-        _same([n, k, dtype], d, "dY and dX")
+        d = _matrix(dX, "dX", _DTYPES)
+        _alike(g, d, "dY and dX")
+        dp, ldd = d[:2]
+    rows, cols, f32 = (n,), (k,), _F32
     wp, wbytes = _workspace(workspace)
-    _check(lib.cbm_layer_norm_backward(n, k, dtype, gp, ldg, xp, ldx, _vector(gamma, "gamma", k), _vector(mean, "mean", n), _vector(rstd, "rstd", n), dp, ldd,
-                                       _vector(dgamma, "dgamma", k), _vector(dbeta, "dbeta", k), wp, wbytes, _stream_ptr(stream)), "cbm_layer_norm_backward")
+    status = lib.cbm_layer_norm_backward(n, k, dtype, gp, ldg, x[0], x[1], _packed(gamma, "gamma", cols, f32), _packed(mean, "mean", rows, f32), _packed(rstd, "rstd", rows, f32), dp, ldd,
+                                         _packed(dgamma, "dgamma", cols, f32), _packed(dbeta, "dbeta", cols, f32), wp, wbytes,
+                                         _current_stream() if stream is None else _stream_ptr(stream))
+    if status:
+        raise CbmError(status, "cbm_layer_norm_backward")
     return dX
-
-
-def _kept(Q, E):
-    """(n, k, arguments) of an 8-bit checkpoint."""
-    qp, ldq, n, k, _ = _matrix(Q, "Q", _INT8)
-    ep, lde, rows, blocks, _ = _matrix(E, "E", _UINT8)
-    if rows != n or blocks != (k + 31) // 32:
-        raise ValueError("E must have a row for each of Q's and a column for each 32 of Q's")
-    return n, k, (qp, ldq, ep, lde)
 
 
 def cbm_checkpoint_save(X, Q, E, stream=None):
     lib = _LIB or _lib()
-    xp, ldx, n, k, dtype = _matrix(X, "X")
-    rows, cols, kept = _kept(Q, E)
-    if (rows, cols) != (n, k):
+    xp, ldx, n, k, dtype = _matrix(X, "X", _DTYPES)
+    kept, rows, cols = _kept(Q, E)
+    if rows != n or cols != k:
         raise ValueError("X and Q must have the same shape")
-    _check(lib.cbm_checkpoint_save(n, k, dtype, xp, ldx, *kept, _stream_ptr(stream)), "cbm_checkpoint_save")
+    status = lib.cbm_checkpoint_save(n, k, dtype, xp, ldx, *kept, _current_stream() if stream is None else _stream_ptr(stream))
+    if status:
+        raise CbmError(status, "cbm_checkpoint_save")
     return Q
 
 
 def cbm_checkpoint_restore(Q, E, X, stream=None):
     lib = _LIB or _lib()
-    xp, ldx, n, k, dtype = _matrix(X, "X")
-    rows, cols, kept = _kept(Q, E)
-    if (rows, cols) != (n, k):
+    xp, ldx, n, k, dtype = _matrix(X, "X", _DTYPES)
+    kept, rows, cols = _kept(Q, E)
+    if rows != n or cols != k:
         raise ValueError("X and Q must have the same shape")
-    _check(lib.cbm_checkpoint_restore(n, k, *kept, dtype, xp, ldx, _stream_ptr(stream)), "cbm_checkpoint_restore")
+    status = lib.cbm_checkpoint_restore(n, k, *kept, dtype, xp, ldx, _current_stream() if stream is None else _stream_ptr(stream))
+    if status:
+        raise CbmError(status, "cbm_checkpoint_restore")
     return X
 
 
 def cbm_checkpoint_relu_backward(Q, E, dY, dX, stream=None):
     lib = _LIB or _lib()
-    gp, ldg, n, k, dtype = _matrix(dY, "dY")
-    dp, ldd, *d = _matrix(dX, "dX")
-    _same([n, k, dtype], d, "dY and dX")
-    rows, cols, kept = _kept(Q, E)
-    if (rows, cols) != (n, k):
+    g, d = _matrix(dY, "dY", _DTYPES), _matrix(dX, "dX", _DTYPES)
+    _alike(g, d, "dY and dX")
+    kept, rows, cols = _kept(Q, E)
+    gp, ldg, n, k, dtype = g
+    if rows != n or cols != k:
         raise ValueError("dY and Q must have the same shape")
-    _check(lib.cbm_checkpoint_relu_backward(n, k, *kept, dtype, gp, ldg, dp, ldd, _stream_ptr(stream)), "cbm_checkpoint_relu_backward")
+    status = lib.cbm_checkpoint_relu_backward(n, k, *kept, dtype, gp, ldg, d[0], d[1], _current_stream() if stream is None else _stream_ptr(stream))
+    if status:
+        raise CbmError(status, "cbm_checkpoint_relu_backward")
     return dX
 
 
@@ -386,33 +414,16 @@ def cbm_checkpoint_workspace_bytes(n: int, k: int, c: int) -> int:
 
 def cbm_checkpoint_weight_grad(Q, E, dY, dW, workspace, stream=None):
     lib = _LIB or _lib()
-    gp, ldg, rows, c, dtype = _matrix(dY, "dY")
-    n, k, kept = _kept(Q, E)
+    gp, ldg, rows, c, dtype = _matrix(dY, "dY", _DTYPES)
+    kept, n, k = _kept(Q, E)
     wp, ldw, kw, cw = _dev_f32(dW, "dW")
     if rows != n or kw != k or cw != c:
         raise ValueError("shape mismatch")
     sp, sbytes = _workspace(workspace)
-    _check(lib.cbm_checkpoint_weight_grad(n, k, c, *kept, dtype, gp, ldg, wp, ldw, sp, sbytes, _stream_ptr(stream)), "cbm_checkpoint_weight_grad")
+    status = lib.cbm_checkpoint_weight_grad(n, k, c, *kept, dtype, gp, ldg, wp, ldw, sp, sbytes, _current_stream() if stream is None else _stream_ptr(stream))
+    if status:
+        raise CbmError(status, "cbm_checkpoint_weight_grad")
     return dW
-
-
-def _labels(t, size):
-    """(address, bits) of `size` labels; none: (None, 64)."""
-    if t is None:
-        return None, 64
-    bits = _LABELS.get(t.dtype)
-    if bits is None:
-        raise ValueError("labels must be int32 or int64")
-    return _vector(t, "labels", size, t.dtype), bits
-
-
-def _packed(t, name, rows, cols, dtype):
-    """Address of a packed device matrix of rows x cols; None stays None."""
-    if t is None:
-        return None
-    if t.dtype is dtype and t.is_cuda and t.shape == (rows, cols) and t.is_contiguous():
-        return t.data_ptr()
-    raise ValueError(f"{name} must be a packed {rows} x {cols} device matrix of {dtype}")
 
 
 def cbm_log_probs_workspace_bytes(n: int, c: int, top: int = 0) -> int:
@@ -421,24 +432,31 @@ def cbm_log_probs_workspace_bytes(n: int, c: int, top: int = 0) -> int:
 
 def cbm_log_probs(Z, labels, logp, entropy=None, stats=None, top_values=None, top_columns=None, workspace=None, stream=None):
     lib = _LIB or _lib()
-    zp, ldz, n, c, dtype = _matrix(Z, "Z")
+    zp, ldz, n, c, dtype = _matrix(Z, "Z", _DTYPES)
     lp, bits = _labels(labels, n)
-    top = 0 if top_values is None else top_values.shape[-1]
-    tv, tc = _packed(top_values, "top_values", n, top, _F32), _packed(top_columns, "top_columns", n, top, _INT32)
+    top, tv, tc, f32, rows = 0, None, None, _F32, (n,)
+    if top_values is not None or top_columns is not None:
+        top = (top_columns if top_values is None else top_values).shape[-1]
+        tv, tc = _packed(top_values, "top_values", (n, top), f32), _packed(top_columns, "top_columns", (n, top), _INT32)
     wp, wbytes = _workspace(workspace)
-    _check(lib.cbm_log_probs(n, c, dtype, zp, ldz, lp, bits, _vector(logp, "logp", n), _vector(entropy, "entropy", n), _packed(stats, "stats", n, 2, _F32), top, tv, tc, wp, wbytes,
-                             _stream_ptr(stream)), "cbm_log_probs")
+    status = lib.cbm_log_probs(n, c, dtype, zp, ldz, lp, bits, _packed(logp, "logp", rows, f32), _packed(entropy, "entropy", rows, f32), _packed(stats, "stats", (n, 2), f32), top, tv, tc,
+                               wp, wbytes, _current_stream() if stream is None else _stream_ptr(stream))
+    if status:
+        raise CbmError(status, "cbm_log_probs")
     return logp
 
 
 def cbm_log_probs_backward(Z, labels, stats, entropy, dlogp, dentropy, dZ, stream=None):
     lib = _LIB or _lib()
-    zp, ldz, n, c, dtype = _matrix(Z, "Z")
-    dp, ldd, *d = _matrix(dZ, "dZ")
-    _same([n, c, dtype], d, "Z and dZ")
+    z, d = _matrix(Z, "Z", _DTYPES), _matrix(dZ, "dZ", _DTYPES)
+    _alike(z, d, "Z and dZ")
+    zp, ldz, n, c, dtype = z
+    rows, f32 = (n,), _F32
     lp, bits = _labels(labels, n)
-    _check(lib.cbm_log_probs_backward(n, c, dtype, zp, ldz, lp, bits, _packed(stats, "stats", n, 2, _F32), _vector(entropy, "entropy", n), _vector(dlogp, "dlogp", n),
-                                      _vector(dentropy, "dentropy", n), dp, ldd, _stream_ptr(stream)), "cbm_log_probs_backward")
+    status = lib.cbm_log_probs_backward(n, c, dtype, zp, ldz, lp, bits, _packed(stats, "stats", (n, 2), f32), _packed(entropy, "entropy", rows, f32), _packed(dlogp, "dlogp", rows, f32),
+                                        _packed(dentropy, "dentropy", rows, f32), d[0], d[1], _current_stream() if stream is None else _stream_ptr(stream))
+    if status:
+        raise CbmError(status, "cbm_log_probs_backward")
     return dZ
 
 
