@@ -16,6 +16,7 @@ namespace {
 
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 constexpr int NORM_THREADS = 256;
+constexpr int FEW_ROWS = 1024;  // so many rows are read twice rather than joined by a second launch
 constexpr int BACK_THREADS = 512, BACK_GROUPS = 512;  // backward: workgroups at most, each with partial sums of dg and db of its own
 
 // Sums of two values over a workgroup, in every thread.  `room` has a pair for every wave, twice: calls take turns (`turn`), so one barrier each is enough (who writes a
@@ -158,15 +159,49 @@ __global__ __launch_bounds__(1024) void cbm_norm_wide_kernel(int64_t n, int k, c
     }
 }
 
+// dg and db of 16 columns over all rows, by a workgroup whose every 16 lanes have a share of the rows.
+template <class T, int THREADS>
+__device__ __forceinline__ void columns_alone(int64_t n, int k, int first, const T* __restrict__ dY, int64_t lddy, const T* __restrict__ X, int64_t ldx, const float* __restrict__ mean,
+                                              const float* __restrict__ rstd, float* __restrict__ dgamma, float* __restrict__ dbeta, floatx2* room) {
+    constexpr int SHARES = THREADS / 16;
+    const int column = first + (threadIdx.x & 15), share = threadIdx.x / 16;
+    float dg = 0.0f, db = 0.0f;
+    if (column < k)
+#pragma unroll 8
+        for (int64_t row = share; row < n; row += SHARES) {
+            const float dy = (float)dY[row * lddy + column];
+            dg += dy * (((float)X[row * ldx + column] - mean[row]) * rstd[row]);
+            db += dy;
+        }
+    room[threadIdx.x] = floatx2{dg, db};
+    __syncthreads();
+    if (threadIdx.x >= 16 || column >= k) return;
+    dg = db = 0.0f;
+#pragma unroll 8
+    for (int i = 0; i < SHARES; ++i) {
+        dg += room[i * 16 + threadIdx.x][0];
+        db += room[i * 16 + threadIdx.x][1];
+    }
+    if (dgamma) dgamma[column] = dg;
+    if (dbeta) dbeta[column] = db;
+}
+
 // Backward in the same shape.  A lane has the same columns in all rows that it meets, so dg and db of these columns add up in its registers; a workgroup adds its
-// lanes' sums in LDS, in a fixed order, and writes one partial row of each to `parts` (workgroup, dg then db, column).
+// lanes' sums in LDS, in a fixed order, and writes one partial row of each to `parts` (workgroup, dg then db, column).  With few rows a second launch would take longer than
+// everything else: workgroups beyond the first `row_groups` then have dg and db of 16 columns each, and read all rows once more.
 template <class T, int V, int LANES, int R, int THREADS, bool WHOLE>
 __global__ __launch_bounds__(THREADS) void cbm_norm_back_kernel(int64_t n, int k, const T* __restrict__ dY, int64_t lddy, const T* __restrict__ X, int64_t ldx,
                                                                 const float* __restrict__ gamma, const float* __restrict__ mean, const float* __restrict__ rstd,
-                                                                T* __restrict__ dX, int64_t lddx, float* __restrict__ parts, bool far) {
+                                                                T* __restrict__ dX, int64_t lddx, float* __restrict__ parts, int row_groups, float* __restrict__ dgamma,
+                                                                float* __restrict__ dbeta, bool far) {
     constexpr int ROWS = THREADS / LANES;
     constexpr int COLUMNS = LANES * R * V;
-    __shared__ floatx2 room[LANES > 64 ? 2 * (LANES / 64) : (THREADS / 64) * COLUMNS];
+    constexpr int ROOM = LANES > 64 ? 2 * (LANES / 64) : (THREADS / 64) * COLUMNS;
+    __shared__ floatx2 room[ROOM > THREADS ? ROOM : THREADS];
+    if ((int)blockIdx.x >= row_groups) {
+        columns_alone<T, THREADS>(n, k, 16 * (blockIdx.x - row_groups), dY, lddy, X, ldx, mean, rstd, dgamma, dbeta, room);
+        return;
+    }
     const int lane = threadIdx.x % LANES;
     int turn = 0;
     float g[R][V], dg[R][V], db[R][V];
@@ -195,7 +230,7 @@ __global__ __launch_bounds__(THREADS) void cbm_norm_back_kernel(int64_t n, int k
         next_r = rstd[at];
     };
     if (AHEAD) load(blockIdx.x);
-    for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < n; row0 += (int64_t)gridDim.x * ROWS) {
+    for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < n; row0 += (int64_t)row_groups * ROWS) {
         const int64_t row = row0 + threadIdx.x / LANES;
         float h[R][V], u[R][V], sum = 0.0f, along = 0.0f;
         if (!AHEAD) load(row);
@@ -205,10 +240,12 @@ __global__ __launch_bounds__(THREADS) void cbm_norm_back_kernel(int64_t n, int k
             widen<V, T>(u[c], next_dy[c]);
         }
         const float m = next_m, r = next_r;
-        if (AHEAD) load(row + gridDim.x);
+        int lane_now = lane;
+        if constexpr (!WHOLE && R * V >= 16) asm volatile("" : "+v"(lane_now));  // (every row's comparisons anew: kept from row to row they need more scalar registers than there are)
+        if (AHEAD) load(row + row_groups);
 #pragma unroll
         for (int c = 0; c < R; ++c) {
-            const Place<V, WHOLE> p(c * LANES + lane, k);
+            const Place<V, WHOLE> p(c * LANES + lane_now, k);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 h[c][j] = (h[c][j] - m) * r;
@@ -228,7 +265,7 @@ __global__ __launch_bounds__(THREADS) void cbm_norm_back_kernel(int64_t n, int k
         if (row >= n) continue;
 #pragma unroll
         for (int c = 0; c < R; ++c) {
-            const Place<V, WHOLE> p(c * LANES + lane, k);
+            const Place<V, WHOLE> p(c * LANES + lane_now, k);
             float dx[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) dx[j] = r * (u[c][j] - sum - h[c][j] * along);
@@ -425,7 +462,9 @@ cbm_status cbm_launch_norm_backward(int64_t n, int32_t k, int32_t type, const vo
     hipStream_t stream = (hipStream_t)stream_;
     const int64_t most = cbm_norm_parts(n);
     int64_t count = 0;  // partial rows written
-    if (!dgamma && !dbeta) parts = nullptr;
+    const bool sums = dgamma || dbeta;
+    bool joined = !sums;
+    if (!sums) parts = nullptr;
     if (n > 0)
         with_shape(type, k, [&](auto t, auto whole) {
             using T = decltype(t);
@@ -435,9 +474,14 @@ cbm_status cbm_launch_norm_backward(int64_t n, int32_t k, int32_t type, const vo
             constexpr int V = 16 / (int)sizeof(T);
             const int64_t pieces = ((int64_t)k + V - 1) / V;
             const bool far = n * k * (int64_t)sizeof(T) >= CBM_FAR_BYTES;
-#define CBM_BACK(V_, LANES, R, THREADS)                                                                                                                                    \
-    cbm_norm_back_kernel<T, V_, LANES, R, THREADS, WHOLE><<<(unsigned)(count = at_most(n, THREADS / LANES, most)), THREADS, 0, stream>>>(n, k, dY, lddy, X, ldx, gamma, mean, rstd, dX, lddx, \
-                                                                                                                                 parts, far)
+            const bool once = sums && n <= FEW_ROWS && pieces <= 1024;  // (dg and db in the same launch)
+            const unsigned alone = once ? (unsigned)(((int64_t)k + 15) / 16) : 0;
+            if (once) parts = nullptr;
+#define CBM_BACK(V_, LANES, R, THREADS)                                                                                                                                              \
+    (count = at_most(n, THREADS / LANES, most),                                                                                                                                      \
+     cbm_norm_back_kernel<T, V_, LANES, R, THREADS, WHOLE><<<(unsigned)(dX || !once ? count : 0) + alone, THREADS, 0, stream>>>(n, k, dY, lddy, X, ldx, gamma, mean, rstd, dX, lddx, parts, \
+                                                                                                                               dX || !once ? (int)count : 0, dgamma, dbeta, far),      \
+     joined = once)
             if (k < V) CBM_BACK(1, 8, 1, BACK_THREADS);
             else if (pieces <= 4) CBM_BACK(V, 4, 1, BACK_THREADS);
             else if (pieces <= 8) CBM_BACK(V, 8, 1, BACK_THREADS);
@@ -459,6 +503,6 @@ cbm_status cbm_launch_norm_backward(int64_t n, int32_t k, int32_t type, const vo
             }
 #undef CBM_BACK
         });
-    if (dgamma || dbeta) hipLaunchKernelGGL(cbm_norm_join_kernel, dim3((unsigned)(((int64_t)k + 31) / 32), 2), dim3(1024), 0, stream, (int)count, k, parts, dgamma, dbeta);
+    if (!joined) hipLaunchKernelGGL(cbm_norm_join_kernel, dim3((unsigned)(((int64_t)k + 31) / 32), 2), dim3(1024), 0, stream, (int)count, k, parts, dgamma, dbeta);
     return launched("layer norm backward launch");
 }
