@@ -282,14 +282,14 @@ inline bool cbm_panel_takes_unaligned(int64_t M, int32_t N, int32_t K) {
 cbm_status cbm_launch_gemm(int64_t M, int32_t N, int32_t K, const float* A, int64_t lda, const float* B, int64_t ldb,
                            float* C, int64_t ldc, void* stream);
 
-// layer norm (cbm_norm.hip)
+// layer norm (train/cbm_norm.hip)
 int64_t cbm_norm_parts(int64_t n);  // partial sums of dgamma and dbeta, 2 k values each
 cbm_status cbm_launch_norm(int64_t n, int32_t k, int32_t type, const void* X, int64_t ldx, const float* gamma, const float* beta, float eps, void* Y, int64_t ldy,
                            float* mean, float* rstd, void* stream);
 cbm_status cbm_launch_norm_backward(int64_t n, int32_t k, int32_t type, const void* dY, int64_t lddy, const void* X, int64_t ldx, const float* gamma, const float* mean,
                                     const float* rstd, void* dX, int64_t lddx, float* dgamma, float* dbeta, float* parts, void* stream);
 
-// activations in 8 bits (cbm_checkpoint.hip)
+// activations in 8 bits (train/cbm_checkpoint.hip)
 int64_t cbm_grad_splits(int64_t n, int32_t k, int32_t c);  // shares of the rows, each with a k x c partial sum; 1: none is needed
 cbm_status cbm_launch_checkpoint_save(int64_t n, int32_t k, int32_t type, const void* X, int64_t ldx, int8_t* Q, int64_t ldq, uint8_t* E, int64_t lde, void* stream);
 // restored values, or with a dY its ReLU backward pass
@@ -298,9 +298,9 @@ cbm_status cbm_launch_checkpoint_load(int64_t n, int32_t k, const int8_t* Q, int
 cbm_status cbm_launch_checkpoint_grad(int64_t n, int32_t k, int32_t c, const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int32_t type, const void* dY, int64_t lddy,
                                       float* dW, int64_t lddw, float* parts, void* stream);
 
-// log probabilities (cbm_scores.hip)
+// log probabilities (train/cbm_scores.hip)
 constexpr int32_t CBM_MOST_TOP = 32;                // alternatives
-int cbm_scores_splits(int64_t n, int32_t c);        // workgroups that share a row; 1: no workspace
+int cbm_scores_splits(int64_t n, int32_t c);        // workgroups that may share a row; 1: no workspace
 size_t cbm_scores_part_bytes(int32_t top);          // of the workspace for each of them
 cbm_status cbm_launch_scores(int64_t n, int32_t c, int32_t type, const void* z, int64_t ldz, const void* labels, int label_bits, float* logp, float* entropy, float* stats, int32_t top,
                              float* values, int32_t* columns, void* parts, void* stream);

@@ -16,7 +16,9 @@ namespace {
 
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 constexpr int NORM_THREADS = 256;
-constexpr int FEW_ROWS = 1024;  // so many rows are read twice rather than joined by a second launch
+// Backward: rows that are read twice rather than joined by a second launch.  Microseconds a call, one launch or two: 1024 x 64 7.5 or 11.4, 1024 x 2048 10.5 or 13.7, 2048 x 64 7.6 or
+// 10.1, 2048 x 512 8.3 or 10.2, 2048 x 2048 19 or 16, 4096 x 64 10 or 10, 4096 x 300 19 or 10.
+bool few_rows(int64_t n, int k) { return n <= 1024 || (n <= 2048 && k <= 512); }
 constexpr int BACK_THREADS = 512, BACK_GROUPS = 512;  // backward: workgroups at most, each with partial sums of dg and db of its own
 
 // Sums of two values over a workgroup, in every thread.  `room` has a pair for every wave, twice: calls take turns (`turn`), so one barrier each is enough (who writes a
@@ -474,7 +476,7 @@ cbm_status cbm_launch_norm_backward(int64_t n, int32_t k, int32_t type, const vo
             constexpr int V = 16 / (int)sizeof(T);
             const int64_t pieces = ((int64_t)k + V - 1) / V;
             const bool far = n * k * (int64_t)sizeof(T) >= CBM_FAR_BYTES;
-            const bool once = sums && n <= FEW_ROWS && pieces <= 1024;  // (dg and db in the same launch)
+            const bool once = sums && few_rows(n, k) && pieces <= 1024;  // (dg and db in the same launch)
             const unsigned alone = once ? (unsigned)(((int64_t)k + 15) / 16) : 0;
             if (once) parts = nullptr;
 #define CBM_BACK(V_, LANES, R, THREADS)                                                                                                                                              \

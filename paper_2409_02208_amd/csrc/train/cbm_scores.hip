@@ -575,10 +575,14 @@ cbm_status launched(const char* what) {
     return CBM_ERR_HIP;
 }
 constexpr int SHORT_ROW = 1024;  // columns that a wave keeps in its registers
+// Columns up to which a workgroup has a row alone whatever the number of rows, since a second launch takes longer than its turns.  Microseconds alone and shared, top 8, captured
+// (calls one after the other): one row of 16,384 columns 5.9 and 9.7 (7.5 and 10.8), 49,152 9.1 and 9.7 (8.8 and 10.9), 65,536 10.4 and 9.7 (10.1 and 10.9); 100 rows of 49,152 11.5 and 13.9.
+constexpr int ALONE = 49152;
 
 }  // namespace
 
-// Workgroups that share a row: some for every compute unit, of 1,024 columns at least (one turn of a workgroup is 2,048).
+// Workgroups that may share a row: some for every compute unit, of 1,024 columns at least (one turn of a workgroup is 2,048).  The workspace has room for them, whether a row of
+// this length is shared or not.
 int cbm_scores_splits(int64_t n, int32_t c) {
     if (c <= SHORT_ROW || n == 0) return 1;
     return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(MOST_SPLITS, 512 / n), ((int64_t)c + 2047) / 2048));
@@ -613,7 +617,7 @@ cbm_status cbm_launch_scores(int64_t n, int32_t c, int32_t type, const void* z, 
         else if (c <= SHORT_ROW) CBM_SCORES(V, 64, R, false);
 #undef CBM_SCORES
         else {
-            const int splits = cbm_scores_splits(n, c);
+            const int splits = c <= ALONE ? 1 : cbm_scores_splits(n, c);
             int share = ((c + splits - 1) / splits + V - 1) / V * V;
             const unsigned grid = (unsigned)std::min<int64_t>(n * splits, 1 << 20);
 #define CBM_LONG(R, TOP) cbm_scores_long_kernel<T, V, R, TOP><<<grid, LONG_THREADS, 0, stream>>>(a, splits, share, (char*)parts)
