@@ -276,3 +276,19 @@ def test_refusals(env):  # noqa: F811
             call(4, 40, 0, 40, 64, p + 2)] == [1] * 7
     assert call(4, (1 << 24) + 1, 0, 1 << 25, 64) == 5
     assert not bool(Z.any()) and bool((dZ == 1).all()) and bool((v == 1).all()) and bool((s == 1).all())
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n,c", [(1, 49152), (1, 49153), (1, 70001), (7, 60000), (300, 50000)])
+def test_ties_and_orders_in_the_longest_rows(env, name, n, c):  # noqa: F811
+    """On both sides of the length from which workgroups share a row: all equal, rising, few different scores, the largest in a few lanes' columns."""
+    torch, cbm = env
+    rng = np.random.default_rng(c + n)
+    kinds = [np.full(c, -2.0), np.arange(c) / 64.0 % 1024, rng.integers(-2, 3, c).astype(np.float64), np.where(np.arange(c) % 2048 < 8, 5.0, rng.standard_normal(c)),
+             np.where(np.arange(c) < c - 40, -math.inf, 1.0)]
+    for first in range(len(kinds)) if n == 1 else (0,):
+        z = np.stack([kinds[(first + i) % len(kinds)] for i in range(n)])
+        Z, _ = _matrix(torch, z, name, 0)
+        labels = rng.integers(0, c, n)
+        for top in (1, 8, 32):
+            _check(torch, Z, labels, _scores(torch, cbm, Z, labels, top), top)
