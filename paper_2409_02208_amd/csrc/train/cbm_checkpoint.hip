@@ -134,6 +134,7 @@ __global__ __launch_bounds__(256) void cbm_checkpoint_load_kernel(int64_t n, int
 // eight rows, four neighbouring columns of Q and two of dY: 128 columns of Q and 64 of dY by 16 rows a wave, with neither LDS nor transposes, only with columns of dW in
 // an order of their own (tile t has columns 4 i + t of Q, and 2 i + t of dY).  x~ is a bf16 value; dY is split into one, two (fp16) or three (fp32) bf16 values that add
 // up to it, so the products are exact and the sums fp32.  The waves of a workgroup and the workgroups of a tile share the rows; a workgroup adds its waves' sums in LDS, in order.
+constexpr int FEW_PARTS = 16;
 constexpr int GRAD_WAVES = 8, GRAD_ROWS = 16, GRAD_K = 128, GRAD_C = 64;
 
 enum GradEdge {  // how the last columns of a row are loaded
@@ -366,6 +367,16 @@ __global__ __launch_bounds__(1024) void cbm_checkpoint_join_kernel(int count, in
     }
 }
 
+// The same with few partial sums: a value a thread.
+__global__ __launch_bounds__(256) void cbm_checkpoint_join_few_kernel(int count, int64_t size, int c, const float* __restrict__ parts, float* __restrict__ dW, int64_t lddw) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
+        float s = 0.0f;
+#pragma unroll 8
+        for (int p = 0; p < count; ++p) s += parts[p * size + i];
+        dW[i / c * lddw + i % c] = s;
+    }
+}
+
 cbm_status launched(const char* what) {
     const hipError_t e = hipGetLastError();
     if (e == hipSuccess) return CBM_OK;
@@ -390,9 +401,22 @@ void along_rows(int64_t n, int64_t pieces, F&& f) {
 
 }  // namespace
 
+// A compute unit holds one workgroup of the gradient at a time, and workgroup b runs on XCD b mod 8, so what s shares take is what the fullest XCD's 32 units take: rounds / s of what one
+// workgroup takes for all rows.  The fewest shares that come within a tenth of the least of that (more of them cost partial sums).  A share has 64 rows at least.
+// (300000 x 300, 100 columns, six tiles: 200 us with 42 shares, of which two XCDs had 36 workgroups.)
 int64_t cbm_grad_splits(int64_t n, int32_t k, int32_t c) {
+    constexpr int64_t UNITS = 32;
     const int64_t tiles = ((int64_t)k + GRAD_K - 1) / GRAD_K * (((int64_t)c + GRAD_C - 1) / GRAD_C);
-    return std::max<int64_t>(1, std::min<int64_t>((256 + tiles - 1) / tiles, (n + 4 * GRAD_ROWS - 1) / (4 * GRAD_ROWS)));
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>((4 * CBM_XCD * UNITS + tiles - 1) / tiles, (n + 4 * GRAD_ROWS - 1) / (4 * GRAD_ROWS)));
+    auto share = [&](int64_t s) {
+        const int64_t fullest = s < CBM_XCD ? (s * tiles + CBM_XCD - 1) / CBM_XCD : (s + CBM_XCD - 1) / CBM_XCD * tiles;  // (the launch says why: shares are dealt out to XCDs)
+        return (double)((fullest + UNITS - 1) / UNITS) / (double)s;
+    };
+    double least = share(1);
+    for (int64_t s = 2; s <= most; ++s) least = std::min(least, share(s));
+    int64_t s = 1;
+    while (share(s) > 1.1 * least) ++s;
+    return s;
 }
 
 cbm_status cbm_launch_checkpoint_save(int64_t n, int32_t k, int32_t type, const void* X, int64_t ldx, int8_t* Q, int64_t ldq, uint8_t* E, int64_t lde, void* stream) {
@@ -442,6 +466,7 @@ cbm_status cbm_launch_checkpoint_grad(int64_t n, int32_t k, int32_t c, const int
             else if (k % 4 || c % 2) cbm_checkpoint_grad_kernel<T, GRAD_SHIFTED><<<grid, 64 * GRAD_WAVES, 0, stream>>>(a, tiles_c, tiles, splits, to, ldp, size);
             else cbm_checkpoint_grad_kernel<T, GRAD_WHOLE><<<grid, 64 * GRAD_WAVES, 0, stream>>>(a, tiles_c, tiles, splits, to, ldp, size);
         });
-    if (splits != 1) cbm_checkpoint_join_kernel<<<(unsigned)std::min<int64_t>((size + 31) / 32, 1 << 20), 1024, 0, stream>>>(splits, size, c, parts, dW, lddw);
+    if (splits != 1 && splits <= FEW_PARTS) cbm_checkpoint_join_few_kernel<<<(unsigned)std::min<int64_t>((size + 255) / 256, 1 << 22), 256, 0, stream>>>(splits, size, c, parts, dW, lddw);
+    else if (splits != 1) cbm_checkpoint_join_kernel<<<(unsigned)std::min<int64_t>((size + 31) / 32, 1 << 20), 1024, 0, stream>>>(splits, size, c, parts, dW, lddw);
     return launched("checkpoint gradient launch");
 }
