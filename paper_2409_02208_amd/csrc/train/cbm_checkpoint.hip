@@ -131,22 +131,33 @@ __global__ __launch_bounds__(256) void cbm_checkpoint_load_kernel(int64_t n, int
 }
 
 // dW = X~^T dY, a sum over the rows.  Both operands lie along their columns in memory and the matrix cores want eight rows of a column in a lane, so a lane loads, for
-// eight rows, four neighbouring columns of Q and two of dY: 128 columns of Q and 64 of dY by 16 rows a wave, with neither LDS nor transposes, only with columns of dW in
-// an order of their own (tile t has columns 4 i + t of Q, and 2 i + t of dY).  x~ is a bf16 value; dY is split into one, two (fp16) or three (fp32) bf16 values that add
+// eight rows, MT (4) neighbouring columns of Q and NT (2) of dY: 32 MT columns of Q and 32 NT of dY by 16 rows a wave, with neither LDS nor transposes, only with columns of dW
+// in an order of their own (tile t has columns MT i + t of Q, and NT i + t of dY).  x~ is a bf16 value; dY is split into one (bf16), two (fp16) or three (fp32) bf16 values that add
 // up to it, so the products are exact and the sums fp32.  The waves of a workgroup and the workgroups of a tile share the rows; a workgroup adds its waves' sums in LDS, in order.
+// Narrow matrices take narrow tiles, of which a compute unit holds two workgroups.
 constexpr int FEW_PARTS = 16;
-constexpr int GRAD_WAVES = 8, GRAD_ROWS = 16, GRAD_K = 128, GRAD_C = 64;
+constexpr int GRAD_WAVES = 8, GRAD_ROWS = 16;
+int grad_mt(int32_t k) { return k <= 32 ? 1 : k <= 64 ? 2 : 4; }
+int grad_nt(int32_t c) { return c <= 32 ? 1 : 2; }
+constexpr int grad_groups(int mt, int nt) { return mt <= 2 && nt == 1 ? 2 : 1; }  // workgroups in a compute unit
 
-enum GradEdge {  // how the last columns of a row are loaded
-    GRAD_WHOLE,    // k is a multiple of 4 and c of 2
-    GRAD_SHIFTED,  // the last load of a row starts earlier, and is shifted
-    GRAD_SINGLE    // k < 4 or c < 2, or strides so long that eight rows are not within 32 bits: value by value
+template <int MT>
+struct GradWord {
+    typedef uint32_t type __attribute__((aligned(1)));
 };
-template <class T>
+template <>
+struct GradWord<2> {
+    typedef uint16_t type __attribute__((aligned(1)));
+};
+template <>
+struct GradWord<1> {
+    typedef uint8_t type;
+};
+template <class T, int MT, int NT>
 struct GradStep {  // what a lane has loaded: eight rows
-    uint32_t q[8];
-    T y[8][2];
-    uint8_t e;  // of row lane / 4 of the sixteen, and block lane % 4 of the 128 columns
+    typename GradWord<MT>::type q[8];
+    T y[8][NT];
+    uint8_t e;  // of row lane / 4 of the sixteen, and block lane % 4 of the tile's columns
 };
 template <class T>
 struct GradArgs {
@@ -159,93 +170,81 @@ struct GradArgs {
     const T* dY;
     int64_t lddy;
 };
-// Rows row0 + 8 half .. + 7 (of the last row where there are none), columns k0 .. + 3 of Q and c0, c0 + 1 of dY.
-template <class T, GradEdge EDGE>
-__device__ __forceinline__ void grad_load(GradStep<T>& s, const GradArgs<T>& a, int64_t row0, int k0, int c0, int half, int block) {
+template <int NT, class T>
+__device__ __forceinline__ void grad_values(T (&to)[NT], const T* y) {
+    const auto v = raw_piece<NT>(y);
+#pragma unroll
+    for (int u = 0; u < NT; ++u) to[u] = v[u];
+}
+// Rows row0 + 8 half .. + 7 (of the last row where there are none), MT columns of Q from at_q on and NT of dY from at_y.
+template <class T, int MT, int NT>
+__device__ __forceinline__ void grad_load(GradStep<T, MT, NT>& s, const GradArgs<T>& a, int64_t row0, int at_q, int at_y, int half, int block) {
     s.e = a.E[min(row0 + (int)(threadIdx.x & 63) / 4, a.n - 1) * a.lde + block];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const int64_t at = min(row0 + 8 * half + j, a.n - 1);
-        const int8_t* q = a.Q + at * a.ldq;
-        const T* y = a.dY + at * a.lddy;
-        if constexpr (EDGE == GRAD_SINGLE) {
-            uint32_t v = 0;
-#pragma unroll
-            for (int t = 0; t < 4; ++t) v |= (uint32_t)(uint8_t)q[min(k0 + t, a.k - 1)] << (8 * t);
-            s.q[j] = v;
-#pragma unroll
-            for (int t = 0; t < 2; ++t) s.y[j][t] = y[min(c0 + t, a.c - 1)];
-        } else {
-            typedef uint32_t Word __attribute__((aligned(1)));
-            s.q[j] = *reinterpret_cast<const Word*>(q + min(k0, a.k - 4));
-            const typename Piece<T, 2>::type pair = *reinterpret_cast<const typename Piece<T, 2>::type*>(y + min(c0, a.c - 2));
-            s.y[j][0] = pair[0];
-            s.y[j][1] = pair[1];
-        }
+        s.q[j] = *reinterpret_cast<const typename GradWord<MT>::type*>(a.Q + at * a.ldq + at_q);
+        grad_values<NT>(s.y[j], a.dY + at * a.lddy + at_y);
         __builtin_amdgcn_sched_barrier(0);  // (a row's addresses at a time: registers)
     }
 }
-
 // The same for rows that are all there, with what all lanes share of an address in scalar registers and a lane's own 32 bits beside it (64-bit products of a row and
 // a stride for each load of each lane took more time than everything else).
-template <class T>
-__device__ __forceinline__ void grad_load_whole(GradStep<T>& s, const GradArgs<T>& a, int64_t row0, uint32_t of_q, uint32_t of_e, uint32_t of_y) {
+template <class T, int MT, int NT>
+__device__ __forceinline__ void grad_load_whole(GradStep<T, MT, NT>& s, const GradArgs<T>& a, int64_t row0, uint32_t of_q, uint32_t of_e, uint32_t of_y) {
     const char *q = (const char*)a.Q + row0 * a.ldq, *e = (const char*)a.E + row0 * a.lde, *y = (const char*)(a.dY + row0 * a.lddy);
     s.e = *reinterpret_cast<const uint8_t*>(e + of_e);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        typedef uint32_t Word __attribute__((aligned(1)));
-        s.q[j] = *reinterpret_cast<const Word*>(q + j * (uint32_t)a.ldq + of_q);
-        const typename Piece<T, 2>::type pair = *reinterpret_cast<const typename Piece<T, 2>::type*>(y + j * (uint32_t)(a.lddy * sizeof(T)) + of_y);
-        s.y[j][0] = pair[0];
-        s.y[j][1] = pair[1];
+        s.q[j] = *reinterpret_cast<const typename GradWord<MT>::type*>(q + j * (uint32_t)a.ldq + of_q);
+        grad_values<NT>(s.y[j], reinterpret_cast<const T*>(y + j * (uint32_t)(a.lddy * sizeof(T)) + of_y));
     }
 }
 
-template <class T, GradEdge EDGE>
-__global__ __launch_bounds__(64 * GRAD_WAVES) void cbm_checkpoint_grad_kernel(GradArgs<T> a, int tiles_c, int tiles, int splits, float* __restrict__ parts, int64_t ldp, int64_t part) {
+// near: eight rows are within 32 bits of an address
+template <class T, int MT, int NT>
+__global__ __launch_bounds__(64 * GRAD_WAVES, 2 * grad_groups(MT, NT)) void cbm_checkpoint_grad_kernel(GradArgs<T> a, int tiles_c, int tiles, int splits, float* __restrict__ parts, int64_t ldp,
+                                                                                                    int64_t part, bool near) {
     constexpr int PARTS = std::is_same<T, float>::value ? 3 : std::is_same<T, _Float16>::value ? 2 : 1;  // 24, 11 and 8 bits, eight a part
-    __shared__ floatx2 room[GRAD_WAVES * 2 * 8 * 64];
+    __shared__ floatx2 room[GRAD_WAVES * NT * 8 * 64];
     // consecutive workgroups run on different XCDs: the tiles of one share of the rows are eight apart, on one XCD, where there are so many shares
     const int b = blockIdx.x, beside = min(CBM_XCD, splits), split = b / (beside * tiles) * beside + b % beside, tile = b / beside % tiles;
     if (split >= splits) return;
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int k0 = tile / tiles_c * GRAD_K + 4 * (lane & 31), c0 = tile % tiles_c * GRAD_C + 2 * (lane & 31);
+    const int k0 = tile / tiles_c * (32 * MT) + MT * (lane & 31), c0 = tile % tiles_c * (32 * NT) + NT * (lane & 31);
+    const int at_q = min(k0, a.k - MT), at_y = min(c0, a.c - NT);  // (the last load of a row starts earlier, and is shifted)
+    const int late_q = 8 * min(k0 - at_q, MT - 1);                 // bits before the lane's first column in what it loads
+    const bool late_y = NT == 2 && c0 > at_y;
     const int64_t steps = (a.n + GRAD_ROWS - 1) / GRAD_ROWS;
     const int64_t first = steps * split / splits, last = steps * (split + 1) / splits;
-    floatx16 acc[4][2];
+    floatx16 acc[MT][NT];
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < NT; ++u)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[t][u][v] = 0.0f;
     uint32_t minus_low = 0xbf80u;
     asm("" : "+s"(minus_low));
-    const int late_q = EDGE == GRAD_SHIFTED ? 8 * max(0, min(k0 - (a.k - 4), 3)) : 0;  // bits before the lane's first column in what it loads
-    const bool late_y = EDGE == GRAD_SHIFTED && c0 > a.c - 2;
-    const int block = min(tile / tiles_c * (GRAD_K / BLOCK) + (lane & 3), (a.k + BLOCK - 1) / BLOCK - 1), from = (32 * half + (lane & 31) / 8) * 4;
-    const uint32_t of_q = (uint32_t)(8 * half * a.ldq + min(k0, a.k - 4)), of_e = (uint32_t)(lane / 4 * a.lde + block),
-                   of_y = (uint32_t)((8 * half * a.lddy + min(c0, a.c - 2)) * (int64_t)sizeof(T));
-    GradStep<T> next;
+    const int block = min(tile / tiles_c * MT + min(lane & 3, MT - 1), (a.k + BLOCK - 1) / BLOCK - 1), from = (32 * half + (lane & 31) / (32 / MT)) * 4;
+    const uint32_t of_q = (uint32_t)(8 * half * a.ldq + at_q), of_e = (uint32_t)(lane / 4 * a.lde + block), of_y = (uint32_t)((8 * half * a.lddy + at_y) * (int64_t)sizeof(T));
+    GradStep<T, MT, NT> next;
     auto load = [&](int64_t step) {
-        if (EDGE == GRAD_SINGLE || (step + 1) * GRAD_ROWS > a.n) grad_load<T, EDGE>(next, a, step * GRAD_ROWS, k0, c0, half, block);
-        else grad_load_whole<T>(next, a, step * GRAD_ROWS, of_q, of_e, of_y);
+        if (!near || (step + 1) * GRAD_ROWS > a.n) grad_load<T, MT, NT>(next, a, step * GRAD_ROWS, at_q, at_y, half, block);
+        else grad_load_whole<T, MT, NT>(next, a, step * GRAD_ROWS, of_q, of_e, of_y);
     };
-    constexpr bool AHEAD = EDGE != GRAD_SINGLE;  // (single values have no registers left for the next step's)
-    if (AHEAD && first + wave < last) load(first + wave);
+    if (first + wave < last) load(first + wave);
     for (int64_t i = first + wave; i < last; i += GRAD_WAVES) {
         struct {
             uint32_t q[8];
-            float step[8], y[2][8];
+            float step[8], y[NT][8];
         } s;
-        if (!AHEAD) load(i);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            s.q[j] = EDGE == GRAD_SHIFTED ? next.q[j] >> late_q : next.q[j];
+            s.q[j] = (uint32_t)next.q[j] >> late_q;
             s.step[j] = step_of(__builtin_amdgcn_ds_bpermute(from + 16 * j, (int)next.e));
-            s.y[0][j] = (float)(EDGE == GRAD_SHIFTED && late_y ? next.y[j][1] : next.y[j][0]);
-            s.y[1][j] = (float)next.y[j][1];
+            s.y[NT - 1][j] = (float)next.y[j][NT - 1];
+            if constexpr (NT == 2) s.y[0][j] = (float)(late_y ? next.y[j][1] : next.y[j][0]);
         }
         if ((i + 1) * GRAD_ROWS > a.n) {
 #pragma unroll
@@ -253,20 +252,21 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void cbm_checkpoint_grad_kernel(Gr
                 if (i * GRAD_ROWS + 8 * half + j >= a.n) {
                     s.q[j] = 0;
                     s.step[j] = 1.0f;
-                    s.y[0][j] = s.y[1][j] = 0.0f;
+#pragma unroll
+                    for (int u = 0; u < NT; ++u) s.y[u][j] = 0.0f;
                 }
         }
-        if (AHEAD && i + GRAD_WAVES < last) load(i + GRAD_WAVES);
-        uintx4 y[2][PARTS];
+        if (i + GRAD_WAVES < last) load(i + GRAD_WAVES);
+        uintx4 y[NT][PARTS];
         if constexpr (PARTS == 1) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < NT; ++u)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) y[u][0][j] = high_halves(s.y[u][2 * j], s.y[u][2 * j + 1]);
         } else {
             float odd = 0.0f;  // NaN where a value of dY has no parts
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < NT; ++u)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     uint32_t part[3];
@@ -277,7 +277,7 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void cbm_checkpoint_grad_kernel(Gr
                 }
             if (__any(odd != odd)) {  // values that are not finite, which are their own high part, or that round up to infinity: parts by truncation
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
+                for (int u = 0; u < NT; ++u)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const float v0 = s.y[u][2 * j], v1 = s.y[u][2 * j + 1];
@@ -292,52 +292,50 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void cbm_checkpoint_grad_kernel(Gr
             }
         }
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
+        for (int t = 0; t < MT; ++t) {
             uintx4 x;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 float v[2];
 #pragma unroll
-                for (int i2 = 0; i2 < 2; ++i2) {
-                    const int r = 2 * j + i2;
-                    const float q = (float)(int8_t)(s.q[r] >> (8 * t));
-                    v[i2] = q * s.step[r];  // (NOT_FINITE: 0 times infinity)
-                }
+                for (int w = 0; w < 2; ++w) v[w] = (float)(int8_t)(s.q[2 * j + w] >> (8 * t)) * s.step[2 * j + w];  // (NOT_FINITE: 0 times infinity)
                 x[j] = high_halves(v[0], v[1]);
             }
 #pragma unroll
             for (int p = PARTS - 1; p >= 0; --p)
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
+                for (int u = 0; u < NT; ++u)
                     acc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y[u][p]), acc[t][u], 0, 0, 0);
         }
     }
-    // The waves' sums, a tile of Q's columns at a time: every wave writes its own, then every thread adds two rows of two neighbouring columns.
+    // The waves' sums, a tile of Q's columns at a time: every wave writes its own, then every thread adds two rows of NT neighbouring columns.
     float* out = parts + split * part;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
+    for (int t = 0; t < MT; ++t) {
         __syncthreads();
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < NT; ++u)
 #pragma unroll
-            for (int v = 0; v < 8; ++v) room[((wave * 2 + u) * 8 + v) * 64 + lane] = floatx2{acc[t][u][2 * v], acc[t][u][2 * v + 1]};
+            for (int v = 0; v < 8; ++v) room[((wave * NT + u) * 8 + v) * 64 + lane] = floatx2{acc[t][u][2 * v], acc[t][u][2 * v + 1]};
         __syncthreads();
-        floatx2 sum[2] = {};
+        floatx2 sum[NT] = {};
 #pragma unroll
         for (int w = 0; w < GRAD_WAVES; ++w)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const floatx2 x = room[((w * 2 + u) * 8 + wave) * 64 + lane];
+            for (int u = 0; u < NT; ++u) {
+                const floatx2 x = room[((w * NT + u) * 8 + wave) * 64 + lane];
                 sum[u][0] += x[0];
                 sum[u][1] += x[1];
             }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int v = 2 * wave + i, row = tile / tiles_c * GRAD_K + 4 * (8 * (v / 4) + 4 * half + v % 4) + t;
+            const int v = 2 * wave + i, row = tile / tiles_c * (32 * MT) + MT * (8 * (v / 4) + 4 * half + v % 4) + t;
             float* to = out + (int64_t)row * ldp + c0;
-            if (row < a.k && c0 + 1 < a.c) {
-                const float both[2] = {sum[0][i], sum[1][i]};
-                store_piece<2>(to, both);
+            if (row < a.k && c0 + NT <= a.c) {
+                float all[NT];
+#pragma unroll
+                for (int u = 0; u < NT; ++u) all[u] = sum[u][i];
+                store_piece<NT>(to, all);
             } else if (row < a.k && c0 < a.c) {
                 *to = sum[0][i];
             }
@@ -401,12 +399,13 @@ void along_rows(int64_t n, int64_t pieces, F&& f) {
 
 }  // namespace
 
-// A compute unit holds one workgroup of the gradient at a time, and workgroup b runs on XCD b mod 8, so what s shares take is what the fullest XCD's 32 units take: rounds / s of what one
+// A compute unit holds one workgroup of the gradient at a time (two with narrow tiles), and workgroup b runs on XCD b mod 8, so what s shares take is what the fullest XCD's 32 units take:
+// rounds / s of what one
 // workgroup takes for all rows.  The fewest shares that come within a tenth of the least of that (more of them cost partial sums).  A share has 64 rows at least.
 // (300000 x 300, 100 columns, six tiles: 200 us with 42 shares, of which two XCDs had 36 workgroups.)
 int64_t cbm_grad_splits(int64_t n, int32_t k, int32_t c) {
-    constexpr int64_t UNITS = 32;
-    const int64_t tiles = ((int64_t)k + GRAD_K - 1) / GRAD_K * (((int64_t)c + GRAD_C - 1) / GRAD_C);
+    const int mt = grad_mt(k), nt = grad_nt(c);
+    const int64_t UNITS = 32 * grad_groups(mt, nt), tiles = ((int64_t)k + 32 * mt - 1) / (32 * mt) * (((int64_t)c + 32 * nt - 1) / (32 * nt));
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>((4 * CBM_XCD * UNITS + tiles - 1) / tiles, (n + 4 * GRAD_ROWS - 1) / (4 * GRAD_ROWS)));
     auto share = [&](int64_t s) {
         const int64_t fullest = s < CBM_XCD ? (s * tiles + CBM_XCD - 1) / CBM_XCD : (s + CBM_XCD - 1) / CBM_XCD * tiles;  // (the launch says why: shares are dealt out to XCDs)
@@ -455,16 +454,19 @@ cbm_status cbm_launch_checkpoint_grad(int64_t n, int32_t k, int32_t c, const int
     if (splits)
         cbm_with_type(type, [&](auto t) {
             using T = decltype(t);
-            const int tiles_c = (int)(((int64_t)c + GRAD_C - 1) / GRAD_C), tiles = (int)(((int64_t)k + GRAD_K - 1) / GRAD_K) * tiles_c;
+            const int mt = grad_mt(k), nt = grad_nt(c), tiles_c = (int)(((int64_t)c + 32 * nt - 1) / (32 * nt)), tiles = (int)(((int64_t)k + 32 * mt - 1) / (32 * mt)) * tiles_c;
             const int beside = std::min(CBM_XCD, splits);
             const unsigned grid = (unsigned)((splits + beside - 1) / beside * beside * tiles);
             const GradArgs<T> a{n, k, c, Q, ldq, E, lde, (const T*)dY, lddy};
             float* to = splits == 1 ? dW : parts;
             const int64_t ldp = splits == 1 ? lddw : c;
-            const int64_t far = std::max(std::max(ldq, lde), lddy * (int64_t)sizeof(T));
-            if (k < 4 || c < 2 || far >= 1 << 27) cbm_checkpoint_grad_kernel<T, GRAD_SINGLE><<<grid, 64 * GRAD_WAVES, 0, stream>>>(a, tiles_c, tiles, splits, to, ldp, size);
-            else if (k % 4 || c % 2) cbm_checkpoint_grad_kernel<T, GRAD_SHIFTED><<<grid, 64 * GRAD_WAVES, 0, stream>>>(a, tiles_c, tiles, splits, to, ldp, size);
-            else cbm_checkpoint_grad_kernel<T, GRAD_WHOLE><<<grid, 64 * GRAD_WAVES, 0, stream>>>(a, tiles_c, tiles, splits, to, ldp, size);
+            const bool near = std::max(std::max(ldq, lde), lddy * (int64_t)sizeof(T)) < 1 << 27;
+            auto go = [&](auto m, auto o) {
+                cbm_checkpoint_grad_kernel<T, decltype(m)::value, decltype(o)::value><<<grid, 64 * GRAD_WAVES, 0, stream>>>(a, tiles_c, tiles, splits, to, ldp, size, near);
+            };
+            using std::integral_constant;
+            auto narrow = [&](auto m) { nt == 1 ? go(m, integral_constant<int, 1>{}) : go(m, integral_constant<int, 2>{}); };
+            mt == 1 ? narrow(integral_constant<int, 1>{}) : mt == 2 ? narrow(integral_constant<int, 2>{}) : narrow(integral_constant<int, 4>{});
         });
     if (splits != 1 && splits <= FEW_PARTS) cbm_checkpoint_join_few_kernel<<<(unsigned)std::min<int64_t>((size + 255) / 256, 1 << 22), 256, 0, stream>>>(splits, size, c, parts, dW, lddw);
     else if (splits != 1) cbm_checkpoint_join_kernel<<<(unsigned)std::min<int64_t>((size + 31) / 32, 1 << 20), 1024, 0, stream>>>(splits, size, c, parts, dW, lddw);
