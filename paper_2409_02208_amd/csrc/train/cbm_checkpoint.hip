@@ -201,8 +201,8 @@ __device__ __forceinline__ void grad_load_whole(GradStep<T, MT, NT>& s, const Gr
     }
 }
 
-// near: eight rows are within 32 bits of an address
-template <class T, int MT, int NT>
+// near: eight rows are within 32 bits of an address.  SHIFT: MT does not divide k, or NT not c (2097152 x 128, 128 columns of bf16 160 us without shifts, 173 with them).
+template <class T, int MT, int NT, bool SHIFT>
 __global__ __launch_bounds__(64 * GRAD_WAVES, 2 * grad_groups(MT, NT)) void cbm_checkpoint_grad_kernel(GradArgs<T> a, int tiles_c, int tiles, int splits, float* __restrict__ parts, int64_t ldp,
                                                                                                     int64_t part, bool near) {
     constexpr int PARTS = std::is_same<T, float>::value ? 3 : std::is_same<T, _Float16>::value ? 2 : 1;  // 24, 11 and 8 bits, eight a part
@@ -241,10 +241,10 @@ __global__ __launch_bounds__(64 * GRAD_WAVES, 2 * grad_groups(MT, NT)) void cbm_
         } s;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            s.q[j] = (uint32_t)next.q[j] >> late_q;
+            s.q[j] = SHIFT ? (uint32_t)next.q[j] >> late_q : (uint32_t)next.q[j];
             s.step[j] = step_of(__builtin_amdgcn_ds_bpermute(from + 16 * j, (int)next.e));
             s.y[NT - 1][j] = (float)next.y[j][NT - 1];
-            if constexpr (NT == 2) s.y[0][j] = (float)(late_y ? next.y[j][1] : next.y[j][0]);
+            if constexpr (NT == 2) s.y[0][j] = (float)(SHIFT && late_y ? next.y[j][1] : next.y[j][0]);
         }
         if ((i + 1) * GRAD_ROWS > a.n) {
 #pragma unroll
@@ -462,7 +462,9 @@ cbm_status cbm_launch_checkpoint_grad(int64_t n, int32_t k, int32_t c, const int
             const int64_t ldp = splits == 1 ? lddw : c;
             const bool near = std::max(std::max(ldq, lde), lddy * (int64_t)sizeof(T)) < 1 << 27;
             auto go = [&](auto m, auto o) {
-                cbm_checkpoint_grad_kernel<T, decltype(m)::value, decltype(o)::value><<<grid, 64 * GRAD_WAVES, 0, stream>>>(a, tiles_c, tiles, splits, to, ldp, size, near);
+                constexpr int MT = decltype(m)::value, NT = decltype(o)::value;
+                if (MT == 4 && NT == 2 && k % MT == 0 && c % NT == 0) cbm_checkpoint_grad_kernel<T, 4, 2, false><<<grid, 64 * GRAD_WAVES, 0, stream>>>(a, tiles_c, tiles, splits, to, ldp, size, near);
+                else cbm_checkpoint_grad_kernel<T, MT, NT, true><<<grid, 64 * GRAD_WAVES, 0, stream>>>(a, tiles_c, tiles, splits, to, ldp, size, near);
             };
             using std::integral_constant;
             auto narrow = [&](auto m) { nt == 1 ? go(m, integral_constant<int, 1>{}) : go(m, integral_constant<int, 2>{}); };
