@@ -479,23 +479,25 @@ cbm_status cbm_launch_norm_backward(int64_t n, int32_t k, int32_t type, const vo
             const bool once = sums && few_rows(n, k) && pieces <= 1024;  // (dg and db in the same launch)
             const unsigned alone = once ? (unsigned)(((int64_t)k + 15) / 16) : 0;
             if (once) parts = nullptr;
-#define CBM_BACK(V_, LANES, R, THREADS)                                                                                                                                              \
-    (count = at_most(n, THREADS / LANES, most),                                                                                                                                      \
+#define CBM_BACK(V_, LANES, R, THREADS, GROUPS)                                                                                                                                           \
+    (count = at_most(n, THREADS / LANES, GROUPS),                                                                                                                                   \
      cbm_norm_back_kernel<T, V_, LANES, R, THREADS, WHOLE><<<(unsigned)(dX || !once ? count : 0) + alone, THREADS, 0, stream>>>(n, k, dY, lddy, X, ldx, gamma, mean, rstd, dX, lddx, parts, \
                                                                                                                                dX || !once ? (int)count : 0, dgamma, dbeta, far),      \
      joined = once)
-            if (k < V) CBM_BACK(1, 8, 1, BACK_THREADS);
-            else if (pieces <= 4) CBM_BACK(V, 4, 1, BACK_THREADS);
-            else if (pieces <= 8) CBM_BACK(V, 8, 1, BACK_THREADS);
-            else if (pieces <= 16) CBM_BACK(V, 16, 1, BACK_THREADS);
-            else if (pieces <= 32) CBM_BACK(V, 32, 1, BACK_THREADS);
-            else if (pieces <= 64) CBM_BACK(V, 64, 1, BACK_THREADS);
-            else if (pieces <= 128) CBM_BACK(V, 64, 2, 256);
-            else if (pieces <= 256) CBM_BACK(V, 256, 1, 256);
-            else if (pieces <= 512) CBM_BACK(V, 256, 2, 256);
-            else if (pieces <= 1024) CBM_BACK(V, 512, 2, 512);
-            else if (V == 4 && pieces <= 2048) CBM_BACK(V, 1024, 2, 1024);
-            else if (pieces <= (V == 4 ? 3072 : 2048)) CBM_BACK(V, 1024, V == 4 ? 3 : 2, 1024);
+            if (k < V) CBM_BACK(1, 8, 1, BACK_THREADS, BACK_GROUPS);
+            else if (pieces <= 4) CBM_BACK(V, 4, 1, BACK_THREADS, BACK_GROUPS);
+            else if (pieces <= 8) CBM_BACK(V, 8, 1, BACK_THREADS, BACK_GROUPS);
+            else if (pieces <= 16) CBM_BACK(V, 16, 1, BACK_THREADS, BACK_GROUPS);
+            else if (pieces <= 32) CBM_BACK(V, 32, 1, BACK_THREADS, BACK_GROUPS);
+            else if (pieces <= 64) CBM_BACK(V, 64, 1, BACK_THREADS, BACK_GROUPS);
+            else if (pieces <= 128) CBM_BACK(V, 64, 2, 256, BACK_GROUPS);
+            else if (pieces <= 256) CBM_BACK(V, 256, 1, 256, BACK_GROUPS);
+            else if (pieces <= 384) CBM_BACK(V, 256, 2, 256, BACK_GROUPS);
+            // half as many workgroups, of twice the waves: partial rows are long here (16384 x 4096 bf16 89.7 us with 512 workgroups, 85.2 with 256; 100000 x 1200 254 and 371)
+            else if (pieces <= 512) CBM_BACK(V, 512, 1, 512, BACK_GROUPS / 2);
+            else if (pieces <= 1024) CBM_BACK(V, 512, 2, 512, BACK_GROUPS / 2);
+            else if (V == 4 && pieces <= 2048) CBM_BACK(V, 1024, 2, 1024, BACK_GROUPS / 2);
+            else if (pieces <= (V == 4 ? 3072 : 2048)) CBM_BACK(V, 1024, V == 4 ? 3 : 2, 1024, BACK_GROUPS / 2);
             else {
                 if (dX) hipLaunchKernelGGL((cbm_norm_back_wide_kernel<T, V, WHOLE>), dim3((unsigned)std::min<int64_t>(n, 512)), dim3(1024), 0, stream, n, k, dY, lddy, X, ldx, gamma, mean, rstd, dX, lddx, far);
                 const int64_t across = (pieces + 255) / 256;
