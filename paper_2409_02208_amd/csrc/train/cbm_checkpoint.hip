@@ -401,21 +401,21 @@ void along_rows(int64_t n, int64_t pieces, F&& f) {
 
 // A compute unit holds one workgroup of the gradient at a time (two with narrow tiles), and workgroup b runs on XCD b mod 8, so what s shares take is what the fullest XCD's 32 units take:
 // rounds / s of what one
-// workgroup takes for all rows.  The fewest shares that come within a tenth of the least of that (more of them cost partial sums).  A share has 64 rows at least.
+// workgroup takes for all rows (more shares cost more partial sums).  A share has 64 rows at least.
 // (300000 x 300, 100 columns, six tiles: 200 us with 42 shares, of which two XCDs had 36 workgroups.)
 int64_t cbm_grad_splits(int64_t n, int32_t k, int32_t c) {
     const int mt = grad_mt(k), nt = grad_nt(c);
     const int64_t UNITS = 32 * grad_groups(mt, nt), tiles = ((int64_t)k + 32 * mt - 1) / (32 * mt) * (((int64_t)c + 32 * nt - 1) / (32 * nt));
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>((4 * CBM_XCD * UNITS + tiles - 1) / tiles, (n + 4 * GRAD_ROWS - 1) / (4 * GRAD_ROWS)));
-    auto share = [&](int64_t s) {
-        const int64_t fullest = s < CBM_XCD ? (s * tiles + CBM_XCD - 1) / CBM_XCD : (s + CBM_XCD - 1) / CBM_XCD * tiles;  // (the launch says why: shares are dealt out to XCDs)
-        return (double)((fullest + UNITS - 1) / UNITS) / (double)s;
+    auto rounds = [&](int64_t s) {
+        const int64_t fullest = s < CBM_XCD ? (s * tiles + CBM_XCD - 1) / CBM_XCD : (s + CBM_XCD - 1) / CBM_XCD * tiles;  // (the kernel says how shares are dealt out to XCDs)
+        return (fullest + UNITS - 1) / UNITS;
     };
-    double least = share(1);
-    for (int64_t s = 2; s <= most; ++s) least = std::min(least, share(s));
-    int64_t s = 1;
-    while (share(s) > 1.1 * least) ++s;
-    return s;
+    // the most shares for each number of rounds, from few rounds to many: the first that another does not beat by a tenth
+    int64_t best = 1;
+    for (int64_t s = 1; s <= most; ++s)
+        if (rounds(s) == rounds(best) ? s > best : (double)rounds(s) * best * 1.1 < (double)rounds(best) * s) best = s;
+    return best;
 }
 
 cbm_status cbm_launch_checkpoint_save(int64_t n, int32_t k, int32_t type, const void* X, int64_t ldx, int8_t* Q, int64_t ldq, uint8_t* E, int64_t lde, void* stream) {
