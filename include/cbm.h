@@ -357,7 +357,7 @@ size_t cbm_layer_norm_workspace_bytes(int64_t n, int32_t k);
  * value other than zero keeps its sign, and x~ is a bf16 value.  A block with a value that is not finite comes back as NaN throughout.
  *   Q   n x k int8, leading dimension ldq >= k: the q.
  *   E   n x ceil(k / 32) uint8, leading dimension lde: e + 127; 255 for a block that is not finite (its q are 0).
- * k not a multiple of 4, or of 32, is not an error; the weights' gradient then loads Q a byte at a time.
+ * k may be any number of columns; a row of Q may start at any byte.
  *   cbm_checkpoint_save           X (n x k, of `type`) -> Q, E.
  *   cbm_checkpoint_restore        Q, E -> X (rounded to `type`; exact in fp32 and bf16).
  *   cbm_checkpoint_relu_backward  dX = dY where q > 0, else 0 (n x k, of `type`; NaN in a block that is not finite): the backward pass of a
@@ -386,7 +386,7 @@ size_t cbm_checkpoint_workspace_bytes(int64_t n, int32_t k, int32_t c);
  *   stats        n x 2: m and l, which the backward pass reads.
  *   top          0 to 32 alternatives: top_values (n x top) receives the largest log p in descending order, top_columns (n x top) their classes, the
  *                lower one first among equal scores; where fewer classes are not ruled out, -infinity and -1.
- *   workspace    cbm_log_probs_workspace_bytes(n, c, top) bytes; may be 0 (few and long rows are shared by several workgroups).
+ *   workspace    cbm_log_probs_workspace_bytes(n, c, top) bytes; 0 but for few rows of over 1,024 columns (those may be shared by several workgroups).
  * logp, entropy and stats may be NULL; fp32, packed.  A row with every class ruled out has m = l = log p[label] = -infinity and entropy 0.  A row
  * with NaN or +infinity has NaN for all of it (0 without a label, classes -1).
  *

@@ -19,7 +19,7 @@ constexpr int NOT_FINITE = 255;  // the code of a block that holds a value that 
 __device__ __forceinline__ float step_of(uint32_t code) { return __uint_as_float(code << 23); }  // 2^(code - 127); of NOT_FINITE: infinity
 __device__ __forceinline__ float value_of(int q, uint32_t code) { return code == NOT_FINITE ? NAN : (float)q * step_of(code); }
 
-// What a lane has of a row: V columns from `at` on, the first `seen` of them another lane's; fewer than V columns where the row has no more (SHORT rows).
+// What a lane has of a row: V columns from `at` on, the first `seen` of them another lane's; fewer than V columns where the row has no more (k < V).
 template <int V, class T>
 __device__ __forceinline__ void load_row_piece(float (&x)[V], const T* row, const Place<V, false>& p, int k) {
     if (k >= V) {
@@ -41,7 +41,8 @@ __device__ __forceinline__ void load_row_bytes(int (&q)[V], const int8_t* row, c
     }
 }
 
-// LANES lanes a row (and a share of its columns: blockIdx.y), R times V columns a lane.  A block of 32 columns is 32 / V lanes.
+// Save.  LANES lanes a row (and a share of its columns: blockIdx.y), R times V columns a lane.  A block of 32 columns is 32 / V lanes, which find its largest value by DPP; nothing
+// else is shared.  Bound by memory: 19717 x 500 fp32 11 to 13 us for 49.6 MB, of which the caches hold some (4 TB/s; waves waiting for 64 % of their cycles).
 template <class T, int LANES, int R>
 __global__ __launch_bounds__(256) void cbm_checkpoint_save_kernel(int64_t n, int k, const T* __restrict__ X, int64_t ldx, int8_t* __restrict__ Q, int64_t ldq,
                                                                   uint8_t* __restrict__ E, int64_t lde) {
@@ -94,7 +95,8 @@ __global__ __launch_bounds__(256) void cbm_checkpoint_save_kernel(int64_t n, int
     }
 }
 
-// GATED: dx = q > 0 ? dy : 0, else x~.
+// Restore, and the backward pass of a ReLU (GATED: dx = q > 0 ? dy : 0), in the shape of saving.  Bound by memory: 19717 x 500 restored to fp32 8.6 to 10 us for 49.6 MB (5 TB/s);
+// gated, 235868 x 128 bf16 32 us for 152 MB (4.7 TB/s; waves waiting for 82 % of their cycles).
 template <class T, int LANES, int R, bool GATED>
 __global__ __launch_bounds__(256) void cbm_checkpoint_load_kernel(int64_t n, int k, const int8_t* __restrict__ Q, int64_t ldq, const uint8_t* __restrict__ E, int64_t lde, const T* dY,
                                                                   int64_t lddy, T* out, int64_t ldo, bool far) {
@@ -134,7 +136,10 @@ __global__ __launch_bounds__(256) void cbm_checkpoint_load_kernel(int64_t n, int
 // eight rows, MT (4) neighbouring columns of Q and NT (2) of dY: 32 MT columns of Q and 32 NT of dY by 16 rows a wave, with neither LDS nor transposes, only with columns of dW
 // in an order of their own (tile t has columns MT i + t of Q, and NT i + t of dY).  x~ is a bf16 value; dY is split into one (bf16), two (fp16) or three (fp32) bf16 values that add
 // up to it, so the products are exact and the sums fp32.  The waves of a workgroup and the workgroups of a tile share the rows; a workgroup adds its waves' sums in LDS, in order.
-// Narrow matrices take narrow tiles, of which a compute unit holds two workgroups.
+// Narrow matrices take narrow tiles, of which a compute unit holds two workgroups (524288 x 32, 32 columns of bf16 45 us with wide tiles, 20 with narrow ones).
+// The next step's loads are under way while a step is multiplied; two steps ahead cost registers and gained nothing (279 us, 292).  2097152 x 128, 128 columns of fp32: 283 us for
+// 1.35 GB (4.8 TB/s) and 206 GFLOP of parts (730 TFLOP/s, the matrix cores busy for 40 % of the cycles): bound by memory, with the vector instructions
+// that split dY and widen Q next to it.  132534 x 100, 47 columns: 16 us, of which 5.5 are there whatever the rows (the launch, first loads, sums in LDS).
 constexpr int FEW_PARTS = 16;
 constexpr int GRAD_WAVES = 8, GRAD_ROWS = 16;
 int grad_mt(int32_t k) { return k <= 32 ? 1 : k <= 64 ? 2 : 4; }
@@ -343,7 +348,8 @@ __global__ __launch_bounds__(64 * GRAD_WAVES, 2 * grad_groups(MT, NT)) void cbm_
     }
 }
 
-// dW from `count` partial sums, in order: 32 values a workgroup, the partial sums shared by its 32 groups of lanes.
+// dW from `count` partial sums, in order: 32 values a workgroup, the partial sums shared by its 32 groups of lanes.  Bound by the latency of a launch and of 16 loads a lane: 256 of
+// 100 x 47 4 to 5 us.
 __global__ __launch_bounds__(1024) void cbm_checkpoint_join_kernel(int count, int64_t size, int c, const float* __restrict__ parts, float* __restrict__ dW, int64_t lddw) {
     __shared__ float room[32][33];
     const int slice = threadIdx.x / 32;
@@ -365,7 +371,7 @@ __global__ __launch_bounds__(1024) void cbm_checkpoint_join_kernel(int count, in
     }
 }
 
-// The same with few partial sums: a value a thread.
+// The same with few partial sums: a value a thread (20000 x 1024, 512 columns: 4 partial sums of 2 MB).
 __global__ __launch_bounds__(256) void cbm_checkpoint_join_few_kernel(int count, int64_t size, int c, const float* __restrict__ parts, float* __restrict__ dW, int64_t lddw) {
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
         float s = 0.0f;
@@ -400,9 +406,8 @@ void along_rows(int64_t n, int64_t pieces, F&& f) {
 }  // namespace
 
 // A compute unit holds one workgroup of the gradient at a time (two with narrow tiles), and workgroup b runs on XCD b mod 8, so what s shares take is what the fullest XCD's 32 units take:
-// rounds / s of what one
-// workgroup takes for all rows (more shares cost more partial sums).  A share has 64 rows at least.
-// (300000 x 300, 100 columns, six tiles: 200 us with 42 shares, of which two XCDs had 36 workgroups.)
+// rounds / s of what one workgroup takes for all rows (more shares cost more partial sums).  A share has 64 rows at least.
+// (300000 x 300, 100 columns, six tiles: 200 us with 42 shares, of which two XCDs had 36 workgroups, 120 with 40.)
 int64_t cbm_grad_splits(int64_t n, int32_t k, int32_t c) {
     const int mt = grad_mt(k), nt = grad_nt(c);
     const int64_t UNITS = 32 * grad_groups(mt, nt), tiles = ((int64_t)k + 32 * mt - 1) / (32 * mt) * (((int64_t)c + 32 * nt - 1) / (32 * nt));
