@@ -1,6 +1,6 @@
-"""ctypes binding of libcbm.so: same names as the C ABI (include/cbm.h), argument
-marshalling only.  PyTorch tensors supply device memory and the stream; every
-step of the product runs in the library's HIP kernels.  There is no fallback:
+"""Binding of libcbm.so: same names as the C ABI (include/cbm.h), argument marshalling
+only, by ctypes, or by the module _calls.so for the operators between the products.
+PyTorch tensors supply device memory and the stream; every step of the product runs in the library's HIP kernels.  There is no fallback:
 a missing library raises."""
 from __future__ import annotations
 
@@ -63,14 +63,12 @@ class cbm_launch_record(C.Structure):
 
 
 _LIB = None
-_F32 = _INT32 = None  # torch.float32 and int32, known once the library is loaded
-_DTYPES = {}  # torch's types of the operators between the products: cbm_dtype, likewise
-_INT8, _UINT8 = {}, {}
-_LABELS = {}  # torch's types of labels: bits
+_F32 = None  # torch.float32, known once the library is loaded
+_CALLS = None
 
 
 def _lib():
-    global _LIB, _F32, _INT32
+    global _LIB, _F32
     if _LIB is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is not built: run `python -m paper_2409_02208_amd.build`")
@@ -78,10 +76,7 @@ def _lib():
         # the library binds to that same runtime: device pointers and streams are only meaningful within one.
         import torch
 
-        _F32, _INT32 = torch.float32, torch.int32
-        _DTYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
-        _INT8[torch.int8] = _UINT8[torch.uint8] = 0
-        _LABELS.update({torch.int32: 32, torch.int64: 64})
+        _F32 = torch.float32
         lib = C.CDLL(LIB_PATH)
         vp, i64, i32, f32p = C.c_void_p, C.c_int64, C.c_int32, C.c_void_p
         lib.cbm_build.argtypes = [i64, i64, vp, vp, C.POINTER(cbm_build_opts), C.POINTER(vp)]
@@ -276,71 +271,21 @@ def cbm_gcn2_forward(h: Handle, X, W0, W1, out, workspace, stream=None):
     return out
 
 
-# The operators between the products.  A small call's time is this code as much as the launch, so every attribute of a tensor is asked for once, and what is checked
-# is compared in one go.
-def _matrix(t, name, dtypes):
-    """(address, leading dimension, rows, columns, code of its type in `dtypes`) of a device matrix."""
-    code = dtypes.get(t.dtype)
-    if code is not None and t.is_cuda:
-        strides = t.stride()
-        if len(strides) == 2:
-            rows, cols = t.shape
-            ld, unit = strides
-            if unit == 1 or cols <= 1:
-                return t.data_ptr(), ld if rows > 1 or ld > cols else cols, rows, cols, code
-    raise ValueError(f"{name} must be a 2-D device tensor of {', '.join(str(d) for d in dtypes)} with unit column stride")
+def _calls():
+    """The module that reads tensors for the operators between the products: a small call's time is the host's."""
+    global _CALLS
+    if _CALLS is None:
+        _lib()  # PyTorch, then the library that the module is linked to
+        if not os.path.exists(os.path.join(_PKG, "_calls.so")):
+            raise RuntimeError("_calls.so is not built: run `python -m paper_2409_02208_amd.build`")
+        from . import _calls as module
 
-
-def _packed(t, name, shape, dtype):
-    """Address of a packed device tensor; None stays None."""
-    if t is None:
-        return None
-    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
-        return t.data_ptr()
-    raise ValueError(f"{name} must be a packed device tensor of {dtype} and shape {tuple(shape)}")
-
-
-def _workspace(t):
-    if t is None:
-        return None, 0
-    if t.is_cuda and t.is_contiguous():
-        return t.data_ptr(), t.nbytes
-    raise ValueError("workspace must be a packed device tensor")
-
-
-def _labels(t, n):
-    """(address, bits) of n labels; none: (None, 64)."""
-    if t is None:
-        return None, 64
-    bits = _LABELS.get(t.dtype)
-    if bits is None:
-        raise ValueError("labels must be int32 or int64")
-    return _packed(t, "labels", (n,), t.dtype), bits
-
-
-def _alike(a, b, what):
-    """Of what _matrix gives: the same rows, columns and type."""
-    if a[2:] != b[2:]:
-        raise ValueError(f"{what} must have the same shape and type")
-
-
-def _kept(Q, E):
-    """(arguments, n, k) of an 8-bit checkpoint."""
-    qp, ldq, n, k, _ = _matrix(Q, "Q", _INT8)
-    ep, lde, rows, blocks, _ = _matrix(E, "E", _UINT8)
-    if rows != n or blocks != (k + 31) // 32:
-        raise ValueError("E must have a row for each of Q's and a column for each 32 of Q's")
-    return (qp, ldq, ep, lde), n, k
+        _CALLS = module
+    return _CALLS
 
 
 def cbm_layer_norm(X, gamma, beta, eps: float, Y, mean=None, rstd=None, stream=None):
-    lib = _LIB or _lib()
-    x, y = _matrix(X, "X", _DTYPES), _matrix(Y, "Y", _DTYPES)
-    _alike(x, y, "X and Y")
-    xp, ldx, n, k, dtype = x
-    rows, cols, f32 = (n,), (k,), _F32
-    status = lib.cbm_layer_norm(n, k, dtype, xp, ldx, _packed(gamma, "gamma", cols, f32), _packed(beta, "beta", cols, f32), eps, y[0], y[1], _packed(mean, "mean", rows, f32),
-                                _packed(rstd, "rstd", rows, f32), _current_stream() if stream is None else _stream_ptr(stream))
+    status = (_CALLS or _calls()).layer_norm(X, gamma, beta, eps, Y, mean, rstd, _current_stream() if stream is None else _stream_ptr(stream))
     if status:
         raise CbmError(status, "cbm_layer_norm")
     return Y
@@ -351,58 +296,28 @@ def cbm_layer_norm_workspace_bytes(n: int, k: int) -> int:
 
 
 def cbm_layer_norm_backward(dY, X, gamma, mean, rstd, dX, dgamma, dbeta, workspace, stream=None):
-    lib = _LIB or _lib()
-    g, x = _matrix(dY, "dY", _DTYPES), _matrix(X, "X", _DTYPES)
-    _alike(g, x, "dY and X")
-    gp, ldg, n, k, dtype = g
-    dp, ldd = None, k
-    if dX is not None:
-        d = _matrix(dX, "dX", _DTYPES)
-        _alike(g, d, "dY and dX")
-        dp, ldd = d[:2]
-    rows, cols, f32 = (n,), (k,), _F32
-    wp, wbytes = _workspace(workspace)
-    status = lib.cbm_layer_norm_backward(n, k, dtype, gp, ldg, x[0], x[1], _packed(gamma, "gamma", cols, f32), _packed(mean, "mean", rows, f32), _packed(rstd, "rstd", rows, f32), dp, ldd,
-                                         _packed(dgamma, "dgamma", cols, f32), _packed(dbeta, "dbeta", cols, f32), wp, wbytes,
-                                         _current_stream() if stream is None else _stream_ptr(stream))
+    status = (_CALLS or _calls()).layer_norm_backward(dY, X, gamma, mean, rstd, dX, dgamma, dbeta, workspace, _current_stream() if stream is None else _stream_ptr(stream))
     if status:
         raise CbmError(status, "cbm_layer_norm_backward")
     return dX
 
 
 def cbm_checkpoint_save(X, Q, E, stream=None):
-    lib = _LIB or _lib()
-    xp, ldx, n, k, dtype = _matrix(X, "X", _DTYPES)
-    kept, rows, cols = _kept(Q, E)
-    if rows != n or cols != k:
-        raise ValueError("X and Q must have the same shape")
-    status = lib.cbm_checkpoint_save(n, k, dtype, xp, ldx, *kept, _current_stream() if stream is None else _stream_ptr(stream))
+    status = (_CALLS or _calls()).checkpoint_save(X, Q, E, _current_stream() if stream is None else _stream_ptr(stream))
     if status:
         raise CbmError(status, "cbm_checkpoint_save")
     return Q
 
 
 def cbm_checkpoint_restore(Q, E, X, stream=None):
-    lib = _LIB or _lib()
-    xp, ldx, n, k, dtype = _matrix(X, "X", _DTYPES)
-    kept, rows, cols = _kept(Q, E)
-    if rows != n or cols != k:
-        raise ValueError("X and Q must have the same shape")
-    status = lib.cbm_checkpoint_restore(n, k, *kept, dtype, xp, ldx, _current_stream() if stream is None else _stream_ptr(stream))
+    status = (_CALLS or _calls()).checkpoint_restore(Q, E, X, _current_stream() if stream is None else _stream_ptr(stream))
     if status:
         raise CbmError(status, "cbm_checkpoint_restore")
     return X
 
 
 def cbm_checkpoint_relu_backward(Q, E, dY, dX, stream=None):
-    lib = _LIB or _lib()
-    g, d = _matrix(dY, "dY", _DTYPES), _matrix(dX, "dX", _DTYPES)
-    _alike(g, d, "dY and dX")
-    kept, rows, cols = _kept(Q, E)
-    gp, ldg, n, k, dtype = g
-    if rows != n or cols != k:
-        raise ValueError("dY and Q must have the same shape")
-    status = lib.cbm_checkpoint_relu_backward(n, k, *kept, dtype, gp, ldg, d[0], d[1], _current_stream() if stream is None else _stream_ptr(stream))
+    status = (_CALLS or _calls()).checkpoint_relu_backward(Q, E, dY, dX, _current_stream() if stream is None else _stream_ptr(stream))
     if status:
         raise CbmError(status, "cbm_checkpoint_relu_backward")
     return dX
@@ -413,14 +328,7 @@ def cbm_checkpoint_workspace_bytes(n: int, k: int, c: int) -> int:
 
 
 def cbm_checkpoint_weight_grad(Q, E, dY, dW, workspace, stream=None):
-    lib = _LIB or _lib()
-    gp, ldg, rows, c, dtype = _matrix(dY, "dY", _DTYPES)
-    kept, n, k = _kept(Q, E)
-    wp, ldw, kw, cw = _dev_f32(dW, "dW")
-    if rows != n or kw != k or cw != c:
-        raise ValueError("shape mismatch")
-    sp, sbytes = _workspace(workspace)
-    status = lib.cbm_checkpoint_weight_grad(n, k, c, *kept, dtype, gp, ldg, wp, ldw, sp, sbytes, _current_stream() if stream is None else _stream_ptr(stream))
+    status = (_CALLS or _calls()).checkpoint_weight_grad(Q, E, dY, dW, workspace, _current_stream() if stream is None else _stream_ptr(stream))
     if status:
         raise CbmError(status, "cbm_checkpoint_weight_grad")
     return dW
@@ -431,30 +339,14 @@ def cbm_log_probs_workspace_bytes(n: int, c: int, top: int = 0) -> int:
 
 
 def cbm_log_probs(Z, labels, logp, entropy=None, stats=None, top_values=None, top_columns=None, workspace=None, stream=None):
-    lib = _LIB or _lib()
-    zp, ldz, n, c, dtype = _matrix(Z, "Z", _DTYPES)
-    lp, bits = _labels(labels, n)
-    top, tv, tc, f32, rows = 0, None, None, _F32, (n,)
-    if top_values is not None or top_columns is not None:
-        top = (top_columns if top_values is None else top_values).shape[-1]
-        tv, tc = _packed(top_values, "top_values", (n, top), f32), _packed(top_columns, "top_columns", (n, top), _INT32)
-    wp, wbytes = _workspace(workspace)
-    status = lib.cbm_log_probs(n, c, dtype, zp, ldz, lp, bits, _packed(logp, "logp", rows, f32), _packed(entropy, "entropy", rows, f32), _packed(stats, "stats", (n, 2), f32), top, tv, tc,
-                               wp, wbytes, _current_stream() if stream is None else _stream_ptr(stream))
+    status = (_CALLS or _calls()).log_probs(Z, labels, logp, entropy, stats, top_values, top_columns, workspace, _current_stream() if stream is None else _stream_ptr(stream))
     if status:
         raise CbmError(status, "cbm_log_probs")
     return logp
 
 
 def cbm_log_probs_backward(Z, labels, stats, entropy, dlogp, dentropy, dZ, stream=None):
-    lib = _LIB or _lib()
-    z, d = _matrix(Z, "Z", _DTYPES), _matrix(dZ, "dZ", _DTYPES)
-    _alike(z, d, "Z and dZ")
-    zp, ldz, n, c, dtype = z
-    rows, f32 = (n,), _F32
-    lp, bits = _labels(labels, n)
-    status = lib.cbm_log_probs_backward(n, c, dtype, zp, ldz, lp, bits, _packed(stats, "stats", (n, 2), f32), _packed(entropy, "entropy", rows, f32), _packed(dlogp, "dlogp", rows, f32),
-                                        _packed(dentropy, "dentropy", rows, f32), d[0], d[1], _current_stream() if stream is None else _stream_ptr(stream))
+    status = (_CALLS or _calls()).log_probs_backward(Z, labels, stats, entropy, dlogp, dentropy, dZ, _current_stream() if stream is None else _stream_ptr(stream))
     if status:
         raise CbmError(status, "cbm_log_probs_backward")
     return dZ

@@ -1,4 +1,4 @@
-"""Compile libcbm.so (HIP kernels + host builder + C ABI) for gfx950, in-tree."""
+"""Compile libcbm.so (HIP kernels + host builder + C ABI) for gfx950, and the CPython module _calls.so that reads tensors for it, in-tree."""
 from __future__ import annotations
 
 import os
@@ -10,6 +10,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libcbm.so")
+CALLS = os.path.join(PKG, "_calls.so")
+CALLS_SOURCE = "train/cbm_python.cpp"
 SOURCES = ["cbm_api.cpp", "cbm_builder.cpp", "cbm_kernels.hip", "cbm_blocks.hip", "cbm_sums.hip", "cbm_flat.hip", "cbm_gemm.hip", "cbm_gemm_split.hip", "cbm_gemm_held.hip", "cbm_build_kernels.hip",
            "train/cbm_api_train.cpp", "train/cbm_norm.hip", "train/cbm_checkpoint.hip", "train/cbm_scores.hip"]
 
@@ -64,6 +66,25 @@ def _run(cmd):
         sys.stderr.write("\n".join(warn) + "\n")
 
 
+def _calls_flags() -> list:
+    """PyTorch's and Python's headers (as system headers: their warnings are theirs)."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+
+    headers = cpp_extension.include_paths() + [sysconfig.get_paths()["include"]]
+    return [f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}"] + [a for d in headers for a in ("-isystem", d)]
+
+
+def link_calls(obj: str) -> None:
+    """PyTorch's libraries are in the process, and libcbm.so beside the module, before it is loaded."""
+    from torch.utils import cpp_extension
+
+    _run([HIPCC, "-shared", "-fPIC", "-no-hip-rt", obj, "-o", CALLS, "-L" + PKG, "-lcbm", "-Wl,-rpath,$ORIGIN"] + ["-L" + d for d in cpp_extension.library_paths()] +
+         ["-ltorch_python", "-ltorch_cpu", "-lc10"])
+
+
 def build(verbose: bool = False) -> str:
     objdir = os.path.join(PKG, "_build")
     os.makedirs(objdir, exist_ok=True)
@@ -74,11 +95,14 @@ def build(verbose: bool = False) -> str:
         objs.append(obj)
         flags = COMMON + (DEVICE + RESOURCES if src.endswith(".hip") else [])
         cmds.append([HIPCC] + flags + ["-c", os.path.join(CSRC, src), "-o", obj])
+    calls = os.path.join(objdir, CALLS_SOURCE.replace("/", "_") + ".o")
+    cmds.append([HIPCC] + COMMON + _calls_flags() + ["-c", os.path.join(CSRC, CALLS_SOURCE), "-o", calls])
     with ThreadPoolExecutor(max_workers=4) as ex:
         list(ex.map(_run, cmds))
     _run([HIPCC, "-shared", "-fPIC"] + DEVICE + objs + ["-o", LIB, "-lpthread"])
+    link_calls(calls)
     if verbose:
-        print("built", LIB)
+        print("built", LIB, CALLS)
     return LIB
 
 
