@@ -50,6 +50,24 @@ __device__ __forceinline__ void row_sum2(float& a, float& b, floatx2* room, int&
     }
 }
 
+// V values of gamma or beta from `at` on; `other` where there are none.
+template <int V>
+__device__ __forceinline__ void load_columns(float (&x)[V], const float* p, int at, float other) {
+    if (p) {
+        constexpr int W = V < 4 ? V : 4;
+#pragma unroll
+        for (int w = 0; w < V; w += W) {
+            float four[W];
+            load_piece<W>(four, p + at + w);
+#pragma unroll
+            for (int j = 0; j < W; ++j) x[w + j] = four[j];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = other;
+    }
+}
+
 // Forward.  LANES lanes have a row, each R pieces of V columns: as few lanes as hold a row in up to two pieces, so that a wave's reductions serve several rows, and a workgroup
 // once a wave would need more than two.  The grid is what the compute units hold at once, and workgroups walk on over the rows, so gamma and beta are loaded once a workgroup
 // (a workgroup for every few rows: 2097152 x 128 fp32 570 us for 454).  Bound by memory: 2097152 x 128 fp32 440 us, 4.9 TB/s of 2.15 GB, waves waiting for 60 % of their cycles;
@@ -66,11 +84,8 @@ __global__ __launch_bounds__(LANES > NORM_THREADS ? LANES : NORM_THREADS) void c
 #pragma unroll
     for (int c = 0; c < R; ++c) {
         const Place<V, WHOLE> p(c * LANES + lane, k);
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            g[c][j] = gamma ? gamma[p.at + j] : 1.0f;
-            b[c][j] = beta ? beta[p.at + j] : 0.0f;
-        }
+        load_columns<V>(g[c], gamma, p.at, 1.0f);
+        load_columns<V>(b[c], beta, p.at, 0.0f);
     }
     typename Piece<T, V>::type next[R];  // AHEAD: of the workgroup's next row, whose loads pass the barriers of this one
     constexpr bool AHEAD = LANES > 64;
@@ -153,8 +168,11 @@ __global__ __launch_bounds__(1024) void cbm_norm_wide_kernel(int64_t n, int k, c
         for (int c = threadIdx.x; c < pieces; c += 1024) {
             const Place<V, WHOLE> p(c, k);
             load_piece<V>(x, x_row + p.at);
+            float g[V], b[V];
+            load_columns<V>(g, gamma, p.at, 1.0f);
+            load_columns<V>(b, beta, p.at, 0.0f);
 #pragma unroll
-            for (int j = 0; j < V; ++j) x[j] = (x[j] - m) * r * (gamma ? gamma[p.at + j] : 1.0f) + (beta ? beta[p.at + j] : 0.0f);
+            for (int j = 0; j < V; ++j) x[j] = (x[j] - m) * r * g[j] + b[j];
             store_piece<V>(Y + row * ldy + p.at, x, far);
         }
         if (threadIdx.x == 0) {
@@ -215,11 +233,9 @@ __global__ __launch_bounds__(THREADS) void cbm_norm_back_kernel(int64_t n, int k
 #pragma unroll
     for (int c = 0; c < R; ++c) {
         const Place<V, WHOLE> p(c * LANES + lane, k);
+        load_columns<V>(g[c], gamma, p.at, 1.0f);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            g[c][j] = gamma ? gamma[p.at + j] : 1.0f;
-            dg[c][j] = db[c][j] = 0.0f;
-        }
+        for (int j = 0; j < V; ++j) dg[c][j] = db[c][j] = 0.0f;
     }
     typename Piece<T, V>::type next_x[R], next_dy[R];
     float next_m, next_r;
@@ -341,9 +357,11 @@ __global__ __launch_bounds__(1024) void cbm_norm_back_wide_kernel(int64_t n, int
             const Place<V, WHOLE> p(c, k);
             load_piece<V>(x, X + row * ldx + p.at);
             load_piece<V>(dy, dY + row * lddy + p.at);
+            float g[V];
+            load_columns<V>(g, gamma, p.at, 1.0f);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float u = dy[j] * (gamma ? gamma[p.at + j] : 1.0f);
+                const float u = dy[j] * g[j];
                 sum += p.counts(j) ? u : 0.0f;
                 along += p.counts(j) ? u * ((x[j] - m) * r) : 0.0f;
             }
@@ -355,8 +373,10 @@ __global__ __launch_bounds__(1024) void cbm_norm_back_wide_kernel(int64_t n, int
             const Place<V, WHOLE> p(c, k);
             load_piece<V>(x, X + row * ldx + p.at);
             load_piece<V>(dy, dY + row * lddy + p.at);
+            float g[V];
+            load_columns<V>(g, gamma, p.at, 1.0f);
 #pragma unroll
-            for (int j = 0; j < V; ++j) x[j] = r * (dy[j] * (gamma ? gamma[p.at + j] : 1.0f) - sum - (x[j] - m) * r * along);
+            for (int j = 0; j < V; ++j) x[j] = r * (dy[j] * g[j] - sum - (x[j] - m) * r * along);
             store_piece<V>(dX + row * lddx + p.at, x, far);
         }
     }
@@ -445,7 +465,7 @@ cbm_status cbm_launch_norm(int64_t n, int32_t k, int32_t type, const void* X_, i
         const int64_t pieces = ((int64_t)k + V - 1) / V;
         const bool far = n * k * (int64_t)sizeof(T) >= CBM_FAR_BYTES;
 #define CBM_NORM(V_, LANES, R)                                                                                                                                              \
-    hipLaunchKernelGGL((cbm_norm_kernel<T, V_, LANES, R, WHOLE>), dim3((unsigned)at_most(n, (LANES > NORM_THREADS ? LANES : NORM_THREADS) / LANES, 256 * (LANES > NORM_THREADS ? 2 : 8))), \
+    hipLaunchKernelGGL((cbm_norm_kernel<T, V_, LANES, R, WHOLE>), dim3((unsigned)at_most(n, (LANES > NORM_THREADS ? LANES : NORM_THREADS) / LANES, 256 * (LANES == 1024 ? 1 : LANES > NORM_THREADS ? 2 : 8))), \
                        dim3(LANES > NORM_THREADS ? LANES : NORM_THREADS), 0, stream, n, k, X, ldx, gamma, beta, eps, Y, ldy, mean, rstd, far)
         if (k < V) CBM_NORM(1, 8, 1);  // (V = 1: every place is whole)
         else if (pieces <= 4) CBM_NORM(V, 4, 1);
