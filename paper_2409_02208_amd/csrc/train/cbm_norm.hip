@@ -68,6 +68,25 @@ __device__ __forceinline__ void load_columns(float (&x)[V], const float* p, int 
     }
 }
 
+// The sums of a piece's columns, those that count.
+template <int V, bool WHOLE>
+__device__ __forceinline__ void store_columns(float* out, const float (&x)[V], const Place<V, WHOLE>& p) {
+    if (p.seen <= 0) {
+        constexpr int W = V < 4 ? V : 4;
+#pragma unroll
+        for (int w = 0; w < V; w += W) {
+            float four[W];
+#pragma unroll
+            for (int j = 0; j < W; ++j) four[j] = x[w + j];
+            store_piece<W>(out + p.at + w, four);
+        }
+    } else if (p.any()) {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (p.counts(j)) out[p.at + j] = x[j];
+    }
+}
+
 // Forward.  LANES lanes have a row, each R pieces of V columns: as few lanes as hold a row in up to two pieces, so that a wave's reductions serve several rows, and a workgroup
 // once a wave would need more than two.  The grid is what the compute units hold at once, and workgroups walk on over the rows, so gamma and beta are loaded once a workgroup
 // (a workgroup for every few rows: 2097152 x 128 fp32 570 us for 454).  Bound by memory: 2097152 x 128 fp32 440 us, 4.9 TB/s of 2.15 GB, waves waiting for 60 % of their cycles;
@@ -301,12 +320,8 @@ __global__ __launch_bounds__(THREADS) void cbm_norm_back_kernel(int64_t n, int k
 #pragma unroll
         for (int c = 0; c < R; ++c) {
             const Place<V, WHOLE> p(c * LANES + lane, k);
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (p.counts(j)) {
-                    out[p.at + j] = dg[c][j];
-                    out[k + p.at + j] = db[c][j];
-                }
+            store_columns<V, WHOLE>(out, dg[c], p);
+            store_columns<V, WHOLE>(out + k, db[c], p);
         }
     } else {
         const int wave = threadIdx.x / 64;
@@ -399,13 +414,9 @@ __global__ __launch_bounds__(256) void cbm_norm_back_columns_kernel(int64_t n, i
             db[j] += dy[j];
         }
     }
-    float* out = parts + (int64_t)blockIdx.y * 2 * k + p.at;
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-        if (p.counts(j)) {
-            out[j] = dg[j];
-            out[k + j] = db[j];
-        }
+    float* out = parts + (int64_t)blockIdx.y * 2 * k;
+    store_columns<V, WHOLE>(out, dg, p);
+    store_columns<V, WHOLE>(out + k, db, p);
 }
 
 // dg and db from `count` partial rows of each, in a fixed order: 32 columns a workgroup, the partial rows shared by its 32 groups of lanes, each with 16 loads under way.  Bound by
