@@ -61,9 +61,9 @@ __global__ __launch_bounds__(256) void cbm_checkpoint_save_kernel(int64_t n, int
             uint32_t largest = 0;
 #pragma unroll
             for (int j = 0; j < V; ++j) largest = max(largest, p.counts(j) ? __float_as_uint(x[i][j]) & 0x7fffffffu : 0u);
-            largest = max(largest, lane_other<1>(largest));
-            largest = max(largest, lane_other<2>(largest));
-            if constexpr (PER_BLOCK == 8) largest = max(largest, lane_other<4>(largest));
+            if constexpr (LANES >= 2) largest = max(largest, lane_other<1>(largest));
+            if constexpr (LANES >= 4) largest = max(largest, lane_other<2>(largest));
+            if constexpr (LANES >= 8 && PER_BLOCK == 8) largest = max(largest, lane_other<4>(largest));
             const bool finite = largest < 0x7f800000u;
             const uint32_t code = finite ? (uint32_t)max((int)(largest >> 23) - 6, 1) : NOT_FINITE;
             const float up = __uint_as_float((254u - (finite ? code : 127u)) << 23);
@@ -396,7 +396,10 @@ void along_rows(int64_t n, int64_t pieces, F&& f) {
         f(lanes, each, dim3((unsigned)std::min<int64_t>((n + ROWS - 1) / ROWS, 1 << 23), (unsigned)((pieces + AT_ONCE - 1) / AT_ONCE)));
     };
     using std::integral_constant;
-    if (pieces <= 8) go(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+    if (pieces <= 1) go(integral_constant<int, 1>{}, integral_constant<int, 1>{});
+    else if (pieces <= 2) go(integral_constant<int, 2>{}, integral_constant<int, 1>{});
+    else if (pieces <= 4) go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+    else if (pieces <= 8) go(integral_constant<int, 8>{}, integral_constant<int, 1>{});
     else if (pieces <= 16) go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
     else if (pieces <= 32) go(integral_constant<int, 32>{}, integral_constant<int, 1>{});
     else if (pieces <= 64) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});

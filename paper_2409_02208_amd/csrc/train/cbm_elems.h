@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "cbm.h"
 
@@ -59,6 +60,15 @@ struct Place {
     __device__ __forceinline__ bool any() const { return seen < V; }
     __device__ __forceinline__ bool counts(int j) const { return WHOLE ? seen <= 0 : j >= seen; }
 };
+
+// f(the largest power of two up to k) for a row of k < V values: one or two such pieces.
+template <int V, class F>
+inline void cbm_narrow_row(int k, F&& f) {
+    if constexpr (V > 1) {
+        if (k >= V / 2) f(std::integral_constant<int, V / 2>{});
+        else cbm_narrow_row<V / 2>(k, f);
+    }
+}
 
 // Sums and maxima over groups of LANES consecutive lanes, the same bits in all of them: inside a row of 16 lanes by DPP, across rows by swaps.
 template <int CTRL>

@@ -16,9 +16,10 @@ namespace {
 
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 constexpr int NORM_THREADS = 256;
-// Backward: rows that are read twice rather than joined by a second launch.  Microseconds a call, one launch or two: 1024 x 64 7.5 or 11.4, 1024 x 2048 10.5 or 13.7, 2048 x 64 7.6 or
-// 10.1, 2048 x 512 8.3 or 10.2, 2048 x 2048 19 or 16, 4096 x 64 10 or 10, 4096 x 300 19 or 10.
-bool few_rows(int64_t n, int k) { return n <= 1024 || (n <= 2048 && k <= 512); }
+// Backward: rows that are read twice rather than joined by a second launch.  Microseconds a call, one launch or two: 300 x 4096 fp32 6.9 or 11.0, 300 x 8000 14.4 or 15.1, 600 x 8000 24.1
+// or 18.0, 1000 x 2048 10.6 or 10.8, 1000 x 4096 17.7 or 14.5, 208 x 12064 bf16 14.4 or 17.0, 512 x 12064 25.0 or 21.4; few columns of many rows leave too little to do at once: 2048 x 64
+// fp32 7.6 or 10.1, 4096 x 64 10 or 10, 4096 x 300 19 or 10.
+bool few_rows(int64_t n, int k) { return (n <= 1024 && n * k <= 5 << 19) || (n <= 2048 && k <= 512); }
 constexpr int BACK_THREADS = 512, BACK_GROUPS = 512;  // backward: workgroups at most, each with partial sums of dg and db of its own
 
 // Sums of two values over a workgroup, in every thread.  `room` has a pair for every wave, twice: calls take turns (`turn`), so one barrier each is enough (who writes a
@@ -475,10 +476,13 @@ cbm_status cbm_launch_norm(int64_t n, int32_t k, int32_t type, const void* X_, i
         constexpr int V = 16 / (int)sizeof(T);
         const int64_t pieces = ((int64_t)k + V - 1) / V;
         const bool far = n * k * (int64_t)sizeof(T) >= CBM_FAR_BYTES;
-#define CBM_NORM(V_, LANES, R)                                                                                                                                              \
-    hipLaunchKernelGGL((cbm_norm_kernel<T, V_, LANES, R, WHOLE>), dim3((unsigned)at_most(n, (LANES > NORM_THREADS ? LANES : NORM_THREADS) / LANES, 256 * (LANES == 1024 ? 1 : LANES > NORM_THREADS ? 2 : 8))), \
-                       dim3(LANES > NORM_THREADS ? LANES : NORM_THREADS), 0, stream, n, k, X, ldx, gamma, beta, eps, Y, ldy, mean, rstd, far)
-        if (k < V) CBM_NORM(1, 8, 1);  // (V = 1: every place is whole)
+#define CBM_NORM(V_, LANES, R)                                                                                                                                                        \
+    cbm_norm_kernel<T, V_, LANES, R, WHOLE><<<(unsigned)at_most(n, (LANES > NORM_THREADS ? LANES : NORM_THREADS) / LANES, 256 * (LANES == 1024 ? 1 : LANES > NORM_THREADS ? 2 : 8)), \
+                                              LANES > NORM_THREADS ? LANES : NORM_THREADS, 0, stream>>>(n, k, X, ldx, gamma, beta, eps, Y, ldy, mean, rstd, far)
+        if (k < V) {
+            if constexpr (!WHOLE) cbm_narrow_row<V>(k, [&](auto v) { k == v() ? CBM_NORM(v(), 1, 1) : CBM_NORM(v(), 2, 1); });
+        } else if (pieces <= 1) CBM_NORM(V, 1, 1);
+        else if (pieces <= 2) CBM_NORM(V, 2, 1);
         else if (pieces <= 4) CBM_NORM(V, 4, 1);
         else if (pieces <= 8) CBM_NORM(V, 8, 1);
         else if (pieces <= 16) CBM_NORM(V, 16, 1);
@@ -513,7 +517,7 @@ cbm_status cbm_launch_norm_backward(int64_t n, int32_t k, int32_t type, const vo
             constexpr int V = 16 / (int)sizeof(T);
             const int64_t pieces = ((int64_t)k + V - 1) / V;
             const bool far = n * k * (int64_t)sizeof(T) >= CBM_FAR_BYTES;
-            const bool once = sums && few_rows(n, k) && pieces <= 1024;  // (dg and db in the same launch)
+            const bool once = sums && few_rows(n, k) && pieces <= (V == 4 ? 3 : 2) * 1024;  // (dg and db in the same launch)
             const unsigned alone = once ? (unsigned)(((int64_t)k + 15) / 16) : 0;
             if (once) parts = nullptr;
 #define CBM_BACK(V_, LANES, R, THREADS, GROUPS)                                                                                                                                           \
@@ -521,7 +525,10 @@ cbm_status cbm_launch_norm_backward(int64_t n, int32_t k, int32_t type, const vo
      cbm_norm_back_kernel<T, V_, LANES, R, THREADS, WHOLE><<<(unsigned)(dX || !once ? count : 0) + alone, THREADS, 0, stream>>>(n, k, dY, lddy, X, ldx, gamma, mean, rstd, dX, lddx, parts, \
                                                                                                                                dX || !once ? (int)count : 0, dgamma, dbeta, far),      \
      joined = once)
-            if (k < V) CBM_BACK(1, 8, 1, BACK_THREADS, BACK_GROUPS);
+            if (k < V) {
+                if constexpr (!WHOLE) cbm_narrow_row<V>(k, [&](auto v) { k == v() ? CBM_BACK(v(), 1, 1, BACK_THREADS, BACK_GROUPS) : CBM_BACK(v(), 2, 1, BACK_THREADS, BACK_GROUPS); });
+            } else if (pieces <= 1) CBM_BACK(V, 1, 1, BACK_THREADS, BACK_GROUPS);
+            else if (pieces <= 2) CBM_BACK(V, 2, 1, BACK_THREADS, BACK_GROUPS);
             else if (pieces <= 4) CBM_BACK(V, 4, 1, BACK_THREADS, BACK_GROUPS);
             else if (pieces <= 8) CBM_BACK(V, 8, 1, BACK_THREADS, BACK_GROUPS);
             else if (pieces <= 16) CBM_BACK(V, 16, 1, BACK_THREADS, BACK_GROUPS);

@@ -93,9 +93,10 @@ __device__ __forceinline__ void write_alternatives(const Scores& a, int64_t row,
     const bool none = m != m;  // of the row's scores is an alternative
     float* values = a.values + (row < a.n ? row : a.n - 1) * a.top;
     int32_t* columns = a.columns + (row < a.n ? row : a.n - 1) * a.top;
-    __shared__ uint64_t room[R == 1 ? 256 / LANES * MOST_TOP : 256 * R * V];  // what a row (a wave) has found
+    constexpr int MOST = LANES * V < MOST_TOP ? LANES * V : MOST_TOP;  // alternatives of a row of one piece a lane
+    __shared__ uint64_t room[R == 1 ? 256 / LANES * MOST : 256 * R * V];  // what a row (a wave) has found
     if constexpr (R == 1 && sizeof(T) == 2) {
-        uint64_t* kept = room + threadIdx.x / LANES * MOST_TOP;
+        uint64_t* kept = room + threadIdx.x / LANES * MOST;
         // A value's 16 bits in order, then its column from behind, make one whole number; every lane's in descending order, then `top` times the largest head.
         uint32_t key[V];
         const int at0 = Place<V, false>(lane, a.c).at;
@@ -111,7 +112,7 @@ __device__ __forceinline__ void write_alternatives(const Scores& a, int64_t row,
                 const uint32_t first = max(key[j], key[j + 1]), second = min(key[j], key[j + 1]);
                 key[j] = first, key[j + 1] = second;
             }
-        for (int r = 0; r < a.top; ++r) {
+        for (int r = 0; r < min(a.top, MOST); ++r) {
             const uint32_t best = lanes_max<LANES>(key[0]);
             const bool mine = key[0] == best;
             if (mine) kept[r] = best;
@@ -123,7 +124,7 @@ __device__ __forceinline__ void write_alternatives(const Scores& a, int64_t row,
         }
         __builtin_amdgcn_wave_barrier();
         for (int r = lane; r < a.top; r += LANES) {
-            const uint32_t best = (uint32_t)kept[r], o = best >> 16, u = o ^ (o & 0x8000u ? 0x8000u : 0xffffu);
+            const uint32_t best = r < MOST ? (uint32_t)kept[r] : 0u, o = best >> 16, u = o ^ (o & 0x8000u ? 0x8000u : 0xffffu);
             if (row >= a.n) break;
             values[r] = none ? NAN : best ? (float)__builtin_bit_cast(T, (uint16_t)u) - m - l : -INFINITY;
             columns[r] = best ? (int32_t)(0xffffu - (best & 0xffffu)) : -1;
@@ -132,7 +133,7 @@ __device__ __forceinline__ void write_alternatives(const Scores& a, int64_t row,
     } else if constexpr (R == 1) {
         // Every lane's values in descending order (neighbours change places only where the later one is larger, so the lower column stays first), then `top` times the
         // largest head: of equal ones the first lane's, whose columns are lower.
-        uint64_t* kept = room + threadIdx.x / LANES * MOST_TOP;
+        uint64_t* kept = room + threadIdx.x / LANES * MOST;
         uint32_t o[V], which[V];
         const int at0 = Place<V, false>(lane, a.c).at;
 #pragma unroll
@@ -151,7 +152,7 @@ __device__ __forceinline__ void write_alternatives(const Scores& a, int64_t row,
                 which[j] = change ? next : here, which[j + 1] = change ? here : next;
             }
         const uint64_t group = (LANES == 64 ? ~0ull : (1ull << LANES) - 1) << (threadIdx.x & 63 & ~(LANES - 1));
-        for (int r = 0; r < a.top; ++r) {
+        for (int r = 0; r < min(a.top, MOST); ++r) {
             const uint32_t best = lanes_max<LANES>(o[0]);
             const uint64_t have = __ballot(o[0] == best) & group;
             const bool mine = o[0] == best && __builtin_amdgcn_mbcnt_hi((uint32_t)(have >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)have, 0)) == 0;
@@ -165,7 +166,7 @@ __device__ __forceinline__ void write_alternatives(const Scores& a, int64_t row,
         }
         __builtin_amdgcn_wave_barrier();
         for (int r = lane; r < a.top; r += LANES) {
-            const uint32_t best = (uint32_t)(kept[r] >> 32);
+            const uint32_t best = r < MOST ? (uint32_t)(kept[r] >> 32) : 0u;
             if (row >= a.n) break;
             values[r] = none ? NAN : best ? in_order(best) - m - l : -INFINITY;
             columns[r] = best ? (int32_t)kept[r] : -1;
@@ -606,14 +607,21 @@ cbm_status cbm_launch_scores(int64_t n, int32_t c, int32_t type, const void* z, 
 #define CBM_SCORES(V_, LANES, R, SELECT) \
     cbm_scores_kernel<T, V_, LANES, R, SELECT><<<(unsigned)std::min<int64_t>((n + 256 / LANES - 1) / (256 / LANES), 1 << 23), 256, 0, stream>>>(a)
         constexpr int R = 16 / V;
-        if (c < V) top > 1 ? CBM_SCORES(1, 8, 1, true) : CBM_SCORES(1, 8, 1, false);
+        if (c < V) cbm_narrow_row<V>(c, [&](auto v) {
+                if (c == v()) top > 1 ? CBM_SCORES(v(), 1, 1, true) : CBM_SCORES(v(), 1, 1, false);
+                else top > 1 ? CBM_SCORES(v(), 2, 1, true) : CBM_SCORES(v(), 2, 1, false);
+            });
         else if (top > 1 && pieces <= 64) {
-            if (pieces <= 4) CBM_SCORES(V, 4, 1, true);
+            if (pieces <= 1) CBM_SCORES(V, 1, 1, true);
+            else if (pieces <= 2) CBM_SCORES(V, 2, 1, true);
+            else if (pieces <= 4) CBM_SCORES(V, 4, 1, true);
             else if (pieces <= 8) CBM_SCORES(V, 8, 1, true);
             else if (pieces <= 16) CBM_SCORES(V, 16, 1, true);
             else if (pieces <= 32) CBM_SCORES(V, 32, 1, true);
             else CBM_SCORES(V, 64, 1, true);
         } else if (top > 1 && c <= SHORT_ROW) CBM_SCORES(V, 64, SHORT_ROW / 64 / V, true);
+        else if (pieces <= 1) CBM_SCORES(V, 1, 1, false);
+        else if (pieces <= 2) CBM_SCORES(V, 2, 1, false);
         else if (pieces <= 4) CBM_SCORES(V, 4, 1, false);
         else if (pieces <= 4 * R) CBM_SCORES(V, 4, R, false);
         else if (pieces <= 8 * R) CBM_SCORES(V, 8, R, false);
@@ -651,7 +659,13 @@ cbm_status cbm_launch_scores_backward(int64_t n, int32_t c, int32_t type, const 
         cbm_scores_back_kernel<T, V_, LANES><<<dim3((unsigned)std::min<int64_t>((n + 256 / LANES - 1) / (256 / LANES), 1 << 23),                                             \
                                                     (unsigned)((pieces + LANES * turns - 1) / (LANES * turns))), 256, 0, stream>>>(a, turns, far);                              \
     }
-        if (c < V) CBM_BACK(1, 8)
+        if (c < V) cbm_narrow_row<V>(c, [&](auto v) {
+                const int64_t pieces = c == v() ? 1 : 2;
+                if (pieces == 1) CBM_BACK(v(), 1)
+                else CBM_BACK(v(), 2)
+            });
+        else if (pieces <= 1) CBM_BACK(V, 1)
+        else if (pieces <= 2) CBM_BACK(V, 2)
         else if (pieces <= 4) CBM_BACK(V, 4)
         else if (pieces <= 8) CBM_BACK(V, 8)
         else if (pieces <= 16) CBM_BACK(V, 16)
