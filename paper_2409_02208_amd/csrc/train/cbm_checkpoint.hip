@@ -41,20 +41,26 @@ __device__ __forceinline__ void load_row_bytes(int (&q)[V], const int8_t* row, c
     }
 }
 
-// Save.  LANES lanes a row (and a share of its columns: blockIdx.y), R times V columns a lane.  A block of 32 columns is 32 / V lanes, which find its largest value by DPP; nothing
+// Save.  LANES lanes a row (and a share of its columns: blockIdx.y), V columns a lane, of R rows; of R places along the row where a wave has it (R = 2).  A block of 32 columns is 32 / V lanes, which find its largest value by DPP; nothing
 // else is shared.  Bound by memory: 19717 x 500 fp32 11 to 13 us for 49.6 MB, of which the caches hold some (4 TB/s; waves waiting for 64 % of their cycles).
 template <class T, int LANES, int R>
 __global__ __launch_bounds__(256) void cbm_checkpoint_save_kernel(int64_t n, int k, const T* __restrict__ X, int64_t ldx, int8_t* __restrict__ Q, int64_t ldq,
                                                                   uint8_t* __restrict__ E, int64_t lde) {
     constexpr int V = 16 / (int)sizeof(T), PER_BLOCK = BLOCK / V;
-    const int lane = threadIdx.x % LANES, first = blockIdx.y * R * LANES + lane, blocks = (k + BLOCK - 1) / BLOCK;
-    for (int64_t row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES; row < n; row += (int64_t)gridDim.x * (256 / LANES)) {
+    constexpr int ROWS = 256 / LANES, ACROSS = LANES == 64 ? R : 1, DOWN = LANES == 64 ? 1 : R;
+    const int lane = threadIdx.x % LANES, first = blockIdx.y * ACROSS * LANES + lane, blocks = (k + BLOCK - 1) / BLOCK;
+    for (int64_t row0 = (int64_t)blockIdx.x * (DOWN * ROWS) + threadIdx.x / LANES; row0 < n; row0 += (int64_t)gridDim.x * (DOWN * ROWS)) {
         float x[R][V];
 #pragma unroll
-        for (int i = 0; i < R; ++i) load_row_piece<V>(x[i], X + row * ldx, Place<V, false>(first + i * LANES, k), k);
+        for (int i = 0; i < R; ++i) {
+            const int64_t row = min(row0 + i % DOWN * ROWS, n - 1);
+            load_row_piece<V>(x[i], X + row * ldx, Place<V, false>(first + i % ACROSS * LANES, k), k);
+        }
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            int c = first + i * LANES;
+            const int64_t row = row0 + i % DOWN * ROWS;
+            if (DOWN > 1 && row >= n) break;
+            int c = first + i % ACROSS * LANES;
             asm volatile("" : "+v"(c));  // (every row's comparisons anew: kept from row to row they are more than the scalar registers hold)
             const Place<V, false> p(c, k);
             // the largest size by its bits, which order sizes, infinity and NaN as they should
@@ -101,21 +107,25 @@ template <class T, int LANES, int R, bool GATED>
 __global__ __launch_bounds__(256) void cbm_checkpoint_load_kernel(int64_t n, int k, const int8_t* __restrict__ Q, int64_t ldq, const uint8_t* __restrict__ E, int64_t lde, const T* dY,
                                                                   int64_t lddy, T* out, int64_t ldo, bool far) {
     constexpr int V = 16 / (int)sizeof(T);
-    const int lane = threadIdx.x % LANES, first = blockIdx.y * R * LANES + lane, blocks = (k + BLOCK - 1) / BLOCK;
-    for (int64_t row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES; row < n; row += (int64_t)gridDim.x * (256 / LANES)) {
+    constexpr int ROWS = 256 / LANES, ACROSS = LANES == 64 ? R : 1, DOWN = LANES == 64 ? 1 : R;
+    const int lane = threadIdx.x % LANES, first = blockIdx.y * ACROSS * LANES + lane, blocks = (k + BLOCK - 1) / BLOCK;
+    for (int64_t row0 = (int64_t)blockIdx.x * (DOWN * ROWS) + threadIdx.x / LANES; row0 < n; row0 += (int64_t)gridDim.x * (DOWN * ROWS)) {
         int q[R][V];
         float x[R][V];
         uint32_t code[R];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const Place<V, false> p(first + i * LANES, k);
+            const int64_t row = min(row0 + i % DOWN * ROWS, n - 1);
+            const Place<V, false> p(first + i % ACROSS * LANES, k);
             load_row_bytes<V>(q[i], Q + row * ldq, p, k);
             if constexpr (GATED) load_row_piece<V>(x[i], dY + row * lddy, p, k);
-            code[i] = E[row * lde + min((first + i * LANES) * V / BLOCK, blocks - 1)];
+            code[i] = E[row * lde + min((first + i % ACROSS * LANES) * V / BLOCK, blocks - 1)];
         }
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            int c = first + i * LANES;
+            const int64_t row = row0 + i % DOWN * ROWS;
+            if (DOWN > 1 && row >= n) break;
+            int c = first + i % ACROSS * LANES;
             asm volatile("" : "+v"(c));  // (as above)
             const Place<V, false> p(c, k);
 #pragma unroll
@@ -388,21 +398,29 @@ cbm_status launched(const char* what) {
     return CBM_ERR_HIP;
 }
 
-// f(lanes a row, pieces a lane, workgroups) for rows of `pieces` pieces
-template <class F>
+// f(lanes a row, pieces a lane, workgroups) for rows of `pieces` pieces.  Four rows a lane, so that its loads are under way together, in fp32 where a row has enough
+// lanes: 2097152 x 64 saved and restored 245 us for 275 with one, 300000 x 100 61 for 69; not in 16 bits, whose pieces are twice the work (235868 x 128 44 for 40), nor where rows are
+// narrow (1000000 x 16 gated 28.2 for 26.6), nor for few workgroups.
+template <class T, class F>
 void along_rows(int64_t n, int64_t pieces, F&& f) {
     auto go = [&](auto lanes, auto each) {
-        constexpr int ROWS = 256 / decltype(lanes)::value, AT_ONCE = decltype(lanes)::value * decltype(each)::value;
+        constexpr int LANES = decltype(lanes)::value, R = decltype(each)::value, ROWS = 256 / LANES * (LANES == 64 ? 1 : R), AT_ONCE = LANES * (LANES == 64 ? R : 1);
         f(lanes, each, dim3((unsigned)std::min<int64_t>((n + ROWS - 1) / ROWS, 1 << 23), (unsigned)((pieces + AT_ONCE - 1) / AT_ONCE)));
     };
     using std::integral_constant;
-    if (pieces <= 1) go(integral_constant<int, 1>{}, integral_constant<int, 1>{});
-    else if (pieces <= 2) go(integral_constant<int, 2>{}, integral_constant<int, 1>{});
-    else if (pieces <= 4) go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
-    else if (pieces <= 8) go(integral_constant<int, 8>{}, integral_constant<int, 1>{});
-    else if (pieces <= 16) go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
-    else if (pieces <= 32) go(integral_constant<int, 32>{}, integral_constant<int, 1>{});
-    else if (pieces <= 64) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    constexpr integral_constant<int, 1> one;
+    auto some = [&](auto lanes) {
+        if constexpr (sizeof(T) == 4)
+            if (n * pieces >= 1 << 20) return go(lanes, integral_constant<int, 4>{});
+        go(lanes, one);
+    };
+    if (pieces <= 1) go(one, one);
+    else if (pieces <= 2) go(integral_constant<int, 2>{}, one);
+    else if (pieces <= 4) go(integral_constant<int, 4>{}, one);
+    else if (pieces <= 8) go(integral_constant<int, 8>{}, one);
+    else if (pieces <= 16) some(integral_constant<int, 16>{});
+    else if (pieces <= 32) some(integral_constant<int, 32>{});
+    else if (pieces <= 64) go(integral_constant<int, 64>{}, one);
     else go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
 }
 
@@ -431,7 +449,7 @@ cbm_status cbm_launch_checkpoint_save(int64_t n, int32_t k, int32_t type, const 
     cbm_with_type(type, [&](auto t) {
         using T = decltype(t);
         constexpr int V = 16 / (int)sizeof(T);
-        along_rows(n, ((int64_t)k + V - 1) / V, [&](auto lanes, auto each, dim3 grid) {
+        along_rows<T>(n, ((int64_t)k + V - 1) / V, [&](auto lanes, auto each, dim3 grid) {
             cbm_checkpoint_save_kernel<T, decltype(lanes)::value, decltype(each)::value><<<grid, 256, 0, (hipStream_t)stream>>>(n, k, (const T*)X, ldx, Q, ldq, E, lde);
         });
     });
@@ -444,7 +462,7 @@ cbm_status cbm_launch_checkpoint_load(int64_t n, int32_t k, const int8_t* Q, int
     cbm_with_type(type, [&](auto t) {
         using T = decltype(t);
         constexpr int V = 16 / (int)sizeof(T);
-        along_rows(n, ((int64_t)k + V - 1) / V, [&](auto lanes, auto each, dim3 grid) {
+        along_rows<T>(n, ((int64_t)k + V - 1) / V, [&](auto lanes, auto each, dim3 grid) {
             constexpr int LANES = decltype(lanes)::value, R = decltype(each)::value;
             const bool far = n * k * (int64_t)sizeof(T) >= CBM_FAR_BYTES;
             if (dY) cbm_checkpoint_load_kernel<T, LANES, R, true><<<grid, 256, 0, (hipStream_t)stream>>>(n, k, Q, ldq, E, lde, (const T*)dY, lddy, (T*)out, ldo, far);
