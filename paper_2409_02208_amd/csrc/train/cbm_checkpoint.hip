@@ -150,7 +150,6 @@ __global__ __launch_bounds__(256) void cbm_checkpoint_load_kernel(int64_t n, int
 // The next step's loads are under way while a step is multiplied; two steps ahead cost registers and gained nothing (279 us, 292).  2097152 x 128, 128 columns of fp32: 283 us for
 // 1.35 GB (4.8 TB/s) and 206 GFLOP of parts (730 TFLOP/s, the matrix cores busy for 40 % of the cycles): bound by memory, with the vector instructions
 // that split dY and widen Q next to it.  132534 x 100, 47 columns: 16 us, of which 5.5 are there whatever the rows (the launch, first loads, sums in LDS).
-constexpr int FEW_PARTS = 16;
 constexpr int GRAD_WAVES = 8, GRAD_ROWS = 16;
 int grad_mt(int32_t k) { return k <= 32 ? 1 : k <= 64 ? 2 : 4; }
 int grad_nt(int32_t c) { return c <= 32 ? 1 : 2; }
@@ -358,36 +357,29 @@ __global__ __launch_bounds__(64 * GRAD_WAVES, 2 * grad_groups(MT, NT)) void cbm_
     }
 }
 
-// dW from `count` partial sums, in order: 32 values a workgroup, the partial sums shared by its 32 groups of lanes.  Bound by the latency of a launch and of 16 loads a lane: 256 of
-// 100 x 47 4 to 5 us.
+// dW from `count` partial sums, in order: 1024 / SLICES values a workgroup, the partial sums shared by its SLICES groups of lanes.  Bound by the latency of a launch and of the loads of
+// a lane, so few partial sums have few slices and a lane up to 16 loads: 256 of 100 x 47 (32 slices) 4 to 5 us, 24 of 572 x 94 (4) 4.7 (8.3 with 32), 4 of 1024 x 512 (1) 5.
+template <int SLICES>
 __global__ __launch_bounds__(1024) void cbm_checkpoint_join_kernel(int count, int64_t size, int c, const float* __restrict__ parts, float* __restrict__ dW, int64_t lddw) {
-    __shared__ float room[32][33];
-    const int slice = threadIdx.x / 32;
-    for (int64_t i0 = (int64_t)blockIdx.x * 32; i0 < size; i0 += (int64_t)gridDim.x * 32) {
-        const int64_t i = i0 + (threadIdx.x & 31);
+    constexpr int VALUES = 1024 / SLICES;
+    __shared__ float room[SLICES > 1 ? SLICES : 1][VALUES + 1];
+    const int slice = threadIdx.x / VALUES, mine = threadIdx.x % VALUES;
+    for (int64_t i0 = (int64_t)blockIdx.x * VALUES; i0 < size; i0 += (int64_t)gridDim.x * VALUES) {
+        const int64_t i = i0 + mine;
         float s = 0.0f;
         if (i < size)
 #pragma unroll 16
-            for (int p = slice; p < count; p += 32) s += parts[p * size + i];
-        room[slice][threadIdx.x & 31] = s;
-        __syncthreads();
-        if (slice == 0 && i < size) {
+            for (int p = slice; p < count; p += SLICES) s += parts[p * size + i];
+        if constexpr (SLICES > 1) {
+            room[slice][mine] = s;
+            __syncthreads();
             s = 0.0f;
+            if (slice == 0)
 #pragma unroll
-            for (int p = 0; p < 32; ++p) s += room[p][threadIdx.x];
-            dW[i / c * lddw + i % c] = s;
+                for (int p = 0; p < SLICES; ++p) s += room[p][mine];
         }
-        __syncthreads();
-    }
-}
-
-// The same with few partial sums: a value a thread (20000 x 1024, 512 columns: 4 partial sums of 2 MB).
-__global__ __launch_bounds__(256) void cbm_checkpoint_join_few_kernel(int count, int64_t size, int c, const float* __restrict__ parts, float* __restrict__ dW, int64_t lddw) {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
-        float s = 0.0f;
-#pragma unroll 8
-        for (int p = 0; p < count; ++p) s += parts[p * size + i];
-        dW[i / c * lddw + i % c] = s;
+        if (slice == 0 && i < size) dW[i / c * lddw + i % c] = s;
+        if constexpr (SLICES > 1) __syncthreads();
     }
 }
 
@@ -496,7 +488,12 @@ cbm_status cbm_launch_checkpoint_grad(int64_t n, int32_t k, int32_t c, const int
             auto narrow = [&](auto m) { nt == 1 ? go(m, integral_constant<int, 1>{}) : go(m, integral_constant<int, 2>{}); };
             mt == 1 ? narrow(integral_constant<int, 1>{}) : mt == 2 ? narrow(integral_constant<int, 2>{}) : narrow(integral_constant<int, 4>{});
         });
-    if (splits != 1 && splits <= FEW_PARTS) cbm_checkpoint_join_few_kernel<<<(unsigned)std::min<int64_t>((size + 255) / 256, 1 << 22), 256, 0, stream>>>(splits, size, c, parts, dW, lddw);
-    else if (splits != 1) cbm_checkpoint_join_kernel<<<(unsigned)std::min<int64_t>((size + 31) / 32, 1 << 20), 1024, 0, stream>>>(splits, size, c, parts, dW, lddw);
+#define CBM_JOIN(SLICES) \
+    cbm_checkpoint_join_kernel<SLICES><<<(unsigned)std::min<int64_t>((size + 1024 / SLICES - 1) / (1024 / SLICES), 1 << 20), 1024, 0, stream>>>(splits, size, c, parts, dW, lddw)
+    if (splits == 1) {
+    } else if (splits <= 16) CBM_JOIN(1);
+    else if (splits <= 96) CBM_JOIN(4);
+    else CBM_JOIN(32);
+#undef CBM_JOIN
     return launched("checkpoint gradient launch");
 }
