@@ -73,10 +73,10 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
     return lanes_all<LANES>(v, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
 
-// The largest whole number that at least `top` lanes of the wave have or exceed, bit by bit; the smallest that is an alternative where fewer lanes have one.
+// The largest whole number of 16 bits and zeros that at least `top` lanes of the wave have or exceed, bit by bit; the smallest that is an alternative where fewer lanes have one.
 __device__ __forceinline__ uint32_t bound_of_heads(uint32_t head, int top) {
     uint32_t bound = 0;
-    for (int bit = 31; bit >= 0; --bit) {
+    for (int bit = 31; bit >= 16; --bit) {
         const int have = __popcll(__ballot(head >= (bound | 1u << bit)));
         if (have >= top) bound |= 1u << bit;
         if (have == top) break;  // (they all exceed what the bits below could add, or the bound is a little low, which costs nothing)
@@ -237,12 +237,15 @@ __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
         }
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const Place<V, false> p(i * LANES + lane, a.c);
+            int piece = i * LANES + lane;
+            if constexpr (R * V > 16) asm volatile("" : "+v"(piece));  // (every row's comparisons anew, a piece's at a time: kept they are more than the scalar registers hold)
+            const Place<V, false> p(piece, a.c);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 x[i][j] = p.counts(j) ? x[i][j] : -INFINITY;
                 m = fmaxf(m, x[i][j]);
             }
+            if constexpr (R * V > 16) __builtin_amdgcn_sched_barrier(0);
         }
         const float own = m;  // of the lane's columns
         m = lanes_max<LANES>(m);
@@ -266,6 +269,7 @@ __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
 #pragma unroll
             for (int i = R - 1; i >= 0; --i) {
                 const Place<V, false> p(i * LANES + lane, a.c);
+                if constexpr (R * V > 16) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int j = V - 1; j >= 0; --j) column = x[i][j] == m ? ~(uint32_t)(p.at + j) : column;
             }
@@ -628,6 +632,8 @@ cbm_status cbm_launch_scores(int64_t n, int32_t c, int32_t type, const void* z, 
         else if (pieces <= 16 * R) CBM_SCORES(V, 16, R, false);
         else if (pieces <= 32 * R) CBM_SCORES(V, 32, R, false);
         else if (c <= SHORT_ROW) CBM_SCORES(V, 64, R, false);
+        else if (top <= 1 && c <= 2 * SHORT_ROW) CBM_SCORES(V, 64, 2 * R, false);
+        else if (top <= 1 && c <= 4 * SHORT_ROW) CBM_SCORES(V, 64, 4 * R, false);
 #undef CBM_SCORES
         else {
             const int splits = c <= ALONE ? 1 : cbm_scores_splits(n, c);
