@@ -285,9 +285,7 @@ __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
     }
 }
 
-// The `top` largest keys of a workgroup of LONG_THREADS.  `head`: a key of each of 64 parts of the collection that is no larger than the largest there, so that the top-th
-// largest head bounds the answer from below (VALUES: only its value does); keys of at least that are collected, with those of `list`, and ranked by counting.
-// VALUES: gives up, and returns false, where there is no room for them; otherwise the caller's parts are so small that there is.
+// What a workgroup of LONG_THREADS finds its alternatives with.
 template <int CAP>
 struct Select {
     uint64_t head[64], list[MOST_TOP], found[CAP];
@@ -295,46 +293,44 @@ struct Select {
     int count, lanes;
     uint16_t lane[LONG_THREADS];
 };
-template <bool VALUES, int CAP, class F>
-__device__ __forceinline__ bool select_keys(Select<CAP>& s, int top, F&& each) {
-    __syncthreads();
-    if (threadIdx.x < 64) {
-        const uint64_t mine = s.head[threadIdx.x];
-        if constexpr (VALUES) {
-            const uint32_t bound = bound_of_heads((uint32_t)(mine >> 32), top);
-            if (threadIdx.x == 0) s.bound = (uint64_t)bound << 32;
-        } else {
-            const int there = __popcll(__ballot(mine != 0));
-            int rank = 0;
-#pragma unroll 2
-            for (int i = 0; i < 64; ++i) rank += lane_value(mine, i) > mine;
-            if (there < top ? threadIdx.x == 0 : mine && rank == top - 1) s.bound = there < top ? 1 : mine;
-        }
-        if (threadIdx.x == 0) s.count = s.lanes = 0;
-    }
-    __syncthreads();
-    const uint64_t bound = s.bound;
-    auto take = [&](uint64_t key) {
-        if (key < bound) return;
-        const int at = atomicAdd(&s.count, 1);
-        if (!VALUES || at < CAP) s.found[at] = key;
-    };
-    each(take);
-    if (!VALUES && (int)threadIdx.x < top) take(s.list[threadIdx.x]);
-    __syncthreads();
-    const int count = s.count;
-    if (VALUES && count > CAP) return false;
-    if ((int)threadIdx.x < top) s.list[threadIdx.x] = 0;
-    __syncthreads();
+// The `top` largest of found[0 .. count) to the list, by counting what is larger (keys differ, so do ranks).
+template <int CAP>
+__device__ __forceinline__ void rank_found(Select<CAP>& s, int top, int count) {
     for (int i = threadIdx.x; i < count; i += LONG_THREADS) {
         const uint64_t mine = s.found[i];
         int rank = 0;
 #pragma unroll 8
         for (int j = 0; j < count; ++j) rank += s.found[j] > mine;
-        if (rank < top) s.list[rank] = mine;  // (keys differ, so do ranks)
+        if (rank < top) s.list[rank] = mine;
     }
     __syncthreads();
-    return true;
+}
+// The `top` largest of the list's keys and of those that each(take) takes.  `head`: the largest of each of 64 parts of these, so that the top-th largest head bounds the answer
+// from below; the parts are so small that there is room for what is as large.
+template <int CAP, class F>
+__device__ __forceinline__ void select_keys(Select<CAP>& s, int top, F&& each) {
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        const uint64_t mine = s.head[threadIdx.x];
+        const int there = __popcll(__ballot(mine != 0));
+        int rank = 0;
+#pragma unroll 2
+        for (int i = 0; i < 64; ++i) rank += lane_value(mine, i) > mine;
+        if (there < top ? threadIdx.x == 0 : mine && rank == top - 1) s.bound = there < top ? 1 : mine;
+        if (threadIdx.x == 0) s.count = 0;
+    }
+    __syncthreads();
+    const uint64_t bound = s.bound;
+    auto take = [&](uint64_t key) {
+        if (key >= bound) s.found[atomicAdd(&s.count, 1)] = key;
+    };
+    each(take);
+    if ((int)threadIdx.x < top) take(s.list[threadIdx.x]);
+    __syncthreads();
+    const int count = s.count;
+    if ((int)threadIdx.x < top) s.list[threadIdx.x] = 0;
+    __syncthreads();
+    rank_found(s, top, count);
 }
 
 __device__ __forceinline__ void write_top(const Scores& a, int64_t row, const uint64_t* list, float m, float l) {
@@ -426,6 +422,7 @@ __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_long_kernel(Scores a,
             four = fmaxf(four, lane_other<2>(four));
             if (threadIdx.x % 4 == 0) sel.head[threadIdx.x / 4] = key_of(ordered(four), 0);
             if ((int)threadIdx.x < MOST_TOP) sel.list[threadIdx.x] = 0;
+            if (threadIdx.x == 0) sel.count = sel.lanes = 0;
         }
         __syncthreads();
         const int w = min((int)threadIdx.x & 63, LONG_THREADS / 64 - 1);
@@ -445,13 +442,22 @@ __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_long_kernel(Scores a,
                 for (int j = 0; j < V; ++j)
                     if (p.counts(j)) f(x[j], p.at + j);
             };
-            const bool done = select_keys<true>(sel, a.top, [&](auto&& take) {  // (the lanes' pieces are shared out, so that they are loaded at once)
-                if (ordered(best) >= (uint32_t)(sel.bound >> 32)) sel.lane[atomicAdd(&sel.lanes, 1)] = (uint16_t)threadIdx.x;
-                __syncthreads();
-                const int lanes = sel.lanes, turns = (end - begin + LONG_THREADS * V - 1) / (LONG_THREADS * V);
-                for (int i = threadIdx.x; i < lanes * turns; i += LONG_THREADS)
-                    scan(begin / V + i / lanes * LONG_THREADS + sel.lane[i % lanes], [&](float v, int column) { take(key_of(ordered(v), column)); });
-            });
+            // what is as large as the bound: the row's maximum where one alternative is asked for
+            const uint32_t bound = a.top == 1 ? max(ordered(m), 1u) : bound_of_heads((uint32_t)(sel.head[threadIdx.x & 63] >> 32), a.top);
+            auto take = [&](float v, int column) {
+                if (ordered(v) < bound) return;
+                const int at = atomicAdd(&sel.count, 1);
+                if (at < CAP) sel.found[at] = key_of(ordered(v), column);
+            };
+            if (ordered(best) >= bound) sel.lane[atomicAdd(&sel.lanes, 1)] = (uint16_t)threadIdx.x;
+            __syncthreads();
+            const int lanes = sel.lanes, turns = (end - begin + LONG_THREADS * V - 1) / (LONG_THREADS * V);
+            for (int i = threadIdx.x; i < lanes * turns; i += LONG_THREADS)  // (the lanes' pieces are shared out, so that they are loaded at once)
+                scan(begin / V + i / lanes * LONG_THREADS + sel.lane[i % lanes], take);
+            __syncthreads();
+            const int count = sel.count;
+            const bool done = count <= CAP;
+            if (done) rank_found(sel, a.top, count);
             if (!done) {
                 float least = -INFINITY;  // the last of the alternatives so far; a later column has to exceed it
                 for (int turn = begin / V; turn * V < end; turn += LONG_THREADS) {
@@ -468,7 +474,7 @@ __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_long_kernel(Scores a,
                         four = other > four ? other : four;
                     }
                     if (threadIdx.x % 4 == 0) sel.head[threadIdx.x / 4] = four;
-                    select_keys<false>(sel, a.top, [&](auto&& take) {
+                    select_keys(sel, a.top, [&](auto&& take) {
                         if (mine >= sel.bound) scan(turn + threadIdx.x, [&](float v, int column) { take(v > least ? key_of(ordered(v), column) : 0); });  // (0 < 1 <= bound)
                     });
                     const uint64_t last = sel.list[a.top - 1];
@@ -522,7 +528,7 @@ __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_join_kernel(Scores a,
         __syncthreads();
         if ((int)threadIdx.x < 64) sel.head[lane] = keys[0];
         if ((int)threadIdx.x < MOST_TOP) sel.list[threadIdx.x] = 0;
-        select_keys<false>(sel, a.top, [&](auto&& take) {
+        select_keys(sel, a.top, [&](auto&& take) {
 #pragma unroll
             for (int i = 0; i < EACH; ++i)
                 if (keys[i]) take(keys[i]);
