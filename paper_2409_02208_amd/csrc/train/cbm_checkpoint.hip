@@ -221,8 +221,8 @@ __global__ __launch_bounds__(64 * GRAD_WAVES, 2 * grad_groups(MT, NT)) void cbm_
                                                                                                     int64_t part, bool near) {
     constexpr int PARTS = std::is_same<T, float>::value ? 3 : std::is_same<T, _Float16>::value ? 2 : 1;  // 24, 11 and 8 bits, eight a part
     __shared__ floatx2 room[GRAD_WAVES * NT * 8 * 64];
-    // consecutive workgroups run on different XCDs: the tiles of one share of the rows are eight apart, on one XCD, where there are so many shares
-    const int b = blockIdx.x, beside = min(CBM_XCD, splits), split = b / (beside * tiles) * beside + b % beside, tile = b / beside % tiles;
+    // workgroup b runs on XCD b mod 8: what an XCD has is neighbouring shares of the rows, all tiles of each as far as that goes
+    const int per = gridDim.x / CBM_XCD, at = blockIdx.x % CBM_XCD * per + blockIdx.x / CBM_XCD, split = at / tiles, tile = at % tiles;
     if (split >= splits) return;
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int k0 = tile / tiles_c * (32 * MT) + MT * (lane & 31), c0 = tile % tiles_c * (32 * NT) + NT * (lane & 31);
@@ -418,21 +418,19 @@ void along_rows(int64_t n, int64_t pieces, F&& f) {
 
 }  // namespace
 
-// A compute unit holds one workgroup of the gradient at a time (two with narrow tiles), and workgroup b runs on XCD b mod 8, so what s shares take is what the fullest XCD's 32 units take:
-// rounds / s of what one workgroup takes for all rows (more shares cost more partial sums).  A share has 64 rows at least.
-// (300000 x 300, 100 columns, six tiles: 200 us with 42 shares, of which two XCDs had 36 workgroups, 120 with 40.)
+// A compute unit holds one workgroup of the gradient at a time (two with narrow tiles), so s shares take ceil(s tiles / units) rounds, each 1 / s of what one workgroup takes for all
+// rows, and more shares cost more partial sums: the most shares for a number of rounds, from few rounds to many, the first that another does not beat by a tenth.  A share has 64 rows at
+// least.  (300000 x 300, 100 columns, six tiles: 200 us with 42 shares of which two XCDs had 36 workgroups for their 32 units, 120 with 40, 116 with 42 and 32
+// workgroups an XCD; 13613 x 323, 359 columns, 18 tiles: 41 us with 40 shares in three rounds, 26 with 14 in one.)
 int64_t cbm_grad_splits(int64_t n, int32_t k, int32_t c) {
     const int mt = grad_mt(k), nt = grad_nt(c);
-    const int64_t UNITS = 32 * grad_groups(mt, nt), tiles = ((int64_t)k + 32 * mt - 1) / (32 * mt) * (((int64_t)c + 32 * nt - 1) / (32 * nt));
-    const int64_t most = std::max<int64_t>(1, std::min<int64_t>((4 * CBM_XCD * UNITS + tiles - 1) / tiles, (n + 4 * GRAD_ROWS - 1) / (4 * GRAD_ROWS)));
-    auto rounds = [&](int64_t s) {
-        const int64_t fullest = s < CBM_XCD ? (s * tiles + CBM_XCD - 1) / CBM_XCD : (s + CBM_XCD - 1) / CBM_XCD * tiles;  // (the kernel says how shares are dealt out to XCDs)
-        return (fullest + UNITS - 1) / UNITS;
-    };
-    // the most shares for each number of rounds, from few rounds to many: the first that another does not beat by a tenth
-    int64_t best = 1;
-    for (int64_t s = 1; s <= most; ++s)
-        if (rounds(s) == rounds(best) ? s > best : (double)rounds(s) * best * 1.1 < (double)rounds(best) * s) best = s;
+    const int64_t units = 32 * CBM_XCD * grad_groups(mt, nt), tiles = ((int64_t)k + 32 * mt - 1) / (32 * mt) * (((int64_t)c + 32 * nt - 1) / (32 * nt));
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(4 * units / tiles, (n + 4 * GRAD_ROWS - 1) / (4 * GRAD_ROWS)));
+    int64_t rounds = (tiles + units - 1) / units, best = std::min(most, rounds * units / tiles);
+    for (int64_t r = rounds + 1; r <= 4; ++r) {
+        const int64_t s = std::min(most, r * units / tiles);
+        if ((double)r * (double)best * 1.1 < (double)rounds * (double)s) rounds = r, best = s;
+    }
     return best;
 }
 
@@ -473,8 +471,7 @@ cbm_status cbm_launch_checkpoint_grad(int64_t n, int32_t k, int32_t c, const int
         cbm_with_type(type, [&](auto t) {
             using T = decltype(t);
             const int mt = grad_mt(k), nt = grad_nt(c), tiles_c = (int)(((int64_t)c + 32 * nt - 1) / (32 * nt)), tiles = (int)(((int64_t)k + 32 * mt - 1) / (32 * mt)) * tiles_c;
-            const int beside = std::min(CBM_XCD, splits);
-            const unsigned grid = (unsigned)((splits + beside - 1) / beside * beside * tiles);
+            const unsigned grid = (unsigned)(((int64_t)splits * tiles + CBM_XCD - 1) / CBM_XCD * CBM_XCD);
             const GradArgs<T> a{n, k, c, Q, ldq, E, lde, (const T*)dY, lddy};
             float* to = splits == 1 ? dW : parts;
             const int64_t ldp = splits == 1 ? lddw : c;
