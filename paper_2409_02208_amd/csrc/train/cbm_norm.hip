@@ -17,9 +17,9 @@ namespace {
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 constexpr int NORM_THREADS = 256;
 // Backward: rows that are read twice rather than joined by a second launch.  Microseconds a call, one launch or two: 300 x 4096 fp32 6.9 or 11.0, 300 x 8000 14.4 or 15.1, 600 x 8000 24.1
-// or 18.0, 1000 x 2048 10.6 or 10.8, 1000 x 4096 17.7 or 14.5, 208 x 12064 bf16 14.4 or 17.0, 512 x 12064 25.0 or 21.4; few columns of many rows leave too little to do at once: 2048 x 64
-// fp32 7.6 or 10.1, 4096 x 64 10 or 10, 4096 x 300 19 or 10.
-bool few_rows(int64_t n, int k) { return (n <= 1024 && n * k <= 5 << 19) || (n <= 2048 && k <= 512); }
+// or 18.0, 1024 x 512 6.4 or 8.2, 1024 x 1000 8.0 or 9.4, 1000 x 4096 17.7 or 14.5, 208 x 12064 bf16 14.4 or 17.0, 512 x 12064 25.0 or 21.4, 1024 x 2500 10.5 or 12.6; more rows are a longer
+// walk for a lane: 2048 x 256 fp32 6.8 or 7.8, 2048 x 512 12.3 or 8.0, 4096 x 64 10 or 10.
+bool few_rows(int64_t n, int k) { return (n <= 1024 && n * k <= 5 << 19) || (n <= 2048 && k <= 256); }
 constexpr int BACK_THREADS = 512, BACK_GROUPS = 512;  // backward: workgroups at most, each with partial sums of dg and db of its own
 
 // Sums of two values over a workgroup, in every thread.  `room` has a pair for every wave, twice: calls take turns (`turn`), so one barrier each is enough (who writes a
