@@ -94,8 +94,8 @@ __device__ __forceinline__ void write_alternatives(const Scores& a, int64_t row,
     float* values = a.values + (row < a.n ? row : a.n - 1) * a.top;
     int32_t* columns = a.columns + (row < a.n ? row : a.n - 1) * a.top;
     constexpr int MOST = LANES * V < MOST_TOP ? LANES * V : MOST_TOP;  // alternatives of a row of one piece a lane
-    __shared__ uint64_t room[R == 1 ? 256 / LANES * MOST : 256 * R * V];  // what a row (a wave) has found
-    if constexpr (R == 1 && sizeof(T) == 2) {
+    __shared__ uint64_t room[LANES < 64 ? 256 / LANES * MOST : 256 * R * V];  // what a row (a wave) has found
+    if constexpr (LANES < 64 && sizeof(T) == 2) {
         uint64_t* kept = room + threadIdx.x / LANES * MOST;
         // A value's 16 bits in order, then its column from behind, make one whole number; every lane's in descending order, then `top` times the largest head.
         uint32_t key[V];
@@ -130,7 +130,7 @@ __device__ __forceinline__ void write_alternatives(const Scores& a, int64_t row,
             columns[r] = best ? (int32_t)(0xffffu - (best & 0xffffu)) : -1;
         }
         __builtin_amdgcn_wave_barrier();  // (kept is the next row's)
-    } else if constexpr (R == 1) {
+    } else if constexpr (LANES < 64) {
         // Every lane's values in descending order (neighbours change places only where the later one is larger, so the lower column stays first), then `top` times the
         // largest head: of equal ones the first lane's, whose columns are lower.
         uint64_t* kept = room + threadIdx.x / LANES * MOST;
@@ -151,7 +151,7 @@ __device__ __forceinline__ void write_alternatives(const Scores& a, int64_t row,
                 o[j] = first, o[j + 1] = second;
                 which[j] = change ? next : here, which[j + 1] = change ? here : next;
             }
-        const uint64_t group = (LANES == 64 ? ~0ull : (1ull << LANES) - 1) << (threadIdx.x & 63 & ~(LANES - 1));
+        const uint64_t group = ((1ull << LANES) - 1) << (threadIdx.x & 63 & ~(LANES - 1));
         for (int r = 0; r < min(a.top, MOST); ++r) {
             const uint32_t best = lanes_max<LANES>(o[0]);
             const uint64_t have = __ballot(o[0] == best) & group;
@@ -174,7 +174,6 @@ __device__ __forceinline__ void write_alternatives(const Scores& a, int64_t row,
         __builtin_amdgcn_wave_barrier();  // (kept is the next row's)
     } else {
         // As for a long row: the top-th largest of the lanes' largest bounds the answer from below; what is as large is collected and ranked by counting.
-        static_assert(R == 1 || LANES == 64, "");
         uint64_t* found = room + threadIdx.x / 64 * (64 * R * V);
         const uint32_t bound = none ? ~0u : bound_of_heads(ordered(own), a.top);
         const float least = in_order(bound);
@@ -186,16 +185,20 @@ __device__ __forceinline__ void write_alternatives(const Scores& a, int64_t row,
             for (int j = 0; j < V; ++j) {
                 const uint64_t takes = none ? 0 : __ballot(x[i][j] >= least);
                 if (!takes) continue;
-                if (x[i][j] >= least) found[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(takes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)takes, 0))] = key_of(ordered(x[i][j]), p.at + j);
+                if (x[i][j] >= least) found[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(takes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)takes, 0))] = (uint64_t)__float_as_uint(x[i][j]) << 32 | (uint32_t)(p.at + j);
                 count += __popcll(takes);
             }
         }
         __builtin_amdgcn_wave_barrier();
+        auto key_at = [&](int i) {
+            const uint64_t both = found[min(i, 64 * R * V - 1)];
+            return i < count ? key_of(ordered(__uint_as_float((uint32_t)(both >> 32))), (int)(uint32_t)both) : 0;
+        };
         for (int i0 = 0; i0 < count; i0 += 64) {
-            const uint64_t mine = i0 + lane < count ? found[i0 + lane] : 0;
+            const uint64_t mine = key_at(i0 + lane);
             int rank = 0;
             for (int j0 = 0; j0 < count; j0 += 64) {
-                const uint64_t other = j0 + lane < count ? found[j0 + lane] : 0;
+                const uint64_t other = j0 == i0 ? mine : key_at(j0 + lane);
                 const int some = min(64, count - j0);
                 for (int j = 0; j < some; ++j) rank += lane_value(other, j) > mine;
             }
@@ -240,11 +243,12 @@ __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
             int piece = i * LANES + lane;
             if constexpr (R * V > 16) asm volatile("" : "+v"(piece));  // (every row's comparisons anew, a piece's at a time: kept they are more than the scalar registers hold)
             const Place<V, false> p(piece, a.c);
+            if (R == 1 || __any(p.seen > 0)) {  // (the last piece of a row, and what lies behind it)
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                x[i][j] = p.counts(j) ? x[i][j] : -INFINITY;
-                m = fmaxf(m, x[i][j]);
+                for (int j = 0; j < V; ++j) x[i][j] = p.counts(j) ? x[i][j] : -INFINITY;
             }
+#pragma unroll
+            for (int j = 0; j < V; ++j) m = fmaxf(m, x[i][j]);
             if constexpr (R * V > 16) __builtin_amdgcn_sched_barrier(0);
         }
         const float own = m;  // of the lane's columns
