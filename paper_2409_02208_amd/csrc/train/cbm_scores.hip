@@ -217,8 +217,9 @@ __device__ __forceinline__ void write_alternatives(const Scores& a, int64_t row,
 
 // Short rows.  LANES lanes a row, each R pieces of V columns.  SELECT: more alternatives than the best one.  Without it four pieces of fp32 (two of 16 bits) a lane, so that many rows share a
 // wave's reductions (235868 x 112 33 us with one piece a lane, 20 with four); with it one piece as long as that is enough, since alternatives come out of sorted lanes.
-// Bound by memory: 235868 x 112 fp32 20 us for 108 MB (5.3 TB/s, some of it out of the caches); with alternatives by vector instructions: 65536 x 1000, top 8 of fp32, 77 us for
-// 262 MB.  19717 x 3 3.1 us, a launch.
+// Bound by memory in fp32: 235868 x 112 20 us for 108 MB (5.3 TB/s, some of it out of the caches), 8192 x 4000 23 us for 131 MB; by vector instructions in 16 bits (21 a value, and a row's
+// reductions: 30310 x 567 bf16 16 us for 35 MB) and with alternatives (65536 x 1000 fp32, top 8, 80 us for 262 MB; 110318 x 133 fp16, top 20, 57 us, 20 times the largest head).  19717 x 3
+// 2.8 us, a launch.
 template <class T, int V, int LANES, int R, bool SELECT>
 __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
     const int lane = threadIdx.x % LANES;
@@ -362,8 +363,8 @@ __device__ __forceinline__ void join_wave(float& m, float& s, float& t) {
 // have met, the maximum is known by then; the top-th largest of these 64 bounds the answer from below, the columns of the few lanes that hold as much are looked through
 // once more (out of L2, most likely), and what is found is ranked.  Where that is more than there is room for (equal scores, or orders that leave the largest
 // to a few lanes), all columns are gone through again in turns of one piece a lane, each of which adds to the list what exceeds it.
-// Bound by memory while rows are many: 4096 x 32000 bf16 with top 8 55.5 us for 262 MB (4.7 TB/s, waves waiting for 52 % of their cycles; 145 with a list kept sorted on the way).
-// One row of 128,000 fp32 in 63 shares: 5.4 us, and 5.4 more for the join, each a launch and three dependent loads.
+// Bound by memory while rows are many: 4096 x 32000 bf16 with top 8 55 us for 262 MB (4.7 TB/s, waves waiting for 52 % of their cycles; 145 with a list kept sorted on the way).
+// One row of 128,000 fp32 in 63 shares: 5.3 us, and 5.4 more for the join, each a launch and three dependent loads.
 template <class T, int V, int R, bool TOP>
 __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_long_kernel(Scores a, int splits, int columns, char* __restrict__ parts) {
     constexpr int TURN = LONG_THREADS * R * V, CAP = TOP ? MOST_TOP * 4 * V + MOST_TOP : 1;
@@ -594,7 +595,9 @@ cbm_status launched(const char* what) {
     cbm_set_error_detail(what, hipGetErrorString(e));
     return CBM_ERR_HIP;
 }
-constexpr int SHORT_ROW = 1024;  // columns that a wave keeps in its registers
+// Columns that a wave keeps in its registers; four times as many where no alternatives but the best are asked for (17261 x 2015 fp32 with the best 24.5 us, by a workgroup a row 51; 8192 x 4000
+// 23 and 34, bf16 18 and 35; with 8,192 columns a wave 8192 x 5000 bf16 took 52, a workgroup a row 35; with alternatives of 2,048 columns 17261 x 2015, top 20, 67, a workgroup 59).
+constexpr int SHORT_ROW = 1024;
 // Columns up to which a workgroup has a row alone whatever the number of rows, since a second launch takes longer than its turns.  Microseconds alone and shared, top 8, captured
 // (calls one after the other): one row of 16,384 columns 5.9 and 9.7 (7.5 and 10.8), 49,152 9.1 and 9.7 (8.8 and 10.9), 65,536 10.4 and 9.7 (10.1 and 10.9); 100 rows of 49,152 11.5 and 13.9.
 constexpr int ALONE = 49152;
