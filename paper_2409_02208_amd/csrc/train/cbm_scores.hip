@@ -377,6 +377,18 @@ __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_long_kernel(Scores a,
         const T* z_row = (const T*)a.z + row * a.ldz;
         const int begin = split * columns, end = min(begin + columns, a.c);
         float m = -INFINITY, s = 0.0f, t = 0.0f;
+        auto rise = [&](float most) {  // the maximum so far, and the sums as seen from it
+            const float now = fmaxf(m, most), base = now == -INFINITY ? 0.0f : now, d = m - base, f = exp_of(d);
+            t = f * (t + fmaxf(d, FAR) * s);
+            s *= f;
+            m = now;
+            return base;
+        };
+        auto add = [&](float z, float base) {
+            const float d = z - base, e = exp_of(d);
+            s += e;
+            t += e * fmaxf(d, FAR);
+        };
         for (int turn = begin; turn < end; turn += TURN) {
             float x[R][V], most = -INFINITY;
 #pragma unroll
@@ -384,34 +396,32 @@ __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_long_kernel(Scores a,
                 const Place<V, false> p(turn / V + i * LONG_THREADS + threadIdx.x, a.c);
                 load_piece<V>(x[i], z_row + p.at);
             }
-            if (turn + TURN > end) {
+            if (turn + TURN <= end) {
+#pragma unroll
+                for (int i = 0; i < R; ++i)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) most = fmaxf(most, x[i][j]);
+                const float base = rise(most);
+#pragma unroll
+                for (int i = 0; i < R; ++i)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) add(x[i][j], base);
+            } else {  // the last turn: a piece at a time, as far as there are any
 #pragma unroll
                 for (int i = 0; i < R; ++i) {
+                    if (turn + i * LONG_THREADS * V >= end) break;
                     const int piece = turn / V + i * LONG_THREADS + threadIdx.x, seen = piece * V < end ? Place<V, false>(piece, a.c).seen : V;
+                    most = -INFINITY;
 #pragma unroll
-                    for (int j = 0; j < V; ++j) x[i][j] = j >= seen ? x[i][j] : -INFINITY;
-                    __builtin_amdgcn_sched_barrier(0);  // (one piece's comparisons at a time: all of them need more scalar registers than there are)
+                    for (int j = 0; j < V; ++j) {
+                        x[i][j] = j >= seen ? x[i][j] : -INFINITY;
+                        most = fmaxf(most, x[i][j]);
+                    }
+                    const float base = rise(most);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) add(x[i][j], base);
                 }
             }
-#pragma unroll
-            for (int i = 0; i < R; ++i)
-#pragma unroll
-                for (int j = 0; j < V; ++j) most = fmaxf(most, x[i][j]);
-            const float now = fmaxf(m, most), base = now == -INFINITY ? 0.0f : now;
-            {
-                const float d = m - base, f = exp_of(d);
-                t = f * (t + fmaxf(d, FAR) * s);
-                s *= f;
-                m = now;
-            }
-#pragma unroll
-            for (int i = 0; i < R; ++i)
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float d = x[i][j] - base, e = exp_of(d);
-                    s += e;
-                    t += e * fmaxf(d, FAR);
-                }
         }
         const float best = m;  // of this lane's columns
         join_wave(m, s, t);
