@@ -94,7 +94,8 @@ __device__ __forceinline__ void write_alternatives(const Scores& a, int64_t row,
     float* values = a.values + (row < a.n ? row : a.n - 1) * a.top;
     int32_t* columns = a.columns + (row < a.n ? row : a.n - 1) * a.top;
     constexpr int MOST = LANES * V < MOST_TOP ? LANES * V : MOST_TOP;  // alternatives of a row of one piece a lane
-    __shared__ uint64_t room[LANES < 64 ? 256 / LANES * MOST : 256 * R * V];  // what a row (a wave) has found
+    constexpr int FOUND = 64 * R * V < 256 ? 64 * R * V : 256;           // room of a wave for candidates
+    __shared__ uint64_t room[LANES < 64 ? 256 / LANES * MOST : 4 * FOUND];  // what a row (a wave) has found
     if constexpr (LANES < 64 && sizeof(T) == 2) {
         uint64_t* kept = room + threadIdx.x / LANES * MOST;
         // A value's 16 bits in order, then its column from behind, make one whole number; every lane's in descending order, then `top` times the largest head.
@@ -173,38 +174,70 @@ __device__ __forceinline__ void write_alternatives(const Scores& a, int64_t row,
         }
         __builtin_amdgcn_wave_barrier();  // (kept is the next row's)
     } else {
-        // As for a long row: the top-th largest of the lanes' largest bounds the answer from below; what is as large is collected and ranked by counting.
-        uint64_t* found = room + threadIdx.x / 64 * (64 * R * V);
+        // As for a long row: the top-th largest of the lanes' largest bounds the answer from below; what is as large is collected and ranked by counting.  Where that is more than there
+        // is room for (many equal scores), the largest score below the last one, `top` times.
+        uint64_t* found = room + threadIdx.x / 64 * FOUND;
+        float* values = a.values + (row < a.n ? row : a.n - 1) * a.top;
+        int32_t* columns = a.columns + (row < a.n ? row : a.n - 1) * a.top;
         const uint32_t bound = none ? ~0u : bound_of_heads(ordered(own), a.top);
         const float least = in_order(bound);
         int count = 0;
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const Place<V, false> p(i * LANES + lane, a.c);
+            const int at = Place<V, false>(i * LANES + lane, a.c).at;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const uint64_t takes = none ? 0 : __ballot(x[i][j] >= least);
                 if (!takes) continue;
-                if (x[i][j] >= least) found[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(takes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)takes, 0))] = (uint64_t)__float_as_uint(x[i][j]) << 32 | (uint32_t)(p.at + j);
+                const int to = count + __builtin_amdgcn_mbcnt_hi((uint32_t)(takes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)takes, 0));
+                if (x[i][j] >= least && to < FOUND) found[to] = (uint64_t)__float_as_uint(x[i][j]) << 32 | (uint32_t)(at + j);
                 count += __popcll(takes);
             }
+            if constexpr (R * V > 16) __builtin_amdgcn_sched_barrier(0);
         }
         __builtin_amdgcn_wave_barrier();
-        auto key_at = [&](int i) {
-            const uint64_t both = found[min(i, 64 * R * V - 1)];
-            return i < count ? key_of(ordered(__uint_as_float((uint32_t)(both >> 32))), (int)(uint32_t)both) : 0;
-        };
-        for (int i0 = 0; i0 < count; i0 += 64) {
-            const uint64_t mine = key_at(i0 + lane);
-            int rank = 0;
-            for (int j0 = 0; j0 < count; j0 += 64) {
-                const uint64_t other = j0 == i0 ? mine : key_at(j0 + lane);
-                const int some = min(64, count - j0);
-                for (int j = 0; j < some; ++j) rank += lane_value(other, j) > mine;
+        if (count <= FOUND) {
+            auto key_at = [&](int i) {
+                const uint64_t both = found[min(i, FOUND - 1)];
+                return i < count ? key_of(ordered(__uint_as_float((uint32_t)(both >> 32))), (int)(uint32_t)both) : 0;
+            };
+            for (int i0 = 0; i0 < count; i0 += 64) {
+                const uint64_t mine = key_at(i0 + lane);
+                int rank = 0;
+                for (int j0 = 0; j0 < count; j0 += 64) {
+                    const uint64_t other = j0 == i0 ? mine : key_at(j0 + lane);
+                    const int some = min(64, count - j0);
+                    for (int j = 0; j < some; ++j) rank += lane_value(other, j) > mine;
+                }
+                if (mine && rank < a.top && row < a.n) {
+                    values[rank] = in_order((uint32_t)(mine >> 32)) - m - l;
+                    columns[rank] = (int32_t)~(uint32_t)mine;
+                }
             }
-            if (mine && rank < a.top && row < a.n) {
-                values[rank] = in_order((uint32_t)(mine >> 32)) - m - l;
-                columns[rank] = (int32_t)~(uint32_t)mine;
+        } else {
+            uint64_t last = ~0ull;
+            for (int r = 0; r < a.top; ++r) {  // (there are more than `top` of them)
+                uint64_t best = 0;
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                    int piece = i * LANES + lane;
+                    asm volatile("" : "+v"(piece));  // (as above, for places and values)
+                    const int at = Place<V, false>(piece, a.c).at;
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        float z = x[i][j];
+                        asm volatile("" : "+v"(z));
+                        const uint64_t key = key_of(ordered(z), at + j);
+                        best = key < last && key > best ? key : best;
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                const uint32_t high = lanes_max<64>((uint32_t)(best >> 32)), low = lanes_max<64>((uint32_t)(best >> 32) == high ? (uint32_t)best : 0u);
+                last = (uint64_t)high << 32 | low;
+                if (lane == r && row < a.n) {
+                    values[r] = in_order(high) - m - l;
+                    columns[r] = (int32_t)~low;
+                }
             }
         }
         if (lane >= count && lane < a.top && row < a.n) {
@@ -218,7 +251,7 @@ __device__ __forceinline__ void write_alternatives(const Scores& a, int64_t row,
 // Short rows.  LANES lanes a row, each R pieces of V columns.  SELECT: more alternatives than the best one.  Without it four pieces of fp32 (two of 16 bits) a lane, so that many rows share a
 // wave's reductions (235868 x 112 33 us with one piece a lane, 20 with four); with it one piece as long as that is enough, since alternatives come out of sorted lanes.
 // Bound by memory in fp32: 235868 x 112 20 us for 108 MB (5.3 TB/s, some of it out of the caches), 8192 x 4000 23 us for 131 MB; by vector instructions in 16 bits (21 a value, and a row's
-// reductions: 30310 x 567 bf16 16 us for 35 MB) and with alternatives (65536 x 1000 fp32, top 8, 80 us for 262 MB; 110318 x 133 fp16, top 20, 57 us, 20 times the largest head).  19717 x 3
+// reductions: 30310 x 567 bf16 16 us for 35 MB) and with alternatives (65536 x 1000 fp32, top 8, 71 us for 262 MB; 110318 x 133 fp16, top 20, 57 us, 20 times the largest head).  19717 x 3
 // 2.8 us, a launch.
 template <class T, int V, int LANES, int R, bool SELECT>
 __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
@@ -242,7 +275,7 @@ __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             int piece = i * LANES + lane;
-            if constexpr (R * V > 16) asm volatile("" : "+v"(piece));  // (every row's comparisons anew, a piece's at a time: kept they are more than the scalar registers hold)
+            if constexpr (R * V > 16 || (SELECT && R > 1)) asm volatile("" : "+v"(piece));  // (every row's comparisons anew, a piece's at a time: kept they are more than the scalar registers hold)
             const Place<V, false> p(piece, a.c);
             if (R == 1 || __any(p.seen > 0)) {  // (the last piece of a row, and what lies behind it)
 #pragma unroll
@@ -250,7 +283,7 @@ __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
             }
 #pragma unroll
             for (int j = 0; j < V; ++j) m = fmaxf(m, x[i][j]);
-            if constexpr (R * V > 16) __builtin_amdgcn_sched_barrier(0);
+            if constexpr (R * V > 16 || (SELECT && R > 1)) __builtin_amdgcn_sched_barrier(0);
         }
         const float own = m;  // of the lane's columns
         m = lanes_max<LANES>(m);
@@ -605,8 +638,9 @@ cbm_status launched(const char* what) {
     cbm_set_error_detail(what, hipGetErrorString(e));
     return CBM_ERR_HIP;
 }
-// Columns that a wave keeps in its registers; four times as many where no alternatives but the best are asked for (17261 x 2015 fp32 with the best 24.5 us, by a workgroup a row 51; 8192 x 4000
-// 23 and 34, bf16 18 and 35; with 8,192 columns a wave 8192 x 5000 bf16 took 52, a workgroup a row 35; with alternatives of 2,048 columns 17261 x 2015, top 20, 67, a workgroup 59).
+// Columns that a wave keeps in its registers in 16 values a lane; a wave has rows of twice as many, four times where no alternatives but the best are asked for (17261 x 2015 fp32 with the best
+// 24.5 us, by a workgroup a row 51, top 8 40 and 54, bf16 30 and 56; 8192 x 4000 with the best 23 and 34, bf16 18 and 35, but top 8 70 and 37; with 8,192 columns a wave 8192 x 5000 bf16
+// took 52, a workgroup a row 35).
 constexpr int SHORT_ROW = 1024;
 // Columns up to which a workgroup has a row alone whatever the number of rows, since a second launch takes longer than its turns.  Microseconds alone and shared, top 8, captured
 // (calls one after the other): one row of 16,384 columns 5.9 and 9.7 (7.5 and 10.8), 49,152 9.1 and 9.7 (8.8 and 10.9), 65,536 10.4 and 9.7 (10.1 and 10.9); 100 rows of 49,152 11.5 and 13.9.
@@ -646,7 +680,8 @@ cbm_status cbm_launch_scores(int64_t n, int32_t c, int32_t type, const void* z, 
             else if (pieces <= 16) CBM_SCORES(V, 16, 1, true);
             else if (pieces <= 32) CBM_SCORES(V, 32, 1, true);
             else CBM_SCORES(V, 64, 1, true);
-        } else if (top > 1 && c <= SHORT_ROW) CBM_SCORES(V, 64, SHORT_ROW / 64 / V, true);
+        } else if (top > 1 && c <= SHORT_ROW) CBM_SCORES(V, 64, R, true);
+        else if (top > 1 && c <= 2 * SHORT_ROW) CBM_SCORES(V, 64, 2 * R, true);
         else if (pieces <= 1) CBM_SCORES(V, 1, 1, false);
         else if (pieces <= 2) CBM_SCORES(V, 2, 1, false);
         else if (pieces <= 4) CBM_SCORES(V, 4, 1, false);
@@ -655,7 +690,7 @@ cbm_status cbm_launch_scores(int64_t n, int32_t c, int32_t type, const void* z, 
         else if (pieces <= 16 * R) CBM_SCORES(V, 16, R, false);
         else if (pieces <= 32 * R) CBM_SCORES(V, 32, R, false);
         else if (c <= SHORT_ROW) CBM_SCORES(V, 64, R, false);
-        else if (top <= 1 && c <= 2 * SHORT_ROW) CBM_SCORES(V, 64, 2 * R, false);
+        else if (c <= 2 * SHORT_ROW) CBM_SCORES(V, 64, 2 * R, false);
         else if (top <= 1 && c <= 4 * SHORT_ROW) CBM_SCORES(V, 64, 4 * R, false);
 #undef CBM_SCORES
         else {
