@@ -323,7 +323,7 @@ __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
     }
 }
 
-// What a workgroup of LONG_THREADS finds its alternatives with.
+// What a workgroup finds its alternatives with.
 template <int CAP>
 struct Select {
     uint64_t head[64], list[MOST_TOP], found[CAP];
@@ -332,9 +332,9 @@ struct Select {
     uint16_t lane[LONG_THREADS];
 };
 // The `top` largest of found[0 .. count) to the list, by counting what is larger (keys differ, so do ranks).
-template <int CAP>
+template <int THREADS, int CAP>
 __device__ __forceinline__ void rank_found(Select<CAP>& s, int top, int count) {
-    for (int i = threadIdx.x; i < count; i += LONG_THREADS) {
+    for (int i = threadIdx.x; i < count; i += THREADS) {
         const uint64_t mine = s.found[i];
         int rank = 0;
 #pragma unroll 8
@@ -345,7 +345,7 @@ __device__ __forceinline__ void rank_found(Select<CAP>& s, int top, int count) {
 }
 // The `top` largest of the list's keys and of those that each(take) takes.  `head`: the largest of each of 64 parts of these, so that the top-th largest head bounds the answer
 // from below; the parts are so small that there is room for what is as large.
-template <int CAP, class F>
+template <int THREADS, int CAP, class F>
 __device__ __forceinline__ void select_keys(Select<CAP>& s, int top, F&& each) {
     __syncthreads();
     if (threadIdx.x < 64) {
@@ -368,7 +368,7 @@ __device__ __forceinline__ void select_keys(Select<CAP>& s, int top, F&& each) {
     const int count = s.count;
     if ((int)threadIdx.x < top) s.list[threadIdx.x] = 0;
     __syncthreads();
-    rank_found(s, top, count);
+    rank_found<THREADS>(s, top, count);
 }
 
 __device__ __forceinline__ void write_top(const Scores& a, int64_t row, const uint64_t* list, float m, float l) {
@@ -392,17 +392,18 @@ __device__ __forceinline__ void join_wave(float& m, float& s, float& t) {
     m = all;
 }
 
-// Long rows.  A workgroup a row, or a share of `columns` of its columns (a multiple of V); R pieces of V columns a lane and turn.  The alternatives come last: of what each four lanes
+// Long rows.  A workgroup (of four waves or one) a row, or a share of `columns` of its columns (a multiple of V); R pieces of V columns a lane and turn.  The alternatives come last: of what each four lanes (one of a single wave)
 // have met, the maximum is known by then; the top-th largest of these 64 bounds the answer from below, the columns of the few lanes that hold as much are looked through
 // once more (out of L2, most likely), and what is found is ranked.  Where that is more than there is room for (equal scores, or orders that leave the largest
 // to a few lanes), all columns are gone through again in turns of one piece a lane, each of which adds to the list what exceeds it.
 // Bound by memory while rows are many: 4096 x 32000 bf16 with top 8 55 us for 262 MB (4.7 TB/s, waves waiting for 52 % of their cycles; 145 with a list kept sorted on the way).
 // One row of 128,000 fp32 in 63 shares: 5.3 us, and 5.4 more for the join, each a launch and three dependent loads.
-template <class T, int V, int R, bool TOP>
-__global__ __launch_bounds__(LONG_THREADS) void cbm_scores_long_kernel(Scores a, int splits, int columns, char* __restrict__ parts) {
-    constexpr int TURN = LONG_THREADS * R * V, CAP = TOP ? MOST_TOP * 4 * V + MOST_TOP : 1;
+template <class T, int V, int R, bool TOP, int THREADS>
+__global__ __launch_bounds__(THREADS) void cbm_scores_long_kernel(Scores a, int splits, int columns, char* __restrict__ parts) {
+    constexpr int TURN = THREADS * R * V, WAVES = THREADS / 64, CAP = TOP ? MOST_TOP * WAVES * V + MOST_TOP : 1;
+    static_assert(WAVES == 1 || WAVES == 4, "");
     __shared__ Select<CAP> sel;
-    __shared__ float room[3][LONG_THREADS / 64];
+    __shared__ float room[3][WAVES];
     const int wave = threadIdx.x / 64;
     for (int64_t item = blockIdx.x; item < a.n * splits; item += gridDim.x) {
         const int64_t row = item / splits;
@@ -426,7 +427,7 @@ __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_long_kernel(Scores a,
             float x[R][V], most = -INFINITY;
 #pragma unroll
             for (int i = 0; i < R; ++i) {
-                const Place<V, false> p(turn / V + i * LONG_THREADS + threadIdx.x, a.c);
+                const Place<V, false> p(turn / V + i * THREADS + threadIdx.x, a.c);
                 load_piece<V>(x[i], z_row + p.at);
             }
             if (turn + TURN <= end) {
@@ -442,8 +443,8 @@ __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_long_kernel(Scores a,
             } else {  // the last turn: a piece at a time, as far as there are any
 #pragma unroll
                 for (int i = 0; i < R; ++i) {
-                    if (turn + i * LONG_THREADS * V >= end) break;
-                    const int piece = turn / V + i * LONG_THREADS + threadIdx.x, seen = piece * V < end ? Place<V, false>(piece, a.c).seen : V;
+                    if (turn + i * THREADS * V >= end) break;
+                    const int piece = turn / V + i * THREADS + threadIdx.x, seen = piece * V < end ? Place<V, false>(piece, a.c).seen : V;
                     most = -INFINITY;
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
@@ -459,26 +460,30 @@ __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_long_kernel(Scores a,
         const float best = m;  // of this lane's columns
         join_wave(m, s, t);
         __syncthreads();
-        if ((threadIdx.x & 63) == 0) {
+        if (WAVES > 1 && (threadIdx.x & 63) == 0) {
             room[0][wave] = m;
             room[1][wave] = s;
             room[2][wave] = t;
         }
-        if constexpr (TOP) {  // a key for each four lanes, of which only the value matters
-            float four = best;
-            four = fmaxf(four, lane_other<1>(four));
-            four = fmaxf(four, lane_other<2>(four));
-            if (threadIdx.x % 4 == 0) sel.head[threadIdx.x / 4] = key_of(ordered(four), 0);
+        if constexpr (TOP) {  // a key for each four lanes (each lane of a wave alone), of which only the value matters
+            float some = best;
+            if constexpr (WAVES == 4) {
+                some = fmaxf(some, lane_other<1>(some));
+                some = fmaxf(some, lane_other<2>(some));
+            }
+            if (threadIdx.x % WAVES == 0) sel.head[threadIdx.x / WAVES] = key_of(ordered(some), 0);
             if ((int)threadIdx.x < MOST_TOP) sel.list[threadIdx.x] = 0;
             if (threadIdx.x == 0) sel.count = sel.lanes = 0;
         }
         __syncthreads();
-        const int w = min((int)threadIdx.x & 63, LONG_THREADS / 64 - 1);
-        const bool first = (threadIdx.x & 63) < LONG_THREADS / 64;
-        m = first ? room[0][w] : -INFINITY;
-        s = first ? room[1][w] : 0.0f;
-        t = first ? room[2][w] : 0.0f;
-        join_wave(m, s, t);
+        if constexpr (WAVES > 1) {
+            const int w = min((int)threadIdx.x & 63, WAVES - 1);
+            const bool first = (threadIdx.x & 63) < WAVES;
+            m = first ? room[0][w] : -INFINITY;
+            s = first ? room[1][w] : 0.0f;
+            t = first ? room[2][w] : 0.0f;
+            join_wave(m, s, t);
+        }
         if constexpr (TOP) {
             // f(value, column) for the lane's columns that count, of the piece `piece`
             auto scan = [&](int piece, auto&& f) {
@@ -499,30 +504,30 @@ __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_long_kernel(Scores a,
             };
             if (ordered(best) >= bound) sel.lane[atomicAdd(&sel.lanes, 1)] = (uint16_t)threadIdx.x;
             __syncthreads();
-            const int lanes = sel.lanes, turns = (end - begin + LONG_THREADS * V - 1) / (LONG_THREADS * V);
-            for (int i = threadIdx.x; i < lanes * turns; i += LONG_THREADS)  // (the lanes' pieces are shared out, so that they are loaded at once)
-                scan(begin / V + i / lanes * LONG_THREADS + sel.lane[i % lanes], take);
+            const int lanes = sel.lanes, turns = (end - begin + THREADS * V - 1) / (THREADS * V);
+            for (int i = threadIdx.x; i < lanes * turns; i += THREADS)  // (the lanes' pieces are shared out, so that they are loaded at once)
+                scan(begin / V + i / lanes * THREADS + sel.lane[i % lanes], take);
             __syncthreads();
             const int count = sel.count;
             const bool done = count <= CAP;
-            if (done) rank_found(sel, a.top, count);
+            if (done) rank_found<THREADS>(sel, a.top, count);
             if (!done) {
                 float least = -INFINITY;  // the last of the alternatives so far; a later column has to exceed it
-                for (int turn = begin / V; turn * V < end; turn += LONG_THREADS) {
+                for (int turn = begin / V; turn * V < end; turn += THREADS) {
                     uint64_t mine = 0;
                     scan(turn + threadIdx.x, [&](float v, int column) {
                         const uint64_t key = v > least ? key_of(ordered(v), column) : 0;
                         mine = key > mine ? key : mine;
                     });
                     if (!__syncthreads_or(mine != 0)) continue;
-                    uint64_t four = mine;
+                    uint64_t some = mine;
 #pragma unroll
-                    for (int step = 1; step <= 2; step *= 2) {
-                        const uint64_t other = (uint64_t)__shfl_xor((unsigned long long)four, step);
-                        four = other > four ? other : four;
+                    for (int step = 1; step < WAVES; step *= 2) {
+                        const uint64_t other = (uint64_t)__shfl_xor((unsigned long long)some, step);
+                        some = other > some ? other : some;
                     }
-                    if (threadIdx.x % 4 == 0) sel.head[threadIdx.x / 4] = four;
-                    select_keys(sel, a.top, [&](auto&& take) {
+                    if (threadIdx.x % WAVES == 0) sel.head[threadIdx.x / WAVES] = some;
+                    select_keys<THREADS>(sel, a.top, [&](auto&& take) {
                         if (mine >= sel.bound) scan(turn + threadIdx.x, [&](float v, int column) { take(v > least ? key_of(ordered(v), column) : 0); });  // (0 < 1 <= bound)
                     });
                     const uint64_t last = sel.list[a.top - 1];
@@ -576,7 +581,7 @@ __global__ __launch_bounds__(LONG_THREADS) void cbm_scores_join_kernel(Scores a,
         __syncthreads();
         if ((int)threadIdx.x < 64) sel.head[lane] = keys[0];
         if ((int)threadIdx.x < MOST_TOP) sel.list[threadIdx.x] = 0;
-        select_keys(sel, a.top, [&](auto&& take) {
+        select_keys<LONG_THREADS>(sel, a.top, [&](auto&& take) {
 #pragma unroll
             for (int i = 0; i < EACH; ++i)
                 if (keys[i]) take(keys[i]);
@@ -645,6 +650,10 @@ constexpr int SHORT_ROW = 1024;
 // Columns up to which a workgroup has a row alone whatever the number of rows, since a second launch takes longer than its turns.  Microseconds alone and shared, top 8, captured
 // (calls one after the other): one row of 16,384 columns 5.9 and 9.7 (7.5 and 10.8), 49,152 9.1 and 9.7 (8.8 and 10.9), 65,536 10.4 and 9.7 (10.1 and 10.9); 100 rows of 49,152 11.5 and 13.9.
 constexpr int ALONE = 49152;
+// Rows that a wave passes through alone, and bytes of each: four waves share a row's values, but each does its reductions.  Microseconds, a wave and four: 52207 x 2273 fp16, top 8, 76 and 195,
+// 17261 x 5000 bf16 36 and 49, top 8 46 and 70, 1024 x 2195 fp32 6.1 and 6.7, 1024 x 5000 bf16 8.0 and 8.0; longer rows leave too few loads under way: 17261 x 5000 fp32, top 20, 99 and 80,
+// 8192 x 16000 bf16, top 8, 77 and 61.
+constexpr int MANY_ROWS = 1024, WAVE_ROW = 16384;
 
 }  // namespace
 
@@ -697,9 +706,11 @@ cbm_status cbm_launch_scores(int64_t n, int32_t c, int32_t type, const void* z, 
             const int splits = c <= ALONE ? 1 : cbm_scores_splits(n, c);
             int share = ((c + splits - 1) / splits + V - 1) / V * V;
             const unsigned grid = (unsigned)std::min<int64_t>(n * splits, 1 << 20);
-#define CBM_LONG(R, TOP) cbm_scores_long_kernel<T, V, R, TOP><<<grid, LONG_THREADS, 0, stream>>>(a, splits, share, (char*)parts)
-            if (share <= 2048) top ? CBM_LONG(8 / V, true) : CBM_LONG(8 / V, false);
-            else top ? CBM_LONG(32 / V, true) : CBM_LONG(32 / V, false);
+#define CBM_LONG(R, TOP, THREADS) cbm_scores_long_kernel<T, V, R, TOP, THREADS><<<grid, THREADS, 0, stream>>>(a, splits, share, (char*)parts)
+            if (n >= MANY_ROWS && c * (int)sizeof(T) <= WAVE_ROW)  // (splits is 1)
+                top ? CBM_LONG(32 / V, true, 64) : CBM_LONG(32 / V, false, 64);
+            else if (share <= 2048) top ? CBM_LONG(8 / V, true, LONG_THREADS) : CBM_LONG(8 / V, false, LONG_THREADS);
+            else top ? CBM_LONG(32 / V, true, LONG_THREADS) : CBM_LONG(32 / V, false, LONG_THREADS);
 #undef CBM_LONG
             if (splits > 1) cbm_scores_join_kernel<T><<<(unsigned)std::min<int64_t>(n, 1 << 20), LONG_THREADS, 0, stream>>>(a, splits, (char*)parts);
         }

@@ -105,3 +105,20 @@ def test_as_many_equal_scores_as_there_is_room_for(env, name, c):  # noqa: F811
     labels = rng.integers(0, c, 9)
     for top in (1, 2, 20, 32):
         _check(torch, Z, labels, _scores(torch, cbm, Z, labels, top), top)
+
+
+# a wave a row: many rows of more columns than stay in registers; the largest scores in a few lanes' columns, equal ones, masks
+@pytest.mark.parametrize("n,c,name", [(1024, 2049, "f32"), (1500, 4096, "f32"), (1024, 4097, "f32"), (1025, 2049, "bf16"), (1024, 5003, "f16"), (1100, 8192, "bf16"), (1100, 8193, "f16")])
+def test_many_rows_of_scores(env, n, c, name):  # noqa: F811
+    torch, cbm = env
+    rng = np.random.default_rng(n + c)
+    z = 3 * rng.standard_normal((n, c))
+    z[::7] = rng.integers(-2, 3, z[::7].shape)
+    z[1::7, : c // 2] = -np.inf
+    z[2::7] = np.where(np.arange(c) % 512 < 8, 20.0 + rng.random(c), z[2::7])
+    z[3], z[10], z[17, 5], z[24, 0] = 1.5, -np.inf, np.nan, np.inf
+    z[31] = np.arange(c) / 512.0
+    Z, _ = _matrix(torch, z, name, 3)
+    labels = rng.integers(-1, c + 1, n)
+    for top in (0, 1, 8, 32):
+        _check(torch, Z, labels, _scores(torch, cbm, Z, labels, top), top)
