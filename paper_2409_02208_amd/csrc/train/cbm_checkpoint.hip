@@ -29,6 +29,12 @@ __device__ __forceinline__ void load_row_piece(float (&x)[V], const T* row, cons
         for (int j = 0; j < V; ++j) x[j] = p.at + j >= 0 ? (float)row[p.at + j] : 0.0f;
     }
 }
+// How many values of a piece may be another lane's as well for the lane to write all of it: in a row's last piece they get the same bits from both lanes where they share the step (and a gradient in
+// place, gated twice, is gated once).
+template <int V>
+__device__ __forceinline__ int most_seen(int k) {
+    return k >= V && (k - V) / BLOCK == (k - 1) / BLOCK ? V - 1 : 0;
+}
 template <int V>
 __device__ __forceinline__ void load_row_bytes(int (&q)[V], const int8_t* row, const Place<V, false>& p, int k) {
     if (k >= V) {
@@ -48,7 +54,7 @@ __global__ __launch_bounds__(256) void cbm_checkpoint_save_kernel(int64_t n, int
                                                                   uint8_t* __restrict__ E, int64_t lde) {
     constexpr int V = 16 / (int)sizeof(T), PER_BLOCK = BLOCK / V;
     constexpr int ROWS = 256 / LANES, ACROSS = LANES == 64 ? R : 1, DOWN = LANES == 64 ? 1 : R;
-    const int lane = threadIdx.x % LANES, first = blockIdx.y * ACROSS * LANES + lane, blocks = (k + BLOCK - 1) / BLOCK;
+    const int lane = threadIdx.x % LANES, first = blockIdx.y * ACROSS * LANES + lane, blocks = (k + BLOCK - 1) / BLOCK, most = most_seen<V>(k);
     for (int64_t row0 = (int64_t)blockIdx.x * (DOWN * ROWS) + threadIdx.x / LANES; row0 < n; row0 += (int64_t)gridDim.x * (DOWN * ROWS)) {
         float x[R][V];
 #pragma unroll
@@ -85,7 +91,7 @@ __global__ __launch_bounds__(256) void cbm_checkpoint_save_kernel(int64_t n, int
                 }
             }
             int8_t* out = Q + row * ldq + p.at;
-            if (p.seen <= 0) {
+            if (p.seen <= most) {
                 typedef uint32_t Words __attribute__((ext_vector_type(V / 4), aligned(1)));
                 Words words;
 #pragma unroll
@@ -108,7 +114,7 @@ __global__ __launch_bounds__(256) void cbm_checkpoint_load_kernel(int64_t n, int
                                                                   int64_t lddy, T* out, int64_t ldo, bool far) {
     constexpr int V = 16 / (int)sizeof(T);
     constexpr int ROWS = 256 / LANES, ACROSS = LANES == 64 ? R : 1, DOWN = LANES == 64 ? 1 : R;
-    const int lane = threadIdx.x % LANES, first = blockIdx.y * ACROSS * LANES + lane, blocks = (k + BLOCK - 1) / BLOCK;
+    const int lane = threadIdx.x % LANES, first = blockIdx.y * ACROSS * LANES + lane, blocks = (k + BLOCK - 1) / BLOCK, most = most_seen<V>(k);
     for (int64_t row0 = (int64_t)blockIdx.x * (DOWN * ROWS) + threadIdx.x / LANES; row0 < n; row0 += (int64_t)gridDim.x * (DOWN * ROWS)) {
         int q[R][V];
         float x[R][V];
@@ -131,7 +137,7 @@ __global__ __launch_bounds__(256) void cbm_checkpoint_load_kernel(int64_t n, int
 #pragma unroll
             for (int j = 0; j < V; ++j) x[i][j] = !GATED ? value_of(q[i][j], code[i]) : code[i] == NOT_FINITE ? NAN : q[i][j] > 0 ? x[i][j] : 0.0f;
             T* to = out + row * ldo + p.at;
-            if (p.seen <= 0) {
+            if (p.seen <= most) {
                 store_piece<V>(to, x[i], far);
             } else if (p.any()) {
 #pragma unroll
