@@ -602,10 +602,11 @@ struct Slopes {
     int64_t lddz;
 };
 // Backward.  LANES lanes a row and a share of its columns (blockIdx.y), V columns a lane and turn; no lane needs another's, since the forward pass kept m and l.  Bound by memory:
-// 132534 x 47 fp32 10.3 to 11.7 us for 51.4 MB (4.7 TB/s, waves waiting for 66 % of their cycles).
+// 132534 x 47 fp32 11 us for 51.4 MB (4.7 TB/s, waves waiting for 66 % of their cycles), bf16 8.1 (10.4 with a row's last piece written value by value).
 template <class T, int V, int LANES>
 __global__ __launch_bounds__(256) void cbm_scores_back_kernel(Slopes a, int turns, bool far) {
     const int lane = threadIdx.x % LANES, pieces = (a.c + V - 1) / V;
+    const int most = a.dz == a.z ? 0 : V - 1;  // of a piece's values that are another lane's as well: they get the same bits twice, but where dz is z that lane may not have read them yet
     for (int64_t row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES; row < a.n; row += (int64_t)gridDim.x * (256 / LANES)) {
         const float m = a.stats[2 * row], l = a.stats[2 * row + 1];
         const int64_t label = a.dlogp ? label_of(a.labels, a.wide_labels, row) : -1;
@@ -626,9 +627,9 @@ __global__ __launch_bounds__(256) void cbm_scores_back_kernel(Slopes a, int turn
                 const float v = own - pr * (slope + of_entropy * (fmaxf(log_p, FAR) + entropy));
                 x[j] = empty ? 0.0f : v;
             }
-            if (p.seen == 0) {
+            if (p.seen <= most) {
                 store_piece<V>(out + p.at, x, far);
-            } else {  // (the other values are another lane's, which may not have read them yet where dz is z)
+            } else {
 #pragma unroll
                 for (int j = 0; j < V; ++j)
                     if (p.counts(j)) out[p.at + j] = (T)x[j];
