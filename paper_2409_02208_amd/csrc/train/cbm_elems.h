@@ -61,12 +61,15 @@ struct Place {
     __device__ __forceinline__ bool counts(int j) const { return WHOLE ? seen <= 0 : j >= seen; }
 };
 
-// f(the largest power of two up to k) for a row of k < V values: one or two such pieces.
+// f(the largest power of two up to k, how many lanes have such a piece each) for a row of k < V values.
 template <int V, class F>
 inline void cbm_narrow_row(int k, F&& f) {
     if constexpr (V > 1) {
-        if (k >= V / 2) f(std::integral_constant<int, V / 2>{});
-        else cbm_narrow_row<V / 2>(k, f);
+        using std::integral_constant;
+        constexpr int HALF = V / 2;
+        if (k < HALF) cbm_narrow_row<HALF>(k, f);
+        else if (k == HALF) f(integral_constant<int, HALF>{}, integral_constant<int, 1>{});
+        else if constexpr (HALF > 1) f(integral_constant<int, HALF>{}, integral_constant<int, 2>{});
     }
 }
 

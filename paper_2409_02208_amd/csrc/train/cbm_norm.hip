@@ -480,10 +480,10 @@ cbm_status cbm_launch_norm(int64_t n, int32_t k, int32_t type, const void* X_, i
 #define CBM_NORM(V_, LANES, R)                                                                                                                                                        \
     cbm_norm_kernel<T, V_, LANES, R, WHOLE><<<(unsigned)at_most(n, (LANES > NORM_THREADS ? LANES : NORM_THREADS) / LANES, 256 * (LANES == 1024 ? 1 : LANES > NORM_THREADS ? 2 : 8)), \
                                               LANES > NORM_THREADS ? LANES : NORM_THREADS, 0, stream>>>(n, k, X, ldx, gamma, beta, eps, Y, ldy, mean, rstd, far)
-        if (k < V) {
-            if constexpr (!WHOLE) cbm_narrow_row<V>(k, [&](auto v) { k == v() ? CBM_NORM(v(), 1, 1) : CBM_NORM(v(), 2, 1); });
-        } else if (pieces <= 1) CBM_NORM(V, 1, 1);
-        else if (pieces <= 2) CBM_NORM(V, 2, 1);
+        if (k <= V) {
+            if constexpr (WHOLE) CBM_NORM(V, 1, 1);
+            else cbm_narrow_row<V>(k, [&](auto v, auto lanes) { CBM_NORM(v(), lanes(), 1); });
+        } else if (pieces <= 2) CBM_NORM(V, 2, 1);
         else if (pieces <= 4) CBM_NORM(V, 4, 1);
         else if (pieces <= 8) CBM_NORM(V, 8, 1);
         else if (pieces <= 16) CBM_NORM(V, 16, 1);
@@ -526,10 +526,10 @@ cbm_status cbm_launch_norm_backward(int64_t n, int32_t k, int32_t type, const vo
      cbm_norm_back_kernel<T, V_, LANES, R, THREADS, WHOLE><<<(unsigned)(dX || !once ? count : 0) + alone, THREADS, 0, stream>>>(n, k, dY, lddy, X, ldx, gamma, mean, rstd, dX, lddx, parts, \
                                                                                                                                dX || !once ? (int)count : 0, dgamma, dbeta, far),      \
      joined = once)
-            if (k < V) {
-                if constexpr (!WHOLE) cbm_narrow_row<V>(k, [&](auto v) { k == v() ? CBM_BACK(v(), 1, 1, BACK_THREADS, BACK_GROUPS) : CBM_BACK(v(), 2, 1, BACK_THREADS, BACK_GROUPS); });
-            } else if (pieces <= 1) CBM_BACK(V, 1, 1, BACK_THREADS, BACK_GROUPS);
-            else if (pieces <= 2) CBM_BACK(V, 2, 1, BACK_THREADS, BACK_GROUPS);
+            if (k <= V) {
+                if constexpr (WHOLE) CBM_BACK(V, 1, 1, BACK_THREADS, BACK_GROUPS);
+                else cbm_narrow_row<V>(k, [&](auto v, auto lanes) { CBM_BACK(v(), lanes(), 1, BACK_THREADS, BACK_GROUPS); });
+            } else if (pieces <= 2) CBM_BACK(V, 2, 1, BACK_THREADS, BACK_GROUPS);
             else if (pieces <= 4) CBM_BACK(V, 4, 1, BACK_THREADS, BACK_GROUPS);
             else if (pieces <= 8) CBM_BACK(V, 8, 1, BACK_THREADS, BACK_GROUPS);
             else if (pieces <= 16) CBM_BACK(V, 16, 1, BACK_THREADS, BACK_GROUPS);

@@ -678,10 +678,7 @@ cbm_status cbm_launch_scores(int64_t n, int32_t c, int32_t type, const void* z, 
 #define CBM_SCORES(V_, LANES, R, SELECT) \
     cbm_scores_kernel<T, V_, LANES, R, SELECT><<<(unsigned)std::min<int64_t>((n + 256 / LANES - 1) / (256 / LANES), 1 << 23), 256, 0, stream>>>(a)
         constexpr int R = 16 / V;
-        if (c < V) cbm_narrow_row<V>(c, [&](auto v) {
-                if (c == v()) top > 1 ? CBM_SCORES(v(), 1, 1, true) : CBM_SCORES(v(), 1, 1, false);
-                else top > 1 ? CBM_SCORES(v(), 2, 1, true) : CBM_SCORES(v(), 2, 1, false);
-            });
+        if (c < V) cbm_narrow_row<V>(c, [&](auto v, auto lanes) { top > 1 ? CBM_SCORES(v(), lanes(), 1, true) : CBM_SCORES(v(), lanes(), 1, false); });
         else if (top > 1 && pieces <= 64) {
             if (pieces <= 1) CBM_SCORES(V, 1, 1, true);
             else if (pieces <= 2) CBM_SCORES(V, 2, 1, true);
@@ -735,10 +732,9 @@ cbm_status cbm_launch_scores_backward(int64_t n, int32_t c, int32_t type, const 
         cbm_scores_back_kernel<T, V_, LANES><<<dim3((unsigned)std::min<int64_t>((n + 256 / LANES - 1) / (256 / LANES), 1 << 23),                                             \
                                                     (unsigned)((pieces + LANES * turns - 1) / (LANES * turns))), 256, 0, stream>>>(a, turns, far);                              \
     }
-        if (c < V) cbm_narrow_row<V>(c, [&](auto v) {
-                const int64_t pieces = c == v() ? 1 : 2;
-                if (pieces == 1) CBM_BACK(v(), 1)
-                else CBM_BACK(v(), 2)
+        if (c < V) cbm_narrow_row<V>(c, [&](auto v, auto lanes) {
+                const int64_t pieces = lanes();
+                CBM_BACK(v(), lanes())
             });
         else if (pieces <= 1) CBM_BACK(V, 1)
         else if (pieces <= 2) CBM_BACK(V, 2)
