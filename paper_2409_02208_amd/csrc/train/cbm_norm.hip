@@ -3,7 +3,8 @@
 //   with h = (x - m) r and u = dy g:  dx = r (u - mean(u) - h mean(u h)),  dg = sum over rows of dy h,  db = sum over rows of dy.
 // All of it is bound by memory: 8 (forward) and 14 (backward) operations a value against 8 and 12 bytes in fp32.  A row is read once and stays in the registers of
 // a group of lanes (a workgroup for wide rows), so the second pass of the variance, which keeps it exact where |m| is large beside the deviations, costs no
-// traffic.  Statistics and sums are fp32; y and dx are rounded once, to their type.
+// traffic.  A sum of k values in fp32 leaves m off by some units of its last place: nothing beside deviations of |m| / 8, but more than those of a row of equal values.  Rows with smaller ones
+// than that (`near_mean`) have m corrected by the mean of the deviations, and the squares added up anew.  Statistics and sums are fp32; y and dx are rounded once, to their type.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -51,6 +52,9 @@ __device__ __forceinline__ void row_sum2(float& a, float& b, floatx2* room, int&
     }
 }
 
+// Whether there are deviations from m (v: their mean square), but so small ones that the rounding of m shows.  False for what is not finite: an infinity stays the mean.
+__device__ __forceinline__ bool near_mean(float v, float m) { return v > 0.0f && v * 64.0f < m * m; }
+
 // V values of gamma or beta from `at` on; `other` where there are none.
 template <int V>
 __device__ __forceinline__ void load_columns(float (&x)[V], const float* p, int at, float other) {
@@ -93,8 +97,11 @@ __device__ __forceinline__ void store_columns(float* out, const float (&x)[V], c
 // (a workgroup for every few rows: 2097152 x 128 fp32 570 us for 454), in pieces of 16 bytes (value by value 16384 x 4096 bf16 took 68 us, so 54).  A row of one piece or two has as many
 // lanes (1218193 x 8 bf16 9.1 us, with eight lanes a row 19).  Bound by memory: 2097152 x 128 fp32 440 us, 4.9 TB/s of 2.15 GB, waves waiting for 60 % of their cycles;
 // 1024 x 64 2.7 us, a launch.
+// Waves of a SIMD: two pieces of fp32 a lane fit eight, if only just (30000 x 1200 51 us, with seven 59).
+template <int V, int LANES, int R>
+constexpr int NORM_WAVES = V == 4 && LANES == 256 && R == 2 ? 8 : 1;
 template <class T, int V, int LANES, int R, bool WHOLE>
-__global__ __launch_bounds__(LANES > NORM_THREADS ? LANES : NORM_THREADS) void cbm_norm_kernel(int64_t n, int k, const T* __restrict__ X, int64_t ldx, const float* __restrict__ gamma,
+__global__ __launch_bounds__(LANES > NORM_THREADS ? LANES : NORM_THREADS, (NORM_WAVES<V, LANES, R>)) void cbm_norm_kernel(int64_t n, int k, const T* __restrict__ X, int64_t ldx, const float* __restrict__ gamma,
                                                                                               const float* __restrict__ beta, float eps, T* __restrict__ Y, int64_t ldy,
                                                                                               float* __restrict__ mean, float* __restrict__ rstd, bool far) {
     constexpr int THREADS = LANES > NORM_THREADS ? LANES : NORM_THREADS, ROWS = THREADS / LANES;
@@ -130,7 +137,7 @@ __global__ __launch_bounds__(LANES > NORM_THREADS ? LANES : NORM_THREADS) void c
             for (int j = 0; j < V; ++j) sum += p.counts(j) ? x[c][j] : 0.0f;
         }
         row_sum2<LANES>(sum, none, room, turn);
-        const float m = sum / (float)k;
+        float m = sum / (float)k;
 #pragma unroll
         for (int c = 0; c < R; ++c) {
             const Place<V, WHOLE> p(c * LANES + lane, k);
@@ -141,6 +148,30 @@ __global__ __launch_bounds__(LANES > NORM_THREADS ? LANES : NORM_THREADS) void c
             }
         }
         row_sum2<LANES>(squares, none, room, turn);
+        const bool near = near_mean(squares / (float)k, m);
+        if (LANES > 64 ? near : __any(near)) {  // (a wave's other rows take off 0, and keep their bits)
+            float off = 0.0f;
+#pragma unroll
+            for (int c = 0; c < R; ++c) {
+                const Place<V, WHOLE> p(c * LANES + lane, k);
+#pragma unroll
+                for (int j = 0; j < V; ++j) off += p.counts(j) ? x[c][j] : 0.0f;
+            }
+            row_sum2<LANES>(off, none, room, turn);
+            off = near ? off / (float)k : 0.0f;
+            m += off;
+            squares = 0.0f;
+#pragma unroll
+            for (int c = 0; c < R; ++c) {
+                const Place<V, WHOLE> p(c * LANES + lane, k);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    x[c][j] -= off;
+                    squares += p.counts(j) ? x[c][j] * x[c][j] : 0.0f;
+                }
+            }
+            row_sum2<LANES>(squares, none, room, turn);
+        }
         const float r = 1.0f / sqrtf(squares / (float)k + eps);
         if (row >= n) continue;  // (only where a row is part of a wave: with a workgroup a row, row0 is the row)
         T* y_row = Y + row * ldy;
@@ -159,7 +190,7 @@ __global__ __launch_bounds__(LANES > NORM_THREADS ? LANES : NORM_THREADS) void c
     }
 }
 
-// Rows of over 16,384 columns, too wide for registers: a workgroup reads its row three times (all but the first time out of L2), which the caches' rate bounds.
+// Rows of over 16,384 columns, too wide for registers: a workgroup reads its row three times (all but the first time out of L2), which the caches' rate bounds; five times if near its mean.
 template <class T, int V, bool WHOLE>
 __global__ __launch_bounds__(1024) void cbm_norm_wide_kernel(int64_t n, int k, const T* __restrict__ X, int64_t ldx, const float* __restrict__ gamma, const float* __restrict__ beta,
                                                              float eps, T* __restrict__ Y, int64_t ldy, float* __restrict__ mean, float* __restrict__ rstd, bool far) {
@@ -168,24 +199,26 @@ __global__ __launch_bounds__(1024) void cbm_norm_wide_kernel(int64_t n, int k, c
     const int pieces = (k + V - 1) / V;
     for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
         const T* x_row = X + row * ldx;
-        float sum = 0.0f, none = 0.0f, x[V];
-        for (int c = threadIdx.x; c < pieces; c += 1024) {
-            const Place<V, WHOLE> p(c, k);
-            load_piece<V>(x, x_row + p.at);
+        float x[V];
+        auto mean_of = [&](auto&& f) {  // of f(value)
+            float sum = 0.0f, none = 0.0f;
+            for (int c = threadIdx.x; c < pieces; c += 1024) {
+                const Place<V, WHOLE> p(c, k);
+                load_piece<V>(x, x_row + p.at);
 #pragma unroll
-            for (int j = 0; j < V; ++j) sum += p.counts(j) ? x[j] : 0.0f;
+                for (int j = 0; j < V; ++j) sum += p.counts(j) ? f(x[j]) : 0.0f;
+            }
+            block_sum2<1024>(sum, none, room, turn);
+            return sum / (float)k;
+        };
+        const float first = mean_of([](float v) { return v; });
+        float m = first, off = 0.0f, variance = mean_of([=](float v) { return (v - first) * (v - first); });
+        if (near_mean(variance, first)) {
+            off = mean_of([=](float v) { return v - first; });
+            m += off;
+            variance = mean_of([=](float v) { return (v - first - off) * (v - first - off); });
         }
-        block_sum2<1024>(sum, none, room, turn);
-        const float m = sum / (float)k;
-        float squares = 0.0f;
-        for (int c = threadIdx.x; c < pieces; c += 1024) {
-            const Place<V, WHOLE> p(c, k);
-            load_piece<V>(x, x_row + p.at);
-#pragma unroll
-            for (int j = 0; j < V; ++j) squares += p.counts(j) ? (x[j] - m) * (x[j] - m) : 0.0f;
-        }
-        block_sum2<1024>(squares, none, room, turn);
-        const float r = 1.0f / sqrtf(squares / (float)k + eps);
+        const float r = 1.0f / sqrtf(variance + eps);
         for (int c = threadIdx.x; c < pieces; c += 1024) {
             const Place<V, WHOLE> p(c, k);
             load_piece<V>(x, x_row + p.at);
@@ -193,7 +226,7 @@ __global__ __launch_bounds__(1024) void cbm_norm_wide_kernel(int64_t n, int k, c
             load_columns<V>(g, gamma, p.at, 1.0f);
             load_columns<V>(b, beta, p.at, 0.0f);
 #pragma unroll
-            for (int j = 0; j < V; ++j) x[j] = (x[j] - m) * r * g[j] + b[j];
+            for (int j = 0; j < V; ++j) x[j] = (x[j] - first - off) * r * g[j] + b[j];
             store_piece<V>(Y + row * ldy + p.at, x, far);
         }
         if (threadIdx.x == 0) {
