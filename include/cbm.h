@@ -354,7 +354,7 @@ size_t cbm_layer_norm_workspace_bytes(int64_t n, int32_t k);
 /*
  * Activations kept in 8 bits until the backward pass.  Each 32 columns of a row (the last block of a row may be shorter) share a step 2^e:
  *   e = max(floor(log2(largest |x| of them)) - 6, -126);  q = sign(x) min(127, max(1, round-to-even(|x| 2^-e))), 0 for x = 0;  x~ = q 2^e.
- * So |x~ - x| <= 2^e (half of that but for the smallest values and the topmost 1 / 256 of a binade), x~ is never larger than its type's largest value, a
+ * So |x~ - x| <= 2^e (half of that but for the smallest values and the topmost 1 / 128 of a binade), x~ is never larger than its type's largest value, a
  * value other than zero keeps its sign, and x~ is a bf16 value.  A block with a value that is not finite comes back as NaN throughout.
  *   Q   n x k int8, leading dimension ldq >= k: the q.
  *   E   n x ceil(k / 32) uint8, leading dimension lde: e + 127; 255 for a block that is not finite (its q are 0).
