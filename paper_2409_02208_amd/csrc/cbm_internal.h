@@ -283,7 +283,7 @@ cbm_status cbm_launch_gemm(int64_t M, int32_t N, int32_t K, const float* A, int6
                            float* C, int64_t ldc, void* stream);
 
 // layer norm (train/cbm_norm.hip)
-int64_t cbm_norm_parts(int64_t n);  // partial sums of dgamma and dbeta, 2 k values each
+int64_t cbm_norm_parts(int64_t n, int32_t k);  // partial sums of dgamma and dbeta, 2 k values each
 cbm_status cbm_launch_norm(int64_t n, int32_t k, int32_t type, const void* X, int64_t ldx, const float* gamma, const float* beta, float eps, void* Y, int64_t ldy,
                            float* mean, float* rstd, void* stream);
 cbm_status cbm_launch_norm_backward(int64_t n, int32_t k, int32_t type, const void* dY, int64_t lddy, const void* X, int64_t ldx, const float* gamma, const float* mean,

@@ -60,7 +60,7 @@ cbm_status cbm_layer_norm(int64_t n, int32_t k, int32_t type, const void* X, int
 }
 
 size_t cbm_layer_norm_workspace_bytes(int64_t n, int32_t k) {
-    return n < 0 || k <= 0 || k > MOST_COLUMNS ? 0 : (size_t)cbm_norm_parts(n) * 2 * (size_t)k * sizeof(float);
+    return n < 0 || k <= 0 || k > MOST_COLUMNS ? 0 : (size_t)cbm_norm_parts(n, k) * 2 * (size_t)k * sizeof(float);
 }
 
 cbm_status cbm_layer_norm_backward(int64_t n, int32_t k, int32_t type, const void* dY, int64_t lddy, const void* X, int64_t ldx, const float* gamma, const float* mean,

@@ -484,6 +484,13 @@ cbm_status launched(const char* what) {
 
 int64_t at_most(int64_t rows, int rows_each, int64_t most) { return std::min<int64_t>((rows + rows_each - 1) / rows_each, most); }
 
+// Backward: pieces of a row that stays in registers, and workgroups with partial rows of their own for a row of `pieces`.  Half as many (of twice the waves) where partial rows are long: 16384 x 4096 bf16
+// 89.7 us with 512 workgroups, 85.2 with 256; 100000 x 1200 254 and 371.  Rows too wide for registers: eight a compute unit, each for 256 pieces and a share of the rows.
+constexpr int64_t back_held(int v) { return (v == 4 ? 3 : 2) * 1024; }
+int64_t back_groups(int v, int64_t pieces) {
+    return pieces <= 384 ? BACK_GROUPS : pieces <= back_held(v) ? BACK_GROUPS / 2 : std::max<int64_t>(1, 2048 / ((pieces + 255) / 256));
+}
+
 // f(a value of the type, whether its 16-byte pieces divide a row of k)
 template <class F>
 void with_shape(int32_t type, int32_t k, F&& f) {
@@ -495,8 +502,10 @@ void with_shape(int32_t type, int32_t k, F&& f) {
 
 }  // namespace
 
-// Partial rows of the backward pass, whatever its shape.
-int64_t cbm_norm_parts(int64_t n) { return std::min<int64_t>(n, BACK_GROUPS); }
+// Partial rows of the backward pass at most, whatever the type and with it the shape.
+int64_t cbm_norm_parts(int64_t n, int32_t k) {
+    return std::min(n, std::max(back_groups(4, ((int64_t)k + 3) / 4), back_groups(8, ((int64_t)k + 7) / 8)));
+}
 
 cbm_status cbm_launch_norm(int64_t n, int32_t k, int32_t type, const void* X_, int64_t ldx, const float* gamma, const float* beta, float eps, void* Y_, int64_t ldy,
                            float* mean, float* rstd, void* stream_) {
@@ -537,7 +546,6 @@ cbm_status cbm_launch_norm(int64_t n, int32_t k, int32_t type, const void* X_, i
 cbm_status cbm_launch_norm_backward(int64_t n, int32_t k, int32_t type, const void* dY_, int64_t lddy, const void* X_, int64_t ldx, const float* gamma, const float* mean,
                                     const float* rstd, void* dX_, int64_t lddx, float* dgamma, float* dbeta, float* parts, void* stream_) {
     hipStream_t stream = (hipStream_t)stream_;
-    const int64_t most = cbm_norm_parts(n);
     int64_t count = 0;  // partial rows written
     const bool sums = dgamma || dbeta;
     bool joined = !sums;
@@ -549,39 +557,37 @@ cbm_status cbm_launch_norm_backward(int64_t n, int32_t k, int32_t type, const vo
             const T *dY = (const T*)dY_, *X = (const T*)X_;
             T* dX = (T*)dX_;
             constexpr int V = 16 / (int)sizeof(T);
-            const int64_t pieces = ((int64_t)k + V - 1) / V;
+            const int64_t pieces = ((int64_t)k + V - 1) / V, groups = back_groups(V, pieces);
             const bool far = n * k * (int64_t)sizeof(T) >= CBM_FAR_BYTES;
-            const bool once = sums && few_rows(n, k) && pieces <= (V == 4 ? 3 : 2) * 1024;  // (dg and db in the same launch)
+            const bool once = sums && few_rows(n, k) && pieces <= back_held(V);  // (dg and db in the same launch)
             const unsigned alone = once ? (unsigned)(((int64_t)k + 15) / 16) : 0;
             if (once) parts = nullptr;
-#define CBM_BACK(V_, LANES, R, THREADS, GROUPS)                                                                                                                                           \
-    (count = at_most(n, THREADS / LANES, GROUPS),                                                                                                                                   \
+#define CBM_BACK(V_, LANES, R, THREADS)                                                                                                                                                   \
+    (count = at_most(n, THREADS / LANES, groups),                                                                                                                                   \
      cbm_norm_back_kernel<T, V_, LANES, R, THREADS, WHOLE><<<(unsigned)(dX || !once ? count : 0) + alone, THREADS, 0, stream>>>(n, k, dY, lddy, X, ldx, gamma, mean, rstd, dX, lddx, parts, \
                                                                                                                                dX || !once ? (int)count : 0, dgamma, dbeta, far),      \
      joined = once)
             if (k <= V) {
-                if constexpr (WHOLE) CBM_BACK(V, 1, 1, BACK_THREADS, BACK_GROUPS);
-                else cbm_narrow_row<V>(k, [&](auto v, auto lanes) { CBM_BACK(v(), lanes(), 1, BACK_THREADS, BACK_GROUPS); });
-            } else if (pieces <= 2) CBM_BACK(V, 2, 1, BACK_THREADS, BACK_GROUPS);
-            else if (pieces <= 4) CBM_BACK(V, 4, 1, BACK_THREADS, BACK_GROUPS);
-            else if (pieces <= 8) CBM_BACK(V, 8, 1, BACK_THREADS, BACK_GROUPS);
-            else if (pieces <= 16) CBM_BACK(V, 16, 1, BACK_THREADS, BACK_GROUPS);
-            else if (pieces <= 32) CBM_BACK(V, 32, 1, BACK_THREADS, BACK_GROUPS);
-            else if (pieces <= 64) CBM_BACK(V, 64, 1, BACK_THREADS, BACK_GROUPS);
-            else if (pieces <= 128) CBM_BACK(V, 64, 2, 256, BACK_GROUPS);
-            else if (pieces <= 256) CBM_BACK(V, 256, 1, 256, BACK_GROUPS);
-            else if (pieces <= 384) CBM_BACK(V, 256, 2, 256, BACK_GROUPS);
-            // half as many workgroups, of twice the waves: partial rows are long here (16384 x 4096 bf16 89.7 us with 512 workgroups, 85.2 with 256; 100000 x 1200 254 and 371)
-            else if (pieces <= 512) CBM_BACK(V, 512, 1, 512, BACK_GROUPS / 2);
-            else if (pieces <= 1024) CBM_BACK(V, 512, 2, 512, BACK_GROUPS / 2);
-            else if (V == 4 && pieces <= 2048) CBM_BACK(V, 1024, 2, 1024, BACK_GROUPS / 2);
-            else if (pieces <= (V == 4 ? 3 : 2) * 1024) CBM_BACK(V, 1024, V == 4 ? 3 : 2, 1024, BACK_GROUPS / 2);
+                if constexpr (WHOLE) CBM_BACK(V, 1, 1, BACK_THREADS);
+                else cbm_narrow_row<V>(k, [&](auto v, auto lanes) { CBM_BACK(v(), lanes(), 1, BACK_THREADS); });
+            } else if (pieces <= 2) CBM_BACK(V, 2, 1, BACK_THREADS);
+            else if (pieces <= 4) CBM_BACK(V, 4, 1, BACK_THREADS);
+            else if (pieces <= 8) CBM_BACK(V, 8, 1, BACK_THREADS);
+            else if (pieces <= 16) CBM_BACK(V, 16, 1, BACK_THREADS);
+            else if (pieces <= 32) CBM_BACK(V, 32, 1, BACK_THREADS);
+            else if (pieces <= 64) CBM_BACK(V, 64, 1, BACK_THREADS);
+            else if (pieces <= 128) CBM_BACK(V, 64, 2, 256);
+            else if (pieces <= 256) CBM_BACK(V, 256, 1, 256);
+            else if (pieces <= 384) CBM_BACK(V, 256, 2, 256);
+            else if (pieces <= 512) CBM_BACK(V, 512, 1, 512);
+            else if (pieces <= 1024) CBM_BACK(V, 512, 2, 512);
+            else if (V == 4 && pieces <= 2048) CBM_BACK(V, 1024, 2, 1024);
+            else if (pieces <= back_held(V)) CBM_BACK(V, 1024, V == 4 ? 3 : 2, 1024);
             else {
                 if (dX) hipLaunchKernelGGL((cbm_norm_back_wide_kernel<T, V, WHOLE>), dim3((unsigned)std::min<int64_t>(n, 512)), dim3(1024), 0, stream, n, k, dY, lddy, X, ldx, gamma, mean, rstd, dX, lddx, far);
-                const int64_t across = (pieces + 255) / 256;
-                count = std::min<int64_t>(most, std::max<int64_t>(1, 2048 / across));
+                count = std::min(n, groups);
                 if (parts)
-                    cbm_norm_back_columns_kernel<T, V, WHOLE><<<dim3((unsigned)across, (unsigned)count), 256, 0, stream>>>(n, k, dY, lddy, X, ldx, mean, rstd, parts);
+                    cbm_norm_back_columns_kernel<T, V, WHOLE><<<dim3((unsigned)((pieces + 255) / 256), (unsigned)count), 256, 0, stream>>>(n, k, dY, lddy, X, ldx, mean, rstd, parts);
             }
 #undef CBM_BACK
         });
