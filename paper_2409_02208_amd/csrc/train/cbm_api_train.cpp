@@ -111,7 +111,7 @@ cbm_status cbm_checkpoint_relu_backward(int64_t n, int32_t k, const int8_t* Q, i
     if (k > MOST_COLUMNS) return CBM_ERR_UNSUPPORTED;
     cbm_status st = CBM_OK;
     const Span dy = matrix(dY, n, k, lddy, bytes, &st);
-    const bool in_place = dX == dY && lddx == lddy;  // (a value is read and written by one lane)
+    const bool in_place = dX == dY && lddx == lddy;  // (what two lanes read and write, of a row's last piece, is the same gated once or twice)
     const Span in[3] = {matrix(Q, n, k, ldq, 1, &st), matrix(E, n, steps(k), lde, 1, &st), in_place ? Span{nullptr, 0, 0} : dy};
     const Span out[1] = {matrix(dX, n, k, lddx, bytes, &st)};
     if (st != CBM_OK) return st;
