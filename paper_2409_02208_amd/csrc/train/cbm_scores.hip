@@ -73,10 +73,12 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
     return lanes_all<LANES>(v, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
 
-// The largest whole number of 16 bits and zeros that at least `top` lanes of the wave have or exceed, bit by bit; the smallest that is an alternative where fewer lanes have one.
+// The largest whole number that at least `top` lanes of the wave have or exceed, bit by bit; the smallest that is an alternative where fewer lanes have one.  All the bits that a T has: scores of
+// N(0, 3) + 1000 differ in the last ones of fp32 only (65536 x 1000, top 8, 69 us, with 16 bits 245; without the offset 65.5 either way).
+template <class T>
 __device__ __forceinline__ uint32_t bound_of_heads(uint32_t head, int top) {
     uint32_t bound = 0;
-    for (int bit = 31; bit >= 16; --bit) {
+    for (int bit = 31; bit >= 32 - 8 * (int)sizeof(T); --bit) {
         const int have = __popcll(__ballot(head >= (bound | 1u << bit)));
         if (have >= top) bound |= 1u << bit;
         if (have == top) break;  // (they all exceed what the bits below could add, or the bound is a little low, which costs nothing)
@@ -179,7 +181,7 @@ __device__ __forceinline__ void write_alternatives(const Scores& a, int64_t row,
         uint64_t* found = room + threadIdx.x / 64 * FOUND;
         float* values = a.values + (row < a.n ? row : a.n - 1) * a.top;
         int32_t* columns = a.columns + (row < a.n ? row : a.n - 1) * a.top;
-        const uint32_t bound = none ? ~0u : bound_of_heads(ordered(own), a.top);
+        const uint32_t bound = none ? ~0u : bound_of_heads<T>(ordered(own), a.top);
         const float least = in_order(bound);
         int count = 0;
 #pragma unroll
@@ -496,7 +498,7 @@ __global__ __launch_bounds__(THREADS) void cbm_scores_long_kernel(Scores a, int 
                     if (p.counts(j)) f(x[j], p.at + j);
             };
             // what is as large as the bound: the row's maximum where one alternative is asked for
-            const uint32_t bound = a.top == 1 ? max(ordered(m), 1u) : bound_of_heads((uint32_t)(sel.head[threadIdx.x & 63] >> 32), a.top);
+            const uint32_t bound = a.top == 1 ? max(ordered(m), 1u) : bound_of_heads<T>((uint32_t)(sel.head[threadIdx.x & 63] >> 32), a.top);
             auto take = [&](float v, int column) {
                 if (ordered(v) < bound) return;
                 const int at = atomicAdd(&sel.count, 1);
@@ -658,8 +660,8 @@ constexpr int MANY_ROWS = 1024, WAVE_ROW = 16384;
 
 }  // namespace
 
-// Workgroups that may share a row: some for every compute unit, of 1,024 columns at least (one turn of a workgroup is 2,048).  The workspace has room for them, whether a row of
-// this length is shared or not.
+// Workgroups that share a row of over ALONE columns: two for every compute unit over all rows, 64 a row at most, of about 2,048 columns or more.  Few shorter rows are asked for a workspace as if
+// they were shared, although each has one workgroup and nothing reads it.
 int cbm_scores_splits(int64_t n, int32_t c) {
     if (c <= SHORT_ROW || n == 0) return 1;
     return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(MOST_SPLITS, 512 / n), ((int64_t)c + 2047) / 2048));
