@@ -387,7 +387,7 @@ size_t cbm_checkpoint_workspace_bytes(int64_t n, int32_t k, int32_t c);
  *   stats        n x 2: m and l, which the backward pass reads.
  *   top          0 to 32 alternatives: top_values (n x top) receives the largest log p in descending order, top_columns (n x top) their classes, the
  *                lower one first among equal scores; where fewer classes are not ruled out, -infinity and -1.
- *   workspace    cbm_log_probs_workspace_bytes(n, c, top) bytes; 0 but for few rows of over 1,024 columns (those may be shared by several workgroups).
+ *   workspace    cbm_log_probs_workspace_bytes(n, c, top) bytes; 0 but for few rows of over 1,024 columns (those of over 49,152 are shared by several workgroups).
  * logp, entropy and stats may be NULL; fp32, packed.  A row with every class ruled out has m = l = log p[label] = -infinity and entropy 0.  A row
  * with NaN or +infinity has NaN for all of it (0 without a label, classes -1).
  *
