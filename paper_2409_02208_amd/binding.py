@@ -1,5 +1,5 @@
 """Binding of libcbm.so: same names as the C ABI (include/cbm.h), argument marshalling
-only, by ctypes, or by the module _calls.so for the operators between the products.
+only, by ctypes, or by the module _calls for the operators between the products.
 PyTorch tensors supply device memory and the stream; every step of the product runs in the library's HIP kernels.  There is no fallback:
 a missing library raises."""
 from __future__ import annotations
@@ -276,10 +276,16 @@ def _calls():
     global _CALLS
     if _CALLS is None:
         _lib()  # PyTorch, then the library that the module is linked to
-        if not os.path.exists(os.path.join(_PKG, "_calls.so")):
-            raise RuntimeError("_calls.so is not built: run `python -m paper_2409_02208_amd.build`")
+        import torch
+        from importlib.machinery import EXTENSION_SUFFIXES
+
+        name = "_calls" + EXTENSION_SUFFIXES[0]
+        if not os.path.exists(os.path.join(_PKG, name)):
+            raise RuntimeError(f"{name} is not built: run `python -m paper_2409_02208_amd.build`")
         from . import _calls as module
 
+        if module.torch_version != torch.__version__.split("+")[0]:
+            raise RuntimeError(f"{name} is built for PyTorch {module.torch_version}, this is {torch.__version__}: run `python -m paper_2409_02208_amd.build`")
         _CALLS = module
     return _CALLS
 

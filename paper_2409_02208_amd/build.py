@@ -1,16 +1,18 @@
-"""Compile libcbm.so (HIP kernels + host builder + C ABI) for gfx950, and the CPython module _calls.so that reads tensors for it, in-tree."""
+"""Compile libcbm.so (HIP kernels + host builder + C ABI) for gfx950, and the CPython module _calls that reads tensors for it, in-tree.  The library needs
+neither PyTorch nor Python; without PyTorch it is built alone."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libcbm.so")
-CALLS = os.path.join(PKG, "_calls.so")
+CALLS = os.path.join(PKG, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
 CALLS_SOURCE = "train/cbm_python.cpp"
 SOURCES = ["cbm_api.cpp", "cbm_builder.cpp", "cbm_kernels.hip", "cbm_blocks.hip", "cbm_sums.hip", "cbm_flat.hip", "cbm_gemm.hip", "cbm_gemm_split.hip", "cbm_gemm_held.hip", "cbm_build_kernels.hip",
            "train/cbm_api_train.cpp", "train/cbm_norm.hip", "train/cbm_checkpoint.hip", "train/cbm_scores.hip"]
@@ -68,8 +70,6 @@ def _run(cmd):
 
 def _calls_flags() -> list:
     """PyTorch's and Python's headers (as system headers: their warnings are theirs)."""
-    import sysconfig
-
     import torch
     from torch.utils import cpp_extension
 
@@ -96,13 +96,20 @@ def build(verbose: bool = False) -> str:
         flags = COMMON + (DEVICE + RESOURCES if src.endswith(".hip") else [])
         cmds.append([HIPCC] + flags + ["-c", os.path.join(CSRC, src), "-o", obj])
     calls = os.path.join(objdir, CALLS_SOURCE.replace("/", "_") + ".o")
-    cmds.append([HIPCC] + COMMON + _calls_flags() + ["-c", os.path.join(CSRC, CALLS_SOURCE), "-o", calls])
+    try:
+        flags = _calls_flags()
+    except ImportError:
+        flags = None
+        sys.stderr.write("PyTorch is not there: the library is built alone, without the module that reads tensors\n")
     with ThreadPoolExecutor(max_workers=4) as ex:
+        module = None if flags is None else ex.submit(_run, [HIPCC] + COMMON + flags + ["-c", os.path.join(CSRC, CALLS_SOURCE), "-o", calls])
         list(ex.map(_run, cmds))
-    _run([HIPCC, "-shared", "-fPIC"] + DEVICE + objs + ["-o", LIB, "-lpthread"])
-    link_calls(calls)
+        _run([HIPCC, "-shared", "-fPIC"] + DEVICE + objs + ["-o", LIB, "-lpthread"])
+        if module is not None:
+            module.result()
+            link_calls(calls)
     if verbose:
-        print("built", LIB, CALLS)
+        print("built", LIB, *([] if module is None else [CALLS]))
     return LIB
 
 

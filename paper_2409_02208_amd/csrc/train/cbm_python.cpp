@@ -2,6 +2,7 @@
 // time is the host's: with tensors read in Python and arguments converted by ctypes, cbm_layer_norm of 1024 x 64 took
 // 7.1 us a call, here it takes 3.8 to 4.1, as long as filling a tensor of one float.
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/version.h>
 
 #include <algorithm>
 #include <cstdint>
@@ -229,4 +230,8 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nul
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__calls() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__calls() {
+    PyObject* m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "torch_version", TORCH_VERSION) < 0) Py_CLEAR(m);  // whose layouts of tensors it reads
+    return m;
+}
