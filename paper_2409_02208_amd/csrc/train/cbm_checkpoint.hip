@@ -48,7 +48,7 @@ __device__ __forceinline__ void load_row_bytes(int (&q)[V], const int8_t* row, c
 }
 
 // Save.  LANES lanes a row (and a share of its columns: blockIdx.y), V columns a lane, of R rows; of R places along the row where a wave has it (R = 2).  A block of 32 columns is 32 / V lanes, which find its largest value by DPP; nothing
-// else is shared.  Bound by memory: 19717 x 500 fp32 11 to 13 us for 49.6 MB, of which the caches hold some (4 TB/s; waves waiting for 64 % of their cycles).
+// else is shared.  Bound by the latency of a lane's few loads: 19717 x 500 fp32 11 to 13 us for 49.6 MB (4 TB/s; waves waiting for 64 % of their cycles; reading and writing as much, and nothing else, 8).
 template <class T, int LANES, int R>
 __global__ __launch_bounds__(256) void cbm_checkpoint_save_kernel(int64_t n, int k, const T* __restrict__ X, int64_t ldx, int8_t* __restrict__ Q, int64_t ldq,
                                                                   uint8_t* __restrict__ E, int64_t lde) {
@@ -108,7 +108,8 @@ __global__ __launch_bounds__(256) void cbm_checkpoint_save_kernel(int64_t n, int
 }
 
 // Restore, and the backward pass of a ReLU (GATED: dx = q > 0 ? dy : 0), in the shape of saving.  Bound by memory: 19717 x 500 restored to fp32 8.6 to 10 us for 49.6 MB (5 TB/s);
-// gated, 235868 x 128 bf16 32 us for 152 MB (4.7 TB/s; waves waiting for 82 % of their cycles).
+// gated, 235868 x 128 bf16 32 us for 152 MB (4.7 TB/s; waves waiting for 82 % of their cycles: a piece of each stream a lane).  Reading and writing as much, and nothing else: 8 and 21, some of it out of the
+// memory-side cache.
 template <class T, int LANES, int R, bool GATED>
 __global__ __launch_bounds__(256) void cbm_checkpoint_load_kernel(int64_t n, int k, const int8_t* __restrict__ Q, int64_t ldq, const uint8_t* __restrict__ E, int64_t lde, const T* dY,
                                                                   int64_t lddy, T* out, int64_t ldo, bool far) {
@@ -153,9 +154,9 @@ __global__ __launch_bounds__(256) void cbm_checkpoint_load_kernel(int64_t n, int
 // in an order of their own (tile t has columns MT i + t of Q, and NT i + t of dY).  x~ is a bf16 value; dY is split into one (bf16), two (fp16) or three (fp32) bf16 values that add
 // up to it, so the products are exact and the sums fp32.  The waves of a workgroup and the workgroups of a tile share the rows; a workgroup adds its waves' sums in LDS, in order.
 // Narrow matrices take narrow tiles, of which a compute unit holds two workgroups (524288 x 32, 32 columns of bf16 45 us with wide tiles, 20 with narrow ones).
-// The next step's loads are under way while a step is multiplied; two steps ahead cost registers and gained nothing (279 us, 292).  2097152 x 128, 128 columns of fp32: 283 us for
-// 1.35 GB (4.8 TB/s) and 206 GFLOP of parts (730 TFLOP/s, the matrix cores busy for 40 % of the cycles): bound by memory, with the vector instructions
-// that split dY and widen Q next to it.  132534 x 100, 47 columns: 16 us, of which 5.5 are there whatever the rows (the launch, first loads, sums in LDS).
+// The next step's loads are under way while a step is multiplied; two steps ahead cost registers and gained nothing (279 us, 292).  2097152 x 128, 128 columns of fp32: 275 us for
+// 1.35 GB (4.9 TB/s; reading alone takes 209) and 206 GFLOP of parts (750 TFLOP/s, the matrix cores busy for 40 % of the cycles): waves wait for a quarter of their cycles only, so it is bound by the vector
+// instructions that split dY and widen Q between the matrix instructions.  Several tiles do both again for each: 300000 x 300, 100 columns 112 us, reading alone 33.  132534 x 100, 47 columns: 16 us, of which 5.5 are there whatever the rows (the launch, first loads, sums in LDS).
 constexpr int GRAD_WAVES = 8, GRAD_ROWS = 16;
 int grad_mt(int32_t k) { return k <= 32 ? 1 : k <= 64 ? 2 : 4; }
 int grad_nt(int32_t c) { return c <= 32 ? 1 : 2; }

@@ -95,8 +95,8 @@ __device__ __forceinline__ void store_columns(float* out, const float (&x)[V], c
 // Forward.  LANES lanes have a row, each R pieces of V columns: as few lanes as hold a row in up to two pieces, so that a wave's reductions serve several rows, and a workgroup
 // once a wave would need more than two.  The grid is what the compute units hold at once, and workgroups walk on over the rows, so gamma and beta are loaded once a workgroup
 // (a workgroup for every few rows: 2097152 x 128 fp32 570 us for 454), in pieces of 16 bytes (value by value 16384 x 4096 bf16 took 68 us, so 54).  A row of one piece or two has as many
-// lanes (1218193 x 8 bf16 9.1 us, with eight lanes a row 19).  Bound by memory: 2097152 x 128 fp32 440 us, 4.9 TB/s of 2.15 GB, waves waiting for 60 % of their cycles;
-// 1024 x 64 2.7 us, a launch.
+// lanes (1218193 x 8 bf16 9.1 us, with eight lanes a row 19).  Bound by memory: 2097152 x 128 fp32 440 us, 4.9 TB/s of 2.15 GB, waves waiting for 60 % of their cycles (a copy
+// alone 386); rows of a workgroup of 1,024 by its barriers too: 30000 x 4099 259 us, a copy 171.  1024 x 64 2.7 us, a launch.
 // Waves of a SIMD: two pieces of fp32 a lane fit eight, if only just (30000 x 1200 51 us, with seven 59).
 template <int V, int LANES, int R>
 constexpr int NORM_WAVES = V == 4 && LANES == 256 && R == 2 ? 8 : 1;
@@ -267,7 +267,7 @@ __device__ __forceinline__ void columns_alone(int64_t n, int k, int first, const
 // lanes' sums in LDS, in a fixed order, and writes one partial row of each to `parts` (workgroup, dg then db, column).  With few rows a second launch would take longer than
 // everything else: workgroups beyond the first `row_groups` then have dg and db of 16 columns each, and read all rows once more.
 // Bound by memory: 132534 x 100 fp32 34.5 us for 159 MB (4.6 TB/s, waves waiting for 80 % of their cycles) and 4 to 5 for the join; 16384 x 4096 bf16 78 us with the join for
-// 403 MB (5.1 TB/s).
+// 403 MB (5.2 TB/s).  Reading and writing as much, and nothing else: 29 and 72.
 template <class T, int V, int LANES, int R, int THREADS, bool WHOLE>
 __global__ __launch_bounds__(THREADS) void cbm_norm_back_kernel(int64_t n, int k, const T* __restrict__ dY, int64_t lddy, const T* __restrict__ X, int64_t ldx,
                                                                 const float* __restrict__ gamma, const float* __restrict__ mean, const float* __restrict__ rstd,

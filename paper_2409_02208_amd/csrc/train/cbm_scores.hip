@@ -252,9 +252,9 @@ __device__ __forceinline__ void write_alternatives(const Scores& a, int64_t row,
 
 // Short rows.  LANES lanes a row, each R pieces of V columns.  SELECT: more alternatives than the best one.  Without it four pieces of fp32 (two of 16 bits) a lane, so that many rows share a
 // wave's reductions (235868 x 112 33 us with one piece a lane, 20 with four); with it one piece as long as that is enough, since alternatives come out of sorted lanes.
-// Bound by memory in fp32: 235868 x 112 20 us for 108 MB (5.3 TB/s, some of it out of the caches), 8192 x 4000 23 us for 131 MB; by vector instructions in 16 bits (21 a value, and a row's
-// reductions: 30310 x 567 bf16 16 us for 35 MB) and with alternatives (65536 x 1000 fp32, top 8, 71 us for 262 MB; 110318 x 133 fp16, top 20, 57 us, 20 times the largest head).  19717 x 3
-// 2.8 us, a launch.
+// Bound by memory in fp32: 235868 x 112 23 us for 108 MB (4.7 TB/s), 8192 x 4000 23 us for 131 MB; by vector instructions in 16 bits (21 a value, and a row's
+// reductions: 30310 x 567 bf16 15 us for 35 MB, reading alone 6.4) and with alternatives (65536 x 1000 fp32, top 8, 71 us for 262 MB, reading alone 41; 110318 x 133 fp16, top 20, 58 us, 20 times the largest
+// head, reading alone 6).  19717 x 3 2.8 us, a launch.
 template <class T, int V, int LANES, int R, bool SELECT>
 __global__ __launch_bounds__(256) void cbm_scores_kernel(Scores a) {
     const int lane = threadIdx.x % LANES;
@@ -398,7 +398,8 @@ __device__ __forceinline__ void join_wave(float& m, float& s, float& t) {
 // have met, the maximum is known by then; the top-th largest of these 64 bounds the answer from below, the columns of the few lanes that hold as much are looked through
 // once more (out of L2, most likely), and what is found is ranked.  Where that is more than there is room for (equal scores, or orders that leave the largest
 // to a few lanes), all columns are gone through again in turns of one piece a lane, each of which adds to the list what exceeds it.
-// Bound by memory while rows are many: 4096 x 32000 bf16 with top 8 55 us for 262 MB (4.7 TB/s, waves waiting for 52 % of their cycles; 145 with a list kept sorted on the way).
+// Bound by memory while rows are many: 4096 x 32000 bf16 with top 8 55 us for 262 MB (4.8 TB/s, waves waiting for 52 % of their cycles: a turn's loads are not under way while the turn before
+// it is added up; reading alone 41; 145 with a list kept sorted on the way).
 // One row of 128,000 fp32 in 63 shares: 5.3 us, and 5.4 more for the join, each a launch and three dependent loads.
 template <class T, int V, int R, bool TOP, int THREADS>
 __global__ __launch_bounds__(THREADS) void cbm_scores_long_kernel(Scores a, int splits, int columns, char* __restrict__ parts) {
@@ -604,7 +605,7 @@ struct Slopes {
     int64_t lddz;
 };
 // Backward.  LANES lanes a row and a share of its columns (blockIdx.y), V columns a lane and turn; no lane needs another's, since the forward pass kept m and l.  Bound by memory:
-// 132534 x 47 fp32 11 us for 51.4 MB (4.7 TB/s, waves waiting for 66 % of their cycles), bf16 8.1 (10.4 with a row's last piece written value by value).
+// 132534 x 47 fp32 11 us for 51.4 MB (4.7 TB/s, waves waiting for 66 % of their cycles; a copy alone, some of it out of the memory-side cache, 7.5), bf16 8.1 (10.4 with a row's last piece written value by value).
 template <class T, int V, int LANES>
 __global__ __launch_bounds__(256) void cbm_scores_back_kernel(Slopes a, int turns, bool far) {
     const int lane = threadIdx.x % LANES, pieces = (a.c + V - 1) / V;
