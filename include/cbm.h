@@ -331,8 +331,8 @@ typedef enum { CBM_F32 = 0, CBM_BF16 = 1, CBM_F16 = 2 } cbm_dtype;
  * cbm_layer_norm -- y = (x - m) r gamma + beta along each row, m = mean(x), r = (mean((x - m)^2) + eps)^-1/2.
  *   X, Y         n x k, of `type`.
  *   gamma, beta  k fp32 values each; NULL stands for ones, zeros.
- *   eps          >= 0 and finite.  A row of equal values has y = beta; with eps = 0 r = infinity and a y of NaN, as the formula says (both exactly in
- *                rows of up to 2^16 columns, whose rounded sums leave whole units of the last place).
+ *   eps          >= 0 and finite.  A row of equal values has y = beta; with eps = 0 r = infinity and a y of NaN, as the formula says (both exactly for values
+ *                of 2^-50 to 2^70 in size in rows of up to 2^16 columns: squares of what rounded sums leave of them are neither lost nor too large).
  *   mean, rstd   receive m and r (n fp32 values each), which the backward pass reads; either may be NULL.
  */
 cbm_status cbm_layer_norm(int64_t n, int32_t k, int32_t type, const void* X, int64_t ldx, const float* gamma, const float* beta,

@@ -70,3 +70,33 @@ def test_the_mean_of_a_row_that_is_not_finite(env, k):  # noqa: F811
     # the variance passes the largest value: r = 0
     assert float(mean[3]) == pytest.approx(torch.finfo(torch.float32).min / k, rel=1e-6) and float(rstd[3]) == 0.0 and not bool(Y[3].any())
     assert bool(Y[4].isfinite().all())
+
+
+@pytest.mark.parametrize("k", [3, 7, 100, 1000, 3001, 16383, 65535])
+def test_equal_values_of_any_size_that_the_header_names(env, k):  # noqa: F811
+    torch, cbm = env
+    X = (torch.tensor([1.1, -1.9, 4 / 3], device="cuda")[:, None] * torch.tensor([2.0 ** -50, 2.0 ** -30, 1.0, 2.0 ** 40, 2.0 ** 69], device="cuda")).reshape(-1, 1).expand(15, k).contiguous()
+    Y, mean, rstd = torch.empty_like(X), torch.empty(15, device="cuda"), torch.empty(15, device="cuda")
+    cbm.cbm_layer_norm(X, None, None, 1e-5, Y, mean, rstd)
+    assert not bool(Y.any()) and torch.equal(mean, X[:, 0])
+    cbm.cbm_layer_norm(X, None, None, 0.0, Y, None, rstd)
+    assert bool(Y.isnan().all()) and bool(rstd.isinf().all())
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("k", [2, 3, 5, 8, 9, 17, 33, 64, 100, 129, 257, 300, 500, 512])
+def test_a_corrected_row_leaves_the_others_their_bits(env, name, k):  # noqa: F811
+    """Rows that share a wave with one whose mean is corrected come out as they do without it."""
+    torch, cbm = env
+    rng = np.random.default_rng(k)
+    x = rng.standard_normal((200, k)) * 3 + 0.7
+    X, _ = _matrix(torch, x, name, 0)
+    x[::9] = 1000.1 + rng.standard_normal((23, k))
+    other, _ = _matrix(torch, x, name, 0)
+    got = []
+    for t in (X, other):
+        Y, mean, rstd = torch.empty_like(t), torch.empty(200, device="cuda"), torch.empty(200, device="cuda")
+        cbm.cbm_layer_norm(t, None, None, 1e-5, Y, mean, rstd)
+        got.append((Y, mean, rstd))
+    rest = torch.arange(200, device="cuda") % 9 != 0
+    assert all(torch.equal(a[rest], b[rest]) for a, b in zip(*got))
