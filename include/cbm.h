@@ -403,6 +403,67 @@ cbm_status cbm_log_probs_backward(int64_t n, int32_t c, int32_t type, const void
                                   const float* stats, const float* entropy, const float* dlogp, const float* dentropy, void* dZ,
                                   int64_t lddz, void* hip_stream);
 
+/*
+ * cbm_gated_linear -- H = a(X Wg) o (X Wu), the gated layer (o: value by value), both projections, the activation and the product in one call:
+ *   X            n x k, Wg and Wu k x m, H n x m, of `type`, any leading dimension.
+ *   activation   a(g) = g / (1 + exp(-g)) (CBM_SILU), g Phi(g) with the normal distribution's Phi (CBM_GELU), max(g, 0) (CBM_RELU).
+ *   G, U         receive X Wg and X Wu (n x m, of `type`), which the backward pass reads; either may be NULL.  H is made of the sums before they are rounded.
+ *   workspace    cbm_gated_linear_workspace_bytes(n, k, m, type) bytes (may be 0).
+ *
+ * cbm_gated_linear_backward -- with dU = dH o a(G) and dG = dH o U o a'(G) (a'(0) = 0 for CBM_RELU), each rounded to `type`:
+ *   dX = dG Wg^T + dU Wu^T (n x k),  dWg = X^T dG,  dWu = X^T dU (k x m), of `type`; each may be NULL, not all three.  dWg and dWu are zeros for n = 0.
+ *   workspace    cbm_gated_linear_backward_workspace_bytes(n, k, m, type) bytes.
+ *
+ * Products of 16-bit types are exact, those of fp32 are made of three bf16 parts of each value (left out is at most 2^-24 of a term; parts below 2^-126 are taken for zero); sums
+ * are fp32.  In fp32, a value that is not finite, or from 2^127 on, makes NaN of every sum that it is part of.
+ */
+typedef enum { CBM_SILU = 0, CBM_GELU = 1, CBM_RELU = 2 } cbm_activation;
+cbm_status cbm_gated_linear(int64_t n, int32_t k, int32_t m, int32_t type, int32_t activation, const void* X, int64_t ldx, const void* Wg, int64_t ldwg,
+                            const void* Wu, int64_t ldwu, void* H, int64_t ldh, void* G, int64_t ldg, void* U, int64_t ldu, void* workspace,
+                            size_t workspace_bytes, void* hip_stream);
+size_t cbm_gated_linear_workspace_bytes(int64_t n, int32_t k, int32_t m, int32_t type);
+cbm_status cbm_gated_linear_backward(int64_t n, int32_t k, int32_t m, int32_t type, int32_t activation, const void* dH, int64_t lddh, const void* X,
+                                     int64_t ldx, const void* Wg, int64_t ldwg, const void* Wu, int64_t ldwu, const void* G, int64_t ldg, const void* U,
+                                     int64_t ldu, void* dX, int64_t lddx, void* dWg, int64_t lddwg, void* dWu, int64_t lddwu, void* workspace,
+                                     size_t workspace_bytes, void* hip_stream);
+size_t cbm_gated_linear_backward_workspace_bytes(int64_t n, int32_t k, int32_t m, int32_t type);
+
+/*
+ * cbm_linear_log_probs -- cbm_log_probs of the scores Z = X W of many classes, without Z in memory: along each row z of it, with m = max z and
+ * l = log sum exp(z - m), log p = z - m - l.
+ *   X            n x d, W d x c, of `type`.  Products and sums as for cbm_gated_linear; Z is not rounded.
+ *   labels, label_bits, logp, stats   as for cbm_log_probs (log p[label], 0 without a label; m and l); logp and stats may be NULL, labels where logp is.
+ *   workspace    cbm_linear_log_probs_workspace_bytes(n, d, c, type) bytes.
+ * A row with a score of NaN or +infinity has NaN for all of it (0 without a label).
+ *
+ * cbm_linear_log_probs_backward -- with dZ = dlogp (1[label] - p), rounded to `type` (fp16: at a size that fits the largest |dlogp|), and nothing for rows without a label,
+ *   dX = dZ W^T (n x d),  dW = X^T dZ (d x c; zeros for n = 0), of `type`; either may be NULL.  Values of X must be finite in rows without a label, too.
+ *   The scores are made again from X and W, a piece of the classes at a time, with m and l from `stats`.
+ *   workspace    cbm_linear_log_probs_backward_workspace_bytes(n, d, c, type) bytes: dZ of a piece (512 MiB or 1,024 classes), and sums.
+ */
+cbm_status cbm_linear_log_probs(int64_t n, int32_t d, int32_t c, int32_t type, const void* X, int64_t ldx, const void* W, int64_t ldw, const void* labels,
+                                int32_t label_bits, float* logp, float* stats, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t cbm_linear_log_probs_workspace_bytes(int64_t n, int32_t d, int32_t c, int32_t type);
+cbm_status cbm_linear_log_probs_backward(int64_t n, int32_t d, int32_t c, int32_t type, const void* X, int64_t ldx, const void* W, int64_t ldw,
+                                         const void* labels, int32_t label_bits, const float* stats, const float* dlogp, void* dX, int64_t lddx, void* dW,
+                                         int64_t lddw, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t cbm_linear_log_probs_backward_workspace_bytes(int64_t n, int32_t d, int32_t c, int32_t type);
+
+/*
+ * cbm_orthogonalise -- the update that a weights' gradient X (m x n, of `type`) stands for where all its directions are to count alike: with
+ * Z = X / (|X| + eps), |X| the root of the sum of squares, and `steps` times
+ *   A = Z Z^T,  Z <- a Z + (b A + c A^2) Z        (of Z^T where m > n, which is the same),
+ * Y = scale Z (of `type`).  Five steps with the usual coefficients bring singular values from 1 / 500 of |X| up to between 0.7 and 1.2.
+ *   steps          0 to 100.  coefficients: a, b and c, on the host; NULL stands for 3.4445, -4.7750, 2.0315.
+ *   eps            >= 0 and finite; a matrix of zeros stays one with eps > 0, and is NaN with eps = 0.
+ *   Y              may be X itself with ldy = ldx.
+ *   workspace      cbm_orthogonalise_workspace_bytes(m, n, type) bytes.
+ * m and n up to 65,536.  Everything between X and Y is held in 32 bits.  A value that is not finite makes NaN of all of Y.
+ */
+cbm_status cbm_orthogonalise(int32_t m, int32_t n, int32_t type, const void* X, int64_t ldx, int32_t steps, const float* coefficients, float eps, float scale,
+                             void* Y, int64_t ldy, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t cbm_orthogonalise_workspace_bytes(int32_t m, int32_t n, int32_t type);
+
 /* Counters of the built format (Properties 1 and 2, Lemma 2.2). */
 cbm_status cbm_stats(const cbm_handle* h, cbm_stats_t* out);
 

@@ -108,3 +108,53 @@ def log_probs_backward(z, labels, stats, entropy, dlogp, dentropy):
     hot[np.arange(n), np.where(given, labels, 0)] = 1.0
     slope = np.where(logs == -np.inf, 0.0, p * (np.where(logs == -np.inf, 0.0, logs) + np.asarray(entropy, dtype=np.float64)[:, None]))
     return a * (hot - p) - np.asarray(dentropy, dtype=np.float64)[:, None] * slope
+
+
+def activation(name, g):
+    """(a(g), a'(g))."""
+    from scipy.special import erfc, expit
+
+    g = np.asarray(g, dtype=np.float64)
+    if name == "relu":
+        return np.where(g <= 0, 0.0, g), (g > 0).astype(np.float64)
+    with np.errstate(over="ignore", invalid="ignore"):
+        if name == "silu":
+            s = expit(g)
+            return g * s, s * (1 + g * expit(-g))
+        below = 0.5 * erfc(-g / np.sqrt(2.0))
+        return g * below, below + g * np.exp(-0.5 * g * g) / np.sqrt(2 * np.pi)
+
+
+def gated_linear(x, wg, wu, name):
+    """(h, g, u)."""
+    x, wg, wu = (np.asarray(a, dtype=np.float64) for a in (x, wg, wu))
+    g, u = x @ wg, x @ wu
+    return activation(name, g)[0] * u, g, u
+
+
+def gated_linear_backward(dh, x, wg, wu, g, u, name):
+    """(dx, dwg, dwu), and dg and du that they are made of."""
+    dh, x, wg, wu, g, u = (np.asarray(a, dtype=np.float64) for a in (dh, x, wg, wu, g, u))
+    value, slope = activation(name, g)
+    du, dg = dh * value, dh * u * slope
+    return dg @ wg.T + du @ wu.T, x.T @ dg, x.T @ du, dg, du
+
+
+def linear_log_probs_backward(x, w, labels, stats, dlogp):
+    """(dx, dw), and dz that they are made of."""
+    x, w = np.asarray(x, dtype=np.float64), np.asarray(w, dtype=np.float64)
+    zero = np.zeros(len(x))
+    dz = log_probs_backward(x @ w, labels, stats, zero, np.where((np.asarray(labels) >= 0) & (np.asarray(labels) < w.shape[1]), dlogp, 0.0), zero)
+    return dz @ w.T, x.T @ dz, dz
+
+
+def orthogonalise(x, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, scale=1.0):
+    z = np.asarray(x, dtype=np.float64)
+    a, b, c = coefficients
+    with np.errstate(divide="ignore", invalid="ignore"):
+        z = z / (np.sqrt((z * z).sum()) + eps)
+    for _ in range(steps):
+        gram = z @ z.T if z.shape[0] <= z.shape[1] else z.T @ z
+        p = a * np.eye(len(gram)) + b * gram + c * gram @ gram
+        z = p @ z if z.shape[0] <= z.shape[1] else z @ p
+    return scale * z

@@ -1,5 +1,5 @@
 """Binding of libcbm.so: same names as the C ABI (include/cbm.h), argument marshalling
-only, by ctypes, or by the module _calls for the operators between the products.
+only, by ctypes, or by the module _calls for the operators of a training step.
 PyTorch tensors supply device memory and the stream; every step of the product runs in the library's HIP kernels.  There is no fallback:
 a missing library raises."""
 from __future__ import annotations
@@ -26,6 +26,9 @@ EXPORTS = [
     "cbm_checkpoint_save", "cbm_checkpoint_restore", "cbm_checkpoint_relu_backward",
     "cbm_checkpoint_weight_grad", "cbm_checkpoint_workspace_bytes",
     "cbm_log_probs", "cbm_log_probs_workspace_bytes", "cbm_log_probs_backward",
+    "cbm_gated_linear", "cbm_gated_linear_workspace_bytes", "cbm_gated_linear_backward", "cbm_gated_linear_backward_workspace_bytes",
+    "cbm_linear_log_probs", "cbm_linear_log_probs_workspace_bytes", "cbm_linear_log_probs_backward", "cbm_linear_log_probs_backward_workspace_bytes",
+    "cbm_orthogonalise", "cbm_orthogonalise_workspace_bytes",
     "cbm_profile_enable", "cbm_profile_read", "cbm_free", "cbm_status_string", "cbm_last_error_detail",
 ]
 
@@ -103,6 +106,16 @@ def _lib():
         lib.cbm_log_probs_workspace_bytes.argtypes = [i64, i32, i32]
         lib.cbm_log_probs_workspace_bytes.restype = C.c_size_t
         lib.cbm_log_probs_backward.argtypes = [i64, i32, i32, vp, i64, vp, i32, f32p, f32p, f32p, f32p, vp, i64, vp]
+        lib.cbm_gated_linear.argtypes = [i64, i32, i32, i32, i32] + [vp, i64] * 6 + [vp, C.c_size_t, vp]
+        lib.cbm_gated_linear_backward.argtypes = [i64, i32, i32, i32, i32] + [vp, i64] * 9 + [vp, C.c_size_t, vp]
+        lib.cbm_linear_log_probs.argtypes = [i64, i32, i32, i32, vp, i64, vp, i64, vp, i32, f32p, f32p, vp, C.c_size_t, vp]
+        lib.cbm_linear_log_probs_backward.argtypes = [i64, i32, i32, i32, vp, i64, vp, i64, vp, i32, f32p, f32p, vp, i64, vp, i64, vp, C.c_size_t, vp]
+        lib.cbm_orthogonalise.argtypes = [i32, i32, i32, vp, i64, i32, vp, C.c_float, C.c_float, vp, i64, vp, C.c_size_t, vp]
+        for name in ("cbm_gated_linear", "cbm_gated_linear_backward", "cbm_linear_log_probs", "cbm_linear_log_probs_backward"):
+            getattr(lib, name + "_workspace_bytes").argtypes = [i64, i32, i32, i32]
+            getattr(lib, name + "_workspace_bytes").restype = C.c_size_t
+        lib.cbm_orthogonalise_workspace_bytes.argtypes = [i32, i32, i32]
+        lib.cbm_orthogonalise_workspace_bytes.restype = C.c_size_t
         lib.cbm_stats.argtypes = [vp, C.POINTER(cbm_stats_t)]
         lib.cbm_get_tree.argtypes = [vp, vp, vp, vp, vp]
         lib.cbm_decompress.argtypes = [vp, vp, vp]
@@ -356,6 +369,80 @@ def cbm_log_probs_backward(Z, labels, stats, entropy, dlogp, dentropy, dZ, strea
     if status:
         raise CbmError(status, "cbm_log_probs_backward")
     return dZ
+
+
+def _type(dtype) -> int:
+    """The C ABI's number for one of the three types of a matrix."""
+    try:
+        return {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}[str(dtype)]
+    except KeyError:
+        raise ValueError(f"{dtype} is not one of float32, bfloat16, float16") from None
+
+
+ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
+
+
+def _activation(name) -> int:
+    try:
+        return ACTIVATIONS[name]
+    except (KeyError, TypeError):
+        raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}") from None
+
+
+def cbm_gated_linear_workspace_bytes(n: int, k: int, m: int, dtype) -> int:
+    return int((_LIB or _lib()).cbm_gated_linear_workspace_bytes(n, k, m, _type(dtype)))
+
+
+def cbm_gated_linear(X, Wg, Wu, H, G=None, U=None, activation: str = "silu", workspace=None, stream=None):
+    status = (_CALLS or _calls()).gated_linear(X, Wg, Wu, H, G, U, _activation(activation), workspace, _current_stream() if stream is None else _stream_ptr(stream))
+    if status:
+        raise CbmError(status, "cbm_gated_linear")
+    return H
+
+
+def cbm_gated_linear_backward_workspace_bytes(n: int, k: int, m: int, dtype) -> int:
+    return int((_LIB or _lib()).cbm_gated_linear_backward_workspace_bytes(n, k, m, _type(dtype)))
+
+
+def cbm_gated_linear_backward(dH, X, Wg, Wu, G, U, dX, dWg, dWu, activation: str = "silu", workspace=None, stream=None):
+    status = (_CALLS or _calls()).gated_linear_backward(dH, X, Wg, Wu, G, U, dX, dWg, dWu, _activation(activation), workspace, _current_stream() if stream is None else _stream_ptr(stream))
+    if status:
+        raise CbmError(status, "cbm_gated_linear_backward")
+    return dX
+
+
+def cbm_linear_log_probs_workspace_bytes(n: int, d: int, c: int, dtype) -> int:
+    return int((_LIB or _lib()).cbm_linear_log_probs_workspace_bytes(n, d, c, _type(dtype)))
+
+
+def cbm_linear_log_probs(X, W, labels, logp, stats=None, workspace=None, stream=None):
+    status = (_CALLS or _calls()).linear_log_probs(X, W, labels, logp, stats, workspace, _current_stream() if stream is None else _stream_ptr(stream))
+    if status:
+        raise CbmError(status, "cbm_linear_log_probs")
+    return logp
+
+
+def cbm_linear_log_probs_backward_workspace_bytes(n: int, d: int, c: int, dtype) -> int:
+    return int((_LIB or _lib()).cbm_linear_log_probs_backward_workspace_bytes(n, d, c, _type(dtype)))
+
+
+def cbm_linear_log_probs_backward(X, W, labels, stats, dlogp, dX, dW, workspace=None, stream=None):
+    status = (_CALLS or _calls()).linear_log_probs_backward(X, W, labels, stats, dlogp, dX, dW, workspace, _current_stream() if stream is None else _stream_ptr(stream))
+    if status:
+        raise CbmError(status, "cbm_linear_log_probs_backward")
+    return dX
+
+
+def cbm_orthogonalise_workspace_bytes(m: int, n: int, dtype) -> int:
+    return int((_LIB or _lib()).cbm_orthogonalise_workspace_bytes(m, n, _type(dtype)))
+
+
+def cbm_orthogonalise(X, Y, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, scale: float = 1.0, workspace=None, stream=None):
+    a, b, c = coefficients
+    status = (_CALLS or _calls()).orthogonalise(X, Y, steps, a, b, c, eps, scale, workspace, _current_stream() if stream is None else _stream_ptr(stream))
+    if status:
+        raise CbmError(status, "cbm_orthogonalise")
+    return Y
 
 
 def cbm_stats(h: Handle) -> dict:

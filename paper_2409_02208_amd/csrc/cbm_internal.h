@@ -306,3 +306,25 @@ cbm_status cbm_launch_scores(int64_t n, int32_t c, int32_t type, const void* z, 
                              float* values, int32_t* columns, void* parts, void* stream);
 cbm_status cbm_launch_scores_backward(int64_t n, int32_t c, int32_t type, const void* z, int64_t ldz, const void* labels, int label_bits, const float* stats, const float* entropy,
                                       const float* dlogp, const float* dentropy, void* dz, int64_t lddz, void* stream);
+
+// gated layer (train/cbm_gated.hip); workspaces in bytes
+int64_t cbm_gated_workspace(int64_t n, int32_t k, int32_t m, int32_t type);
+cbm_status cbm_launch_gated(int64_t n, int32_t k, int32_t m, int32_t type, int32_t act, const void* X, int64_t ldx, const void* Wg, int64_t ldwg, const void* Wu, int64_t ldwu, void* H,
+                            int64_t ldh, void* G, int64_t ldg, void* U, int64_t ldu, void* workspace, void* stream);
+int64_t cbm_gated_back_workspace(int64_t n, int32_t k, int32_t m, int32_t type);
+cbm_status cbm_launch_gated_backward(int64_t n, int32_t k, int32_t m, int32_t type, int32_t act, const void* dH, int64_t lddh, const void* X, int64_t ldx, const void* Wg, int64_t ldwg,
+                                     const void* Wu, int64_t ldwu, const void* G, int64_t ldg, const void* U, int64_t ldu, void* dX, int64_t lddx, void* dWg, int64_t lddwg, void* dWu,
+                                     int64_t lddwu, void* workspace, void* stream);
+
+// log probabilities of a layer's classes (train/cbm_classes.hip)
+int64_t cbm_classes_workspace(int64_t n, int32_t d, int32_t c, int32_t type);
+cbm_status cbm_launch_classes(int64_t n, int32_t d, int32_t c, int32_t type, const void* X, int64_t ldx, const void* W, int64_t ldw, const void* labels, int label_bits, float* logp, float* stats,
+                              void* workspace, void* stream);
+int64_t cbm_classes_back_workspace(int64_t n, int32_t d, int32_t c, int32_t type);
+cbm_status cbm_launch_classes_backward(int64_t n, int32_t d, int32_t c, int32_t type, const void* X, int64_t ldx, const void* W, int64_t ldw, const void* labels, int label_bits,
+                                       const float* stats, const float* dlogp, void* dX, int64_t lddx, void* dW, int64_t lddw, void* workspace, void* stream);
+
+// orthogonal update (train/cbm_orthogonal.hip)
+int64_t cbm_orthogonal_workspace(int32_t m, int32_t n, int32_t type);
+cbm_status cbm_launch_orthogonal(int32_t m, int32_t n, int32_t type, const void* X, int64_t ldx, int32_t steps, const float* abc, float eps, float scale, void* Y, int64_t ldy, void* workspace,
+                                 void* stream);

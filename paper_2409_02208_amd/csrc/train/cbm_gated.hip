@@ -1,0 +1,198 @@
+// Gated layer: H = act(X Wg) o (X Wu), and its backward pass.
+#include <algorithm>
+
+#include "cbm_internal.h"
+#include "cbm_products.h"
+#include "cbm_tiles.h"
+
+namespace {
+
+constexpr int BM = 128, BN = 128;
+
+template <int ACT>
+__device__ __forceinline__ float activated(float g) {
+    if constexpr (ACT == CBM_RELU) return g <= 0.0f ? 0.0f : g;  // (NaN stays)
+    if constexpr (ACT == CBM_SILU) return g / (1.0f + __expf(-g));
+    return 0.5f * g * erfcf(g * -0.70710678f);
+}
+// the activation and its slope
+template <int ACT>
+__device__ __forceinline__ void activated(float g, float& value, float& slope) {
+    if constexpr (ACT == CBM_RELU) {
+        value = activated<ACT>(g);
+        slope = g > 0.0f ? 1.0f : 0.0f;
+    } else if constexpr (ACT == CBM_SILU) {
+        const float s = 1.0f / (1.0f + __expf(-g));
+        value = g * s;
+        slope = s * fmaf(g, 1.0f - s, 1.0f);
+    } else {
+        const float below = 0.5f * erfcf(g * -0.70710678f);
+        value = g * below;
+        slope = fmaf(g, 0.39894228f * __expf(-0.5f * g * g), below);
+    }
+}
+template <class F>
+void with_activation(int32_t act, F&& f) {
+    using std::integral_constant;
+    if (act == CBM_SILU) f(integral_constant<int, CBM_SILU>{});
+    else if (act == CBM_GELU) f(integral_constant<int, CBM_GELU>{});
+    else f(integral_constant<int, CBM_RELU>{});
+}
+
+// Both projections in one product: a wave's tiles of 32 columns come from Wg and Wu in turn, so a lane has both sums of a value of H.
+template <class T, int ACT>
+__global__ __launch_bounds__(256, 2) void cbm_gated_kernel(CbmOperand<T> a, CbmOperand<T> b, int64_t chunks, T* __restrict__ H, int64_t ldh, T* __restrict__ G, int64_t ldg,
+                                                        T* __restrict__ U, int64_t ldu) {
+    typedef CbmTiles<T, BM, BN, 2, 2, ALONG_K, ACROSS_K, PAIR_ROWS> Tiles;
+    __shared__ uintx4 lds[Tiles::UNITS];
+    const CbmTilePlace at = cbm_tile_place((a.count + BM - 1) / BM, (b.count + BN / 2 - 1) / (BN / 2), 1);
+    if (!at.any) return;
+    Tiles t;
+    t.run(lds, a, b, at.m, at.n, 0, chunks);
+    const int l32 = threadIdx.x & 31, half = threadIdx.x >> 5 & 1;
+#pragma unroll
+    for (int i = 0; i < Tiles::TM; ++i) {
+        const int64_t r = at.m * BM + t.first_row() + 32 * i + l32;
+        if (r >= a.count) continue;
+#pragma unroll
+        for (int j = 0; j < Tiles::TN; j += 2)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int64_t c = at.n * (BN / 2) + t.first_column() / 2 + 16 * j + 8 * q + 4 * half;
+                float g[4], u[4], h[4];
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    g[v] = t.acc[i][j][4 * q + v];
+                    u[v] = t.acc[i][j + 1][4 * q + v];
+                    h[v] = activated<ACT>(g[v]) * u[v];
+                }
+                cbm_put4<T>(H + r * ldh, c, b.count, h);
+                if (G) cbm_put4<T>(G + r * ldg, c, b.count, g);
+                if (U) cbm_put4<T>(U + r * ldu, c, b.count, u);
+            }
+    }
+}
+
+// dG and dU side by side in `out`, from column 0 and column `at` on, rounded to the type (half a step each, as much as the gradients that are made of them are rounded by); zeros between.
+template <class T, int ACT>
+__global__ __launch_bounds__(256) void cbm_gated_slopes_kernel(int64_t n, int m, const T* __restrict__ dH, int64_t lddh, const T* __restrict__ G, int64_t ldg, const T* __restrict__ U,
+                                                            int64_t ldu, T* __restrict__ out, int64_t at) {
+    constexpr int V = 16 / (int)sizeof(T);
+    const int64_t pieces = at / V;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n * pieces; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / pieces;
+        const int c = (int)(i % pieces) * V;
+        float dh[V] = {}, g[V] = {}, u[V] = {}, dg[V], du[V];
+        if (c + V <= m) {
+            load_piece<V>(dh, dH + r * lddh + c);
+            load_piece<V>(g, G + r * ldg + c);
+            load_piece<V>(u, U + r * ldu + c);
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (c + j < m) {
+                    dh[j] = (float)dH[r * lddh + c + j];
+                    g[j] = (float)G[r * ldg + c + j];
+                    u[j] = (float)U[r * ldu + c + j];
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            float value, slope;
+            activated<ACT>(g[j], value, slope);
+            du[j] = c + j < m ? dh[j] * value : 0.0f;
+            dg[j] = c + j < m ? dh[j] * u[j] * slope : 0.0f;
+        }
+        store_piece<V>(out + r * 2 * at + c, dg);
+        store_piece<V>(out + r * 2 * at + at + c, du);
+    }
+}
+
+int64_t padded(int32_t m) { return ((int64_t)m + 63) / 64 * 64; }
+int64_t rounded16(int64_t bytes) { return (bytes + 15) / 16 * 16; }
+
+}  // namespace
+
+int64_t cbm_gated_workspace(int64_t, int32_t, int32_t, int32_t) { return 0; }
+
+cbm_status cbm_launch_gated(int64_t n, int32_t k, int32_t m, int32_t type, int32_t act, const void* X, int64_t ldx, const void* Wg, int64_t ldwg, const void* Wu, int64_t ldwu, void* H,
+                            int64_t ldh, void* G, int64_t ldg, void* U, int64_t ldu, void*, void* stream) {
+    if (n == 0) return CBM_OK;
+    cbm_with_type(type, [&](auto t) {
+        using T = decltype(t);
+        const CbmOperand<T> a{{(const T*)X, nullptr}, {ldx, 0}, n, k, 0}, b{{(const T*)Wg, (const T*)Wu}, {ldwg, ldwu}, m, k, 0};
+        const int64_t tiles = (n + BM - 1) / BM * (((int64_t)m + BN / 2 - 1) / (BN / 2)), chunk = 8 * CbmTileType<T>::KG;
+        with_activation(act, [&](auto which) {
+            cbm_gated_kernel<T, decltype(which)::value><<<(unsigned)((tiles + CBM_XCD - 1) / CBM_XCD * CBM_XCD), 256, 0, (hipStream_t)stream>>>(a, b, (k + chunk - 1) / chunk, (T*)H, ldh,
+                                                                                                                                      (T*)G, ldg, (T*)U, ldu);
+        });
+    });
+    return cbm_launched("gated layer launch");
+}
+
+int64_t cbm_gated_back_workspace(int64_t n, int32_t k, int32_t m, int32_t type) {
+    const int64_t at = padded(m), bytes = type == CBM_F32 ? 4 : 2;
+    int64_t parts = 0;
+    const int64_t dx = cbm_product_parts(n, k, 2 * at, type), dw = cbm_product_parts(k, 2 * at, n, type);
+    if (dx > 1) parts = dx * n * k;
+    if (dw > 1) parts = std::max(parts, dw * k * 2 * at);
+    return rounded16(n * 2 * at * bytes) + 4 * parts;
+}
+
+cbm_status cbm_launch_gated_backward(int64_t n, int32_t k, int32_t m, int32_t type, int32_t act, const void* dH, int64_t lddh, const void* X, int64_t ldx, const void* Wg, int64_t ldwg,
+                                     const void* Wu, int64_t ldwu, const void* G, int64_t ldg, const void* U, int64_t ldu, void* dX, int64_t lddx, void* dWg, int64_t lddwg, void* dWu,
+                                     int64_t lddwu, void* workspace, void* stream) {
+    const int64_t at = padded(m), bytes = type == CBM_F32 ? 4 : 2;
+    float* parts = (float*)((char*)workspace + rounded16(n * 2 * at * bytes));
+    if (n > 0)
+        cbm_with_type(type, [&](auto t) {
+            using T = decltype(t);
+            const int64_t blocks = (n * (at * (int64_t)sizeof(T) / 16) + 255) / 256;
+            with_activation(act, [&](auto which) {
+                cbm_gated_slopes_kernel<T, decltype(which)::value><<<(unsigned)std::min<int64_t>(blocks, 1 << 22), 256, 0, (hipStream_t)stream>>>(n, m, (const T*)dH, lddh, (const T*)G, ldg,
+                                                                                                                                      (const T*)U, ldu, (T*)workspace, at);
+            });
+        });
+    CbmProduct p{};
+    p.type = p.out.type = type;
+    p.parts = parts;
+    p.out.alpha = 1.0f;
+    p.A = workspace;
+    p.lda = 2 * at;
+    if (dX && n > 0) {
+        p.M = n;
+        p.N = k;
+        p.K = m;
+        p.at = at;
+        p.B[0] = Wg;
+        p.B[1] = Wu;
+        p.ldb[0] = ldwg;
+        p.ldb[1] = ldwu;
+        p.out.C[0] = dX;
+        p.out.ldc[0] = lddx;
+        p.out.columns = k;
+        p.parts = cbm_product_parts(n, k, 2 * at, type) > 1 ? parts : nullptr;
+        cbm_launch_tiles(p, stream);
+    }
+    if (dWg || dWu) {
+        p.M = k;
+        p.N = 2 * at;
+        p.K = n;
+        p.at = 0;
+        p.A = X;
+        p.lda = ldx;
+        p.a_across = p.b_across = true;
+        p.B[0] = workspace;
+        p.B[1] = nullptr;
+        p.ldb[0] = 2 * at;
+        p.out.C[0] = dWg;
+        p.out.C[1] = dWu;
+        p.out.ldc[0] = lddwg;
+        p.out.ldc[1] = lddwu;
+        p.out.columns = m;
+        p.out.at = at;
+        p.parts = cbm_product_parts(k, 2 * at, n, type) > 1 ? parts : nullptr;
+        cbm_launch_tiles(p, stream);
+    }
+    return cbm_launched("gated layer backward launch");
+}

@@ -5,6 +5,7 @@
 #include <torch/version.h>
 
 #include <algorithm>
+#include <array>
 #include <cstdint>
 #include <sstream>
 #include <string>
@@ -223,9 +224,102 @@ PyObject* log_probs_backward(PyObject*, PyObject* const* args, Py_ssize_t count)
     });
 }
 
+// A matrix that may be None, as large as rows x cols otherwise.
+Matrix optional(PyObject* o, const char* name, const Matrix& like, const char* why) {
+    if (o == Py_None) return {nullptr, like.cols, like.rows, like.cols, like.type};
+    const Matrix m = matrix(o, name);
+    alike(m, like, why);
+    return m;
+}
+int32_t whole(PyObject* o) {
+    const long v = PyLong_AsLong(o);
+    if (PyErr_Occurred()) throw python_error();
+    if (v < INT32_MIN || v > INT32_MAX) throw Refused{"a whole number is out of range"};
+    return (int32_t)v;
+}
+float number(PyObject* o) {
+    const double v = PyFloat_AsDouble(o);
+    if (PyErr_Occurred()) throw python_error();
+    return (float)v;
+}
+
+PyObject* gated_linear(PyObject*, PyObject* const* args, Py_ssize_t count) {  // X, Wg, Wu, H, G, U, activation, workspace, stream
+    return call<9>(args, count, [](PyObject* const* a, void* stream) {
+        const Matrix x = matrix(a[0], "X"), g = matrix(a[1], "Wg"), u = matrix(a[2], "Wu"), h = matrix(a[3], "H");
+        alike(g, u, "Wg and Wu must have the same shape and type");
+        if (x.cols != g.rows || x.type != g.type || h.type != x.type || h.rows != x.rows || h.cols != g.cols) throw Refused{"X, Wg and H must be n x k, k x m and n x m, of one type"};
+        const Matrix kg = optional(a[4], "G", h, "G and H must have the same shape and type"), ku = optional(a[5], "U", h, "U and H must have the same shape and type");
+        const int32_t act = whole(a[6]);
+        const Workspace w(a[7]);
+        return [=] {
+            return cbm_gated_linear(x.rows, columns(x.cols), columns(g.cols), x.type, act, x.p, x.ld, g.p, g.ld, u.p, u.ld, h.p, h.ld, kg.p, kg.ld, ku.p, ku.ld, w.p, w.bytes, stream);
+        };
+    });
+}
+
+PyObject* gated_linear_backward(PyObject*, PyObject* const* args, Py_ssize_t count) {  // dH, X, Wg, Wu, G, U, dX, dWg, dWu, activation, workspace, stream
+    return call<12>(args, count, [](PyObject* const* a, void* stream) {
+        const Matrix d = matrix(a[0], "dH"), x = matrix(a[1], "X"), wg = matrix(a[2], "Wg"), wu = matrix(a[3], "Wu"), g = matrix(a[4], "G"), u = matrix(a[5], "U");
+        alike(wg, wu, "Wg and Wu must have the same shape and type");
+        alike(d, g, "dH and G must have the same shape and type");
+        alike(d, u, "dH and U must have the same shape and type");
+        if (x.cols != wg.rows || x.type != wg.type || d.type != x.type || d.rows != x.rows || d.cols != wg.cols) throw Refused{"X, Wg and dH must be n x k, k x m and n x m, of one type"};
+        const Matrix dx = optional(a[6], "dX", x, "X and dX must have the same shape and type"), dg = optional(a[7], "dWg", wg, "Wg and dWg must have the same shape and type"),
+                     du = optional(a[8], "dWu", wg, "Wu and dWu must have the same shape and type");
+        const int32_t act = whole(a[9]);
+        const Workspace w(a[10]);
+        return [=] {
+            return cbm_gated_linear_backward(x.rows, columns(x.cols), columns(wg.cols), x.type, act, d.p, d.ld, x.p, x.ld, wg.p, wg.ld, wu.p, wu.ld, g.p, g.ld, u.p, u.ld, dx.p, dx.ld,
+                                             dg.p, dg.ld, du.p, du.ld, w.p, w.bytes, stream);
+        };
+    });
+}
+
+PyObject* linear_log_probs(PyObject*, PyObject* const* args, Py_ssize_t count) {  // X, W, labels, logp, stats, workspace, stream
+    return call<7>(args, count, [](PyObject* const* a, void* stream) {
+        const Matrix x = matrix(a[0], "X"), w = matrix(a[1], "W");
+        if (x.cols != w.rows || x.type != w.type) throw Refused{"X and W must be n x d and d x c, of one type"};
+        const Labels labels(a[2], x.rows);
+        float *logp = floats(a[3], "logp", {x.rows}), *stats = floats(a[4], "stats", {x.rows, 2});
+        const Workspace room(a[5]);
+        return [=] {
+            return cbm_linear_log_probs(x.rows, columns(x.cols), columns(w.cols), x.type, x.p, x.ld, w.p, w.ld, labels.p, labels.bits, logp, stats, room.p, room.bytes, stream);
+        };
+    });
+}
+
+PyObject* linear_log_probs_backward(PyObject*, PyObject* const* args, Py_ssize_t count) {  // X, W, labels, stats, dlogp, dX, dW, workspace, stream
+    return call<9>(args, count, [](PyObject* const* a, void* stream) {
+        const Matrix x = matrix(a[0], "X"), w = matrix(a[1], "W");
+        if (x.cols != w.rows || x.type != w.type) throw Refused{"X and W must be n x d and d x c, of one type"};
+        const Labels labels(a[2], x.rows);
+        const float *stats = floats(a[3], "stats", {x.rows, 2}), *dlogp = floats(a[4], "dlogp", {x.rows});
+        const Matrix dx = optional(a[5], "dX", x, "X and dX must have the same shape and type"), dw = optional(a[6], "dW", w, "W and dW must have the same shape and type");
+        const Workspace room(a[7]);
+        return [=] {
+            return cbm_linear_log_probs_backward(x.rows, columns(x.cols), columns(w.cols), x.type, x.p, x.ld, w.p, w.ld, labels.p, labels.bits, stats, dlogp, dx.p, dx.ld, dw.p, dw.ld,
+                                                 room.p, room.bytes, stream);
+        };
+    });
+}
+
+PyObject* orthogonalise(PyObject*, PyObject* const* args, Py_ssize_t count) {  // X, Y, steps, a, b, c, eps, scale, workspace, stream
+    return call<10>(args, count, [](PyObject* const* a, void* stream) {
+        const Matrix x = matrix(a[0], "X"), y = matrix(a[1], "Y");
+        alike(x, y, "X and Y must have the same shape and type");
+        const int32_t steps = whole(a[2]);
+        const std::array<float, 3> abc{number(a[3]), number(a[4]), number(a[5])};
+        const float eps = number(a[6]), scale = number(a[7]);
+        const Workspace w(a[8]);
+        return [=] { return cbm_orthogonalise(columns(x.rows), columns(x.cols), x.type, x.p, x.ld, steps, abc.data(), eps, scale, y.p, y.ld, w.p, w.bytes, stream); };
+    });
+}
+
 #define CBM_METHOD(name) {#name, (PyCFunction)(void (*)())name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {CBM_METHOD(layer_norm), CBM_METHOD(layer_norm_backward), CBM_METHOD(checkpoint_save), CBM_METHOD(checkpoint_restore), CBM_METHOD(checkpoint_relu_backward),
-                         CBM_METHOD(checkpoint_weight_grad), CBM_METHOD(log_probs), CBM_METHOD(log_probs_backward), {nullptr, nullptr, 0, nullptr}};
+                         CBM_METHOD(checkpoint_weight_grad), CBM_METHOD(log_probs), CBM_METHOD(log_probs_backward),
+                         CBM_METHOD(gated_linear), CBM_METHOD(gated_linear_backward), CBM_METHOD(linear_log_probs), CBM_METHOD(linear_log_probs_backward), CBM_METHOD(orthogonalise),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
