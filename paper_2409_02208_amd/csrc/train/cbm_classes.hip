@@ -1,13 +1,12 @@
 // Log probabilities of labels straight from a layer's outputs and the classes' weights, Z = X W, without keeping Z, and the gradients of both.
 #include <algorithm>
 
+#include "cbm_aligned.h"
 #include "cbm_internal.h"
 #include "cbm_products.h"
-#include "cbm_tiles.h"
 
 namespace {
 
-constexpr int BM = 128, BN = 128, WN = 2;  // WN: waves along a tile's columns, each with a partial result of its own
 constexpr float LOG2E = 1.44269504f;
 
 // m and sum exp(z - m) of two sets of scores as one
@@ -16,55 +15,57 @@ struct Sums {
 };
 __device__ __forceinline__ Sums joined(Sums a, Sums b) {
     const float m = fmaxf(a.m, b.m), away = m == -INFINITY ? 0.0f : m;  // (NaN is in s)
-    return {m, a.s * exp2f((a.m - away) * LOG2E) + b.s * exp2f((b.m - away) * LOG2E)};
+    return {m, a.s * __builtin_amdgcn_exp2f((a.m - away) * LOG2E) + b.s * __builtin_amdgcn_exp2f((b.m - away) * LOG2E)};
 }
 
 __device__ __forceinline__ int64_t label_of(const void* labels, int bits, int64_t r) { return bits == 64 ? ((const int64_t*)labels)[r] : ((const int32_t*)labels)[r]; }
 
 // A wave's part of each of its rows: the largest score and the sum, and the label's score where it is among them.
-template <class T>
-__global__ __launch_bounds__(256, 2) void cbm_classes_kernel(CbmOperand<T> a, CbmOperand<T> b, int64_t chunks, const void* __restrict__ labels, int label_bits, Sums* __restrict__ parts,
+template <class Tiles, class T>
+__global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_classes_kernel(CbmOperand<T> a, CbmOperand<T> b, int64_t chunks, const void* __restrict__ labels, int label_bits, Sums* __restrict__ parts,
                                                           float* __restrict__ chosen) {
-    typedef CbmTiles<T, BM, BN, 2, WN, ALONG_K, ACROSS_K, SINGLE> Tiles;
+    constexpr int BM = Tiles::ROWS, BN = Tiles::COLUMNS, WN = Tiles::ACROSS;
     __shared__ uintx4 lds[Tiles::UNITS];
     const int64_t tiles_n = (b.count + BN - 1) / BN;
     const CbmTilePlace at = cbm_tile_place((a.count + BM - 1) / BM, tiles_n, 1);
     if (!at.any) return;
     Tiles t;
-    t.run(lds, a, b, at.m, at.n, 0, chunks);
+    t.run(lds, a, b, at.m, at.n, 0, (int)chunks);
     const int l32 = threadIdx.x & 31, half = threadIdx.x >> 5 & 1;
-    const int64_t c0 = at.n * BN + t.first_column() + 4 * half;  // the lane's first column
+    const int64_t c0 = (int64_t)at.n * BN + t.first_column() + 4 * half;  // the lane's first column
+    const int left = (int)min(b.count - c0, (int64_t)4096);                            // and columns from there on
 #pragma unroll
     for (int i = 0; i < Tiles::TM; ++i) {
-        const int64_t r = at.m * BM + t.first_row() + 32 * i + l32;
+        __builtin_amdgcn_sched_barrier(0);  // (32 rows at a time: registers)
+        const int64_t r = (int64_t)at.m * BM + t.first_row() + 32 * i + l32;
         int64_t given = labels && r < a.count ? label_of(labels, label_bits, r) : -1;
         if (given >= b.count) given = -1;
         const int label = (int)max(min(given - c0, (int64_t)4096), (int64_t)-1);
         Sums all{-INFINITY, 0.0f};
         float z = 0.0f;
-        if ((at.n + 1) * BN > b.count)
-#pragma unroll
-            for (int j = 0; j < Tiles::TN; ++j)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) t.acc[i][j][v] = c0 + 32 * j + 8 * (v / 4) + v % 4 < b.count ? t.acc[i][j][v] : -INFINITY;
+        int here = left;
+        asm("" : "+v"(here));  // (or a mask for each column stays in scalar registers)
+        auto score = [&](int j, int v) { return 32 * j + 8 * (v / 4) + v % 4 < here ? t.acc[i][j][v] : -INFINITY; };
 #pragma unroll
         for (int j = 0; j < Tiles::TN; ++j)
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
-                all.m = fmaxf(all.m, t.acc[i][j][v]);
+                all.m = fmaxf(all.m, score(j, v));
                 z = label == 32 * j + 8 * (v / 4) + v % 4 ? t.acc[i][j][v] : z;
             }
         const float away = all.m == -INFINITY ? 0.0f : all.m;
+        __builtin_amdgcn_sched_barrier(0);
+        asm("" : "+v"(here));
 #pragma unroll
         for (int j = 0; j < Tiles::TN; ++j)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) all.s += exp2f((t.acc[i][j][v] - away) * LOG2E);
+            for (int v = 0; v < 16; ++v) all.s += __builtin_amdgcn_exp2f((score(j, v) - away) * LOG2E);
         Sums low, high;  // the halves' sums, in the same order in both
         lane_pair<32>(all.m, [&](float x, float y) { low.m = x, high.m = y; return x; });
         lane_pair<32>(all.s, [&](float x, float y) { low.s = x, high.s = y; return x; });
         all = joined(low, high);
         if (r >= a.count) continue;
-        if (half == 0) parts[r * (tiles_n * WN) + at.n * WN + t.wave() / 2] = all;
+        if (half == 0) parts[r * (tiles_n * WN) + at.n * WN + t.across()] = all;
         if (label >= 0 && label < 32 * Tiles::TN && !(label & 4)) chosen[r] = z;
     }
 }
@@ -78,7 +79,7 @@ __global__ __launch_bounds__(256) void cbm_classes_join_kernel(int64_t n, int64_
     Sums all{-INFINITY, 0.0f};
     for (int64_t i = lane; i < count; i += 64) all = joined(all, parts[r * count + i]);
     const float m = lanes_all<64>(all.m, [](float a, float b) { return fmaxf(a, b); }), away = m == -INFINITY ? 0.0f : m;
-    const float s = lanes_sum<64>(all.s * exp2f((all.m - away) * LOG2E));
+    const float s = lanes_sum<64>(all.s * __builtin_amdgcn_exp2f((all.m - away) * LOG2E));
     if (lane) return;
     const bool bad = !(s < INFINITY);
     const float largest = bad ? NAN : m, l = bad ? NAN : logf(s);
@@ -108,41 +109,38 @@ __global__ __launch_bounds__(1024) void cbm_classes_scale_kernel(int64_t n, cons
 }
 
 // dZ of columns first .. first + b.count - 1, rounded to the type (half a step, as much as the gradients that are made of it are rounded by).
-template <class T>
-__global__ __launch_bounds__(256, 2) void cbm_classes_slopes_kernel(CbmOperand<T> a, CbmOperand<T> b, int64_t chunks, int64_t first, int64_t c, const void* __restrict__ labels, int label_bits,
+template <class Tiles, class T>
+__global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_classes_slopes_kernel(CbmOperand<T> a, CbmOperand<T> b, int64_t chunks, int64_t first, int64_t c, const void* __restrict__ labels, int label_bits,
                                                                  const float* __restrict__ stats, const float* __restrict__ dlogp, const float* __restrict__ scale, T* __restrict__ dZ,
                                                                  int64_t lddz) {
-    typedef CbmTiles<T, BM, BN, 2, WN, ALONG_K, ACROSS_K, SINGLE> Tiles;
+    constexpr int BM = Tiles::ROWS, BN = Tiles::COLUMNS, WN = Tiles::ACROSS;
     __shared__ uintx4 lds[Tiles::UNITS];
     const CbmTilePlace at = cbm_tile_place((a.count + BM - 1) / BM, (b.count + BN - 1) / BN, 1);
     if (!at.any) return;
     Tiles t;
-    t.run(lds, a, b, at.m, at.n, 0, chunks);
+    t.run(lds, a, b, at.m, at.n, 0, (int)chunks);
     const int l32 = threadIdx.x & 31, half = threadIdx.x >> 5 & 1;
 #pragma unroll
     for (int i = 0; i < Tiles::TM; ++i) {
-        const int64_t r = at.m * BM + t.first_row() + 32 * i + l32;
-        if (r >= a.count) continue;
-        int64_t label = label_of(labels, label_bits, r);
-        const float m = stats[2 * r], l = stats[2 * r + 1];
+        __builtin_amdgcn_sched_barrier(0);  // (32 rows at a time: registers)
+        const int64_t r = (int64_t)at.m * BM + t.first_row() + 32 * i + l32;
+        const int64_t at_r = min(r, a.count - 1), label = label_of(labels, label_bits, at_r);
+        const float m = stats[2 * at_r], l = stats[2 * at_r + 1];
         const bool none = label < 0 || label >= c || m == -INFINITY;
-        float up = dlogp[r];
+        float up = dlogp[at_r];
         if (scale) up *= scale[1];
-        label -= first;
+        const int mine = (int)max(min(label - first - ((int64_t)at.n * BN + t.first_column() + 4 * half), (int64_t)4096), (int64_t)-1);  // the label's place among the lane's columns
 #pragma unroll
         for (int j = 0; j < Tiles::TN; ++j)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int64_t col = at.n * BN + t.first_column() + 32 * j + 8 * q + 4 * half;
-                float v[4];
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const float p = exp2f(((t.acc[i][j][4 * q + w] - m) - l) * LOG2E);
-                    v[w] = none ? 0.0f : up * ((col + w == label ? 1.0f : 0.0f) - p);
-                }
-                cbm_put4<T>(dZ + r * lddz, col, b.count, v);
+            for (int v = 0; v < 16; ++v) {
+                const float p = __builtin_amdgcn_exp2f(((t.acc[i][j][v] - m) - l) * LOG2E);
+                t.acc[i][j][v] = none ? 0.0f : up * ((mine == 32 * j + 8 * (v / 4) + v % 4 ? 1.0f : 0.0f) - p);
             }
     }
+    t.pieces(lds, at.m, at.n, [&](int64_t r, int64_t col, float (&v)[4]) {
+        if (r < a.count) cbm_put4<T>(dZ + r * lddz, col, b.count, v);
+    });
 }
 
 int64_t rounded16(int64_t bytes) { return (bytes + 15) / 16 * 16; }
@@ -173,31 +171,42 @@ Room back_room(int64_t n, int32_t d, int32_t c, int32_t type) {
     return r;
 }
 
-template <class T>
-int64_t chunks_of(int64_t k) {
-    const int64_t chunk = 8 * CbmTileType<T>::KG;
-    return (k + chunk - 1) / chunk;
-}
-unsigned grid_of(int64_t n, int64_t c) {
-    const int64_t tiles = (n + BM - 1) / BM * ((c + BN - 1) / BN);
-    return (unsigned)((tiles + CBM_XCD - 1) / CBM_XCD * CBM_XCD);
+// f(tiles, grid) for a product n x d . d x c of scores
+template <class T, class F>
+void with_tiles(int64_t n, int64_t d, int64_t c, const CbmOperand<T>& a, const CbmOperand<T>& b, int32_t type, F&& f) {
+    auto run = [&](auto* tiles_type) {
+        typedef std::remove_pointer_t<decltype(tiles_type)> Tiles;
+        const int64_t tiles = (n + Tiles::ROWS - 1) / Tiles::ROWS * ((c + Tiles::COLUMNS - 1) / Tiles::COLUMNS);
+        f(tiles_type, (unsigned)((tiles + CBM_XCD - 1) / CBM_XCD * CBM_XCD), (d + Tiles::BK - 1) / Tiles::BK);
+    };
+    if constexpr (sizeof(T) == 2)
+        if (cbm_units(a.p[0], a.ld[0], d) && cbm_units(b.p[0], b.ld[0], c)) {
+            if (cbm_product_tile(n, c, d, type) == 256) run((CbmAlignedTiles<T, 256, 256, ALONG_K, ACROSS_K, SINGLE>*)nullptr);
+            else run((CbmAlignedTiles<T, 128, 128, ALONG_K, ACROSS_K, SINGLE>*)nullptr);
+            return;
+        }
+    run((CbmTiles<T, 128, 128, 2, 2, ALONG_K, ACROSS_K, SINGLE>*)nullptr);
 }
 
 }  // namespace
 
-int64_t cbm_classes_workspace(int64_t n, int32_t, int32_t c, int32_t) { return rounded16(n * (((int64_t)c + BN - 1) / BN) * WN * (int64_t)sizeof(Sums)) + 4 * n; }
+int64_t cbm_classes_workspace(int64_t n, int32_t, int32_t c, int32_t) { return rounded16(n * (((int64_t)c + 127) / 128 * 2) * (int64_t)sizeof(Sums)) + 4 * n; }
 
 cbm_status cbm_launch_classes(int64_t n, int32_t d, int32_t c, int32_t type, const void* X, int64_t ldx, const void* W, int64_t ldw, const void* labels, int label_bits, float* logp, float* stats,
                               void* workspace, void* stream_) {
     hipStream_t stream = (hipStream_t)stream_;
     if (n == 0) return CBM_OK;
-    const int64_t count = ((int64_t)c + BN - 1) / BN * WN;
+    int64_t count = 0;  // parts of a row: of the waves along a tile's columns
     Sums* parts = (Sums*)workspace;
-    float* chosen = (float*)((char*)workspace + rounded16(n * count * (int64_t)sizeof(Sums)));
+    float* chosen = (float*)((char*)workspace + rounded16(n * (((int64_t)c + 127) / 128 * 2) * (int64_t)sizeof(Sums)));
     cbm_with_type(type, [&](auto t) {
         using T = decltype(t);
         const CbmOperand<T> a{{(const T*)X, nullptr}, {ldx, 0}, n, d, 0}, b{{(const T*)W, nullptr}, {ldw, 0}, c, d, 0};
-        cbm_classes_kernel<T><<<grid_of(n, c), 256, 0, stream>>>(a, b, chunks_of<T>(d), logp ? labels : nullptr, label_bits, parts, chosen);
+        with_tiles<T>(n, d, c, a, b, type, [&](auto* tiles_type, unsigned grid, int64_t chunks) {
+            typedef std::remove_pointer_t<decltype(tiles_type)> Tiles;
+            count = ((int64_t)c + Tiles::COLUMNS - 1) / Tiles::COLUMNS * Tiles::ACROSS;
+            cbm_classes_kernel<Tiles, T><<<grid, 256, 0, stream>>>(a, b, chunks, logp ? labels : nullptr, label_bits, parts, chosen);
+        });
     });
     cbm_classes_join_kernel<<<(unsigned)((n + 3) / 4), 256, 0, stream>>>(n, c, count, labels, label_bits, parts, chosen, logp, stats);
     return cbm_launched("linear log probabilities launch");
@@ -220,7 +229,10 @@ cbm_status cbm_launch_classes_backward(int64_t n, int32_t d, int32_t c, int32_t 
             cbm_with_type(type, [&](auto t) {
                 using T = decltype(t);
                 const CbmOperand<T> a{{(const T*)X, nullptr}, {ldx, 0}, n, d, 0}, b{{(const T*)Wp, nullptr}, {ldw, 0}, width, d, 0};
-                cbm_classes_slopes_kernel<T><<<grid_of(n, width), 256, 0, stream>>>(a, b, chunks_of<T>(d), first, c, labels, label_bits, stats, dlogp, scale, (T*)workspace, piece);
+                with_tiles<T>(n, d, width, a, b, type, [&](auto* tiles_type, unsigned grid, int64_t chunks) {
+                    cbm_classes_slopes_kernel<std::remove_pointer_t<decltype(tiles_type)>, T><<<grid, 256, 0, stream>>>(a, b, chunks, first, c, labels, label_bits, stats, dlogp, scale, (T*)workspace,
+                                                                                                              piece);
+                });
             });
         CbmProduct p{};
         p.type = p.out.type = type;
@@ -254,7 +266,7 @@ cbm_status cbm_launch_classes_backward(int64_t n, int32_t d, int32_t c, int32_t 
             p.ldb[0] = piece;
             p.out.C[0] = (char*)dW + first * bytes;
             p.out.ldc[0] = lddw;
-            p.out.columns = width;
+            p.out.columns = (int32_t)width;
             p.out.sums = nullptr;
             p.parts = cbm_product_parts(d, width, n, type) > 1 ? parts : nullptr;
             cbm_launch_tiles(p, stream);

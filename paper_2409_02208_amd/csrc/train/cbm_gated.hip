@@ -1,13 +1,11 @@
 // Gated layer: H = act(X Wg) o (X Wu), and its backward pass.
 #include <algorithm>
 
+#include "cbm_aligned.h"
 #include "cbm_internal.h"
 #include "cbm_products.h"
-#include "cbm_tiles.h"
 
 namespace {
-
-constexpr int BM = 128, BN = 128;
 
 template <int ACT>
 __device__ __forceinline__ float activated(float g) {
@@ -40,37 +38,23 @@ void with_activation(int32_t act, F&& f) {
 }
 
 // Both projections in one product: a wave's tiles of 32 columns come from Wg and Wu in turn, so a lane has both sums of a value of H.
-template <class T, int ACT>
-__global__ __launch_bounds__(256, 2) void cbm_gated_kernel(CbmOperand<T> a, CbmOperand<T> b, int64_t chunks, T* __restrict__ H, int64_t ldh, T* __restrict__ G, int64_t ldg,
-                                                        T* __restrict__ U, int64_t ldu) {
-    typedef CbmTiles<T, BM, BN, 2, 2, ALONG_K, ACROSS_K, PAIR_ROWS> Tiles;
+template <class Tiles, class T, int ACT>
+__global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_gated_kernel(CbmOperand<T> a, CbmOperand<T> b, int64_t chunks, T* __restrict__ H, int64_t ldh, T* __restrict__ G, int64_t ldg,
+                                                                    T* __restrict__ U, int64_t ldu) {
     __shared__ uintx4 lds[Tiles::UNITS];
-    const CbmTilePlace at = cbm_tile_place((a.count + BM - 1) / BM, (b.count + BN / 2 - 1) / (BN / 2), 1);
+    const CbmTilePlace at = cbm_tile_place((a.count + Tiles::ROWS - 1) / Tiles::ROWS, (b.count + Tiles::COLUMNS / 2 - 1) / (Tiles::COLUMNS / 2), 1);
     if (!at.any) return;
     Tiles t;
-    t.run(lds, a, b, at.m, at.n, 0, chunks);
-    const int l32 = threadIdx.x & 31, half = threadIdx.x >> 5 & 1;
+    t.run(lds, a, b, at.m, at.n, 0, (int)chunks);
+    t.pairs(lds, at.m, at.n, [&](int64_t r, int64_t c, float (&g)[4], float (&u)[4]) {
+        if (r >= a.count) return;
+        float h[4];
 #pragma unroll
-    for (int i = 0; i < Tiles::TM; ++i) {
-        const int64_t r = at.m * BM + t.first_row() + 32 * i + l32;
-        if (r >= a.count) continue;
-#pragma unroll
-        for (int j = 0; j < Tiles::TN; j += 2)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int64_t c = at.n * (BN / 2) + t.first_column() / 2 + 16 * j + 8 * q + 4 * half;
-                float g[4], u[4], h[4];
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    g[v] = t.acc[i][j][4 * q + v];
-                    u[v] = t.acc[i][j + 1][4 * q + v];
-                    h[v] = activated<ACT>(g[v]) * u[v];
-                }
-                cbm_put4<T>(H + r * ldh, c, b.count, h);
-                if (G) cbm_put4<T>(G + r * ldg, c, b.count, g);
-                if (U) cbm_put4<T>(U + r * ldu, c, b.count, u);
-            }
-    }
+        for (int v = 0; v < 4; ++v) h[v] = activated<ACT>(g[v]) * u[v];
+        cbm_put4<T>(H + r * ldh, c, b.count, h);
+        if (G) cbm_put4<T>(G + r * ldg, c, b.count, g);
+        if (U) cbm_put4<T>(U + r * ldu, c, b.count, u);
+    });
 }
 
 // dG and dU side by side in `out`, from column 0 and column `at` on, rounded to the type (half a step each, as much as the gradients that are made of them are rounded by); zeros between.
@@ -121,11 +105,21 @@ cbm_status cbm_launch_gated(int64_t n, int32_t k, int32_t m, int32_t type, int32
     cbm_with_type(type, [&](auto t) {
         using T = decltype(t);
         const CbmOperand<T> a{{(const T*)X, nullptr}, {ldx, 0}, n, k, 0}, b{{(const T*)Wg, (const T*)Wu}, {ldwg, ldwu}, m, k, 0};
-        const int64_t tiles = (n + BM - 1) / BM * (((int64_t)m + BN / 2 - 1) / (BN / 2)), chunk = 8 * CbmTileType<T>::KG;
-        with_activation(act, [&](auto which) {
-            cbm_gated_kernel<T, decltype(which)::value><<<(unsigned)((tiles + CBM_XCD - 1) / CBM_XCD * CBM_XCD), 256, 0, (hipStream_t)stream>>>(a, b, (k + chunk - 1) / chunk, (T*)H, ldh,
-                                                                                                                                      (T*)G, ldg, (T*)U, ldu);
-        });
+        auto run = [&](auto* tiles_type) {
+            typedef std::remove_pointer_t<decltype(tiles_type)> Tiles;
+            const int64_t tiles = (n + Tiles::ROWS - 1) / Tiles::ROWS * (((int64_t)m + Tiles::COLUMNS / 2 - 1) / (Tiles::COLUMNS / 2));
+            with_activation(act, [&](auto which) {
+                cbm_gated_kernel<Tiles, T, decltype(which)::value><<<(unsigned)((tiles + CBM_XCD - 1) / CBM_XCD * CBM_XCD), 256, 0, (hipStream_t)stream>>>(
+                    a, b, (k + Tiles::BK - 1) / Tiles::BK, (T*)H, ldh, (T*)G, ldg, (T*)U, ldu);
+            });
+        };
+        if constexpr (sizeof(T) == 2)
+            if (cbm_units(a.p[0], ldx, k) && cbm_units(b.p[0], ldwg, m) && cbm_units(b.p[1], ldwu, m) && ldwg == ldwu) {
+                if (cbm_product_tile(n, 2 * (int64_t)m, k, type) == 256) run((CbmAlignedTiles<T, 256, 256, ALONG_K, ACROSS_K, PAIR_ROWS>*)nullptr);
+                else run((CbmAlignedTiles<T, 128, 128, ALONG_K, ACROSS_K, PAIR_ROWS>*)nullptr);
+                return;
+            }
+        run((CbmTiles<T, 128, 128, 2, 2, ALONG_K, ACROSS_K, PAIR_ROWS>*)nullptr);
     });
     return cbm_launched("gated layer launch");
 }
@@ -190,7 +184,7 @@ cbm_status cbm_launch_gated_backward(int64_t n, int32_t k, int32_t m, int32_t ty
         p.out.ldc[0] = lddwg;
         p.out.ldc[1] = lddwu;
         p.out.columns = m;
-        p.out.at = at;
+        p.out.at = (int32_t)at;
         p.parts = cbm_product_parts(k, 2 * at, n, type) > 1 ? parts : nullptr;
         cbm_launch_tiles(p, stream);
     }

@@ -86,7 +86,8 @@ cbm_status cbm_launch_orthogonal(int32_t m, int32_t n, int32_t type, const void*
             p.ldb[0] = across ? N : K;
             p.b_across = across;
             p.out.C[0] = c;
-            p.out.ldc[0] = p.out.columns = p.out.ldm = N;
+            p.out.ldc[0] = p.out.ldm = N;
+            p.out.columns = (int32_t)N;
             p.out.alpha = alpha;
             p.out.more = more;
             p.out.beta = beta;

@@ -10,8 +10,8 @@ struct CbmProductOut {
     int32_t type;        // cbm_dtype of what is written
     void* C[2];          // columns from `at` on belong to the second one's first (0: there is one)
     int64_t ldc[2];
-    int64_t columns;     // of each
-    int64_t at;
+    int32_t columns;     // of each
+    int32_t at;
     bool transposed;     // value (r, c) goes to C[c, r]
     float alpha, beta;
     const float* factor; // on the device; may be NULL
@@ -35,5 +35,7 @@ struct CbmProduct {
     float* parts;  // cbm_product_parts() M x N values, packed, where that is more than one
 };
 int64_t cbm_product_parts(int64_t M, int64_t N, int64_t K, int32_t type);
+// 256 or 128: the tiles that a product whose units go straight to LDS is made in
+int cbm_product_tile(int64_t M, int64_t N, int64_t K, int32_t type);
 void cbm_launch_tiles(const CbmProduct& p, void* stream);
 cbm_status cbm_launched(const char* what);  // the status of the launches since the last look

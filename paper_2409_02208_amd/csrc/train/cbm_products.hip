@@ -1,13 +1,12 @@
 // Products in tiles with a plain end: sums scaled, added to and rounded.  The gradients of the operators that are made of products, and the steps of the orthogonal update.
 #include <algorithm>
+#include <type_traits>
 
+#include "cbm_aligned.h"
 #include "cbm_internal.h"
 #include "cbm_products.h"
-#include "cbm_tiles.h"
 
 namespace {
-
-constexpr int BM = 128, BN = 128;
 
 template <class TO>
 __device__ __forceinline__ void finish(const CbmProductOut& o, int64_t M, int64_t N, int64_t r, int64_t c, float (&v)[4]) {
@@ -42,16 +41,14 @@ __device__ __forceinline__ void finish(const CbmProductOut& o, int64_t M, int64_
     }
 }
 
-template <class T, class TO, CbmTileOrder OA, CbmTileOrder OB, CbmTilePair PAIR>
-__global__ __launch_bounds__(256, 2) void cbm_product_kernel(CbmOperand<T> a, CbmOperand<T> b, int64_t chunks, int64_t splits, CbmProductOut o, float* __restrict__ parts) {
-    typedef CbmTiles<T, BM, BN, 2, 2, OA, OB, PAIR> Tiles;
+template <class Tiles, class T, class TO>
+__global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_product_kernel(CbmOperand<T> a, CbmOperand<T> b, int64_t chunks, int64_t splits, CbmProductOut o, float* __restrict__ parts) {
     __shared__ uintx4 lds[Tiles::UNITS];
-    const CbmTilePlace at = cbm_tile_place((a.count + BM - 1) / BM, (b.count + BN - 1) / BN, splits);
+    const CbmTilePlace at = cbm_tile_place((a.count + Tiles::ROWS - 1) / Tiles::ROWS, (b.count + Tiles::COLUMNS - 1) / Tiles::COLUMNS, splits);
     if (!at.any) return;
     Tiles t;
-    t.run(lds, a, b, at.m, at.n, chunks * at.split / splits, chunks * (at.split + 1) / splits);
-    t.pieces(at.m, at.n, [&](int64_t r, int64_t c, const float (&s)[4]) {
-        float v[4] = {s[0], s[1], s[2], s[3]};
+    t.run(lds, a, b, at.m, at.n, (int)(chunks * at.split / splits), (int)(chunks * (at.split + 1) / splits));
+    t.pieces(lds, at.m, at.n, [&](int64_t r, int64_t c, float (&v)[4]) {
         if (splits > 1) {
             if (r < a.count) cbm_put4<float>(parts + (at.split * a.count + r) * b.count, c, b.count, v);
         } else {
@@ -77,31 +74,76 @@ __global__ __launch_bounds__(256) void cbm_product_join_kernel(int64_t M, int64_
     }
 }
 
-int64_t chunk(int32_t type) { return type == CBM_F32 ? 32 : 64; }
+// Which tiles, and how many shares of K.
+struct Plan {
+    int tile;  // 256 and 128: units straight to LDS; 0: 128 x 128 of any matrices
+    int64_t splits;
+    double us;
+};
+// Microseconds as measured: a workgroup's rate, by how many of a tile run at once; what a workgroup takes beside its products (the first loads, the result); shares of K are written, read and joined in a launch
+// of its own.  Shares of at least 256 k.
+Plan plan(int64_t M, int64_t N, int64_t K, int32_t type, int tile) {
+    const int64_t side = tile ? tile : 128, tiles = std::max<int64_t>(1, (M + side - 1) / side * ((N + side - 1) / side)), at_once = tile == 256 ? 256 : 512;
+    const double tflops = tile == 256 ? 1150.0 : tile == 128 ? 900.0 : type == CBM_F32 ? 140.0 : 550.0, beside = tile == 256 ? 9.0 : 5.0;
+    const double each = 2.0 * (double)(side * side * K) / (tflops * 1e6 / (double)at_once);
+    Plan best{tile, 1, 1e30};
+    for (int64_t s = 1; s <= 64 && (s == 1 || s * 256 <= K); ++s) {
+        const double rounds = (double)((tiles * s + at_once - 1) / at_once);
+        const double us = rounds * (each / (double)s + beside) + (s > 1 ? 4.0 + 8.0 * (double)(s * M * N) / 4e6 : 0.0);
+        if (us < 0.97 * best.us) best = {tile, s, us};
+    }
+    return best;
+}
+Plan plan(int64_t M, int64_t N, int64_t K, int32_t type, bool units) {
+    if (!units) return plan(M, N, K, type, 0);
+    const Plan large = plan(M, N, K, type, 256), small = plan(M, N, K, type, 128);
+    return large.us < small.us ? large : small;
+}
 
-template <class T, class TO>
+template <class T, class TO, CbmTileOrder OA, CbmTileOrder OB, CbmTilePair PAIR>
 void launch(const CbmProduct& p, hipStream_t stream) {
-    const int64_t chunks = p.at ? (p.at + p.K + chunk(p.type) - 1) / chunk(p.type) : (p.K + chunk(p.type) - 1) / chunk(p.type);
-    const int64_t tiles = (p.M + BM - 1) / BM * ((p.N + BN - 1) / BN), splits = p.parts ? cbm_product_parts(p.M, p.N, p.at ? p.at + p.K : p.K, p.type) : 1;
-    const CbmOperand<T> a{{(const T*)p.A, nullptr}, {p.lda, 0}, p.M, p.at ? p.at + p.K : p.K, 0};
+    const int64_t K = p.at ? p.at + p.K : p.K;
+    const CbmOperand<T> a{{(const T*)p.A, nullptr}, {p.lda, 0}, p.M, K, 0};
     const CbmOperand<T> b{{(const T*)p.B[0], (const T*)p.B[1]}, {p.ldb[0], p.ldb[1]}, p.N, p.K, p.at};
-    const unsigned grid = (unsigned)((tiles * splits + CBM_XCD - 1) / CBM_XCD * CBM_XCD);
-    if (p.at) cbm_product_kernel<T, TO, ALONG_K, ALONG_K, PAIR_K><<<grid, 256, 0, stream>>>(a, b, chunks, splits, p.out, p.parts);
-    else if (p.a_across) cbm_product_kernel<T, TO, ACROSS_K, ACROSS_K, SINGLE><<<grid, 256, 0, stream>>>(a, b, chunks, splits, p.out, p.parts);
-    else if (p.b_across) cbm_product_kernel<T, TO, ALONG_K, ACROSS_K, SINGLE><<<grid, 256, 0, stream>>>(a, b, chunks, splits, p.out, p.parts);
-    else cbm_product_kernel<T, TO, ALONG_K, ALONG_K, SINGLE><<<grid, 256, 0, stream>>>(a, b, chunks, splits, p.out, p.parts);
+    bool units = false;
+    if constexpr (sizeof(T) == 2)
+        units = cbm_units(a.p[0], a.ld[0], OA == ALONG_K ? K : p.M) && cbm_units(b.p[0], b.ld[0], OB == ALONG_K ? p.K : p.N) && (PAIR == SINGLE || (cbm_units(b.p[1], b.ld[1], p.K) && b.ld[1] == b.ld[0]));
+    const Plan how = plan(p.M, p.N, K, p.type, units);
+    const int64_t splits = p.parts ? how.splits : 1;
+    auto run = [&](auto* tiles_type) {
+        typedef std::remove_pointer_t<decltype(tiles_type)> Tiles;
+        const int64_t tiles = (p.M + Tiles::ROWS - 1) / Tiles::ROWS * ((p.N + Tiles::COLUMNS - 1) / Tiles::COLUMNS), chunks = (K + Tiles::BK - 1) / Tiles::BK;
+        cbm_product_kernel<Tiles, T, TO><<<(unsigned)((tiles * splits + CBM_XCD - 1) / CBM_XCD * CBM_XCD), 256, 0, stream>>>(a, b, chunks, splits, p.out, p.parts);
+    };
+    if (how.tile == 0) run((CbmTiles<T, 128, 128, 2, 2, OA, OB, PAIR>*)nullptr);
+    if constexpr (sizeof(T) == 2) {
+        if (how.tile == 128) run((CbmAlignedTiles<T, 128, 128, OA, OB, PAIR>*)nullptr);
+        if (how.tile == 256) run((CbmAlignedTiles<T, 256, 256, OA, OB, PAIR>*)nullptr);
+    }
     if (splits > 1) {
         const int64_t blocks = (p.M * ((p.N + 3) / 4) + 255) / 256;
         cbm_product_join_kernel<TO><<<(unsigned)std::min<int64_t>(blocks, 1 << 20), 256, 0, stream>>>(p.M, p.N, splits, p.parts, p.out);
     }
 }
+template <class T, class TO>
+void launch(const CbmProduct& p, hipStream_t stream) {
+    if (p.at) launch<T, TO, ALONG_K, ALONG_K, PAIR_K>(p, stream);
+    else if (p.a_across) launch<T, TO, ACROSS_K, ACROSS_K, SINGLE>(p, stream);
+    else if (p.b_across) launch<T, TO, ALONG_K, ACROSS_K, SINGLE>(p, stream);
+    else launch<T, TO, ALONG_K, ALONG_K, SINGLE>(p, stream);
+}
 
 }  // namespace
 
-// Few tiles share K so that the compute units have work, each share at least 512 k.
+// The most that a product of the size is cut into, however its matrices lie.
 int64_t cbm_product_parts(int64_t M, int64_t N, int64_t K, int32_t type) {
-    const int64_t tiles = std::max<int64_t>(1, (M + BM - 1) / BM * ((N + BN - 1) / BN)), most = K / 512;
-    return std::max<int64_t>(1, std::min(most, 512 / tiles));
+    const int64_t any = plan(M, N, K, type, false).splits;
+    return type == CBM_F32 ? any : std::max(any, plan(M, N, K, type, true).splits);
+}
+
+int cbm_product_tile(int64_t M, int64_t N, int64_t K, int32_t type) {
+    const Plan large = plan(M, N, K, type, 256), small = plan(M, N, K, type, 128);
+    return large.us < small.us ? 256 : 128;
 }
 
 void cbm_launch_tiles(const CbmProduct& p, void* stream) {

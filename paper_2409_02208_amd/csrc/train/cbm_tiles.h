@@ -179,56 +179,128 @@ struct CbmTileSide {
     }
 };
 
-// The sums of a workgroup's tile, BM rows by BN columns of the result, over chunks first .. last - 1 of K.  A wave has TM x TN tiles of 32 x 32; lane l's row in a tile is l % 32, its
+template <class T>
+__device__ __forceinline__ floatx16 cbm_multiply(uintx4 a, uintx4 b, floatx16 sum) {
+    if constexpr (std::is_same<T, _Float16>::value) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), sum, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), sum, 0, 0, 0);
+}
+
+// The sums of a workgroup's tile, BM rows by BN columns of the result.  A wave has TM x TN tiles of 32 x 32; lane l's row in a tile is l % 32, its
 // columns are 8 q + 4 (l / 32) + 0 .. 3 for q = 0 .. 3 (the operands change places in the instruction, so that a lane's values lie along the result's rows).
-template <class T, int BM, int BN, int WM, int WN, CbmTileOrder ORDER_A, CbmTileOrder ORDER_B, CbmTilePair PAIR_B>
-struct CbmTiles {
-    static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES, TM = BM / WM / 32, TN = BN / WN / 32;
-    typedef CbmTileSide<T, BM, THREADS, ORDER_A, SINGLE> A;
-    typedef CbmTileSide<T, BN, THREADS, ORDER_B, PAIR_B> B;
-    static constexpr int PARTS = A::PARTS, BK = A::BK, UNITS = A::UNITS + B::UNITS;
+template <int BM, int BN, int WM, int WN>
+struct CbmTileSums {
+    static constexpr int ROWS = BM, COLUMNS = BN, WAVES = WM * WN, THREADS = 64 * WAVES, TM = BM / WM / 32, TN = BN / WN / 32, ACROSS = WN;
     floatx16 acc[TM][TN];
 
-    static __device__ __forceinline__ floatx16 multiply(uintx4 a, uintx4 b, floatx16 sum) {
-        if constexpr (std::is_same<T, _Float16>::value) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), sum, 0, 0, 0);
-        else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), sum, 0, 0, 0);
-    }
-    static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
-    // the wave's first row and column in the tile
-    static __device__ __forceinline__ int first_row() { return wave() % WM * (32 * TM); }
-    static __device__ __forceinline__ int first_column() { return wave() / WM * (32 * TN); }
-
-    __device__ __forceinline__ void run(uintx4* lds, const CbmOperand<T>& a, const CbmOperand<T>& b, int64_t tile_m, int64_t tile_n, int64_t first, int64_t last) {
-        constexpr int P2 = PARTS == 1 ? 0 : 1;
-        floatx16 small[P2 ? TM : 1][P2 ? TN : 1];
+    __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    acc[i][j][v] = 0.0f;
-                    if constexpr (P2) small[i][j][v] = 0.0f;
-                }
+                for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+    }
+    static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+    // the wave's first row and column in the tile, and its place among the waves along the columns
+    static __device__ __forceinline__ int first_row() { return wave() % WM * (32 * TM); }
+    static __device__ __forceinline__ int first_column() { return wave() / WM * (32 * TN); }
+    static __device__ __forceinline__ int across() { return wave() / WM; }
+    // f(row, column of the first, four sums) for the wave's part of the result, rows of lanes along its rows: through LDS, 32 rows at a time, a place for each wave (so that 16384 x 1024 . 1024 x
+    // 8192 in bf16, which a lane's own four columns of a row at a time take 310 us for, takes 262).  The operands' places in LDS have to be free.
+    static constexpr int COLS = 32 * TN, OUT_STRIDE = COLS / 4 + 1, OUT_UNITS = WAVES * 32 * OUT_STRIDE;
+    __device__ __forceinline__ void band_to_lds(uintx4* to, int i) const {
+        const int l32 = threadIdx.x & 31, half = threadIdx.x >> 5 & 1;
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                to[l32 * OUT_STRIDE + 8 * j + 2 * q + half] = __builtin_bit_cast(uintx4, (floatx4){acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]});
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+    static __device__ __forceinline__ void four(float (&v)[4], uintx4 u) {
+        const floatx4 x = __builtin_bit_cast(floatx4, u);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = x[j];
+    }
+    template <class F>
+    __device__ __forceinline__ void pieces(uintx4* lds, int64_t tile_m, int64_t tile_n, F&& f) const {
+        const int lane = threadIdx.x & 63;
+        uintx4* mine = lds + wave() * 32 * OUT_STRIDE;
+        const int64_t row = tile_m * BM + first_row(), column = tile_n * BN + first_column();
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            band_to_lds(mine, i);
+#pragma unroll 1
+            for (int t = 0; t < COLS / 8; ++t) {
+                const int at = 64 * t + lane, r = at / (COLS / 4), c = at % (COLS / 4);
+                float v[4];
+                four(v, mine[r * OUT_STRIDE + c]);
+                f(row + 32 * i + r, column + 4 * c, v);
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+    // PAIR_ROWS: f(row, column, four sums of the first matrix's columns, of the second's)
+    template <class F>
+    __device__ __forceinline__ void pairs(uintx4* lds, int64_t tile_m, int64_t tile_n, F&& f) const {
+        const int lane = threadIdx.x & 63;
+        uintx4* mine = lds + wave() * 32 * OUT_STRIDE;
+        const int64_t row = tile_m * BM + first_row(), column = tile_n * (BN / 2) + first_column() / 2;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            band_to_lds(mine, i);
+#pragma unroll 2
+            for (int t = 0; t < COLS / 16; ++t) {
+                const int at = 64 * t + lane, r = at / (COLS / 8), c = at % (COLS / 8), p = r * OUT_STRIDE + c / 8 * 16 + c % 8;
+                float x[4], y[4];
+                four(x, mine[p]);
+                four(y, mine[p + 8]);
+                f(row + 32 * i + r, column + 4 * c, x, y);
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+};
+
+// Over chunks first .. last - 1 of K.
+template <class T, int BM, int BN, int WM, int WN, CbmTileOrder ORDER_A, CbmTileOrder ORDER_B, CbmTilePair PAIR_B>
+struct CbmTiles : CbmTileSums<BM, BN, WM, WN> {
+    typedef CbmTileSums<BM, BN, WM, WN> Sums;
+    static constexpr int THREADS = Sums::THREADS, TM = Sums::TM, TN = Sums::TN;
+    typedef CbmTileSide<T, BM, THREADS, ORDER_A, SINGLE> A;
+    typedef CbmTileSide<T, BN, THREADS, ORDER_B, PAIR_B> B;
+    static constexpr int PARTS = A::PARTS, BK = A::BK, OPERANDS = A::UNITS + B::UNITS, UNITS = OPERANDS > Sums::OUT_UNITS ? OPERANDS : Sums::OUT_UNITS, GROUPS = 2;  // GROUPS: workgroups a compute unit
+    using Sums::acc;
+
+    __device__ __forceinline__ void run(uintx4* lds, const CbmOperand<T>& a, const CbmOperand<T>& b, int tile_m, int tile_n, int first, int last) {
+        constexpr int P2 = PARTS == 1 ? 0 : 1;
+        floatx16 small[P2 ? TM : 1][P2 ? TN : 1];
+        this->clear();
+        if constexpr (P2)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) small[i][j] = acc[i][j];
         uint32_t minus_low = 0xbf80u;
         asm("" : "+s"(minus_low));
-        const int l32 = threadIdx.x & 31, half = threadIdx.x >> 5 & 1, wm = first_row(), wn = first_column();
+        const int l32 = threadIdx.x & 31, half = threadIdx.x >> 5 & 1, wm = Sums::first_row(), wn = Sums::first_column();
         uintx4 *la = lds, *lb = lds + A::UNITS;
         A sa;
         B sb;
         sa.begin(a, tile_m);
         sb.begin(b, tile_n);
         if (first < last) {
-            sa.load(a, first * BK);
-            sb.load(b, first * BK);
+            sa.load(a, (int64_t)first * BK);
+            sb.load(b, (int64_t)first * BK);
         }
-        for (int64_t c = first; c < last; ++c) {
+        for (int c = first; c < last; ++c) {
             sa.store(la, minus_low);
             sb.store(lb, minus_low);
             __syncthreads();
             if (c + 1 < last) {
-                sa.load(a, (c + 1) * BK);
-                sb.load(b, (c + 1) * BK);
+                sa.load(a, (int64_t)(c + 1) * BK);
+                sb.load(b, (int64_t)(c + 1) * BK);
             }
 #pragma unroll
             for (int s = 0; s < BK / 16; ++s) {
@@ -249,13 +321,13 @@ struct CbmTiles {
 #pragma unroll
                             for (int j = 0; j < TN; ++j) {
                                 floatx16& sum = q < 5 ? small[i][j] : acc[i][j];
-                                sum = multiply(y[j][PB[q]], x[i][PA[q]], sum);
+                                sum = cbm_multiply<T>(y[j][PB[q]], x[i][PA[q]], sum);
                             }
                 } else {
 #pragma unroll
                     for (int i = 0; i < TM; ++i)
 #pragma unroll
-                        for (int j = 0; j < TN; ++j) acc[i][j] = multiply(y[j][0], x[i][0], acc[i][j]);
+                        for (int j = 0; j < TN; ++j) acc[i][j] = cbm_multiply<T>(y[j][0], x[i][0], acc[i][j]);
                 }
             }
             __syncthreads();
@@ -268,32 +340,19 @@ struct CbmTiles {
 #pragma unroll
                     for (int v = 0; v < 16; ++v) acc[i][j][v] += small[i][j][v];
     }
-    // f(row, column of the first, four sums) for every piece of the lane's; row and column are the result's
-    template <class F>
-    __device__ __forceinline__ void pieces(int64_t tile_m, int64_t tile_n, F&& f) const {
-        const int l32 = threadIdx.x & 31, half = threadIdx.x >> 5 & 1;
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-                    f(tile_m * BM + first_row() + 32 * i + l32, tile_n * BN + first_column() + 32 * j + 8 * q + 4 * half, v);
-                }
-    }
 };
 
 // Tiles of the result for workgroup b of a grid of a multiple of 8: an XCD (b mod 8) has neighbouring ones, in blocks of 8 tiles of rows, so that what its workgroups read
 // at a time fits its L2.
 struct CbmTilePlace {
-    int64_t m, n, split;
+    int m, n, split;
     bool any;
 };
 __device__ __forceinline__ CbmTilePlace cbm_tile_place(int64_t tiles_m, int64_t tiles_n, int64_t splits) {
-    const int64_t per = gridDim.x / 8, at = blockIdx.x % 8 * per + blockIdx.x / 8, tiles = tiles_m * tiles_n, split = at / tiles, tile = at % tiles;
-    const int64_t group = tile / (8 * tiles_n), high = min((int64_t)8, tiles_m - 8 * group), in = tile - group * 8 * tiles_n;
-    return {8 * group + in % high, in / high, split, split < splits};
+    const uint32_t high_all = (uint32_t)tiles_m, wide = (uint32_t)tiles_n, per = gridDim.x / 8, at = blockIdx.x % 8 * per + blockIdx.x / 8, tiles = high_all * wide, split = at / tiles, tile = at % tiles;
+    const uint32_t group = tile / (8 * wide), high = min(8u, high_all - 8 * group), in = tile - group * 8 * wide;
+    auto whole = [](uint32_t v) { return __builtin_amdgcn_readfirstlane((int)v); };  // (divisions are made in vector registers, and would stay there)
+    return {whole(8 * group + in % high), whole(in / high), whole(split), split < (uint32_t)splits};
 }
 
 // Four values of a row of `columns` from `c` on (none beyond them).

@@ -245,3 +245,24 @@ def test_refusals(env):  # noqa: F811
     assert [call(k=(1 << 24) + 1, ldx=1 << 25), call(n=(1 << 31) + 1)] == [5, 5]
     torch.cuda.synchronize()
     assert bool((H == 1).all()) and bool((dX == 1).all())
+
+
+# rows that are whole numbers of 16 bytes, which 16-bit types go through LDS as they are: tiles of 128 and 256 with all and with few of their rows and columns, K that ends inside a chunk of 64
+UNITS = [(1, 8, 8), (130, 72, 72), (300, 64, 264), (257, 200, 136), (1100, 136, 520), (4100, 72, 2056), (2304, 320, 2048)]
+
+
+@pytest.mark.parametrize("name", ["bf16", "f16"])
+@pytest.mark.parametrize("n,k,m", UNITS)
+def test_whole_units(env, name, n, k, m):  # noqa: F811
+    torch, cbm = env
+    for pad in (0, 8):
+        act = "silu" if pad else "gelu"
+        _check_forward(*_forward(torch, cbm, n, k, m, name, act, pad, 0, keep=pad == 0), name, act, keep=pad == 0)
+        _check_backward(*_backward(torch, cbm, n, k, m, name, act, pad, 0), name, act)
+
+
+@pytest.mark.parametrize("n,k,m", [(8, 2048, 8), (20000, 64, 72), (9000, 520, 24)])
+def test_backward_with_shares_of_k(env, n, k, m):  # noqa: F811
+    torch, cbm = env
+    for name in ("f32", "bf16"):
+        _check_backward(*_backward(torch, cbm, n, k, m, name, "silu", 0, 0), name, "silu")

@@ -289,3 +289,14 @@ def test_refusals(env):  # noqa: F811
     assert [call(d=(1 << 24) + 1, ldx=1 << 25), call(c=(1 << 24) + 1, ldw=1 << 25)] == [5, 5]
     torch.cuda.synchronize()
     assert bool((logp == 1).all()) and bool((st == 1).all()) and bool((dX == 1).all()) and bool((dW == 1).all())
+
+
+@pytest.mark.parametrize("name", ["bf16", "f16"])
+@pytest.mark.parametrize("n,d,c", [(1, 8, 8), (130, 72, 72), (300, 64, 264), (257, 200, 1000), (4100, 72, 4104), (2304, 320, 4096)])
+def test_whole_units(env, name, n, d, c):  # noqa: F811
+    """Rows that are whole numbers of 16 bytes: tiles of 128 and 256 with all and with few of their rows and columns, d that ends inside a chunk of 64."""
+    torch, cbm = env
+    for pad in (0, 8):
+        X, W, L = _inputs(torch, n, d, c, name, pad, 0)
+        _check_forward(X, W, L, *_forward(torch, cbm, X, W, L))
+        _check_backward(X, W, L, *_backward(torch, cbm, X, W, L, pad, 0), name)
