@@ -1,9 +1,17 @@
 // The orthogonal update: a matrix's singular values driven towards one by products alone.
+//
+// Z (s x l, the shorter side first) is held as two fp16 parts that add up to 22 bits of each value, at a power of two times its size that fits the largest it can have: Z's singular values are at most one at first, and
+// each step's largest follows from the coefficients, so the host knows a bound of every entry.  Three products of parts (hh, hl, lh) then stand for one in 32 bits: what is left out is 2^-22 of a term, and
+// sums are fp32.  (update_large's error is that of its 16 bits; in fp32, 500 x 1333, 1.1e-6 with three bf16 parts and six products.)  Nothing below 2^-25 of 2^-14 of the largest bound is lost.
+//
+// All operands lie along k: Z and its transpose are both kept (Z Z^T reads rows of the one, P Z rows of P and of the other), A and P = a I + b A + c A^2 are symmetric: their tiles on one side of the diagonal are
+// made, and written to both.  A row in memory is blocks of 32 values: their high parts, then their low parts, 128 bytes together, so that a chunk of 64 halves is 32 k of both parts.
 #include <algorithm>
+#include <cmath>
 
+#include "cbm_aligned.h"
 #include "cbm_internal.h"
 #include "cbm_products.h"
-#include "cbm_tiles.h"
 
 namespace {
 
@@ -14,10 +22,11 @@ template <class T>
 __global__ __launch_bounds__(256) void cbm_orthogonal_norm_kernel(int64_t m, int64_t n, const T* __restrict__ X, int64_t ldx, double* __restrict__ parts) {
     __shared__ double room[256];
     double s = 0.0;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < m * n; i += (int64_t)gridDim.x * 256) {
-        const double x = (double)(float)X[i / n * ldx + i % n];
-        s += x * x;
-    }
+    for (int64_t r = blockIdx.x; r < m; r += gridDim.x)
+        for (int64_t c = threadIdx.x; c < n; c += 256) {
+            const double x = (double)(float)X[r * ldx + c];
+            s += x * x;
+        }
     room[threadIdx.x] = s;
     __syncthreads();
     for (int step = 128; step; step /= 2) {
@@ -27,81 +36,406 @@ __global__ __launch_bounds__(256) void cbm_orthogonal_norm_kernel(int64_t m, int
     if (threadIdx.x == 0) parts[blockIdx.x] = room[0];
 }
 
-// The matrix, or its transpose, over its norm + eps, in 32 bits.
+// A matrix in parts: rows of blocks of 32 columns.
+struct Halves {
+    _Float16* p;
+    int64_t rows, columns;
+    __host__ __device__ int64_t ld() const { return (columns + 31) / 32 * 64; }
+    __host__ __device__ int64_t bytes() const { return rows * ld() * 2; }
+};
+__device__ __forceinline__ void cut(float v, _Float16& h, _Float16& l) {
+    h = (_Float16)v;
+    l = (_Float16)(v - (float)h);
+}
+// Four values of row r from column c on, columns a multiple of four, zeros beyond the last (up to a whole block: products read those).
+__device__ __forceinline__ void put_halves(const Halves& x, int64_t r, int64_t c, const float (&v)[4]) {
+    if (r >= x.rows || c >= x.ld() / 2) return;
+    typedef _Float16 Four __attribute__((ext_vector_type(4)));
+    Four h, l;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        _Float16 a, b;
+        cut(c + j < x.columns ? v[j] : 0.0f, a, b);
+        h[j] = a;
+        l[j] = b;
+    }
+    _Float16* to = x.p + r * x.ld() + c / 32 * 64 + c % 32;
+    *reinterpret_cast<Four*>(to) = h;
+    *reinterpret_cast<Four*>(to + 32) = l;
+}
+
+// Z at 2^up times its size and its transpose, from X or its transpose over its norm + eps, a block of 32 x 32 a workgroup.
 template <class T>
-__global__ __launch_bounds__(256) void cbm_orthogonal_begin_kernel(int64_t m, int64_t n, const T* __restrict__ X, int64_t ldx, bool transposed, float eps, const double* __restrict__ parts,
-                                                                float* __restrict__ out) {
+__global__ __launch_bounds__(256) void cbm_orthogonal_begin_kernel(const T* __restrict__ X, int64_t ldx, bool transposed, float eps, float up, const double* __restrict__ parts, Halves z, Halves zt) {
+    __shared__ float room[32][33];
+    __shared__ double squares[4];
+    double s = parts[threadIdx.x];
+#pragma unroll
+    for (int step = 1; step < 64; step *= 2) s += __shfl_xor(s, step);
+    if (threadIdx.x % 64 == 0) squares[threadIdx.x / 64] = s;
+    __syncthreads();
+    const double size = sqrt((squares[0] + squares[1]) + (squares[2] + squares[3])) + (double)eps;
+    const int64_t r0 = (int64_t)blockIdx.y * 32, c0 = (int64_t)blockIdx.x * 32;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {  // along X's rows
+        const int slow = threadIdx.x / 32 + 8 * i, fast = threadIdx.x % 32;
+        const int64_t r = r0 + (transposed ? fast : slow), c = c0 + (transposed ? slow : fast);
+        float v = 0.0f;
+        if (r < z.rows && c < z.columns) v = (float)((double)(float)(transposed ? X[c * ldx + r] : X[r * ldx + c]) / size) * up;
+        room[r - r0][c - c0] = v;
+    }
+    __syncthreads();
+    const int row = threadIdx.x / 8, four = threadIdx.x % 8 * 4;
+    const float along[4] = {room[row][four], room[row][four + 1], room[row][four + 2], room[row][four + 3]}, across[4] = {room[four][row], room[four + 1][row], room[four + 2][row], room[four + 3][row]};
+    put_halves(z, r0 + row, c0 + four, along);
+    put_halves(zt, c0 + row, r0 + four, across);
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void cbm_orthogonal_scaled_kernel(int64_t m, int64_t n, const T* __restrict__ X, int64_t ldx, float eps, float scale, const double* __restrict__ parts, T* __restrict__ Y,
+                                                                 int64_t ldy) {
     double s = 0.0;
     for (int i = 0; i < PARTS; ++i) s += parts[i];
     const double size = sqrt(s) + (double)eps;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < m * n; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / n, c = i % n;  // of `out`
-        const double x = (double)(float)(transposed ? X[c * ldx + r] : X[r * ldx + c]);
-        out[i] = (float)(x / size);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < m * n; i += (int64_t)gridDim.x * 256) Y[i / n * ldy + i % n] = (T)(scale * (float)((double)(float)X[i / n * ldx + i % n] / size));
+}
+
+// The sums of a tile of B x B of a product of matrices in parts, as CbmAlignedTiles makes them: a step of 16 k is three products, and its units are read as the first of them and the one before go on.
+template <int B>
+struct HalvesTiles : CbmTileSums<B, B, 2, 2> {
+    typedef CbmTileSums<B, B, 2, 2> Sums;
+    typedef CbmAlignedSide<_Float16, B, ALONG_K, SINGLE> Side;
+    static constexpr int TM = Sums::TM, TN = Sums::TN, BK = 64, SLOT = Side::UNITS, UNITS = 5 * SLOT, GROUPS = B == 256 ? 1 : 2, LOADS = Side::LOADS, HALF = LOADS / 2;
+    static_assert(UNITS >= Sums::OUT_UNITS, "");
+    using Sums::acc;
+
+    __device__ __forceinline__ void run(uintx4* lds, const CbmOperand<_Float16>& a, const CbmOperand<_Float16>& b, int tile_m, int tile_n, int last) {
+        this->clear();
+        const int wave = Sums::wave(), wm = Sums::first_row(), wn = Sums::first_column();
+        Side sa, sb;
+        sa.begin(a, tile_m, wave);
+        sb.begin(b, tile_n, wave);
+        auto load = [&](auto whole, Side& s, const CbmOperand<_Float16>& o, int c, uintx4* to, int i) { s.template load<decltype(whole)::value>(o, c, o.K, to, wave, i); };
+        uintx4 *a0 = lds, *b0 = lds + SLOT, *a1 = lds + 2 * SLOT, *b1 = lds + 3 * SLOT, *a2 = lds + 4 * SLOT;
+        constexpr std::false_type some;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load(some, sa, a, 0, a0, i);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load(some, sb, b, 0, b0, i);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load(some, sa, a, 1, a1, i);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load(some, sb, b, 1, b1, i);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load(some, sa, a, 2, a2, i);
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(3 * LOADS) : "memory");
+        uintx4 xh[2][TM], yh[2][TN], xl[TM], yl[TN];
+        auto read = [&](const uintx4* la, const uintx4* lb, int s, uintx4 (&x)[TM], uintx4 (&y)[TN]) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i) x[i] = Side::unit(la, wm + 32 * i, s);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) y[j] = Side::unit(lb, wn + 32 * j, s);
+        };
+        auto multiply = [&](const uintx4 (&x)[TM], const uintx4 (&y)[TN]) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] = cbm_multiply<_Float16>(y[j], x[i], acc[i][j]);
+        };
+        // a read, or a load, between two products
+        auto order = [&](auto products_) {
+            constexpr int PRODUCTS = decltype(products_)::value, READS = TM + TN, AT_ONCE = PRODUCTS / 2 >= READS ? 1 : READS, GROUPS_OF_READS = (READS + AT_ONCE - 1) / AT_ONCE;
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+#pragma unroll
+            for (int i = 0; i < GROUPS_OF_READS; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x100, AT_ONCE, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < HALF; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            }
+            constexpr int LEFT = PRODUCTS - 1 - GROUPS_OF_READS - HALF;
+            if constexpr (LEFT > 0) __builtin_amdgcn_sched_group_barrier(0x008, LEFT, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        using std::integral_constant;
+        read(a0, b0, 0, xh[0], yh[0]);
+        auto chunk = [&](auto whole, int c) {
+            read(a0, b0, 2, xl, yl);
+#pragma unroll
+            for (int i = HALF; i < LOADS; ++i) load(whole, sb, b, c + 1, b1, i);
+            multiply(xh[0], yh[0]);
+            order(integral_constant<int, TM * TN>{});
+            read(a0, b0, 1, xh[1], yh[1]);
+#pragma unroll
+            for (int i = 0; i < HALF; ++i) load(whole, sa, a, c + 2, a2, i);
+            multiply(xh[0], yl);
+            multiply(xl, yh[0]);
+            order(integral_constant<int, 2 * TM * TN>{});
+            read(a0, b0, 3, xl, yl);
+#pragma unroll
+            for (int i = HALF; i < LOADS; ++i) load(whole, sa, a, c + 2, a2, i);
+            multiply(xh[1], yh[1]);
+            order(integral_constant<int, TM * TN>{});
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            read(a1, b1, 0, xh[0], yh[0]);
+#pragma unroll
+            for (int i = 0; i < HALF; ++i) load(whole, sb, b, c + 2, a0, i);
+            multiply(xh[1], yl);
+            multiply(xl, yh[1]);
+            order(integral_constant<int, 2 * TM * TN>{});
+            uintx4 *fa = a0, *fb = b0;
+            a0 = a1, b0 = b1, a1 = a2, b1 = fa, a2 = fb;
+        };
+        int c = 0;
+        for (; c + 2 < last; ++c) chunk(std::true_type{}, c);
+        for (; c < last; ++c) chunk(std::false_type{}, c);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+    // f(row, column of the first, four sums) and g(column, row of the first, four sums): along the rows and along the columns of the result
+    template <class F, class G>
+    __device__ __forceinline__ void both(uintx4* lds, int tile_m, int tile_n, F&& f, bool down, G&& g) const {
+        const int lane = threadIdx.x & 63;
+        uintx4* mine = lds + Sums::wave() * 32 * Sums::OUT_STRIDE;
+        const int64_t row = (int64_t)tile_m * B + Sums::first_row(), column = (int64_t)tile_n * B + Sums::first_column();
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            this->band_to_lds(mine, i);
+#pragma unroll 1
+            for (int t = 0; t < Sums::COLS / 8; ++t) {
+                const int at = 64 * t + lane, r = at / (Sums::COLS / 4), c = at % (Sums::COLS / 4);
+                float v[4];
+                Sums::four(v, mine[r * Sums::OUT_STRIDE + c]);
+                f(row + 32 * i + r, column + 4 * c, v);
+                if (down) mine[r * Sums::OUT_STRIDE + c] = __builtin_bit_cast(uintx4, (floatx4){v[0], v[1], v[2], v[3]});  // (as f left them)
+            }
+            if (down) {
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                const float* of = (const float*)mine;
+#pragma unroll 1
+                for (int t = 0; t < Sums::COLS / 8; ++t) {
+                    const int r = lane % 8 * 4, c = t * 8 + lane / 8;
+                    float v[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = of[(r + j) * (4 * Sums::OUT_STRIDE) + c];
+                    g(column + c, row + 32 * i + r, v);
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+};
+
+enum { GRAM, POLYNOMIAL, STEP, LAST };
+struct ProductArgs {
+    Halves a, b;     // rows of both, along k
+    Halves out, outt;  // GRAM, POLYNOMIAL: out; STEP: both
+    Halves gram;     // POLYNOMIAL
+    float up;        // of the sums, to the size that is written
+    float of_gram, of_one;  // POLYNOMIAL: times the Gram matrix as it is kept, and on the diagonal
+    void* Y;         // LAST
+    int64_t ldy;
+    bool transposed;
+};
+
+// Tile `at` of those on and below the diagonal.
+__device__ __forceinline__ void below(int at, int& m, int& n) {
+    m = (int)((sqrtf(8.0f * (float)at + 1.0f) - 1.0f) * 0.5f);
+    while ((int64_t)(m + 1) * (m + 2) / 2 <= at) ++m;
+    while ((int64_t)m * (m + 1) / 2 > at) --m;
+    n = at - (int)((int64_t)m * (m + 1) / 2);
+}
+
+template <int B, int MODE, class T>
+__global__ __launch_bounds__(256, HalvesTiles<B>::GROUPS) void cbm_orthogonal_product_kernel(ProductArgs p) {
+    typedef HalvesTiles<B> Tiles;
+    __shared__ uintx4 lds[Tiles::UNITS];
+    int m, n;
+    const int tiles_m = (int)((p.a.rows + B - 1) / B), tiles_n = (int)((p.b.rows + B - 1) / B);
+    if constexpr (MODE == GRAM || MODE == POLYNOMIAL) {
+        const int at = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
+        if (at >= tiles_m * (tiles_m + 1) / 2) return;
+        below(at, m, n);
+        m = __builtin_amdgcn_readfirstlane(m);
+        n = __builtin_amdgcn_readfirstlane(n);
+    } else {
+        const CbmTilePlace at = cbm_tile_place(tiles_m, tiles_n, 1);
+        if (!at.any) return;
+        m = at.m, n = at.n;
+    }
+    Tiles t;
+    t.run(lds, {{p.a.p, nullptr}, {p.a.ld(), 0}, p.a.rows, p.a.ld(), 0}, {{p.b.p, nullptr}, {p.b.ld(), 0}, p.b.rows, p.b.ld(), 0}, m, n, (int)(p.a.ld() / 64));
+    if constexpr (MODE == LAST) {
+        t.pieces(lds, m, n, [&](int64_t r, int64_t c, float (&v)[4]) {
+            if (r >= p.a.rows) return;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] *= p.up;
+            T* Y = (T*)p.Y;
+            if (!p.transposed) cbm_put4<T>(Y + r * p.ldy, c, p.b.rows, v);
+            else
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (c + j < p.b.rows) Y[(c + j) * p.ldy + r] = (T)v[j];
+        });
+    } else {
+        t.both(
+            lds, m, n,
+            [&](int64_t r, int64_t c, float (&v)[4]) {
+                float g[4] = {};
+                if constexpr (MODE == POLYNOMIAL)
+                    if (r < p.gram.rows && c < p.gram.rows) {
+                        typedef _Float16 Four __attribute__((ext_vector_type(4)));
+                        const _Float16* from = p.gram.p + r * p.gram.ld() + c / 32 * 64 + c % 32;
+                        const Four h = *reinterpret_cast<const Four*>(from), l = *reinterpret_cast<const Four*>(from + 32);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) g[j] = (float)h[j] + (float)l[j];
+                    }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    v[j] *= p.up;
+                    if constexpr (MODE == POLYNOMIAL) v[j] = fmaf(p.of_gram, g[j], v[j]) + (r == c + j ? p.of_one : 0.0f);
+                    if (r >= p.a.rows) v[j] = 0.0f;  // (rows beyond the last are the last one's again; down a column they are zeros)
+                }
+                put_halves(p.out, r, c, v);
+            },
+            MODE == STEP || m != n, [&](int64_t c, int64_t r, float (&v)[4]) { put_halves(MODE == STEP ? p.outt : p.out, c, r, v); });
     }
 }
 
-template <class T>
-__global__ __launch_bounds__(256) void cbm_orthogonal_end_kernel(int64_t m, int64_t n, const float* __restrict__ x, bool transposed, float scale, T* __restrict__ Y, int64_t ldy) {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < m * n; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / n, c = i % n;  // of Y
-        Y[r * ldy + c] = (T)(scale * x[transposed ? c * m + r : i]);
+int64_t rounded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// Largest |f| on [0, top] of an odd polynomial a x + b x^3 + c x^5, and of a + b x^2 + c x^4: at an end or where the slope is zero.
+double largest(const float* abc, double top, bool odd) {
+    const double a = abc[0], b = abc[1], c = abc[2];
+    auto f = [&](double x) { return std::fabs((a + b * x * x + c * x * x * x * x) * (odd ? x : 1.0)); };
+    double most = std::max(f(0.0), f(top));
+    // odd: a + 3 b y + 5 c y^2 = 0 in y = x^2; even: x = 0 or b + 2 c y = 0
+    double roots[2] = {-1.0, -1.0};
+    if (odd) {
+        const double q = 9 * b * b - 20 * a * c;
+        if (c == 0.0) roots[0] = b == 0.0 ? -1.0 : -a / (3 * b);
+        else if (q >= 0.0) {
+            roots[0] = (-3 * b + std::sqrt(q)) / (10 * c);
+            roots[1] = (-3 * b - std::sqrt(q)) / (10 * c);
+        }
+    } else if (c != 0.0) {
+        roots[0] = -b / (2 * c);
     }
+    for (double y : roots)
+        if (y > 0.0 && y < top * top) most = std::max(most, f(std::sqrt(y)));
+    return most;
+}
+// The power of two at which values up to `most` are kept: at most 2^14 there.
+int power(double most) {
+    if (!(most > 0.0)) return 0;
+    return (int)std::max(-100.0, std::min(100.0, 14.0 - std::ceil(std::log2(most))));
 }
 
-int64_t padded(int64_t v) { return (v + 3) / 4 * 4; }
-unsigned blocks_of(int64_t values) { return (unsigned)std::min<int64_t>((values + 255) / 256, 1 << 20); }
+struct Room {
+    int64_t squares, z[2], zt[2], gram, poly, bytes;
+};
+Room room_of(int64_t s, int64_t l) {
+    Room r;
+    const int64_t z = rounded(Halves{nullptr, s, l}.bytes()), zt = rounded(Halves{nullptr, l, s}.bytes()), sq = rounded(Halves{nullptr, s, s}.bytes());
+    r.squares = 0;
+    r.z[0] = rounded(PARTS * 8);
+    r.z[1] = r.z[0] + z;
+    r.zt[0] = r.z[1] + z;
+    r.zt[1] = r.zt[0] + zt;
+    r.gram = r.zt[1] + zt;
+    r.poly = r.gram + sq;
+    r.bytes = r.poly + sq;
+    return r;
+}
+
+// f(tile's side) of the tiles that take least: rounds of workgroups, each its products at what a compute unit's share reaches and what it takes beside them.
+template <class F>
+void with_tile(int64_t M, int64_t N, int64_t K, bool half, F&& f) {
+    double best = 1e30;
+    int side = 256;
+    for (int b : {256, 128, 64}) {
+        const int64_t m = (M + b - 1) / b, tiles = half ? m * (m + 1) / 2 : m * ((N + b - 1) / b), at_once = b == 256 ? 256 : 512;
+        const double each = 6.0 * b * b * (double)K / ((b == 256 ? 1250.0 : b == 128 ? 1050.0 : 500.0) * 1e6 / (double)at_once) * (b != 256 && tiles <= 256 ? 0.6 : 1.0);
+        const double us = (double)((tiles + at_once - 1) / at_once) * (each + (b == 256 ? 12.0 : b == 128 ? 5.0 : 3.0));
+        if (us < best) best = us, side = b;
+    }
+    using std::integral_constant;
+    if (side == 256) f(integral_constant<int, 256>{});
+    else if (side == 128) f(integral_constant<int, 128>{});
+    else f(integral_constant<int, 64>{});
+}
+
+template <int MODE, class T>
+void product(const ProductArgs& p, hipStream_t stream) {
+    const bool half = MODE == GRAM || MODE == POLYNOMIAL;
+    with_tile(p.a.rows, p.b.rows, p.a.columns, half, [&](auto side) {
+        constexpr int B = decltype(side)::value;
+        const int64_t m = (p.a.rows + B - 1) / B, tiles = half ? m * (m + 1) / 2 : m * ((p.b.rows + B - 1) / B);
+        cbm_orthogonal_product_kernel<B, MODE, T><<<(unsigned)((tiles + CBM_XCD - 1) / CBM_XCD * CBM_XCD), 256, 0, stream>>>(p);
+    });
+}
 
 }  // namespace
 
-int64_t cbm_orthogonal_workspace(int32_t m, int32_t n, int32_t) {
-    const int64_t s = std::min(m, n), l = std::max(m, n);
-    const int64_t parts = std::max(cbm_product_parts(s, s, l, CBM_F32) * s * s, cbm_product_parts(s, l, s, CBM_F32) * s * l);
-    return PARTS * 8 + 4 * (2 * padded(s * l) + 2 * padded(s * s) + parts);
-}
+int64_t cbm_orthogonal_workspace(int32_t m, int32_t n, int32_t) { return room_of(std::min(m, n), std::max(m, n)).bytes; }
 
 cbm_status cbm_launch_orthogonal(int32_t m, int32_t n, int32_t type, const void* X, int64_t ldx, int32_t steps, const float* abc, float eps, float scale, void* Y, int64_t ldy, void* workspace,
                                  void* stream_) {
     hipStream_t stream = (hipStream_t)stream_;
     const bool tall = m > n;
     const int64_t s = std::min(m, n), l = std::max(m, n);
-    double* squares = (double*)workspace;
-    float *x = (float*)(squares + PARTS), *other = x + padded(s * l), *gram = other + padded(s * l), *poly = gram + padded(s * s), *parts = poly + padded(s * s);
+    const Room room = room_of(s, l);
+    char* base = (char*)workspace;
+    double* squares = (double*)(base + room.squares);
+    double top = 1.0 + 0x1p-10;  // a bound of Z's singular values
+    int up = power(top);
+    Halves z{(_Float16*)(base + room.z[0]), s, l}, zt{(_Float16*)(base + room.zt[0]), l, s};
+    const Halves gram{(_Float16*)(base + room.gram), s, s}, poly{(_Float16*)(base + room.poly), s, s};
     cbm_with_type(type, [&](auto t) {
         using T = decltype(t);
         cbm_orthogonal_norm_kernel<T><<<PARTS, 256, 0, stream>>>(m, n, (const T*)X, ldx, squares);
-        cbm_orthogonal_begin_kernel<T><<<blocks_of(s * l), 256, 0, stream>>>(s, l, (const T*)X, ldx, tall, eps, squares, x);
-    });
-    for (int i = 0; i < steps; ++i) {
-        CbmProduct p{};
-        p.type = p.out.type = CBM_F32;
-        p.out.first = p.out.last = true;
-        auto run = [&](int64_t M, int64_t N, int64_t K, const float* a, const float* b, bool across, float* c, float alpha, const float* more, float beta) {
-            p.M = M;
-            p.N = N;
-            p.K = K;
-            p.A = a;
-            p.lda = K;
-            p.B[0] = b;
-            p.ldb[0] = across ? N : K;
-            p.b_across = across;
-            p.out.C[0] = c;
-            p.out.ldc[0] = p.out.ldm = N;
-            p.out.columns = (int32_t)N;
-            p.out.alpha = alpha;
-            p.out.more = more;
-            p.out.beta = beta;
-            p.parts = parts;
-            cbm_launch_tiles(p, stream);
-        };
-        run(s, s, l, x, x, false, gram, 1.0f, nullptr, 0.0f);
-        run(s, s, s, gram, gram, false, poly, abc[2], gram, abc[1]);  // (the Gram matrix is symmetric)
-        run(s, l, s, poly, x, true, other, 1.0f, x, abc[0]);
-        std::swap(x, other);
-    }
-    cbm_with_type(type, [&](auto t) {
-        using T = decltype(t);
-        cbm_orthogonal_end_kernel<T><<<blocks_of(s * l), 256, 0, stream>>>(m, n, x, tall, scale, (T*)Y, ldy);
+        if (steps == 0) {
+            cbm_orthogonal_scaled_kernel<T><<<(unsigned)std::min<int64_t>((s * l + 255) / 256, 1 << 20), 256, 0, stream>>>(m, n, (const T*)X, ldx, eps, scale, squares, (T*)Y, ldy);
+            return;
+        }
+        cbm_orthogonal_begin_kernel<T><<<dim3((unsigned)((l + 31) / 32), (unsigned)((s + 31) / 32)), 256, 0, stream>>>((const T*)X, ldx, tall, eps, (float)std::ldexp(1.0, up), squares, z, zt);
+        for (int i = 0; i < steps; ++i) {
+            const int up_gram = power(top * top), up_poly = power(largest(abc, top, false));
+            top = largest(abc, top, true) * (1.0 + 0x1p-10);
+            const int up_next = power(top);
+            ProductArgs p{};
+            p.a = p.b = z;
+            p.out = gram;
+            p.up = (float)std::ldexp(1.0, up_gram - 2 * up);
+            product<GRAM, float>(p, stream);
+            p.a = p.b = p.gram = gram;
+            p.out = poly;
+            p.up = (float)std::ldexp((double)abc[2], up_poly - 2 * up_gram);
+            p.of_gram = (float)std::ldexp((double)abc[1], up_poly - up_gram);
+            p.of_one = (float)std::ldexp((double)abc[0], up_poly);
+            product<POLYNOMIAL, float>(p, stream);
+            p.a = poly;
+            p.b = zt;
+            if (i + 1 < steps) {
+                p.out = {(_Float16*)(base + room.z[(i + 1) % 2]), s, l};
+                p.outt = {(_Float16*)(base + room.zt[(i + 1) % 2]), l, s};
+                p.up = (float)std::ldexp(1.0, up_next - up - up_poly);
+                product<STEP, float>(p, stream);
+                z = p.out;
+                zt = p.outt;
+                up = up_next;
+            } else {
+                p.Y = Y;
+                p.ldy = ldy;
+                p.transposed = tall;
+                p.up = (float)std::ldexp((double)scale, -up - up_poly);
+                product<LAST, T>(p, stream);
+            }
+        }
     });
     return cbm_launched("orthogonal update launch");
 }
