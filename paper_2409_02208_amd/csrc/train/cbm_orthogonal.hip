@@ -306,6 +306,167 @@ __global__ __launch_bounds__(256, HalvesTiles<B>::GROUPS) void cbm_orthogonal_pr
     }
 }
 
+// Small matrices: everything in one workgroup's LDS, Z and A (which P takes the place of), rows of blocks as in memory and one unit more, so that sixteen neighbouring rows' units fall on different banks.
+// Tiles of 16 x 16 go to the waves in turn.  Z's columns, which P Z wants, are turned as they are read.
+constexpr int SMALL_STEPS = 16, SMALL_WAVES = 16;
+struct SmallArgs {
+    int rows, columns, steps;  // of Z
+    bool transposed;
+    float eps, first, last;              // powers: of Z at first, and back to its size (and Y's scale) at last
+    float gram[SMALL_STEPS], square[SMALL_STEPS], of_gram[SMALL_STEPS], of_one[SMALL_STEPS], next[SMALL_STEPS];
+};
+__host__ __device__ constexpr int small_pitch(int k) { return k * 4 + 16; }  // bytes of a row of k (a multiple of 32) values in parts
+
+typedef float floatx4s __attribute__((ext_vector_type(4)));
+struct SmallTile {
+    floatx4s hh, hl, lh;
+    __device__ __forceinline__ floatx4s sum() const { return hh + (hl + lh); }
+};
+__device__ __forceinline__ f16x8 small_unit(const char* at) { return *reinterpret_cast<const f16x8*>(at); }
+// eight k of column `lane % 16` from k 8 (lane / 16) on: `at` is the block's first row at the sixteen columns
+__device__ __forceinline__ f16x8 small_turned(const char* at, int pitch) {
+    typedef short Four __attribute__((ext_vector_type(4)));
+    const int lane = threadIdx.x & 63;
+    const char* p = at + (8 * (lane >> 4) + (lane >> 2 & 3)) * pitch + (lane & 3) * 8;
+    struct {
+        Four low, high;
+    } v;
+    v.low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) Four*)p);
+    v.high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) Four*)(p + 4 * pitch));
+    return __builtin_bit_cast(f16x8, v);
+}
+// Rows m .. m + 15 of x times rows n .. n + 15 of y (TURNED: times columns n .. n + 15), over `blocks` of 32 k.  Lane l has row l % 16 and columns 4 (l / 16) on.
+template <bool TURNED>
+__device__ __forceinline__ SmallTile small_product(const char* x, int px, int m, const char* y, int py, int n, int blocks) {
+    const int lane = threadIdx.x & 63, of = (lane >> 4) * 16;
+    SmallTile t{};
+    for (int b = 0; b < blocks; ++b) {
+        const char *ax = x + (m + (lane & 15)) * px + b * 128 + of, *ay = TURNED ? y + b * 32 * py + n / 32 * 128 + n % 32 * 2 : y + (n + (lane & 15)) * py + b * 128 + of;
+        const f16x8 xh = small_unit(ax), xl = small_unit(ax + 64), yh = TURNED ? small_turned(ay, py) : small_unit(ay), yl = TURNED ? small_turned(ay + 64, py) : small_unit(ay + 64);
+        t.hh = __builtin_amdgcn_mfma_f32_16x16x32_f16(yh, xh, t.hh, 0, 0, 0);
+        t.hl = __builtin_amdgcn_mfma_f32_16x16x32_f16(yl, xh, t.hl, 0, 0, 0);
+        t.lh = __builtin_amdgcn_mfma_f32_16x16x32_f16(yh, xl, t.lh, 0, 0, 0);
+    }
+    return t;
+}
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ char* small_place(char* x, int pitch, int m, int n) {  // of a lane's four values
+    const int lane = threadIdx.x & 63, c = n + (lane >> 4) * 4;
+    return x + (m + (lane & 15)) * pitch + c / 32 * 128 + c % 32 * 2;
+}
+__device__ __forceinline__ void small_put(char* at, const float (&v)[4]) {
+    f16x4 h, l;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        _Float16 a, b;
+        cut(v[j], a, b);
+        h[j] = a;
+        l[j] = b;
+    }
+    *reinterpret_cast<f16x4*>(at) = h;
+    *reinterpret_cast<f16x4*>(at + 64) = l;
+}
+
+// SIDE: the most rows and columns
+template <class T, int SIDE>
+__global__ __launch_bounds__(64 * SMALL_WAVES) void cbm_orthogonal_small_kernel(SmallArgs p, const T* X, int64_t ldx, T* Y, int64_t ldy) {
+    __shared__ uintx4 all[2 * SIDE * small_pitch(SIDE) / 16];
+    __shared__ double squares[SMALL_WAVES];
+    constexpr int EACH = SIDE * SIDE / (64 * SMALL_WAVES), TILES = SIDE / 16 * (SIDE / 16) / SMALL_WAVES;
+    const int s = (p.rows + 31) / 32 * 32, l = (p.columns + 31) / 32 * 32, pz = small_pitch(l), pg = small_pitch(s), wave = threadIdx.x >> 6;
+    char *z = (char*)all, *g = z + s * pz;
+    // X's values, zeros beyond it, neighbouring threads along its rows
+    const int height = p.transposed ? p.columns : p.rows, width = p.transposed ? p.rows : p.columns, c0 = threadIdx.x % SIDE, r0 = threadIdx.x / SIDE;
+    double sum = 0.0;
+#pragma unroll 4
+    for (int i = 0; i < EACH; ++i) {
+        const int r = r0 + 64 * SMALL_WAVES / SIDE * i;
+        if (r >= height || c0 >= width) continue;
+        const double v = (double)(float)X[r * ldx + c0];
+        sum += v * v;
+    }
+#pragma unroll
+    for (int step = 1; step < 64; step *= 2) sum += __shfl_xor(sum, step);
+    if (threadIdx.x % 64 == 0) squares[wave] = sum;
+    __syncthreads();
+    sum = 0.0;
+    for (int i = 0; i < SMALL_WAVES; ++i) sum += squares[i];
+    const double size = sqrt(sum) + (double)p.eps;
+#pragma unroll 4
+    for (int i = 0; i < EACH; ++i) {  // (read again, from L2: kept in registers, 128 x 128 spill)
+        const int r = r0 + 64 * SMALL_WAVES / SIDE * i, zr = p.transposed ? c0 : r, zc = p.transposed ? r : c0;
+        if (zr >= s || zc >= l) continue;
+        _Float16 h, low;
+        cut(r < height && c0 < width ? (float)((double)(float)X[r * ldx + c0] / size) * p.first : 0.0f, h, low);
+        _Float16* to = (_Float16*)(z + zr * pz + zc / 32 * 128 + zc % 32 * 2);
+        to[0] = h;
+        to[32] = low;
+    }
+    __syncthreads();
+    const int square = s / 16 * (s / 16), whole = s / 16 * (l / 16);
+    for (int step = 0; step < p.steps; ++step) {
+        int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        asm volatile("" : "+s"(wave));  // (or all tiles' places stay in scalar registers from step to step)
+        for (int t = wave; t < square; t += SMALL_WAVES) {
+            const int m = t / (s / 16) * 16, n = t % (s / 16) * 16;
+            const floatx4s a = small_product<false>(z, pz, m, z, pz, n, l / 32).sum();
+            const float out[4] = {a[0] * p.gram[step], a[1] * p.gram[step], a[2] * p.gram[step], a[3] * p.gram[step]};
+            small_put(small_place(g, pg, m, n), out);
+        }
+        __syncthreads();
+        floatx4s acc[TILES];
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) {
+            const int t = wave + SMALL_WAVES * i, m = t / (s / 16) * 16, n = t % (s / 16) * 16;
+            if (t >= square) continue;
+            acc[i] = small_product<false>(g, pg, m, g, pg, n, s / 32).sum();
+            const char* at = small_place(g, pg, m, n);
+            const f16x4 h = *reinterpret_cast<const f16x4*>(at), low = *reinterpret_cast<const f16x4*>(at + 64);
+            const int lane = threadIdx.x & 63, r = m + (lane & 15), c = n + (lane >> 4) * 4;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(p.of_gram[step], (float)h[j] + (float)low[j], acc[i][j] * p.square[step]) + (r == c + j ? p.of_one[step] : 0.0f);
+        }
+        __syncthreads();
+        asm volatile("" : "+s"(wave));
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) {
+            const int t = wave + SMALL_WAVES * i;
+            if (t >= square) continue;
+            const float out[4] = {acc[i][0], acc[i][1], acc[i][2], acc[i][3]};
+            small_put(small_place(g, pg, t / (s / 16) * 16, t % (s / 16) * 16), out);
+        }
+        __syncthreads();
+        asm volatile("" : "+s"(wave));
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) {
+            const int t = wave + SMALL_WAVES * i;
+            if (t >= whole) continue;
+            acc[i] = small_product<true>(g, pg, t / (l / 16) * 16, z, pz, t % (l / 16) * 16, s / 32).sum();
+        }
+        __syncthreads();
+        const bool end = step + 1 == p.steps;
+        const float up = end ? p.last : p.next[step];
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) {
+            const int t = wave + SMALL_WAVES * i, m = t / (l / 16) * 16, n = t % (l / 16) * 16;
+            if (t >= whole) continue;
+            const float out[4] = {acc[i][0] * up, acc[i][1] * up, acc[i][2] * up, acc[i][3] * up};
+            if (!end) {
+                small_put(small_place(z, pz, m, n), out);
+                continue;
+            }
+            const int lane = threadIdx.x & 63, r = m + (lane & 15), c = n + (lane >> 4) * 4;
+            if (r >= p.rows) continue;
+            if (!p.transposed) cbm_put4<T>(Y + r * ldy, c, p.columns, out);
+            else
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (c + j < p.columns) Y[(c + j) * ldy + r] = (T)out[j];
+        }
+        __syncthreads();
+    }
+}
+
 int64_t rounded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
 // Largest |f| on [0, top] of an odd polynomial a x + b x^3 + c x^5, and of a + b x^2 + c x^4: at an end or where the slope is zero.
@@ -334,6 +495,25 @@ int power(double most) {
     if (!(most > 0.0)) return 0;
     return (int)std::max(-100.0, std::min(100.0, 14.0 - std::ceil(std::log2(most))));
 }
+
+// What a step multiplies its sums by: to the size that A is kept at, to P's, A as it is kept and one to P's, to the size that the next Z is kept at; and the power of two back to Z's own size.
+// `top` and `up`, a bound of Z's singular values and the power that it is kept at, become the next Z's.
+struct Powers {
+    float gram, square, of_gram, of_one, next;
+    int back;
+    Powers(const float* abc, double& top, int& up) {
+        const int up_gram = power(top * top), up_poly = power(largest(abc, top, false));
+        top = largest(abc, top, true) * (1.0 + 0x1p-10);
+        const int up_next = power(top);
+        gram = (float)std::ldexp(1.0, up_gram - 2 * up);
+        square = (float)std::ldexp((double)abc[2], up_poly - 2 * up_gram);
+        of_gram = (float)std::ldexp((double)abc[1], up_poly - up_gram);
+        of_one = (float)std::ldexp((double)abc[0], up_poly);
+        next = (float)std::ldexp(1.0, up_next - up - up_poly);
+        back = -up - up_poly;
+        up = up_next;
+    }
+};
 
 struct Room {
     int64_t squares, z[2], zt[2], gram, poly, bytes;
@@ -393,6 +573,30 @@ cbm_status cbm_launch_orthogonal(int32_t m, int32_t n, int32_t type, const void*
     double* squares = (double*)(base + room.squares);
     double top = 1.0 + 0x1p-10;  // a bound of Z's singular values
     int up = power(top);
+    if (l <= 128 && steps > 0 && steps <= SMALL_STEPS) {
+        SmallArgs p{};
+        p.rows = (int)s;
+        p.columns = (int)l;
+        p.steps = steps;
+        p.transposed = tall;
+        p.eps = eps;
+        p.first = (float)std::ldexp(1.0, up);
+        for (int i = 0; i < steps; ++i) {
+            const Powers w(abc, top, up);
+            p.gram[i] = w.gram;
+            p.square[i] = w.square;
+            p.of_gram[i] = w.of_gram;
+            p.of_one[i] = w.of_one;
+            p.next[i] = w.next;
+            p.last = (float)std::ldexp((double)scale, w.back);
+        }
+        cbm_with_type(type, [&](auto t) {
+            using T = decltype(t);
+            if (l <= 64) cbm_orthogonal_small_kernel<T, 64><<<1, 64 * SMALL_WAVES, 0, stream>>>(p, (const T*)X, ldx, (T*)Y, ldy);
+            else cbm_orthogonal_small_kernel<T, 128><<<1, 64 * SMALL_WAVES, 0, stream>>>(p, (const T*)X, ldx, (T*)Y, ldy);
+        });
+        return cbm_launched("orthogonal update launch");
+    }
     Halves z{(_Float16*)(base + room.z[0]), s, l}, zt{(_Float16*)(base + room.zt[0]), l, s};
     const Halves gram{(_Float16*)(base + room.gram), s, s}, poly{(_Float16*)(base + room.poly), s, s};
     cbm_with_type(type, [&](auto t) {
@@ -404,35 +608,32 @@ cbm_status cbm_launch_orthogonal(int32_t m, int32_t n, int32_t type, const void*
         }
         cbm_orthogonal_begin_kernel<T><<<dim3((unsigned)((l + 31) / 32), (unsigned)((s + 31) / 32)), 256, 0, stream>>>((const T*)X, ldx, tall, eps, (float)std::ldexp(1.0, up), squares, z, zt);
         for (int i = 0; i < steps; ++i) {
-            const int up_gram = power(top * top), up_poly = power(largest(abc, top, false));
-            top = largest(abc, top, true) * (1.0 + 0x1p-10);
-            const int up_next = power(top);
+            const Powers w(abc, top, up);
             ProductArgs p{};
             p.a = p.b = z;
             p.out = gram;
-            p.up = (float)std::ldexp(1.0, up_gram - 2 * up);
+            p.up = w.gram;
             product<GRAM, float>(p, stream);
             p.a = p.b = p.gram = gram;
             p.out = poly;
-            p.up = (float)std::ldexp((double)abc[2], up_poly - 2 * up_gram);
-            p.of_gram = (float)std::ldexp((double)abc[1], up_poly - up_gram);
-            p.of_one = (float)std::ldexp((double)abc[0], up_poly);
+            p.up = w.square;
+            p.of_gram = w.of_gram;
+            p.of_one = w.of_one;
             product<POLYNOMIAL, float>(p, stream);
             p.a = poly;
             p.b = zt;
             if (i + 1 < steps) {
                 p.out = {(_Float16*)(base + room.z[(i + 1) % 2]), s, l};
                 p.outt = {(_Float16*)(base + room.zt[(i + 1) % 2]), l, s};
-                p.up = (float)std::ldexp(1.0, up_next - up - up_poly);
+                p.up = w.next;
                 product<STEP, float>(p, stream);
                 z = p.out;
                 zt = p.outt;
-                up = up_next;
             } else {
                 p.Y = Y;
                 p.ldy = ldy;
                 p.transposed = tall;
-                p.up = (float)std::ldexp((double)scale, -up - up_poly);
+                p.up = (float)std::ldexp((double)scale, w.back);
                 product<LAST, T>(p, stream);
             }
         }
