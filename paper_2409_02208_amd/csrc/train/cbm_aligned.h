@@ -38,9 +38,9 @@ struct CbmAlignedSide {
             row = 8 * (((slot >> 1) ^ 2 * (k & 3)) << 1 | (slot & 1));
         }
     }
-    __device__ __forceinline__ void begin(const CbmOperand<T>& o, int64_t tile, int wave) {
+    __device__ __forceinline__ void begin(const CbmOperand<T>& o, int64_t tile, int wave, int rows = B) {  // tiles of `rows` rows
         const int lane = threadIdx.x & 63;
-        const int64_t first = tile * B;
+        const int64_t first = tile * rows;
         step = (ORDER == ALONG_K ? BK : BK * o.ld[0]) * 2;
         if constexpr (PAIR != PAIR_ROWS)
 #pragma unroll

@@ -230,6 +230,93 @@ struct HalvesTiles : CbmTileSums<B, B, 2, 2> {
     }
 };
 
+// The same for few tiles, of 64 x 64: each of the four waves has all of the tile for a quarter of K, with units of its own in LDS, so that no wave waits for another until they add up.  (500 x 1333's Gram matrix, 36
+// tiles of 42 chunks: waves with a quarter of the tile 21 us, a step of two products between barriers; this 7.)
+struct HalvesShares {
+    typedef CbmAlignedSide<_Float16, 256, ALONG_K, SINGLE> Side;  // (a wave's loads are 64 rows)
+    static constexpr int ROWS = 64, COLUMNS = 64, GROUPS = 1, LOADS = Side::LOADS, SLOT = 64 * 8, OUT_STRIDE = 17, UNITS = 4 * 4 * SLOT;
+    static_assert(LOADS == 8 && UNITS >= 4 * 64 * OUT_STRIDE, "");
+
+    __device__ __forceinline__ void run(uintx4* lds, const CbmOperand<_Float16>& a, const CbmOperand<_Float16>& b, int tile_m, int tile_n, int last) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+        floatx16 acc[2][2] = {};
+        Side sa, sb;
+        sa.begin(a, tile_m, 0, 64);
+        sb.begin(b, tile_n, 0, 64);
+        uintx4 *here = lds + wave * 4 * SLOT, *next = here + 2 * SLOT;
+        auto load = [&](int c, uintx4* to) {  // (zeros beyond the last chunk: as many loads are under way to the end)
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) sa.template load<false>(a, c, a.K, to, 0, i);
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) sb.template load<false>(b, c, b.K, to + SLOT, 0, i);
+        };
+        load(wave, here);
+        load(wave + 4, next);
+        for (int c = wave; c < last; c += 4) {
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS) : "memory");
+            uintx4 x[2][4], y[2][4];
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    x[i][s] = Side::unit(here, 32 * i, s);
+                    y[i][s] = Side::unit(here + SLOT, 32 * i, s);
+                }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            load(c + 8, here);
+#pragma unroll
+            for (int p = 0; p < 6; ++p)  // high by high, high by low, low by high, of either half of the chunk
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) acc[i][j] = cbm_multiply<_Float16>(y[j][p % 2 + (p / 2 == 1 ? 2 : 0)], x[i][p % 2 + (p / 2 == 2 ? 2 : 0)], acc[i][j]);
+            uintx4* t = here;
+            here = next;
+            next = t;
+        }
+        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+        uintx4* mine = lds + wave * 64 * OUT_STRIDE;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    mine[(32 * i + (lane & 31)) * OUT_STRIDE + 8 * j + 2 * q + (lane >> 5)] =
+                        __builtin_bit_cast(uintx4, (floatx4){acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]});
+        __syncthreads();
+    }
+    template <class F, class G>
+    __device__ __forceinline__ void both(uintx4* lds, int tile_m, int tile_n, F&& f, bool down, G&& g) const {
+        const int lane = threadIdx.x & 63, first = 16 * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // a wave's rows
+        const int64_t row = (int64_t)tile_m * 64 + first, column = (int64_t)tile_n * 64;
+#pragma unroll 1
+        for (int t = 0; t < 4; ++t) {
+            const int r = 4 * t + lane / 16, c = lane % 16;
+            uintx4* at = lds + (first + r) * OUT_STRIDE + c;
+            floatx4 sum = __builtin_bit_cast(floatx4, at[0]);
+#pragma unroll
+            for (int w = 1; w < 4; ++w) sum += __builtin_bit_cast(floatx4, at[w * 64 * OUT_STRIDE]);
+            float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+            f(row + r, column + 4 * c, v);
+            at[0] = __builtin_bit_cast(uintx4, (floatx4){v[0], v[1], v[2], v[3]});
+        }
+        if (!down) return;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        const float* of = (const float*)(lds + first * OUT_STRIDE);
+#pragma unroll 1
+        for (int t = 0; t < 4; ++t) {
+            const int r = lane % 4 * 4, c = t * 16 + lane / 4;
+            float v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = of[(r + j) * (4 * OUT_STRIDE) + c];
+            g(column + c, row + r, v);
+        }
+    }
+};
+
 enum { GRAM, POLYNOMIAL, STEP, LAST };
 struct ProductArgs {
     Halves a, b;     // rows of both, along k
@@ -250,9 +337,9 @@ __device__ __forceinline__ void below(int at, int& m, int& n) {
     n = at - (int)((int64_t)m * (m + 1) / 2);
 }
 
-template <int B, int MODE, class T>
-__global__ __launch_bounds__(256, HalvesTiles<B>::GROUPS) void cbm_orthogonal_product_kernel(ProductArgs p) {
-    typedef HalvesTiles<B> Tiles;
+template <class Tiles, int MODE, class T>
+__global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_orthogonal_product_kernel(ProductArgs p) {
+    constexpr int B = Tiles::ROWS;
     __shared__ uintx4 lds[Tiles::UNITS];
     int m, n;
     const int tiles_m = (int)((p.a.rows + B - 1) / B), tiles_n = (int)((p.b.rows + B - 1) / B);
@@ -270,17 +357,15 @@ __global__ __launch_bounds__(256, HalvesTiles<B>::GROUPS) void cbm_orthogonal_pr
     Tiles t;
     t.run(lds, {{p.a.p, nullptr}, {p.a.ld(), 0}, p.a.rows, p.a.ld(), 0}, {{p.b.p, nullptr}, {p.b.ld(), 0}, p.b.rows, p.b.ld(), 0}, m, n, (int)(p.a.ld() / 64));
     if constexpr (MODE == LAST) {
-        t.pieces(lds, m, n, [&](int64_t r, int64_t c, float (&v)[4]) {
-            if (r >= p.a.rows) return;
+        T* Y = (T*)p.Y;
+        t.both(
+            lds, m, n,
+            [&](int64_t r, int64_t c, float (&v)[4]) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] *= p.up;
-            T* Y = (T*)p.Y;
-            if (!p.transposed) cbm_put4<T>(Y + r * p.ldy, c, p.b.rows, v);
-            else
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (c + j < p.b.rows) Y[(c + j) * p.ldy + r] = (T)v[j];
-        });
+                for (int j = 0; j < 4; ++j) v[j] *= p.up;
+                if (!p.transposed && r < p.a.rows) cbm_put4<T>(Y + r * p.ldy, c, p.b.rows, v);
+            },
+            p.transposed, [&](int64_t c, int64_t r, float (&v)[4]) { if (c < p.b.rows) cbm_put4<T>(Y + c * p.ldy, r, p.a.rows, v); });
     } else {
         t.both(
             lds, m, n,
@@ -532,30 +617,29 @@ Room room_of(int64_t s, int64_t l) {
     return r;
 }
 
-// f(tile's side) of the tiles that take least: rounds of workgroups, each its products at what a compute unit's share reaches and what it takes beside them.
+// f(the tiles that take least): rounds of workgroups, each its products at what a compute unit's share reaches and what it takes beside them.
 template <class F>
-void with_tile(int64_t M, int64_t N, int64_t K, bool half, F&& f) {
+void with_tiles(int64_t M, int64_t N, int64_t K, bool half, F&& f) {
     double best = 1e30;
     int side = 256;
     for (int b : {256, 128, 64}) {
-        const int64_t m = (M + b - 1) / b, tiles = half ? m * (m + 1) / 2 : m * ((N + b - 1) / b), at_once = b == 256 ? 256 : 512;
-        const double each = 6.0 * b * b * (double)K / ((b == 256 ? 1250.0 : b == 128 ? 1050.0 : 500.0) * 1e6 / (double)at_once) * (b != 256 && tiles <= 256 ? 0.6 : 1.0);
+        const int64_t m = (M + b - 1) / b, tiles = half ? m * (m + 1) / 2 : m * ((N + b - 1) / b), at_once = b == 128 ? 512 : 256;
+        const double each = 6.0 * b * b * (double)K / ((b == 256 ? 1250.0 : b == 128 ? 1050.0 : 500.0) * 1e6 / (double)at_once) * (b == 128 && tiles <= 256 ? 0.6 : 1.0);
         const double us = (double)((tiles + at_once - 1) / at_once) * (each + (b == 256 ? 12.0 : b == 128 ? 5.0 : 3.0));
         if (us < best) best = us, side = b;
     }
-    using std::integral_constant;
-    if (side == 256) f(integral_constant<int, 256>{});
-    else if (side == 128) f(integral_constant<int, 128>{});
-    else f(integral_constant<int, 64>{});
+    if (side == 256) f((HalvesTiles<256>*)nullptr);
+    else if (side == 128) f((HalvesTiles<128>*)nullptr);
+    else f((HalvesShares*)nullptr);
 }
 
 template <int MODE, class T>
 void product(const ProductArgs& p, hipStream_t stream) {
     const bool half = MODE == GRAM || MODE == POLYNOMIAL;
-    with_tile(p.a.rows, p.b.rows, p.a.columns, half, [&](auto side) {
-        constexpr int B = decltype(side)::value;
-        const int64_t m = (p.a.rows + B - 1) / B, tiles = half ? m * (m + 1) / 2 : m * ((p.b.rows + B - 1) / B);
-        cbm_orthogonal_product_kernel<B, MODE, T><<<(unsigned)((tiles + CBM_XCD - 1) / CBM_XCD * CBM_XCD), 256, 0, stream>>>(p);
+    with_tiles(p.a.rows, p.b.rows, p.a.columns, half, [&](auto* tiles_type) {
+        typedef std::remove_pointer_t<decltype(tiles_type)> Tiles;
+        const int64_t m = (p.a.rows + Tiles::ROWS - 1) / Tiles::ROWS, tiles = half ? m * (m + 1) / 2 : m * ((p.b.rows + Tiles::ROWS - 1) / Tiles::ROWS);
+        cbm_orthogonal_product_kernel<Tiles, MODE, T><<<(unsigned)((tiles + CBM_XCD - 1) / CBM_XCD * CBM_XCD), 256, 0, stream>>>(p);
     });
 }
 
