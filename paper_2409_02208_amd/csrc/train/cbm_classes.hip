@@ -2,6 +2,7 @@
 #include <algorithm>
 
 #include "cbm_aligned.h"
+#include "cbm_few_rows.h"
 #include "cbm_internal.h"
 #include "cbm_products.h"
 
@@ -31,43 +32,69 @@ __global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_classes_kernel(CbmOper
     if (!at.any) return;
     Tiles t;
     t.run(lds, a, b, at.m, at.n, 0, (int)chunks);
-    const int l32 = threadIdx.x & 31, half = threadIdx.x >> 5 & 1;
-    const int64_t c0 = (int64_t)at.n * BN + t.first_column() + 4 * half;  // the lane's first column
-    const int left = (int)min(b.count - c0, (int64_t)4096);                            // and columns from there on
+    // 32 rows at a time through LDS: two lanes a row, each half of the wave's columns
+    constexpr int EACH = Tiles::COLS / 8;  // pieces of four
+    const int lane = threadIdx.x & 63, half = lane & 1;
+    const int64_t c0 = (int64_t)at.n * BN + t.first_column();                   // the wave's first column
+    const int left = (int)min(b.count - c0, (int64_t)4096) - 4 * EACH * half;   // columns from the lane's first on
+    uintx4* band = lds + t.wave() * 32 * Tiles::OUT_STRIDE;
 #pragma unroll
     for (int i = 0; i < Tiles::TM; ++i) {
-        __builtin_amdgcn_sched_barrier(0);  // (32 rows at a time: registers)
-        const int64_t r = (int64_t)at.m * BM + t.first_row() + 32 * i + l32;
-        int64_t given = labels && r < a.count ? label_of(labels, label_bits, r) : -1;
-        if (given >= b.count) given = -1;
-        const int label = (int)max(min(given - c0, (int64_t)4096), (int64_t)-1);
-        Sums all{-INFINITY, 0.0f};
-        float z = 0.0f;
-        int here = left;
-        asm("" : "+v"(here));  // (or a mask for each column stays in scalar registers)
-        auto score = [&](int j, int v) { return 32 * j + 8 * (v / 4) + v % 4 < here ? t.acc[i][j][v] : -INFINITY; };
-#pragma unroll
-        for (int j = 0; j < Tiles::TN; ++j)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                all.m = fmaxf(all.m, score(j, v));
-                z = label == 32 * j + 8 * (v / 4) + v % 4 ? t.acc[i][j][v] : z;
-            }
-        const float away = all.m == -INFINITY ? 0.0f : all.m;
         __builtin_amdgcn_sched_barrier(0);
-        asm("" : "+v"(here));
+        t.band_to_lds(band, i);
+        const int64_t r = (int64_t)at.m * BM + t.first_row() + 32 * i + lane / 2;
+        const uintx4* row = band + lane / 2 * Tiles::OUT_STRIDE;
+        if (labels && half == 0 && r < a.count) {
+            const int64_t label = label_of(labels, label_bits, r), place = label - c0;
+            if (label < b.count && place >= 0 && place < Tiles::COLS) chosen[r] = ((const float*)row)[place];
+        }
+        float z[EACH][4];
 #pragma unroll
-        for (int j = 0; j < Tiles::TN; ++j)
+        for (int k = 0; k < EACH; ++k) t.four(z[k], row[EACH * half + k]);
+        if (c0 + Tiles::COLS > b.count) {
+            int here = left;
+            asm("" : "+v"(here));  // (or a mask for each column stays in scalar registers from band to band)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) all.s += __builtin_amdgcn_exp2f((score(j, v) - away) * LOG2E);
-        Sums low, high;  // the halves' sums, in the same order in both
-        lane_pair<32>(all.m, [&](float x, float y) { low.m = x, high.m = y; return x; });
-        lane_pair<32>(all.s, [&](float x, float y) { low.s = x, high.s = y; return x; });
-        all = joined(low, high);
-        if (r >= a.count) continue;
-        if (half == 0) parts[r * (tiles_n * WN) + at.n * WN + t.across()] = all;
-        if (label >= 0 && label < 32 * Tiles::TN && !(label & 4)) chosen[r] = z;
+            for (int k = 0; k < EACH; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) z[k][j] = 4 * k + j < here ? z[k][j] : -INFINITY;
+        }
+        Sums all{-INFINITY, 0.0f};
+#pragma unroll
+        for (int k = 0; k < EACH; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) all.m = fmaxf(all.m, z[k][j]);
+        const float away = all.m == -INFINITY ? 0.0f : all.m;
+#pragma unroll
+        for (int k = 0; k < EACH; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) all.s += __builtin_amdgcn_exp2f((z[k][j] - away) * LOG2E);
+        const Sums other{lane_other<1>(all.m), lane_other<1>(all.s)};
+        all = half ? joined(other, all) : joined(all, other);
+        if (r < a.count && half == 0) parts[r * (tiles_n * WN) + at.n * WN + t.across()] = all;
+        __builtin_amdgcn_wave_barrier();
     }
+}
+
+// A few rows: W is read once, a workgroup for each 128 bytes of columns, whose scores of a row are a part.
+constexpr int FEW_WAVES = 8;
+template <class T, int NR>
+__global__ __launch_bounds__(64 * FEW_WAVES) void cbm_classes_few_kernel(int64_t n, int64_t d, int64_t c, const T* __restrict__ X, int64_t ldx, const T* __restrict__ W, int64_t ldw,
+                                                                      const void* __restrict__ labels, int label_bits, Sums* __restrict__ parts, float* __restrict__ chosen) {
+    typedef CbmFewRows<T, NR, 1, 8, FEW_WAVES> Rows;
+    __shared__ typename Rows::Room room;
+    const int64_t piece = cbm_few_piece(), first = piece * Rows::COLS, above = (int64_t)blockIdx.y * NR;
+    if (first >= c) return;
+    Rows::run(room, X + above * ldx, ldx, n - above, d, {W}, {ldw}, c, first);
+    const int in = threadIdx.x >> 6, lane = threadIdx.x & 63;  // a wave a row
+    const int64_t r = above + in;
+    if (r >= n || in >= NR) return;
+    const bool some = lane < Rows::COLS && first + lane < c;
+    const float z = some ? Rows::total(room, 0, in, lane < Rows::COLS ? lane : 0) : -INFINITY;
+    const float m = lanes_all<64>(z, [](float a, float b) { return fmaxf(a, b); }), away = m == -INFINITY ? 0.0f : m;
+    const float s = lanes_sum<64>(__builtin_amdgcn_exp2f((z - away) * LOG2E));
+    if (lane == 0) parts[r * ((c + Rows::COLS - 1) / Rows::COLS) + piece] = {m, s};
+    if (labels && some && label_of(labels, label_bits, r) == first + lane) chosen[r] = z;
 }
 
 // A wave a row: its parts in order, a lane's 64 apart, then over the lanes.
@@ -120,6 +147,8 @@ __global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_classes_slopes_kernel(
     Tiles t;
     t.run(lds, a, b, at.m, at.n, 0, (int)chunks);
     const int l32 = threadIdx.x & 31, half = threadIdx.x >> 5 & 1;
+    int hot[Tiles::TM];
+    float up[Tiles::TM];
 #pragma unroll
     for (int i = 0; i < Tiles::TM; ++i) {
         __builtin_amdgcn_sched_barrier(0);  // (32 rows at a time: registers)
@@ -127,22 +156,26 @@ __global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_classes_slopes_kernel(
         const int64_t at_r = min(r, a.count - 1), label = label_of(labels, label_bits, at_r);
         const float m = stats[2 * at_r], l = stats[2 * at_r + 1];
         const bool none = label < 0 || label >= c || m == -INFINITY;
-        float up = dlogp[at_r];
-        if (scale) up *= scale[1];
-        const int mine = (int)max(min(label - first - ((int64_t)at.n * BN + t.first_column() + 4 * half), (int64_t)4096), (int64_t)-1);  // the label's place among the lane's columns
+        const float slope = none ? 0.0f : scale ? dlogp[at_r] * scale[1] : dlogp[at_r], from = none ? 0.0f : m, down = none ? -INFINITY : -l * LOG2E;
+        const int64_t place = label - first - ((int64_t)at.n * BN + t.first_column());
+        hot[i] = none || place < 0 || place >= 32 * Tiles::TN ? -1 : (int)place;  // the label's place among the wave's columns
+        up[i] = slope;
 #pragma unroll
         for (int j = 0; j < Tiles::TN; ++j)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const float p = __builtin_amdgcn_exp2f(((t.acc[i][j][v] - m) - l) * LOG2E);
-                t.acc[i][j][v] = none ? 0.0f : up * ((mine == 32 * j + 8 * (v / 4) + v % 4 ? 1.0f : 0.0f) - p);
-            }
+            for (int v = 0; v < 16; ++v) t.acc[i][j][v] = -slope * __builtin_amdgcn_exp2f(fmaf(t.acc[i][j][v] - from, LOG2E, down));
     }
-    t.pieces(lds, at.m, at.n, [&](int64_t r, int64_t col, float (&v)[4]) {
-        if (r < a.count) cbm_put4<T>(dZ + r * lddz, col, b.count, v);
-    });
+    t.pieces(
+        lds, at.m, at.n, [&](int64_t r, int64_t col, float (&v)[4]) {
+            if (r < a.count) cbm_put4<T>(dZ + r * lddz, col, b.count, v);
+        },
+        [&](int i, float* row) {  // a lane's row in LDS: the label's own
+            if (half == 0 && hot[i] >= 0) row[hot[i]] += up[i];
+        });
 }
 
+// parts of a row's scores: of 32 columns at least where rows are few, of 64 else
+int64_t most_parts(int64_t n, int32_t c) { return std::max(n <= cbm_most_few_rows<float> ? ((int64_t)c + 31) / 32 : 0, ((int64_t)c + 127) / 128 * 2); }
 int64_t rounded16(int64_t bytes) { return (bytes + 15) / 16 * 16; }
 int64_t bytes_of(int32_t type) { return type == CBM_F32 ? 4 : 2; }
 
@@ -190,7 +223,7 @@ void with_tiles(int64_t n, int64_t d, int64_t c, const CbmOperand<T>& a, const C
 
 }  // namespace
 
-int64_t cbm_classes_workspace(int64_t n, int32_t, int32_t c, int32_t) { return rounded16(n * (((int64_t)c + 127) / 128 * 2) * (int64_t)sizeof(Sums)) + 4 * n; }
+int64_t cbm_classes_workspace(int64_t n, int32_t, int32_t c, int32_t) { return rounded16(n * most_parts(n, c) * (int64_t)sizeof(Sums)) + 4 * n; }
 
 cbm_status cbm_launch_classes(int64_t n, int32_t d, int32_t c, int32_t type, const void* X, int64_t ldx, const void* W, int64_t ldw, const void* labels, int label_bits, float* logp, float* stats,
                               void* workspace, void* stream_) {
@@ -198,10 +231,18 @@ cbm_status cbm_launch_classes(int64_t n, int32_t d, int32_t c, int32_t type, con
     if (n == 0) return CBM_OK;
     int64_t count = 0;  // parts of a row: of the waves along a tile's columns
     Sums* parts = (Sums*)workspace;
-    float* chosen = (float*)((char*)workspace + rounded16(n * (((int64_t)c + 127) / 128 * 2) * (int64_t)sizeof(Sums)));
+    float* chosen = (float*)((char*)workspace + rounded16(n * most_parts(n, c) * (int64_t)sizeof(Sums)));
     cbm_with_type(type, [&](auto t) {
         using T = decltype(t);
         const CbmOperand<T> a{{(const T*)X, nullptr}, {ldx, 0}, n, d, 0}, b{{(const T*)W, nullptr}, {ldw, 0}, c, d, 0};
+        constexpr int V = 16 / (int)sizeof(T);
+        if (n <= cbm_most_few_rows<T> && c >= V) {
+            count = ((int64_t)c + 8 * V - 1) / (8 * V);
+            cbm_with_few_rows(n, [&](auto rows) {
+                cbm_classes_few_kernel<T, decltype(rows)::value><<<dim3((unsigned)((count + 7) / 8 * 8), (unsigned)((n + CBM_FEW_ROWS - 1) / CBM_FEW_ROWS)), 64 * FEW_WAVES, 0, stream>>>(n, d, c, (const T*)X, ldx, (const T*)W, ldw, logp ? labels : nullptr, label_bits, parts, chosen);
+            });
+            return;
+        }
         with_tiles<T>(n, d, c, a, b, type, [&](auto* tiles_type, unsigned grid, int64_t chunks) {
             typedef std::remove_pointer_t<decltype(tiles_type)> Tiles;
             count = ((int64_t)c + Tiles::COLUMNS - 1) / Tiles::COLUMNS * Tiles::ACROSS;

@@ -2,6 +2,7 @@
 #include <algorithm>
 
 #include "cbm_aligned.h"
+#include "cbm_few_rows.h"
 #include "cbm_internal.h"
 #include "cbm_products.h"
 
@@ -57,6 +58,26 @@ __global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_gated_kernel(CbmOperan
     });
 }
 
+// A few rows: the weights are read once, in pieces of 64 bytes of a row, a workgroup for each 64 bytes of columns.
+constexpr int few_waves(int rows) { return rows >= 8 ? 8 : 16; }
+template <class T, int NR, int ACT>
+__global__ __launch_bounds__(64 * few_waves(NR)) void cbm_gated_few_kernel(int64_t n, int64_t k, int64_t m, const T* __restrict__ X, int64_t ldx, const T* __restrict__ Wg, int64_t ldwg,
+                                                                    const T* __restrict__ Wu, int64_t ldwu, T* __restrict__ H, int64_t ldh, T* __restrict__ G, int64_t ldg, T* __restrict__ U,
+                                                                    int64_t ldu) {
+    typedef CbmFewRows<T, NR, 2, 4, few_waves(NR)> Rows;
+    __shared__ typename Rows::Room room;
+    const int64_t first = cbm_few_piece() * Rows::COLS, above = (int64_t)blockIdx.y * NR;
+    if (first >= m) return;
+    Rows::run(room, X + above * ldx, ldx, n - above, k, {Wg, Wu}, {ldwg, ldwu}, m, first);
+    const int in = threadIdx.x / Rows::COLS, j = threadIdx.x % Rows::COLS;
+    const int64_t c = first + j, r = above + in;
+    if (r >= n || in >= NR || c >= m) return;
+    const float g = Rows::total(room, 0, in, j), u = Rows::total(room, 1, in, j);
+    H[r * ldh + c] = (T)(activated<ACT>(g) * u);
+    if (G) G[r * ldg + c] = (T)g;
+    if (U) U[r * ldu + c] = (T)u;
+}
+
 // dG and dU side by side in `out`, from column 0 and column `at` on, rounded to the type (half a step each, as much as the gradients that are made of them are rounded by); zeros between.
 template <class T, int ACT>
 __global__ __launch_bounds__(256) void cbm_gated_slopes_kernel(int64_t n, int m, const T* __restrict__ dH, int64_t lddh, const T* __restrict__ G, int64_t ldg, const T* __restrict__ U,
@@ -105,6 +126,16 @@ cbm_status cbm_launch_gated(int64_t n, int32_t k, int32_t m, int32_t type, int32
     cbm_with_type(type, [&](auto t) {
         using T = decltype(t);
         const CbmOperand<T> a{{(const T*)X, nullptr}, {ldx, 0}, n, k, 0}, b{{(const T*)Wg, (const T*)Wu}, {ldwg, ldwu}, m, k, 0};
+        constexpr int V = 16 / (int)sizeof(T);
+        if (n <= cbm_most_few_rows<T> && m >= V) {
+            cbm_with_few_rows(n, [&](auto rows) {
+                with_activation(act, [&](auto which) {
+                    cbm_gated_few_kernel<T, decltype(rows)::value, decltype(which)::value><<<dim3((unsigned)(((int64_t)m + 32 * V - 1) / (32 * V) * 8), (unsigned)((n + CBM_FEW_ROWS - 1) / CBM_FEW_ROWS)), 64 * few_waves(decltype(rows)::value), 0, (hipStream_t)stream>>>(
+                        n, k, m, (const T*)X, ldx, (const T*)Wg, ldwg, (const T*)Wu, ldwu, (T*)H, ldh, (T*)G, ldg, (T*)U, ldu);
+                });
+            });
+            return;
+        }
         auto run = [&](auto* tiles_type) {
             typedef std::remove_pointer_t<decltype(tiles_type)> Tiles;
             const int64_t tiles = (n + Tiles::ROWS - 1) / Tiles::ROWS * (((int64_t)m + Tiles::COLUMNS / 2 - 1) / (Tiles::COLUMNS / 2));

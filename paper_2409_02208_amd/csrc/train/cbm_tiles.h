@@ -223,14 +223,23 @@ struct CbmTileSums {
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] = x[j];
     }
-    template <class F>
-    __device__ __forceinline__ void pieces(uintx4* lds, int64_t tile_m, int64_t tile_n, F&& f) const {
+    struct Nothing {
+        __device__ __forceinline__ void operator()(int, float*) const {}
+    };
+    // change(i, row): of lanes 0 .. 31, band i's sums of the lane's row before f sees them
+    template <class F, class G = Nothing>
+    __device__ __forceinline__ void pieces(uintx4* lds, int64_t tile_m, int64_t tile_n, F&& f, G&& change = G()) const {
         const int lane = threadIdx.x & 63;
         uintx4* mine = lds + wave() * 32 * OUT_STRIDE;
         const int64_t row = tile_m * BM + first_row(), column = tile_n * BN + first_column();
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             band_to_lds(mine, i);
+            if constexpr (!std::is_same<std::remove_reference_t<G>, Nothing>::value) {
+                change(i, (float*)(mine + (lane & 31) * OUT_STRIDE));
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            }
 #pragma unroll 1
             for (int t = 0; t < COLS / 8; ++t) {
                 const int at = 64 * t + lane, r = at / (COLS / 4), c = at % (COLS / 4);
