@@ -50,7 +50,7 @@ __global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_classes_kernel(CbmOper
         }
         float z[EACH][4];
 #pragma unroll
-        for (int k = 0; k < EACH; ++k) t.four(z[k], row[EACH * half + k]);
+        for (int k = 0; k < EACH; ++k) t.from_lds(z[k], row + EACH * half + k);
         if (c0 + Tiles::COLS > b.count) {
             int here = left;
             asm("" : "+v"(here));  // (or a mask for each column stays in scalar registers from band to band)
@@ -165,9 +165,10 @@ __global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_classes_slopes_kernel(
 #pragma unroll
             for (int v = 0; v < 16; ++v) t.acc[i][j][v] = -slope * __builtin_amdgcn_exp2f(fmaf(t.acc[i][j][v] - from, LOG2E, down));
     }
-    t.pieces(
-        lds, at.m, at.n, [&](int64_t r, int64_t col, float (&v)[4]) {
-            if (r < a.count) cbm_put4<T>(dZ + r * lddz, col, b.count, v);
+    constexpr int W = cbm_wide<T>;
+    t.template pieces<W>(
+        lds, at.m, at.n, [&](int64_t r, int64_t col, float (&v)[W]) {
+            if (r < a.count) cbm_put(dZ + r * lddz, col, b.count, v);
         },
         [&](int i, float* row) {  // a lane's row in LDS: the label's own
             if (half == 0 && hot[i] >= 0) row[hot[i]] += up[i];

@@ -41,20 +41,21 @@ void with_activation(int32_t act, F&& f) {
 // Both projections in one product: a wave's tiles of 32 columns come from Wg and Wu in turn, so a lane has both sums of a value of H.
 template <class Tiles, class T, int ACT>
 __global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_gated_kernel(CbmOperand<T> a, CbmOperand<T> b, int64_t chunks, T* __restrict__ H, int64_t ldh, T* __restrict__ G, int64_t ldg,
-                                                                    T* __restrict__ U, int64_t ldu) {
+                                                                    T* __restrict__ U, int64_t ldu, bool far) {
     __shared__ uintx4 lds[Tiles::UNITS];
     const CbmTilePlace at = cbm_tile_place((a.count + Tiles::ROWS - 1) / Tiles::ROWS, (b.count + Tiles::COLUMNS / 2 - 1) / (Tiles::COLUMNS / 2), 1);
     if (!at.any) return;
     Tiles t;
     t.run(lds, a, b, at.m, at.n, 0, (int)chunks);
-    t.pairs(lds, at.m, at.n, [&](int64_t r, int64_t c, float (&g)[4], float (&u)[4]) {
+    constexpr int W = cbm_wide<T>;
+    t.template pairs<W>(lds, at.m, at.n, [&](int64_t r, int64_t c, float (&g)[W], float (&u)[W]) {
         if (r >= a.count) return;
-        float h[4];
+        float h[W];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) h[v] = activated<ACT>(g[v]) * u[v];
-        cbm_put4<T>(H + r * ldh, c, b.count, h);
-        if (G) cbm_put4<T>(G + r * ldg, c, b.count, g);
-        if (U) cbm_put4<T>(U + r * ldu, c, b.count, u);
+        for (int v = 0; v < W; ++v) h[v] = activated<ACT>(g[v]) * u[v];
+        cbm_put(H + r * ldh, c, b.count, h, far);
+        if (G) cbm_put(G + r * ldg, c, b.count, g, far);
+        if (U) cbm_put(U + r * ldu, c, b.count, u, far);
     });
 }
 
@@ -141,7 +142,7 @@ cbm_status cbm_launch_gated(int64_t n, int32_t k, int32_t m, int32_t type, int32
             const int64_t tiles = (n + Tiles::ROWS - 1) / Tiles::ROWS * (((int64_t)m + Tiles::COLUMNS / 2 - 1) / (Tiles::COLUMNS / 2));
             with_activation(act, [&](auto which) {
                 cbm_gated_kernel<Tiles, T, decltype(which)::value><<<(unsigned)((tiles + CBM_XCD - 1) / CBM_XCD * CBM_XCD), 256, 0, (hipStream_t)stream>>>(
-                    a, b, (k + Tiles::BK - 1) / Tiles::BK, (T*)H, ldh, (T*)G, ldg, (T*)U, ldu);
+                    a, b, (k + Tiles::BK - 1) / Tiles::BK, (T*)H, ldh, (T*)G, ldg, (T*)U, ldu, n * m * (int64_t)sizeof(T) >= CBM_FAR_BYTES);
             });
         };
         if constexpr (sizeof(T) == 2)

@@ -208,7 +208,7 @@ struct HalvesTiles : CbmTileSums<B, B, 2, 2> {
             for (int t = 0; t < Sums::COLS / 8; ++t) {
                 const int at = 64 * t + lane, r = at / (Sums::COLS / 4), c = at % (Sums::COLS / 4);
                 float v[4];
-                Sums::four(v, mine[r * Sums::OUT_STRIDE + c]);
+                Sums::from_lds(v, mine + r * Sums::OUT_STRIDE + c);
                 f(row + 32 * i + r, column + 4 * c, v);
                 if (down) mine[r * Sums::OUT_STRIDE + c] = __builtin_bit_cast(uintx4, (floatx4){v[0], v[1], v[2], v[3]});  // (as f left them)
             }
@@ -363,9 +363,9 @@ __global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_orthogonal_product_ker
             [&](int64_t r, int64_t c, float (&v)[4]) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[j] *= p.up;
-                if (!p.transposed && r < p.a.rows) cbm_put4<T>(Y + r * p.ldy, c, p.b.rows, v);
+                if (!p.transposed && r < p.a.rows) cbm_put(Y + r * p.ldy, c, p.b.rows, v);
             },
-            p.transposed, [&](int64_t c, int64_t r, float (&v)[4]) { if (c < p.b.rows) cbm_put4<T>(Y + c * p.ldy, r, p.a.rows, v); });
+            p.transposed, [&](int64_t c, int64_t r, float (&v)[4]) { if (c < p.b.rows) cbm_put(Y + c * p.ldy, r, p.a.rows, v); });
     } else {
         t.both(
             lds, m, n,
@@ -542,7 +542,7 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void cbm_orthogonal_small_kernel(
             }
             const int lane = threadIdx.x & 63, r = m + (lane & 15), c = n + (lane >> 4) * 4;
             if (r >= p.rows) continue;
-            if (!p.transposed) cbm_put4<T>(Y + r * ldy, c, p.columns, out);
+            if (!p.transposed) cbm_put(Y + r * ldy, c, p.columns, out);
             else
 #pragma unroll
                 for (int j = 0; j < 4; ++j)

@@ -8,24 +8,24 @@
 
 namespace {
 
-template <class TO>
-__device__ __forceinline__ void finish(const CbmProductOut& o, int64_t M, int64_t N, int64_t r, int64_t c, float (&v)[4]) {
+template <class TO, int W>
+__device__ __forceinline__ void finish(const CbmProductOut& o, int64_t M, int64_t N, int64_t r, int64_t c, float (&v)[W]) {
     if (r >= M || c >= N) return;
     if (o.sums) {
         float* s = o.sums + r * N + c;
         if (!o.first)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < W; ++j)
                 if (c + j < N) v[j] += s[j];
-        if (!o.last) return cbm_put4<float>(o.sums + r * N, c, N, v);
+        if (!o.last) return cbm_put<W>(o.sums + r * N, c, N, v);
     }
     float up = o.alpha;
     if (o.factor) up *= *o.factor;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] *= up;
+    for (int j = 0; j < W; ++j) v[j] *= up;
     if (o.more)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < W; ++j)
             if (c + j < N) v[j] = fmaf(o.beta, o.more[r * o.ldm + c + j], v[j]);
     const bool second = o.at && c >= o.at;
     if (second) c -= o.at;
@@ -34,10 +34,10 @@ __device__ __forceinline__ void finish(const CbmProductOut& o, int64_t M, int64_
     if (!C) return;
     if (o.transposed) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < W; ++j)
             if (c + j < o.columns) C[(c + j) * ld + r] = (TO)v[j];
     } else {
-        cbm_put4<TO>(C + r * ld, c, o.columns, v);
+        cbm_put<W>(C + r * ld, c, o.columns, v);
     }
 }
 
@@ -48,9 +48,10 @@ __global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_product_kernel(CbmOper
     if (!at.any) return;
     Tiles t;
     t.run(lds, a, b, at.m, at.n, (int)(chunks * at.split / splits), (int)(chunks * (at.split + 1) / splits));
-    t.pieces(lds, at.m, at.n, [&](int64_t r, int64_t c, float (&v)[4]) {
+    constexpr int W = cbm_wide<TO>;
+    t.template pieces<W>(lds, at.m, at.n, [&](int64_t r, int64_t c, float (&v)[W]) {
         if (splits > 1) {
-            if (r < a.count) cbm_put4<float>(parts + (at.split * a.count + r) * b.count, c, b.count, v);
+            if (r < a.count) cbm_put<W>(parts + (at.split * a.count + r) * b.count, c, b.count, v);
         } else {
             finish<TO>(o, a.count, b.count, r, c, v);
         }

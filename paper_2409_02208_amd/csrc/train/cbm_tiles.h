@@ -218,16 +218,20 @@ struct CbmTileSums {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     }
-    static __device__ __forceinline__ void four(float (&v)[4], uintx4 u) {
-        const floatx4 x = __builtin_bit_cast(floatx4, u);
+    template <int W>
+    static __device__ __forceinline__ void from_lds(float (&v)[W], const uintx4* p) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = x[j];
+        for (int k = 0; k < W / 4; ++k) {
+            const floatx4 x = __builtin_bit_cast(floatx4, p[k]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[4 * k + j] = x[j];
+        }
     }
     struct Nothing {
         __device__ __forceinline__ void operator()(int, float*) const {}
     };
-    // change(i, row): of lanes 0 .. 31, band i's sums of the lane's row before f sees them
-    template <class F, class G = Nothing>
+    // W sums a lane at a time.  change(i, row): of lanes 0 .. 31, band i's sums of the lane's row before f sees them
+    template <int W, class F, class G = Nothing>
     __device__ __forceinline__ void pieces(uintx4* lds, int64_t tile_m, int64_t tile_n, F&& f, G&& change = G()) const {
         const int lane = threadIdx.x & 63;
         uintx4* mine = lds + wave() * 32 * OUT_STRIDE;
@@ -241,17 +245,17 @@ struct CbmTileSums {
                 __builtin_amdgcn_wave_barrier();
             }
 #pragma unroll 1
-            for (int t = 0; t < COLS / 8; ++t) {
-                const int at = 64 * t + lane, r = at / (COLS / 4), c = at % (COLS / 4);
-                float v[4];
-                four(v, mine[r * OUT_STRIDE + c]);
-                f(row + 32 * i + r, column + 4 * c, v);
+            for (int t = 0; t < COLS / 2 / W; ++t) {
+                const int at = 64 * t + lane, r = at / (COLS / W), c = at % (COLS / W);
+                float v[W];
+                from_lds(v, mine + r * OUT_STRIDE + W / 4 * c);
+                f(row + 32 * i + r, column + W * c, v);
             }
             __builtin_amdgcn_wave_barrier();
         }
     }
-    // PAIR_ROWS: f(row, column, four sums of the first matrix's columns, of the second's)
-    template <class F>
+    // PAIR_ROWS: f(row, column, W sums of the first matrix's columns, of the second's)
+    template <int W, class F>
     __device__ __forceinline__ void pairs(uintx4* lds, int64_t tile_m, int64_t tile_n, F&& f) const {
         const int lane = threadIdx.x & 63;
         uintx4* mine = lds + wave() * 32 * OUT_STRIDE;
@@ -259,12 +263,12 @@ struct CbmTileSums {
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             band_to_lds(mine, i);
-#pragma unroll 2
-            for (int t = 0; t < COLS / 16; ++t) {
-                const int at = 64 * t + lane, r = at / (COLS / 8), c = at % (COLS / 8), p = r * OUT_STRIDE + c / 8 * 16 + c % 8;
-                float x[4], y[4];
-                four(x, mine[p]);
-                four(y, mine[p + 8]);
+#pragma unroll 1
+            for (int t = 0; t < COLS / 4 / W; ++t) {
+                const int at = 64 * t + lane, r = at / (COLS / 2 / W), c = at % (COLS / 2 / W) * (W / 4), p = r * OUT_STRIDE + c / 8 * 16 + c % 8;
+                float x[W], y[W];
+                from_lds(x, mine + p);
+                from_lds(y, mine + p + 8);
                 f(row + 32 * i + r, column + 4 * c, x, y);
             }
             __builtin_amdgcn_wave_barrier();
@@ -364,14 +368,17 @@ __device__ __forceinline__ CbmTilePlace cbm_tile_place(int64_t tiles_m, int64_t 
     return {whole(8 * group + in % high), whole(in / high), whole(split), split < (uint32_t)splits};
 }
 
-// Four values of a row of `columns` from `c` on (none beyond them).
-template <class T>
-__device__ __forceinline__ void cbm_put4(T* row, int64_t c, int64_t columns, const float (&v)[4]) {
-    if (c + 4 <= columns) {
-        store_piece<4>(row + c, v);
+// W values of a row of `columns` from `c` on (none beyond them); far: past the caches.
+template <int W, class T>
+__device__ __forceinline__ void cbm_put(T* row, int64_t c, int64_t columns, const float (&v)[W], bool far = false) {
+    if (c + W <= columns) {
+        store_piece<W>(row + c, v, far);
     } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < W; ++j)
             if (c + j < columns) row[c + j] = (T)v[j];
     }
 }
+// values of 16 bytes
+template <class T>
+constexpr int cbm_wide = 16 / (int)sizeof(T);
