@@ -140,7 +140,7 @@ template <class Tiles, class T>
 __global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_classes_slopes_kernel(CbmOperand<T> a, CbmOperand<T> b, int64_t chunks, int64_t first, int64_t c, const void* __restrict__ labels, int label_bits,
                                                                  const float* __restrict__ stats, const float* __restrict__ dlogp, const float* __restrict__ scale, T* __restrict__ dZ,
                                                                  int64_t lddz) {
-    constexpr int BM = Tiles::ROWS, BN = Tiles::COLUMNS, WN = Tiles::ACROSS;
+    constexpr int BM = Tiles::ROWS, BN = Tiles::COLUMNS;
     __shared__ uintx4 lds[Tiles::UNITS];
     const CbmTilePlace at = cbm_tile_place((a.count + BM - 1) / BM, (b.count + BN - 1) / BN, 1);
     if (!at.any) return;
@@ -168,7 +168,7 @@ __global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_classes_slopes_kernel(
     constexpr int W = cbm_wide<T>;
     t.template pieces<W>(
         lds, at.m, at.n, [&](int64_t r, int64_t col, float (&v)[W]) {
-            if (r < a.count) cbm_put(dZ + r * lddz, col, b.count, v);
+            if (r < a.count) cbm_put(dZ + r * lddz, col, b.count, v, true);
         },
         [&](int i, float* row) {  // a lane's row in LDS: the label's own
             if (half == 0 && hot[i] >= 0) row[hot[i]] += up[i];

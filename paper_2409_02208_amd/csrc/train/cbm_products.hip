@@ -113,7 +113,7 @@ Plan plan(int64_t M, int64_t N, int64_t K, int32_t type, int tile) {
     const double tflops = tile == 256 ? 1150.0 : tile == 128 ? 900.0 : type == CBM_F32 ? 140.0 : 550.0, beside = tile == 256 ? 9.0 : 5.0;
     const double each = 2.0 * (double)(side * side * K) / (tflops * 1e6 / (double)at_once);
     Plan best{tile, 1, 1e30};
-    for (int64_t s = 1; s <= 64 && (s == 1 || (s * 256 <= K && tiles <= 1024)); ++s) {
+    for (int64_t s = 1; s <= 128 && (s == 1 || (s * 256 <= K && tiles <= 1024)); ++s) {
         const double rounds = (double)((tiles * s + at_once - 1) / at_once);
         const double us = rounds * (each / (double)s + beside) + (s > 1 ? 4.0 + 8.0 * (double)(s * M * N) / 4e6 : 0.0);
         if (us < 0.97 * best.us) best = {tile, s, us};

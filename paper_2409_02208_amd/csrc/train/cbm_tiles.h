@@ -39,9 +39,9 @@ template <class T, int B, int THREADS, CbmTileOrder ORDER, CbmTilePair PAIR>
 struct CbmTileSide {
     static constexpr int PARTS = CbmTileType<T>::PARTS, KG = CbmTileType<T>::KG, BK = 8 * KG;
     static constexpr int EACH = B * KG / THREADS;  // units a thread stages
-    // Places of units in LDS: neighbouring rows, neighbouring groups of eight rows and neighbouring k each fall on different banks.
-    static constexpr int STRIDE = B + 9, PLANE = KG * STRIDE, UNITS = PARTS * PLANE;
-    static __device__ __forceinline__ int place(int kg, int row) { return kg * STRIDE + (row & 7) * (B / 8 + 1) + (row >> 3); }
+    // Places of units in LDS: sixteen neighbouring rows, sixteen groups of four rows (or of two) and four rows of four k each fall on different banks.
+    static constexpr int STRIDE = B + 17, PLANE = KG * STRIDE, UNITS = PARTS * PLANE;
+    static __device__ __forceinline__ int place(int kg, int row) { return kg * STRIDE + (row & 3) * (B / 4 + 4) + (row >> 2); }
     static_assert(B * KG % THREADS == 0 && THREADS % KG == 0, "");
     typedef typename Piece<T, EACH>::type Across;
     typedef typename Piece<T, 16 / (int)sizeof(T)>::type Quad;  // 16 bytes
@@ -51,7 +51,7 @@ struct CbmTileSide {
     const T* second[PAIR == PAIR_K ? EACH : 1];
     int64_t ld;
     int shift;     // ACROSS_K: columns that the thread loads and another one has: its own come after them
-    bool element;  // ACROSS_K: fewer columns than a thread has
+    bool element = false;  // ACROSS_K: fewer columns than a thread has
     int most;      // the last column, as seen from the thread's first (element)
     int kg0, row0;
     union {
@@ -83,16 +83,16 @@ struct CbmTileSide {
             base[0] = o.p[which] + from + 8 * kg0 * ld;
         }
     }
+    // the thread's units of the chunk at k0
     __device__ __forceinline__ void load(const CbmOperand<T>& o, int64_t k0) {
-        int64_t K = o.K;
+        const int64_t K = o.K;
         if constexpr (ORDER == ALONG_K) {
             const bool other = PAIR == PAIR_K && k0 >= o.at;
             if (other) k0 -= o.at;
-            const bool whole = k0 + BK <= K;
 #pragma unroll
             for (int i = 0; i < EACH; ++i) {
                 const T* p = (PAIR == PAIR_K && other ? second[PAIR == PAIR_K ? i : 0] : base[i]) + k0;
-                if (whole || k0 + 8 * kg0 + 8 <= K) {
+                if (k0 + BK <= K || k0 + 8 * kg0 + 8 <= K) {
 #pragma unroll
                     for (int q = 0; q < QUADS; ++q) raw.along[i][q] = *reinterpret_cast<const Quad*>(p + q * (16 / (int)sizeof(T)));
                 } else {
@@ -142,39 +142,28 @@ struct CbmTileSide {
 #pragma unroll
         for (int i = 0; i < 3; ++i) lds[i * PLANE + at] = q[i];
     }
-    __device__ __forceinline__ void store(uintx4* lds, uint32_t minus_low) {
-        if constexpr (ORDER == ALONG_K) {
+    // unit i to LDS
+    __device__ __forceinline__ void store(uintx4* lds, uint32_t minus_low, int i) {
+        const int at = ORDER == ALONG_K ? place(kg0, row0 + i * (THREADS / KG))
+                       : i < shift      ? kg0 * STRIDE + B + 16  // (columns that another thread has go to a place that nobody reads)
+                                        : place(kg0, row0 + i - shift);
+        if constexpr (PARTS == 1) {
+            if constexpr (ORDER == ALONG_K) {
+                lds[at] = __builtin_bit_cast(uintx4, raw.along[i][0]);
+            } else {
+                typedef uint32_t Words __attribute__((ext_vector_type(EACH / 2)));
+                uintx4 q;
 #pragma unroll
-            for (int i = 0; i < EACH; ++i) {
-                const int at = place(kg0, row0 + i * (THREADS / KG));
-                if constexpr (PARTS == 1) {
-                    lds[at] = __builtin_bit_cast(uintx4, raw.along[i][0]);
-                } else {
-                    float x[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] = raw.along[i][j / 4][j % 4];
-                    put(lds, at, x, minus_low);
-                }
+                for (int j = 0; j < 4; ++j)
+                    q[j] = __builtin_amdgcn_perm(__builtin_bit_cast(Words, raw.across[2 * j + 1])[i / 2], __builtin_bit_cast(Words, raw.across[2 * j])[i / 2],
+                                                 i % 2 ? 0x07060302u : 0x05040100u);
+                lds[at] = q;
             }
         } else {
+            float x[8];
 #pragma unroll
-            for (int i = 0; i < EACH; ++i) {
-                const int at = i < shift ? kg0 * STRIDE + B + 7 : place(kg0, row0 + i - shift);  // (columns that another thread has go to a place that nobody reads)
-                if constexpr (PARTS == 1) {
-                    typedef uint32_t Words __attribute__((ext_vector_type(EACH / 2)));
-                    uintx4 q;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        q[j] = __builtin_amdgcn_perm(__builtin_bit_cast(Words, raw.across[2 * j + 1])[i / 2], __builtin_bit_cast(Words, raw.across[2 * j])[i / 2],
-                                                     i % 2 ? 0x07060302u : 0x05040100u);
-                    lds[at] = q;
-                } else {
-                    float x[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] = raw.across[j][i];
-                    put(lds, at, x, minus_low);
-                }
-            }
+            for (int j = 0; j < 8; ++j) x[j] = ORDER == ALONG_K ? (float)raw.along[i][j / 4][j % 4] : (float)raw.across[j][i];
+            put(lds, at, x, minus_low);
         }
     }
 };
@@ -308,15 +297,19 @@ struct CbmTiles : CbmTileSums<BM, BN, WM, WN> {
             sb.load(b, (int64_t)first * BK);
         }
         for (int c = first; c < last; ++c) {
-            sa.store(la, minus_low);
-            sb.store(lb, minus_low);
+#pragma unroll
+            for (int i = 0; i < A::EACH; ++i) sa.store(la, minus_low, i);
+#pragma unroll
+            for (int i = 0; i < B::EACH; ++i) sb.store(lb, minus_low, i);
             __syncthreads();
             if (c + 1 < last) {
                 sa.load(a, (int64_t)(c + 1) * BK);
                 sb.load(b, (int64_t)(c + 1) * BK);
             }
+            const int left = P2 && PAIR_B != PAIR_K ? (int)min(b.K - (int64_t)c * BK, (int64_t)BK) : BK;  // (K = 100: seven steps of 16 instead of eight)
 #pragma unroll
             for (int s = 0; s < BK / 16; ++s) {
+                if (s > 0 && 16 * s >= left) break;
                 uintx4 x[TM][PARTS], y[TN][PARTS];
 #pragma unroll
                 for (int p = 0; p < PARTS; ++p) {
