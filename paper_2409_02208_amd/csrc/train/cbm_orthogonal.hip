@@ -20,20 +20,24 @@ constexpr int PARTS = 256;  // workgroups that share the sum of squares
 // Squares in 64 bits: no value of fp32 overflows or vanishes there.
 template <class T>
 __global__ __launch_bounds__(256) void cbm_orthogonal_norm_kernel(int64_t m, int64_t n, const T* __restrict__ X, int64_t ldx, double* __restrict__ parts) {
-    __shared__ double room[256];
+    __shared__ double room[4];
     double s = 0.0;
-    for (int64_t r = blockIdx.x; r < m; r += gridDim.x)
-        for (int64_t c = threadIdx.x; c < n; c += 256) {
-            const double x = (double)(float)X[r * ldx + c];
-            s += x * x;
-        }
-    room[threadIdx.x] = s;
-    __syncthreads();
-    for (int step = 128; step; step /= 2) {
-        if ((int)threadIdx.x < step) room[threadIdx.x] += room[threadIdx.x + step];
-        __syncthreads();
+    const uint32_t wide = (uint32_t)((n + 1023) / 1024);  // pieces of a row, of four values a thread
+    for (uint32_t i = blockIdx.x; i < (uint32_t)m * wide; i += gridDim.x) {
+        const uint32_t r = i / wide;
+        const T* row = X + (int64_t)r * ldx;
+        const int64_t c = (int64_t)(i - r * wide) * 1024 + threadIdx.x;
+        float x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = c + 256 * j < n ? (float)row[c + 256 * j] : 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s += (double)x[j] * (double)x[j];
     }
-    if (threadIdx.x == 0) parts[blockIdx.x] = room[0];
+#pragma unroll
+    for (int step = 1; step < 64; step *= 2) s += __shfl_xor(s, step);
+    if (threadIdx.x % 64 == 0) room[threadIdx.x / 64] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) parts[blockIdx.x] = (room[0] + room[1]) + (room[2] + room[3]);
 }
 
 // A matrix in parts: rows of blocks of 32 columns.
@@ -74,14 +78,14 @@ __global__ __launch_bounds__(256) void cbm_orthogonal_begin_kernel(const T* __re
     for (int step = 1; step < 64; step *= 2) s += __shfl_xor(s, step);
     if (threadIdx.x % 64 == 0) squares[threadIdx.x / 64] = s;
     __syncthreads();
-    const double size = sqrt((squares[0] + squares[1]) + (squares[2] + squares[3])) + (double)eps;
+    const double by = (double)up / (sqrt((squares[0] + squares[1]) + (squares[2] + squares[3])) + (double)eps);
     const int64_t r0 = (int64_t)blockIdx.y * 32, c0 = (int64_t)blockIdx.x * 32;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {  // along X's rows
         const int slow = threadIdx.x / 32 + 8 * i, fast = threadIdx.x % 32;
         const int64_t r = r0 + (transposed ? fast : slow), c = c0 + (transposed ? slow : fast);
         float v = 0.0f;
-        if (r < z.rows && c < z.columns) v = (float)((double)(float)(transposed ? X[c * ldx + r] : X[r * ldx + c]) / size) * up;
+        if (r < z.rows && c < z.columns) v = (float)((double)(float)(transposed ? X[c * ldx + r] : X[r * ldx + c]) * by);
         room[r - r0][c - c0] = v;
     }
     __syncthreads();
@@ -105,7 +109,7 @@ template <int B>
 struct HalvesTiles : CbmTileSums<B, B, 2, 2> {
     typedef CbmTileSums<B, B, 2, 2> Sums;
     typedef CbmAlignedSide<_Float16, B, ALONG_K, SINGLE> Side;
-    static constexpr int TM = Sums::TM, TN = Sums::TN, BK = 64, SLOT = Side::UNITS, UNITS = 5 * SLOT, GROUPS = B == 256 ? 1 : 2, LOADS = Side::LOADS, HALF = LOADS / 2;
+    static constexpr int TM = Sums::TM, TN = Sums::TN, BK = 64, SLOT = Side::UNITS, UNITS = 5 * SLOT, GROUPS = B > 128 ? 1 : 2, LOADS = Side::LOADS, HALF = LOADS / 2;
     static_assert(UNITS >= Sums::OUT_UNITS, "");
     using Sums::acc;
 
@@ -392,163 +396,147 @@ __global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_orthogonal_product_ker
 }
 
 // Small matrices: everything in one workgroup's LDS, Z and A (which P takes the place of), rows of blocks as in memory and one unit more, so that sixteen neighbouring rows' units fall on different banks.
-// Tiles of 16 x 16 go to the waves in turn.  Z's columns, which P Z wants, are turned as they are read.
-constexpr int SMALL_STEPS = 16, SMALL_WAVES = 16;
+// A wave has a tile of 32 x 32.  Z's columns, which P Z wants, are turned as they are read.  What bounds it is one compute unit's LDS and the five barriers of a step: 64 x 64 in tiles of 16 x 16, which read
+// twice as much, 16.5 us for five steps.
+constexpr int SMALL_STEPS = 16;
 struct SmallArgs {
     int rows, columns, steps;  // of Z
     bool transposed;
     float eps, first, last;              // powers: of Z at first, and back to its size (and Y's scale) at last
     float gram[SMALL_STEPS], square[SMALL_STEPS], of_gram[SMALL_STEPS], of_one[SMALL_STEPS], next[SMALL_STEPS];
 };
-__host__ __device__ constexpr int small_pitch(int k) { return k * 4 + 16; }  // bytes of a row of k (a multiple of 32) values in parts
+constexpr int small_pitch(int k) { return k * 4 + 16; }  // bytes of a row of k (a multiple of 32) values in parts
 
-typedef float floatx4s __attribute__((ext_vector_type(4)));
-struct SmallTile {
-    floatx4s hh, hl, lh;
-    __device__ __forceinline__ floatx4s sum() const { return hh + (hl + lh); }
-};
-__device__ __forceinline__ f16x8 small_unit(const char* at) { return *reinterpret_cast<const f16x8*>(at); }
-// eight k of column `lane % 16` from k 8 (lane / 16) on: `at` is the block's first row at the sixteen columns
-__device__ __forceinline__ f16x8 small_turned(const char* at, int pitch) {
+__device__ __forceinline__ uintx4 small_unit(const char* at) { return *reinterpret_cast<const uintx4*>(at); }
+// eight k of column lane % 32 from k 8 (lane / 32) on: `at` is the first row's first column
+template <int PITCH>
+__device__ __forceinline__ uintx4 small_turned(const char* at) {
     typedef short Four __attribute__((ext_vector_type(4)));
     const int lane = threadIdx.x & 63;
-    const char* p = at + (8 * (lane >> 4) + (lane >> 2 & 3)) * pitch + (lane & 3) * 8;
+    const char* p = at + (8 * (lane >> 5) + (lane >> 2 & 3)) * PITCH + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
     struct {
         Four low, high;
     } v;
     v.low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) Four*)p);
-    v.high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) Four*)(p + 4 * pitch));
-    return __builtin_bit_cast(f16x8, v);
+    v.high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) Four*)(p + 4 * PITCH));
+    return __builtin_bit_cast(uintx4, v);
 }
-// Rows m .. m + 15 of x times rows n .. n + 15 of y (TURNED: times columns n .. n + 15), over `blocks` of 32 k.  Lane l has row l % 16 and columns 4 (l / 16) on.
-template <bool TURNED>
-__device__ __forceinline__ SmallTile small_product(const char* x, int px, int m, const char* y, int py, int n, int blocks) {
-    const int lane = threadIdx.x & 63, of = (lane >> 4) * 16;
-    SmallTile t{};
-    for (int b = 0; b < blocks; ++b) {
-        const char *ax = x + (m + (lane & 15)) * px + b * 128 + of, *ay = TURNED ? y + b * 32 * py + n / 32 * 128 + n % 32 * 2 : y + (n + (lane & 15)) * py + b * 128 + of;
-        const f16x8 xh = small_unit(ax), xl = small_unit(ax + 64), yh = TURNED ? small_turned(ay, py) : small_unit(ay), yl = TURNED ? small_turned(ay + 64, py) : small_unit(ay + 64);
-        t.hh = __builtin_amdgcn_mfma_f32_16x16x32_f16(yh, xh, t.hh, 0, 0, 0);
-        t.hl = __builtin_amdgcn_mfma_f32_16x16x32_f16(yl, xh, t.hl, 0, 0, 0);
-        t.lh = __builtin_amdgcn_mfma_f32_16x16x32_f16(yh, xl, t.lh, 0, 0, 0);
+// Rows m .. m + 31 of x times rows n .. n + 31 of y (TURNED: times columns n .. n + 31), over K.  Lane l has row l % 32 and columns 8 q + 4 (l / 32) on.
+template <bool TURNED, int K, int PX, int PY>
+__device__ __forceinline__ floatx16 small_product(const char* x, int m, const char* y, int n) {
+    const int lane = threadIdx.x & 63, of = (lane >> 5) * 16;
+    const char *ax = x + (m + (lane & 31)) * PX + of, *ay = TURNED ? y + n * 4 : y + (n + (lane & 31)) * PY + of;
+    floatx16 high{}, hl{}, lh{};  // (three chains: a product waits for the one before in its own)
+#pragma unroll
+    for (int s = 0; s < K / 16; ++s) {
+        const int at = s / 2 * 128 + s % 2 * 32;
+        const uintx4 xh = small_unit(ax + at), xl = small_unit(ax + at + 64), yh = TURNED ? small_turned<PY>(ay + 16 * s * PY) : small_unit(ay + at),
+                     yl = TURNED ? small_turned<PY>(ay + 16 * s * PY + 64) : small_unit(ay + at + 64);
+        high = cbm_multiply<_Float16>(yh, xh, high);
+        hl = cbm_multiply<_Float16>(yl, xh, hl);
+        lh = cbm_multiply<_Float16>(yh, xl, lh);
     }
-    return t;
+    return high + (hl + lh);
 }
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ char* small_place(char* x, int pitch, int m, int n) {  // of a lane's four values
-    const int lane = threadIdx.x & 63, c = n + (lane >> 4) * 4;
-    return x + (m + (lane & 15)) * pitch + c / 32 * 128 + c % 32 * 2;
-}
-__device__ __forceinline__ void small_put(char* at, const float (&v)[4]) {
-    f16x4 h, l;
+// f(q, columns 8 q + 4 (lane / 32) on of the lane's row in x) of a tile
+template <class F>
+__device__ __forceinline__ void small_places(char* x, int pitch, int m, int n, F&& f) {
+    const int lane = threadIdx.x & 63;
+    char* row = x + (m + (lane & 31)) * pitch + n * 4 + (lane >> 5) * 8;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        _Float16 a, b;
-        cut(v[j], a, b);
-        h[j] = a;
-        l[j] = b;
-    }
-    *reinterpret_cast<f16x4*>(at) = h;
-    *reinterpret_cast<f16x4*>(at + 64) = l;
+    for (int q = 0; q < 4; ++q) f(q, row + 16 * q);
+}
+__device__ __forceinline__ void small_put(char* x, int pitch, int m, int n, const floatx16& v, float up) {
+    small_places(x, pitch, m, n, [&](int q, char* at) {
+        f16x4 h, l;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            _Float16 a, b;
+            cut(v[4 * q + j] * up, a, b);
+            h[j] = a;
+            l[j] = b;
+        }
+        *reinterpret_cast<f16x4*>(at) = h;
+        *reinterpret_cast<f16x4*>(at + 64) = l;
+    });
 }
 
-// SIDE: the most rows and columns
-template <class T, int SIDE>
-__global__ __launch_bounds__(64 * SMALL_WAVES) void cbm_orthogonal_small_kernel(SmallArgs p, const T* X, int64_t ldx, T* Y, int64_t ldy) {
-    __shared__ uintx4 all[2 * SIDE * small_pitch(SIDE) / 16];
-    __shared__ double squares[SMALL_WAVES];
-    constexpr int EACH = SIDE * SIDE / (64 * SMALL_WAVES), TILES = SIDE / 16 * (SIDE / 16) / SMALL_WAVES;
-    const int s = (p.rows + 31) / 32 * 32, l = (p.columns + 31) / 32 * 32, pz = small_pitch(l), pg = small_pitch(s), wave = threadIdx.x >> 6;
-    char *z = (char*)all, *g = z + s * pz;
+// S x L: Z's rows and columns with zeros beyond them.
+template <class T, int S, int L>
+__global__ __launch_bounds__(S * L / 16) void cbm_orthogonal_small_kernel(SmallArgs p, const T* X, int64_t ldx, T* Y, int64_t ldy) {
+    constexpr int PZ = small_pitch(L), PG = small_pitch(S), WAVES = S / 32 * (L / 32), THREADS = 64 * WAVES, EACH = L * L / THREADS;
+    static_assert(S <= L, "");
+    __shared__ uintx4 all[S * (PZ + PG) / 16];
+    __shared__ double squares[WAVES];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    char *z = (char*)all, *g = z + S * PZ;
     // X's values, zeros beyond it, neighbouring threads along its rows
-    const int height = p.transposed ? p.columns : p.rows, width = p.transposed ? p.rows : p.columns, c0 = threadIdx.x % SIDE, r0 = threadIdx.x / SIDE;
+    const int height = p.transposed ? p.columns : p.rows, width = p.transposed ? p.rows : p.columns, c0 = threadIdx.x % L, r0 = threadIdx.x / L;
     double sum = 0.0;
-#pragma unroll 4
+#pragma unroll 8
     for (int i = 0; i < EACH; ++i) {
-        const int r = r0 + 64 * SMALL_WAVES / SIDE * i;
+        const int r = r0 + THREADS / L * i;
         if (r >= height || c0 >= width) continue;
         const double v = (double)(float)X[r * ldx + c0];
         sum += v * v;
     }
 #pragma unroll
     for (int step = 1; step < 64; step *= 2) sum += __shfl_xor(sum, step);
-    if (threadIdx.x % 64 == 0) squares[wave] = sum;
+    if (lane == 0) squares[wave] = sum;
     __syncthreads();
     sum = 0.0;
-    for (int i = 0; i < SMALL_WAVES; ++i) sum += squares[i];
-    const double size = sqrt(sum) + (double)p.eps;
-#pragma unroll 4
-    for (int i = 0; i < EACH; ++i) {  // (read again, from L2: kept in registers, 128 x 128 spill)
-        const int r = r0 + 64 * SMALL_WAVES / SIDE * i, zr = p.transposed ? c0 : r, zc = p.transposed ? r : c0;
-        if (zr >= s || zc >= l) continue;
+    for (int i = 0; i < WAVES; ++i) sum += squares[i];
+    const double up = (double)p.first / (sqrt(sum) + (double)p.eps);
+#pragma unroll 8
+    for (int i = 0; i < EACH; ++i) {  // (read again, from L2)
+        const int r = r0 + THREADS / L * i, zr = p.transposed ? c0 : r, zc = p.transposed ? r : c0;
+        if (zr >= S || zc >= L) continue;
         _Float16 h, low;
-        cut(r < height && c0 < width ? (float)((double)(float)X[r * ldx + c0] / size) * p.first : 0.0f, h, low);
-        _Float16* to = (_Float16*)(z + zr * pz + zc / 32 * 128 + zc % 32 * 2);
+        cut(r < height && c0 < width ? (float)((double)(float)X[r * ldx + c0] * up) : 0.0f, h, low);
+        _Float16* to = (_Float16*)(z + zr * PZ + zc / 32 * 128 + zc % 32 * 2);
         to[0] = h;
         to[32] = low;
     }
+    // a step's factors: a lane each
+    const int mine = lane % SMALL_STEPS, m = wave / (L / 32) * 32, n = wave % (L / 32) * 32;
+    const float gram = p.gram[mine], square = p.square[mine], by_gram = p.of_gram[mine], by_one = p.of_one[mine], by_next = p.next[mine];
     __syncthreads();
-    const int square = s / 16 * (s / 16), whole = s / 16 * (l / 16);
-    for (int step = 0; step < p.steps; ++step) {
-        int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        asm volatile("" : "+s"(wave));  // (or all tiles' places stay in scalar registers from step to step)
-        for (int t = wave; t < square; t += SMALL_WAVES) {
-            const int m = t / (s / 16) * 16, n = t % (s / 16) * 16;
-            const floatx4s a = small_product<false>(z, pz, m, z, pz, n, l / 32).sum();
-            const float out[4] = {a[0] * p.gram[step], a[1] * p.gram[step], a[2] * p.gram[step], a[3] * p.gram[step]};
-            small_put(small_place(g, pg, m, n), out);
+    floatx16 acc{};
+    for (int step = 0;; ++step) {
+        auto of_step = [&](float v) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), step)); };
+        if (n < S) small_put(g, PG, m, n, small_product<false, L, PZ, PZ>(z, m, z, n), of_step(gram));
+        __syncthreads();
+        if (n < S) {
+            acc = small_product<false, S, PG, PG>(g, m, g, n);
+            const float up_square = of_step(square), of_gram = of_step(by_gram), of_one = of_step(by_one);
+            const int r = m + (lane & 31), c = n + 4 * (lane >> 5);
+            small_places(g, PG, m, n, [&](int q, const char* at) {
+                const f16x4 h = *reinterpret_cast<const f16x4*>(at), low = *reinterpret_cast<const f16x4*>(at + 64);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[4 * q + j] = fmaf(of_gram, (float)h[j] + (float)low[j], acc[4 * q + j] * up_square) + (r == c + 8 * q + j ? of_one : 0.0f);
+            });
         }
         __syncthreads();
-        floatx4s acc[TILES];
-#pragma unroll
-        for (int i = 0; i < TILES; ++i) {
-            const int t = wave + SMALL_WAVES * i, m = t / (s / 16) * 16, n = t % (s / 16) * 16;
-            if (t >= square) continue;
-            acc[i] = small_product<false>(g, pg, m, g, pg, n, s / 32).sum();
-            const char* at = small_place(g, pg, m, n);
-            const f16x4 h = *reinterpret_cast<const f16x4*>(at), low = *reinterpret_cast<const f16x4*>(at + 64);
-            const int lane = threadIdx.x & 63, r = m + (lane & 15), c = n + (lane >> 4) * 4;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(p.of_gram[step], (float)h[j] + (float)low[j], acc[i][j] * p.square[step]) + (r == c + j ? p.of_one[step] : 0.0f);
-        }
+        if (n < S) small_put(g, PG, m, n, acc, 1.0f);
         __syncthreads();
-        asm volatile("" : "+s"(wave));
-#pragma unroll
-        for (int i = 0; i < TILES; ++i) {
-            const int t = wave + SMALL_WAVES * i;
-            if (t >= square) continue;
-            const float out[4] = {acc[i][0], acc[i][1], acc[i][2], acc[i][3]};
-            small_put(small_place(g, pg, t / (s / 16) * 16, t % (s / 16) * 16), out);
-        }
+        acc = small_product<true, S, PG, PZ>(g, m, z, n);
+        if (step + 1 >= p.steps) break;
         __syncthreads();
-        asm volatile("" : "+s"(wave));
-#pragma unroll
-        for (int i = 0; i < TILES; ++i) {
-            const int t = wave + SMALL_WAVES * i;
-            if (t >= whole) continue;
-            acc[i] = small_product<true>(g, pg, t / (l / 16) * 16, z, pz, t % (l / 16) * 16, s / 32).sum();
-        }
+        small_put(z, PZ, m, n, acc, of_step(by_next));
         __syncthreads();
-        const bool end = step + 1 == p.steps;
-        const float up = end ? p.last : p.next[step];
+    }
+    const int r = m + (lane & 31);
+    if (r >= p.rows) return;
 #pragma unroll
-        for (int i = 0; i < TILES; ++i) {
-            const int t = wave + SMALL_WAVES * i, m = t / (l / 16) * 16, n = t % (l / 16) * 16;
-            if (t >= whole) continue;
-            const float out[4] = {acc[i][0] * up, acc[i][1] * up, acc[i][2] * up, acc[i][3] * up};
-            if (!end) {
-                small_put(small_place(z, pz, m, n), out);
-                continue;
-            }
-            const int lane = threadIdx.x & 63, r = m + (lane & 15), c = n + (lane >> 4) * 4;
-            if (r >= p.rows) continue;
-            if (!p.transposed) cbm_put(Y + r * ldy, c, p.columns, out);
-            else
+    for (int q = 0; q < 4; ++q) {
+        const int c = n + 8 * q + 4 * (lane >> 5);
+        const float out[4] = {acc[4 * q] * p.last, acc[4 * q + 1] * p.last, acc[4 * q + 2] * p.last, acc[4 * q + 3] * p.last};
+        if (!p.transposed) cbm_put(Y + r * ldy, c, p.columns, out);
+        else
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (c + j < p.columns) Y[(c + j) * ldy + r] = (T)out[j];
-        }
-        __syncthreads();
+            for (int j = 0; j < 4; ++j)
+                if (c + j < p.columns) Y[(c + j) * ldy + r] = (T)out[j];
     }
 }
 
@@ -617,18 +605,20 @@ Room room_of(int64_t s, int64_t l) {
     return r;
 }
 
-// f(the tiles that take least): rounds of workgroups, each its products at what a compute unit's share reaches and what it takes beside them.
+// f(the tiles that take least): rounds of workgroups, each its products at what a compute unit's share reaches and what it takes beside them.  (4096 x 4096's Gram matrix is 136 tiles of 256 on and below the
+// diagonal, which take as long as 256 of them, and 253 of 192: 231 and 191 us.)
 template <class F>
 void with_tiles(int64_t M, int64_t N, int64_t K, bool half, F&& f) {
     double best = 1e30;
     int side = 256;
-    for (int b : {256, 128, 64}) {
+    for (int b : {256, 192, 128, 64}) {
         const int64_t m = (M + b - 1) / b, tiles = half ? m * (m + 1) / 2 : m * ((N + b - 1) / b), at_once = b == 128 ? 512 : 256;
-        const double each = 6.0 * b * b * (double)K / ((b == 256 ? 1250.0 : b == 128 ? 1050.0 : 500.0) * 1e6 / (double)at_once) * (b == 128 && tiles <= 256 ? 0.6 : 1.0);
-        const double us = (double)((tiles + at_once - 1) / at_once) * (each + (b == 256 ? 12.0 : b == 128 ? 5.0 : 3.0));
+        const double each = 6.0 * b * b * (double)K / ((b == 256 ? 1250.0 : b == 192 ? 1150.0 : b == 128 ? 1050.0 : 500.0) * 1e6 / (double)at_once) * (b == 128 && tiles <= 256 ? 0.6 : 1.0);
+        const double us = (double)((tiles + at_once - 1) / at_once) * (each + (b == 256 ? 12.0 : b == 192 ? 9.0 : b == 128 ? 5.0 : 3.0));
         if (us < best) best = us, side = b;
     }
     if (side == 256) f((HalvesTiles<256>*)nullptr);
+    else if (side == 192) f((HalvesTiles<192>*)nullptr);
     else if (side == 128) f((HalvesTiles<128>*)nullptr);
     else f((HalvesShares*)nullptr);
 }
@@ -676,8 +666,15 @@ cbm_status cbm_launch_orthogonal(int32_t m, int32_t n, int32_t type, const void*
         }
         cbm_with_type(type, [&](auto t) {
             using T = decltype(t);
-            if (l <= 64) cbm_orthogonal_small_kernel<T, 64><<<1, 64 * SMALL_WAVES, 0, stream>>>(p, (const T*)X, ldx, (T*)Y, ldy);
-            else cbm_orthogonal_small_kernel<T, 128><<<1, 64 * SMALL_WAVES, 0, stream>>>(p, (const T*)X, ldx, (T*)Y, ldy);
+            auto go = [&](auto rows, auto columns) {
+                constexpr int S = decltype(rows)::value, L = decltype(columns)::value;
+                cbm_orthogonal_small_kernel<T, S, L><<<1, S * L / 16, 0, stream>>>(p, (const T*)X, ldx, (T*)Y, ldy);
+            };
+            using std::integral_constant;
+            if (l <= 32) go(integral_constant<int, 32>{}, integral_constant<int, 32>{});
+            else if (l <= 64) go(integral_constant<int, 64>{}, integral_constant<int, 64>{});
+            else if (s <= 64) go(integral_constant<int, 64>{}, integral_constant<int, 128>{});
+            else go(integral_constant<int, 128>{}, integral_constant<int, 128>{});
         });
         return cbm_launched("orthogonal update launch");
     }
