@@ -135,9 +135,9 @@ __global__ __launch_bounds__(1024) void cbm_classes_scale_kernel(int64_t n, cons
     scale[1] = most > 0.0f ? 0x1p15f / most : 0.0f;
 }
 
-// dZ of columns first .. first + b.count - 1, rounded to the type (half a step, as much as the gradients that are made of it are rounded by).
+// dZ of columns first .. first + width - 1, rounded to the type (half a step, as much as the gradients that are made of it are rounded by).
 template <class Tiles, class T>
-__global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_classes_slopes_kernel(CbmOperand<T> a, CbmOperand<T> b, int64_t chunks, int64_t first, int64_t c, const void* __restrict__ labels, int label_bits,
+__global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_classes_slopes_kernel(CbmOperand<T> a, CbmOperand<T> b, int64_t width, int64_t chunks, int64_t first, int64_t c, const void* __restrict__ labels, int label_bits,
                                                                  const float* __restrict__ stats, const float* __restrict__ dlogp, const float* __restrict__ scale, T* __restrict__ dZ,
                                                                  int64_t lddz) {
     constexpr int BM = Tiles::ROWS, BN = Tiles::COLUMNS;
@@ -168,7 +168,12 @@ __global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_classes_slopes_kernel(
     constexpr int W = cbm_wide<T>;
     t.template pieces<W>(
         lds, at.m, at.n, [&](int64_t r, int64_t col, float (&v)[W]) {
-            if (r < a.count) cbm_put(dZ + r * lddz, col, b.count, v, true);
+            if (r >= a.count) return;
+            if (col + W > width)
+#pragma unroll
+                for (int j = 0; j < W; ++j)
+                    if (col + j >= width) v[j] = 0.0f;  // (products of 16 bits read whole units)
+            cbm_put(dZ + r * lddz, col, (width + 7) / 8 * 8, v, true);
         },
         [&](int i, float* row) {  // a lane's row in LDS: the label's own
             if (half == 0 && hot[i] >= 0) row[hot[i]] += up[i];
@@ -186,36 +191,83 @@ int64_t piece_of(int64_t n, int32_t c, int32_t type) {
     return std::min<int64_t>(((int64_t)c + 7) / 8 * 8, std::max<int64_t>(fit, 1024));
 }
 
+// Copies of X, rows of whole units, and of W turned.
+struct Copies {
+    int64_t ld, weights, bytes;  // where the weights begin; X is first
+};
+Copies copies_of(int64_t n, int32_t d, int32_t c, int32_t type) {
+    if (!cbm_may_pack(n, d, c, type)) return {};
+    const int64_t ld = cbm_whole(d, 8);
+    return {ld, 2 * n * ld, 2 * (n + cbm_whole(c, 8)) * ld};
+}
+
 struct Room {
-    int64_t scale, sums, parts, bytes;  // where they begin; dZ is first
+    int64_t scale, sums, copies, parts, bytes;  // where they begin; dZ is first
 };
 Room back_room(int64_t n, int32_t d, int32_t c, int32_t type) {
-    const int64_t piece = piece_of(n, c, type), last = c % piece ? c % piece : piece;
+    const int64_t piece = piece_of(n, c, type), last = c % piece ? c % piece : piece, wide = cbm_whole(d, 8);
     int64_t parts = 0;
     for (int64_t w : {piece, last}) {
         const int64_t dx = cbm_product_parts(n, d, w, type), dw = cbm_product_parts(d, w, n, type);
-        if (dx > 1) parts = std::max(parts, dx * n * d);
-        if (dw > 1) parts = std::max(parts, dw * d * w);
+        if (dx > 1) parts = std::max(parts, dx * n * wide);
+        if (dw > 1) parts = std::max(parts, dw * wide * cbm_whole(w, 8));
     }
     Room r;
     r.scale = rounded16(n * piece * bytes_of(type));
     r.sums = r.scale + 16;
-    r.parts = r.sums + (piece < c ? rounded16(4 * n * d) : 0);
+    r.copies = r.sums + (piece < c ? rounded16(4 * n * wide) : 0);
+    r.parts = r.copies + copies_of(n, d, c, type).bytes;
     r.bytes = r.parts + 4 * parts;
     return r;
 }
 
-// f(tiles, grid) for a product n x d . d x c of scores
+// X and W as the scores' products read them: as they lie, or copies.
+template <class T>
+struct Operands {
+    CbmOperand<T> a, b;
+    bool units, turned;
+    Operands(int64_t n, int32_t d, int32_t c, int32_t type, const void* X, int64_t ldx, const void* W, int64_t ldw, char* room, hipStream_t stream)
+        : a{{(const T*)X, nullptr}, {ldx, 0}, n, d, 0}, b{{(const T*)W, nullptr}, {ldw, 0}, c, d, 0}, units(false), turned(false) {
+        if constexpr (sizeof(T) == 2) {
+            const Copies copies = copies_of(n, d, c, type);
+            const bool whole = cbm_units(b.p[0], ldw, c);
+            units = cbm_units(a.p[0], ldx, d);
+            if (!units && copies.bytes) {
+                cbm_launch_pack(X, ldx, n, d, false, room, copies.ld, 0, 0, stream);
+                a = {{(const T*)room, nullptr}, {copies.ld, 0}, n, copies.ld, 0};
+                units = true;
+            }
+            turned = units && copies.bytes && (!whole || n >= CBM_TURN_ROWS);
+            if (turned) {
+                cbm_launch_pack(W, ldw, c, d, true, room + copies.weights, copies.ld, 0, 0, stream);
+                b = {{(const T*)(room + copies.weights), nullptr}, {copies.ld, 0}, c, copies.ld, 0};
+            }
+            units = units && (turned || whole);
+        }
+    }
+    // columns `first` .. first + width - 1
+    CbmOperand<T> some(int64_t first, int64_t width) const {
+        CbmOperand<T> o = b;
+        o.p[0] += turned ? first * b.ld[0] : first;
+        o.count = width;
+        return o;
+    }
+};
+
+// f(tiles, grid, chunks) for a product n x d . d x c of scores
 template <class T, class F>
-void with_tiles(int64_t n, int64_t d, int64_t c, const CbmOperand<T>& a, const CbmOperand<T>& b, int32_t type, F&& f) {
+void with_tiles(int64_t n, int64_t d, int64_t c, const Operands<T>& o, int32_t type, F&& f) {
     auto run = [&](auto* tiles_type) {
         typedef std::remove_pointer_t<decltype(tiles_type)> Tiles;
         const int64_t tiles = (n + Tiles::ROWS - 1) / Tiles::ROWS * ((c + Tiles::COLUMNS - 1) / Tiles::COLUMNS);
         f(tiles_type, (unsigned)((tiles + CBM_XCD - 1) / CBM_XCD * CBM_XCD), (d + Tiles::BK - 1) / Tiles::BK);
     };
     if constexpr (sizeof(T) == 2)
-        if (cbm_units(a.p[0], a.ld[0], d) && cbm_units(b.p[0], b.ld[0], c)) {
-            if (cbm_product_tile(n, c, d, type) == 256) run((CbmAlignedTiles<T, 256, 256, ALONG_K, ACROSS_K, SINGLE>*)nullptr);
+        if (o.units) {
+            const bool large = cbm_product_tile(n, c, d, type) == 256;
+            if (o.turned && large) run((CbmAlignedTiles<T, 256, 256, ALONG_K, ALONG_K, SINGLE>*)nullptr);
+            else if (o.turned) run((CbmAlignedTiles<T, 128, 128, ALONG_K, ALONG_K, SINGLE>*)nullptr);
+            else if (large) run((CbmAlignedTiles<T, 256, 256, ALONG_K, ACROSS_K, SINGLE>*)nullptr);
             else run((CbmAlignedTiles<T, 128, 128, ALONG_K, ACROSS_K, SINGLE>*)nullptr);
             return;
         }
@@ -224,7 +276,9 @@ void with_tiles(int64_t n, int64_t d, int64_t c, const CbmOperand<T>& a, const C
 
 }  // namespace
 
-int64_t cbm_classes_workspace(int64_t n, int32_t, int32_t c, int32_t) { return rounded16(n * most_parts(n, c) * (int64_t)sizeof(Sums)) + 4 * n; }
+int64_t cbm_classes_workspace(int64_t n, int32_t d, int32_t c, int32_t type) {
+    return rounded16(n * most_parts(n, c) * (int64_t)sizeof(Sums)) + rounded16(4 * n) + copies_of(n, d, c, type).bytes;
+}
 
 cbm_status cbm_launch_classes(int64_t n, int32_t d, int32_t c, int32_t type, const void* X, int64_t ldx, const void* W, int64_t ldw, const void* labels, int label_bits, float* logp, float* stats,
                               void* workspace, void* stream_) {
@@ -235,7 +289,6 @@ cbm_status cbm_launch_classes(int64_t n, int32_t d, int32_t c, int32_t type, con
     float* chosen = (float*)((char*)workspace + rounded16(n * most_parts(n, c) * (int64_t)sizeof(Sums)));
     cbm_with_type(type, [&](auto t) {
         using T = decltype(t);
-        const CbmOperand<T> a{{(const T*)X, nullptr}, {ldx, 0}, n, d, 0}, b{{(const T*)W, nullptr}, {ldw, 0}, c, d, 0};
         constexpr int V = 16 / (int)sizeof(T);
         if (n <= cbm_most_few_rows<T> && c >= V) {
             count = ((int64_t)c + 8 * V - 1) / (8 * V);
@@ -244,10 +297,11 @@ cbm_status cbm_launch_classes(int64_t n, int32_t d, int32_t c, int32_t type, con
             });
             return;
         }
-        with_tiles<T>(n, d, c, a, b, type, [&](auto* tiles_type, unsigned grid, int64_t chunks) {
+        const Operands<T> o(n, d, c, type, X, ldx, W, ldw, (char*)chosen + rounded16(4 * n), stream);
+        with_tiles<T>(n, d, c, o, type, [&](auto* tiles_type, unsigned grid, int64_t chunks) {
             typedef std::remove_pointer_t<decltype(tiles_type)> Tiles;
             count = ((int64_t)c + Tiles::COLUMNS - 1) / Tiles::COLUMNS * Tiles::ACROSS;
-            cbm_classes_kernel<Tiles, T><<<grid, 256, 0, stream>>>(a, b, chunks, logp ? labels : nullptr, label_bits, parts, chosen);
+            cbm_classes_kernel<Tiles, T><<<grid, 256, 0, stream>>>(o.a, o.b, chunks, logp ? labels : nullptr, label_bits, parts, chosen);
         });
     });
     cbm_classes_join_kernel<<<(unsigned)((n + 3) / 4), 256, 0, stream>>>(n, c, count, labels, label_bits, parts, chosen, logp, stats);
@@ -260,59 +314,70 @@ cbm_status cbm_launch_classes_backward(int64_t n, int32_t d, int32_t c, int32_t 
                                        const float* stats, const float* dlogp, void* dX, int64_t lddx, void* dW, int64_t lddw, void* workspace, void* stream_) {
     hipStream_t stream = (hipStream_t)stream_;
     const Room room = back_room(n, d, c, type);
-    const int64_t piece = piece_of(n, c, type), bytes = bytes_of(type);
+    const int64_t piece = piece_of(n, c, type);
     float *scale = (float*)((char*)workspace + room.scale), *sums = (float*)((char*)workspace + room.sums), *parts = (float*)((char*)workspace + room.parts);
     if (type != CBM_F16) scale = nullptr;
     if (scale && n > 0) cbm_classes_scale_kernel<<<1, 1024, 0, stream>>>(n, dlogp, scale);
-    for (int64_t first = 0; first < c; first += piece) {
-        const int64_t width = std::min<int64_t>(piece, c - first);
-        const void* Wp = (const char*)W + first * bytes;
-        if (n > 0)
-            cbm_with_type(type, [&](auto t) {
-                using T = decltype(t);
-                const CbmOperand<T> a{{(const T*)X, nullptr}, {ldx, 0}, n, d, 0}, b{{(const T*)Wp, nullptr}, {ldw, 0}, width, d, 0};
-                with_tiles<T>(n, d, width, a, b, type, [&](auto* tiles_type, unsigned grid, int64_t chunks) {
-                    cbm_classes_slopes_kernel<std::remove_pointer_t<decltype(tiles_type)>, T><<<grid, 256, 0, stream>>>(a, b, chunks, first, c, labels, label_bits, stats, dlogp, scale, (T*)workspace,
-                                                                                                              piece);
+    cbm_with_type(type, [&](auto t) {
+        using T = decltype(t);
+        const Operands<T> o(n, d, c, type, X, ldx, W, ldw, (char*)workspace + room.copies, n > 0 ? stream : nullptr);
+        for (int64_t first = 0; first < c; first += piece) {
+            const int64_t width = std::min<int64_t>(piece, c - first);
+            const CbmOperand<T> b = o.some(first, width);
+            if (n > 0)
+                with_tiles<T>(n, d, width, o, type, [&](auto* tiles_type, unsigned grid, int64_t chunks) {
+                    cbm_classes_slopes_kernel<std::remove_pointer_t<decltype(tiles_type)>, T><<<grid, 256, 0, stream>>>(o.a, b, width, chunks, first, c, labels, label_bits, stats, dlogp, scale,
+                                                                                                              (T*)workspace, piece);
                 });
-            });
-        CbmProduct p{};
-        p.type = p.out.type = type;
-        p.out.alpha = 1.0f;
-        p.out.factor = n > 0 ? scale : nullptr;
-        p.A = workspace;
-        p.lda = piece;
-        if (dX && n > 0) {
-            p.M = n;
-            p.N = d;
-            p.K = width;
-            p.B[0] = Wp;
-            p.ldb[0] = ldw;
-            p.out.C[0] = dX;
-            p.out.ldc[0] = lddx;
-            p.out.columns = d;
-            p.out.sums = piece < c ? sums : nullptr;
-            p.out.first = first == 0;
-            p.out.last = first + piece >= c;
-            p.parts = cbm_product_parts(n, d, width, type) > 1 ? parts : nullptr;
-            cbm_launch_tiles(p, stream);
+            CbmProduct p{};
+            p.type = type;
+            p.out.factor = n > 0 ? scale : nullptr;
+            p.A = workspace;
+            p.lda = piece;
+            if (dX && n > 0) {
+                p.M = n;
+                p.N = d;
+                p.K = width;
+                p.B[0] = (const T*)W + first;
+                p.ldb[0] = ldw;
+                if (o.turned && !cbm_units((const T*)W, ldw, c)) {  // (dZ has whole units, and zeros beyond the last class; so has the copy)
+                    p.B[0] = b.p[0];
+                    p.ldb[0] = p.N = b.ld[0];
+                    p.K = cbm_whole(width, 8);
+                    p.b_across = true;
+                }
+                p.out.C[0] = dX;
+                p.out.ldc[0] = lddx;
+                p.out.columns = d;
+                p.out.sums = piece < c ? sums : nullptr;
+                p.out.first = first == 0;
+                p.out.last = first + piece >= c;
+                p.parts = cbm_product_parts(n, d, width, type) > 1 ? parts : nullptr;
+                cbm_launch_tiles(p, stream);
+            }
+            if (dW) {
+                p.M = d;
+                p.N = width;
+                p.K = n;
+                p.A = X;
+                p.lda = ldx;
+                if (o.a.p[0] != (const T*)X) {
+                    p.A = o.a.p[0];
+                    p.lda = p.M = o.a.ld[0];
+                    p.out.rows = d;
+                }
+                if (sizeof(T) == 2) p.N = cbm_whole(width, 8);
+                p.a_across = p.b_across = true;
+                p.B[0] = workspace;
+                p.ldb[0] = piece;
+                p.out.C[0] = (T*)dW + first;
+                p.out.ldc[0] = lddw;
+                p.out.columns = (int32_t)width;
+                p.out.sums = nullptr;
+                p.parts = cbm_product_parts(d, width, n, type) > 1 ? parts : nullptr;
+                cbm_launch_tiles(p, stream);
+            }
         }
-        if (dW) {
-            p.M = d;
-            p.N = width;
-            p.K = n;
-            p.A = X;
-            p.lda = ldx;
-            p.a_across = p.b_across = true;
-            p.B[0] = workspace;
-            p.ldb[0] = piece;
-            p.out.C[0] = (char*)dW + first * bytes;
-            p.out.ldc[0] = lddw;
-            p.out.columns = (int32_t)width;
-            p.out.sums = nullptr;
-            p.parts = cbm_product_parts(d, width, n, type) > 1 ? parts : nullptr;
-            cbm_launch_tiles(p, stream);
-        }
-    }
+    });
     return cbm_launched("linear log probabilities backward launch");
 }

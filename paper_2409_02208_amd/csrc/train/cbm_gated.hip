@@ -40,10 +40,10 @@ void with_activation(int32_t act, F&& f) {
 
 // Both projections in one product: a wave's tiles of 32 columns come from Wg and Wu in turn, so a lane has both sums of a value of H.
 template <class Tiles, class T, int ACT>
-__global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_gated_kernel(CbmOperand<T> a, CbmOperand<T> b, int64_t chunks, T* __restrict__ H, int64_t ldh, T* __restrict__ G, int64_t ldg,
+__global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_gated_kernel(CbmOperand<T> a, CbmOperand<T> b, int64_t m, int64_t chunks, T* __restrict__ H, int64_t ldh, T* __restrict__ G, int64_t ldg,
                                                                     T* __restrict__ U, int64_t ldu, bool far) {
     __shared__ uintx4 lds[Tiles::UNITS];
-    const CbmTilePlace at = cbm_tile_place((a.count + Tiles::ROWS - 1) / Tiles::ROWS, (b.count + Tiles::COLUMNS / 2 - 1) / (Tiles::COLUMNS / 2), 1);
+    const CbmTilePlace at = cbm_tile_place((a.count + Tiles::ROWS - 1) / Tiles::ROWS, (m + Tiles::COLUMNS / 2 - 1) / (Tiles::COLUMNS / 2), 1);
     if (!at.any) return;
     Tiles t;
     t.run(lds, a, b, at.m, at.n, 0, (int)chunks);
@@ -53,9 +53,9 @@ __global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_gated_kernel(CbmOperan
         float h[W];
 #pragma unroll
         for (int v = 0; v < W; ++v) h[v] = activated<ACT>(g[v]) * u[v];
-        cbm_put(H + r * ldh, c, b.count, h, far);
-        if (G) cbm_put(G + r * ldg, c, b.count, g, far);
-        if (U) cbm_put(U + r * ldu, c, b.count, u, far);
+        cbm_put(H + r * ldh, c, m, h, far);
+        if (G) cbm_put(G + r * ldg, c, m, g, far);
+        if (U) cbm_put(U + r * ldu, c, m, u, far);
     });
 }
 
@@ -114,19 +114,30 @@ __global__ __launch_bounds__(256) void cbm_gated_slopes_kernel(int64_t n, int m,
     }
 }
 
-int64_t padded(int32_t m) { return ((int64_t)m + 63) / 64 * 64; }
-int64_t rounded16(int64_t bytes) { return (bytes + 15) / 16 * 16; }
+}  // namespace
+
+namespace {
+
+// Copies of X (n x k, rows of whole units) and of the weights turned, blocks of 32 columns of Wg and Wu in turn (rows of the result's columns).
+struct Copies {
+    int64_t ld, weights, bytes;  // where the weights begin; X is first
+};
+Copies copies_of(int64_t n, int32_t k, int32_t m, int32_t type) {
+    if (!cbm_may_pack(n, k, 2 * (int64_t)m, type)) return {};
+    const int64_t ld = cbm_whole(k, 8);
+    return {ld, 2 * n * ld, 2 * n * ld + 4 * cbm_whole(m, 32) * ld};
+}
 
 }  // namespace
 
-int64_t cbm_gated_workspace(int64_t, int32_t, int32_t, int32_t) { return 0; }
+int64_t cbm_gated_workspace(int64_t n, int32_t k, int32_t m, int32_t type) { return copies_of(n, k, m, type).bytes; }
 
 cbm_status cbm_launch_gated(int64_t n, int32_t k, int32_t m, int32_t type, int32_t act, const void* X, int64_t ldx, const void* Wg, int64_t ldwg, const void* Wu, int64_t ldwu, void* H,
-                            int64_t ldh, void* G, int64_t ldg, void* U, int64_t ldu, void*, void* stream) {
+                            int64_t ldh, void* G, int64_t ldg, void* U, int64_t ldu, void* workspace, void* stream) {
     if (n == 0) return CBM_OK;
+    const Copies copies = copies_of(n, k, m, type);
     cbm_with_type(type, [&](auto t) {
         using T = decltype(t);
-        const CbmOperand<T> a{{(const T*)X, nullptr}, {ldx, 0}, n, k, 0}, b{{(const T*)Wg, (const T*)Wu}, {ldwg, ldwu}, m, k, 0};
         constexpr int V = 16 / (int)sizeof(T);
         if (n <= cbm_most_few_rows<T> && m >= V) {
             cbm_with_few_rows(n, [&](auto rows) {
@@ -137,39 +148,78 @@ cbm_status cbm_launch_gated(int64_t n, int32_t k, int32_t m, int32_t type, int32
             });
             return;
         }
-        auto run = [&](auto* tiles_type) {
+        auto run = [&](auto* tiles_type, const CbmOperand<T>& a, const CbmOperand<T>& b) {
             typedef std::remove_pointer_t<decltype(tiles_type)> Tiles;
             const int64_t tiles = (n + Tiles::ROWS - 1) / Tiles::ROWS * (((int64_t)m + Tiles::COLUMNS / 2 - 1) / (Tiles::COLUMNS / 2));
             with_activation(act, [&](auto which) {
                 cbm_gated_kernel<Tiles, T, decltype(which)::value><<<(unsigned)((tiles + CBM_XCD - 1) / CBM_XCD * CBM_XCD), 256, 0, (hipStream_t)stream>>>(
-                    a, b, (k + Tiles::BK - 1) / Tiles::BK, (T*)H, ldh, (T*)G, ldg, (T*)U, ldu, n * m * (int64_t)sizeof(T) >= CBM_FAR_BYTES);
+                    a, b, m, (k + Tiles::BK - 1) / Tiles::BK, (T*)H, ldh, (T*)G, ldg, (T*)U, ldu, n * m * (int64_t)sizeof(T) >= CBM_FAR_BYTES);
             });
         };
-        if constexpr (sizeof(T) == 2)
-            if (cbm_units(a.p[0], ldx, k) && cbm_units(b.p[0], ldwg, m) && cbm_units(b.p[1], ldwu, m) && ldwg == ldwu) {
-                if (cbm_product_tile(n, 2 * (int64_t)m, k, type) == 256) run((CbmAlignedTiles<T, 256, 256, ALONG_K, ACROSS_K, PAIR_ROWS>*)nullptr);
-                else run((CbmAlignedTiles<T, 128, 128, ALONG_K, ACROSS_K, PAIR_ROWS>*)nullptr);
+        CbmOperand<T> a{{(const T*)X, nullptr}, {ldx, 0}, n, k, 0}, b{{(const T*)Wg, (const T*)Wu}, {ldwg, ldwu}, m, k, 0};
+        if constexpr (sizeof(T) == 2) {
+            const bool large = cbm_product_tile(n, 2 * (int64_t)m, k, type) == 256;
+            bool units = cbm_units(a.p[0], ldx, k);
+            const bool whole = cbm_units(b.p[0], ldwg, m) && cbm_units(b.p[1], ldwu, m) && ldwg == ldwu;
+            if (!units && copies.bytes) {
+                cbm_launch_pack(X, ldx, n, k, false, workspace, copies.ld, 0, 0, stream);
+                a = {{(const T*)workspace, nullptr}, {copies.ld, 0}, n, copies.ld, 0};
+                units = true;
+            }
+            if (units && copies.bytes && (!whole || n >= CBM_TURN_ROWS)) {
+                T* turned = (T*)((char*)workspace + copies.weights);
+                cbm_launch_pack(Wg, ldwg, m, k, true, turned, copies.ld, 64, 0, stream);
+                cbm_launch_pack(Wu, ldwu, m, k, true, turned, copies.ld, 64, 32, stream);
+                b = {{turned, nullptr}, {copies.ld, 0}, 2 * cbm_whole(m, 32), copies.ld, 0};
+                if (large) run((CbmAlignedTiles<T, 256, 256, ALONG_K, ALONG_K, SINGLE>*)nullptr, a, b);
+                else run((CbmAlignedTiles<T, 128, 128, ALONG_K, ALONG_K, SINGLE>*)nullptr, a, b);
                 return;
             }
-        run((CbmTiles<T, 128, 128, 2, 2, ALONG_K, ACROSS_K, PAIR_ROWS>*)nullptr);
+            if (units && whole) {
+                if (large) run((CbmAlignedTiles<T, 256, 256, ALONG_K, ACROSS_K, PAIR_ROWS>*)nullptr, a, b);
+                else run((CbmAlignedTiles<T, 128, 128, ALONG_K, ACROSS_K, PAIR_ROWS>*)nullptr, a, b);
+                return;
+            }
+        }
+        run((CbmTiles<T, 128, 128, 2, 2, ALONG_K, ACROSS_K, PAIR_ROWS>*)nullptr, a, b);
     });
     return cbm_launched("gated layer launch");
 }
 
-int64_t cbm_gated_back_workspace(int64_t n, int32_t k, int32_t m, int32_t type) {
-    const int64_t at = padded(m), bytes = type == CBM_F32 ? 4 : 2;
+namespace {
+
+// dG and dU side by side, copies of X and of the weights (rows of whole units), shares of K.
+struct BackRoom {
+    int64_t at, x, weights, parts, bytes;  // column of dU; where they begin
+    bool copies;
+};
+BackRoom back_room(int64_t n, int32_t k, int32_t m, int32_t type) {
+    BackRoom r{};
+    const int64_t bytes = type == CBM_F32 ? 4 : 2, wide = cbm_whole(k, 8);
+    r.at = cbm_whole(m, 64);
+    r.copies = cbm_may_pack(n, k, 2 * (int64_t)m, type);
+    r.x = cbm_whole(n * 2 * r.at * bytes, 16);
+    r.weights = r.x + (r.copies ? 2 * n * wide : 0);
+    r.parts = r.weights + (r.copies ? 4 * k * r.at : 0);
     int64_t parts = 0;
-    const int64_t dx = cbm_product_parts(n, k, 2 * at, type), dw = cbm_product_parts(k, 2 * at, n, type);
+    const int64_t dx = cbm_product_parts(n, k, 2 * r.at, type), dw = cbm_product_parts(wide, 2 * r.at, n, type);
     if (dx > 1) parts = dx * n * k;
-    if (dw > 1) parts = std::max(parts, dw * k * 2 * at);
-    return rounded16(n * 2 * at * bytes) + 4 * parts;
+    if (dw > 1) parts = std::max(parts, dw * wide * 2 * r.at);
+    r.bytes = r.parts + 4 * parts;
+    return r;
 }
+
+}  // namespace
+
+int64_t cbm_gated_back_workspace(int64_t n, int32_t k, int32_t m, int32_t type) { return back_room(n, k, m, type).bytes; }
 
 cbm_status cbm_launch_gated_backward(int64_t n, int32_t k, int32_t m, int32_t type, int32_t act, const void* dH, int64_t lddh, const void* X, int64_t ldx, const void* Wg, int64_t ldwg,
                                      const void* Wu, int64_t ldwu, const void* G, int64_t ldg, const void* U, int64_t ldu, void* dX, int64_t lddx, void* dWg, int64_t lddwg, void* dWu,
                                      int64_t lddwu, void* workspace, void* stream) {
-    const int64_t at = padded(m), bytes = type == CBM_F32 ? 4 : 2;
-    float* parts = (float*)((char*)workspace + rounded16(n * 2 * at * bytes));
+    const BackRoom room = back_room(n, k, m, type);
+    const int64_t at = room.at;
+    char* base = (char*)workspace;
+    float* parts = (float*)(base + room.parts);
     if (n > 0)
         cbm_with_type(type, [&](auto t) {
             using T = decltype(t);
@@ -180,11 +230,10 @@ cbm_status cbm_launch_gated_backward(int64_t n, int32_t k, int32_t m, int32_t ty
             });
         });
     CbmProduct p{};
-    p.type = p.out.type = type;
-    p.parts = parts;
-    p.out.alpha = 1.0f;
+    p.type = type;
     p.A = workspace;
     p.lda = 2 * at;
+    auto in_units = [&](const void* q, int64_t ld, int64_t along) { return cbm_units((const _Float16*)q, ld, along); };
     if (dX && n > 0) {
         p.M = n;
         p.N = k;
@@ -194,6 +243,15 @@ cbm_status cbm_launch_gated_backward(int64_t n, int32_t k, int32_t m, int32_t ty
         p.B[1] = Wu;
         p.ldb[0] = ldwg;
         p.ldb[1] = ldwu;
+        if (room.copies && !(in_units(Wg, ldwg, m) && in_units(Wu, ldwu, m) && ldwg == ldwu)) {
+            for (int i = 0; i < 2; ++i) {
+                void* to = base + room.weights + i * 2 * k * at;
+                cbm_launch_pack(p.B[i], p.ldb[i], k, m, false, to, at, 0, 0, stream);
+                p.B[i] = to;
+                p.ldb[i] = at;
+            }
+            p.K = at;  // (zeros beyond m)
+        }
         p.out.C[0] = dX;
         p.out.ldc[0] = lddx;
         p.out.columns = k;
@@ -208,6 +266,12 @@ cbm_status cbm_launch_gated_backward(int64_t n, int32_t k, int32_t m, int32_t ty
         p.A = X;
         p.lda = ldx;
         p.a_across = p.b_across = true;
+        if (room.copies && n > 0 && !in_units(X, ldx, k)) {
+            p.lda = p.M = cbm_whole(k, 8);
+            p.out.rows = k;
+            p.A = base + room.x;
+            cbm_launch_pack(X, ldx, n, k, false, base + room.x, p.lda, 0, 0, stream);
+        }
         p.B[0] = workspace;
         p.B[1] = nullptr;
         p.ldb[0] = 2 * at;
@@ -217,7 +281,7 @@ cbm_status cbm_launch_gated_backward(int64_t n, int32_t k, int32_t m, int32_t ty
         p.out.ldc[1] = lddwu;
         p.out.columns = m;
         p.out.at = (int32_t)at;
-        p.parts = cbm_product_parts(k, 2 * at, n, type) > 1 ? parts : nullptr;
+        p.parts = cbm_product_parts(cbm_whole(k, 8), 2 * at, n, type) > 1 ? parts : nullptr;
         cbm_launch_tiles(p, stream);
     }
     return cbm_launched("gated layer backward launch");

@@ -1,4 +1,4 @@
-// Products in tiles with a plain end: sums scaled, added to and rounded.  The gradients of the operators that are made of products, and the steps of the orthogonal update.
+// Products in tiles with a plain end: sums added to, scaled and rounded.  The gradients of the operators that are made of products.
 #include <algorithm>
 #include <type_traits>
 
@@ -8,9 +8,9 @@
 
 namespace {
 
-template <class TO, int W>
-__device__ __forceinline__ void finish(const CbmProductOut& o, int64_t M, int64_t N, int64_t r, int64_t c, float (&v)[W]) {
-    if (r >= M || c >= N) return;
+template <class T, int W>
+__device__ __forceinline__ void finish(const CbmProductOut& o, int64_t N, int64_t r, int64_t c, float (&v)[W]) {
+    if (r >= o.rows || c >= N) return;
     if (o.sums) {
         float* s = o.sums + r * N + c;
         if (!o.first)
@@ -19,47 +19,35 @@ __device__ __forceinline__ void finish(const CbmProductOut& o, int64_t M, int64_
                 if (c + j < N) v[j] += s[j];
         if (!o.last) return cbm_put<W>(o.sums + r * N, c, N, v);
     }
-    float up = o.alpha;
-    if (o.factor) up *= *o.factor;
+    if (o.factor) {
+        const float up = *o.factor;
 #pragma unroll
-    for (int j = 0; j < W; ++j) v[j] *= up;
-    if (o.more)
-#pragma unroll
-        for (int j = 0; j < W; ++j)
-            if (c + j < N) v[j] = fmaf(o.beta, o.more[r * o.ldm + c + j], v[j]);
+        for (int j = 0; j < W; ++j) v[j] *= up;
+    }
     const bool second = o.at && c >= o.at;
     if (second) c -= o.at;
-    TO* C = (TO*)o.C[second];
-    const int64_t ld = o.ldc[second];
-    if (!C) return;
-    if (o.transposed) {
-#pragma unroll
-        for (int j = 0; j < W; ++j)
-            if (c + j < o.columns) C[(c + j) * ld + r] = (TO)v[j];
-    } else {
-        cbm_put<W>(C + r * ld, c, o.columns, v);
-    }
+    if (o.C[second]) cbm_put((T*)o.C[second] + r * o.ldc[second], c, o.columns, v);
 }
 
-template <class Tiles, class T, class TO>
+template <class Tiles, class T>
 __global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_product_kernel(CbmOperand<T> a, CbmOperand<T> b, int64_t chunks, int64_t splits, CbmProductOut o, float* __restrict__ parts) {
     __shared__ uintx4 lds[Tiles::UNITS];
     const CbmTilePlace at = cbm_tile_place((a.count + Tiles::ROWS - 1) / Tiles::ROWS, (b.count + Tiles::COLUMNS - 1) / Tiles::COLUMNS, splits);
     if (!at.any) return;
     Tiles t;
     t.run(lds, a, b, at.m, at.n, (int)(chunks * at.split / splits), (int)(chunks * (at.split + 1) / splits));
-    constexpr int W = cbm_wide<TO>;
+    constexpr int W = cbm_wide<T>;
     t.template pieces<W>(lds, at.m, at.n, [&](int64_t r, int64_t c, float (&v)[W]) {
         if (splits > 1) {
             if (r < a.count) cbm_put<W>(parts + (at.split * a.count + r) * b.count, c, b.count, v);
         } else {
-            finish<TO>(o, a.count, b.count, r, c, v);
+            finish<T>(o, b.count, r, c, v);
         }
     });
 }
 
 // The shares of K of a product, added in order: four values a thread, SLICES threads for the shares of a value where values are few (100 x 512, 64 shares: 34 us with one thread, 6 with eight).
-template <class TO, int SLICES>
+template <class T, int SLICES>
 __global__ __launch_bounds__(256) void cbm_product_join_kernel(int64_t M, int64_t N, int64_t splits, const float* __restrict__ parts, CbmProductOut o) {
     constexpr int PIECES = 256 / SLICES;
     __shared__ floatx4 room[SLICES > 1 ? SLICES : 1][PIECES];
@@ -95,8 +83,48 @@ __global__ __launch_bounds__(256) void cbm_product_join_kernel(int64_t M, int64_
                     for (int j = 0; j < 4; ++j) v[j] += x[j];
                 }
         }
-        if (slice == 0 && i < count) finish<TO>(o, M, N, r, c, v);
+        if (slice == 0 && i < count) finish<T>(o, N, r, c, v);
         if constexpr (SLICES > 1) __syncthreads();
+    }
+}
+
+// 64 x 64 values a workgroup, through LDS.
+__global__ __launch_bounds__(256) void cbm_pack_kernel(const uint16_t* __restrict__ from, int64_t ld, int64_t rows, int64_t columns, bool turned, uint16_t* __restrict__ to, int64_t ldt, int64_t blocks,
+                                                     int64_t at) {
+    __shared__ uint16_t room[64][66];  // [row][column]
+    typedef uint16_t Four __attribute__((ext_vector_type(4), aligned(2)));
+    const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
+    const int64_t high = turned ? columns : rows, wide = turned ? rows : columns, h0 = turned ? c0 : r0, w0 = turned ? r0 : c0;  // as `from` lies
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int h = threadIdx.x / 16 + 16 * i, w = threadIdx.x % 16 * 4;
+        uint16_t v[4] = {};
+        if (h0 + h < high) {
+            const uint16_t* p = from + (h0 + h) * ld + w0 + w;
+            if (w0 + w + 4 <= wide) {
+                const Four x = *reinterpret_cast<const Four*>(p);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = x[j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (w0 + w + j < wide) v[j] = p[j];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) (turned ? room[w + j][h] : room[h][w + j]) = v[j];
+    }
+    __syncthreads();
+    typedef uint16_t Eight __attribute__((ext_vector_type(8)));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = threadIdx.x / 8 + 32 * i, c = threadIdx.x % 8 * 8;
+        if (r0 + r >= (rows + 7) / 8 * 8 || c0 + c >= ldt) continue;
+        Eight v;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = room[r][c + j];
+        const int64_t row = r0 + r, out = blocks ? row / 32 * blocks + row % 32 + at : row;
+        *reinterpret_cast<Eight*>(to + out * ldt + c0 + c) = v;
     }
 }
 
@@ -109,6 +137,7 @@ struct Plan {
 // Microseconds as measured: a workgroup's rate, by how many of a tile run at once; what a workgroup takes beside its products (the first loads, the result); shares of K are written, read and joined in a launch
 // of its own.  Shares of at least 256 k.
 Plan plan(int64_t M, int64_t N, int64_t K, int32_t type, int tile) {
+    M = cbm_whole(M, 8), N = cbm_whole(N, 8), K = cbm_whole(K, 64);  // (a copy in whole units has the same plan)
     const int64_t side = tile ? tile : 128, tiles = std::max<int64_t>(1, (M + side - 1) / side * ((N + side - 1) / side)), at_once = tile == 256 ? 256 : 512;
     const double tflops = tile == 256 ? 1150.0 : tile == 128 ? 900.0 : type == CBM_F32 ? 140.0 : 550.0, beside = tile == 256 ? 9.0 : 5.0;
     const double each = 2.0 * (double)(side * side * K) / (tflops * 1e6 / (double)at_once);
@@ -126,7 +155,7 @@ Plan plan(int64_t M, int64_t N, int64_t K, int32_t type, bool units) {
     return large.us < small.us ? large : small;
 }
 
-template <class T, class TO, CbmTileOrder OA, CbmTileOrder OB, CbmTilePair PAIR>
+template <class T, CbmTileOrder OA, CbmTileOrder OB, CbmTilePair PAIR>
 void launch(const CbmProduct& p, hipStream_t stream) {
     const int64_t K = p.at ? p.at + p.K : p.K;
     const CbmOperand<T> a{{(const T*)p.A, nullptr}, {p.lda, 0}, p.M, K, 0};
@@ -134,12 +163,14 @@ void launch(const CbmProduct& p, hipStream_t stream) {
     bool units = false;
     if constexpr (sizeof(T) == 2)
         units = cbm_units(a.p[0], a.ld[0], OA == ALONG_K ? K : p.M) && cbm_units(b.p[0], b.ld[0], OB == ALONG_K ? p.K : p.N) && (PAIR == SINGLE || (cbm_units(b.p[1], b.ld[1], p.K) && b.ld[1] == b.ld[0]));
-    const Plan how = plan(p.M, p.N, K, p.type, units);
+    const Plan how = plan(p.M, p.N, p.at ? 2 * p.at : K, p.type, units);
     const int64_t splits = p.parts ? how.splits : 1;
+    CbmProductOut out = p.out;
+    if (!out.rows) out.rows = p.M;
     auto run = [&](auto* tiles_type) {
         typedef std::remove_pointer_t<decltype(tiles_type)> Tiles;
         const int64_t tiles = (p.M + Tiles::ROWS - 1) / Tiles::ROWS * ((p.N + Tiles::COLUMNS - 1) / Tiles::COLUMNS), chunks = (K + Tiles::BK - 1) / Tiles::BK;
-        cbm_product_kernel<Tiles, T, TO><<<(unsigned)((tiles * splits + CBM_XCD - 1) / CBM_XCD * CBM_XCD), 256, 0, stream>>>(a, b, chunks, splits, p.out, p.parts);
+        cbm_product_kernel<Tiles, T><<<(unsigned)((tiles * splits + CBM_XCD - 1) / CBM_XCD * CBM_XCD), 256, 0, stream>>>(a, b, chunks, splits, out, p.parts);
     };
     if (how.tile == 0) run((CbmTiles<T, 128, 128, 2, 2, OA, OB, PAIR>*)nullptr);
     if constexpr (sizeof(T) == 2) {
@@ -150,18 +181,18 @@ void launch(const CbmProduct& p, hipStream_t stream) {
         const int64_t pieces = p.M * ((p.N + 3) / 4);
         auto join = [&](auto slices) {
             constexpr int SLICES = decltype(slices)::value, EACH = 256 / SLICES;
-            cbm_product_join_kernel<TO, SLICES><<<(unsigned)std::min<int64_t>((pieces + EACH - 1) / EACH, 1 << 20), 256, 0, stream>>>(p.M, p.N, splits, p.parts, p.out);
+            cbm_product_join_kernel<T, SLICES><<<(unsigned)std::min<int64_t>((pieces + EACH - 1) / EACH, 1 << 20), 256, 0, stream>>>(p.M, p.N, splits, p.parts, out);
         };
         if (splits >= 8 && pieces < 1 << 16) join(std::integral_constant<int, 8>{});
         else join(std::integral_constant<int, 1>{});
     }
 }
-template <class T, class TO>
+template <class T>
 void launch(const CbmProduct& p, hipStream_t stream) {
-    if (p.at) launch<T, TO, ALONG_K, ALONG_K, PAIR_K>(p, stream);
-    else if (p.a_across) launch<T, TO, ACROSS_K, ACROSS_K, SINGLE>(p, stream);
-    else if (p.b_across) launch<T, TO, ALONG_K, ACROSS_K, SINGLE>(p, stream);
-    else launch<T, TO, ALONG_K, ALONG_K, SINGLE>(p, stream);
+    if (p.at) launch<T, ALONG_K, ALONG_K, PAIR_K>(p, stream);
+    else if (p.a_across) launch<T, ACROSS_K, ACROSS_K, SINGLE>(p, stream);
+    else if (p.b_across) launch<T, ALONG_K, ACROSS_K, SINGLE>(p, stream);
+    else launch<T, ALONG_K, ALONG_K, SINGLE>(p, stream);
 }
 
 }  // namespace
@@ -172,17 +203,22 @@ int64_t cbm_product_parts(int64_t M, int64_t N, int64_t K, int32_t type) {
     return type == CBM_F32 ? any : std::max(any, plan(M, N, K, type, true).splits);
 }
 
+void cbm_launch_pack(const void* from, int64_t ld, int64_t rows, int64_t columns, bool turned, void* to, int64_t ldt, int64_t blocks, int64_t at, void* stream) {
+    // (a grid is 65,535 high at most)
+    for (int64_t r = 0; r < rows; r += 4194240) {  // (a multiple of 64)
+        const int64_t some = std::min<int64_t>(rows - r, 4194240);
+        cbm_pack_kernel<<<dim3((unsigned)((ldt + 63) / 64), (unsigned)((some + 63) / 64)), 256, 0, (hipStream_t)stream>>>((const uint16_t*)from + (turned ? r : r * ld), ld, some, columns, turned,
+                                                                                                                (uint16_t*)to + (blocks ? r / 32 * blocks : r) * ldt, ldt, blocks, at);
+    }
+}
+
 int cbm_product_tile(int64_t M, int64_t N, int64_t K, int32_t type) {
     const Plan large = plan(M, N, K, type, 256), small = plan(M, N, K, type, 128);
     return large.us < small.us ? 256 : 128;
 }
 
 void cbm_launch_tiles(const CbmProduct& p, void* stream) {
-    cbm_with_type(p.type, [&](auto t) {
-        using T = decltype(t);
-        if constexpr (std::is_same<T, float>::value) cbm_with_type(p.out.type, [&](auto to) { launch<float, decltype(to)>(p, (hipStream_t)stream); });
-        else launch<T, T>(p, (hipStream_t)stream);
-    });
+    cbm_with_type(p.type, [&](auto t) { launch<decltype(t)>(p, (hipStream_t)stream); });
 }
 
 cbm_status cbm_launched(const char* what) {

@@ -266,3 +266,47 @@ def test_backward_with_shares_of_k(env, n, k, m):  # noqa: F811
     torch, cbm = env
     for name in ("f32", "bf16"):
         _check_backward(*_backward(torch, cbm, n, k, m, name, "silu", 0, 0), name, "silu")
+
+
+def _gpu(torch, n, k, name, pad, offset, scale=1.0):
+    t, whole = _matrix(torch, np.zeros((0, k)), name, 0)
+    whole = torch.full((offset + n * (k + pad),), math.nan, dtype=_type(torch, name), device="cuda")
+    t = whole[offset:].view(n, k + pad)[:, :k]
+    t.copy_(torch.randn((n, k), device="cuda") * scale)
+    return t
+
+
+def _within(got, want, bound, name):
+    bound = bound + ROUNDING[name] * (want.abs() + bound) + LEAST[name]
+    assert bool(((got.double() - want).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("name", ["bf16", "f16"])
+@pytest.mark.parametrize("pad,offset", [(0, 0), (1, 1), (8, 0)])
+@pytest.mark.parametrize("n,k,m", [(12001, 515, 4099), (4097, 512, 12288), (1025, 1000, 25000)])
+def test_large_products(env, name, n, k, m, pad, offset):  # noqa: F811
+    """Matrices of odd widths, strides and addresses are copied into rows of whole units, and the weights of many rows turned.  Against 64 bits on the GPU."""
+    torch, cbm = env
+    torch.manual_seed(n)
+    X, Wg, Wu = _gpu(torch, n, k, name, pad, offset), _gpu(torch, k, m, name, pad, offset, k ** -0.5), _gpu(torch, k, m, name, pad, offset, k ** -0.5)
+    H, G, U_, dX, dWg, dWu = (_gpu(torch, *s, name, pad, offset) for s in ((n, m), (n, m), (n, m), (n, k), (k, m), (k, m)))
+    need = max(cbm.cbm_gated_linear_workspace_bytes(n, k, m, X.dtype), cbm.cbm_gated_linear_backward_workspace_bytes(n, k, m, X.dtype))
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    cbm.cbm_gated_linear(X, Wg, Wu, H, G, U_, activation="relu", workspace=ws)
+    x, wg, wu = X.double(), Wg.double(), Wu.double()
+    g, u = x @ wg, x @ wu
+    of_g, of_u = SUM(k) * (x.abs() @ wg.abs()), SUM(k) * (x.abs() @ wu.abs())
+    _within(G, g, of_g, name)
+    _within(U_, u, of_u, name)
+    _within(H, g.clamp_min(0) * u, of_g * (u.abs() + of_u) + g.abs() * of_u, name)
+    del g, u, of_g, of_u
+    dH = _gpu(torch, n, m, name, pad, offset)
+    cbm.cbm_gated_linear_backward(dH, X, Wg, Wu, G, U_, dX, dWg, dWu, activation="relu", workspace=ws)
+    dh, g, u = dH.double(), G.double(), U_.double()
+    du, dg = dh * g.clamp_min(0), dh * u * (g > 0)
+    del dh, g, u
+    half = 1.01 * ROUNDING[name]  # of dG and dU, and fp16's smallest values
+    t = lambda a: a.t().contiguous()  # noqa: E731
+    for got, want, terms in ((dX, dg @ t(wg) + du @ t(wu), dg.abs() @ t(wg.abs()) + du.abs() @ t(wu.abs())), (dWg, t(x) @ dg, t(x.abs()) @ dg.abs()), (dWu, t(x) @ du, t(x.abs()) @ du.abs())):
+        # (fp16's smallest dG and dU: 2^-25 each, of at most 40,000 terms of size below 6)
+        _within(got, want, (half + SUM(max(n, 2 * m))) * terms + (0.01 if name == "f16" else 0.0), name)

@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 
 from oracle import train_oracle as orc
-from test_gpu_gated_linear import SUM, TYPES, _near, _rounded
+from test_gpu_gated_linear import SUM, TYPES, _gpu, _near, _rounded, _within
 from test_gpu_layer_norm import _matrix, _numbers, _type, _untouched, env  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -300,3 +300,44 @@ def test_whole_units(env, name, n, d, c):  # noqa: F811
         X, W, L = _inputs(torch, n, d, c, name, pad, 0)
         _check_forward(X, W, L, *_forward(torch, cbm, X, W, L))
         _check_backward(X, W, L, *_backward(torch, cbm, X, W, L, pad, 0), name)
+
+
+@pytest.mark.parametrize("name", ["bf16", "f16"])
+@pytest.mark.parametrize("pad,offset", [(0, 0), (1, 1), (8, 0)])
+@pytest.mark.parametrize("n,d,c", [(12001, 515, 8199), (4097, 512, 24576), (1025, 1000, 50001), (300007, 258, 1061)])
+def test_large_products(env, name, n, d, c, pad, offset):  # noqa: F811
+    """Matrices of odd widths, strides and addresses are copied into rows of whole units, and the weights of many rows turned; the last size in several pieces, with a short last unit.  Against 64 bits on the
+    GPU."""
+    torch, cbm = env
+    torch.manual_seed(n)
+    X, W = _gpu(torch, n, d, name, pad, offset), _gpu(torch, d, c, name, pad, offset, 3 * d ** -0.5)
+    L = torch.randint(-1, c + 1, (n,), device="cuda")
+    need = max(cbm.cbm_linear_log_probs_workspace_bytes(n, d, c, X.dtype), cbm.cbm_linear_log_probs_backward_workspace_bytes(n, d, c, X.dtype))
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    logp, stats = torch.empty(n, device="cuda"), torch.empty((n, 2), device="cuda")
+    cbm.cbm_linear_log_probs(X, W, L, logp, stats, workspace=ws)
+    x, w = X.double(), W.double()
+    z = x @ w
+    largest, l = z.amax(dim=1), torch.logsumexp(z, dim=1)
+    given = (L >= 0) & (L < c)
+    want = torch.where(given, z.gather(1, L.clamp(0, c - 1)[:, None])[:, 0] - l, torch.zeros_like(l))
+    # a score's sum is off by at most SUM(d) of its terms' sizes, which add up to less than 3 sqrt(d) 2 on average here and never to five times that; exponents of up to 20, c / 32 + 40 additions
+    bound = SUM(d) * 30 * math.sqrt(d) + U * (6 * 20 + c / 32 + 100)
+    assert float((logp - want).abs().max()) <= 3 * bound and float((stats[:, 0] - largest).abs().max()) <= bound and float((stats[:, 1] - (l - largest)).abs().max()) <= 2 * bound
+    scale = 1024.0 if name == "f16" else 1.0
+    dlogp = (torch.rand(n, device="cuda") + 0.5) * (-scale / n)
+    dX, dW = _gpu(torch, n, d, name, pad, offset), _gpu(torch, d, c, name, pad, offset)
+    cbm.cbm_linear_log_probs_backward(X, W, L, stats, dlogp, dX, dW, workspace=ws)
+    a = (dlogp * given).double()[:, None]
+    dz = torch.exp(z - stats.double().sum(1, keepdim=True)).neg_()
+    del z
+    dz[torch.arange(n, device="cuda"), L.clamp(0, c - 1)] += 1.0
+    dz *= a
+    # a dz is off by its rounding and by what its exponent is off by
+    of = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11}[name] * 1.01 + 4 * bound
+    least = 2.0 ** -25 * 2.0 ** -15 * float(dlogp.abs().max()) if name == "f16" else 0.0
+    t = lambda a: a.t().contiguous()  # noqa: E731
+    size = dz.abs()
+    off = of * size + least + 4 * bound * a.abs() * 1e-3
+    _within(dX, dz @ t(w), SUM(c) * (size @ t(w.abs())) + off @ t(w.abs()), name)
+    _within(dW, t(x) @ dz, SUM(n) * (t(x.abs()) @ size) + t(x.abs()) @ off, name)
