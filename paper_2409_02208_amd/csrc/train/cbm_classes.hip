@@ -104,7 +104,20 @@ __global__ __launch_bounds__(256) void cbm_classes_join_kernel(int64_t n, int64_
     const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (r >= n) return;
     Sums all{-INFINITY, 0.0f};
-    for (int64_t i = lane; i < count; i += 64) all = joined(all, parts[r * count + i]);
+    constexpr int AHEAD = 8;  // (one row of 32,000 columns has 500 parts: their loads under way together, and one maximum for eight: 19.5 -> 17.9 us)
+    for (int64_t i = lane; i < count; i += 64 * AHEAD) {
+        Sums some[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) some[k] = i + 64 * k < count ? parts[r * count + i + 64 * k] : Sums{-INFINITY, 0.0f};
+        float m = all.m;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) m = fmaxf(m, some[k].m);
+        const float away = m == -INFINITY ? 0.0f : m;
+        float s = all.s * __builtin_amdgcn_exp2f((all.m - away) * LOG2E);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) s += some[k].s * __builtin_amdgcn_exp2f((some[k].m - away) * LOG2E);
+        all = {m, s};
+    }
     const float m = lanes_all<64>(all.m, [](float a, float b) { return fmaxf(a, b); }), away = m == -INFINITY ? 0.0f : m;
     const float s = lanes_sum<64>(all.s * __builtin_amdgcn_exp2f((all.m - away) * LOG2E));
     if (lane) return;

@@ -238,7 +238,7 @@ struct HalvesTiles : CbmTileSums<B, B, 2, 2> {
 // tiles of 42 chunks: waves with a quarter of the tile 21 us, a step of two products between barriers; this 7.)
 struct HalvesShares {
     typedef CbmAlignedSide<_Float16, 256, ALONG_K, SINGLE> Side;  // (a wave's loads are 64 rows)
-    static constexpr int ROWS = 64, COLUMNS = 64, GROUPS = 1, LOADS = Side::LOADS, SLOT = 64 * 8, OUT_STRIDE = 17, UNITS = 4 * 4 * SLOT;
+    static constexpr int ROWS = 64, GROUPS = 1, LOADS = Side::LOADS, SLOT = 64 * 8, OUT_STRIDE = 17, UNITS = 4 * 4 * SLOT;
     static_assert(LOADS == 8 && UNITS >= 4 * 64 * OUT_STRIDE, "");
 
     __device__ __forceinline__ void run(uintx4* lds, const CbmOperand<_Float16>& a, const CbmOperand<_Float16>& b, int tile_m, int tile_n, int last) {
