@@ -436,7 +436,7 @@ size_t cbm_gated_linear_backward_workspace_bytes(int64_t n, int32_t k, int32_t m
  *   workspace    cbm_linear_log_probs_workspace_bytes(n, d, c, type) bytes.
  * A row with a score of NaN or +infinity has NaN for all of it (0 without a label).
  *
- * cbm_linear_log_probs_backward -- with dZ = dlogp (1[label] - p), rounded to `type` (fp16: at a size that fits the largest |dlogp|), and nothing for rows without a label,
+ * cbm_linear_log_probs_backward -- with dZ = dlogp (1[label] - p), rounded to `type` (16 bits: at 2^15 over the largest finite |dlogp| of its size), and nothing for rows without a label,
  *   dX = dZ W^T (n x d),  dW = X^T dZ (d x c; zeros for n = 0), of `type`; either may be NULL.  Values of X must be finite in rows without a label, too.
  *   The scores are made again from X and W, a piece of the classes at a time, with m and l from `stats`.
  *   workspace    cbm_linear_log_probs_backward_workspace_bytes(n, d, c, type) bytes: dZ of a piece (512 MiB or 1,024 classes), and sums.

@@ -133,19 +133,27 @@ __global__ __launch_bounds__(256) void cbm_classes_join_kernel(int64_t n, int64_
     }
 }
 
-// fp16: the gradients of a batch's scores are small beside 2^-14.  They are kept at 2^15 over the largest |dlogp| of their size, where 1 - p fits and a p down to 2^-29 keeps all its bits; what is
-// made of them is multiplied by the factor, scale[0], and they by scale[1] dlogp.
+// Types of 16 bits: dZ is kept at 2^15 over the largest finite |dlogp| of its size; what is made of it is multiplied by the factor, scale[0], and dlogp by scale[1].  In fp16 the gradients of a batch's
+// scores would be small beside 2^-14: here 1 - p fits and a p down to 2^-29 keeps all its bits.  In both types the rows of a mean, which all have the same dlogp, have their labels' own 1 - p just below a
+// power of two, where half a step is 2^-9 (bf16) of it at most and p itself where that is less; at 1 / n it would be up to 2^-8, the same for every row, and nothing evens it out.
 __global__ __launch_bounds__(1024) void cbm_classes_scale_kernel(int64_t n, const float* __restrict__ dlogp, float* __restrict__ scale) {
     __shared__ float room[16];
-    float most = 0.0f;
-    for (int64_t i = threadIdx.x; i < n; i += 1024) most = fmaxf(most, fabsf(dlogp[i]));
+    constexpr int AHEAD = 8;
+    float most = 0x1p-100f;  // (neither factor overflows)
+    for (int64_t i = threadIdx.x; i < n; i += 1024 * AHEAD) {
+        float v[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) v[k] = fabsf(dlogp[min(i + 1024 * k, n - 1)]);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) most = v[k] < INFINITY ? fmaxf(most, v[k]) : most;
+    }
     most = lanes_all<64>(most, [](float a, float b) { return fmaxf(a, b); });
     if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = most;
     __syncthreads();
     if (threadIdx.x) return;
     for (int i = 1; i < 16; ++i) most = fmaxf(most, room[i]);
     scale[0] = most * 0x1p-15f;
-    scale[1] = most > 0.0f ? 0x1p15f / most : 0.0f;
+    scale[1] = 0x1p15f / most;
 }
 
 // dZ of columns first .. first + width - 1, rounded to the type (half a step, as much as the gradients that are made of it are rounded by).
@@ -169,14 +177,17 @@ __global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_classes_slopes_kernel(
         const int64_t at_r = min(r, a.count - 1), label = label_of(labels, label_bits, at_r);
         const float m = stats[2 * at_r], l = stats[2 * at_r + 1];
         const bool none = label < 0 || label >= c || m == -INFINITY;
-        const float slope = none ? 0.0f : scale ? dlogp[at_r] * scale[1] : dlogp[at_r], from = none ? 0.0f : m, down = none ? -INFINITY : -l * LOG2E;
+        const float slope = none ? 0.0f : scale ? dlogp[at_r] * scale[1] : dlogp[at_r], from = none ? 0.0f : m, down = none ? -INFINITY : -l * (sizeof(T) == 4 ? 1.0f : LOG2E);
         const int64_t place = label - first - ((int64_t)at.n * BN + t.first_column());
         hot[i] = none || place < 0 || place >= 32 * Tiles::TN ? -1 : (int)place;  // the label's place among the wave's columns
         up[i] = slope;
 #pragma unroll
         for (int j = 0; j < Tiles::TN; ++j)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) t.acc[i][j][v] = -slope * __builtin_amdgcn_exp2f(fmaf(t.acc[i][j][v] - from, LOG2E, down));
+            for (int v = 0; v < 16; ++v) {
+                const float under = t.acc[i][j][v] - from;
+                t.acc[i][j][v] = -slope * (sizeof(T) == 4 ? cbm_exp<T>(under + down) : __builtin_amdgcn_exp2f(fmaf(under, LOG2E, down)));
+            }
     }
     constexpr int W = cbm_wide<T>;
     t.template pieces<W>(
@@ -329,7 +340,7 @@ cbm_status cbm_launch_classes_backward(int64_t n, int32_t d, int32_t c, int32_t 
     const Room room = back_room(n, d, c, type);
     const int64_t piece = piece_of(n, c, type);
     float *scale = (float*)((char*)workspace + room.scale), *sums = (float*)((char*)workspace + room.sums), *parts = (float*)((char*)workspace + room.parts);
-    if (type != CBM_F16) scale = nullptr;
+    if (type == CBM_F32) scale = nullptr;
     if (scale && n > 0) cbm_classes_scale_kernel<<<1, 1024, 0, stream>>>(n, dlogp, scale);
     cbm_with_type(type, [&](auto t) {
         using T = decltype(t);

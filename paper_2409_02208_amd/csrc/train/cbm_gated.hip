@@ -8,26 +8,26 @@
 
 namespace {
 
-template <int ACT>
+template <class T, int ACT>
 __device__ __forceinline__ float activated(float g) {
     if constexpr (ACT == CBM_RELU) return g <= 0.0f ? 0.0f : g;  // (NaN stays)
-    if constexpr (ACT == CBM_SILU) return g / (1.0f + __expf(-g));
+    if constexpr (ACT == CBM_SILU) return g / (1.0f + cbm_exp<T>(-g));
     return 0.5f * g * erfcf(g * -0.70710678f);
 }
 // the activation and its slope
-template <int ACT>
+template <class T, int ACT>
 __device__ __forceinline__ void activated(float g, float& value, float& slope) {
     if constexpr (ACT == CBM_RELU) {
-        value = activated<ACT>(g);
+        value = activated<T, ACT>(g);
         slope = g > 0.0f ? 1.0f : 0.0f;
     } else if constexpr (ACT == CBM_SILU) {
-        const float s = 1.0f / (1.0f + __expf(-g));
+        const float s = 1.0f / (1.0f + cbm_exp<T>(-g));
         value = g * s;
         slope = s * fmaf(g, 1.0f - s, 1.0f);
     } else {
         const float below = 0.5f * erfcf(g * -0.70710678f);
         value = g * below;
-        slope = fmaf(g, 0.39894228f * __expf(-0.5f * g * g), below);
+        slope = fmaf(g, 0.39894228f * cbm_exp<T>(-0.5f * g * g), below);
     }
 }
 template <class F>
@@ -52,7 +52,7 @@ __global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_gated_kernel(CbmOperan
         if (r >= a.count) return;
         float h[W];
 #pragma unroll
-        for (int v = 0; v < W; ++v) h[v] = activated<ACT>(g[v]) * u[v];
+        for (int v = 0; v < W; ++v) h[v] = activated<T, ACT>(g[v]) * u[v];
         cbm_put(H + r * ldh, c, m, h, far);
         if (G) cbm_put(G + r * ldg, c, m, g, far);
         if (U) cbm_put(U + r * ldu, c, m, u, far);
@@ -74,7 +74,7 @@ __global__ __launch_bounds__(64 * few_waves(NR)) void cbm_gated_few_kernel(int64
     const int64_t c = first + j, r = above + in;
     if (r >= n || in >= NR || c >= m) return;
     const float g = Rows::total(room, 0, in, j), u = Rows::total(room, 1, in, j);
-    H[r * ldh + c] = (T)(activated<ACT>(g) * u);
+    H[r * ldh + c] = (T)(activated<T, ACT>(g) * u);
     if (G) G[r * ldg + c] = (T)g;
     if (U) U[r * ldu + c] = (T)u;
 }
@@ -105,7 +105,7 @@ __global__ __launch_bounds__(256) void cbm_gated_slopes_kernel(int64_t n, int m,
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             float value, slope;
-            activated<ACT>(g[j], value, slope);
+            activated<T, ACT>(g[j], value, slope);
             du[j] = c + j < m ? dh[j] * value : 0.0f;
             dg[j] = c + j < m ? dh[j] * u[j] * slope : 0.0f;
         }

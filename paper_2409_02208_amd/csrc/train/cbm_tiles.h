@@ -21,6 +21,15 @@ struct CbmTileType<float> {
     static constexpr int PARTS = 3, KG = 4;
 };
 
+// e^x from 2^x.  fp32: with what x log2(e) loses when it is rounded, which at an x of -20 is twenty steps of the result.
+template <class T>
+__device__ __forceinline__ float cbm_exp(float x) {
+    const float t = x * 1.44269504f;
+    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_exp2f(t);
+    const float lost = fmaxf(fmaf(x, 1.44269504f, -t) + x * 1.92596299e-8f, -1.0f);  // (NaN where x is infinite)
+    return __builtin_amdgcn_exp2f(t) * fmaf(lost, 0.693147181f, 1.0f);
+}
+
 enum CbmTileOrder { ALONG_K, ACROSS_K };
 
 // One operand of a product: `count` rows of `K` values.  ALONG_K: value (r, k) is p[r ld + k]; ACROSS_K: p[k ld + r].  Two matrices may share the operand: PAIR_K, the second one's k follow

@@ -139,6 +139,55 @@ def test_small_gradients_in_fp16_are_not_lost(env):  # noqa: F811
     _check_backward(X, W, L, *_backward(torch, cbm, X, W, L, 0, 0, size=1e-5), "f16")
 
 
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("n", [1, 130, 9001])
+def test_a_mean_is_not_rounded_alike_in_every_row(env, name, n):  # noqa: F811
+    """The same dlogp in every row, which the type would round by almost half a step; scores of zero, so that p is 2^-10 everywhere and a label's 1 - p is at most that far from a value of the type."""
+    torch, cbm = env
+    d, c = 40, 1024
+    rng = np.random.default_rng(n)
+    X, W = _matrix(torch, rng.standard_normal((n, d)), name, 0)[0], _matrix(torch, np.zeros((d, c)), name, 0)[0]
+    L = torch.from_numpy(rng.integers(0, c, n)).cuda()
+    stats = torch.tensor([0.0, math.log(c)], device="cuda").repeat(n, 1)
+    half = {"f32": U, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}[name]
+    a = -(1 + 0.97 * half) * 2.0 ** -7
+    dX, dW = torch.ones_like(X), torch.empty_like(W)
+    ws = torch.empty(cbm.cbm_linear_log_probs_backward_workspace_bytes(n, d, c, X.dtype), dtype=torch.uint8, device="cuda")
+    cbm.cbm_linear_log_probs_backward(X, W, L, stats, torch.full((n,), a, device="cuda"), dX, dW, workspace=ws)
+    x = _numbers(X)
+    dz = np.full((n, c), -float(np.float32(a)) / c)
+    dz[np.arange(n), L.cpu().numpy()] += float(np.float32(a))
+    # 1 - p: 2^-10 where the type lacks it; p: the logarithm's rounding and the exponential's; the factor's two; then the sum and the result's own rounding
+    size = np.abs(dz) * (12 * U + (2.0 ** -10 if name == "bf16" else 0.0))
+    least = 2.0 ** -25 * 2.0 ** -15 * abs(a) if name == "f16" else 0.0
+    _near(dW, x.T @ dz, _rounded(x.T @ dz, SUM(n) * (np.abs(x.T) @ np.abs(dz)) + np.abs(x.T) @ (size + least), name))
+    assert not bool(dX.any())
+
+
+@pytest.mark.parametrize("name", TYPES)
+def test_slopes_that_are_not_finite_or_nothing(env, name):  # noqa: F811
+    """A row's infinite or missing slope is its own (and that of the weights' sums), and none at all leaves zeros."""
+    torch, cbm = env
+    n, d, c = 200, 24, 300
+    X, W, L = _inputs(torch, n, d, c, name, 0, 0)
+    L.clamp_(0, c - 1)
+    ws = torch.empty(cbm.cbm_linear_log_probs_backward_workspace_bytes(n, d, c, X.dtype), dtype=torch.uint8, device="cuda")
+    stats = _forward(torch, cbm, X, W, L)[1]
+    a, rows = -torch.rand(n, device="cuda") - 0.1, torch.ones(n, dtype=torch.bool, device="cuda")
+    some = []
+    for bad in (0.0, math.nan, math.inf):
+        a[[3, 150]] = bad
+        dX, dW = torch.empty_like(X), torch.empty_like(W)
+        cbm.cbm_linear_log_probs_backward(X, W, L, stats, a, dX, dW, workspace=ws)
+        some.append(dX)
+    rows[[3, 150]] = False
+    assert torch.equal(some[0][rows], some[1][rows]) and torch.equal(some[0][rows], some[2][rows])
+    assert not bool(some[0][~rows].any()) and not bool(some[1][~rows].isfinite().any()) and not bool(some[2][~rows].isfinite().any())
+    for size in (0.0, 1e-42):
+        cbm.cbm_linear_log_probs_backward(X, W, L, stats, torch.full_like(a, size), dX, dW, workspace=ws)
+        assert float(dX.abs().max()) <= 1e-38 and float(dW.abs().max()) <= 1e-38
+
+
 def test_backward_against_differences(env):  # noqa: F811
     torch, cbm = env
     X, W, L = _inputs(torch, 5, 4, 6, "f32", 0, 0)
