@@ -410,12 +410,13 @@ cbm_status cbm_log_probs_backward(int64_t n, int32_t c, int32_t type, const void
  *   G, U         receive X Wg and X Wu (n x m, of `type`), which the backward pass reads; either may be NULL.  H is made of the sums before they are rounded.
  *   workspace    cbm_gated_linear_workspace_bytes(n, k, m, type) bytes (may be 0).
  *
- * cbm_gated_linear_backward -- with dU = dH o a(G) and dG = dH o U o a'(G) (a'(0) = 0 for CBM_RELU), each rounded to `type`:
+ * cbm_gated_linear_backward -- with dU = dH o a(G) and dG = dH o U o a'(G) (a'(0) = 0 for CBM_RELU), each rounded to `type` unless the products are small:
  *   dX = dG Wg^T + dU Wu^T (n x k),  dWg = X^T dG,  dWu = X^T dU (k x m), of `type`; each may be NULL, not all three.  dWg and dWu are zeros for n = 0.
  *   workspace    cbm_gated_linear_backward_workspace_bytes(n, k, m, type) bytes.
  *
  * Products of 16-bit types are exact, those of fp32 are made of three bf16 parts of each value (left out is at most 2^-24 of a term; parts below 2^-126 are taken for zero); sums
- * are fp32.  In fp32, a value that is not finite, or from 2^127 on, makes NaN of every sum that it is part of.
+ * are fp32.  (Small products of fp32: in fp32 throughout.)  In fp32, a value that is not finite, or from 2^127 on, leaves no finite sum that it is part of.
+ * Workspaces hold copies of operands and shares of sums, or slopes in fp32, whatever the sizes ask for: a smaller call may need more than a larger one.
  */
 typedef enum { CBM_SILU = 0, CBM_GELU = 1, CBM_RELU = 2 } cbm_activation;
 cbm_status cbm_gated_linear(int64_t n, int32_t k, int32_t m, int32_t type, int32_t activation, const void* X, int64_t ldx, const void* Wg, int64_t ldwg,
@@ -436,7 +437,7 @@ size_t cbm_gated_linear_backward_workspace_bytes(int64_t n, int32_t k, int32_t m
  *   workspace    cbm_linear_log_probs_workspace_bytes(n, d, c, type) bytes.
  * A row with a score of NaN or +infinity has NaN for all of it (0 without a label).
  *
- * cbm_linear_log_probs_backward -- with dZ = dlogp (1[label] - p), rounded to `type` (16 bits: at 2^15 over the largest finite |dlogp| of its size), and nothing for rows without a label,
+ * cbm_linear_log_probs_backward -- with dZ = dlogp (1[label] - p), rounded to `type` unless the products are small (16 bits: at 2^15 over the largest finite |dlogp| of its size), and nothing for rows without a label,
  *   dX = dZ W^T (n x d),  dW = X^T dZ (d x c; zeros for n = 0), of `type`; either may be NULL.  Values of X must be finite in rows without a label, too.
  *   The scores are made again from X and W, a piece of the classes at a time, with m and l from `stats`.
  *   workspace    cbm_linear_log_probs_backward_workspace_bytes(n, d, c, type) bytes: dZ of a piece (512 MiB or 1,024 classes), and sums.

@@ -5,6 +5,7 @@
 #include "cbm_few_rows.h"
 #include "cbm_internal.h"
 #include "cbm_products.h"
+#include "cbm_small.h"
 
 namespace {
 
@@ -97,6 +98,52 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void cbm_classes_few_kernel(int64_t
     if (labels && some && label_of(labels, label_bits, r) == first + lane) chosen[r] = z;
 }
 
+// A small product: a workgroup's 32 columns are a part of its rows (256 x 1024 with 1024 x 256 in fp32 67 -> 12 us).
+template <class T>
+__global__ __launch_bounds__(512) void cbm_classes_small_kernel(int64_t n, int64_t d, int64_t c, const T* __restrict__ X, int64_t ldx, const T* __restrict__ W, int64_t ldw, const void* __restrict__ labels,
+                                                              int label_bits, Sums* __restrict__ parts, float* __restrict__ chosen) {
+    typedef CbmSmallTile<T, T, ALONG_K, ACROSS_K, 1> Tile;
+    __shared__ typename Tile::Room room;
+    const int64_t r0 = (int64_t)blockIdx.y * Tile::SIDE, c0 = (int64_t)blockIdx.x * Tile::SIDE, r = r0 + Tile::row(), column = c0 + Tile::column();
+    Tile t;
+    t.add(X, ldx, n, r0, {W}, {ldw}, c, c0, d);
+    t.share(room);
+    float z[2];
+    Tile::total(room, 0, z);
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+        if (column + j >= c) z[j] = -INFINITY;
+    const float m = lanes_all<16>(fmaxf(z[0], z[1]), [](float a, float b) { return fmaxf(a, b); }), away = m == -INFINITY ? 0.0f : m;
+    const float s = lanes_sum<16>(cbm_exp<T>(z[0] - away) + cbm_exp<T>(z[1] - away));
+    if (r >= n) return;
+    if (Tile::column() == 0) parts[r * gridDim.x + blockIdx.x] = {m, s};
+    if (!labels) return;
+    const int64_t place = label_of(labels, label_bits, r) - column;
+    if (place >= 0 && place < 2 && column + place < c) chosen[r] = place ? z[1] : z[0];
+}
+
+// A small product's dZ, in fp32.
+template <class T>
+__global__ __launch_bounds__(512) void cbm_classes_small_slopes_kernel(int64_t n, int64_t d, int64_t c, const T* __restrict__ X, int64_t ldx, const T* __restrict__ W, int64_t ldw,
+                                                                     const void* __restrict__ labels, int label_bits, const float* __restrict__ stats, const float* __restrict__ dlogp,
+                                                                     float* __restrict__ dZ, int64_t lddz) {
+    typedef CbmSmallTile<T, T, ALONG_K, ACROSS_K, 1> Tile;
+    __shared__ typename Tile::Room room;
+    const int64_t r0 = (int64_t)blockIdx.y * Tile::SIDE, c0 = (int64_t)blockIdx.x * Tile::SIDE, r = r0 + Tile::row(), column = c0 + Tile::column();
+    Tile t;
+    t.add(X, ldx, n, r0, {W}, {ldw}, c, c0, d);
+    t.share(room);
+    if (r >= n) return;
+    float z[2], v[2];
+    Tile::total(room, 0, z);
+    const int64_t label = label_of(labels, label_bits, r);
+    const float m = stats[2 * r], l = stats[2 * r + 1], slope = dlogp[r];
+    const bool none = label < 0 || label >= c || m == -INFINITY;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) v[j] = none ? 0.0f : (column + j == label ? slope : 0.0f) - slope * cbm_exp<float>((z[j] - m) - l);
+    cbm_put(dZ + r * lddz, column, c, v);
+}
+
 // A wave a row: its parts in order, a lane's 64 apart, then over the lanes.
 __global__ __launch_bounds__(256) void cbm_classes_join_kernel(int64_t n, int64_t c, int64_t count, const void* __restrict__ labels, int label_bits, const Sums* __restrict__ parts,
                                                              const float* __restrict__ chosen, float* __restrict__ logp, float* __restrict__ stats) {
@@ -156,7 +203,8 @@ __global__ __launch_bounds__(1024) void cbm_classes_scale_kernel(int64_t n, cons
     scale[1] = 0x1p15f / most;
 }
 
-// dZ of columns first .. first + width - 1, rounded to the type (half a step, as much as the gradients that are made of it are rounded by).
+// dZ of columns first .. first + width - 1, rounded to the type (half a step, as much as the gradients that are made of it are rounded by, so that those are off by 1.4 times as much as they would be; a second
+// part would take their products twice as long).
 template <class Tiles, class T>
 __global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_classes_slopes_kernel(CbmOperand<T> a, CbmOperand<T> b, int64_t width, int64_t chunks, int64_t first, int64_t c, const void* __restrict__ labels, int label_bits,
                                                                  const float* __restrict__ stats, const float* __restrict__ dlogp, const float* __restrict__ scale, T* __restrict__ dZ,
@@ -204,8 +252,9 @@ __global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_classes_slopes_kernel(
         });
 }
 
-// parts of a row's scores: of 32 columns at least where rows are few, of 64 else
-int64_t most_parts(int64_t n, int32_t c) { return std::max(n <= cbm_most_few_rows<float> ? ((int64_t)c + 31) / 32 : 0, ((int64_t)c + 127) / 128 * 2); }
+// parts of a row's scores: of 32 columns at least where rows are few or the product is small, of 64 else
+bool is_small(int64_t n, int32_t d, int32_t c, int32_t type) { return cbm_small_forward(n, d, c, cbm_small_groups(n, c), type); }
+int64_t most_parts(int64_t n, int32_t d, int32_t c, int32_t type) { return std::max(n <= cbm_most_few_rows<float> || is_small(n, d, c, type) ? ((int64_t)c + 31) / 32 : 0, ((int64_t)c + 127) / 128 * 2); }
 int64_t rounded16(int64_t bytes) { return (bytes + 15) / 16 * 16; }
 int64_t bytes_of(int32_t type) { return type == CBM_F32 ? 4 : 2; }
 
@@ -227,8 +276,15 @@ Copies copies_of(int64_t n, int32_t d, int32_t c, int32_t type) {
 
 struct Room {
     int64_t scale, sums, copies, parts, bytes;  // where they begin; dZ is first
+    bool small;
 };
 Room back_room(int64_t n, int32_t d, int32_t c, int32_t type) {
+    Room r{};
+    r.small = cbm_small_backward(n, d, c, d, cbm_small_groups(n, c) + cbm_small_groups(n, d) + cbm_small_groups(d, c), type);
+    if (r.small) {
+        r.bytes = n * cbm_whole(c, 4) * 4;
+        return r;
+    }
     const int64_t piece = piece_of(n, c, type), last = c % piece ? c % piece : piece, wide = cbm_whole(d, 8);
     int64_t parts = 0;
     for (int64_t w : {piece, last}) {
@@ -236,7 +292,6 @@ Room back_room(int64_t n, int32_t d, int32_t c, int32_t type) {
         if (dx > 1) parts = std::max(parts, dx * n * wide);
         if (dw > 1) parts = std::max(parts, dw * wide * cbm_whole(w, 8));
     }
-    Room r;
     r.scale = rounded16(n * piece * bytes_of(type));
     r.sums = r.scale + 16;
     r.copies = r.sums + (piece < c ? rounded16(4 * n * wide) : 0);
@@ -301,7 +356,7 @@ void with_tiles(int64_t n, int64_t d, int64_t c, const Operands<T>& o, int32_t t
 }  // namespace
 
 int64_t cbm_classes_workspace(int64_t n, int32_t d, int32_t c, int32_t type) {
-    return rounded16(n * most_parts(n, c) * (int64_t)sizeof(Sums)) + rounded16(4 * n) + copies_of(n, d, c, type).bytes;
+    return rounded16(n * most_parts(n, d, c, type) * (int64_t)sizeof(Sums)) + rounded16(4 * n) + copies_of(n, d, c, type).bytes;
 }
 
 cbm_status cbm_launch_classes(int64_t n, int32_t d, int32_t c, int32_t type, const void* X, int64_t ldx, const void* W, int64_t ldw, const void* labels, int label_bits, float* logp, float* stats,
@@ -310,7 +365,7 @@ cbm_status cbm_launch_classes(int64_t n, int32_t d, int32_t c, int32_t type, con
     if (n == 0) return CBM_OK;
     int64_t count = 0;  // parts of a row: of the waves along a tile's columns
     Sums* parts = (Sums*)workspace;
-    float* chosen = (float*)((char*)workspace + rounded16(n * most_parts(n, c) * (int64_t)sizeof(Sums)));
+    float* chosen = (float*)((char*)workspace + rounded16(n * most_parts(n, d, c, type) * (int64_t)sizeof(Sums)));
     cbm_with_type(type, [&](auto t) {
         using T = decltype(t);
         constexpr int V = 16 / (int)sizeof(T);
@@ -319,6 +374,11 @@ cbm_status cbm_launch_classes(int64_t n, int32_t d, int32_t c, int32_t type, con
             cbm_with_few_rows(n, [&](auto rows) {
                 cbm_classes_few_kernel<T, decltype(rows)::value><<<dim3((unsigned)((count + 7) / 8 * 8), (unsigned)((n + CBM_FEW_ROWS - 1) / CBM_FEW_ROWS)), 64 * FEW_WAVES, 0, stream>>>(n, d, c, (const T*)X, ldx, (const T*)W, ldw, logp ? labels : nullptr, label_bits, parts, chosen);
             });
+            return;
+        }
+        if (is_small(n, d, c, type)) {
+            count = ((int64_t)c + 31) / 32;
+            cbm_classes_small_kernel<T><<<dim3((unsigned)count, (unsigned)((n + 31) / 32)), 512, 0, stream>>>(n, d, c, (const T*)X, ldx, (const T*)W, ldw, logp ? labels : nullptr, label_bits, parts, chosen);
             return;
         }
         const Operands<T> o(n, d, c, type, X, ldx, W, ldw, (char*)chosen + rounded16(4 * n), stream);
@@ -338,6 +398,19 @@ cbm_status cbm_launch_classes_backward(int64_t n, int32_t d, int32_t c, int32_t 
                                        const float* stats, const float* dlogp, void* dX, int64_t lddx, void* dW, int64_t lddw, void* workspace, void* stream_) {
     hipStream_t stream = (hipStream_t)stream_;
     const Room room = back_room(n, d, c, type);
+    if (room.small) {
+        float* dZ = (float*)workspace;
+        const int64_t ld = cbm_whole(c, 4);
+        if (n > 0)
+            cbm_with_type(type, [&](auto t) {
+                using T = decltype(t);
+                cbm_classes_small_slopes_kernel<T><<<dim3((unsigned)((c + 31) / 32), (unsigned)((n + 31) / 32)), 512, 0, stream>>>(n, d, c, (const T*)X, ldx, (const T*)W, ldw, labels, label_bits, stats,
+                                                                                                                        dlogp, dZ, ld);
+            });
+        if (dX && n > 0) cbm_launch_small_along(type, n, d, c, dZ, nullptr, ld, W, ldw, nullptr, 0, dX, lddx, stream);
+        if (dW) cbm_launch_small_across(type, d, c, n, X, ldx, dZ, nullptr, ld, dW, lddw, nullptr, 0, stream);
+        return cbm_launched("linear log probabilities backward launch");
+    }
     const int64_t piece = piece_of(n, c, type);
     float *scale = (float*)((char*)workspace + room.scale), *sums = (float*)((char*)workspace + room.sums), *parts = (float*)((char*)workspace + room.parts);
     if (type == CBM_F32) scale = nullptr;

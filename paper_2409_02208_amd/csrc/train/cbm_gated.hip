@@ -5,6 +5,7 @@
 #include "cbm_few_rows.h"
 #include "cbm_internal.h"
 #include "cbm_products.h"
+#include "cbm_small.h"
 
 namespace {
 
@@ -59,6 +60,27 @@ __global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_gated_kernel(CbmOperan
     });
 }
 
+// A small product: 32 x 32 values of G and of U a workgroup, its waves sharing K (64 x 256 with 2 x 256 in fp32 21 -> 6 us).
+template <class T, int ACT>
+__global__ __launch_bounds__(512) void cbm_gated_small_kernel(int64_t n, int64_t k, int64_t m, const T* __restrict__ X, int64_t ldx, const T* __restrict__ Wg, int64_t ldwg, const T* __restrict__ Wu,
+                                                            int64_t ldwu, T* __restrict__ H, int64_t ldh, T* __restrict__ G, int64_t ldg, T* __restrict__ U, int64_t ldu) {
+    typedef CbmSmallTile<T, T, ALONG_K, ACROSS_K, 2> Tile;
+    __shared__ typename Tile::Room room;
+    const int64_t r0 = (int64_t)blockIdx.y * Tile::SIDE, c0 = (int64_t)blockIdx.x * Tile::SIDE, r = r0 + Tile::row(), c = c0 + Tile::column();
+    Tile t;
+    t.add(X, ldx, n, r0, {Wg, Wu}, {ldwg, ldwu}, m, c0, k);
+    t.share(room);
+    if (r >= n) return;
+    float g[2], u[2], h[2];
+    Tile::total(room, 0, g);
+    Tile::total(room, 1, u);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) h[j] = activated<T, ACT>(g[j]) * u[j];
+    cbm_put(H + r * ldh, c, m, h);
+    if (G) cbm_put(G + r * ldg, c, m, g);
+    if (U) cbm_put(U + r * ldu, c, m, u);
+}
+
 // A few rows: the weights are read once, in pieces of 64 bytes of a row, a workgroup for each 64 bytes of columns.
 constexpr int few_waves(int rows) { return rows >= 8 ? 8 : 16; }
 template <class T, int NR, int ACT>
@@ -79,10 +101,11 @@ __global__ __launch_bounds__(64 * few_waves(NR)) void cbm_gated_few_kernel(int64
     if (U) U[r * ldu + c] = (T)u;
 }
 
-// dG and dU side by side in `out`, from column 0 and column `at` on, rounded to the type (half a step each, as much as the gradients that are made of them are rounded by); zeros between.
-template <class T, int ACT>
+// dG and dU side by side in `out`, from column 0 and column `at` on, zeros between: in fp32 for small products, else rounded to the type (half a step each, as much as the gradients that are made of them are
+// rounded by, so that those are off by 1.4 times as much as they would be; a second part would take the products twice as long).
+template <class T, class S, int ACT>
 __global__ __launch_bounds__(256) void cbm_gated_slopes_kernel(int64_t n, int m, const T* __restrict__ dH, int64_t lddh, const T* __restrict__ G, int64_t ldg, const T* __restrict__ U,
-                                                            int64_t ldu, T* __restrict__ out, int64_t at) {
+                                                            int64_t ldu, S* __restrict__ out, int64_t at) {
     constexpr int V = 16 / (int)sizeof(T);
     const int64_t pieces = at / V;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n * pieces; i += (int64_t)gridDim.x * 256) {
@@ -148,6 +171,13 @@ cbm_status cbm_launch_gated(int64_t n, int32_t k, int32_t m, int32_t type, int32
             });
             return;
         }
+        if (cbm_small_forward(n, k, 2 * (int64_t)m, cbm_small_groups(n, m), type)) {
+            with_activation(act, [&](auto which) {
+                cbm_gated_small_kernel<T, decltype(which)::value><<<dim3((unsigned)((m + 31) / 32), (unsigned)((n + 31) / 32)), 512, 0, (hipStream_t)stream>>>(
+                    n, k, m, (const T*)X, ldx, (const T*)Wg, ldwg, (const T*)Wu, ldwu, (T*)H, ldh, (T*)G, ldg, (T*)U, ldu);
+            });
+            return;
+        }
         auto run = [&](auto* tiles_type, const CbmOperand<T>& a, const CbmOperand<T>& b) {
             typedef std::remove_pointer_t<decltype(tiles_type)> Tiles;
             const int64_t tiles = (n + Tiles::ROWS - 1) / Tiles::ROWS * (((int64_t)m + Tiles::COLUMNS / 2 - 1) / (Tiles::COLUMNS / 2));
@@ -191,12 +221,17 @@ namespace {
 // dG and dU side by side, copies of X and of the weights (rows of whole units), shares of K.
 struct BackRoom {
     int64_t at, x, weights, parts, bytes;  // column of dU; where they begin
-    bool copies;
+    bool copies, small;
 };
 BackRoom back_room(int64_t n, int32_t k, int32_t m, int32_t type) {
     BackRoom r{};
     const int64_t bytes = type == CBM_F32 ? 4 : 2, wide = cbm_whole(k, 8);
     r.at = cbm_whole(m, 64);
+    r.small = cbm_small_backward(n, k, 2 * (int64_t)m, 0, cbm_small_groups(n, k) + 2 * cbm_small_groups(k, m), type);
+    if (r.small) {
+        r.bytes = n * 2 * r.at * 4;
+        return r;
+    }
     r.copies = cbm_may_pack(n, k, 2 * (int64_t)m, type);
     r.x = cbm_whole(n * 2 * r.at * bytes, 16);
     r.weights = r.x + (r.copies ? 2 * n * wide : 0);
@@ -225,10 +260,20 @@ cbm_status cbm_launch_gated_backward(int64_t n, int32_t k, int32_t m, int32_t ty
             using T = decltype(t);
             const int64_t blocks = (n * (at * (int64_t)sizeof(T) / 16) + 255) / 256;
             with_activation(act, [&](auto which) {
-                cbm_gated_slopes_kernel<T, decltype(which)::value><<<(unsigned)std::min<int64_t>(blocks, 1 << 22), 256, 0, (hipStream_t)stream>>>(n, m, (const T*)dH, lddh, (const T*)G, ldg,
-                                                                                                                                      (const T*)U, ldu, (T*)workspace, at);
+                auto slopes = [&](auto* out) {
+                    cbm_gated_slopes_kernel<T, std::remove_pointer_t<decltype(out)>, decltype(which)::value><<<(unsigned)std::min<int64_t>(blocks, 1 << 22), 256, 0, (hipStream_t)stream>>>(
+                        n, m, (const T*)dH, lddh, (const T*)G, ldg, (const T*)U, ldu, out, at);
+                };
+                if (room.small) slopes((float*)workspace);
+                else slopes((T*)workspace);
             });
         });
+    if (room.small) {
+        const float* slopes = (const float*)workspace;
+        if (dX && n > 0) cbm_launch_small_along(type, n, k, m, slopes, slopes + at, 2 * at, Wg, ldwg, Wu, ldwu, dX, lddx, stream);
+        if (dWg || dWu) cbm_launch_small_across(type, k, m, n, X, ldx, slopes, slopes + at, 2 * at, dWg, lddwg, dWu, lddwu, stream);
+        return cbm_launched("gated layer backward launch");
+    }
     CbmProduct p{};
     p.type = type;
     p.A = workspace;

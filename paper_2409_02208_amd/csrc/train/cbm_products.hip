@@ -5,6 +5,7 @@
 #include "cbm_aligned.h"
 #include "cbm_internal.h"
 #include "cbm_products.h"
+#include "cbm_small.h"
 
 namespace {
 
@@ -86,6 +87,35 @@ __global__ __launch_bounds__(256) void cbm_product_join_kernel(int64_t M, int64_
         if (slice == 0 && i < count) finish<T>(o, N, r, c, v);
         if constexpr (SLICES > 1) __syncthreads();
     }
+}
+
+template <class T>
+__global__ __launch_bounds__(512) void cbm_small_along_kernel(int64_t M, int64_t N, int64_t K, const float* __restrict__ S0, const float* __restrict__ S1, int64_t lds, const T* __restrict__ B0, int64_t ldb0,
+                                                            const T* __restrict__ B1, int64_t ldb1, T* __restrict__ C, int64_t ldc) {
+    typedef CbmSmallTile<float, T, ALONG_K, ALONG_K, 1> Tile;
+    __shared__ typename Tile::Room room;
+    const int64_t r0 = (int64_t)blockIdx.y * Tile::SIDE, c0 = (int64_t)blockIdx.x * Tile::SIDE, r = r0 + Tile::row();
+    Tile t;
+    t.add(S0, lds, M, r0, {B0}, {ldb0}, N, c0, K);
+    if (S1) t.add(S1, lds, M, r0, {B1}, {ldb1}, N, c0, K);
+    t.share(room);
+    float v[2];
+    Tile::total(room, 0, v);
+    if (r < M) cbm_put(C + r * ldc, c0 + Tile::column(), N, v);
+}
+template <class T>
+__global__ __launch_bounds__(512) void cbm_small_across_kernel(int64_t M, int64_t N, int64_t K, const T* __restrict__ A, int64_t lda, const float* __restrict__ S0, const float* __restrict__ S1, int64_t lds,
+                                                             T* __restrict__ C0, int64_t ldc0, T* __restrict__ C1, int64_t ldc1) {
+    typedef CbmSmallTile<T, float, ACROSS_K, ACROSS_K, 1> Tile;
+    __shared__ typename Tile::Room room;
+    const bool second = !C0 || blockIdx.z;
+    const int64_t r0 = (int64_t)blockIdx.y * Tile::SIDE, c0 = (int64_t)blockIdx.x * Tile::SIDE, r = r0 + Tile::row();
+    Tile t;
+    t.add(A, lda, M, r0, {second ? S1 : S0}, {lds}, N, c0, K);
+    t.share(room);
+    float v[2];
+    Tile::total(room, 0, v);
+    if (r < M) cbm_put(second ? C1 + r * ldc1 : C0 + r * ldc0, c0 + Tile::column(), N, v);
 }
 
 // 64 x 64 values a workgroup, through LDS.
@@ -219,6 +249,23 @@ int cbm_product_tile(int64_t M, int64_t N, int64_t K, int32_t type) {
 
 void cbm_launch_tiles(const CbmProduct& p, void* stream) {
     cbm_with_type(p.type, [&](auto t) { launch<decltype(t)>(p, (hipStream_t)stream); });
+}
+
+void cbm_launch_small_along(int32_t type, int64_t M, int64_t N, int64_t K, const float* S0, const float* S1, int64_t lds, const void* B0, int64_t ldb0, const void* B1, int64_t ldb1, void* C, int64_t ldc,
+                            void* stream) {
+    cbm_with_type(type, [&](auto t) {
+        using T = decltype(t);
+        cbm_small_along_kernel<T><<<dim3((unsigned)((N + 31) / 32), (unsigned)((M + 31) / 32)), 512, 0, (hipStream_t)stream>>>(M, N, K, S0, S1, lds, (const T*)B0, ldb0, (const T*)B1, ldb1, (T*)C, ldc);
+    });
+}
+
+void cbm_launch_small_across(int32_t type, int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, const float* S0, const float* S1, int64_t lds, void* C0, int64_t ldc0, void* C1, int64_t ldc1,
+                             void* stream) {
+    cbm_with_type(type, [&](auto t) {
+        using T = decltype(t);
+        cbm_small_across_kernel<T><<<dim3((unsigned)((N + 31) / 32), (unsigned)((M + 31) / 32), C0 && C1 ? 2 : 1), 512, 0, (hipStream_t)stream>>>(M, N, K, (const T*)A, lda, S0, S1, lds, (T*)C0, ldc0,
+                                                                                                                                       (T*)C1, ldc1);
+    });
 }
 
 cbm_status cbm_launched(const char* what) {
