@@ -2,6 +2,7 @@
 // time is the host's: with tensors read in Python and arguments converted by ctypes, cbm_layer_norm of 1024 x 64 took
 // 7.1 us a call, here it takes 3.8 to 4.1, as long as filling a tensor of one float.
 #include <torch/csrc/autograd/python_variable.h>
+#include <c10/core/impl/DeviceGuardImplInterface.h>
 #include <torch/version.h>
 
 #include <algorithm>
@@ -243,8 +244,20 @@ float number(PyObject* o) {
     return (float)v;
 }
 
+// The operators that are made of products launch on the current device, whose stream and rates they assume.
+template <int ARGUMENTS, class F>
+PyObject* call_here(PyObject* const* args, Py_ssize_t count, F&& f) {
+    return call<ARGUMENTS>(args, count, [&](PyObject* const* a, void* stream) {
+        auto enqueue = f(a, stream);
+        const c10::Device here = c10::impl::getDeviceGuardImpl(c10::DeviceType::CUDA)->getDevice();
+        for (int i = 0; i < ARGUMENTS; ++i)
+            if (THPVariable_Check(a[i]) && THPVariable_Unpack(a[i]).device() != here) throw Refused{"all tensors must be on the current device"};
+        return enqueue;
+    });
+}
+
 PyObject* gated_linear(PyObject*, PyObject* const* args, Py_ssize_t count) {  // X, Wg, Wu, H, G, U, activation, workspace, stream
-    return call<9>(args, count, [](PyObject* const* a, void* stream) {
+    return call_here<9>(args, count, [](PyObject* const* a, void* stream) {
         const Matrix x = matrix(a[0], "X"), g = matrix(a[1], "Wg"), u = matrix(a[2], "Wu"), h = matrix(a[3], "H");
         alike(g, u, "Wg and Wu must have the same shape and type");
         if (x.cols != g.rows || x.type != g.type || h.type != x.type || h.rows != x.rows || h.cols != g.cols) throw Refused{"X, Wg and H must be n x k, k x m and n x m, of one type"};
@@ -258,7 +271,7 @@ PyObject* gated_linear(PyObject*, PyObject* const* args, Py_ssize_t count) {  //
 }
 
 PyObject* gated_linear_backward(PyObject*, PyObject* const* args, Py_ssize_t count) {  // dH, X, Wg, Wu, G, U, dX, dWg, dWu, activation, workspace, stream
-    return call<12>(args, count, [](PyObject* const* a, void* stream) {
+    return call_here<12>(args, count, [](PyObject* const* a, void* stream) {
         const Matrix d = matrix(a[0], "dH"), x = matrix(a[1], "X"), wg = matrix(a[2], "Wg"), wu = matrix(a[3], "Wu"), g = matrix(a[4], "G"), u = matrix(a[5], "U");
         alike(wg, wu, "Wg and Wu must have the same shape and type");
         alike(d, g, "dH and G must have the same shape and type");
@@ -276,7 +289,7 @@ PyObject* gated_linear_backward(PyObject*, PyObject* const* args, Py_ssize_t cou
 }
 
 PyObject* linear_log_probs(PyObject*, PyObject* const* args, Py_ssize_t count) {  // X, W, labels, logp, stats, workspace, stream
-    return call<7>(args, count, [](PyObject* const* a, void* stream) {
+    return call_here<7>(args, count, [](PyObject* const* a, void* stream) {
         const Matrix x = matrix(a[0], "X"), w = matrix(a[1], "W");
         if (x.cols != w.rows || x.type != w.type) throw Refused{"X and W must be n x d and d x c, of one type"};
         const Labels labels(a[2], x.rows);
@@ -289,7 +302,7 @@ PyObject* linear_log_probs(PyObject*, PyObject* const* args, Py_ssize_t count) {
 }
 
 PyObject* linear_log_probs_backward(PyObject*, PyObject* const* args, Py_ssize_t count) {  // X, W, labels, stats, dlogp, dX, dW, workspace, stream
-    return call<9>(args, count, [](PyObject* const* a, void* stream) {
+    return call_here<9>(args, count, [](PyObject* const* a, void* stream) {
         const Matrix x = matrix(a[0], "X"), w = matrix(a[1], "W");
         if (x.cols != w.rows || x.type != w.type) throw Refused{"X and W must be n x d and d x c, of one type"};
         const Labels labels(a[2], x.rows);
@@ -304,7 +317,7 @@ PyObject* linear_log_probs_backward(PyObject*, PyObject* const* args, Py_ssize_t
 }
 
 PyObject* orthogonalise(PyObject*, PyObject* const* args, Py_ssize_t count) {  // X, Y, steps, a, b, c, eps, scale, workspace, stream
-    return call<10>(args, count, [](PyObject* const* a, void* stream) {
+    return call_here<10>(args, count, [](PyObject* const* a, void* stream) {
         const Matrix x = matrix(a[0], "X"), y = matrix(a[1], "Y");
         alike(x, y, "X and Y must have the same shape and type");
         const int32_t steps = whole(a[2]);

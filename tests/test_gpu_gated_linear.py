@@ -119,6 +119,20 @@ def test_backward(env, name, n, k, m):  # noqa: F811
         _check_backward(*_backward(torch, cbm, n, k, m, name, act, pad, offset, outputs=on), name, act, on)
 
 
+MANY_ROWS = [(40001, 31, 8), (20003, 65, 47), (9001, 17, 300), (5001, 63, 130), (33, 40, 8200)]  # tiles through LDS, where the rest above is small
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("n,k,m", MANY_ROWS)
+def test_many_rows_or_columns(env, name, n, k, m):  # noqa: F811
+    torch, cbm = env
+    for i, (pad, offset) in enumerate(((0, 0), (3, 1), (8, 8))):
+        act = ("silu", "gelu", "relu")[(i + n + k) % 3]
+        _check_forward(*_forward(torch, cbm, n, k, m, name, act, pad, offset, keep=i != 1), name, act, keep=i != 1)
+        on = ((True, True, True), (True, False, True), (False, True, False))[i]
+        _check_backward(*_backward(torch, cbm, n, k, m, name, act, pad, offset, outputs=on), name, act, on)
+
+
 def test_small_gradients_in_fp16_are_not_lost(env):  # noqa: F811
     """Gradients below fp16's smallest normal value, 2^-14: rounded to multiples of 2^-24, and counted."""
     torch, cbm = env

@@ -107,6 +107,18 @@ def test_backward(env, name, n, d, c):  # noqa: F811
 
 
 @pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("n,d,c", [(40001, 31, 8), (20003, 65, 47), (9001, 17, 300), (5001, 63, 130), (65, 40, 16400)])
+def test_many_rows_or_classes(env, name, n, d, c):  # noqa: F811
+    """Tiles through LDS, where most sizes above are small."""
+    torch, cbm = env
+    for i, (pad, offset, bits) in enumerate(((0, 0, 64), (5, 1, 32), (8, 8, 64))):
+        X, W, L = _inputs(torch, n, d, c, name, pad, offset, bits)
+        _check_forward(X, W, L, *_forward(torch, cbm, X, W, L))
+        on = ((True, True), (True, False), (False, True))[i]
+        _check_backward(X, W, L, *_backward(torch, cbm, X, W, L, pad, offset, outputs=on, equal=i == 2), name, on)
+
+
+@pytest.mark.parametrize("name", TYPES)
 def test_pieces_of_the_classes(env, name):  # noqa: F811
     """More rows than 512 MiB hold scores for: several pieces, the last one short."""
     torch, cbm = env
