@@ -415,7 +415,7 @@ cbm_status cbm_log_probs_backward(int64_t n, int32_t c, int32_t type, const void
  *   workspace    cbm_gated_linear_backward_workspace_bytes(n, k, m, type) bytes.
  *
  * Products of 16-bit types are exact, those of fp32 are made of three bf16 parts of each value (left out is at most 2^-24 of a term; parts below 2^-126 are taken for zero); sums
- * are fp32.  (Small products of fp32: in fp32 throughout.)  In fp32, a value that is not finite, or from 2^127 on, leaves no finite sum that it is part of.
+ * are fp32.  (Small products of fp32: in fp32 throughout.)  In fp32, a value that is not finite leaves no finite sum that it is part of, one from 2^127 on may leave none.
  * Workspaces hold copies of operands and shares of sums, or slopes in fp32, whatever the sizes ask for: a smaller call may need more than a larger one.
  */
 typedef enum { CBM_SILU = 0, CBM_GELU = 1, CBM_RELU = 2 } cbm_activation;
@@ -459,7 +459,8 @@ size_t cbm_linear_log_probs_backward_workspace_bytes(int64_t n, int32_t d, int32
  *   eps            >= 0 and finite; a matrix of zeros stays one with eps > 0, and is NaN with eps = 0.
  *   Y              may be X itself with ldy = ldx.
  *   workspace      cbm_orthogonalise_workspace_bytes(m, n, type) bytes.
- * m and n up to 65,536.  Everything between X and Y is held in 32 bits.  A value that is not finite makes NaN of all of Y.
+ * m and n up to 65,536.  Between X and Y values are held in two parts of 16 bits each, 22 bits together, at powers of two that follow from the coefficients; sums are fp32.  Coefficients are refused
+ * (CBM_ERR_UNSUPPORTED) where, on what the steps before may make of [0, 1], |a + b s^2 + c s^4| passes 16 |a| or 2^100, or s passes 2^24.  A value that is not finite makes NaN of all of Y.
  */
 cbm_status cbm_orthogonalise(int32_t m, int32_t n, int32_t type, const void* X, int64_t ldx, int32_t steps, const float* coefficients, float eps, float scale,
                              void* Y, int64_t ldy, void* workspace, size_t workspace_bytes, void* hip_stream);

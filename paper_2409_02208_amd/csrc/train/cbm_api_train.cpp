@@ -186,7 +186,7 @@ cbm_status cbm_log_probs_backward(int64_t n, int32_t c, int32_t type, const void
 }
 
 size_t cbm_gated_linear_workspace_bytes(int64_t n, int32_t k, int32_t m, int32_t type) {
-    return n <= 0 || k <= 0 || m <= 0 || k > MOST_COLUMNS || m > MOST_COLUMNS || !element_bytes(type) ? 0 : (size_t)cbm_gated_workspace(n, k, m, type);
+    return n <= 0 || k <= 0 || m <= 0 || n > MOST_ROWS || k > MOST_COLUMNS || m > MOST_COLUMNS || !element_bytes(type) ? 0 : (size_t)cbm_gated_workspace(n, k, m, type);
 }
 
 cbm_status cbm_gated_linear(int64_t n, int32_t k, int32_t m, int32_t type, int32_t activation, const void* X, int64_t ldx, const void* Wg, int64_t ldwg, const void* Wu, int64_t ldwu, void* H,

@@ -148,49 +148,50 @@ __global__ __launch_bounds__(512) void cbm_classes_small_slopes_kernel(int64_t n
 __global__ __launch_bounds__(256) void cbm_classes_join_kernel(int64_t n, int64_t c, int64_t count, const void* __restrict__ labels, int label_bits, const Sums* __restrict__ parts,
                                                              const float* __restrict__ chosen, float* __restrict__ logp, float* __restrict__ stats) {
     const int lane = threadIdx.x & 63;
-    const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (r >= n) return;
-    Sums all{-INFINITY, 0.0f};
-    constexpr int AHEAD = 8;  // (one row of 32,000 columns has 500 parts: their loads under way together, and one maximum for eight: 19.5 -> 17.9 us)
-    for (int64_t i = lane; i < count; i += 64 * AHEAD) {
-        Sums some[AHEAD];
+    for (int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); r < n; r += (int64_t)gridDim.x * 4) {
+        Sums all{-INFINITY, 0.0f};
+        constexpr int AHEAD = 8;  // (one row of 32,000 columns has 500 parts: their loads under way together, and one maximum for eight: 19.5 -> 17.9 us)
+        for (int64_t i = lane; i < count; i += 64 * AHEAD) {
+            Sums some[AHEAD];
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) some[k] = i + 64 * k < count ? parts[r * count + i + 64 * k] : Sums{-INFINITY, 0.0f};
-        float m = all.m;
+            for (int k = 0; k < AHEAD; ++k) some[k] = i + 64 * k < count ? parts[r * count + i + 64 * k] : Sums{-INFINITY, 0.0f};
+            float m = all.m;
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) m = fmaxf(m, some[k].m);
-        const float away = m == -INFINITY ? 0.0f : m;
-        float s = all.s * __builtin_amdgcn_exp2f((all.m - away) * LOG2E);
+            for (int k = 0; k < AHEAD; ++k) m = fmaxf(m, some[k].m);
+            const float away = m == -INFINITY ? 0.0f : m;
+            float s = all.s * __builtin_amdgcn_exp2f((all.m - away) * LOG2E);
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) s += some[k].s * __builtin_amdgcn_exp2f((some[k].m - away) * LOG2E);
-        all = {m, s};
-    }
-    const float m = lanes_all<64>(all.m, [](float a, float b) { return fmaxf(a, b); }), away = m == -INFINITY ? 0.0f : m;
-    const float s = lanes_sum<64>(all.s * __builtin_amdgcn_exp2f((all.m - away) * LOG2E));
-    if (lane) return;
-    const bool bad = !(s < INFINITY);
-    const float largest = bad ? NAN : m, l = bad ? NAN : logf(s);
-    if (stats) {
-        stats[2 * r] = largest;
-        stats[2 * r + 1] = l;
-    }
-    if (logp) {
-        const int64_t label = label_of(labels, label_bits, r);
-        logp[r] = label < 0 || label >= c ? 0.0f : bad ? NAN : m == -INFINITY ? m : (chosen[r] - m) - l;
+            for (int k = 0; k < AHEAD; ++k) s += some[k].s * __builtin_amdgcn_exp2f((some[k].m - away) * LOG2E);
+            all = {m, s};
+        }
+        const float m = lanes_all<64>(all.m, [](float a, float b) { return fmaxf(a, b); }), away = m == -INFINITY ? 0.0f : m;
+        const float s = lanes_sum<64>(all.s * __builtin_amdgcn_exp2f((all.m - away) * LOG2E));
+        if (lane) continue;
+        const bool bad = !(s < INFINITY);
+        const float largest = bad ? NAN : m, l = bad ? NAN : logf(s);
+        if (stats) {
+            stats[2 * r] = largest;
+            stats[2 * r + 1] = l;
+        }
+        if (logp) {
+            const int64_t label = label_of(labels, label_bits, r);
+            logp[r] = label < 0 || label >= c ? 0.0f : bad ? NAN : m == -INFINITY ? m : (chosen[r] - m) - l;
+        }
     }
 }
 
 // Types of 16 bits: dZ is kept at 2^15 over the largest finite |dlogp| of its size; what is made of it is multiplied by the factor, scale[0], and dlogp by scale[1].  In fp16 the gradients of a batch's
 // scores would be small beside 2^-14: here 1 - p fits and a p down to 2^-29 keeps all its bits.  In both types the rows of a mean, which all have the same dlogp, have their labels' own 1 - p just below a
 // power of two, where half a step is 2^-9 (bf16) of it at most and p itself where that is less; at 1 / n it would be up to 2^-8, the same for every row, and nothing evens it out.
-__global__ __launch_bounds__(1024) void cbm_classes_scale_kernel(int64_t n, const float* __restrict__ dlogp, float* __restrict__ scale) {
+constexpr int SCALE_GROUPS = 256;
+__global__ __launch_bounds__(1024) void cbm_classes_scale_kernel(int64_t n, const float* __restrict__ from, float* __restrict__ scale, float* __restrict__ parts) {
     __shared__ float room[16];
     constexpr int AHEAD = 8;
     float most = 0x1p-100f;  // (neither factor overflows)
-    for (int64_t i = threadIdx.x; i < n; i += 1024 * AHEAD) {
+    for (int64_t i = (int64_t)blockIdx.x * 1024 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 1024 * AHEAD) {
         float v[AHEAD];
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) v[k] = fabsf(dlogp[min(i + 1024 * k, n - 1)]);
+        for (int k = 0; k < AHEAD; ++k) v[k] = fabsf(from[min(i + (int64_t)gridDim.x * 1024 * k, n - 1)]);
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) most = v[k] < INFINITY ? fmaxf(most, v[k]) : most;
     }
@@ -199,6 +200,10 @@ __global__ __launch_bounds__(1024) void cbm_classes_scale_kernel(int64_t n, cons
     __syncthreads();
     if (threadIdx.x) return;
     for (int i = 1; i < 16; ++i) most = fmaxf(most, room[i]);
+    if (parts) {
+        parts[blockIdx.x] = most;
+        return;
+    }
     scale[0] = most * 0x1p-15f;
     scale[1] = 0x1p15f / most;
 }
@@ -293,7 +298,7 @@ Room back_room(int64_t n, int32_t d, int32_t c, int32_t type) {
         if (dw > 1) parts = std::max(parts, dw * wide * cbm_whole(w, 8));
     }
     r.scale = rounded16(n * piece * bytes_of(type));
-    r.sums = r.scale + 16;
+    r.sums = r.scale + 16 + 4 * SCALE_GROUPS;
     r.copies = r.sums + (piece < c ? rounded16(4 * n * wide) : 0);
     r.parts = r.copies + copies_of(n, d, c, type).bytes;
     r.bytes = r.parts + 4 * parts;
@@ -388,7 +393,7 @@ cbm_status cbm_launch_classes(int64_t n, int32_t d, int32_t c, int32_t type, con
             cbm_classes_kernel<Tiles, T><<<grid, 256, 0, stream>>>(o.a, o.b, chunks, logp ? labels : nullptr, label_bits, parts, chosen);
         });
     });
-    cbm_classes_join_kernel<<<(unsigned)((n + 3) / 4), 256, 0, stream>>>(n, c, count, labels, label_bits, parts, chosen, logp, stats);
+    cbm_classes_join_kernel<<<(unsigned)std::min<int64_t>((n + 3) / 4, 1 << 20), 256, 0, stream>>>(n, c, count, labels, label_bits, parts, chosen, logp, stats);
     return cbm_launched("linear log probabilities launch");
 }
 
@@ -414,7 +419,12 @@ cbm_status cbm_launch_classes_backward(int64_t n, int32_t d, int32_t c, int32_t 
     const int64_t piece = piece_of(n, c, type);
     float *scale = (float*)((char*)workspace + room.scale), *sums = (float*)((char*)workspace + room.sums), *parts = (float*)((char*)workspace + room.parts);
     if (type == CBM_F32) scale = nullptr;
-    if (scale && n > 0) cbm_classes_scale_kernel<<<1, 1024, 0, stream>>>(n, dlogp, scale);
+    if (scale && n > 0) {
+        float* most = scale + 4;
+        const bool many = n > 1 << 16;  // (of a million rows one workgroup takes 80 us)
+        if (many) cbm_classes_scale_kernel<<<SCALE_GROUPS, 1024, 0, stream>>>(n, dlogp, nullptr, most);
+        cbm_classes_scale_kernel<<<1, 1024, 0, stream>>>(many ? SCALE_GROUPS : n, many ? most : dlogp, scale, nullptr);
+    }
     cbm_with_type(type, [&](auto t) {
         using T = decltype(t);
         const Operands<T> o(n, d, c, type, X, ldx, W, ldw, (char*)workspace + room.copies, n > 0 ? stream : nullptr);

@@ -2,7 +2,7 @@
 //
 // Z (s x l, the shorter side first) is held as two fp16 parts that add up to 22 bits of each value, at a power of two times its size that fits the largest it can have: Z's singular values are at most one at first, and
 // each step's largest follows from the coefficients, so the host knows a bound of every entry.  Three products of parts (hh, hl, lh) then stand for one in 32 bits: what is left out is 2^-22 of a term, and
-// sums are fp32.  (update_large's error is that of its 16 bits; in fp32, 500 x 1333, 1.1e-6 with three bf16 parts and six products.)  Nothing below 2^-25 of 2^-14 of the largest bound is lost.
+// sums are fp32.  (500 x 1333 in fp32: error 1.4e-6; with three bf16 parts and six products 1.1e-6, and twice as long.)  Nothing below 2^-25 of 2^-14 of the largest bound is lost.
 //
 // All operands lie along k: Z and its transpose are both kept (Z Z^T reads rows of the one, P Z rows of P and of the other), A and P = a I + b A + c A^2 are symmetric: their tiles on one side of the diagonal are
 // made, and written to both.  A row in memory is blocks of 32 values: their high parts, then their low parts, 128 bytes together, so that a chunk of 64 halves is 32 k of both parts.
@@ -235,7 +235,7 @@ struct HalvesTiles : CbmTileSums<B, B, 2, 2> {
 };
 
 // The same for few tiles, of 64 x 64: each of the four waves has all of the tile for a quarter of K, with units of its own in LDS, so that no wave waits for another until they add up.  (500 x 1333's Gram matrix, 36
-// tiles of 42 chunks: waves with a quarter of the tile 21 us, a step of two products between barriers; this 7.)
+// tiles of 42 chunks: waves with a quarter of the tile 21 us, a step of two products between barriers; this 12.)
 struct HalvesShares {
     typedef CbmAlignedSide<_Float16, 256, ALONG_K, SINGLE> Side;  // (a wave's loads are 64 rows)
     static constexpr int ROWS = 64, GROUPS = 1, LOADS = Side::LOADS, SLOT = 64 * 8, OUT_STRIDE = 17, UNITS = 4 * 4 * SLOT;
@@ -588,6 +588,18 @@ struct Powers {
     }
 };
 
+// Whether the bounds stay where the powers of two reach, 2^24 for Z and 2^100 for P, and near what they bound: singular values near zero, most of a matrix's, have |a| in P, and the lower parts of its values
+// there would go below fp16's smallest if the bound were far above that (a, b, c = 2, -3, 50: 0.4 % off after two steps of 150 x 200).
+bool stays(const float* abc, int steps) {
+    double top = 1.0 + 0x1p-10;
+    for (int i = 0; i < steps; ++i) {
+        const double most = largest(abc, top, false);
+        if (!(top <= 0x1p24) || !(most <= 0x1p100) || !(most <= 16.0 * std::fabs((double)abc[0]))) return false;
+        top = largest(abc, top, true) * (1.0 + 0x1p-10);
+    }
+    return true;
+}
+
 struct Room {
     int64_t squares, z[2], zt[2], gram, poly, bytes;
 };
@@ -640,6 +652,7 @@ int64_t cbm_orthogonal_workspace(int32_t m, int32_t n, int32_t) { return room_of
 cbm_status cbm_launch_orthogonal(int32_t m, int32_t n, int32_t type, const void* X, int64_t ldx, int32_t steps, const float* abc, float eps, float scale, void* Y, int64_t ldy, void* workspace,
                                  void* stream_) {
     hipStream_t stream = (hipStream_t)stream_;
+    if (!stays(abc, steps)) return CBM_ERR_UNSUPPORTED;
     const bool tall = m > n;
     const int64_t s = std::min(m, n), l = std::max(m, n);
     const Room room = room_of(s, l);

@@ -162,3 +162,25 @@ def test_refusals(env):  # noqa: F811
     assert [call(m=65537), call(n=65537, ld=70000)] == [5, 5]
     torch.cuda.synchronize()
     assert bool((Y == 1).all())
+
+
+def test_coefficients_that_diverge_are_refused(env):  # noqa: F811
+    torch, cbm = env
+    for m, n in ((8, 8), (200, 150)):
+        X, Y = torch.ones((m, n), device="cuda"), torch.full((m, n), 3.0, device="cuda")
+        ws = torch.empty(cbm.cbm_orthogonalise_workspace_bytes(m, n, torch.float32), dtype=torch.uint8, device="cuda")
+        for abc, steps in (((100.0, 0.0, 0.0), 6), ((1e20, 0.0, 0.0), 2), ((0.0, 0.0, 1e31), 1), ((3.0, 3.0, 3.0), 100), ((2.0, -3.0, 50.0), 2), ((0.0, 1.0, 0.0), 1)):
+            with pytest.raises(cbm.CbmError) as e:
+                cbm.cbm_orthogonalise(X, Y, steps=steps, coefficients=abc, workspace=ws)
+            assert e.value.status == 5
+        assert bool((Y == 3).all())
+        cbm.cbm_orthogonalise(X, Y, steps=100, workspace=ws)  # (the usual ones stay)
+        assert bool(Y.isfinite().all())
+
+
+@pytest.mark.parametrize("m,n", [(30, 20), (150, 200)])
+def test_large_and_small_coefficients(env, m, n):  # noqa: F811
+    torch, cbm = env
+    x = np.random.default_rng(8).standard_normal((m, n))
+    for abc, steps in (((10.0, 0.0, 0.0), 6), ((0.01, 0.0, 0.0), 6), ((1.5, -0.5, 0.0), 12), ((1e25, 0.0, 0.0), 1)):
+        _check(torch, cbm, x, "f32", steps=steps, coefficients=abc)
