@@ -17,21 +17,32 @@ namespace {
 
 constexpr int PARTS = 256;  // workgroups that share the sum of squares
 
-// Squares in 64 bits: no value of fp32 overflows or vanishes there.
+// Squares in 64 bits: no value of fp32 overflows or vanishes there.  Four pieces of 16 bytes a thread under way (4096 x 4096 in bf16 one value at a time 105 us).
 template <class T>
 __global__ __launch_bounds__(256) void cbm_orthogonal_norm_kernel(int64_t m, int64_t n, const T* __restrict__ X, int64_t ldx, double* __restrict__ parts) {
+    constexpr int V = 16 / (int)sizeof(T), AHEAD = 4;
     __shared__ double room[4];
     double s = 0.0;
-    const uint32_t wide = (uint32_t)((n + 1023) / 1024);  // pieces of a row, of four values a thread
-    for (uint32_t i = blockIdx.x; i < (uint32_t)m * wide; i += gridDim.x) {
-        const uint32_t r = i / wide;
-        const T* row = X + (int64_t)r * ldx;
-        const int64_t c = (int64_t)(i - r * wide) * 1024 + threadIdx.x;
-        float x[4];
+    const uint32_t wide = (uint32_t)((n + 256 * V - 1) / (256 * V)), count = (uint32_t)m * wide;  // pieces of a row, of V values a thread
+    for (uint32_t i = blockIdx.x; i < count; i += AHEAD * gridDim.x) {
+        float x[AHEAD][V];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = c + 256 * j < n ? (float)row[c + 256 * j] : 0.0f;
+        for (int k = 0; k < AHEAD; ++k) {
+            const uint32_t at = min(i + k * gridDim.x, count - 1), r = at / wide;
+            const T* row = X + (int64_t)r * ldx;
+            const int64_t c = ((int64_t)(at - r * wide) * 256 + threadIdx.x) * V;
+            const bool any = i + k * gridDim.x < count;
+            if (any && c + V <= n) {
+                load_piece<V>(x[k], row + c);
+            } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s += (double)x[j] * (double)x[j];
+                for (int j = 0; j < V; ++j) x[k][j] = any && c + j < n ? (float)row[c + j] : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j) s += (double)x[k][j] * (double)x[k][j];
     }
 #pragma unroll
     for (int step = 1; step < 64; step *= 2) s += __shfl_xor(s, step);
@@ -234,19 +245,20 @@ struct HalvesTiles : CbmTileSums<B, B, 2, 2> {
     }
 };
 
-// The same for few tiles, of 64 x 64: each of the four waves has all of the tile for a quarter of K, with units of its own in LDS, so that no wave waits for another until they add up.  (500 x 1333's Gram matrix, 36
-// tiles of 42 chunks: waves with a quarter of the tile 21 us, a step of two products between barriers; this 12.)
+// The same for few tiles, of 64 x 64 or of 32 x 32: each wave has all of the tile for its share of K, with units of its own in LDS, so that no wave waits for another until they add up.  (500 x 1333's Gram
+// matrix: 36 tiles of 64 x 64 whose four waves have a quarter of the tile 21 us, of K 12.9; 136 of 32 x 32 whose eight waves share K 8.0.  Its steps, 168 or 672 tiles: 10.0 and 15.)
+template <int B, int WAVES>
 struct HalvesShares {
-    typedef CbmAlignedSide<_Float16, 256, ALONG_K, SINGLE> Side;  // (a wave's loads are 64 rows)
-    static constexpr int ROWS = 64, GROUPS = 1, LOADS = Side::LOADS, SLOT = 64 * 8, OUT_STRIDE = 17, UNITS = 4 * 4 * SLOT;
-    static_assert(LOADS == 8 && UNITS >= 4 * 64 * OUT_STRIDE, "");
+    typedef CbmAlignedSide<_Float16, 4 * B, ALONG_K, SINGLE> Side;  // (a wave's loads are B rows)
+    static constexpr int ROWS = B, THREADS = 64 * WAVES, GROUPS = 1, LOADS = Side::LOADS, SLOT = B * 8, TM = B / 32, OUT_STRIDE = B / 4 + 1, UNITS = WAVES * 4 * SLOT;
+    static_assert(LOADS == B / 8 && UNITS >= WAVES * B * OUT_STRIDE && WAVES >= 4, "");
 
     __device__ __forceinline__ void run(uintx4* lds, const CbmOperand<_Float16>& a, const CbmOperand<_Float16>& b, int tile_m, int tile_n, int last) {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-        floatx16 acc[2][2] = {};
+        floatx16 acc[TM][TM] = {};
         Side sa, sb;
-        sa.begin(a, tile_m, 0, 64);
-        sb.begin(b, tile_n, 0, 64);
+        sa.begin(a, tile_m, 0, B);
+        sb.begin(b, tile_n, 0, B);
         uintx4 *here = lds + wave * 4 * SLOT, *next = here + 2 * SLOT;
         auto load = [&](int c, uintx4* to) {  // (zeros beyond the last chunk: as many loads are under way to the end)
 #pragma unroll
@@ -255,53 +267,56 @@ struct HalvesShares {
             for (int i = 0; i < LOADS; ++i) sb.template load<false>(b, c, b.K, to + SLOT, 0, i);
         };
         load(wave, here);
-        load(wave + 4, next);
-        for (int c = wave; c < last; c += 4) {
+        load(wave + WAVES, next);
+        for (int c = wave; c < last; c += WAVES) {
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS) : "memory");
-            uintx4 x[2][4], y[2][4];
+            uintx4 x[TM][4], y[TM][4];
 #pragma unroll
             for (int s = 0; s < 4; ++s)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 0; i < TM; ++i) {
                     x[i][s] = Side::unit(here, 32 * i, s);
                     y[i][s] = Side::unit(here + SLOT, 32 * i, s);
                 }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_sched_barrier(0);
-            load(c + 8, here);
+            load(c + 2 * WAVES, here);
 #pragma unroll
             for (int p = 0; p < 6; ++p)  // high by high, high by low, low by high, of either half of the chunk
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < TM; ++i)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) acc[i][j] = cbm_multiply<_Float16>(y[j][p % 2 + (p / 2 == 1 ? 2 : 0)], x[i][p % 2 + (p / 2 == 2 ? 2 : 0)], acc[i][j]);
+                    for (int j = 0; j < TM; ++j) acc[i][j] = cbm_multiply<_Float16>(y[j][p % 2 + (p / 2 == 1 ? 2 : 0)], x[i][p % 2 + (p / 2 == 2 ? 2 : 0)], acc[i][j]);
             uintx4* t = here;
             here = next;
             next = t;
         }
         asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-        uintx4* mine = lds + wave * 64 * OUT_STRIDE;
+        uintx4* mine = lds + wave * B * OUT_STRIDE;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < TM; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
                     mine[(32 * i + (lane & 31)) * OUT_STRIDE + 8 * j + 2 * q + (lane >> 5)] =
                         __builtin_bit_cast(uintx4, (floatx4){acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]});
         __syncthreads();
     }
+    // four waves, a quarter of the rows each
     template <class F, class G>
     __device__ __forceinline__ void both(uintx4* lds, int tile_m, int tile_n, F&& f, bool down, G&& g) const {
-        const int lane = threadIdx.x & 63, first = 16 * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // a wave's rows
-        const int64_t row = (int64_t)tile_m * 64 + first, column = (int64_t)tile_n * 64;
+        constexpr int R = B / 4, QUADS = R / 4;
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = R * wave;
+        if (wave >= 4) return;
+        const int64_t row = (int64_t)tile_m * B + first, column = (int64_t)tile_n * B;
 #pragma unroll 1
-        for (int t = 0; t < 4; ++t) {
-            const int r = 4 * t + lane / 16, c = lane % 16;
+        for (int t = 0; t < R * B / 256; ++t) {
+            const int r = (256 / B) * t + lane / (B / 4), c = lane % (B / 4);
             uintx4* at = lds + (first + r) * OUT_STRIDE + c;
             floatx4 sum = __builtin_bit_cast(floatx4, at[0]);
 #pragma unroll
-            for (int w = 1; w < 4; ++w) sum += __builtin_bit_cast(floatx4, at[w * 64 * OUT_STRIDE]);
+            for (int w = 1; w < WAVES; ++w) sum += __builtin_bit_cast(floatx4, at[w * B * OUT_STRIDE]);
             float v[4] = {sum[0], sum[1], sum[2], sum[3]};
             f(row + r, column + 4 * c, v);
             at[0] = __builtin_bit_cast(uintx4, (floatx4){v[0], v[1], v[2], v[3]});
@@ -311,8 +326,8 @@ struct HalvesShares {
         __builtin_amdgcn_wave_barrier();
         const float* of = (const float*)(lds + first * OUT_STRIDE);
 #pragma unroll 1
-        for (int t = 0; t < 4; ++t) {
-            const int r = lane % 4 * 4, c = t * 16 + lane / 4;
+        for (int t = 0; t < B * QUADS / 64; ++t) {
+            const int r = lane % QUADS * 4, c = t * (64 / QUADS) + lane / QUADS;
             float v[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] = of[(r + j) * (4 * OUT_STRIDE) + c];
@@ -342,7 +357,7 @@ __device__ __forceinline__ void below(int at, int& m, int& n) {
 }
 
 template <class Tiles, int MODE, class T>
-__global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_orthogonal_product_kernel(ProductArgs p) {
+__global__ __launch_bounds__(Tiles::THREADS, Tiles::GROUPS) void cbm_orthogonal_product_kernel(ProductArgs p) {
     constexpr int B = Tiles::ROWS;
     __shared__ uintx4 lds[Tiles::UNITS];
     int m, n;
@@ -623,16 +638,17 @@ template <class F>
 void with_tiles(int64_t M, int64_t N, int64_t K, bool half, F&& f) {
     double best = 1e30;
     int side = 256;
-    for (int b : {256, 192, 128, 64}) {
+    for (int b : {256, 192, 128, 64, 32}) {
         const int64_t m = (M + b - 1) / b, tiles = half ? m * (m + 1) / 2 : m * ((N + b - 1) / b), at_once = b == 128 ? 512 : 256;
-        const double each = 6.0 * b * b * (double)K / ((b == 256 ? 1250.0 : b == 192 ? 1150.0 : b == 128 ? 1050.0 : 500.0) * 1e6 / (double)at_once) * (b == 128 && tiles <= 256 ? 0.6 : 1.0);
-        const double us = (double)((tiles + at_once - 1) / at_once) * (each + (b == 256 ? 12.0 : b == 192 ? 9.0 : b == 128 ? 5.0 : 3.0));
+        const double each = 6.0 * b * b * (double)K / ((b == 256 ? 1250.0 : b == 192 ? 1150.0 : b == 128 ? 1050.0 : b == 64 ? 800.0 : 450.0) * 1e6 / (double)at_once) * (b == 128 && tiles <= 256 ? 0.6 : 1.0);
+        const double us = (double)((tiles + at_once - 1) / at_once) * (each + (b == 256 ? 12.0 : b == 192 ? 9.0 : b == 128 ? 5.0 : b == 64 ? 7.0 : 4.0));
         if (us < best) best = us, side = b;
     }
     if (side == 256) f((HalvesTiles<256>*)nullptr);
     else if (side == 192) f((HalvesTiles<192>*)nullptr);
     else if (side == 128) f((HalvesTiles<128>*)nullptr);
-    else f((HalvesShares*)nullptr);
+    else if (side == 64) f((HalvesShares<64, 4>*)nullptr);
+    else f((HalvesShares<32, 8>*)nullptr);
 }
 
 template <int MODE, class T>
@@ -641,7 +657,7 @@ void product(const ProductArgs& p, hipStream_t stream) {
     with_tiles(p.a.rows, p.b.rows, p.a.columns, half, [&](auto* tiles_type) {
         typedef std::remove_pointer_t<decltype(tiles_type)> Tiles;
         const int64_t m = (p.a.rows + Tiles::ROWS - 1) / Tiles::ROWS, tiles = half ? m * (m + 1) / 2 : m * ((p.b.rows + Tiles::ROWS - 1) / Tiles::ROWS);
-        cbm_orthogonal_product_kernel<Tiles, MODE, T><<<(unsigned)((tiles + CBM_XCD - 1) / CBM_XCD * CBM_XCD), 256, 0, stream>>>(p);
+        cbm_orthogonal_product_kernel<Tiles, MODE, T><<<(unsigned)((tiles + CBM_XCD - 1) / CBM_XCD * CBM_XCD), Tiles::THREADS, 0, stream>>>(p);
     });
 }
 
