@@ -355,6 +355,8 @@ void with_tiles(int64_t n, int64_t d, int64_t c, const Operands<T>& o, int32_t t
             else run((CbmAlignedTiles<T, 128, 128, ALONG_K, ACROSS_K, SINGLE>*)nullptr);
             return;
         }
+    if constexpr (sizeof(T) == 4)
+        if (cbm_is_narrow(c, type)) return run((CbmTiles<T, 256, 64, 4, 1, ALONG_K, ACROSS_K, SINGLE>*)nullptr);
     run((CbmTiles<T, 128, 128, 2, 2, ALONG_K, ACROSS_K, SINGLE>*)nullptr);
 }
 

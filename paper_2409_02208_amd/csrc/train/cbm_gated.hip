@@ -211,6 +211,8 @@ cbm_status cbm_launch_gated(int64_t n, int32_t k, int32_t m, int32_t type, int32
                 return;
             }
         }
+        if constexpr (sizeof(T) == 4)
+            if (cbm_is_narrow(2 * (int64_t)m, type)) return run((CbmTiles<T, 256, 64, 4, 1, ALONG_K, ACROSS_K, PAIR_ROWS>*)nullptr, a, b);
         run((CbmTiles<T, 128, 128, 2, 2, ALONG_K, ACROSS_K, PAIR_ROWS>*)nullptr, a, b);
     });
     return cbm_launched("gated layer launch");

@@ -63,4 +63,6 @@ void cbm_launch_small_along(int32_t type, int64_t M, int64_t N, int64_t K, const
                             void* stream);
 void cbm_launch_small_across(int32_t type, int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, const float* S0, const float* S1, int64_t lds, void* C0, int64_t ldc0, void* C1, int64_t ldc1,
                              void* stream);
+// fp32 with so few columns: tiles of 256 x 64, which waste half as much as those of 128 x 128.
+inline bool cbm_is_narrow(int64_t columns, int32_t type) { return type == CBM_F32 && columns <= 64; }
 cbm_status cbm_launched(const char* what);  // the status of the launches since the last look

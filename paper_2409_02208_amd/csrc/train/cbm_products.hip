@@ -168,7 +168,8 @@ struct Plan {
 // of its own.  Shares of at least 256 k.
 Plan plan(int64_t M, int64_t N, int64_t K, int32_t type, int tile) {
     M = cbm_whole(M, 8), N = cbm_whole(N, 8), K = cbm_whole(K, 64);  // (a copy in whole units has the same plan)
-    const int64_t side = tile ? tile : 128, tiles = std::max<int64_t>(1, (M + side - 1) / side * ((N + side - 1) / side)), at_once = tile == 256 ? 256 : 512;
+    const bool narrow = !tile && cbm_is_narrow(N, type);
+    const int64_t side = tile ? tile : 128, tiles = std::max<int64_t>(1, narrow ? (M + 255) / 256 : (M + side - 1) / side * ((N + side - 1) / side)), at_once = tile == 256 ? 256 : 512;
     const double tflops = tile == 256 ? 1150.0 : tile == 128 ? 900.0 : type == CBM_F32 ? 140.0 : 550.0, beside = tile == 256 ? 9.0 : 5.0;
     const double each = 2.0 * (double)(side * side * K) / (tflops * 1e6 / (double)at_once);
     Plan best{tile, 1, 1e30};
@@ -202,7 +203,9 @@ void launch(const CbmProduct& p, hipStream_t stream) {
         const int64_t tiles = (p.M + Tiles::ROWS - 1) / Tiles::ROWS * ((p.N + Tiles::COLUMNS - 1) / Tiles::COLUMNS), chunks = (K + Tiles::BK - 1) / Tiles::BK;
         cbm_product_kernel<Tiles, T><<<(unsigned)((tiles * splits + CBM_XCD - 1) / CBM_XCD * CBM_XCD), 256, 0, stream>>>(a, b, chunks, splits, out, p.parts);
     };
-    if (how.tile == 0) run((CbmTiles<T, 128, 128, 2, 2, OA, OB, PAIR>*)nullptr);
+    if constexpr (sizeof(T) == 4)
+        if (cbm_is_narrow(p.N, p.type)) run((CbmTiles<T, OA == ALONG_K ? 256 : 128, 64, OA == ALONG_K ? 4 : 2, OA == ALONG_K ? 1 : 2, OA, OB, PAIR>*)nullptr);  // (registers)
+    if (how.tile == 0 && !cbm_is_narrow(p.N, p.type)) run((CbmTiles<T, 128, 128, 2, 2, OA, OB, PAIR>*)nullptr);
     if constexpr (sizeof(T) == 2) {
         if (how.tile == 128) run((CbmAlignedTiles<T, 128, 128, OA, OB, PAIR>*)nullptr);
         if (how.tile == 256) run((CbmAlignedTiles<T, 256, 256, OA, OB, PAIR>*)nullptr);
