@@ -144,17 +144,18 @@ __global__ __launch_bounds__(512) void cbm_classes_small_slopes_kernel(int64_t n
     cbm_put(dZ + r * lddz, column, c, v);
 }
 
-// A wave a row: its parts in order, a lane's 64 apart, then over the lanes.
+// A row's parts in order, those of LANES lanes LANES apart, then over the lanes: a wave a row, or a lane a row where many have few parts.
+template <int LANES>
 __global__ __launch_bounds__(256) void cbm_classes_join_kernel(int64_t n, int64_t c, int64_t count, const void* __restrict__ labels, int label_bits, const Sums* __restrict__ parts,
                                                              const float* __restrict__ chosen, float* __restrict__ logp, float* __restrict__ stats) {
-    const int lane = threadIdx.x & 63;
-    for (int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); r < n; r += (int64_t)gridDim.x * 4) {
+    const int lane = threadIdx.x % LANES;
+    for (int64_t r = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES; r < n; r += (int64_t)gridDim.x * (256 / LANES)) {
         Sums all{-INFINITY, 0.0f};
-        constexpr int AHEAD = 8;  // (one row of 32,000 columns has 500 parts: their loads under way together, and one maximum for eight: 19.5 -> 17.9 us)
-        for (int64_t i = lane; i < count; i += 64 * AHEAD) {
+        constexpr int AHEAD = LANES == 1 ? 2 : 8;  // (one row of 32,000 columns has 500 parts: their loads under way together, and one maximum for eight: 19.5 -> 17.9 us)
+        for (int64_t i = lane; i < count; i += LANES * AHEAD) {
             Sums some[AHEAD];
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) some[k] = i + 64 * k < count ? parts[r * count + i + 64 * k] : Sums{-INFINITY, 0.0f};
+            for (int k = 0; k < AHEAD; ++k) some[k] = i + LANES * k < count ? parts[r * count + i + LANES * k] : Sums{-INFINITY, 0.0f};
             float m = all.m;
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) m = fmaxf(m, some[k].m);
@@ -164,8 +165,8 @@ __global__ __launch_bounds__(256) void cbm_classes_join_kernel(int64_t n, int64_
             for (int k = 0; k < AHEAD; ++k) s += some[k].s * __builtin_amdgcn_exp2f((some[k].m - away) * LOG2E);
             all = {m, s};
         }
-        const float m = lanes_all<64>(all.m, [](float a, float b) { return fmaxf(a, b); }), away = m == -INFINITY ? 0.0f : m;
-        const float s = lanes_sum<64>(all.s * __builtin_amdgcn_exp2f((all.m - away) * LOG2E));
+        const float m = lanes_all<LANES>(all.m, [](float a, float b) { return fmaxf(a, b); }), away = m == -INFINITY ? 0.0f : m;
+        const float s = lanes_sum<LANES>(all.s * __builtin_amdgcn_exp2f((all.m - away) * LOG2E));
         if (lane) continue;
         const bool bad = !(s < INFINITY);
         const float largest = bad ? NAN : m, l = bad ? NAN : logf(s);
@@ -395,7 +396,14 @@ cbm_status cbm_launch_classes(int64_t n, int32_t d, int32_t c, int32_t type, con
             cbm_classes_kernel<Tiles, T><<<grid, 256, 0, stream>>>(o.a, o.b, chunks, logp ? labels : nullptr, label_bits, parts, chosen);
         });
     });
-    cbm_classes_join_kernel<<<(unsigned)std::min<int64_t>((n + 3) / 4, 1 << 20), 256, 0, stream>>>(n, c, count, labels, label_bits, parts, chosen, logp, stats);
+    auto join = [&](auto lanes) {
+        constexpr int ROWS = 256 / decltype(lanes)::value;
+        cbm_classes_join_kernel<decltype(lanes)::value><<<(unsigned)std::min<int64_t>((n + ROWS - 1) / ROWS, 1 << 20), 256, 0, stream>>>(n, c, count, labels, label_bits, parts, chosen, logp, stats);
+    };
+    // (us with 64 lanes a row / these: 2097152 x 128 with 128 x 40 857 / 325; 65536 x 64 with 64 x 1000 93 / 80)
+    if (count <= 8 && n >= 4096) join(std::integral_constant<int, 1>{});
+    else if (count <= 64 && n >= 4096) join(std::integral_constant<int, 8>{});
+    else join(std::integral_constant<int, 64>{});
     return cbm_launched("linear log probabilities launch");
 }
 

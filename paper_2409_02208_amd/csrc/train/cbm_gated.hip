@@ -228,7 +228,7 @@ struct BackRoom {
 BackRoom back_room(int64_t n, int32_t k, int32_t m, int32_t type) {
     BackRoom r{};
     const int64_t bytes = type == CBM_F32 ? 4 : 2, wide = cbm_whole(k, 8);
-    r.at = cbm_whole(m, 64);
+    r.at = cbm_whole(m, type == CBM_F32 ? 32 : 64);  // (chunks of the products)
     r.small = cbm_small_backward(n, k, 2 * (int64_t)m, 0, cbm_small_groups(n, k) + 2 * cbm_small_groups(k, m), type);
     if (r.small) {
         r.bytes = n * 2 * r.at * 4;
