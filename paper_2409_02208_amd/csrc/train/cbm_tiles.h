@@ -203,8 +203,8 @@ struct CbmTileSums {
     static __device__ __forceinline__ int first_row() { return wave() % WM * (32 * TM); }
     static __device__ __forceinline__ int first_column() { return wave() / WM * (32 * TN); }
     static __device__ __forceinline__ int across() { return wave() / WM; }
-    // f(row, column of the first, four sums) for the wave's part of the result, rows of lanes along its rows: through LDS, 32 rows at a time, a place for each wave (so that 16384 x 1024 . 1024 x
-    // 8192 in bf16, which a lane's own four columns of a row at a time take 310 us for, takes 262).  The operands' places in LDS have to be free.
+    // f(row, column of the first, four sums) for the wave's part of the result, rows of lanes along its rows: through LDS, 32 rows at a time, a place for each wave (65536 x 1024 with 2 x 4096
+    // in bf16: pieces of 8 bytes 1596 us, of 16, and past the caches where the result does not fit them, 1342).  The operands' places in LDS have to be free.
     static constexpr int COLS = 32 * TN, OUT_STRIDE = COLS / 4 + 1, OUT_UNITS = WAVES * 32 * OUT_STRIDE;
     __device__ __forceinline__ void band_to_lds(uintx4* to, int i) const {
         const int l32 = threadIdx.x & 31, half = threadIdx.x >> 5 & 1;
