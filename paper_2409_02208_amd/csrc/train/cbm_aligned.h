@@ -4,6 +4,8 @@
 // Five places of an operand's 64 k each go round: both operands of a chunk, both of the next and the first of the one after.  A wave has 128 x 128 (or 64 x 64) sums and issues, between two products, at most
 // one read of LDS (the next step's units) or one load: loads issued together wait for the queue to take them, and the products behind them too.  8192 x 4096 . 4096 x 8192 in bf16 (a card whose library product
 // takes 405 us): two places of both operands, loads together 554 us; five places of 32 k, loads between products 500 (half of each 128-byte line a request); this 440.
+// Both operands across k ask for twice as many reads, of half the size: eight at a time, or the last come too late (weights' gradients of 16384 x 1024 with 2 x 4096, slopes and all, two at a time 416 us, four 397,
+// eight 394, all sixteen 396; with both along k, the gradient of X, one at a time 288, two 293, four 303).
 #pragma once
 
 #include "cbm_tiles.h"
@@ -140,7 +142,7 @@ struct CbmAlignedTiles : CbmTileSums<BM, BN, 2, 2> {
             for (int i = 0; i < TM; ++i)
 #pragma unroll
                 for (int j = 0; j < TN; ++j) acc[i][j] = cbm_multiply<T>(y[S & 1][j], x[S & 1][i], acc[i][j]);
-            constexpr int READS = TM * A::READS + TN * B::READS, AT_ONCE = (2 * READS + TM * TN - 1) / (TM * TN);
+            constexpr int READS = TM * A::READS + TN * B::READS, AT_ONCE = READS > 12 ? 8 : (2 * READS + TM * TN - 1) / (TM * TN);
             __builtin_amdgcn_sched_group_barrier(0x008, 1, S);
 #pragma unroll
             for (int i = 0; i < READS; i += AT_ONCE) {
