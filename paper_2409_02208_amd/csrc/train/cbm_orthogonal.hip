@@ -412,7 +412,7 @@ __global__ __launch_bounds__(Tiles::THREADS, Tiles::GROUPS) void cbm_orthogonal_
 
 // Small matrices: everything in one workgroup's LDS, Z and A (which P takes the place of), rows of blocks as in memory and one unit more, so that sixteen neighbouring rows' units fall on different banks.
 // A wave has a tile of 32 x 32.  Z's columns, which P Z wants, are turned as they are read.  What bounds it is one compute unit's LDS and the five barriers of a step (five steps of 64 x 64
-// 18 us, of 128 x 128 45; the launches of the general way take 75 at 129 x 130).
+// 18 us, of 128 x 128 45, of 16 x 300 26 and of 64 x 250 35; the launches of the general way take 75 at 64 x 500 or 129 x 130).
 constexpr int SMALL_STEPS = 16;
 struct SmallArgs {
     int rows, columns, steps;  // of Z
@@ -480,22 +480,27 @@ __device__ __forceinline__ void small_put(char* x, int pitch, int m, int n, cons
 // S x L: Z's rows and columns with zeros beyond them.
 template <class T, int S, int L>
 __global__ __launch_bounds__(S * L / 16) void cbm_orthogonal_small_kernel(SmallArgs p, const T* X, int64_t ldx, T* Y, int64_t ldy) {
-    constexpr int PZ = small_pitch(L), PG = small_pitch(S), WAVES = S / 32 * (L / 32), THREADS = 64 * WAVES, EACH = L * L / THREADS;
+    constexpr int PZ = small_pitch(L), PG = small_pitch(S), WAVES = S / 32 * (L / 32), THREADS = 64 * WAVES, EACH = S * L / THREADS;
     static_assert(S <= L, "");
     __shared__ uintx4 all[S * (PZ + PG) / 16];
     __shared__ double squares[WAVES];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     char *z = (char*)all, *g = z + S * PZ;
-    // X's values, zeros beyond it, neighbouring threads along its rows
-    const int height = p.transposed ? p.columns : p.rows, width = p.transposed ? p.rows : p.columns, c0 = threadIdx.x % L, r0 = threadIdx.x / L;
+    // X's values, neighbouring threads along its rows; zeros beyond it
+    const uint32_t height = p.transposed ? p.columns : p.rows, width = p.transposed ? p.rows : p.columns, down = THREADS / width, along = THREADS % width, r0 = threadIdx.x / width, c0 = threadIdx.x - r0 * width;
+    auto next = [&](uint32_t& r, uint32_t& c) {
+        c += along;
+        r += down + (c >= width ? 1 : 0);
+        c -= c >= width ? width : 0;
+    };
+    float x[EACH];
     double sum = 0.0;
-#pragma unroll 8
-    for (int i = 0; i < EACH; ++i) {
-        const int r = r0 + THREADS / L * i;
-        if (r >= height || c0 >= width) continue;
-        const double v = (double)(float)X[r * ldx + c0];
-        sum += v * v;
-    }
+    uint32_t xr = r0, xc = c0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i, next(xr, xc)) x[i] = xr < height ? (float)X[xr * ldx + xc] : 0.0f;
+    for (int i = threadIdx.x; i < S * PZ / 16; i += THREADS) all[i] = (uintx4){0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) sum += (double)x[i] * (double)x[i];
 #pragma unroll
     for (int step = 1; step < 64; step *= 2) sum += __shfl_xor(sum, step);
     if (lane == 0) squares[wave] = sum;
@@ -503,12 +508,13 @@ __global__ __launch_bounds__(S * L / 16) void cbm_orthogonal_small_kernel(SmallA
     sum = 0.0;
     for (int i = 0; i < WAVES; ++i) sum += squares[i];
     const double up = (double)p.first / (sqrt(sum) + (double)p.eps);
-#pragma unroll 8
-    for (int i = 0; i < EACH; ++i) {  // (read again, from L2)
-        const int r = r0 + THREADS / L * i, zr = p.transposed ? c0 : r, zc = p.transposed ? r : c0;
-        if (zr >= S || zc >= L) continue;
+    xr = r0, xc = c0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i, next(xr, xc)) {
+        if (xr >= height) continue;
+        const uint32_t zr = p.transposed ? xc : xr, zc = p.transposed ? xr : xc;
         _Float16 h, low;
-        cut(r < height && c0 < width ? (float)((double)(float)X[r * ldx + c0] * up) : 0.0f, h, low);
+        cut((float)((double)x[i] * up), h, low);
         _Float16* to = (_Float16*)(z + zr * PZ + zc / 32 * 128 + zc % 32 * 2);
         to[0] = h;
         to[32] = low;
@@ -676,7 +682,7 @@ cbm_status cbm_launch_orthogonal(int32_t m, int32_t n, int32_t type, const void*
     double* squares = (double*)(base + room.squares);
     double top = 1.0 + 0x1p-10;  // a bound of Z's singular values
     int up = power(top);
-    if (l <= 128 && steps > 0 && steps <= SMALL_STEPS) {
+    if (l <= (s <= 32 ? 512 : s <= 64 ? 256 : 128) && steps > 0 && steps <= SMALL_STEPS) {
         SmallArgs p{};
         p.rows = (int)s;
         p.columns = (int)l;
@@ -702,8 +708,11 @@ cbm_status cbm_launch_orthogonal(int32_t m, int32_t n, int32_t type, const void*
             using std::integral_constant;
             if (l <= 32) go(integral_constant<int, 32>{}, integral_constant<int, 32>{});
             else if (l <= 64) go(integral_constant<int, 64>{}, integral_constant<int, 64>{});
-            else if (s <= 64) go(integral_constant<int, 64>{}, integral_constant<int, 128>{});
-            else go(integral_constant<int, 128>{}, integral_constant<int, 128>{});
+            else if (s <= 64 && l <= 128) go(integral_constant<int, 64>{}, integral_constant<int, 128>{});
+            else if (l <= 128) go(integral_constant<int, 128>{}, integral_constant<int, 128>{});
+            else if (s <= 32 && l <= 256) go(integral_constant<int, 32>{}, integral_constant<int, 256>{});
+            else if (s <= 32) go(integral_constant<int, 32>{}, integral_constant<int, 512>{});
+            else go(integral_constant<int, 64>{}, integral_constant<int, 256>{});
         });
         return cbm_launched("orthogonal update launch");
     }

@@ -184,3 +184,13 @@ def test_large_and_small_coefficients(env, m, n):  # noqa: F811
     x = np.random.default_rng(8).standard_normal((m, n))
     for abc, steps in (((10.0, 0.0, 0.0), 6), ((0.01, 0.0, 0.0), 6), ((1.5, -0.5, 0.0), 12), ((1e25, 0.0, 0.0), 1)):
         _check(torch, cbm, x, "f32", steps=steps, coefficients=abc)
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("m,n", [(1, 129), (31, 129), (3, 255), (32, 256), (256, 17), (32, 257), (20, 511), (512, 32), (1, 512), (33, 130), (64, 256), (256, 64), (250, 63), (34, 255), (513, 32), (257, 33), (65, 129)])
+def test_thin_matrices(env, name, m, n):  # noqa: F811
+    """Short sides of up to 32 and 64 with long ones up to 512 and 256, and the next beyond."""
+    torch, cbm = env
+    x = np.random.default_rng(m + 1000 * n).standard_normal((m, n))
+    for pad, offset, in_place in ((0, 0, False), (5, 3, True)):
+        _check(torch, cbm, x, name, pad, offset, in_place)
