@@ -277,7 +277,8 @@ struct Copies {
 Copies copies_of(int64_t n, int32_t d, int32_t c, int32_t type) {
     if (!cbm_may_pack(n, d, c, type)) return {};
     const int64_t ld = cbm_whole(d, 8);
-    return {ld, 2 * n * ld, 2 * (n + cbm_whole(c, 8)) * ld};
+    const int64_t x = 2 * cbm_whole(n, 8) * ld;
+    return {ld, x, x + 2 * cbm_whole(c, 8) * ld};
 }
 
 struct Room {

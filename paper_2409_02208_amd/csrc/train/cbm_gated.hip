@@ -148,7 +148,8 @@ struct Copies {
 Copies copies_of(int64_t n, int32_t k, int32_t m, int32_t type) {
     if (!cbm_may_pack(n, k, 2 * (int64_t)m, type)) return {};
     const int64_t ld = cbm_whole(k, 8);
-    return {ld, 2 * n * ld, 2 * n * ld + 4 * cbm_whole(m, 32) * ld};
+    const int64_t x = 2 * cbm_whole(n, 8) * ld;
+    return {ld, x, x + 4 * cbm_whole(m, 32) * ld};
 }
 
 }  // namespace
@@ -236,8 +237,8 @@ BackRoom back_room(int64_t n, int32_t k, int32_t m, int32_t type) {
     }
     r.copies = cbm_may_pack(n, k, 2 * (int64_t)m, type);
     r.x = cbm_whole(n * 2 * r.at * bytes, 16);
-    r.weights = r.x + (r.copies ? 2 * n * wide : 0);
-    r.parts = r.weights + (r.copies ? 4 * k * r.at : 0);
+    r.weights = r.x + (r.copies ? 2 * cbm_whole(n, 8) * wide : 0);
+    r.parts = r.weights + (r.copies ? 4 * wide * r.at : 0);
     int64_t parts = 0;
     const int64_t dx = cbm_product_parts(n, k, 2 * r.at, type), dw = cbm_product_parts(wide, 2 * r.at, n, type);
     if (dx > 1) parts = dx * n * k;
@@ -292,7 +293,7 @@ cbm_status cbm_launch_gated_backward(int64_t n, int32_t k, int32_t m, int32_t ty
         p.ldb[1] = ldwu;
         if (room.copies && !(in_units(Wg, ldwg, m) && in_units(Wu, ldwu, m) && ldwg == ldwu)) {
             for (int i = 0; i < 2; ++i) {
-                void* to = base + room.weights + i * 2 * k * at;
+                void* to = base + room.weights + i * 2 * cbm_whole(k, 8) * at;
                 cbm_launch_pack(p.B[i], p.ldb[i], k, m, false, to, at, 0, 0, stream);
                 p.B[i] = to;
                 p.ldb[i] = at;

@@ -37,7 +37,7 @@ int64_t cbm_product_parts(int64_t M, int64_t N, int64_t K, int32_t type);
 inline bool cbm_may_pack(int64_t rows, int64_t K, int64_t columns, int32_t type) { return type != CBM_F32 && rows >= 1024 && K >= 256 && 2e-11 * (double)rows * (double)K * (double)columns >= 1.0; }
 constexpr int64_t CBM_TURN_ROWS = 4096;  // from so many rows on turning pays
 inline int64_t cbm_whole(int64_t v, int64_t of) { return (v + of - 1) / of * of; }
-// Rows of `columns` values and zeros up to ldt, a multiple of 8, and rows of zeros up to a multiple of 8: row r at row `blocks` (r / 32) + r % 32 + `at` where blocks are asked for, else r.  turned: value
+// Rows of `columns` values and zeros up to ldt, a multiple of 8, and rows of zeros up to a multiple of 8, which a copy's place has room for: row r at row `blocks` (r / 32) + r % 32 + `at` where blocks are asked for, else r.  turned: value
 // (r, c) is from[c ld + r].
 void cbm_launch_pack(const void* from, int64_t ld, int64_t rows, int64_t columns, bool turned, void* to, int64_t ldt, int64_t blocks, int64_t at, void* stream);
 // 256 or 128: the tiles that a product whose units go straight to LDS is made in
