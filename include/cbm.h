@@ -437,7 +437,8 @@ size_t cbm_gated_linear_backward_workspace_bytes(int64_t n, int32_t k, int32_t m
  *   workspace    cbm_linear_log_probs_workspace_bytes(n, d, c, type) bytes.
  * A row with a score of NaN or +infinity has NaN for all of it (0 without a label).
  *
- * cbm_linear_log_probs_backward -- with dZ = dlogp (1[label] - p), rounded to `type` unless the products are small (16 bits: at 2^15 over the largest finite |dlogp| of its size), and nothing for rows without a label,
+ * cbm_linear_log_probs_backward -- with dZ = dlogp (1[label] - p), and nothing for rows without a label or a distribution (m of -infinity), whatever dlogp has there; rounded to `type` unless the products are
+ * small (16 bits: at 2^15 over the largest finite |dlogp| of the other rows of its size, so that in fp16 what is 2^-40 of that and less is lost),
  *   dX = dZ W^T (n x d),  dW = X^T dZ (d x c; zeros for n = 0), of `type`; either may be NULL.  Values of X must be finite in rows without a label, too.
  *   The scores are made again from X and W, a piece of the classes at a time, with m and l from `stats`.
  *   workspace    cbm_linear_log_probs_backward_workspace_bytes(n, d, c, type) bytes: dZ of a piece (512 MiB or 1,024 classes), and sums.

@@ -181,18 +181,27 @@ __global__ __launch_bounds__(256) void cbm_classes_join_kernel(int64_t n, int64_
     }
 }
 
-// Types of 16 bits: dZ is kept at 2^15 over the largest finite |dlogp| of its size; what is made of it is multiplied by the factor, scale[0], and dlogp by scale[1].  In fp16 the gradients of a batch's
+// Types of 16 bits: dZ is kept at 2^15 over the largest finite |dlogp| of its size, of the rows that have a label and a distribution (nothing comes of the others, whatever dlogp has there); what is made of it is multiplied by the factor, scale[0], and dlogp by scale[1].  In fp16 the gradients of a batch's
 // scores would be small beside 2^-14: here 1 - p fits and a p down to 2^-29 keeps all its bits.  In both types the rows of a mean, which all have the same dlogp, have their labels' own 1 - p just below a
 // power of two, where half a step is 2^-9 (bf16) of it at most and p itself where that is less; at 1 / n it would be up to 2^-8, the same for every row, and nothing evens it out.
 constexpr int SCALE_GROUPS = 256;
-__global__ __launch_bounds__(1024) void cbm_classes_scale_kernel(int64_t n, const float* __restrict__ from, float* __restrict__ scale, float* __restrict__ parts) {
+__global__ __launch_bounds__(1024) void cbm_classes_scale_kernel(int64_t n, const float* __restrict__ from, const void* __restrict__ labels, int label_bits, int64_t c, const float* __restrict__ stats,
+                                                               float* __restrict__ scale, float* __restrict__ parts) {  // labels: NULL where `from` has parts
     __shared__ float room[16];
     constexpr int AHEAD = 8;
     float most = 0x1p-100f;  // (neither factor overflows)
     for (int64_t i = (int64_t)blockIdx.x * 1024 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 1024 * AHEAD) {
         float v[AHEAD];
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) v[k] = fabsf(from[min(i + (int64_t)gridDim.x * 1024 * k, n - 1)]);
+        for (int k = 0; k < AHEAD; ++k) {
+            const int64_t r = min(i + (int64_t)gridDim.x * 1024 * k, n - 1);
+            v[k] = fabsf(from[r]);
+            if (labels) {
+                const int64_t label = label_of(labels, label_bits, r);
+                const float m = stats[2 * r];
+                if (label < 0 || label >= c || m == -INFINITY) v[k] = 0.0f;
+            }
+        }
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) most = v[k] < INFINITY ? fmaxf(most, v[k]) : most;
     }
@@ -433,8 +442,8 @@ cbm_status cbm_launch_classes_backward(int64_t n, int32_t d, int32_t c, int32_t 
     if (scale && n > 0) {
         float* most = scale + 4;
         const bool many = n > 1 << 16;  // (of a million rows one workgroup takes 80 us)
-        if (many) cbm_classes_scale_kernel<<<SCALE_GROUPS, 1024, 0, stream>>>(n, dlogp, nullptr, most);
-        cbm_classes_scale_kernel<<<1, 1024, 0, stream>>>(many ? SCALE_GROUPS : n, many ? most : dlogp, scale, nullptr);
+        if (many) cbm_classes_scale_kernel<<<SCALE_GROUPS, 1024, 0, stream>>>(n, dlogp, labels, label_bits, c, stats, nullptr, most);
+        cbm_classes_scale_kernel<<<1, 1024, 0, stream>>>(many ? SCALE_GROUPS : n, many ? most : dlogp, many ? nullptr : labels, label_bits, c, stats, scale, nullptr);
     }
     cbm_with_type(type, [&](auto t) {
         using T = decltype(t);
