@@ -192,15 +192,23 @@ __global__ __launch_bounds__(1024) void cbm_classes_scale_kernel(int64_t n, cons
     float most = 0x1p-100f;  // (neither factor overflows)
     for (int64_t i = (int64_t)blockIdx.x * 1024 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 1024 * AHEAD) {
         float v[AHEAD];
+        auto row = [&](int k) { return min(i + (int64_t)gridDim.x * 1024 * k, n - 1); };
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            const int64_t r = min(i + (int64_t)gridDim.x * 1024 * k, n - 1);
-            v[k] = fabsf(from[r]);
-            if (labels) {
-                const int64_t label = label_of(labels, label_bits, r);
-                const float m = stats[2 * r];
-                if (label < 0 || label >= c || m == -INFINITY) v[k] = 0.0f;
-            }
+        for (int k = 0; k < AHEAD; ++k) v[k] = fabsf(from[row(k)]);
+        if (labels) {
+            int64_t label[AHEAD];
+            float m[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) m[k] = stats[2 * row(k)];
+            if (label_bits == 64)
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) label[k] = ((const int64_t*)labels)[row(k)];
+            else
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) label[k] = ((const int32_t*)labels)[row(k)];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+                if (label[k] < 0 || label[k] >= c || m[k] == -INFINITY) v[k] = 0.0f;
         }
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) most = v[k] < INFINITY ? fmaxf(most, v[k]) : most;
