@@ -410,7 +410,8 @@ cbm_status cbm_log_probs_backward(int64_t n, int32_t c, int32_t type, const void
  *   G, U         receive X Wg and X Wu (n x m, of `type`), which the backward pass reads; either may be NULL.  H is made of the sums before they are rounded.
  *   workspace    cbm_gated_linear_workspace_bytes(n, k, m, type) bytes (may be 0).
  *
- * cbm_gated_linear_backward -- with dU = dH o a(G) and dG = dH o U o a'(G) (a'(0) = 0 for CBM_RELU), each rounded to `type` unless the products are small:
+ * cbm_gated_linear_backward -- with dU = dH o a(G) and dG = dH o U o a'(G) (a'(0) = 0 for CBM_RELU), each rounded to `type` unless the products are small (fp16: at a power of two that puts the largest finite one between 2^3
+ * and 65504, so that what is 2^-28 of it and less may be lost):
  *   dX = dG Wg^T + dU Wu^T (n x k),  dWg = X^T dG,  dWu = X^T dU (k x m), of `type`; each may be NULL, not all three.  dWg and dWu are zeros for n = 0.
  *   workspace    cbm_gated_linear_backward_workspace_bytes(n, k, m, type) bytes.
  *

@@ -103,11 +103,41 @@ __global__ __launch_bounds__(64 * few_waves(NR)) void cbm_gated_few_kernel(int64
 
 // dG and dU side by side in `out`, from column 0 and column `at` on, zeros between: in fp32 for small products, else rounded to the type (half a step each, as much as the gradients that are made of them are
 // rounded by, so that those are off by 1.4 times as much as they would be; a second part would take the products twice as long).
+// Rounded to fp16 they are kept at a power of two, or products of what fp16 holds would not fit it (65504^2) or vanish (2^-48) where the gradients do not.  It goes by the largest finite one, which the launch that
+// makes them finds out: at 2^10 first, and once more, by a launch that otherwise ends at once, where that puts the largest outside 2^3 to 65504, at the power that puts it below 2^15.  What is made of them is
+// multiplied by scale[0].  (16384 x 4096: 124 and 5 us, or 124 and 130 where they are made twice; in bf16 one launch takes 111.)
+constexpr int SLOPE_GROUPS = 2048;  // parts of the largest (all of them are read by every group of the second launch: of 8192 parts that takes 25 us instead of 5)
+constexpr float SLOPES_AT = 0x1p10f, LEAST_SLOPE = 0x1p3f, MOST_SLOPE = 65504.0f;
+template <class T, class S>
+constexpr bool cbm_scaled_slopes = sizeof(S) == 2 && !std::is_same<T, __bf16>::value;
+
+__device__ __forceinline__ float largest_of_group(float most, float (&room)[4]) {
+    most = lanes_all<64>(most, [](float a, float b) { return fmaxf(a, b); });
+    if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = most;
+    __syncthreads();
+    return fmaxf(fmaxf(room[0], room[1]), fmaxf(room[2], room[3]));
+}
+
+// again: of `most` as the first launch left it
 template <class T, class S, int ACT>
 __global__ __launch_bounds__(256) void cbm_gated_slopes_kernel(int64_t n, int m, const T* __restrict__ dH, int64_t lddh, const T* __restrict__ G, int64_t ldg, const T* __restrict__ U,
-                                                            int64_t ldu, S* __restrict__ out, int64_t at) {
+                                                            int64_t ldu, S* __restrict__ out, int64_t at, float* __restrict__ scale, float* __restrict__ most, bool again) {
     constexpr int V = 16 / (int)sizeof(T);
+    constexpr bool SCALED = cbm_scaled_slopes<T, S>;
     const int64_t pieces = at / V;
+    float up = 1.0f, largest = 0.0f;
+    __shared__ float room[SCALED ? 4 : 1];
+    if constexpr (SCALED) {
+        up = SLOPES_AT;
+        if (again) {
+            for (uint32_t i = threadIdx.x; i < gridDim.x; i += 256) largest = fmaxf(largest, most[i]);
+            largest = largest_of_group(largest, room);
+            const bool fits = largest == 0.0f || (largest * SLOPES_AT >= LEAST_SLOPE && largest * SLOPES_AT <= MOST_SLOPE);
+            if (!fits) up = ldexpf(1.0f, min(14 - ilogbf(largest), 100));
+            if (blockIdx.x == 0 && threadIdx.x == 0) scale[0] = 1.0f / up;
+            if (fits) return;
+        }
+    }
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n * pieces; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / pieces;
         const int c = (int)(i % pieces) * V;
@@ -131,9 +161,20 @@ __global__ __launch_bounds__(256) void cbm_gated_slopes_kernel(int64_t n, int m,
             activated<T, ACT>(g[j], value, slope);
             du[j] = c + j < m ? dh[j] * value : 0.0f;
             dg[j] = c + j < m ? dh[j] * u[j] * slope : 0.0f;
+            if constexpr (SCALED) {
+                const float a = fabsf(du[j]), b = fabsf(dg[j]);
+                largest = fmaxf(largest, fmaxf(a < INFINITY ? a : 0.0f, b < INFINITY ? b : 0.0f));
+                du[j] *= up;
+                dg[j] *= up;
+            }
         }
         store_piece<V>(out + r * 2 * at + c, dg);
         store_piece<V>(out + r * 2 * at + at + c, du);
+    }
+    if constexpr (SCALED) {
+        if (again) return;
+        largest = largest_of_group(largest, room);
+        if (threadIdx.x == 0) most[blockIdx.x] = largest;
     }
 }
 
@@ -221,9 +262,9 @@ cbm_status cbm_launch_gated(int64_t n, int32_t k, int32_t m, int32_t type, int32
 
 namespace {
 
-// dG and dU side by side, copies of X and of the weights (rows of whole units), shares of K.
+// dG and dU side by side, their power of two and largest ones, copies of X and of the weights (rows of whole units), shares of K.
 struct BackRoom {
-    int64_t at, x, weights, parts, bytes;  // column of dU; where they begin
+    int64_t at, scale, x, weights, parts, bytes;  // column of dU; where they begin
     bool copies, small;
 };
 BackRoom back_room(int64_t n, int32_t k, int32_t m, int32_t type) {
@@ -236,7 +277,8 @@ BackRoom back_room(int64_t n, int32_t k, int32_t m, int32_t type) {
         return r;
     }
     r.copies = cbm_may_pack(n, k, 2 * (int64_t)m, type);
-    r.x = cbm_whole(n * 2 * r.at * bytes, 16);
+    r.scale = cbm_whole(n * 2 * r.at * bytes, 16);
+    r.x = r.scale + (type == CBM_F16 ? 16 + 4 * SLOPE_GROUPS : 0);
     r.weights = r.x + (r.copies ? 2 * cbm_whole(n, 8) * wide : 0);
     r.parts = r.weights + (r.copies ? 4 * wide * r.at : 0);
     int64_t parts = 0;
@@ -257,15 +299,18 @@ cbm_status cbm_launch_gated_backward(int64_t n, int32_t k, int32_t m, int32_t ty
     const BackRoom room = back_room(n, k, m, type);
     const int64_t at = room.at;
     char* base = (char*)workspace;
-    float* parts = (float*)(base + room.parts);
+    float *parts = (float*)(base + room.parts), *scale = type == CBM_F16 && !room.small && n > 0 ? (float*)(base + room.scale) : nullptr;
     if (n > 0)
         cbm_with_type(type, [&](auto t) {
             using T = decltype(t);
             const int64_t blocks = (n * (at * (int64_t)sizeof(T) / 16) + 255) / 256;
             with_activation(act, [&](auto which) {
                 auto slopes = [&](auto* out) {
-                    cbm_gated_slopes_kernel<T, std::remove_pointer_t<decltype(out)>, decltype(which)::value><<<(unsigned)std::min<int64_t>(blocks, 1 << 22), 256, 0, (hipStream_t)stream>>>(
-                        n, m, (const T*)dH, lddh, (const T*)G, ldg, (const T*)U, ldu, out, at);
+                    using S = std::remove_pointer_t<decltype(out)>;
+                    const unsigned grid = (unsigned)std::min<int64_t>(blocks, cbm_scaled_slopes<T, S> ? SLOPE_GROUPS : 1 << 22);
+                    for (int again = 0; again < (cbm_scaled_slopes<T, S> ? 2 : 1); ++again)
+                        cbm_gated_slopes_kernel<T, S, decltype(which)::value><<<grid, 256, 0, (hipStream_t)stream>>>(n, m, (const T*)dH, lddh, (const T*)G, ldg, (const T*)U, ldu, out, at, scale,
+                                                                                                                    scale ? scale + 4 : nullptr, again != 0);
                 };
                 if (room.small) slopes((float*)workspace);
                 else slopes((T*)workspace);
@@ -281,6 +326,7 @@ cbm_status cbm_launch_gated_backward(int64_t n, int32_t k, int32_t m, int32_t ty
     p.type = type;
     p.A = workspace;
     p.lda = 2 * at;
+    p.out.factor = scale;
     auto in_units = [&](const void* q, int64_t ld, int64_t along) { return cbm_units((const _Float16*)q, ld, along); };
     if (dX && n > 0) {
         p.M = n;

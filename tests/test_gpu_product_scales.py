@@ -58,3 +58,56 @@ def test_rows_without_a_label_or_a_distribution_say_nothing_about_the_rest(env, 
     off = given[:, None] * (size + ROUNDING[name] * (np.abs(dz) + size) + least)
     _near(want[0], dz @ w.T, _rounded(dz @ w.T, SUM(c) * ((np.abs(dz) + off) @ np.abs(w.T)) + off @ np.abs(w.T), name))
     _near(want[1], x.T @ dz, _rounded(x.T @ dz, SUM(n) * (np.abs(x.T) @ (np.abs(dz) + off)) + np.abs(x.T) @ off, name))
+
+
+# sizes of dH, U, X and the weights: dG and dU beyond fp16's largest value, below its smallest, of one entry alone beyond it, and as they usually are; the gradients can be held in all of them
+SLOPES = {"large": (300.0, 300.0, 1e-4, 1e-3), "tiny": (2.0 ** -14, 2.0 ** -12, 512.0, 512.0), "small": (2.0 ** -18, 1.0, 1.0, 1.0), "usual": (0.01, 1.0, 1.0, 0.2), "near one": (1.0, 1.0, 1.0, 0.2)}
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("sizes", SLOPES)
+@pytest.mark.parametrize("n,k,m,act", [(20003, 65, 47, "relu"), (9001, 17, 300, "silu"), (5000, 64, 264, "gelu"), (4100, 136, 1024, "silu")])
+def test_slopes_of_a_gated_layer_of_any_size(env, name, sizes, n, k, m, act):  # noqa: F811
+    torch, cbm = env
+    of_dh, of_u, of_x, of_w = SLOPES[sizes]
+    rng = np.random.default_rng(n + len(sizes))
+    dH, X, Wg, Wu, G, U_ = (_matrix(torch, s * rng.standard_normal(shape), name, 0)[0]
+                            for s, shape in ((of_dh, (n, m)), (of_x, (n, k)), (of_w, (k, m)), (of_w, (k, m)), (2.0, (n, m)), (of_u, (n, m))))
+    outs = [torch.empty_like(t) for t in (X, Wg, Wu)]
+    ws = torch.full((cbm.cbm_gated_linear_backward_workspace_bytes(n, k, m, X.dtype),), 255, dtype=torch.uint8, device="cuda")
+    cbm.cbm_gated_linear_backward(dH, X, Wg, Wu, G, U_, *outs, activation=act, workspace=ws)
+    dh, x, wg, wu, g, u = (_numbers(t) for t in (dH, X, Wg, Wu, G, U_))
+    dx, dwg, dwu, dg, du = orc.gated_linear_backward(dh, x, wg, wu, g, u, act)
+    assert max(np.abs(v).max() for v in (dx, dwg, dwu)) < 60000  # (fp16 holds the gradients)
+    # the activation: exp's argument is off by |g| 2^-24 of it, erfc's by g^2 2^-23; the type's rounding, where fp16's smallest values are those of the largest slope at 2^3
+    of = (np.abs(g) + (np.minimum(g * g, 64.0) if act == "gelu" else 0.0) + 16) * 2 * U * (np.abs(g) + 1)
+    least = 2.0 ** -28 * max(np.abs(dg).max(), np.abs(du).max()) if name == "f16" else 0.0
+    half = ROUNDING[name]
+    of_dg, of_du = (b + half * (np.abs(v) + b) + least for v, b in ((dg, np.abs(dh * u) * of + 3 * U * np.abs(dg)), (du, np.abs(dh) * of + 2 * U * np.abs(du))))
+    bound = sum(SUM(2 * m + 128) * ((np.abs(v) + o) @ np.abs(w.T)) + o @ np.abs(w.T) for v, o, w in ((dg, of_dg, wg), (du, of_du, wu)))
+    _near(outs[0], dx, _rounded(dx, bound, name))
+    for got, want, v, o in ((outs[1], dwg, dg, of_dg), (outs[2], dwu, du, of_du)):
+        _near(got, want, _rounded(want, SUM(n) * (np.abs(x.T) @ (np.abs(v) + o)) + np.abs(x.T) @ o, name))
+
+
+@pytest.mark.parametrize("n,k,m", [(9001, 17, 300), (4100, 136, 1024)])
+def test_slopes_of_a_gated_layer_that_are_not_finite_or_nothing(env, n, k, m):  # noqa: F811
+    """In fp16: rows without such a slope come out as if there were none, whatever the others' size, and slopes of zero give zeros."""
+    torch, cbm = env
+    rng = np.random.default_rng(n)
+    dH, X, Wg, Wu, G, U_ = (_matrix(torch, s * rng.standard_normal(shape), "f16", 0)[0]
+                            for s, shape in ((1e-4, (n, m)), (1.0, (n, k)), (0.2, (k, m)), (0.2, (k, m)), (2.0, (n, m)), (1.0, (n, m))))
+    ws = torch.empty(cbm.cbm_gated_linear_backward_workspace_bytes(n, k, m, X.dtype), dtype=torch.uint8, device="cuda")
+    rows = torch.ones(n, dtype=torch.bool, device="cuda")
+    rows[[3, n - 1]] = False
+    some = []
+    for bad in (0.0, math.nan, math.inf):
+        dH[[3, n - 1]] = bad
+        outs = [torch.ones_like(t) for t in (X, Wg, Wu)]
+        cbm.cbm_gated_linear_backward(dH, X, Wg, Wu, G, U_, *outs, workspace=ws)
+        some.append(outs[0])
+    assert torch.equal(some[0][rows], some[1][rows]) and torch.equal(some[0][rows], some[2][rows])
+    assert not bool(some[0][~rows].any()) and not bool(some[1][~rows].isfinite().any()) and not bool(some[2][~rows].isfinite().any())
+    assert bool(some[0][rows].isfinite().all()) and bool(some[0][rows].any())
+    cbm.cbm_gated_linear_backward(dH.zero_(), X, Wg, Wu, G, U_, *outs, workspace=ws)
+    assert not any(bool(t.any()) for t in outs)
