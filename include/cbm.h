@@ -435,7 +435,7 @@ size_t cbm_gated_linear_backward_workspace_bytes(int64_t n, int32_t k, int32_t m
  * l = log sum exp(z - m), log p = z - m - l.
  *   X            n x d, W d x c, of `type`.  Products and sums as for cbm_gated_linear; Z is not rounded.
  *   labels, label_bits, logp, stats   as for cbm_log_probs (log p[label], 0 without a label; m and l); logp and stats may be NULL, labels where logp is.
- *   workspace    cbm_linear_log_probs_workspace_bytes(n, d, c, type) bytes.
+ *   workspace    cbm_linear_log_probs_workspace_bytes(n, d, c, type) bytes: up to 512 MiB of maxima and sums, by rows, and copies of operands.
  * A row with a score of NaN or +infinity has NaN for all of it (0 without a label).
  *
  * cbm_linear_log_probs_backward -- with dZ = dlogp (1[label] - p), and nothing for rows without a label or a distribution (m of -infinity), whatever dlogp has there; rounded to `type` unless the products are

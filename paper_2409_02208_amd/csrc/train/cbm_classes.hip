@@ -279,6 +279,11 @@ __global__ __launch_bounds__(256, Tiles::GROUPS) void cbm_classes_slopes_kernel(
 bool is_small(int64_t n, int32_t d, int32_t c, int32_t type) { return cbm_small_forward(n, d, c, cbm_small_groups(n, c), type); }
 int64_t most_parts(int64_t n, int32_t d, int32_t c, int32_t type) { return std::max(n <= cbm_most_few_rows<float> || is_small(n, d, c, type) ? ((int64_t)c + 31) / 32 : 0, ((int64_t)c + 127) / 128 * 2); }
 int64_t rounded16(int64_t bytes) { return (bytes + 15) / 16 * 16; }
+// Rows whose parts are kept at a time: 512 MiB of them, at least 256 rows.  (Also what keeps a launch below 2^32 threads: 2^18 tiles of 128 x 128 at most.)
+int64_t band_of(int64_t n, int32_t d, int32_t c, int32_t type) {
+    const int64_t fit = ((int64_t)512 << 20) / (most_parts(n, d, c, type) * (int64_t)sizeof(Sums)) / 256 * 256;
+    return std::min(n, std::max<int64_t>(fit, 256));
+}
 int64_t bytes_of(int32_t type) { return type == CBM_F32 ? 4 : 2; }
 
 // Columns of a piece of the classes whose dZ is kept at a time: 512 MiB, at least 1,024 columns.
@@ -348,6 +353,13 @@ struct Operands {
             units = units && (turned || whole);
         }
     }
+    // rows `first` .. first + height - 1 of X
+    CbmOperand<T> rows(int64_t first, int64_t height) const {
+        CbmOperand<T> o = a;
+        o.p[0] += first * a.ld[0];
+        o.count = height;
+        return o;
+    }
     // columns `first` .. first + width - 1
     CbmOperand<T> some(int64_t first, int64_t width) const {
         CbmOperand<T> o = b;
@@ -382,46 +394,54 @@ void with_tiles(int64_t n, int64_t d, int64_t c, const Operands<T>& o, int32_t t
 }  // namespace
 
 int64_t cbm_classes_workspace(int64_t n, int32_t d, int32_t c, int32_t type) {
-    return rounded16(n * most_parts(n, d, c, type) * (int64_t)sizeof(Sums)) + rounded16(4 * n) + copies_of(n, d, c, type).bytes;
+    const int64_t band = band_of(n, d, c, type);
+    return rounded16(band * most_parts(n, d, c, type) * (int64_t)sizeof(Sums)) + rounded16(4 * band) + copies_of(n, d, c, type).bytes;
 }
 
 cbm_status cbm_launch_classes(int64_t n, int32_t d, int32_t c, int32_t type, const void* X, int64_t ldx, const void* W, int64_t ldw, const void* labels, int label_bits, float* logp, float* stats,
                               void* workspace, void* stream_) {
     hipStream_t stream = (hipStream_t)stream_;
     if (n == 0) return CBM_OK;
-    int64_t count = 0;  // parts of a row: of the waves along a tile's columns
+    const int64_t band = band_of(n, d, c, type);
     Sums* parts = (Sums*)workspace;
-    float* chosen = (float*)((char*)workspace + rounded16(n * most_parts(n, d, c, type) * (int64_t)sizeof(Sums)));
+    float* chosen = (float*)((char*)workspace + rounded16(band * most_parts(n, d, c, type) * (int64_t)sizeof(Sums)));
+    // rows r0 .. r0 + rows - 1 from their `count` parts each, of the waves along a tile's columns
+    auto join = [&](int64_t r0, int64_t rows, int64_t count) {
+        auto go = [&](auto lanes) {
+            constexpr int LANES = decltype(lanes)::value, ROWS = 256 / LANES;
+            cbm_classes_join_kernel<LANES><<<(unsigned)std::min<int64_t>((rows + ROWS - 1) / ROWS, 1 << 20), 256, 0, stream>>>(
+                rows, c, count, (const char*)labels + r0 * (label_bits / 8), label_bits, parts, chosen, logp ? logp + r0 : nullptr, stats ? stats + 2 * r0 : nullptr);
+        };
+        // (us with 64 lanes a row / these: 2097152 x 128 with 128 x 40 857 / 325; 65536 x 64 with 64 x 1000 93 / 80)
+        if (count <= 8 && rows >= 4096) go(std::integral_constant<int, 1>{});
+        else if (count <= 64 && rows >= 4096) go(std::integral_constant<int, 8>{});
+        else go(std::integral_constant<int, 64>{});
+    };
     cbm_with_type(type, [&](auto t) {
         using T = decltype(t);
         constexpr int V = 16 / (int)sizeof(T);
         if (n <= cbm_most_few_rows<T> && c >= V) {
-            count = ((int64_t)c + 8 * V - 1) / (8 * V);
+            const int64_t count = ((int64_t)c + 8 * V - 1) / (8 * V);
             cbm_with_few_rows(n, [&](auto rows) {
                 cbm_classes_few_kernel<T, decltype(rows)::value><<<dim3((unsigned)((count + 7) / 8 * 8), (unsigned)((n + CBM_FEW_ROWS - 1) / CBM_FEW_ROWS)), 64 * FEW_WAVES, 0, stream>>>(n, d, c, (const T*)X, ldx, (const T*)W, ldw, logp ? labels : nullptr, label_bits, parts, chosen);
             });
-            return;
+            return join(0, n, count);
         }
         if (is_small(n, d, c, type)) {
-            count = ((int64_t)c + 31) / 32;
+            const int64_t count = ((int64_t)c + 31) / 32;
             cbm_classes_small_kernel<T><<<dim3((unsigned)count, (unsigned)((n + 31) / 32)), 512, 0, stream>>>(n, d, c, (const T*)X, ldx, (const T*)W, ldw, logp ? labels : nullptr, label_bits, parts, chosen);
-            return;
+            return join(0, n, count);
         }
-        const Operands<T> o(n, d, c, type, X, ldx, W, ldw, (char*)chosen + rounded16(4 * n), stream);
-        with_tiles<T>(n, d, c, o, type, [&](auto* tiles_type, unsigned grid, int64_t chunks) {
-            typedef std::remove_pointer_t<decltype(tiles_type)> Tiles;
-            count = ((int64_t)c + Tiles::COLUMNS - 1) / Tiles::COLUMNS * Tiles::ACROSS;
-            cbm_classes_kernel<Tiles, T><<<grid, 256, 0, stream>>>(o.a, o.b, chunks, logp ? labels : nullptr, label_bits, parts, chosen);
-        });
+        const Operands<T> o(n, d, c, type, X, ldx, W, ldw, (char*)chosen + rounded16(4 * band), stream);
+        for (int64_t r0 = 0; r0 < n; r0 += band) {
+            const int64_t rows = std::min(band, n - r0);
+            with_tiles<T>(rows, d, c, o, type, [&](auto* tiles_type, unsigned grid, int64_t chunks) {
+                typedef std::remove_pointer_t<decltype(tiles_type)> Tiles;
+                cbm_classes_kernel<Tiles, T><<<grid, 256, 0, stream>>>(o.rows(r0, rows), o.b, chunks, logp ? (const char*)labels + r0 * (label_bits / 8) : nullptr, label_bits, parts, chosen);
+                join(r0, rows, ((int64_t)c + Tiles::COLUMNS - 1) / Tiles::COLUMNS * Tiles::ACROSS);
+            });
+        }
     });
-    auto join = [&](auto lanes) {
-        constexpr int ROWS = 256 / decltype(lanes)::value;
-        cbm_classes_join_kernel<decltype(lanes)::value><<<(unsigned)std::min<int64_t>((n + ROWS - 1) / ROWS, 1 << 20), 256, 0, stream>>>(n, c, count, labels, label_bits, parts, chosen, logp, stats);
-    };
-    // (us with 64 lanes a row / these: 2097152 x 128 with 128 x 40 857 / 325; 65536 x 64 with 64 x 1000 93 / 80)
-    if (count <= 8 && n >= 4096) join(std::integral_constant<int, 1>{});
-    else if (count <= 64 && n >= 4096) join(std::integral_constant<int, 8>{});
-    else join(std::integral_constant<int, 64>{});
     return cbm_launched("linear log probabilities launch");
 }
 

@@ -1,4 +1,4 @@
-"""Workspaces of the operators that are made of products hold what their copies write (host functions: no GPU needed)."""
+"""Workspaces of the operators that are made of products: they hold what their copies write, and what they hold is bounded (host functions: no GPU needed)."""
 import pytest
 import torch
 
@@ -31,3 +31,11 @@ def test_forward_passes_have_room_for_whole_groups_of_rows(n, k, m, dtype):
     assert cbm.cbm_gated_linear_workspace_bytes(n, k, m, dtype) >= 2 * _whole(n, 8) * wide + 2 * 2 * _whole(m, 32) * wide
     assert cbm.cbm_linear_log_probs_workspace_bytes(n, k, 2 * m, dtype) >= 2 * _whole(n, 8) * wide + 2 * _whole(2 * m, 8) * wide + 4 * n
     assert cbm.cbm_linear_log_probs_backward_workspace_bytes(n, k, 2 * m, dtype) >= 2 * _whole(n, 8) * wide + 2 * _whole(2 * m, 8) * wide + 2 * n * min(2 * m, 1024)
+
+
+@pytest.mark.parametrize("dtype,type_", [(torch.float32, 0), (torch.bfloat16, 1), (torch.float16, 2)])
+@pytest.mark.parametrize("n,d,c", [(2097152, 8, 131072), (65536, 8, 131072), (1 << 31, 8, 128), (300, 4, 1 << 24), (4096, 1024, 32000)])
+def test_parts_of_rows_are_bounded(n, d, c, dtype, type_):
+    """A maximum and a sum for 64 columns of a row (32 of up to 32 rows), 512 MiB at a time."""
+    copies = 0 if type_ == 0 else 2 * _whole(n, 8) * _whole(d, 8) + 2 * _whole(c, 8) * _whole(d, 8)
+    assert 0 < cbm.cbm_linear_log_probs_workspace_bytes(n, d, c, dtype) <= (512 << 20) + 4 * n + 32 + copies
