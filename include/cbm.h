@@ -418,6 +418,7 @@ cbm_status cbm_log_probs_backward(int64_t n, int32_t c, int32_t type, const void
  * Products of 16-bit types are exact, those of fp32 are made of three bf16 parts of each value (left out is at most 2^-24 of a term; parts below 2^-126 are taken for zero); sums
  * are fp32.  (Small products of fp32: in fp32 throughout.)  In fp32, a value that is not finite leaves no finite sum that it is part of, one from 2^127 on may leave none.
  * Workspaces hold copies of operands and shares of sums, or slopes in fp32, whatever the sizes ask for: a smaller call may need more than a larger one.
+ * Up to 2^31 rows; CBM_ERR_UNSUPPORTED (and a workspace of 0 bytes) where a product has 2^24 tiles of 128 x 128 values or more: n x 2 m forward, n x k and k x 2 m backward.
  */
 typedef enum { CBM_SILU = 0, CBM_GELU = 1, CBM_RELU = 2 } cbm_activation;
 cbm_status cbm_gated_linear(int64_t n, int32_t k, int32_t m, int32_t type, int32_t activation, const void* X, int64_t ldx, const void* Wg, int64_t ldwg,
@@ -443,6 +444,7 @@ size_t cbm_gated_linear_backward_workspace_bytes(int64_t n, int32_t k, int32_t m
  *   dX = dZ W^T (n x d),  dW = X^T dZ (d x c; zeros for n = 0), of `type`; either may be NULL.  Values of X must be finite in rows without a label, too.
  *   The scores are made again from X and W, a piece of the classes at a time, with m and l from `stats`.
  *   workspace    cbm_linear_log_probs_backward_workspace_bytes(n, d, c, type) bytes: dZ of a piece (512 MiB or 1,024 classes), and sums.
+ *                CBM_ERR_UNSUPPORTED (and 0 bytes) where a product, n x the classes of a piece, n x d or d x those, has 2^24 tiles of 128 x 128 values or more.
  */
 cbm_status cbm_linear_log_probs(int64_t n, int32_t d, int32_t c, int32_t type, const void* X, int64_t ldx, const void* W, int64_t ldw, const void* labels,
                                 int32_t label_bits, float* logp, float* stats, void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -445,11 +445,21 @@ cbm_status cbm_launch_classes(int64_t n, int32_t d, int32_t c, int32_t type, con
     return cbm_launched("linear log probabilities launch");
 }
 
-int64_t cbm_classes_back_workspace(int64_t n, int32_t d, int32_t c, int32_t type) { return back_room(n, d, c, type).bytes; }
+namespace {
+
+bool back_too_large(int64_t n, int32_t d, int32_t c, int32_t type) {
+    const int64_t piece = piece_of(n, c, type);
+    return cbm_too_many_tiles(n, piece) || cbm_too_many_tiles(n, cbm_whole(d, 8)) || cbm_too_many_tiles(cbm_whole(d, 8), piece);
+}
+
+}  // namespace
+
+int64_t cbm_classes_back_workspace(int64_t n, int32_t d, int32_t c, int32_t type) { return back_too_large(n, d, c, type) ? 0 : back_room(n, d, c, type).bytes; }
 
 cbm_status cbm_launch_classes_backward(int64_t n, int32_t d, int32_t c, int32_t type, const void* X, int64_t ldx, const void* W, int64_t ldw, const void* labels, int label_bits,
                                        const float* stats, const float* dlogp, void* dX, int64_t lddx, void* dW, int64_t lddw, void* workspace, void* stream_) {
     hipStream_t stream = (hipStream_t)stream_;
+    if (back_too_large(n, d, c, type)) return CBM_ERR_UNSUPPORTED;
     const Room room = back_room(n, d, c, type);
     if (room.small) {
         float* dZ = (float*)workspace;

@@ -195,11 +195,12 @@ Copies copies_of(int64_t n, int32_t k, int32_t m, int32_t type) {
 
 }  // namespace
 
-int64_t cbm_gated_workspace(int64_t n, int32_t k, int32_t m, int32_t type) { return copies_of(n, k, m, type).bytes; }
+int64_t cbm_gated_workspace(int64_t n, int32_t k, int32_t m, int32_t type) { return cbm_too_many_tiles(n, 2 * (int64_t)m) ? 0 : copies_of(n, k, m, type).bytes; }
 
 cbm_status cbm_launch_gated(int64_t n, int32_t k, int32_t m, int32_t type, int32_t act, const void* X, int64_t ldx, const void* Wg, int64_t ldwg, const void* Wu, int64_t ldwu, void* H,
                             int64_t ldh, void* G, int64_t ldg, void* U, int64_t ldu, void* workspace, void* stream) {
     if (n == 0) return CBM_OK;
+    if (cbm_too_many_tiles(n, 2 * (int64_t)m)) return CBM_ERR_UNSUPPORTED;
     const Copies copies = copies_of(n, k, m, type);
     cbm_with_type(type, [&](auto t) {
         using T = decltype(t);
@@ -291,11 +292,18 @@ BackRoom back_room(int64_t n, int32_t k, int32_t m, int32_t type) {
 
 }  // namespace
 
-int64_t cbm_gated_back_workspace(int64_t n, int32_t k, int32_t m, int32_t type) { return back_room(n, k, m, type).bytes; }
+namespace {
+
+bool back_too_large(int64_t n, int32_t k, int32_t m) { return cbm_too_many_tiles(n, k) || cbm_too_many_tiles(cbm_whole(k, 8), 2 * cbm_whole(m, 64)); }
+
+}  // namespace
+
+int64_t cbm_gated_back_workspace(int64_t n, int32_t k, int32_t m, int32_t type) { return back_too_large(n, k, m) ? 0 : back_room(n, k, m, type).bytes; }
 
 cbm_status cbm_launch_gated_backward(int64_t n, int32_t k, int32_t m, int32_t type, int32_t act, const void* dH, int64_t lddh, const void* X, int64_t ldx, const void* Wg, int64_t ldwg,
                                      const void* Wu, int64_t ldwu, const void* G, int64_t ldg, const void* U, int64_t ldu, void* dX, int64_t lddx, void* dWg, int64_t lddwg, void* dWu,
                                      int64_t lddwu, void* workspace, void* stream) {
+    if (back_too_large(n, k, m)) return CBM_ERR_UNSUPPORTED;
     const BackRoom room = back_room(n, k, m, type);
     const int64_t at = room.at;
     char* base = (char*)workspace;

@@ -30,6 +30,8 @@ struct CbmProduct {
     CbmProductOut out;
     float* parts;  // cbm_product_parts() M x N values, packed, where that is more than one
 };
+// A launch has fewer than 2^32 threads, 256 for each tile of 128 x 128 values or larger, in a grid of a multiple of eight.
+inline bool cbm_too_many_tiles(int64_t rows, int64_t columns) { return ((rows + 127) / 128 * ((columns + 127) / 128) + 7) / 8 * 8 >= (int64_t)1 << 24; }
 int64_t cbm_product_parts(int64_t M, int64_t N, int64_t K, int32_t type);
 // Large products of 16-bit values: matrices that do not lie in whole units of 16 bytes are copied so that they do, and a matrix whose rows of k many rows of the other meet is turned to lie along k; their
 // workspace has room for it.  (us as they lie / copied, forward and backward, odd strides: 100000 x 1001 with 2 x 1001 columns 777 / 675 and 1447 / 1326; 16384 x 333 with 2 x 500 38 / 47, 105 / 108;

@@ -1,8 +1,9 @@
-"""Workspaces of the operators that are made of products: they hold what their copies write, and what they hold is bounded (host functions: no GPU needed)."""
+"""Workspaces of the operators that are made of products: they hold what their copies write, and what they hold is bounded; sizes that no launch can have are refused (host functions: no GPU needed)."""
 import pytest
 import torch
 
 import paper_2409_02208_amd as cbm
+from paper_2409_02208_amd import binding
 
 WIDE = [torch.bfloat16, torch.float16]
 
@@ -39,3 +40,31 @@ def test_parts_of_rows_are_bounded(n, d, c, dtype, type_):
     """A maximum and a sum for 64 columns of a row (32 of up to 32 rows), 512 MiB at a time."""
     copies = 0 if type_ == 0 else 2 * _whole(n, 8) * _whole(d, 8) + 2 * _whole(c, 8) * _whole(d, 8)
     assert 0 < cbm.cbm_linear_log_probs_workspace_bytes(n, d, c, dtype) <= (512 << 20) + 4 * n + 32 + copies
+
+
+FAR = 1 << 48  # between operands that are only addresses here
+
+
+def _at(i):
+    return (i + 1) * FAR
+
+
+@pytest.mark.parametrize("type_", [0, 1, 2])
+@pytest.mark.parametrize("n,k,m", [(1 << 31, 1, 64), (1 << 30, 8, 128), (1 << 24, 4, 1 << 14)])
+def test_products_of_too_many_tiles_are_refused(n, k, m, type_):
+    """2^24 tiles of 256 threads are as many threads as no launch has: an error before anything is launched."""
+    lib = binding._lib()
+    assert lib.cbm_gated_linear_workspace_bytes(n, k, m, type_) == 0
+    assert lib.cbm_gated_linear(n, k, m, type_, 0, _at(0), k, _at(1), m, _at(2), m, _at(3), m, None, m, None, m, None, 0, None) == 5
+    # X's gradient has as many with the sides the other way round
+    assert lib.cbm_gated_linear_backward_workspace_bytes(n, 2 * m, k, type_) == 0
+    assert lib.cbm_gated_linear_backward(n, 2 * m, k, type_, 0, _at(0), k, _at(1), 2 * m, _at(2), k, _at(3), k, _at(4), k, _at(5), k, _at(6), 2 * m, None, k, None, k, None, 0, None) == 5
+
+
+@pytest.mark.parametrize("type_", [0, 1, 2])
+@pytest.mark.parametrize("n,d,c", [(1 << 31, 8, 8), (1 << 30, 256, 2), (1 << 28, 8, 1024)])
+def test_gradients_of_too_many_tiles_are_refused(n, d, c, type_):
+    lib = binding._lib()
+    assert lib.cbm_linear_log_probs_backward_workspace_bytes(n, d, c, type_) == 0
+    assert lib.cbm_linear_log_probs_backward(n, d, c, type_, _at(0), d, _at(1), c, _at(2), 64, _at(3), _at(4), _at(5), d, _at(6), c, None, 0, None) == 5
+    assert lib.cbm_linear_log_probs_backward_workspace_bytes(1 << 20, d, c, type_) > 0
