@@ -638,18 +638,10 @@ Room room_of(int64_t s, int64_t l) {
     return r;
 }
 
-// f(the tiles that take least): rounds of workgroups, each its products at what a compute unit's share reaches and what it takes beside them.  (4096 x 4096's Gram matrix is 136 tiles of 256 on and below the
-// diagonal, which take as long as 256 of them, and 253 of 192: 231 and 191 us.)
+// f(the tiles that take least)
 template <class F>
 void with_tiles(int64_t M, int64_t N, int64_t K, bool half, F&& f) {
-    double best = 1e30;
-    int side = 256;
-    for (int b : {256, 192, 128, 64, 32}) {
-        const int64_t m = (M + b - 1) / b, tiles = half ? m * (m + 1) / 2 : m * ((N + b - 1) / b), at_once = b == 128 ? 512 : 256;
-        const double each = 6.0 * b * b * (double)K / ((b == 256 ? 1250.0 : b == 192 ? 1150.0 : b == 128 ? 1050.0 : b == 64 ? 800.0 : 450.0) * 1e6 / (double)at_once) * (b == 128 && tiles <= 256 ? 0.6 : 1.0);
-        const double us = (double)((tiles + at_once - 1) / at_once) * (each + (b == 256 ? 12.0 : b == 192 ? 9.0 : b == 128 ? 5.0 : b == 64 ? 7.0 : 4.0));
-        if (us < best) best = us, side = b;
-    }
+    const int side = cbm_orthogonal_side(M, N, K, half);
     if (side == 256) f((HalvesTiles<256>*)nullptr);
     else if (side == 192) f((HalvesTiles<192>*)nullptr);
     else if (side == 128) f((HalvesTiles<128>*)nullptr);

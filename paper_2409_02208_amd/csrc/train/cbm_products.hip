@@ -158,34 +158,6 @@ __global__ __launch_bounds__(256) void cbm_pack_kernel(const uint16_t* __restric
     }
 }
 
-// Which tiles, and how many shares of K.
-struct Plan {
-    int tile;  // 256 and 128: units straight to LDS; 0: 128 x 128 of any matrices
-    int64_t splits;
-    double us;
-};
-// Microseconds as measured: a workgroup's rate, by how many of a tile run at once; what a workgroup takes beside its products (the first loads, the result); shares of K are written, read and joined in a launch
-// of its own.  Shares of at least 256 k.
-Plan plan(int64_t M, int64_t N, int64_t K, int32_t type, int tile) {
-    M = cbm_whole(M, 8), N = cbm_whole(N, 8), K = cbm_whole(K, 64);  // (a copy in whole units has the same plan)
-    const bool narrow = !tile && cbm_is_narrow(N, type);
-    const int64_t side = tile ? tile : 128, tiles = std::max<int64_t>(1, narrow ? (M + 255) / 256 : (M + side - 1) / side * ((N + side - 1) / side)), at_once = tile == 256 ? 256 : 512;
-    const double tflops = tile == 256 ? 1150.0 : tile == 128 ? 900.0 : type == CBM_F32 ? 140.0 : 550.0, beside = tile == 256 ? 9.0 : 5.0;
-    const double each = 2.0 * (double)(side * side * K) / (tflops * 1e6 / (double)at_once);
-    Plan best{tile, 1, 1e30};
-    for (int64_t s = 1; s <= 128 && (s == 1 || (s * 256 <= K && tiles <= 1024)); ++s) {
-        const double rounds = (double)((tiles * s + at_once - 1) / at_once);
-        const double us = rounds * (each / (double)s + beside) + (s > 1 ? 4.0 + 8.0 * (double)(s * M * N) / 4e6 : 0.0);
-        if (us < 0.97 * best.us) best = {tile, s, us};
-    }
-    return best;
-}
-Plan plan(int64_t M, int64_t N, int64_t K, int32_t type, bool units) {
-    if (!units) return plan(M, N, K, type, 0);
-    const Plan large = plan(M, N, K, type, 256), small = plan(M, N, K, type, 128);
-    return large.us < small.us ? large : small;
-}
-
 template <class T, CbmTileOrder OA, CbmTileOrder OB, CbmTilePair PAIR>
 void launch(const CbmProduct& p, hipStream_t stream) {
     const int64_t K = p.at ? p.at + p.K : p.K;
@@ -194,7 +166,7 @@ void launch(const CbmProduct& p, hipStream_t stream) {
     bool units = false;
     if constexpr (sizeof(T) == 2)
         units = cbm_units(a.p[0], a.ld[0], OA == ALONG_K ? K : p.M) && cbm_units(b.p[0], b.ld[0], OB == ALONG_K ? p.K : p.N) && (PAIR == SINGLE || (cbm_units(b.p[1], b.ld[1], p.K) && b.ld[1] == b.ld[0]));
-    const Plan how = plan(p.M, p.N, p.at ? 2 * p.at : K, p.type, units);
+    const CbmPlan how = cbm_plan(p.M, p.N, p.at ? 2 * p.at : K, p.type, units);
     const int64_t splits = p.parts ? how.splits : 1;
     CbmProductOut out = p.out;
     if (!out.rows) out.rows = p.M;
@@ -230,12 +202,6 @@ void launch(const CbmProduct& p, hipStream_t stream) {
 
 }  // namespace
 
-// The most that a product of the size is cut into, however its matrices lie.
-int64_t cbm_product_parts(int64_t M, int64_t N, int64_t K, int32_t type) {
-    const int64_t any = plan(M, N, K, type, false).splits;
-    return type == CBM_F32 ? any : std::max(any, plan(M, N, K, type, true).splits);
-}
-
 void cbm_launch_pack(const void* from, int64_t ld, int64_t rows, int64_t columns, bool turned, void* to, int64_t ldt, int64_t blocks, int64_t at, void* stream) {
     // (a grid is 65,535 high at most)
     for (int64_t r = 0; r < rows; r += 4194240) {  // (a multiple of 64)
@@ -243,11 +209,6 @@ void cbm_launch_pack(const void* from, int64_t ld, int64_t rows, int64_t columns
         cbm_pack_kernel<<<dim3((unsigned)((ldt + 63) / 64), (unsigned)((some + 63) / 64)), 256, 0, (hipStream_t)stream>>>((const uint16_t*)from + (turned ? r : r * ld), ld, some, columns, turned,
                                                                                                                 (uint16_t*)to + (blocks ? r / 32 * blocks : r) * ldt, ldt, blocks, at);
     }
-}
-
-int cbm_product_tile(int64_t M, int64_t N, int64_t K, int32_t type) {
-    const Plan large = plan(M, N, K, type, 256), small = plan(M, N, K, type, 128);
-    return large.us < small.us ? 256 : 128;
 }
 
 void cbm_launch_tiles(const CbmProduct& p, void* stream) {
