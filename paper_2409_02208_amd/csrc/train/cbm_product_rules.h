@@ -10,8 +10,8 @@
 inline bool cbm_too_many_tiles(int64_t rows, int64_t columns) { return ((rows + 127) / 128 * ((columns + 127) / 128) + 7) / 8 * 8 >= (int64_t)1 << 24; }
 // Large products of 16-bit values: matrices that do not lie in whole units of 16 bytes are copied so that they do, and a matrix whose rows of k many rows of the other meet is turned to lie along k; their
 // workspace has room for it.  (us as they lie / copied, forward and backward, odd strides: 100000 x 1001 with 2 x 1001 columns 777 / 675 and 1447 / 1326; 16384 x 333 with 2 x 500 38 / 47, 105 / 108;
-// 1024 x 1000 with 2 x 4000 37 / 48, 105 / 104.  Turned: 65536 x 1024 with 2 x 4096 1342 / 1218.)
-inline bool cbm_may_pack(int64_t rows, int64_t K, int64_t columns, int32_t type) { return type != CBM_F32 && rows >= 1024 && K >= 256 && 2e-11 * (double)rows * (double)K * (double)columns >= 1.0; }
+// 1024 x 1000 with 2 x 4000 37 / 48, 105 / 104.  Turned: 65536 x 1024 with 2 x 4096 1342 / 1218.)  A copy's row is shorter than 2^22 values, as that of any matrix whose units go straight to LDS (cbm_units).
+inline bool cbm_may_pack(int64_t rows, int64_t K, int64_t columns, int32_t type) { return type != CBM_F32 && rows >= 1024 && K >= 256 && K <= (1 << 22) - 8 && 2e-11 * (double)rows * (double)K * (double)columns >= 1.0; }
 constexpr int64_t CBM_TURN_ROWS = 4096;  // from so many rows on turning pays
 inline int64_t cbm_whole(int64_t v, int64_t of) { return (v + of - 1) / of * of; }
 // fp32 with so few columns: tiles of 256 x 64, which waste half as much as those of 128 x 128.

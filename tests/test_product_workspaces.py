@@ -42,6 +42,14 @@ def test_parts_of_rows_are_bounded(n, d, c, dtype, type_):
     assert 0 < cbm.cbm_linear_log_probs_workspace_bytes(n, d, c, dtype) <= (512 << 20) + 4 * n + 32 + copies
 
 
+@pytest.mark.parametrize("dtype", WIDE)
+@pytest.mark.parametrize("n,k,m", [(1024, (1 << 23) + 35 * 2048, 128), (1025, 1 << 24, 1000), (1024, 1 << 22, 512), (4096, (1 << 22) - 7, 64)])
+def test_rows_of_four_million_values_and_more_are_not_copied(n, k, m, dtype):
+    """Tiles that read whole units reach their rows by 32 bits from the first: 256 rows of 2^23 values are beyond them."""
+    assert cbm.cbm_gated_linear_workspace_bytes(n, k, m, dtype) == 0
+    assert cbm.cbm_linear_log_probs_workspace_bytes(n, k, 2 * m, dtype) <= 8 * n * _whole(2 * m, 128) + 4 * n + 32
+
+
 FAR = 1 << 48  # between operands that are only addresses here
 
 
