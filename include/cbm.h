@@ -463,7 +463,8 @@ size_t cbm_linear_log_probs_backward_workspace_bytes(int64_t n, int32_t d, int32
  *   eps            >= 0 and finite; a matrix of zeros stays one with eps > 0, and is NaN with eps = 0.
  *   Y              may be X itself with ldy = ldx.
  *   workspace      cbm_orthogonalise_workspace_bytes(m, n, type) bytes.
- * m and n up to 65,536.  Between X and Y values are held in two parts of 16 bits each, 22 bits together, at powers of two that follow from the coefficients; sums are fp32.  Coefficients are refused
+ * m and n up to 65,536.  Between X and Y values are held in two parts of 16 bits each, 22 bits together, at powers of two that follow from the coefficients; sums are fp32.  (A value of Z is held to 2^-38 at
+ * best: where eps is far above |X|, so that Z is small, it and Y keep as many bits fewer as its values are below 2^-16.)  Coefficients are refused
  * (CBM_ERR_UNSUPPORTED) where, on what the steps before may make of [0, 1], |a + b s^2 + c s^4| passes 16 |a| or 2^100, or s passes 2^24.  A value that is not finite makes NaN of all of Y.
  */
 cbm_status cbm_orthogonalise(int32_t m, int32_t n, int32_t type, const void* X, int64_t ldx, int32_t steps, const float* coefficients, float eps, float scale,
